@@ -446,6 +446,85 @@ int deer_moe_mlp(const void* x, const void* w_router, const void* w_gate_up, con
                  void* y, int M, int hid, int E, int I, int top_k, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * (7) The verifier layer in 8 bits: the weight stream and the KV stream, which
+ * bound the step (Section 3.2's parallel pass reads both once per block), at half
+ * their bytes.  A value is held as an e4m3 code c and an fp32 scale s that a group
+ * of values shares: value = c * s with
+ *     s = max(amax / 448, 2^-126) over the group,  c = e4m3(value / s),
+ * both divisions in fp32, rounded to nearest.  A NaN or an infinity makes its own
+ * group's scale NaN or infinite (its values read back as NaN) and touches no other.
+ * Groups: 128 consecutive columns of a row (the last may be shorter); 128 x 128
+ * blocks of a weight (rows x columns, edge blocks smaller); one page of 16 tokens
+ * of one KV head.
+ *
+ * deer_rmsnorm_quant: h = x + residual (residual may be NULL: h = x);
+ *   codes, scales of y = h / sqrt(mean(h^2) + eps) * gamma;  total = h in bf16.
+ *   x, residual, total bf16 [M][hid]; gamma bf16 [hid]; codes e4m3 [M][hid]; scales f32 [M][ceil(hid / 128)].
+ *   total may be NULL; it may be x or residual itself.  fp32 throughout: y is taken from the unrounded h and
+ *   rounded once, to its code.  hid a multiple of 16, at most 65536.
+ * deer_quantize: codes, scales of x bf16 [M][K] (gated = 0), or of silu(x[m][c]) * x[m][K + c], x bf16 [M][2 K]
+ *   (gated = 1).  K a multiple of 16.
+ * deer_linear_quant: y[m][n] = sum_c x[m][c] w[n][c] (+ residual[m][n]) of the values that codes and scales stand for.
+ *   x e4m3 [M][K], x_scale f32 [M][ceil(K / 128)]; w e4m3 [N][K], w_scale f32 [ceil(N / 128)][ceil(K / 128)];
+ *   residual, y bf16 [M][N] (residual may be NULL or y itself).  K and N multiples of 16, at least 16.
+ *   Products and the sums over 128 columns come from the tensor cores' fp32 accumulator; the scaled sums over the
+ *   column groups are fp32.  No workspace.
+ * ---------------------------------------------------------------------- */
+int deer_rmsnorm_quant(const void* x, const void* residual, const void* gamma, void* total, void* codes, float* scales,
+                       int M, int hid, float eps, void* stream);
+int deer_quantize(const void* x, int gated, void* codes, float* scales, int M, int K, void* stream);
+int deer_linear_quant(const void* x, const float* x_scale, const void* w, const float* w_scale, const void* residual, void* y,
+                      int M, int K, int N, void* stream);
+
+/* A paged cache in 8 bits.  The integer state of deer_kv_desc is the same (one page table may serve bf16 and 8-bit
+ * caches of different layers); k_pool / v_pool are e4m3 [num_pages][Hkv][16][D], and each page and head has one scale:
+ *   k_scale, v_scale  f32  [num_pages][Hkv]
+ *   k_tail, v_tail    bf16 [max_seqs][Hkv][48][D]   the tokens behind the last full page: token t in row t mod 48
+ * A token is quantised once, from bf16, when its page is full; until then it is a tail row.  So a scale never depends
+ * on a draft that was rejected, and nothing is ever quantised twice.  deer_kv_reserve, deer_kv_commit,
+ * deer_accept_commit, deer_kv_status and the rotary calls take such a handle as any other; deer_block_attn,
+ * deer_block_attn_rows and deer_verify_step_host refuse it (DEER_ERR_UNSUPPORTED). */
+typedef struct deer_kv_quant_desc {
+    float* k_scale;
+    float* v_scale;
+    void*  k_tail;
+    void*  v_tail;
+} deer_kv_quant_desc;
+
+#define DEER_TAIL_ROWS 48
+
+/* `desc` and `quant` are host pointers; their contents are copied. */
+int deer_kv_create_quant(deer_kv** kv, const deer_kv_desc* desc, const deer_kv_quant_desc* quant);
+
+/* The rows that a step keeps enter an 8-bit cache: rows 0 .. keep[b] - 1 of k_rows / v_rows bf16 [B][k][Hkv][D] become
+ * the tokens seq_len[s] .. of sequence s = seq_ids[b] (keep clamped to [0, k]; NULL keeps all k).  Pages that become
+ * full are quantised, the tokens behind them become tail rows.  seq_len is NOT changed: call deer_kv_commit (or
+ * deer_kv_commit_rows) with the same keep afterwards, once for all layers that share the integer state.  The pages
+ * must be mapped (deer_kv_reserve).  k is not limited to a draft block: a prompt enters with one call.  seq_ids
+ * distinct.  Repeating a call before the commit gives the same cache again if k <= 32, or if seq_len is a multiple
+ * of 16 (a longer run that starts inside a page may end on tail rows that it read).
+ * Errors: the status word as deer_kv_commit (DEER_ERR_BAD_PAGE: a page that becomes full is not mapped; it is skipped). */
+int deer_kv_store(deer_kv* kv, const int32_t* seq_ids, const void* k_rows, const void* v_rows, const int32_t* keep, int B, int k,
+                  void* stream);
+
+/* deer_kv_reserve and deer_kv_commit for a run of any number of rows (k up to 2^24), for prompts. */
+int deer_kv_reserve_rows(deer_kv* kv, const int32_t* seq_ids, int B, int k, void* stream);
+int deer_kv_commit_rows(deer_kv* kv, const int32_t* seq_ids, const int32_t* keep, int B, int k, void* stream);
+
+/* Block attention (as deer_block_attn_rows, without the append) against an 8-bit cache: the keys are the tokens of the
+ * full pages (codes times their page's scale), the tail rows, and the block rows that mask and row_state allow.
+ * row_state: bidirectional mask only, or NULL; the output rows of absent positions are zero.  Scores and probabilities:
+ * fp32; queries enter exactly (to 2^-18 of a row's largest magnitude); probabilities enter the second product rounded to
+ * 11 bits.  A NaN or an infinity in a value row reaches only the rows that see it.
+ *   workspace  >= deer_block_attn_quant_workspace_bytes(...) bytes, 16-byte aligned, contents arbitrary; one call at a
+ *              time per workspace. */
+size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, int Hkv, int D, int max_seq_len);
+int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
+                          const void* q, const void* k_blk, const void* v_blk, void* out, const int32_t* row_state,
+                          int B, int k, int Hq, int mask, float scale, int max_seq_len,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * One whole greedy verify step with HOST inputs and outputs (Algorithm 1, one
  * iteration of the while loop on the verifier side): copies the block's
  * q/k_blk/v_blk, hidden states and draft ids from host memory to the device

@@ -557,3 +557,133 @@ def moe_mlp(x, w_router, w_gate_up, w_down, top_k, renormalise=True):
             act = swiglu(gu[:inter], gu[inter:])
             y[m] += wts[m, j] * linear(act[None, :], w_down[e])[0]
     return y
+
+
+# --------------------------------------------------------------------------
+# (7) the 8-bit verifier layer -- e4m3 codes with one scale per group of
+#     values (128 columns of a row, 128 x 128 of a weight, one page of one head)
+# --------------------------------------------------------------------------
+
+E4M3_MAX = 448.0
+SCALE_MIN = 2.0 ** -126
+GROUP = 128
+
+
+def e4m3_step(v):
+    """Distance between neighbouring e4m3 values at |v| (three bits behind the leading one, none below 2^-9)."""
+    a = np.maximum(np.abs(np.asarray(v, dtype=np.float64)), 2.0 ** -6)
+    return 2.0 ** (np.floor(np.log2(a)) - 3.0)
+
+
+def e4m3_round(v):
+    """Nearest e4m3 value, halves to the even code, beyond 448 saturated; NaN stays NaN."""
+    v = np.asarray(v, dtype=np.float64)
+    step = e4m3_step(np.where(np.isfinite(v), v, 0.0))
+    return np.clip(np.round(v / step) * step, -E4M3_MAX, E4M3_MAX)
+
+
+def quant_scale(amax):
+    """fp32 scale of a group whose largest magnitude is ``amax``."""
+    return np.maximum(np.float32(amax) / np.float32(E4M3_MAX), np.float32(SCALE_MIN))
+
+
+def quantise(v, scale):
+    """Codes (as the values of e4m3) of ``v`` under ``scale``; the quotient is the fp32 one."""
+    q = (np.asarray(v, dtype=np.float32) / np.asarray(scale, dtype=np.float32)).astype(np.float64)
+    return e4m3_round(q)
+
+
+def quantise_rows(y):
+    """y [M, K] -> codes [M, K], scales [M, ceil(K / 128)]."""
+    M, K = y.shape
+    G = -(-K // GROUP)
+    codes, scales = np.zeros((M, K)), np.zeros((M, G), dtype=np.float32)
+    for g in range(G):
+        part = y[:, g * GROUP:(g + 1) * GROUP]
+        scales[:, g] = quant_scale(np.abs(part).max(axis=1))
+        codes[:, g * GROUP:(g + 1) * GROUP] = quantise(part, scales[:, g:g + 1])
+    return codes, scales
+
+
+def dequantise_rows(codes, scales):
+    return codes * np.repeat(scales.astype(np.float64), GROUP, axis=1)[:, :codes.shape[1]]
+
+
+def quantise_weight(w):
+    """w [N, K] -> codes [N, K], scales [ceil(N / 128), ceil(K / 128)], one per 128 x 128 block."""
+    N, K = w.shape
+    scales = np.zeros((-(-N // GROUP), -(-K // GROUP)), dtype=np.float32)
+    codes = np.zeros((N, K))
+    for i in range(scales.shape[0]):
+        for j in range(scales.shape[1]):
+            at = np.s_[i * GROUP:(i + 1) * GROUP, j * GROUP:(j + 1) * GROUP]
+            scales[i, j] = quant_scale(np.abs(w[at]).max())
+            codes[at] = quantise(w[at], scales[i, j])
+    return codes, scales
+
+
+def dequantise_weight(codes, scales):
+    N, K = codes.shape
+    return codes * np.repeat(np.repeat(scales.astype(np.float64), GROUP, axis=0)[:N], GROUP, axis=1)[:, :K]
+
+
+class QuantKV:
+    """An 8-bit paged cache: full pages as codes with one scale per page and head, the tokens behind the last full page
+    as they came (token t in tail row t mod 48).  Integer state as PagedKV."""
+
+    TAIL = 48
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, page_table, seq_len, page_size=16):
+        self.codes = [np.array(k_codes, dtype=np.float64), np.array(v_codes, dtype=np.float64)]
+        self.scale = [np.array(k_scale, dtype=np.float32), np.array(v_scale, dtype=np.float32)]
+        self.tail = [np.array(k_tail, dtype=np.float64), np.array(v_tail, dtype=np.float64)]
+        self.page_table, self.seq_len, self.page = np.array(page_table), np.array(seq_len), page_size
+
+    def store(self, seq_ids, k_rows, v_rows, keep):
+        """Rows 0 .. keep[b] - 1 become tokens seq_len .. of sequence seq_ids[b]; seq_len stays."""
+        for b, s in enumerate(np.asarray(seq_ids)):
+            n, kp = int(self.seq_len[s]), int(keep[b])
+            for x, rows in ((0, k_rows), (1, v_rows)):
+                first = n // self.page * self.page
+                old = [self.tail[x][s, :, t % self.TAIL].copy() for t in range(first, n)]
+                toks = old + [np.asarray(rows[b, j], dtype=np.float64) for j in range(kp)]      # [Hkv, D] each, from token `first`
+                n_full = (n + kp) // self.page - first // self.page
+                for i in range(n_full):
+                    whole = np.stack(toks[i * self.page:(i + 1) * self.page], axis=1)           # [Hkv, 16, D]
+                    pg = int(self.page_table[s, first // self.page + i])
+                    for h in range(whole.shape[0]):
+                        sc = quant_scale(np.abs(whole[h]).max())
+                        self.scale[x][pg, h] = sc
+                        self.codes[x][pg, h] = quantise(whole[h], sc)
+                for j, v in enumerate(toks):
+                    t = first + j
+                    if t >= n and t >= (n + kp) // self.page * self.page:
+                        self.tail[x][s, :, t % self.TAIL] = v
+
+    def gather(self, s):
+        """Committed tokens of sequence s as dense [n, Hkv, D] keys and values."""
+        n = int(self.seq_len[s])
+        out = []
+        for x in (0, 1):
+            rows = []
+            for t in range(n):
+                if t < n // self.page * self.page:
+                    pg = int(self.page_table[s, t // self.page])
+                    rows.append(self.codes[x][pg, :, t % self.page] * self.scale[x][pg].astype(np.float64)[:, None])
+                else:
+                    rows.append(self.tail[x][s, :, t % self.TAIL])
+            out.append(np.stack(rows) if rows else np.zeros((0,) + self.codes[x].shape[1:2] + self.codes[x].shape[3:]))
+        return out
+
+
+def quant_block_attention(q, k_blk, v_blk, qkv, seq_ids, mask, scale, row_state=None):
+    """block_attention against a QuantKV: every sequence's tokens are gathered dense, then the same definition."""
+    outs = []
+    for b, s in enumerate(np.asarray(seq_ids)):
+        kd, vd = qkv.gather(s)
+        n = kd.shape[0]
+        pool = lambda d: d.transpose(1, 0, 2)[None]                       # one page that holds all n tokens
+        outs.append(block_attention(q[b:b + 1], k_blk[b:b + 1], v_blk[b:b + 1], pool(kd), pool(vd), np.zeros((1, 1), dtype=np.int64),
+                                    np.array([n]), [0], mask, scale, page_size=max(n, 1),
+                                    row_state=None if row_state is None else row_state[b:b + 1]))
+    return np.concatenate(outs)

@@ -32,6 +32,8 @@ EXPORTS = [
     "deer_truncate", "deer_accept_truncated", "deer_block_attn_rows", "deer_refill", "deer_refresh_rows",
     "deer_moe_workspace_bytes", "deer_moe_route", "deer_moe_mlp",
     "deer_layer_workspace_bytes", "deer_linear_qkv_rope", "deer_linear_residual_norm", "deer_linear_swiglu",
+    "deer_rmsnorm_quant", "deer_quantize", "deer_linear_quant", "deer_kv_create_quant", "deer_kv_store",
+    "deer_kv_reserve_rows", "deer_kv_commit_rows", "deer_block_attn_quant_workspace_bytes", "deer_block_attn_quant",
 ]
 
 
@@ -46,6 +48,10 @@ class deer_kv_desc(Structure):
                 ("n_pages", c_void_p), ("free_stack", c_void_p), ("free_top", c_void_p), ("status", c_void_p),
                 ("num_pages", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("page_size", c_int32),
                 ("max_seqs", c_int32), ("max_pages", c_int32)]
+
+
+class deer_kv_quant_desc(Structure):
+    _fields_ = [("k_scale", c_void_p), ("v_scale", c_void_p), ("k_tail", c_void_p), ("v_tail", c_void_p)]
 
 
 class deer_step_dev(Structure):
@@ -130,6 +136,17 @@ def lib() -> ctypes.CDLL:
     L.deer_verify_step_host.argtypes = [c_void_p, POINTER(deer_step_dev), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                         c_void_p, c_int, c_int, c_int, c_int, c_int, c_float, c_int, c_void_p, c_void_p,
                                         c_void_p, c_void_p]
+    L.deer_rmsnorm_quant.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_float, c_void_p]
+    L.deer_quantize.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p]
+    L.deer_linear_quant.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p]
+    L.deer_kv_create_quant.argtypes = [POINTER(c_void_p), POINTER(deer_kv_desc), POINTER(deer_kv_quant_desc)]
+    L.deer_kv_store.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p]
+    L.deer_kv_reserve_rows.argtypes = [c_void_p, c_void_p, c_int, c_int, c_void_p]
+    L.deer_kv_commit_rows.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p]
+    L.deer_block_attn_quant_workspace_bytes.restype = c_size_t
+    L.deer_block_attn_quant_workspace_bytes.argtypes = [c_int] * 6
+    L.deer_block_attn_quant.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
+                                        c_int, c_float, c_int, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
         getattr(L, name)          # every declared entry point must be exported
     _lib = L
@@ -160,6 +177,10 @@ class KVCache:
     """Device tensors of one paged cache plus the library handle over them."""
 
     def __init__(self, k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top):
+        self._describe(k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top)
+        _check(lib().deer_kv_create(ctypes.byref(self.handle), ctypes.byref(self.desc)))
+
+    def _describe(self, k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top):
         self.k_pool, self.v_pool = k_pool, v_pool
         self.page_table, self.seq_len, self.n_pages = page_table, seq_len, n_pages
         self.free_stack, self.free_top = free_stack, free_top
@@ -169,7 +190,6 @@ class KVCache:
                                  _ptr(free_stack), _ptr(free_top), _ptr(self.status),
                                  num_pages, Hkv, D, page, page_table.shape[0], page_table.shape[1])
         self.handle = c_void_p()
-        _check(lib().deer_kv_create(ctypes.byref(self.handle), ctypes.byref(self.desc)))
 
     @classmethod
     def from_layout(cls, layout, k_pool, v_pool, device="cuda"):
@@ -196,6 +216,84 @@ class KVCache:
             self.close()
         except Exception:
             pass
+
+
+DEER_TAIL_ROWS = 48
+
+
+class KVCacheQuant(KVCache):
+    """A paged cache in 8 bits: pools of ``torch.float8_e4m3fn`` with one fp32 scale per page and head, and the bf16
+    tail rows of the tokens behind each sequence's last full page."""
+
+    def __init__(self, k_pool, v_pool, k_scale, v_scale, k_tail, v_tail, page_table, seq_len, n_pages, free_stack, free_top):
+        num_pages, Hkv, _, D = k_pool.shape
+        assert k_pool.dtype == v_pool.dtype == torch.float8_e4m3fn and v_pool.shape == k_pool.shape
+        assert k_scale.shape == v_scale.shape == (num_pages, Hkv) and k_scale.dtype == v_scale.dtype == torch.float32
+        assert k_tail.shape == v_tail.shape == (page_table.shape[0], Hkv, DEER_TAIL_ROWS, D)
+        assert k_tail.dtype == v_tail.dtype == torch.bfloat16
+        self._describe(k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top)
+        self.k_scale, self.v_scale, self.k_tail, self.v_tail = k_scale, v_scale, k_tail, v_tail
+        quant = deer_kv_quant_desc(_ptr(k_scale), _ptr(v_scale), _ptr(k_tail), _ptr(v_tail))
+        _check(lib().deer_kv_create_quant(ctypes.byref(self.handle), ctypes.byref(self.desc), ctypes.byref(quant)))
+
+    @classmethod
+    def empty(cls, num_pages, n_kv_heads, head_dim, max_seqs, max_pages, device="cuda"):
+        """A cache without tokens, every page on the free stack."""
+        z = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype, device=device)
+        pool = lambda: z(num_pages, n_kv_heads, 16, head_dim, dtype=torch.float8_e4m3fn)
+        scale = lambda: z(num_pages, n_kv_heads, dtype=torch.float32)
+        tail = lambda: z(max_seqs, n_kv_heads, DEER_TAIL_ROWS, head_dim, dtype=torch.bfloat16)
+        return cls(pool(), pool(), scale(), scale(), tail(), tail(), torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                   z(max_seqs), z(max_seqs), torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                   torch.full((1,), num_pages, dtype=torch.int32, device=device))
+
+    def layer(self):
+        """Another layer's cache over the same page table, lengths and free stack, with pools of its own."""
+        same = lambda t: torch.zeros_like(t)
+        return KVCacheQuant(same(self.k_pool), same(self.v_pool), same(self.k_scale), same(self.v_scale), same(self.k_tail),
+                            same(self.v_tail), self.page_table, self.seq_len, self.n_pages, self.free_stack, self.free_top)
+
+
+def deer_kv_store(kv: KVCacheQuant, seq_ids, k_rows, v_rows, keep=None, stream=None) -> None:
+    B, k = k_rows.shape[:2]
+    _check(lib().deer_kv_store(kv.handle, _ptr(seq_ids), _ptr(k_rows), _ptr(v_rows), _ptr(keep), B, k, _stream(stream)))
+
+
+def deer_kv_reserve_rows(kv: KVCache, seq_ids: torch.Tensor, k: int, stream=None) -> None:
+    _check(lib().deer_kv_reserve_rows(kv.handle, _ptr(seq_ids), seq_ids.numel(), k, _stream(stream)))
+
+
+def deer_kv_commit_rows(kv: KVCache, seq_ids: torch.Tensor, keep: torch.Tensor, k: int, stream=None) -> None:
+    _check(lib().deer_kv_commit_rows(kv.handle, _ptr(seq_ids), _ptr(keep), seq_ids.numel(), k, _stream(stream)))
+
+
+def deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, max_seq_len) -> int:
+    return lib().deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, max_seq_len)
+
+
+def deer_block_attn_quant(kv: KVCacheQuant, seq_ids, q, k_blk, v_blk, out, row_state, mask, scale, max_seq_len, workspace, stream=None):
+    B, k, Hq, D = q.shape
+    _check(lib().deer_block_attn_quant(kv.handle, _ptr(seq_ids), _ptr(q), _ptr(k_blk), _ptr(v_blk), _ptr(out), _ptr(row_state), B, k, Hq,
+                                       int(mask), float(scale), int(max_seq_len), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                       _stream(stream)))
+
+
+def deer_rmsnorm_quant(x, gamma, codes, scales, eps, residual=None, total=None, stream=None):
+    M, hid = x.shape
+    _check(lib().deer_rmsnorm_quant(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(total), _ptr(codes), _ptr(scales), M, hid, float(eps),
+                                    _stream(stream)))
+
+
+def deer_quantize(x, codes, scales, gated=False, stream=None):
+    M, K = codes.shape
+    _check(lib().deer_quantize(_ptr(x), 1 if gated else 0, _ptr(codes), _ptr(scales), M, K, _stream(stream)))
+
+
+def deer_linear_quant(x, x_scale, w, w_scale, y, residual=None, stream=None):
+    M, K = x.shape
+    _check(lib().deer_linear_quant(_ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(residual), _ptr(y), M, K, w.shape[0],
+                                   _stream(stream)))
 
 
 def deer_kv_reserve(kv: KVCache, seq_ids: torch.Tensor, k: int, stream=None) -> None:

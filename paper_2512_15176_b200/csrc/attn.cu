@@ -365,6 +365,7 @@ extern "C" int deer_block_attn_rows(deer_kv* kv, const int32_t* seq_ids, const v
                                     void* out, const int32_t* row_state, int B, int k, int Hq, int mask, int append, float scale,
                                     int max_seq_len, void* workspace, size_t workspace_bytes, void* stream) {
     DEER_CHECK_ARG(kv && seq_ids && q && k_blk && v_blk && out, DEER_ERR_INVALID_ARG, "deer_block_attn: null argument");
+    DEER_CHECK_ARG(!kv->quant, DEER_ERR_UNSUPPORTED, "deer_block_attn: the cache holds 8-bit pools (deer_block_attn_quant reads them)");
     DEER_CHECK_ARG(!row_state || mask == DEER_MASK_BIDIR, DEER_ERR_INVALID_ARG,
                    "deer_block_attn_rows: row states belong to the bidirectional mask");
     DEER_CHECK_ARG(deer_aligned16(q) && deer_aligned16(k_blk) && deer_aligned16(v_blk) && deer_aligned16(out) &&

@@ -1,0 +1,502 @@
+// Block attention against an 8-bit paged cache (Section 3.2's parallel pass with the KV stream at half its bytes).
+//
+// The keys of a sequence with n committed tokens: floor(n / 16) full pages of e4m3 codes with one scale per page and
+// head, n mod 16 tail rows in bf16, and the block's own k rows in bf16.
+//
+// Warp-level kernel.  A page of one KV head is 16 tokens: exactly one contraction step of the second product and two
+// column tiles of the first.  A warp takes whole pages: each lane brings 16-byte pieces of K and V straight into
+// registers -- the pieces are laid out so that they ARE the operand fragments (the contraction index of q . k and the
+// column index of p v may be permuted freely, as long as the other side is permuted alike), so no byte passes through
+// shared memory -- and the codes become fp16 exactly.  The page's K scale multiplies the 16 scores; its V scale
+// multiplies the page's product before it joins the fp32 sums, so scales of any size work.  Queries are brought to
+// fp16 by a power of two per row (exact to 2^-24 of the row's largest), probabilities are at most 2^12 and keep fp16's
+// 11 bits down to 2^-26 of the row's maximum.  The warps of a block take pages in turn with running maxima of their
+// own, and meet in shared memory at the end; a context is cut into chunks over thread blocks, which a second kernel
+// joins.
+
+#include <cuda_fp16.h>
+
+#include "attn_quant.cuh"
+
+namespace attnq {
+
+constexpr int ROWS = 16;                       // query rows of a tile
+constexpr int WARPS = 4;
+constexpr float P_BIAS = 12.f;                 // probabilities are held as 2^12 p
+
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two e4m3 codes (the low or the high half of w) as fp16, exactly.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
+    uint32_t r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l;}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+    uint32_t r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, h;}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+
+// Lane (g8, t4) = (lane / 4, lane % 4).  Contraction step (hc, w) of q . k: this lane's four contraction indices are
+// the dims hc * 64 + t4 * 16 + w * 4 + 0..3.  Column tile j of p v: column g8 is dim g8 * (D / 8) + j, so that this
+// lane's accumulators are the dims t4 * (D / 4) + 0 .. D / 4 - 1 of rows g8 and g8 + 8.
+template <int D>
+__global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) {
+    constexpr int HC = D / 64;                 // 16-byte pieces of a key row per lane
+    constexpr int ND = D / 8;                  // column tiles of the output
+    constexpr int VW = D / 32;                 // 32-bit words of a value row per lane (16-byte or 8-byte piece)
+    __shared__ float s_o[WARPS][ROWS][D];
+    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
+    const int Hkv = p.kv.n_kv_heads;
+    const int c = blockIdx.x, kvh = blockIdx.y / p.row_tiles, rt = blockIdx.y % p.row_tiles, b = blockIdx.z;
+    pdl_trigger();
+    pdl_wait();
+    int s, n;
+    if (!sequence_of(p, b, &s, &n, c == 0 && blockIdx.y == 0 && tid == 0)) return;
+    const int n_chunks = chunks_of(p, n);
+    if (c >= n_chunks) return;
+    const int R = p.G * p.k;
+    const int page_lo = c * p.chunk_pages, page_hi = min(n / PAGE, page_lo + p.chunk_pages);
+    const int n_tail = n % PAGE;
+    const int32_t* pt_row = p.kv.page_table + (size_t)s * p.kv.max_pages;
+
+    uint32_t present, decoded;
+    attn::row_state_sets(p.row_state, b, p.k, lane, &present, &decoded);
+
+    // ---- this lane's two query rows ----
+    int row[2], blk_row[2];
+    const __nv_bfloat16* q_row[2];
+    uint32_t cols[2];                                          // block rows that the row sees
+    bool live[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        row[u] = rt * ROWS + g8 + u * 8;
+        const int rr = min(row[u], R - 1);
+        blk_row[u] = rr / p.G;
+        const int st = p.row_state ? p.row_state[(size_t)b * p.k + blk_row[u]] : 1;
+        live[u] = row[u] < R && st >= 0;
+        cols[u] = attn::visible_rows(p.mask, blk_row[u], st, present, decoded);
+        q_row[u] = p.q + ((size_t)(b * p.k + blk_row[u]) * p.Hq + kvh * p.G + rr % p.G) * D;
+    }
+    uint32_t qf[HC * 4][4];
+    float f_row[2];                                            // scale * log2(e) * the power of two taken out of the row
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        float qv[HC][16];
+        uint32_t m = 0;
+#pragma unroll
+        for (int hc = 0; hc < HC; ++hc) {
+            quant::load_bf16x16(q_row[u] + hc * 64 + t4 * 16, qv[hc]);
+            m = max(m, quant::amax16(qv[hc]));
+        }
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        // 2^-e with 2^e <= max < 2^(e+1); a row with a NaN or an infinity stays as it is (and gives NaN)
+        int e = (int)(m >> 23) - 127;
+        if (e == 128) e = 0;
+        const float down = __uint_as_float((uint32_t)max(127 - e, 1) << 23);
+        f_row[u] = p.scale_log2 / down;
+#pragma unroll
+        for (int hc = 0; hc < HC; ++hc)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                qf[hc * 4 + w][u] = pack_f16(qv[hc][w * 4] * down, qv[hc][w * 4 + 1] * down);
+                qf[hc * 4 + w][2 + u] = pack_f16(qv[hc][w * 4 + 2] * down, qv[hc][w * 4 + 3] * down);
+            }
+    }
+
+    float o[ND][4];
+#pragma unroll
+    for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};     // l: this lane's columns only, until the end
+
+    // Scores of 16 keys (two column tiles) in the log2 domain -> probabilities; raises the running maximum.
+    auto softmax16 = [&](float (&sc)[2][4]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float mx = quad_max(fmaxf(fmaxf(sc[0][2 * u], sc[0][2 * u + 1]), fmaxf(sc[1][2 * u], sc[1][2 * u + 1])));
+            const float mn = fmaxf(m_run[u], mx);
+            if (__any_sync(0xffffffffu, mn > m_run[u])) {
+                const float corr = mn == -INFINITY ? 1.f : exp2f(m_run[u] - mn);
+                l_run[u] *= corr;
+#pragma unroll
+                for (int j = 0; j < ND; ++j) {
+                    o[j][2 * u] *= corr;
+                    o[j][2 * u + 1] *= corr;
+                }
+                m_run[u] = mn;
+            }
+            const float base = (mn == -INFINITY ? 0.f : mn) - P_BIAS;
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float pr = exp2f(sc[t][2 * u + e] - base);
+                    sc[t][2 * u + e] = pr;
+                    sum += pr;
+                }
+            l_run[u] += sum;
+        }
+    };
+
+    // ---- full pages: this warp takes every WARPS-th page of the chunk ----
+    struct Page {
+        uint4 k[2][HC];                        // keys g8, g8 + 8 of the page
+        uint32_t v[4][VW];                     // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
+        float ks, vs;
+    };
+    auto load_page = [&](int page, Page& x) {
+        int pg = page < p.kv.max_pages ? pt_row[page] : -1;
+        if (pg < 0 || pg >= p.kv.num_pages) {
+            if (lane == 0) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
+            pg = 0;                                            // inside the pool; the status word flags the result
+        }
+        const size_t slab = (size_t)pg * Hkv + kvh;
+        const uint8_t* kp = static_cast<const uint8_t*>(p.kv.k_pool) + slab * PAGE * D;
+        const uint8_t* vp = static_cast<const uint8_t*>(p.kv.v_pool) + slab * PAGE * D;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int hc = 0; hc < HC; ++hc) x.k[t][hc] = __ldcg(reinterpret_cast<const uint4*>(kp + (t * 8 + g8) * D + hc * 64 + t4 * 16));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint8_t* src = vp + (2 * t4 + (e & 1) + (e >> 1) * 8) * D + g8 * (D / 8);
+            if (D == 128) {
+                const uint4 w = __ldcg(reinterpret_cast<const uint4*>(src));
+                x.v[e][0] = w.x; x.v[e][1] = w.y; x.v[e][VW - 2] = w.z; x.v[e][VW - 1] = w.w;
+            } else {
+                const uint2 w = __ldcg(reinterpret_cast<const uint2*>(src));
+                x.v[e][0] = w.x; x.v[e][1] = w.y;
+            }
+        }
+        x.ks = __ldcg(p.kq.k_scale + slab);
+        x.vs = __ldcg(p.kq.v_scale + slab);
+    };
+    Page nx;
+    if (page_lo + warp < page_hi) load_page(page_lo + warp, nx);
+    for (int page = page_lo + warp; page < page_hi; page += WARPS) {
+        const Page x = nx;
+        if (page + WARPS < page_hi) load_page(page + WARPS, nx);
+        float sc[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+#pragma unroll
+            for (int hc = 0; hc < HC; ++hc) {
+                const uint32_t w[4] = {x.k[t][hc].x, x.k[t][hc].y, x.k[t][hc].z, x.k[t][hc].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16_16816(sc[t], qf[hc * 4 + i], codes_lo(w[i]), codes_hi(w[i]));
+            }
+            const float f0 = f_row[0] * x.ks, f1 = f_row[1] * x.ks;
+            sc[t][0] *= f0; sc[t][1] *= f0; sc[t][2] *= f1; sc[t][3] *= f1;
+        }
+        softmax16(sc);
+        const uint32_t pa[4] = {pack_f16(sc[0][0], sc[0][1]), pack_f16(sc[0][2], sc[0][3]), pack_f16(sc[1][0], sc[1][1]), pack_f16(sc[1][2], sc[1][3])};
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {      // dims 4 w + 2 h, + 1: the codes of two tokens side by side
+                const uint32_t a = __byte_perm(x.v[0][w], x.v[1][w], h ? 0x7362 : 0x5140);
+                const uint32_t d = __byte_perm(x.v[2][w], x.v[3][w], h ? 0x7362 : 0x5140);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float r[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma_f16_16816(r, pa, e ? codes_hi(a) : codes_lo(a), e ? codes_hi(d) : codes_lo(d));
+                    const int j = w * 4 + h * 2 + e;
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[j][z] = fmaf(r[z], x.vs, o[j][z]);
+                }
+            }
+        }
+    }
+
+    // ---- what is bf16: the tail rows and the block's own, 16 at a time, with the chunk that is last ----
+    if (c == n_chunks - 1) {
+        const int n_blk = (p.k + PAGE - 1) / PAGE;
+        for (int it = (n_tail ? 0 : 1) + warp; it <= n_blk; it += WARPS) {         // 0: the tail, 1 ..: block rows
+            const bool is_tail = it == 0;
+            const int j0 = (it - 1) * PAGE;                                        // first block row
+            const int valid = is_tail ? n_tail : min(PAGE, p.k - j0);
+            const size_t stride = is_tail ? D : (size_t)Hkv * D;
+            const size_t off = is_tail ? (((size_t)s * Hkv + kvh) * DEER_TAIL_ROWS + (n / PAGE % 3) * PAGE) * D
+                                       : ((size_t)(b * p.k + j0) * Hkv + kvh) * D;
+            const __nv_bfloat16* kr = (is_tail ? static_cast<const __nv_bfloat16*>(p.kq.k_tail) : p.k_blk) + off;
+            const __nv_bfloat16* vr = (is_tail ? static_cast<const __nv_bfloat16*>(p.kq.v_tail) : p.v_blk) + off;
+            // rows that hold something, and those that each of my two query rows sees, as bits of this group of 16
+            const uint32_t has = is_tail ? (1u << valid) - 1u : (present >> j0) & ((1u << valid) - 1u);
+            const uint32_t see[2] = {is_tail ? has : (cols[0] >> j0) & has, is_tail ? has : (cols[1] >> j0) & has};
+            float sc[2][4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+                const int tok = t * 8 + g8;
+                const bool on = (has >> tok) & 1u;
+#pragma unroll
+                for (int hc = 0; hc < HC; ++hc)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const int d0 = hc * 64 + t4 * 16 + z * 8;                  // two contraction steps of four dims each
+                        const uint4 kv = on ? *reinterpret_cast<const uint4*>(kr + (size_t)tok * stride + d0) : make_uint4(0, 0, 0, 0);
+                        const uint4 qa = *reinterpret_cast<const uint4*>(q_row[0] + d0), qb = *reinterpret_cast<const uint4*>(q_row[1] + d0);
+                        const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
+                        mma_bf16_16816(sc[t], a0, kv.x, kv.y);
+                        mma_bf16_16816(sc[t], a1, kv.z, kv.w);
+                    }
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                    sc[t][z] = (see[z >> 1] >> (t * 8 + t4 * 2 + (z & 1))) & 1u ? sc[t][z] * p.scale_log2 : -INFINITY;
+            }
+            softmax16(sc);
+            // values: a NaN or an infinity must reach only the rows that see it, so such a group of rows goes element by element
+            uint4 vv[4][D / 64];               // D / 8 bf16 of four tokens
+            uint32_t worst = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int tok = 2 * t4 + (e & 1) + (e >> 1) * 8;
+                const bool on = (has >> tok) & 1u;
+#pragma unroll
+                for (int z = 0; z < D / 64; ++z) {
+                    vv[e][z] = on ? *reinterpret_cast<const uint4*>(vr + (size_t)tok * stride + g8 * (D / 8) + z * 8) : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {vv[e][z].x, vv[e][z].y, vv[e][z].z, vv[e][z].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) worst = max(worst, max(w[y] & 0x7fffu, (w[y] >> 16) & 0x7fffu));
+                }
+            }
+            if (!__any_sync(0xffffffffu, worst >= 0x7f80u)) {
+                // bf16 probabilities would lose three bits against the pages' fp16: two terms carry 16
+                uint32_t pa[4], pb[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const float x0 = sc[z >> 1][(z & 1) * 2], x1 = sc[z >> 1][(z & 1) * 2 + 1];
+                    pa[z] = pack_bf16(x0, x1);
+                    pb[z] = pack_bf16(x0 - __uint_as_float(pa[z] << 16), x1 - __uint_as_float(pa[z] & 0xffff0000u));
+                }
+#pragma unroll
+                for (int z = 0; z < D / 64; ++z) {
+                    const uint32_t w0[4] = {vv[0][z].x, vv[0][z].y, vv[0][z].z, vv[0][z].w}, w1[4] = {vv[1][z].x, vv[1][z].y, vv[1][z].z, vv[1][z].w};
+                    const uint32_t w2[4] = {vv[2][z].x, vv[2][z].y, vv[2][z].z, vv[2][z].w}, w3[4] = {vv[3][z].x, vv[3][z].y, vv[3][z].z, vv[3][z].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t b0 = __byte_perm(w0[y], w1[y], e ? 0x7632 : 0x5410), b1 = __byte_perm(w2[y], w3[y], e ? 0x7632 : 0x5410);
+                            mma_bf16_16816(o[z * 8 + y * 2 + e], pa, b0, b1);
+                            mma_bf16_16816(o[z * 8 + y * 2 + e], pb, b0, b1);
+                        }
+                }
+            } else {
+                for (int tok = 0; tok < valid; ++tok) {
+                    const int src = (g8 << 2) | ((tok & 7) >> 1);
+                    float pr[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const float x0 = __shfl_sync(0xffffffffu, sc[0][2 * u], src), x1 = __shfl_sync(0xffffffffu, sc[0][2 * u + 1], src);
+                        const float x2 = __shfl_sync(0xffffffffu, sc[1][2 * u], src), x3 = __shfl_sync(0xffffffffu, sc[1][2 * u + 1], src);
+                        pr[u] = tok < 8 ? ((tok & 1) ? x1 : x0) : ((tok & 1) ? x3 : x2);
+                    }
+                    const __nv_bfloat16* v = vr + (size_t)tok * stride + t4 * (D / 4);
+#pragma unroll
+                    for (int j = 0; j < ND; ++j) {
+                        const float v0 = __bfloat162float(v[j]), v1 = __bfloat162float(v[ND + j]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            if ((see[u] >> tok) & 1u) {
+                                o[j][2 * u] = fmaf(pr[u], v0, o[j][2 * u]);
+                                o[j][2 * u + 1] = fmaf(pr[u], v1, o[j][2 * u + 1]);
+                            }
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- the warps meet ----
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const float l = quad_sum(l_run[u]);
+        if (t4 == 0) {
+            s_m[warp][g8 + u * 8] = m_run[u];
+            s_l[warp][g8 + u * 8] = live[u] ? l : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+            s_o[warp][g8 + u * 8][t4 * (D / 4) + j] = o[j][2 * u];
+            s_o[warp][g8 + u * 8][t4 * (D / 4) + ND + j] = o[j][2 * u + 1];
+        }
+    }
+    __syncthreads();
+    // 8 threads per row, D / 8 dims each
+    const int r = tid >> 3, d0 = (tid & 7) * (D / 8), rr = rt * ROWS + r;
+    if (rr >= R) return;
+    const int i = rr / p.G;
+    const bool absent = p.row_state && p.row_state[(size_t)b * p.k + i] < 0;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, s_m[w][r]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float l = 0.f, wt[WARPS];
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        wt[w] = s_m[w][r] == -INFINITY ? 0.f : exp2f(s_m[w][r] - base);
+        if (s_l[w][r] != s_l[w][r]) wt[w] = 1.f;               // a NaN passes on, whatever the maxima are
+        l += wt[w] * s_l[w][r];
+    }
+    const float inv = (absent || l == 0.f) ? 0.f : 1.f / l;
+    float acc[D / 8];
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) {
+        acc[d] = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) acc[d] = wt[w] != 0.f ? fmaf(wt[w], s_o[w][r][d0 + d], acc[d]) : acc[d];
+        acc[d] = absent ? 0.f : acc[d] * inv;
+    }
+    const size_t orow = (size_t)(b * p.k + i) * p.Hq + kvh * p.G + rr % p.G;
+    if (n_chunks == 1) {
+        __nv_bfloat16* dst = p.out + orow * D + d0;
+#pragma unroll
+        for (int d = 0; d < D / 8; d += 8)
+            *reinterpret_cast<uint4*>(dst + d) = make_uint4(pack_bf16(acc[d], acc[d + 1]), pack_bf16(acc[d + 2], acc[d + 3]),
+                                                            pack_bf16(acc[d + 4], acc[d + 5]), pack_bf16(acc[d + 6], acc[d + 7]));
+    } else {
+        const size_t slot = (size_t)c * p.B * p.k * p.Hq + orow;
+        float* dst = p.part_o + slot * D + d0;
+#pragma unroll
+        for (int d = 0; d < D / 8; d += 4) *reinterpret_cast<float4*>(dst + d) = make_float4(acc[d], acc[d + 1], acc[d + 2], acc[d + 3]);
+        if ((tid & 7) == 0) p.part_lse[slot] = (absent || l == 0.f) ? -INFINITY : mx + log2f(l);
+    }
+}
+
+// One warp per output row: joins the chunks' partial results.
+template <int D>
+__global__ void __launch_bounds__(256) attn_quant_merge_kernel(const Params p) {
+    constexpr int PER = D / 32;
+    const int lane = threadIdx.x & 31;
+    const size_t n_rows = (size_t)p.B * p.k * p.Hq;
+    const size_t orow = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_trigger();
+    pdl_wait();
+    if (orow >= n_rows) return;
+    int s, n;
+    if (!sequence_of(p, (int)(orow / ((size_t)p.k * p.Hq)), &s, &n, false)) return;
+    const int n_chunks = chunks_of(p, n);
+    if (n_chunks == 1) return;                                 // written by its only chunk
+    float mx = -INFINITY;
+    for (int c = lane; c < n_chunks; c += 32) mx = fmaxf(mx, p.part_lse[(size_t)c * n_rows + orow]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float acc[PER], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = 0.f;
+    for (int c = 0; c < n_chunks; ++c) {
+        const float lse = p.part_lse[(size_t)c * n_rows + orow];
+        const float w = lse == -INFINITY ? 0.f : exp2f(lse - base);
+        const float* src = p.part_o + ((size_t)c * n_rows + orow) * D + lane * PER;
+        sum += w;
+        if (w != 0.f) {                                        // a NaN joins
+#pragma unroll
+            for (int e = 0; e < PER; ++e) acc[e] = fmaf(w, src[e], acc[e]);
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    __nv_bfloat16* dst = p.out + orow * D + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; e += 2) *reinterpret_cast<__nv_bfloat162*>(dst + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+}
+
+struct Plan {
+    int row_tiles, chunk_pages, chunks;
+};
+// The context is cut so that about four blocks per SM share the work, in chunks of two pages per warp at least.
+static Plan plan(int B, int k, int Hq, int Hkv, int max_seq_len) {
+    Plan pl;
+    pl.row_tiles = (Hq / Hkv * k + ROWS - 1) / ROWS;
+    const long long units = (long long)B * Hkv * pl.row_tiles, pages = max_seq_len / PAGE;
+    const long long want = (4LL * deer_sm_count() + units - 1) / units;
+    long long per = (pages + want - 1) / want;
+    if (per < 2 * WARPS) per = 2 * WARPS;
+    per = (per + WARPS - 1) / WARPS * WARPS;
+    pl.chunk_pages = (int)per;
+    pl.chunks = pages > per ? (int)((pages + per - 1) / per) : 1;
+    return pl;
+}
+
+}  // namespace attnq
+
+using namespace attnq;
+
+extern "C" size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, int Hkv, int D, int max_seq_len) {
+    if (B <= 0 || k <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || D <= 0 || max_seq_len < 0) return 0;
+    const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
+    return pl.chunks == 1 ? 16 : (size_t)pl.chunks * B * k * Hq * (D + 1) * sizeof(float);
+}
+
+extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const void* q, const void* k_blk, const void* v_blk, void* out,
+                                     const int32_t* row_state, int B, int k, int Hq, int mask, float scale, int max_seq_len,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    DEER_CHECK_ARG(kv && seq_ids && q && k_blk && v_blk && out, DEER_ERR_INVALID_ARG, "deer_block_attn_quant: null argument");
+    DEER_CHECK_ARG(kv->quant, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: the cache holds bf16 pools (deer_block_attn reads them)");
+    DEER_CHECK_ARG(!row_state || mask == DEER_MASK_BIDIR, DEER_ERR_INVALID_ARG,
+                   "deer_block_attn_quant: row states belong to the bidirectional mask");
+    DEER_CHECK_ARG(deer_aligned16(q) && deer_aligned16(k_blk) && deer_aligned16(v_blk) && deer_aligned16(out) && deer_aligned16(workspace),
+                   DEER_ERR_INVALID_ARG, "deer_block_attn_quant: pointers must be 16-byte aligned");
+    DEER_CHECK_ARG(k >= 1 && k <= DEER_MAX_BLOCK, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: k must be in [1, 32]");
+    DEER_CHECK_ARG(B >= 0 && B <= 65535, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: B must be in [0, 65535]");
+    const int Hkv = kv->d.n_kv_heads, D = kv->d.head_dim;
+    DEER_CHECK_ARG(Hq > 0 && Hq % Hkv == 0, DEER_ERR_INVALID_ARG, "deer_block_attn_quant: Hq must be a positive multiple of Hkv");
+    DEER_CHECK_ARG(mask == DEER_MASK_CAUSAL || mask == DEER_MASK_BIDIR, DEER_ERR_INVALID_ARG, "deer_block_attn_quant: bad mask");
+    DEER_CHECK_ARG(max_seq_len >= 0, DEER_ERR_INVALID_ARG, "deer_block_attn_quant: max_seq_len must be >= 0");
+    if (B == 0) return DEER_OK;
+    const size_t need = deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, max_seq_len);
+    DEER_CHECK_ARG(workspace && workspace_bytes >= need, DEER_ERR_WORKSPACE,
+                   "deer_block_attn_quant: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+    const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
+    DEER_CHECK_ARG((long long)Hkv * pl.row_tiles <= 65535, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: too many heads");
+    Params p = {};
+    p.kv = kv->d;
+    p.kq = kv->q;
+    p.seq_ids = seq_ids;
+    p.row_state = row_state;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k_blk = static_cast<const __nv_bfloat16*>(k_blk);
+    p.v_blk = static_cast<const __nv_bfloat16*>(v_blk);
+    p.out = static_cast<__nv_bfloat16*>(out);
+    const size_t n_rows = (size_t)B * k * Hq;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = p.part_o + (size_t)pl.chunks * n_rows * D;
+    p.B = B;
+    p.k = k;
+    p.Hq = Hq;
+    p.G = Hq / Hkv;
+    p.mask = mask;
+    p.max_seq_len = max_seq_len;
+    p.scale_log2 = scale * LOG2E;
+    p.row_tiles = pl.row_tiles;
+    p.chunk_pages = pl.chunk_pages;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const dim3 grid((unsigned)pl.chunks, (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
+    DEER_CUDA(launch_pdl(D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
+    if (pl.chunks > 1)
+        DEER_CUDA(launch_pdl(D == 128 ? attn_quant_merge_kernel<128> : attn_quant_merge_kernel<64>, dim3((unsigned)((n_rows + 7) / 8)), dim3(256), 0, st, p));
+    return DEER_OK;
+}

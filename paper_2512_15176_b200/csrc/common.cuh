@@ -10,6 +10,8 @@
 
 struct deer_kv {
     deer_kv_desc d;
+    bool quant;                // 8-bit pools with scales and tail rows (deer_kv_create_quant): q is set
+    deer_kv_quant_desc q;
 };
 
 // ---- host-side error text (per thread) -------------------------------------
@@ -33,6 +35,7 @@ void deer_set_error(const char* fmt, ...);
     } while (0)
 
 static inline bool deer_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static inline bool deer_aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Streaming multiprocessors of the current device (asked once per device).  Grids and workspaces are sized by it.
 // Where no device can be asked (a host without a GPU sizing a workspace) it is a B200's 148.

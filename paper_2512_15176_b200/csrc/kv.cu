@@ -42,7 +42,23 @@ extern "C" int deer_kv_create(deer_kv** kv, const deer_kv_desc* desc) {
     deer_kv* h = new (std::nothrow) deer_kv;
     DEER_CHECK_ARG(h, DEER_ERR_INVALID_ARG, "deer_kv_create: out of host memory");
     h->d = d;
+    h->quant = false;
+    h->q = deer_kv_quant_desc{};
     *kv = h;
+    return DEER_OK;
+}
+
+extern "C" int deer_kv_create_quant(deer_kv** kv, const deer_kv_desc* desc, const deer_kv_quant_desc* quant) {
+    DEER_CHECK_ARG(kv && desc && quant, DEER_ERR_INVALID_ARG, "deer_kv_create_quant: null argument");
+    DEER_CHECK_ARG(quant->k_scale && quant->v_scale && quant->k_tail && quant->v_tail, DEER_ERR_INVALID_ARG,
+                   "deer_kv_create_quant: null device pointer in quant");
+    DEER_CHECK_ARG(deer_aligned16(quant->k_tail) && deer_aligned16(quant->v_tail) &&
+                       (reinterpret_cast<uintptr_t>(quant->k_scale) & 3u) == 0 && (reinterpret_cast<uintptr_t>(quant->v_scale) & 3u) == 0,
+                   DEER_ERR_INVALID_ARG, "deer_kv_create_quant: tails must be 16-byte aligned, scales 4-byte aligned");
+    const int rc = deer_kv_create(kv, desc);
+    if (rc != DEER_OK) return rc;
+    (*kv)->quant = true;
+    (*kv)->q = *quant;
     return DEER_OK;
 }
 
@@ -62,6 +78,7 @@ extern "C" int deer_kv_status(deer_kv* kv, int32_t* code, void* stream) {
 
 // ---- kernels ---------------------------------------------------------------
 constexpr int KV_THREADS = 1024;
+constexpr int KV_MAX_ROWS = 1 << 24;       // of one reserve / commit: 1024 sequences of them stay far inside 32 bits of pages
 
 // Exclusive scan of one int per thread over the block; returns the exclusive
 // prefix, *total gets the block sum.
@@ -215,8 +232,14 @@ kv_accept_commit_kernel(deer_kv_desc d, const int32_t* __restrict__ seq_ids, int
 // ---- entry points ----------------------------------------------------------
 extern "C" int deer_kv_reserve(deer_kv* kv, const int32_t* seq_ids, int B, int k, void* stream) {
     DEER_CHECK_ARG(kv && seq_ids, DEER_ERR_INVALID_ARG, "deer_kv_reserve: null argument");
-    DEER_CHECK_ARG(B >= 0 && B <= KV_THREADS, DEER_ERR_UNSUPPORTED, "deer_kv_reserve: B must be in [0, %d]", KV_THREADS);
     DEER_CHECK_ARG(k >= 0 && k <= DEER_MAX_BLOCK, DEER_ERR_UNSUPPORTED, "deer_kv_reserve: k must be in [0, 32]");
+    return deer_kv_reserve_rows(kv, seq_ids, B, k, stream);
+}
+
+extern "C" int deer_kv_reserve_rows(deer_kv* kv, const int32_t* seq_ids, int B, int k, void* stream) {
+    DEER_CHECK_ARG(kv && seq_ids, DEER_ERR_INVALID_ARG, "deer_kv_reserve: null argument");
+    DEER_CHECK_ARG(B >= 0 && B <= KV_THREADS, DEER_ERR_UNSUPPORTED, "deer_kv_reserve: B must be in [0, %d]", KV_THREADS);
+    DEER_CHECK_ARG(k >= 0 && k <= KV_MAX_ROWS, DEER_ERR_UNSUPPORTED, "deer_kv_reserve_rows: k must be in [0, 2^24]");
     if (B == 0) return DEER_OK;
     DEER_CUDA(launch_pdl(kv_reserve_kernel, dim3(1), dim3(KV_THREADS), 0, static_cast<cudaStream_t>(stream), kv->d, seq_ids, B, k));
     return DEER_OK;
@@ -224,8 +247,14 @@ extern "C" int deer_kv_reserve(deer_kv* kv, const int32_t* seq_ids, int B, int k
 
 extern "C" int deer_kv_commit(deer_kv* kv, const int32_t* seq_ids, const int32_t* keep, int B, int k, void* stream) {
     DEER_CHECK_ARG(kv && seq_ids && keep, DEER_ERR_INVALID_ARG, "deer_kv_commit: null argument");
-    DEER_CHECK_ARG(B >= 0 && B <= KV_THREADS, DEER_ERR_UNSUPPORTED, "deer_kv_commit: B must be in [0, %d]", KV_THREADS);
     DEER_CHECK_ARG(k >= 0 && k <= DEER_MAX_BLOCK, DEER_ERR_UNSUPPORTED, "deer_kv_commit: k must be in [0, 32]");
+    return deer_kv_commit_rows(kv, seq_ids, keep, B, k, stream);
+}
+
+extern "C" int deer_kv_commit_rows(deer_kv* kv, const int32_t* seq_ids, const int32_t* keep, int B, int k, void* stream) {
+    DEER_CHECK_ARG(kv && seq_ids && keep, DEER_ERR_INVALID_ARG, "deer_kv_commit: null argument");
+    DEER_CHECK_ARG(B >= 0 && B <= KV_THREADS, DEER_ERR_UNSUPPORTED, "deer_kv_commit: B must be in [0, %d]", KV_THREADS);
+    DEER_CHECK_ARG(k >= 0 && k <= KV_MAX_ROWS, DEER_ERR_UNSUPPORTED, "deer_kv_commit_rows: k must be in [0, 2^24]");
     if (B == 0) return DEER_OK;
     DEER_CUDA(launch_pdl(kv_commit_kernel, dim3(1), dim3(KV_THREADS), 0, static_cast<cudaStream_t>(stream), kv->d, seq_ids, keep, B, k));
     return DEER_OK;

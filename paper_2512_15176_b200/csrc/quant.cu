@@ -1,0 +1,235 @@
+// The row-wise quantisers of the 8-bit verifier layer -- residual + RMSNorm, a plain copy, the SiLU gate, each with
+// e4m3 codes and one scale per 128 columns as output -- and the store of a step's kept rows into an 8-bit paged cache.
+// All are one pass over their data: the bytes bound them when there are many rows, a launch and two dependent memory
+// round trips when there are few.
+
+#include "quant.cuh"
+
+namespace quant {
+
+// y = (x + residual) / rms * gamma per row.  A thread keeps its 16 columns (per chunk of 16 * THREADS) in registers
+// between the two phases -- the sum of squares over the row, the codes of the eight-lane groups -- so a row is read once.
+template <int THREADS, int CHUNKS>
+__global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloat16* x, const __nv_bfloat16* residual,
+                                                                const __nv_bfloat16* __restrict__ gamma, __nv_bfloat16* total,
+                                                                uint8_t* __restrict__ codes, float* __restrict__ scales, int hid, float eps) {
+    __shared__ float part[THREADS / 32];
+    const size_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int groups = (hid + GROUP - 1) / GROUP;
+    pdl_trigger();
+    pdl_wait();
+    float h[CHUNKS][16];
+    float ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int col = (c * THREADS + tid) * 16;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) h[c][j] = 0.f;
+        if (col < hid) {
+            load_bf16x16(x + row * hid + col, h[c]);
+            if (residual) {
+                float r[16];
+                load_bf16x16(residual + row * hid + col, r);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) h[c][j] += r[j];
+            }
+            if (total) {
+                uint32_t t[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t[j] = pack_bf16(h[c][2 * j], h[c][2 * j + 1]);
+                *reinterpret_cast<uint4*>(total + row * hid + col) = make_uint4(t[0], t[1], t[2], t[3]);
+                *reinterpret_cast<uint4*>(total + row * hid + col + 8) = make_uint4(t[4], t[5], t[6], t[7]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) ss += h[c][j] * h[c][j];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    if (lane == 0) part[warp] = ss;
+    __syncthreads();
+    float tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) tot += part[w];
+    const float inv = rsqrtf(tot / (float)hid + eps);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int col = (c * THREADS + tid) * 16;
+        if (c * THREADS * 16 >= hid) break;
+        if (col < hid) {
+            float g[16];
+            load_bf16x16(gamma + col, g);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) h[c][j] = h[c][j] * inv * g[j];
+        }
+        const float s = scale_of(max8(amax16(h[c])));
+        if (col < hid) {
+            *reinterpret_cast<uint4*>(codes + row * hid + col) = codes16(h[c], s);
+            if ((lane & 7) == 0) scales[row * groups + col / GROUP] = s;
+        }
+    }
+}
+
+// Eight lanes per group of 128 columns, groups of all rows laid end to end.
+template <bool GATED>
+__global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __restrict__ x, uint8_t* __restrict__ codes,
+                                                       float* __restrict__ scales, int M, int K) {
+    const int groups = (K + GROUP - 1) / GROUP;
+    const size_t item = (size_t)blockIdx.x * 32 + (threadIdx.x >> 3);          // group index over all rows
+    const size_t row = item / groups;
+    const int g = (int)(item % groups);
+    const int col = g * GROUP + (threadIdx.x & 7) * 16;
+    pdl_trigger();
+    pdl_wait();
+    const bool on = row < (size_t)M && col < K;
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+    if (on) {
+        const __nv_bfloat16* src = x + row * (size_t)(GATED ? 2 * (size_t)K : K) + col;
+        load_bf16x16(src, v);
+        if (GATED) {
+            float u[16];
+            load_bf16x16(src + K, u);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = v[j] / (1.f + __expf(-v[j])) * u[j];
+        }
+    }
+    const float s = scale_of(max8(amax16(v)));
+    if (on) {
+        *reinterpret_cast<uint4*>(codes + row * K + col) = codes16(v, s);
+        if ((threadIdx.x & 7) == 0) scales[row * groups + g] = s;
+    }
+}
+
+// ---- the store into an 8-bit paged cache -----------------------------------------------------------------------
+// One thread block per (page that the new rows can touch, KV head, sequence), its first half for K, its second for V;
+// a thread holds 16 dims of one token.  Index 0 is the page that seq_len stands in; it alone reads tail rows, and it
+// also writes the new ones -- after its own are in registers -- because the page behind the last full one may share
+// their places (page mod 3).
+template <int D>
+__global__ void __launch_bounds__(2 * D) kv_store_kernel(deer_kv_desc kv, deer_kv_quant_desc q, const int32_t* __restrict__ seq_ids,
+                                                         const __nv_bfloat16* __restrict__ k_rows, const __nv_bfloat16* __restrict__ v_rows,
+                                                         const int32_t* __restrict__ keep, int k) {
+    constexpr int PER_ROW = D / 16;                       // threads of a token
+    __shared__ uint32_t part[2 * D / 32];
+    const int tid = threadIdx.x;
+    const bool is_v = tid >= D;
+    const int t16 = (tid % D) / PER_ROW, col = (tid % PER_ROW) * 16;
+    const int h = blockIdx.y, b = blockIdx.z, Hkv = kv.n_kv_heads;
+    pdl_trigger();
+    pdl_wait();
+    const int s = seq_ids[b];
+    if (s < 0 || s >= kv.max_seqs) {
+        if (tid == 0) deer_report(kv.status, DEER_ERR_INVALID_ARG);
+        return;
+    }
+    const int n = kv.seq_len[s];
+    if (n < 0 || n / DEER_PAGE_SIZE > kv.max_pages) {
+        if (tid == 0) deer_report(kv.status, DEER_ERR_INVALID_ARG);
+        return;
+    }
+    const int kp = keep ? min(max(keep[b], 0), k) : k;
+    const int end = n + kp;
+    const int page = n / DEER_PAGE_SIZE + (int)blockIdx.x;
+    const bool full = (page + 1) * DEER_PAGE_SIZE <= end;
+    if (kp == 0 || (!full && blockIdx.x != 0)) return;
+    const __nv_bfloat16* rows = (is_v ? v_rows : k_rows) + (size_t)b * k * Hkv * D;
+    __nv_bfloat16* tail = static_cast<__nv_bfloat16*>(is_v ? q.v_tail : q.k_tail) + ((size_t)s * Hkv + h) * DEER_TAIL_ROWS * D;
+    const int t = page * DEER_PAGE_SIZE + t16;            // this thread's token
+    if (full) {
+        float v[16];
+        load_bf16x16(t < n ? tail + (size_t)(t % DEER_TAIL_ROWS) * D + col : rows + ((size_t)(t - n) * Hkv + h) * D + col, v);
+        uint32_t m = amax16(v);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if ((tid & 31) == 0) part[tid >> 5] = m;
+        __syncthreads();                                  // (also: the tail rows of this page are in registers)
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) m = max(m, part[(is_v ? D / 32 : 0) + w]);
+        const float sc = scale_of(m);
+        const int pg = page < kv.max_pages ? kv.page_table[(size_t)s * kv.max_pages + page] : -1;
+        if (pg < 0 || pg >= kv.num_pages) {
+            if (tid == 0) deer_report(kv.status, DEER_ERR_BAD_PAGE);
+        } else {
+            const size_t slab = (size_t)pg * Hkv + h;
+            uint8_t* pool = static_cast<uint8_t*>(is_v ? kv.v_pool : kv.k_pool) + (slab * DEER_PAGE_SIZE + t16) * D + col;
+            *reinterpret_cast<uint4*>(pool) = codes16(v, sc);
+            if (tid % D == 0) (is_v ? q.v_scale : q.k_scale)[slab] = sc;
+        }
+    }
+    if (blockIdx.x == 0) {                                // the rows behind the last full page
+        const int tt = end / DEER_PAGE_SIZE * DEER_PAGE_SIZE + t16;
+        if (tt >= n && tt < end) {
+            const uint4* src = reinterpret_cast<const uint4*>(rows + ((size_t)(tt - n) * Hkv + h) * D + col);
+            uint4* dst = reinterpret_cast<uint4*>(tail + (size_t)(tt % DEER_TAIL_ROWS) * D + col);
+            dst[0] = src[0];
+            dst[1] = src[1];
+        }
+    }
+}
+
+}  // namespace quant
+
+using namespace quant;
+
+extern "C" int deer_rmsnorm_quant(const void* x, const void* residual, const void* gamma, void* total, void* codes, float* scales,
+                                  int M, int hid, float eps, void* stream) {
+    DEER_CHECK_ARG(x && gamma && codes && scales, DEER_ERR_INVALID_ARG, "deer_rmsnorm_quant: null argument");
+    DEER_CHECK_ARG(deer_aligned16(x) && deer_aligned16(residual) && deer_aligned16(gamma) && deer_aligned16(total) && deer_aligned16(codes) &&
+                       deer_aligned4(scales),
+                   DEER_ERR_INVALID_ARG, "deer_rmsnorm_quant: pointers must be 16-byte aligned (scales: 4)");
+    DEER_CHECK_ARG(M >= 0, DEER_ERR_INVALID_ARG, "deer_rmsnorm_quant: M must be >= 0");
+    DEER_CHECK_ARG(hid >= 16 && hid % 16 == 0 && hid <= 65536, DEER_ERR_UNSUPPORTED,
+                   "deer_rmsnorm_quant: hid must be a multiple of 16 in [16, 65536]");
+    if (M == 0) return DEER_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto run = [&](auto kernel, int threads) {
+        return launch_pdl(kernel, dim3((unsigned)M), dim3((unsigned)threads), 0, st, static_cast<const __nv_bfloat16*>(x),
+                          static_cast<const __nv_bfloat16*>(residual), static_cast<const __nv_bfloat16*>(gamma),
+                          static_cast<__nv_bfloat16*>(total), static_cast<uint8_t*>(codes), scales, hid, eps);
+    };
+    if (hid <= 2048) DEER_CUDA(run(rmsnorm_quant_kernel<128, 1>, 128));
+    else if (hid <= 4096) DEER_CUDA(run(rmsnorm_quant_kernel<256, 1>, 256));
+    else if (hid <= 8192) DEER_CUDA(run(rmsnorm_quant_kernel<512, 1>, 512));
+    else if (hid <= 16384) DEER_CUDA(run(rmsnorm_quant_kernel<512, 2>, 512));
+    else DEER_CUDA(run(rmsnorm_quant_kernel<1024, 4>, 1024));
+    return DEER_OK;
+}
+
+extern "C" int deer_quantize(const void* x, int gated, void* codes, float* scales, int M, int K, void* stream) {
+    DEER_CHECK_ARG(x && codes && scales, DEER_ERR_INVALID_ARG, "deer_quantize: null argument");
+    DEER_CHECK_ARG(deer_aligned16(x) && deer_aligned16(codes) && deer_aligned4(scales), DEER_ERR_INVALID_ARG,
+                   "deer_quantize: pointers must be 16-byte aligned (scales: 4)");
+    DEER_CHECK_ARG(M >= 0, DEER_ERR_INVALID_ARG, "deer_quantize: M must be >= 0");
+    DEER_CHECK_ARG(K >= 16 && K % 16 == 0, DEER_ERR_UNSUPPORTED, "deer_quantize: K must be a multiple of 16");
+    if (M == 0) return DEER_OK;
+    const long long items = (long long)M * ((K + GROUP - 1) / GROUP), blocks = (items + 31) / 32;
+    DEER_CHECK_ARG(blocks <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_quantize: too many rows");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    DEER_CUDA(launch_pdl(gated ? quantize_kernel<true> : quantize_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st,
+                         static_cast<const __nv_bfloat16*>(x), static_cast<uint8_t*>(codes), scales, M, K));
+    return DEER_OK;
+}
+
+extern "C" int deer_kv_store(deer_kv* kv, const int32_t* seq_ids, const void* k_rows, const void* v_rows, const int32_t* keep, int B, int k,
+                             void* stream) {
+    DEER_CHECK_ARG(kv && seq_ids && k_rows && v_rows, DEER_ERR_INVALID_ARG, "deer_kv_store: null argument");
+    DEER_CHECK_ARG(kv->quant, DEER_ERR_UNSUPPORTED, "deer_kv_store: the cache holds bf16 pools (deer_block_attn appends to those)");
+    DEER_CHECK_ARG(deer_aligned16(k_rows) && deer_aligned16(v_rows), DEER_ERR_INVALID_ARG, "deer_kv_store: pointers must be 16-byte aligned");
+    DEER_CHECK_ARG(B >= 0 && B <= 65535, DEER_ERR_UNSUPPORTED, "deer_kv_store: B must be in [0, 65535]");
+    DEER_CHECK_ARG(k >= 0 && k <= (1 << 24), DEER_ERR_UNSUPPORTED, "deer_kv_store: k must be in [0, 2^24]");
+    DEER_CHECK_ARG(kv->d.n_kv_heads <= 65535, DEER_ERR_UNSUPPORTED, "deer_kv_store: too many KV heads");
+    if (B == 0 || k == 0) return DEER_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // k rows that start anywhere in a page fill at most (15 + k) / 16 pages to their end (at least one block: k >= 1)
+    const dim3 grid((unsigned)((15 + k) / DEER_PAGE_SIZE), (unsigned)kv->d.n_kv_heads, (unsigned)B);
+    auto run = [&](auto kernel, int threads) {
+        return launch_pdl(kernel, grid, dim3((unsigned)threads), 0, st, kv->d, kv->q, seq_ids, static_cast<const __nv_bfloat16*>(k_rows),
+                          static_cast<const __nv_bfloat16*>(v_rows), keep, k);
+    };
+    if (kv->d.head_dim == 128) DEER_CUDA(run(kv_store_kernel<128>, 256));
+    else DEER_CUDA(run(kv_store_kernel<64>, 128));
+    return DEER_OK;
+}

@@ -76,6 +76,10 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* tm,
         ::"r"(dst), "l"(tm), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v)
         : "memory");
 }
+// Brings a tile into L2 only: nothing observes it, so it may run ahead of the wait for the kernel before.
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* tm, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(tm), "r"(x), "r"(y) : "memory");
+}
 // ---- TMA tile stores (shared -> global), tracked by the issuing thread's bulk groups ----
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src, int x, int y) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(x), "r"(y)
@@ -137,6 +141,16 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
         : "memory");
 }
 
+// D[tmem] (+)= A[smem] * B[smem], 8-bit x 8-bit -> fp32 (contraction of 32 per instruction).
+__device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
 // Shared-memory operand descriptor, 128-byte swizzle, tile base 1024-byte aligned.
 //   K-major operand ([rows][64] bf16, the contraction index contiguous): sbo = bytes between 8-row groups.
 //   MN-major operand ([k][64] bf16, the row/column index contiguous): lbo = bytes between 64-element groups
@@ -157,6 +171,9 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_kmajor(uint32_t addr) { retu
 __device__ __forceinline__ uint32_t make_idesc_bf16(int n, int b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(b_mn_major & 1) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
+
+// kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N = n, both operands K-major.
+__device__ __forceinline__ uint32_t make_idesc_e4m3(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 
 // Tensor-memory loads/stores: thread = lane of the warp's 32-lane quarter, N consecutive 32-bit columns.
 #define TMEM_LD_X16(taddr, r)                                                                                         \
@@ -285,6 +302,10 @@ inline int make_map(CUtensorMap* tm, CUtensorMapDataType dtype, const void* base
 inline int make_map_bf16(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                          const uint32_t* box) {
     return make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rank, dims, strides_bytes, box);
+}
+inline int make_map_u8(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                       const uint32_t* box) {
+    return make_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rank, dims, strides_bytes, box);
 }
 inline int make_map_f32(CUtensorMap* tm, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                         const uint32_t* box) {

@@ -173,6 +173,7 @@ extern "C" int deer_verify_step_host(deer_kv* kv, const deer_step_dev* dev, cons
     DEER_CHECK_ARG(kv && dev && w && q_host && k_blk_host && v_blk_host && h_host && draft_ids_host && accept_len_host &&
                        out_ids_host && n_out_host,
                    DEER_ERR_INVALID_ARG, "deer_verify_step_host: null argument");
+    DEER_CHECK_ARG(!kv->quant, DEER_ERR_UNSUPPORTED, "deer_verify_step_host: the cache holds 8-bit pools");
     DEER_CHECK_ARG(B > 0 && k >= 1 && k <= DEER_MAX_BLOCK, DEER_ERR_UNSUPPORTED, "deer_verify_step_host: bad B or k");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 

@@ -1,0 +1,417 @@
+"""The 8-bit calls on the GPU against the oracle in 64 bits.
+
+Tolerances, derived:
+  codes      the device's quotient y / s may differ from the oracle's by the fp32 roundings on the way (DELTA, relative), so a
+             code is within half an e4m3 step of the oracle's quotient plus that; s within 2 DELTA.
+  linear     one bf16 rounding of the result (2^-8), and fp32 accumulation: at most (K / 128 + 16) additions of 2^-24
+             relative to the sum of magnitudes for K <= 16384, i.e. below 2^-16 of it.
+  attention  one bf16 rounding (2^-8), and probabilities with 9 significant bits or more (2^-9 each, of sum p |v|);
+             the scores' fp32 sums move p by less than 2^-12 at these magnitudes.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import deer_oracle as O
+from paper_2512_15176_b200 import workload as W
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+
+
+def f64(t):
+    return t.to(torch.float64).cpu().numpy()
+
+
+def check_codes(codes, scales, y64, delta, label):
+    """codes [M, K], scales [M, G] of the device against the fp64 values y64."""
+    K = y64.shape[1]
+    got, s = f64(codes), f64(scales)
+    G = -(-K // 128)
+    want_s = np.stack([np.maximum(np.abs(y64[:, g * 128:(g + 1) * 128]).max(axis=1) / 448.0, 2.0 ** -126) for g in range(G)], 1)
+    assert (np.abs(s - want_s) <= 2 * delta * want_s).all(), label
+    q = y64 / np.repeat(want_s, 128, axis=1)[:, :K]
+    err = np.abs(got - np.clip(q, -448, 448))
+    tol = O.e4m3_step(q) / 2 + 4 * delta * np.abs(q) + 1e-12
+    assert np.isfinite(got).all() and (err <= tol).all(), f"{label}: {np.max(err - tol)}"
+
+
+@pytest.mark.parametrize("M,K,res,total", [(1, 16, False, False), (3, 128, True, True), (37, 2048, True, True), (5, 2064, True, False),
+                                           (2, 4096, False, True), (9, 4112, True, True), (4, 8192, True, True), (3, 8208, False, False),
+                                           (2, 16400, True, True), (1, 65536, True, True), (300, 144, True, True)])
+def test_rmsnorm_quant(M, K, res, total):
+    from paper_2512_15176_b200 import binding as L
+    x, g = W.normal(201, "x", (M, K), 1.7), W.normal(201, "g", (K,), 1.0)
+    r = W.normal(201, "r", (M, K), 1.0) if res else None
+    x[0, :: 41] *= 30.0
+    G = -(-K // 128)
+    codes = torch.full((M + 1, K), 2.0, device="cuda").to(F8)
+    scales = torch.full((M + 1, G), 7.0, device="cuda")
+    tot = torch.full((M + 1, K), 5.0, dtype=torch.bfloat16, device="cuda")
+    L.deer_rmsnorm_quant(x.cuda(), g.cuda(), codes[:M], scales[:M], 1e-6, residual=r.cuda() if res else None, total=tot[:M] if total else None)
+    torch.cuda.synchronize()
+    h = f64(x) + (f64(r) if res else 0.0)
+    check_codes(codes[:M], scales[:M], O.rmsnorm(h, f64(g), 1e-6), 2e-6, f"rmsnorm {M}x{K}")
+    if total:
+        assert (f64(tot[:M]) == f64(torch.from_numpy(h.astype(np.float32)).to(torch.bfloat16))).all()
+    # what lies behind the last row stays
+    assert (f64(codes[M]) == 2).all() and (scales[M] == 7).all() and (tot[M] == 5).all()
+
+
+def test_rmsnorm_quant_total_in_place():
+    from paper_2512_15176_b200 import binding as L
+    M, K = 33, 4096
+    x, r, g = (W.normal(202, n, s, 1.0).cuda() for n, s in (("x", (M, K)), ("r", (M, K)), ("g", (K,))))
+    outs = []
+    for into in (None, "x", "r"):
+        xx, rr = x.clone(), r.clone()
+        tot = {None: torch.empty_like(x), "x": xx, "r": rr}[into]
+        codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, 32, device="cuda")
+        L.deer_rmsnorm_quant(xx, g, codes, scales, 1e-6, residual=rr, total=tot)
+        outs.append((codes.view(torch.uint8), scales, tot))
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], o))
+
+
+@pytest.mark.parametrize("M,K,gated", [(1, 16, False), (3, 128, True), (33, 208, True), (5, 4096, False), (64, 1536, True), (257, 1040, False)])
+def test_quantize(M, K, gated):
+    from paper_2512_15176_b200 import binding as L
+    x = W.normal(203, "x", (M, 2 * K if gated else K), 2.0)
+    G = -(-K // 128)
+    codes = torch.full((M + 1, K), 2.0, device="cuda").to(F8)
+    scales = torch.full((M + 1, G), 7.0, device="cuda")
+    L.deer_quantize(x.cuda(), codes[:M], scales[:M], gated=gated)
+    torch.cuda.synchronize()
+    x64 = f64(x)
+    y = O.swiglu(x64[:, :K], x64[:, K:]) if gated else x64
+    if gated:
+        check_codes(codes[:M], scales[:M], y, 8e-6, f"gated {M}x{K}")
+    else:                                                  # nothing is rounded before the quotient: bit-exact
+        want_c, want_s = O.quantise_rows(y)
+        assert (f64(codes[:M]) == want_c).all() and (scales[:M].cpu().numpy() == want_s).all()
+    assert (f64(codes[M]) == 2).all() and (scales[M] == 7).all()
+
+
+def test_quantize_zeros_nan_inf_and_tiny_groups():
+    """A group of zeros has codes 0; a NaN or an infinity poisons its own group of 128 columns and no other."""
+    from paper_2512_15176_b200 import binding as L
+    x = W.normal(204, "x", (4, 512), 1.0)
+    x[0] = 0.0
+    x[1, 130] = float("nan")
+    x[2, 300] = float("inf")
+    x[3, :128] = 2.0 ** -130                               # subnormal: below the smallest scale
+    codes, scales = torch.empty(4, 512, dtype=F8, device="cuda"), torch.empty(4, 4, device="cuda")
+    L.deer_quantize(x.cuda(), codes, scales)
+    v = (codes.float().view(4, 4, 128) * scales[:, :, None]).cpu()
+    assert (v[0] == 0).all() and (scales[0] == 2.0 ** -126).all()
+    assert v[1, 1].isnan().all() and v[1, [0, 2, 3]].isfinite().all()
+    assert v[2, 2].isnan().all() and v[2, [0, 1, 3]].isfinite().all()
+    assert (v[3, 0] == 2.0 ** -130).all()
+
+
+def _linear_inputs(M, K, N, seed=205):
+    x, w = W.normal(seed, "x", (M, K), 1.0, dtype=torch.float32), W.normal(seed, "w", (N, K), 1.0, dtype=torch.float32)
+    w = w * torch.exp(torch.linspace(-2, 2, N))[:, None]
+    xc, xs = O.quantise_rows(f64(x))
+    wc, ws = O.quantise_weight(f64(w))
+    dev = lambda c: torch.from_numpy(c).float().to(F8).cuda()
+    return (dev(xc), torch.from_numpy(xs).cuda(), dev(wc), torch.from_numpy(ws).cuda()), O.dequantise_rows(xc, xs), O.dequantise_weight(wc, ws)
+
+
+@pytest.mark.parametrize("M,K,N,res", [(1, 128, 128, False), (1, 4096, 4096, True), (7, 1024, 272, True), (16, 16, 16, False), (17, 208, 144, True),
+                                       (32, 4096, 1024, True), (33, 640, 2000, False), (64, 2048, 512, True), (65, 1296, 400, True),
+                                       (128, 1024, 1040, True), (129, 512, 4096, False), (256, 2048, 384, True), (300, 1536, 656, True),
+                                       (513, 272, 128, True), (32, 12288, 256, False)])
+def test_linear_quant(M, K, N, res):
+    from paper_2512_15176_b200 import binding as L
+    dev, x64, w64 = _linear_inputs(M, K, N)
+    r = W.normal(205, "r", (M, N), 3.0) if res else None
+    y = torch.full((M + 1, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    L.deer_linear_quant(*dev, y[:M], residual=r.cuda() if res else None)
+    torch.cuda.synchronize()
+    want = x64 @ w64.T + (f64(r) if res else 0.0)
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -16 * (np.abs(x64) @ np.abs(w64).T) + 1e-30
+    err = np.abs(f64(y[:M]) - want)
+    assert np.isfinite(f64(y[:M])).all() and (err <= tol).all(), f"{np.max(err / tol)}"
+    assert (y[M] == 9).all()
+    # the same bits again, and with the residual in place of the output
+    y2 = r.cuda() if res else torch.empty_like(y[:M])
+    L.deer_linear_quant(*dev, y2, residual=y2 if res else None)
+    assert torch.equal(y2, y[:M])
+
+
+def test_linear_quant_nan_stays_in_its_row_and_column():
+    from paper_2512_15176_b200 import binding as L
+    (x, xs, w, ws), _, _ = _linear_inputs(40, 512, 384)
+    xs[5, 2] = float("nan")
+    ws[1, 3] = float("inf")                                # rows 128 .. 255 of w
+    y = torch.empty(40, 384, dtype=torch.bfloat16, device="cuda")
+    L.deer_linear_quant(x, xs, w, ws, y)
+    bad = ~y.isfinite()
+    assert bad[5].all() and bad[:, 128:256].all()
+    bad[5] = False
+    bad[:, 128:256] = False
+    assert not bad.any()
+
+
+# ---- the 8-bit cache -------------------------------------------------------------------------------------------
+
+def _cache(lengths, Hkv, D, room, seed, spare=3, device="cuda"):
+    """A cache with random codes, scales and tails on the device, and the oracle's copy of it.  Pages in random order;
+    every sequence can hold its length plus `room`."""
+    from paper_2512_15176_b200 import binding as L
+    rng = np.random.default_rng(seed)
+    need = [-(-(n + room) // 16) for n in lengths]
+    total, width, S = sum(need) + spare, max(max(need), 1), len(lengths)
+    order = rng.permutation(total)
+    table = np.full((S, width), -1, dtype=np.int32)
+    at = 0
+    for s, c in enumerate(need):
+        table[s, :c] = order[at:at + c]
+        at += c
+    free = order[at:]
+    stack = np.zeros(total, dtype=np.int32)
+    stack[:len(free)] = free
+    g = torch.Generator().manual_seed(seed)
+    codes = lambda: (torch.randn(total, Hkv, 16, D, generator=g) * 120).clamp(-448, 448).to(F8)
+    scale = lambda: torch.exp(torch.randn(total, Hkv, generator=g)) / 120
+    tail = lambda: torch.randn(S, Hkv, 48, D, generator=g).to(torch.bfloat16)
+    kp, vp, ks, vs, kt, vt = codes(), codes(), scale(), scale(), tail(), tail()
+    i32 = lambda a: torch.as_tensor(np.asarray(a, dtype=np.int32), device=device)
+    kv = L.KVCacheQuant(*(t.to(device) for t in (kp, vp, ks, vs, kt, vt)), i32(table), i32(lengths), i32(need), i32(stack), i32([len(free)]))
+    okv = O.QuantKV(f64(kp), f64(vp), ks.numpy(), vs.numpy(), f64(kt), f64(vt), table, np.asarray(lengths))
+    return kv, okv
+
+
+def _same_cache(kv, okv, label=""):
+    for x, (pool, scale, tail) in enumerate(((kv.k_pool, kv.k_scale, kv.k_tail), (kv.v_pool, kv.v_scale, kv.v_tail))):
+        assert (scale.cpu().numpy() == okv.scale[x]).all(), label
+        assert (f64(pool) == okv.codes[x]).all(), label
+        assert (f64(tail) == okv.tail[x]).all(), label
+
+
+def _ids(n):
+    return torch.arange(n, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths,k,keep", [([0], 1, [1]), ([15], 1, [1]), ([15, 16, 17, 0], 1, [1, 1, 0, 1]), ([3, 31, 47, 100], 32, [32, 17, 1, 0]),
+                                            ([14, 30], 18, [18, 2]), ([0, 5, 16], 77, [77, 60, 76]), ([9, 1], 400, [399, 64]), ([40], 5, [3])])
+def test_store(lengths, k, keep, D):
+    """Bit-exact pools, scales and tails, what the call does not touch included; repeated, it changes nothing."""
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache(lengths, 2, D, k, 301)
+    B = len(lengths)
+    kr, vr = W.normal(301, "k", (B, k, 2, D), 1.0), W.normal(301, "v", (B, k, 2, D), 3.0)
+    kr[0, 0] = 0.0
+    ids = list(range(B))[::-1]
+    dev = [torch.tensor(ids, dtype=torch.int32, device="cuda"), kr.cuda(), vr.cuda(), torch.tensor(keep, dtype=torch.int32, device="cuda")]
+    okv.store(ids, f64(kr), f64(vr), keep)
+    for turn in range(2 if k <= 32 else 1):
+        L.deer_kv_store(kv, *dev)
+        torch.cuda.synchronize()
+        assert L.deer_kv_status(kv) == 0
+        _same_cache(kv, okv, f"turn {turn}")
+    assert (kv.seq_len.cpu().numpy() == okv.seq_len).all()
+
+
+def test_store_clamps_keep_and_reports_unmapped_pages():
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache([10, 20], 2, 64, 32, 302)
+    kr, vr = W.normal(302, "k", (2, 8, 2, 64), 1.0), W.normal(302, "v", (2, 8, 2, 64), 1.0)
+    L.deer_kv_store(kv, _ids(2), kr.cuda(), vr.cuda(), torch.tensor([99, -5], dtype=torch.int32, device="cuda"))
+    okv.store([0, 1], f64(kr), f64(vr), [8, 0])
+    _same_cache(kv, okv)
+    kv.page_table[0, 0] = -1
+    before = kv.k_pool.view(torch.uint8).clone()
+    L.deer_kv_store(kv, _ids(1), kr[:1].cuda(), vr[:1].cuda())
+    assert L.deer_kv_status(kv) == L.DEER_ERR_BAD_PAGE and torch.equal(before, kv.k_pool.view(torch.uint8))
+    kv.page_table[0, 0] = kv.k_pool.shape[0]
+    L.deer_kv_store(kv, _ids(1), kr[:1].cuda(), vr[:1].cuda())
+    assert L.deer_kv_status(kv) == L.DEER_ERR_BAD_PAGE and torch.equal(before, kv.k_pool.view(torch.uint8))
+    L.deer_kv_store(kv, _ids(1) + 7, kr[:1].cuda(), vr[:1].cuda())
+    assert L.deer_kv_status(kv) == L.DEER_ERR_INVALID_ARG
+
+
+def check_attention(out, q, kb, vb, okv, ids, mask, scale, states, label):
+    q64, k64, v64 = f64(q), f64(kb), f64(vb)
+    want = O.quant_block_attention(q64, k64, v64, okv, ids, mask, scale, states)
+    a = O.QuantKV(okv.codes[0], np.abs(okv.codes[1]), *okv.scale, okv.tail[0], np.abs(okv.tail[1]), okv.page_table, okv.seq_len)
+    mass = O.quant_block_attention(q64, k64, np.abs(v64), a, ids, mask, scale, states)       # sum p |v|
+    got = f64(out)
+    err, tol = np.abs(got - want), 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 2.0 ** -12) * mass + 1e-30
+    assert np.isfinite(got).all(), label
+    assert (err <= tol).all(), f"{label}: {np.max(err / tol)}"
+
+
+CASES = [
+    # lengths, k, Hq, Hkv, D, mask
+    ([0], 1, 2, 1, 64, "causal"), ([1], 1, 8, 8, 128, "causal"), ([15, 16, 17], 1, 4, 2, 128, "causal"), ([0, 31, 33], 5, 8, 2, 64, "causal"),
+    ([1003], 1, 32, 8, 128, "causal"), ([5000, 3], 1, 8, 2, 64, "causal"), ([300, 77, 1024], 32, 16, 4, 128, "causal"),
+    ([129, 0], 32, 8, 1, 128, "bidir"), ([700, 16], 17, 6, 2, 128, "states"), ([31, 250, 0, 64], 32, 4, 4, 64, "states"),
+    ([2500], 32, 32, 8, 128, "causal"), ([1500, 1111], 32, 16, 2, 128, "states"), ([640], 31, 7, 1, 128, "causal"), ([97], 9, 40, 2, 128, "bidir"),
+]
+
+
+@pytest.mark.parametrize("lengths,k,Hq,Hkv,D,mask", CASES)
+def test_attention(lengths, k, Hq, Hkv, D, mask):
+    from paper_2512_15176_b200 import binding as L
+    B = len(lengths)
+    kv, okv = _cache(lengths, Hkv, D, 0, 401)
+    q, kb, vb = (W.normal(401, n, (B, k, h, D), 1.0) for n, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    states = None
+    if mask == "states":
+        states = W.rng(401, "states").integers(-1, 2, size=(B, k)).astype(np.int32)
+        states[-1] = -1                                    # a sequence whose rows are all absent
+    m = L.DEER_MASK_CAUSAL if mask == "causal" else L.DEER_MASK_BIDIR
+    ids = list(range(B))[::-1]
+    out = torch.full((B + 1, k, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    msl = max(lengths)
+    need = L.deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, msl)
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")          # NaN patterns: nothing unwritten may be read
+    L.deer_block_attn_quant(kv, torch.tensor(ids, dtype=torch.int32, device="cuda"), q.cuda(), kb.cuda(), vb.cuda(), out[:B],
+                            None if states is None else torch.from_numpy(states).cuda(), m, 1 / math.sqrt(D), msl, ws[:need])
+    torch.cuda.synchronize()
+    assert L.deer_kv_status(kv) == 0
+    check_attention(out[:B], q, kb, vb, okv, ids, m, 1 / math.sqrt(D), states, f"{lengths} {k} {mask}")
+    assert out[B].isnan().all() and (ws[need:] == 255).all()
+
+
+@pytest.mark.parametrize("k,Hq,Hkv,D", [(1, 4, 1, 128), (8, 4, 2, 64), (32, 16, 4, 128), (16, 8, 1, 128)])
+def test_attention_spread_scales_and_scores(k, Hq, Hkv, D):
+    """Page scales over forty octaves (pages of zeros among them), a dominating key late in the context over a long
+    background whose tiny weights add up, and queries of very different size."""
+    from paper_2512_15176_b200 import binding as L
+    n = 2000
+    kv, okv = _cache([n], Hkv, D, 0, 402)
+    rng = np.random.default_rng(402)
+    vs = np.exp2(rng.uniform(-20, 20, size=okv.scale[1].shape)).astype(np.float32)
+    vs[rng.integers(0, len(vs), 9)] = np.float32(2.0 ** -126)
+    okv.scale[1][:] = vs
+    zero = int(okv.page_table[0, 5])
+    okv.codes[1][zero] = 0.0
+    okv.codes[0][int(okv.page_table[0, 7])] = 0.0
+    okv.scale[0][:] = (okv.scale[0] * 0.02).astype(np.float32)                 # a flat background ...
+    big = int(okv.page_table[0, 100])
+    okv.scale[0][big] = np.float32(0.02)
+    kv.v_scale.copy_(torch.from_numpy(okv.scale[1]))
+    kv.k_scale.copy_(torch.from_numpy(okv.scale[0]))
+    kv.v_pool.copy_(torch.from_numpy(okv.codes[1]).float().to(F8))
+    kv.k_pool.copy_(torch.from_numpy(okv.codes[0]).float().to(F8))
+    q, kb, vb = (W.normal(402, x, (1, k, h, D), 1.0) for x, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    q[0, 0] *= 2.0 ** -20
+    if k > 2:
+        q[0, 1] = 0.0
+    out = torch.empty(1, k, Hq, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((L.deer_block_attn_quant_workspace_bytes(1, k, Hq, Hkv, D, n),), 255, dtype=torch.uint8, device="cuda")
+    L.deer_block_attn_quant(kv, _ids(1), q.cuda(), kb.cuda(), vb.cuda(), out, None, L.DEER_MASK_CAUSAL, 1 / math.sqrt(D), n, ws)
+    check_attention(out, q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, "spread")
+
+
+@pytest.mark.parametrize("k,Hq,Hkv,D", [(4, 2, 1, 64), (32, 16, 4, 128), (20, 8, 1, 128)])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_attention_nonfinite_rows_reach_only_rows_that_see_them(k, Hq, Hkv, D, what):
+    from paper_2512_15176_b200 import binding as L
+    n, bad = 200, float(what)
+    kv, okv = _cache([n], Hkv, D, 0, 403)
+    q, kb, vb = (W.normal(403, x, (1, k, h, D), 1.0) for x, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    clean = (q.clone(), kb.clone(), vb.clone())
+    j = k - 2
+    vb[0, j, 0, 3] = bad                                   # seen by rows j.. (causal)
+    kb[0, k - 1, 0, 5] = float("nan")                      # seen by the last row alone
+    ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(1, k, Hq, Hkv, D, n), dtype=torch.uint8, device="cuda")
+    out = torch.empty(1, k, Hq, D, dtype=torch.bfloat16, device="cuda")
+    run = lambda m, st: L.deer_block_attn_quant(kv, _ids(1), q.cuda(), kb.cuda(), vb.cuda(), out, st, m, 1 / math.sqrt(D), n, ws)
+    run(L.DEER_MASK_CAUSAL, None)
+    G = Hq // Hkv
+    got = out.float().cpu()
+    assert got[0, :j].isfinite().all()
+    assert (got[0, j, :G, 3].isnan() if what == "nan" else got[0, j, :G, 3] == bad).all()
+    assert got[0, j, :G, :3].isfinite().all() and got[0, j, :G, 4:].isfinite().all()
+    assert got[0, k - 1, :G].isnan().all()
+    assert got[0, :, G:].isfinite().all()                  # the other KV heads' rows
+    want = O.quant_block_attention(f64(clean[0]), f64(clean[1]), f64(clean[2]), okv, [0], 0, 1 / math.sqrt(D))
+    assert np.abs(f64(out[0, :j]) - want[0, :j]).max() <= 2.0 ** -6 * np.abs(want).max()
+    # absent positions hold anything
+    st = torch.zeros(1, k, dtype=torch.int32)
+    st[0, j:] = -1
+    st[0, 0] = 1
+    run(L.DEER_MASK_BIDIR, st.cuda())
+    check_attention(out, clean[0], torch.where(kb.isfinite(), kb, 0), torch.where(vb.isfinite(), vb, 0), okv, [0], 1, 1 / math.sqrt(D), st.numpy(), "absent")
+
+
+def test_attention_skips_sequences_it_cannot_use():
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache([40, 500], 2, 128, 0, 404)
+    q, kb, vb = (W.normal(404, x, (2, 4, h, 128), 1.0).cuda() for x, h in (("q", 4), ("k", 2), ("v", 2)))
+    out = torch.full((2, 4, 4, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(2, 4, 4, 2, 128, 100), dtype=torch.uint8, device="cuda")
+    L.deer_block_attn_quant(kv, _ids(2), q, kb, vb, out, None, 0, 0.1, 100, ws)           # sequence 1 is longer than max_seq_len
+    assert L.deer_kv_status(kv) == L.DEER_ERR_INVALID_ARG
+    check_attention(out[:1], q[:1], kb[:1], vb[:1], okv, [0], 0, 0.1, None, "first")
+    kv.page_table[0, 1] = kv.k_pool.shape[0] + 5
+    L.deer_block_attn_quant(kv, _ids(1), q[:1], kb[:1], vb[:1], out[:1], None, 0, 0.1, 100, ws)
+    assert L.deer_kv_status(kv) == L.DEER_ERR_BAD_PAGE
+
+
+@pytest.mark.parametrize("k", [1, 32])
+def test_pools_past_four_gigabytes(k):
+    """Pages at the far end of pools of more than 2^32 bytes: store there, then read."""
+    from paper_2512_15176_b200 import binding as L
+    Hkv, D, pages = 8, 128, (1 << 32) // (8 * 16 * 128) + 40
+    kv = L.KVCacheQuant.empty(pages, Hkv, D, 1, 8)
+    kv.free_stack.copy_(torch.arange(pages, dtype=torch.int32, device="cuda"))            # the highest pages first
+    kr, vr = W.normal(405, "k", (1, 100, Hkv, D), 1.0), W.normal(405, "v", (1, 100, Hkv, D), 1.0)
+    L.deer_kv_reserve_rows(kv, _ids(1), 100)
+    L.deer_kv_store(kv, _ids(1), kr.cuda(), vr.cuda())
+    L.deer_kv_commit_rows(kv, _ids(1), torch.tensor([100], dtype=torch.int32, device="cuda"), 100)
+    assert L.deer_kv_status(kv) == 0
+    table = kv.page_table.cpu().numpy()
+    assert table[0, 0] == pages - 1 and kv.seq_len.item() == 100
+    z = lambda *s: np.zeros(s)
+    okv = O.QuantKV(z(7, Hkv, 16, D), z(7, Hkv, 16, D), z(7, Hkv), z(7, Hkv), z(1, Hkv, 48, D), z(1, Hkv, 48, D), np.arange(7)[None], np.array([0]))
+    okv.store([0], f64(kr), f64(vr), [100])
+    okv.seq_len[:] = 100
+    assert (f64(kv.k_pool[torch.from_numpy(table[0, :6].astype(np.int64)).cuda()].float()) == okv.codes[0][:6]).all()
+    q, kb, vb = (W.normal(406, x, (1, k, h, D), 1.0) for x, h in (("q", 32), ("k", Hkv), ("v", Hkv)))
+    out = torch.empty(1, k, 32, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(1, k, 32, Hkv, D, 100), dtype=torch.uint8, device="cuda")
+    L.deer_block_attn_quant(kv, _ids(1), q.cuda(), kb.cuda(), vb.cuda(), out, None, 0, 1 / math.sqrt(D), 100, ws)
+    check_attention(out, q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, "far pages")
+
+
+def test_reserve_store_commit_soak():
+    """Rounds of reserve, attention, store and commit with random keeps, rejected rows included, then a prompt: the
+    cache and the lengths follow the oracle bit by bit, the attention within its tolerance."""
+    from paper_2512_15176_b200 import binding as L
+    Hkv, Hq, D, S = 2, 8, 128, 3
+    kv = L.KVCacheQuant.empty(64, Hkv, D, S, 24)
+    z = lambda *s: np.zeros(s)
+    okv = O.QuantKV(z(64, Hkv, 16, D), z(64, Hkv, 16, D), z(64, Hkv), z(64, Hkv), z(S, Hkv, 48, D), z(S, Hkv, 48, D), np.zeros((S, 24), dtype=np.int64),
+                    np.zeros(S, dtype=np.int64))
+    rng = np.random.default_rng(7)
+    for turn in range(8):
+        k = 90 if turn == 0 else int(rng.integers(1, 33))
+        kr, vr = W.normal(500 + turn, "k", (S, k, Hkv, D), 1.0), W.normal(500 + turn, "v", (S, k, Hkv, D), 1.0)
+        keep = rng.integers(0, k + 1, size=S)
+        kd = torch.tensor(keep, dtype=torch.int32, device="cuda")
+        (L.deer_kv_reserve_rows if k > 32 else L.deer_kv_reserve)(kv, _ids(S), k)
+        okv.page_table = kv.page_table.cpu().numpy()
+        if k <= 32:
+            q = W.normal(500 + turn, "q", (S, k, Hq, D), 1.0)
+            out = torch.empty(S, k, Hq, D, dtype=torch.bfloat16, device="cuda")
+            msl = int(okv.seq_len.max())
+            ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(S, k, Hq, Hkv, D, msl), dtype=torch.uint8, device="cuda")
+            L.deer_block_attn_quant(kv, _ids(S), q.cuda(), kr.cuda(), vr.cuda(), out, None, 0, 1 / math.sqrt(D), msl, ws)
+            check_attention(out, q, kr, vr, okv, np.arange(S), 0, 1 / math.sqrt(D), None, f"turn {turn}")
+        L.deer_kv_store(kv, _ids(S), kr.cuda(), vr.cuda(), kd)
+        okv.store(np.arange(S), f64(kr), f64(vr), keep)
+        (L.deer_kv_commit_rows if k > 32 else L.deer_kv_commit)(kv, _ids(S), kd, k)
+        okv.seq_len = okv.seq_len + keep
+        assert L.deer_kv_status(kv) == 0
+        assert (kv.seq_len.cpu().numpy() == okv.seq_len).all()
+        assert (kv.n_pages.cpu().numpy() == -(-okv.seq_len // 16)).all()
+        _same_cache(kv, okv, f"turn {turn}")
