@@ -13,6 +13,8 @@
 // the column groups; the partial sums meet in shared memory (every block of the cluster adds up, in rank order, its
 // part of the tile's rows of x), so there is no workspace, no second kernel, and the order of the sums is fixed.
 //
+// More than 128 rows: the second kernel, pairs of blocks, the rows of x on the lanes (see there).
+//
 // Warp roles: warp 0 = TMA producer, warp 1 = MMA issuer (+ TMEM owner), the others = epilogue.  All waits are bounded;
 // a block whose wait runs out leaves its output unwritten (and so does its cluster).
 
@@ -27,16 +29,16 @@ using quant::GROUP;
 constexpr int BN = 128;                        // weight rows (output columns) of a tile
 constexpr int W_BYTES = BN * GROUP;            // 16 KB per stage
 
-// NT rows of x per tile; stages such that two blocks fit an SM (one for NT = 256).
+// NT rows of x per tile; stages such that two blocks fit an SM, whose tensor memory then suffices for both (a block
+// allocates it before it lets the next kernel in, so blocks that share an SM never wait for one another's columns).
 template <int NT>
 struct Cfg {
     static constexpr int STAGE = W_BYTES + NT * GROUP;
-    static constexpr int STAGES = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : NT == 128 ? 3 : 4;
+    static constexpr int STAGES = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3;
     static constexpr int NBUF = NT <= 64 ? 4 : 2;                 // accumulators in TMEM
     static constexpr int TMEM_COLS = NT * NBUF < 64 ? 64 : NT * NBUF;
-    static constexpr int EPI_WARPS = NT == 256 ? 8 : 4;
+    static constexpr int EPI_WARPS = 4;
     static constexpr int THREADS = 64 + EPI_WARPS * 32;
-    static constexpr int COLS = NT == 256 ? 128 : NT;             // accumulator columns of one epilogue thread
     static constexpr int SMEM = STAGES * STAGE + 1024 /*alignment slack*/ + 2 * NT * 4 /*scales*/ + (2 * STAGES + 2 * NBUF) * 8 + 16;
 };
 
@@ -60,7 +62,7 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
 }
 
 template <int NT>
-__global__ void __launch_bounds__(Cfg<NT>::THREADS, NT == 256 ? 1 : 2)
+__global__ void __launch_bounds__(Cfg<NT>::THREADS, 2)
 linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Args a) {
     using C = Cfg<NT>;
     constexpr int EPI_THREADS = C::EPI_WARPS * 32;
@@ -108,7 +110,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     tcgen05_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    float acc[C::COLS];
+    uint64_t acc[NT / 2];                          // two rows of x each
     if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < ng; ++i) {
@@ -138,68 +140,66 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         }
     } else {
         const int et = tid - 64;                                   // 0 .. EPI_THREADS - 1
-        const int half = NT == 256 ? (et >> 7) : 0;                // which 128 accumulator columns
-        const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * 128);
+        const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll
-        for (int j = 0; j < C::COLS; ++j) acc[j] = 0.f;
-        // thread et brings the scale of row m0 + et, four column groups ahead
+        for (int j = 0; j < NT / 2; ++j) acc[j] = 0;
+        // thread et brings the scale of row m0 + et, a column group ahead (eight groups share a 32-byte sector)
         const bool brings = et < NT;
         const float* xs = (brings && m0 + et < a.M) ? a.x_scale + (size_t)(m0 + et) * a.groups + g0 : nullptr;
         const float* ws = a.w_scale + (size_t)(n0 / GROUP) * a.groups + g0;
-        float nx[4], nw[4];
-        auto fetch = [&](int i0) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                nx[u] = (xs && i0 + u < ng) ? xs[i0 + u] : 0.f;
-                nw[u] = (xs && i0 + u < ng) ? ws[i0 + u] : 0.f;
-            }
-        };
-        fetch(0);
+        float nx = xs ? xs[0] : 0.f, nw = xs ? ws[0] : 0.f;
         bool alive = true;
-        for (int i0 = 0; i0 < ng; i0 += 4) {
-            float s4[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) s4[u] = nx[u] * nw[u];
-            fetch(i0 + 4);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = i0 + u;
-                if (i >= ng) break;
-                const int b = i % C::NBUF;
-                float* slot = sc + (i & 1) * NT;
-                if (brings) slot[et] = s4[u];
-                asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
-                // a warp whose wait ran out keeps meeting the others at the barrier
-                const bool got = alive && mbar_wait(tfull(b), (uint32_t)(i / C::NBUF) & 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, got)) {
-                    alive = false;
-                    continue;
-                }
-                tcgen05_fence_after();
-                const float4* s_row = reinterpret_cast<const float4*>(slot + half * 128);
-#pragma unroll
-                for (int c = 0; c < C::COLS; c += 16) {
-                    uint32_t r[16];
-                    TMEM_LD_X16(t_lane + (uint32_t)(b * NT + c), r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 16; j += 4) {
-                        const float4 s = s_row[(c + j) / 4];
-                        acc[c + j] = fmaf(__uint_as_float(r[j]), s.x, acc[c + j]);
-                        acc[c + j + 1] = fmaf(__uint_as_float(r[j + 1]), s.y, acc[c + j + 1]);
-                        acc[c + j + 2] = fmaf(__uint_as_float(r[j + 2]), s.z, acc[c + j + 2]);
-                        acc[c + j + 3] = fmaf(__uint_as_float(r[j + 3]), s.w, acc[c + j + 3]);
-                    }
-                }
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(tempty(b));
+        for (int i = 0; i < ng; ++i) {
+            const int b = i % C::NBUF;
+            float* slot = sc + (i & 1) * NT;
+            if (brings) slot[et] = nx * nw;
+            if (xs && i + 1 < ng) {
+                nx = xs[i + 1];
+                nw = ws[i + 1];
             }
+            asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
+            // a warp whose wait ran out keeps meeting the others at the barrier
+            const bool got = alive && mbar_wait(tfull(b), (uint32_t)(i / C::NBUF) & 1u, abort_flag);
+            if (!__all_sync(0xffffffffu, got)) {
+                alive = false;
+                continue;
+            }
+            tcgen05_fence_after();
+            const ulonglong2* s_row = reinterpret_cast<const ulonglong2*>(slot);
+            const uint32_t taddr = t_lane + (uint32_t)(b * NT);
+            auto add16 = [&](int c, const uint32_t (&v)[16]) {
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const ulonglong2 s = s_row[(c + j) / 4];
+                    fma_f32x2(acc[(c + j) / 2], v[j], v[j + 1], s.x);
+                    fma_f32x2(acc[(c + j) / 2 + 1], v[j + 2], v[j + 3], s.y);
+                }
+            };
+            if (NT <= 64) {                                        // 16 columns in flight while the 16 before them are added
+                uint32_t r[2][16];
+                TMEM_LD_X16(taddr, r[0]);
+#pragma unroll
+                for (int c = 0; c < NT; c += 16) {
+                    tmem_wait_ld();
+                    if (c + 16 < NT) TMEM_LD_X16(taddr + c + 16, r[(c / 16 + 1) & 1]);
+                    add16(c, r[(c / 16) & 1]);
+                }
+            } else {                                               // 128 sums leave no registers for that
+#pragma unroll
+                for (int c = 0; c < NT; c += 16) {
+                    uint32_t r[16];
+                    TMEM_LD_X16(taddr + c, r);
+                    tmem_wait_ld();
+                    add16(c, r);
+                }
+            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty(b));
         }
     }
 
     // ---- the tile's rows of x: this block writes all of them, or adds up its part of the cluster's partial sums ----
-    const int et = tid - 64, half = NT == 256 ? (et >> 7) : 0;
     const int lane_row = (warp & 3) * 32 + lane;                   // TMEM lane = output column within the tile
     const int n = n0 + lane_row;
     auto put = [&](int j, float v) {                               // row m0 + j of the output
@@ -212,14 +212,24 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     if (a.split == 1) {
         if (warp >= 2 && !*abort_flag) {
 #pragma unroll
-            for (int j = 0; j < C::COLS; ++j) put(half * 128 + j, acc[j]);
+            for (int j = 0; j < NT; j += 2) {
+                float lo, hi;
+                unpack_f32x2(acc[j / 2], lo, hi);
+                put(j, lo);
+                put(j + 1, hi);
+            }
         }
     } else {
         // every operand that was requested has been consumed (or the block is aborting and writes nothing): the ring is free
         float* buf = reinterpret_cast<float*>(ring);               // [NT][128]
         if (warp >= 2 && !*abort_flag) {
 #pragma unroll
-            for (int j = 0; j < C::COLS; ++j) buf[(half * 128 + j) * BN + lane_row] = acc[j];
+            for (int j = 0; j < NT; j += 2) {
+                float lo, hi;
+                unpack_f32x2(acc[j / 2], lo, hi);
+                buf[j * BN + lane_row] = lo;
+                buf[(j + 1) * BN + lane_row] = hi;
+            }
         }
         __syncwarp();
         cluster_sync();
@@ -228,7 +238,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         for (int r = 0; r < a.split; ++r) good = good && ld_cluster_u32(map_to_cta(flag_addr, (uint32_t)r)) == 0;
         if (warp >= 2 && good) {
             const int lo = NT * rank / a.split, hi = NT * (rank + 1) / a.split;
-            for (int j = lo + half; j < hi; j += C::EPI_WARPS / 4) {
+            for (int j = lo; j < hi; ++j) {
                 if (m0 + j >= a.M) break;
                 float v = 0.f;
                 for (int r = 0; r < a.split; ++r) v += ld_cluster_f32(map_to_cta(ring_addr + (uint32_t)((j * BN + lane_row) * 4), (uint32_t)r));
@@ -252,28 +262,220 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     }
 }
 
+// ---- more than 128 rows of x: pairs of blocks ---------------------------------------------------------------------
+// A cluster of two shares tiles of 256 rows of x (128 on each block's TMEM lanes) by BNP rows of w: one cta_group::2 MMA
+// reads half of the weight rows from each block's shared memory, so a block stages 128 + BNP / 2 rows per column group
+// where a tile of its own would take 128 + BNP.  A row of x per thread makes the scale of a column group ONE number per
+// thread and 128 columns -- no shared memory, no barrier between the epilogue's warps -- and eight epilogue warps, half
+// of the columns each, keep the sums in registers.  Clusters walk the tiles of the product, the tiles of 256 rows of x
+// that share weight rows next to each other in time.  Block 0 of the pair issues the MMAs; its `full` barriers count both
+// blocks' bytes, `empty` and `accumulator full` arrive in both blocks, both blocks' epilogue warps free an accumulator.
+template <int BNP>
+struct PairCfg {
+    static constexpr int HALF = BNP / 2;                          // weight rows a block stages; columns of an epilogue warp
+    static constexpr int X_BYTES = 128 * GROUP;
+    static constexpr int STAGE = X_BYTES + HALF * GROUP;
+    static constexpr int STAGES = BNP == 256 ? 6 : 8;
+    static constexpr int TMEM_COLS = 2 * BNP;
+    static constexpr int THREADS = 64 + 8 * 32;
+    static constexpr int SMEM = STAGES * STAGE + 1024 + (2 * STAGES + 4) * 8 + 16;
+};
+
+template <int BNP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<BNP>::THREADS, 1)
+linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Args a) {
+    using C = PairCfg<BNP>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + C::STAGES * C::STAGE);   // full, empty [STAGES]; tfull, tempty [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int cluster = (int)blockIdx.x >> 1, n_clusters = (int)gridDim.x >> 1;
+    const int tiles = a.m_tiles * ((a.N + BNP - 1) / BNP);
+
+    const uint32_t ring_addr = smem_u32(ring), bar_base = smem_u32(bars);
+    auto full = [&](int s) { return bar_base + 8u * s; };
+    auto empty = [&](int s) { return bar_base + 8u * (C::STAGES + s); };
+    auto tfull = [&](int b) { return bar_base + 8u * (2 * C::STAGES + b); };
+    auto tempty = [&](int b) { return bar_base + 8u * (2 * C::STAGES + 2 + b); };
+    if (tid == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(tfull(b), 1);
+            mbar_init(tempty(b), 16);                              // eight epilogue warps in each of the two blocks
+        }
+        *abort_flag = 0;
+        mbar_init_fence();
+    }
+    if (warp == 0 && lane == 0) {
+        prefetch_tensormap(&tm_w);
+        prefetch_tensormap(&tm_x);
+        const int n0 = cluster / a.m_tiles * BNP + (int)rank * C::HALF;
+        for (int i = 0; i < a.groups && i < C::STAGES && n0 < a.N; ++i) tma_prefetch_2d(&tm_w, i * GROUP, n0);
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), C::TMEM_COLS);
+    pdl_trigger();
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync();                                                // the peer's barriers exist before anything signals them
+    tcgen05_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int t = cluster; t < tiles && ok; t += n_clusters) {
+                const int m0 = t % a.m_tiles * 256 + (int)rank * 128, n0 = t / a.m_tiles * BNP + (int)rank * C::HALF;
+                for (int i = 0; i < a.groups; ++i, ++it) {
+                    const int s = it % C::STAGES;
+                    if (!mbar_wait(empty(s), ((uint32_t)(it / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                    if (rank == 0) mbar_expect_tx(full(s), 2u * C::STAGE);
+                    const uint32_t lead_full = map_to_cta(full(s), 0);
+                    tma_load_2d_pair(ring_addr + s * C::STAGE + C::X_BYTES, &tm_w, i * GROUP, n0, lead_full);
+                    tma_load_2d_pair(ring_addr + s * C::STAGE, &tm_x, i * GROUP, m0, lead_full);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            const uint32_t idesc = make_idesc_e4m3_pair(BNP);
+            int it = 0;
+            bool ok = true;
+            for (int t = cluster; t < tiles && ok; t += n_clusters) {
+                for (int i = 0; i < a.groups; ++i, ++it) {
+                    const int s = it % C::STAGES, b = it & 1;
+                    if (!mbar_wait(tempty(b), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(full(s), (uint32_t)(it / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    tcgen05_fence_after();
+                    const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
+                    const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + C::X_BYTES);
+#pragma unroll
+                    for (int kk = 0; kk < GROUP / 32; ++kk)
+                        umma_f8_ss_pair(tmem_base + (uint32_t)(b * BNP), xd + (uint64_t)(kk * 2), wd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
+                    umma_commit_pair(empty(s), 3);
+                    umma_commit_pair(tfull(b), 3);
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;      // TMEM lanes; which half of the columns
+        const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * C::HALF);
+        const uint32_t lead_tempty[2] = {map_to_cta(tempty(0), 0), map_to_cta(tempty(1), 0)};
+        int it = 0;
+        bool alive = true;
+        for (int t = cluster; t < tiles && alive; t += n_clusters) {
+            const int m = t % a.m_tiles * 256 + (int)rank * 128 + quarter * 32 + lane;
+            const int n0 = t / a.m_tiles * BNP + half * C::HALF;
+            const float* xs = a.x_scale + (size_t)(m < a.M ? m : 0) * a.groups;
+            const float* ws = a.w_scale + (size_t)(n0 < a.N ? n0 / GROUP : 0) * a.groups;
+            uint64_t acc[C::HALF / 2];
+#pragma unroll
+            for (int j = 0; j < C::HALF / 2; ++j) acc[j] = 0;
+            float nx = xs[0], nw = ws[0];
+            for (int i = 0; i < a.groups; ++i, ++it) {
+                const int b = it & 1;
+                const float sc = nx * nw;
+                if (i + 1 < a.groups) {                            // the next column group's scales
+                    nx = xs[i + 1];
+                    nw = ws[i + 1];
+                }
+                const bool got = mbar_wait(tfull(b), (uint32_t)(it >> 1) & 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
+                tcgen05_fence_after();
+                const uint64_t s2 = pack_f32x2(sc, sc);
+                uint32_t r[2][16];
+                TMEM_LD_X16(t_lane + (uint32_t)(b * BNP), r[0]);
+#pragma unroll
+                for (int c = 0; c < C::HALF; c += 16) {
+                    tmem_wait_ld();
+                    if (c + 16 < C::HALF) TMEM_LD_X16(t_lane + (uint32_t)(b * BNP + c + 16), r[(c / 16 + 1) & 1]);
+                    const uint32_t(&v)[16] = r[(c / 16) & 1];
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) fma_f32x2(acc[(c + j) / 2], v[j], v[j + 1], s2);
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_peer(lead_tempty[b]);
+            }
+            if (!alive || m >= a.M) continue;
+            __nv_bfloat16* dst = a.y + (size_t)m * a.N + n0;
+            const __nv_bfloat16* res = a.residual ? a.residual + (size_t)m * a.N + n0 : nullptr;
+#pragma unroll
+            for (int c = 0; c < C::HALF; c += 16) {                // N is a multiple of 16: whole pieces of 32 bytes
+                if (n0 + c >= a.N) break;
+                float v[16];
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) unpack_f32x2(acc[(c + j) / 2], v[j], v[j + 1]);
+                if (res) {
+                    float r[16];
+                    quant::load_bf16x16(res + c, r);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] += r[j];
+                }
+#pragma unroll
+                for (int h = 0; h < 16; h += 8)
+                    *reinterpret_cast<uint4*>(dst + c + h) = make_uint4(pack_bf16(v[h], v[h + 1]), pack_bf16(v[h + 2], v[h + 3]),
+                                                                        pack_bf16(v[h + 4], v[h + 5]), pack_bf16(v[h + 6], v[h + 7]));
+            }
+        }
+    }
+
+    // ---- tear-down: neither block leaves while the other may still signal it or read its shared memory ----
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+        __syncthreads();
+    }
+    cluster_sync();
+    if (warp == 1) {
+        __syncwarp();
+        tcgen05_fence_after();
+        tmem_dealloc_pair(tmem_base, C::TMEM_COLS);
+    }
+}
+
+static int operand_maps(CUtensorMap* tm_w, CUtensorMap* tm_x, const Args& a, const void* w, const void* x, uint32_t w_rows, uint32_t x_rows) {
+    const uint64_t str[1] = {(uint64_t)a.K};
+    const uint64_t dims_w[2] = {(uint64_t)a.K, (uint64_t)a.N}, dims_x[2] = {(uint64_t)a.K, (uint64_t)a.M};
+    const uint32_t box_w[2] = {GROUP, w_rows}, box_x[2] = {GROUP, x_rows};
+    const int rc = make_map_u8(tm_w, w, 2, dims_w, str, box_w);
+    return rc != DEER_OK ? rc : make_map_u8(tm_x, x, 2, dims_x, str, box_x);
+}
+
+template <int BNP>
+int launch_pair(Args a, const void* x, const void* w, cudaStream_t st) {
+    using C = PairCfg<BNP>;
+    CUtensorMap tm_w, tm_x;
+    const int rc = operand_maps(&tm_w, &tm_x, a, w, x, C::HALF, 128);
+    if (rc != DEER_OK) return rc;
+    a.m_tiles = (a.M + 255) / 256;
+    const long long tiles = (long long)a.m_tiles * ((a.N + BNP - 1) / BNP);
+    DEER_CHECK_ARG(tiles <= 0x3fffffffLL, DEER_ERR_UNSUPPORTED, "deer_linear_quant: too many tiles");
+    const long long clusters = tiles < deer_sm_count() / 2 ? tiles : deer_sm_count() / 2;
+    DEER_CUDA(cudaFuncSetAttribute(linear_quant_pair_kernel<BNP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    DEER_CUDA(launch_pdl(linear_quant_pair_kernel<BNP>, dim3((unsigned)(2 * clusters)), dim3(C::THREADS), (size_t)C::SMEM, st, tm_w, tm_x, a));
+    return DEER_OK;
+}
+
 template <int NT>
 int launch(Args a, const void* x, const void* w, cudaStream_t st) {
     using C = Cfg<NT>;
     CUtensorMap tm_w, tm_x;
-    const uint64_t str[1] = {(uint64_t)a.K};
-    {
-        const uint64_t dims[2] = {(uint64_t)a.K, (uint64_t)a.N};
-        const uint32_t box[2] = {GROUP, BN};
-        const int rc = make_map_u8(&tm_w, w, 2, dims, str, box);
-        if (rc != DEER_OK) return rc;
-    }
-    {
-        const uint64_t dims[2] = {(uint64_t)a.K, (uint64_t)a.M};
-        const uint32_t box[2] = {GROUP, NT};
-        const int rc = make_map_u8(&tm_x, x, 2, dims, str, box);
-        if (rc != DEER_OK) return rc;
-    }
+    const int rc = operand_maps(&tm_w, &tm_x, a, w, x, BN, NT);
+    if (rc != DEER_OK) return rc;
     a.m_tiles = (a.M + NT - 1) / NT;
     const long long tiles = (long long)((a.N + BN - 1) / BN) * a.m_tiles;
-    // As many blocks of a cluster as still fit beside each other (two per SM, one for NT = 256) with at least four
-    // column groups each.
-    const long long room = (long long)deer_sm_count() * (NT == 256 ? 1 : 2);
+    // As many blocks to a cluster as still fit beside each other (two per SM), with at least four column groups each.
+    const long long room = 2LL * deer_sm_count();
     a.split = 1;
     while (a.split < 8 && tiles * a.split * 2 <= room && a.groups >= a.split * 2 * 4) a.split *= 2;
     DEER_CHECK_ARG(tiles * a.split <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_linear_quant: too many tiles");
@@ -324,5 +526,5 @@ extern "C" int deer_linear_quant(const void* x, const float* x_scale, const void
     if (M <= 32) return launch<32>(a, x, w, st);
     if (M <= 64) return launch<64>(a, x, w, st);
     if (M <= 128) return launch<128>(a, x, w, st);
-    return launch<256>(a, x, w, st);
+    return launch_pair<256>(a, x, w, st);
 }

@@ -174,6 +174,8 @@ __device__ __forceinline__ uint32_t make_idesc_bf16(int n, int b_mn_major) {
 
 // kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N = n, both operands K-major.
 __device__ __forceinline__ uint32_t make_idesc_e4m3(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+// The same with M = 256 across a CTA pair.
+__device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (16u << 24); }
 
 // Tensor-memory loads/stores: thread = lane of the warp's 32-lane quarter, N consecutive 32-bit columns.
 #define TMEM_LD_X16(taddr, r)                                                                                         \
@@ -202,6 +204,20 @@ __device__ __forceinline__ uint32_t make_idesc_e4m3(int n) { return (1u << 4) | 
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])         \
                  : "memory")
 
+// Two fp32 at once: acc += r * s, both halves.  (Volatile: the operands come from tensor memory, whose loads are complete
+// only after tmem_wait_ld, an ordering the compiler cannot see in the registers.)
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ void fma_f32x2(uint64_t& acc, uint32_t r_lo, uint32_t r_hi, uint64_t s) {
+    asm volatile("{\n\t.reg .b64 r;\n\tmov.b64 r, {%1, %2};\n\tfma.rn.f32x2 %0, r, %3, %0;\n\t}" : "+l"(acc) : "r"(r_lo), "r"(r_hi), "l"(s));
+}
+
 // ---- CTA pairs (cluster of two, cta_group::2) -------------------------------------------
 // One MMA spans both CTAs' tensor memory (M = 256: 128 rows each) and reads the 128-row operand and half
 // of the other operand from each CTA's shared memory, at the same offsets in both.
@@ -218,6 +234,11 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// The same for a hand-over of tensor memory alone, which tcgen05.fence orders: the release at cluster scope above costs a
+// memory barrier that waits for everything the thread has in flight.
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // All threads of both CTAs.
 __device__ __forceinline__ void cluster_sync() {
@@ -242,6 +263,14 @@ __device__ __forceinline__ void umma_bf16_ss_pair(uint32_t d_tmem, uint64_t a_de
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_f8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
