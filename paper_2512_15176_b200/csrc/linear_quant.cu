@@ -360,15 +360,15 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
 #pragma unroll
                     for (int kk = 0; kk < GROUP / 32; ++kk)
                         umma_f8_ss_pair(tmem_base + (uint32_t)(b * BNP), xd + (uint64_t)(kk * 2), wd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
-                    umma_commit_pair(empty(s), 3);
                     umma_commit_pair(tfull(b), 3);
+                    umma_commit_pair(empty(s), 3);
                 }
             }
         }
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;      // TMEM lanes; which half of the columns
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * C::HALF);
-        const uint32_t lead_tempty[2] = {map_to_cta(tempty(0), 0), map_to_cta(tempty(1), 0)};
+        const uint32_t lead_tempty = map_to_cta(tempty(0), 0);
         int it = 0;
         bool alive = true;
         for (int t = cluster; t < tiles && alive; t += n_clusters) {
@@ -396,14 +396,17 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
 #pragma unroll
                 for (int c = 0; c < C::HALF; c += 16) {
                     tmem_wait_ld();
-                    if (c + 16 < C::HALF) TMEM_LD_X16(t_lane + (uint32_t)(b * BNP + c + 16), r[(c / 16 + 1) & 1]);
+                    if (c + 16 < C::HALF) {
+                        TMEM_LD_X16(t_lane + (uint32_t)(b * BNP + c + 16), r[(c / 16 + 1) & 1]);
+                    } else {                                       // the accumulator has been read
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_peer(lead_tempty + 8u * b);
+                    }
                     const uint32_t(&v)[16] = r[(c / 16) & 1];
 #pragma unroll
                     for (int j = 0; j < 16; j += 2) fma_f32x2(acc[(c + j) / 2], v[j], v[j + 1], s2);
                 }
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_peer(lead_tempty[b]);
             }
             if (!alive || m >= a.M) continue;
             __nv_bfloat16* dst = a.y + (size_t)m * a.N + n0;
