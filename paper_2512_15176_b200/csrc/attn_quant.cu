@@ -20,7 +20,7 @@
 
 namespace attnq {
 
-constexpr int ROWS = 16;                       // query rows of a tile
+constexpr int ROWS = ROWS_SMALL;
 constexpr int WARPS = 4;
 constexpr float P_BIAS = 12.f;                 // probabilities are held as 2^12 p
 
@@ -447,8 +447,12 @@ using namespace attnq;
 
 extern "C" size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, int Hkv, int D, int max_seq_len) {
     if (B <= 0 || k <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || D <= 0 || max_seq_len < 0) return 0;
+    // room for whichever kernel the call ends up using
     const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
-    return pl.chunks == 1 ? 16 : (size_t)pl.chunks * B * k * Hq * (D + 1) * sizeof(float);
+    const size_t small = pl.chunks == 1 ? 16 : (size_t)pl.chunks * B * k * Hq * (D + 1) * sizeof(float);
+    if (!umma_supported(D, k, Hq / Hkv, 0, 1.f)) return small;
+    const size_t large = umma_workspace_bytes(B, k, Hq, Hkv, max_seq_len);
+    return large > small ? large : small;
 }
 
 extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const void* q, const void* k_blk, const void* v_blk, void* out,
@@ -471,7 +475,7 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     DEER_CHECK_ARG(workspace && workspace_bytes >= need, DEER_ERR_WORKSPACE,
                    "deer_block_attn_quant: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
     const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
-    DEER_CHECK_ARG((long long)Hkv * pl.row_tiles <= 65535, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: too many heads");
+    DEER_CHECK_ARG((long long)Hkv * pl.row_tiles <= 65535 && Hq <= 65535, DEER_ERR_UNSUPPORTED, "deer_block_attn_quant: too many heads");
     Params p = {};
     p.kv = kv->d;
     p.kq = kv->q;
@@ -494,6 +498,7 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     p.row_tiles = pl.row_tiles;
     p.chunk_pages = pl.chunk_pages;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (umma_supported(D, k, p.G, (long long)kv->d.num_pages * Hkv * PAGE, scale)) return launch_umma(p, workspace, st);
     const dim3 grid((unsigned)pl.chunks, (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
     DEER_CUDA(launch_pdl(D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
     if (pl.chunks > 1)

@@ -27,6 +27,13 @@ struct Params {
     int chunk_pages;           // full pages per context chunk
 };
 
+constexpr int ROWS_SMALL = 16;   // query rows of a warp-level tile
+
+// tcgen05 variant (attn_quant_umma.cu).
+bool umma_supported(int D, int k, int G, long long pool_rows, float scale);
+size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len);
+int launch_umma(const Params& p, void* workspace, cudaStream_t st);
+
 #ifdef __CUDACC__
 // Sequence of index b in the call: its cache slot and committed length; false (and the status word) if it cannot be used.
 __device__ __forceinline__ bool sequence_of(const Params& p, int b, int* s, int* n, bool report) {

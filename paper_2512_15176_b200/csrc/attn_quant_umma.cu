@@ -1,0 +1,763 @@
+// Block attention against an 8-bit paged cache on the 5th-generation tensor cores (head_dim 128).
+//
+// The work is split as in the bf16 kernel: a unit is one (sequence, KV head, row tile of 128 query rows), its keys come in
+// tiles of 64 -- four full pages, and one last tile for what is bf16, the tail rows and the block's own -- and the tiles
+// of all units, laid end to end, are cut into one equal share per thread block (attn_share.cuh).
+//
+// Both products run on 8-bit operands as the cache holds them; nothing of the KV stream is converted:
+//   S = Q K^T   Q is split into two e4m3 terms per row, q = 2^x (q1 + q2): a bf16 value has 8 significant bits, e4m3 has 4,
+//               so the two terms are exact except for elements below 2^-17 of their row's largest (absolute error 2^-18 of
+//               that).  Two e4m3 MMAs at twice the bf16 rate cost what one bf16 MMA would, and K needs half the bytes.
+//   O += P V    P is split into three e5m2 terms, the leading 9 bits of its fp16 form (an e5m2 value is an fp16 one with
+//               the low byte cut off): three bits each, and fp16's range, which the weights of a long flat context need
+//               (e4m3's two terms would lose every key 2^-17 below the row's largest).
+// A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  The bf16 tile is
+// split into two e4m3 terms per token, scaled by a power of two of its own, and meets the same operand layouts.
+//
+// Exponentials are taken against a reference per row, chosen in the first tile (the row's maximum there, held as 2^11, and
+// the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
+//
+// Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
+// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 TMA producer, 1 / 2 issuers
+// of S for group 0 / 1, 3 issuer of O, 4..7 and 8..11 softmax, 12..15 splitters (queries of the next segment, bf16 tiles).
+// All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
+
+#include <cuda_fp16.h>
+
+#include "attn_quant.cuh"
+#include "attn_share.cuh"
+#include "sm100.cuh"
+
+namespace attnq {
+namespace umma {
+
+using namespace sm100;
+using attn::AttnParams;
+using attn::MAX_SEGS;
+using attn::Seg;
+
+constexpr int HD = 128;
+constexpr int TILE = 64;                       // keys per tile
+constexpr int PAGES = TILE / PAGE;
+constexpr int T_BYTES = TILE * HD;             // one 8-bit operand tile, 8 KB
+constexpr int SLOT_BYTES = 2 * T_BYTES;        // K then V
+constexpr int NSLOT = 6;
+constexpr int Q_BYTES = 2 * 128 * HD;          // both terms, 32 KB; two of them: the next segment's queries are split early
+constexpr int BT_BYTES = 4 * T_BYTES;          // bf16 tile: K terms, V terms
+constexpr int BT_COLS = 48;                    // 15 tail rows and 32 block rows at most
+constexpr int THREADS = 512;
+constexpr int TMEM_COLS = 512;                 // S [g * 64, +64)  P [128 + g * 48, +48)  O [256 + g * 128, +128)
+constexpr int P_COL = 128, P_COLS = 48, O_COL = 256;
+constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^28 above e5m2's last bit
+
+// mbarrier indices
+constexpr int BAR_Q_FULL = 0;                  // [2]  count 4: the splitter warps
+constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 2: both S issuers
+constexpr int BAR_BT_FULL = 4;                 // count 4
+constexpr int BAR_BT_EMPTY = 5;                // count 1: the issuer of O
+constexpr int BAR_S_FULL = 6;                  // [2]
+constexpr int BAR_S_FREE = 8;                  // [2]  count 4: the group's warps
+constexpr int BAR_P_READY = 10;                // [2]  count 4
+constexpr int BAR_O_DONE = 12;                 // [2]
+constexpr int BAR_MEET = 14;                   // [4]  count 2: the two warps of a lane quarter
+constexpr int BAR_PART = 18;                   // [4]  count 2
+constexpr int BAR_K_FULL = 22;                 // [NSLOT]
+constexpr int BAR_V_FULL = BAR_K_FULL + NSLOT;
+constexpr int BAR_SLOT_EMPTY = BAR_V_FULL + NSLOT;
+constexpr int N_BARS = BAR_SLOT_EMPTY + NSLOT;
+
+struct Shared {                                // behind the operand buffers
+    uint64_t bars[N_BARS];
+    float q_factor[2][128];                    // per query row: scale * log2(e) * the power of two taken out of it
+    float bt_k[BT_COLS], bt_v[BT_COLS];        // powers of two taken out of the bf16 tile's tokens
+    float meet[2][3][128];                     // per group and row: reference, sum, V reference
+    uint32_t tmem_slot;
+    int abort_flag;
+    int n_seg;
+    int bt_bad[2];                             // bf16 tile number x has a NaN or an infinity among its values: [x & 1] == x + 1
+    long long cursor;
+    Seg segs[MAX_SEGS];
+};
+constexpr int SMEM_BYTES = 2 * Q_BYTES + NSLOT * SLOT_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
+
+struct QParams {
+    AttnParams a;
+    deer_kv_quant_desc kq;
+};
+
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Tiles of sequence b: its full pages four at a time and the bf16 tile; 0 if the sequence cannot be used.
+__device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out, int* s_out) {
+    const int s = p.seq_ids[b];
+    int n = -1;
+    if (s >= 0 && s < p.kv.max_seqs) n = p.kv.seq_len[s];
+    if (n_out) *n_out = n;
+    if (s_out) *s_out = s;
+    if (n < 0 || n > p.max_seq_len) return 0;
+    return (n / PAGE + PAGES - 1) / PAGES + 1;
+}
+
+// Power of two that brings a group's largest magnitude to [128, 256) (nothing but zeros: 1).
+__device__ __forceinline__ float to_256(uint32_t amax_bits) {
+    const int f = amax_bits ? 127 + 7 + 127 - (int)(amax_bits >> 23) : 127;
+    return __uint_as_float((uint32_t)min(max(f, 1), 254) << 23);
+}
+// Sixteen values times `up`, as two terms of e4m3 codes (a row with a NaN or an infinity: NaN codes).
+__device__ __forceinline__ void split16(const float (&v)[16], float up, bool bad, uint4* t1, uint4* t2) {
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t lo[2], hi[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float x0 = v[j * 4 + h * 2] * up, x1 = v[j * 4 + h * 2 + 1] * up;
+            lo[h] = __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw back = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)lo[h], __NV_E4M3);
+            const float2 y = __half22float2(__half2(back));
+            hi[h] = __nv_cvt_float2_to_fp8x2(make_float2(x0 - y.x, x1 - y.y), __NV_SATFINITE, __NV_E4M3);
+        }
+        a[j] = bad ? 0x7f7f7f7fu : (lo[0] | (lo[1] << 16));
+        b[j] = bad ? 0u : (hi[0] | (hi[1] << 16));
+    }
+    *t1 = make_uint4(a[0], a[1], a[2], a[3]);
+    *t2 = make_uint4(b[0], b[1], b[2], b[3]);
+}
+
+__global__ void __launch_bounds__(THREADS, 1)
+attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const QParams qp) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    unsigned char* sQ = smem;                                  // [2 buffers][2 terms][128 rows][128 B]
+    unsigned char* ring = sQ + 2 * Q_BYTES;                    // [NSLOT][K, V][64 tokens][128 B]
+    unsigned char* bt = ring + NSLOT * SLOT_BYTES;             // [K term 1, K term 2, V term 1, V term 2][64][128 B]
+    Shared& sh = *reinterpret_cast<Shared*>(bt + BT_BYTES);
+    volatile int* abort_flag = &sh.abort_flag;
+    const AttnParams& p = qp.a;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int Hkv = p.kv.n_kv_heads;
+    const int HR = Hkv * p.row_tiles;
+    const int j = blockIdx.x;
+    const int jg = j / p.row_tiles, rt = j % p.row_tiles;      // group of blocks that walk the same share; my row tile
+    const int ncg = p.nc / p.row_tiles;
+
+    const uint32_t bar_base = smem_u32(sh.bars);
+    auto bar = [&](int idx) { return bar_base + 8u * idx; };
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(BAR_Q_FULL + i), 4);
+            mbar_init(bar(BAR_Q_EMPTY + i), 2);
+            mbar_init(bar(BAR_S_FULL + i), 1);
+            mbar_init(bar(BAR_S_FREE + i), 4);
+            mbar_init(bar(BAR_P_READY + i), 4);
+            mbar_init(bar(BAR_O_DONE + i), 1);
+        }
+        mbar_init(bar(BAR_BT_FULL), 4);
+        mbar_init(bar(BAR_BT_EMPTY), 1);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(bar(BAR_MEET + i), 2);
+            mbar_init(bar(BAR_PART + i), 2);
+        }
+        for (int i = 0; i < NSLOT; ++i) {
+            mbar_init(bar(BAR_K_FULL + i), 1);
+            mbar_init(bar(BAR_V_FULL + i), 1);
+            mbar_init(bar(BAR_SLOT_EMPTY + i), 1);
+        }
+        sh.abort_flag = 0;
+        sh.bt_bad[0] = sh.bt_bad[1] = 0;
+        mbar_init_fence();
+        prefetch_tensormap(&tm_k);
+        prefetch_tensormap(&tm_v);
+    }
+    pdl_trigger();
+    pdl_wait();
+
+    // ---- this block's share of the flattened tile list ----
+    long long T = 0;
+    for (int b = lane; b < p.B; b += 32) {
+        const int tiles = seq_tiles(p, b, nullptr, nullptr);
+        T += tiles;
+        // a sequence that cannot be used has no tiles, so no block will write its units' merge entries: do it here
+        if (tiles == 0 && j == 0 && warp == 0)
+            for (int hr = 0; hr < HR; ++hr) p.unit_parts[(size_t)b * HR + hr] = make_int2(-1, -1);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) T += __shfl_xor_sync(0xffffffffu, T, o);
+    T *= Hkv;
+    const long long share_lo = attn::share_begin(T, jg, ncg), share_hi = attn::share_begin(T, jg + 1, ncg);
+    if (j == 0 && tid == 0) *p.total_tiles = T;
+    if (share_hi <= share_lo) return;
+
+    if (warp == 1) tmem_alloc(smem_u32(&sh.tmem_slot), TMEM_COLS);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem_base = sh.tmem_slot;
+    const uint32_t q_addr = smem_u32(sQ), ring_addr = smem_u32(ring), bt_addr = smem_u32(bt);
+
+    // Counters that run across segments and rounds; every role advances its own copy identically.
+    int it = 0;          // tiles so far: group it & 1, that group's phase it >> 1
+    int rs = 0;          // page tiles so far: ring slot rs % NSLOT
+    int nb = 0;          // bf16 tiles so far
+    int sg = 0;          // segments so far: Q buffer sg & 1
+    long long cursor = share_lo;
+    while (cursor < share_hi) {
+        if (warp == 0) {
+            long long next;
+            const int ns = attn::build_segments(p, Hkv, rt, cursor, share_hi, sh.segs, &next, lane,
+                                                [&](int b, int* n, int* s) { return seq_tiles(p, b, n, s); });
+            if (lane == 0) {
+                sh.n_seg = ns;
+                sh.cursor = next;
+            }
+        }
+        __syncthreads();
+        const int n_seg = sh.n_seg;
+        cursor = sh.cursor;
+
+        if (warp == 0) {
+            // ---------------- TMA producer: lanes 0..3 the pages of K, 4..7 those of V ----------------
+            const int pj = lane & 3, is_v = (lane >> 2) & 1;
+            const int no_row = p.kv.num_pages * Hkv * PAGE;    // beyond the pool: reads as zero
+            bool ok = true;
+            for (int si = 0; si < n_seg && ok; ++si) {
+                const Seg g = sh.segs[si];
+                const int kvh = g.hr / p.row_tiles, full = g.n / PAGE;
+                const int last_tile = (full + PAGES - 1) / PAGES;
+                const int32_t* pt_row = p.kv.page_table + (size_t)g.s * p.kv.max_pages;
+                auto page_of = [&](int t) -> int {
+                    const int lp = t * PAGES + pj;
+                    if (lane >= 8 || t >= g.t_b || lp >= full) return -2;          // nothing there
+                    return lp < p.kv.max_pages ? pt_row[lp] : -1;
+                };
+                int pg_cur = page_of(g.t_a), pg_next = page_of(g.t_a + 1);
+                for (int t = g.t_a; t < g.t_b && t < last_tile; ++t, ++rs) {
+                    const int sl = rs % NSLOT;
+                    int pg = pg_cur;
+                    pg_cur = pg_next;
+                    pg_next = page_of(t + 2);
+                    int oks = 1;
+                    if (lane == 0) oks = mbar_wait(bar(BAR_SLOT_EMPTY + sl), ((uint32_t)(rs / NSLOT) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                    if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
+                    if (lane == 0) {
+                        mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);
+                        mbar_expect_tx(bar(BAR_V_FULL + sl), T_BYTES);
+                    }
+                    __syncwarp();
+                    if (lane < 8) {
+                        if (pg != -2 && (pg < 0 || pg >= p.kv.num_pages)) {
+                            deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
+                            pg = -2;
+                        }
+                        tma_load_2d(ring_addr + sl * SLOT_BYTES + is_v * T_BYTES + pj * PAGE * HD, is_v ? &tm_v : &tm_k, 0,
+                                    pg == -2 ? no_row : (pg * Hkv + kvh) * PAGE, bar((is_v ? BAR_V_FULL : BAR_K_FULL) + sl));
+                    }
+                }
+            }
+        } else if (warp <= 2) {
+            // ---------------- issuers of S: warp 1 for group 0, warp 2 for group 1 ----------------
+            if (lane == 0) {
+                const int grp = warp - 1;
+                const uint32_t idesc = make_idesc_e4m3(TILE);
+                const uint32_t d_tmem = tmem_base + (uint32_t)(grp * TILE);
+                bool ok = true;
+                for (int si = 0; si < n_seg && ok; ++si, ++sg) {
+                    const Seg g = sh.segs[si];
+                    const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                    const int qb = sg & 1;
+                    if (!mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
+                    const uint64_t qd = smem_desc_sw128_kmajor(q_addr + qb * Q_BYTES);
+                    for (int t = g.t_a; t < g.t_b; ++t, ++it) {
+                        const bool blk = t == last_tile;
+                        if ((it & 1) == grp) {
+                            if (!mbar_wait(bar(BAR_S_FREE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                            if (!blk) {
+                                const int sl = rs % NSLOT;
+                                if (!mbar_wait(bar(BAR_K_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
+                                tcgen05_fence_after();
+                                const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * SLOT_BYTES);
+#pragma unroll
+                                for (int kk = 0; kk < 8; ++kk)             // four steps of 32 dims for each term of Q
+                                    umma_f8_ss(d_tmem, qd + (uint64_t)(((kk >> 2) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
+                                               kd + (uint64_t)((kk & 3) * 2), idesc, kk != 0 ? 1u : 0u);
+                            } else {
+                                if (!mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag)) { ok = false; break; }
+                                tcgen05_fence_after();
+                                const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
+#pragma unroll
+                                for (int kk = 0; kk < 16; ++kk)            // and for each term of K
+                                    umma_f8_ss(d_tmem, qd + (uint64_t)((((kk >> 2) & 1) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
+                                               kd + (uint64_t)(((kk >> 3) * T_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0 ? 1u : 0u);
+                            }
+                            umma_commit(bar(BAR_S_FULL + grp));
+                        }
+                        if (blk) ++nb;
+                        else ++rs;
+                    }
+                    if (ok) umma_commit(bar(BAR_Q_EMPTY + qb));
+                }
+            }
+        } else if (warp == 3) {
+            // ---------------- issuer of O += P V, both groups ----------------
+            if (lane == 0) {
+                const uint32_t idesc = make_idesc_e5m2_e4m3_mn(HD);
+                bool ok = true;
+                for (int si = 0; si < n_seg && ok; ++si) {
+                    const Seg g = sh.segs[si];
+                    const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                    for (int t = g.t_a; t < g.t_b; ++t, ++it) {
+                        const int grp = it & 1;
+                        const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(P_COL + grp * P_COLS);
+                        const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
+                        if (!mbar_wait(bar(BAR_P_READY + grp), (uint32_t)(it >> 1) & 1u, abort_flag)) { ok = false; break; }
+                        if (t != last_tile) {
+                            const int sl = rs % NSLOT;
+                            if (!mbar_wait(bar(BAR_V_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
+                            tcgen05_fence_after();
+                            // 32 tokens per MMA: four groups of eight, 1 KB apart; term x of P in columns x * 16 ..
+                            const uint64_t vd = smem_desc_sw128(ring_addr + sl * SLOT_BYTES + T_BYTES, 1024, 1024);
+#pragma unroll
+                            for (int kk = 0; kk < 6; ++kk)
+                                umma_f8_ts(o_tmem, p_tmem + (uint32_t)((kk >> 1) * 16 + (kk & 1) * 8), vd + (uint64_t)(((kk & 1) * 4096) >> 4), idesc,
+                                           kk != 0 ? 1u : keep);
+                            umma_commit(bar(BAR_SLOT_EMPTY + sl));         // S of this tile was complete before its softmax
+                            ++rs;
+                        } else {
+                            tcgen05_fence_after();                         // (the tile was full before its S)
+                            const uint64_t vd = smem_desc_sw128(bt_addr + 2 * T_BYTES, 1024, 1024);
+#pragma unroll
+                            for (int kk = 0; kk < 12; ++kk)
+                                umma_f8_ts(o_tmem, p_tmem + (uint32_t)(((kk >> 1) % 3) * 16 + (kk & 1) * 8),
+                                           vd + (uint64_t)(((kk / 6) * T_BYTES + (kk & 1) * 4096) >> 4), idesc, kk != 0 ? 1u : keep);
+                            umma_commit(bar(BAR_BT_EMPTY));
+                        }
+                        umma_commit(bar(BAR_O_DONE + grp));
+                    }
+                }
+            }
+        } else if (warp >= 12) {
+            // ---------------- splitters ----------------
+            const int st = tid - 384;                                      // 0..127
+            const int c16 = st & 7;                                        // 16-dim piece of a row
+            bool ok = true;
+            for (int si = 0; si < n_seg && ok; ++si, ++sg) {
+                const Seg g = sh.segs[si];
+                const int kvh = g.hr / p.row_tiles, last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                const int i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
+                const int qb = sg & 1;
+                ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+#pragma unroll 2
+                for (int r = st >> 3; r < 128; r += 16) {
+                    float v[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] = 0.f;
+                    if (r < rows)
+                        quant::load_bf16x16(p.q + ((size_t)(g.b * p.k + i0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * HD + c16 * 16, v);
+                    const uint32_t m = quant::max8(quant::amax16(v));
+                    const float up = to_256(m);
+                    uint4 t1, t2;
+                    split16(v, up, m >= 0x7f800000u, &t1, &t2);
+                    unsigned char* dst = sQ + qb * Q_BYTES + r * HD + ((c16 ^ (r & 7)) << 4);
+                    *reinterpret_cast<uint4*>(dst) = t1;
+                    *reinterpret_cast<uint4*>(dst + Q_BYTES / 2) = t2;
+                    if (c16 == 0) sh.q_factor[qb][r] = p.scale_log2 / up;
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_Q_FULL + qb));
+                if (g.t_b != last_tile + 1) continue;
+                // the bf16 tile: tail rows, then block rows
+                ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                uint32_t present, decoded;
+                attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
+                const int n_tail = g.n % PAGE;
+                const size_t tail0 = (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (g.n / PAGE % 3) * PAGE) * HD;
+                int bad_v = 0;
+#pragma unroll 2
+                for (int x = st >> 3; x < 2 * TILE; x += 16) {
+                    const int tok = x & (TILE - 1), is_v = x / TILE, jb = tok - n_tail;
+                    float v[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] = 0.f;
+                    if (tok < n_tail)
+                        quant::load_bf16x16(static_cast<const __nv_bfloat16*>(is_v ? qp.kq.v_tail : qp.kq.k_tail) + tail0 + (size_t)tok * HD + c16 * 16, v);
+                    else if (jb < p.k && ((present >> jb) & 1u))
+                        quant::load_bf16x16((is_v ? p.v_blk : p.k_blk) + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16, v);
+                    uint32_t m = quant::amax16(v);
+                    if (is_v && m >= 0x7f800000u) {                        // added to the rows that see it at the end
+                        bad_v = 1;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (quant::mag_bits(v[e]) >= 0x7f800000u) v[e] = 0.f;
+                        m = quant::amax16(v);
+                    }
+                    m = quant::max8(m);
+                    const bool bad = m >= 0x7f800000u;
+                    const float up = to_256(m);
+                    uint4 t1, t2;
+                    split16(v, up, false, &t1, &t2);
+                    unsigned char* dst = bt + is_v * 2 * T_BYTES + tok * HD + ((c16 ^ (tok & 7)) << 4);
+                    *reinterpret_cast<uint4*>(dst) = t1;
+                    *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
+                    if (c16 == 0 && tok < BT_COLS) (is_v ? sh.bt_v : sh.bt_k)[tok] = bad ? __uint_as_float(0x7fc00000u) : 1.f / up;
+                }
+                if (__any_sync(0xffffffffu, bad_v) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_BT_FULL));
+                ++nb;
+            }
+        } else {
+            // ---------------- softmax: one query row per thread, the group's tiles ----------------
+            const int grp = (warp - 4) >> 2, quarter = warp & 3;
+            const int row = quarter * 32 + lane;
+            const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+            const uint32_t s_tmem = t_lane + (uint32_t)(grp * TILE), p_tmem = t_lane + (uint32_t)(P_COL + grp * P_COLS);
+            bool alive = true;
+            for (int si = 0; si < n_seg && alive; ++si, ++sg) {
+                const Seg g = sh.segs[si];
+                const int kvh = g.hr / p.row_tiles, full = g.n / PAGE, last_tile = (full + PAGES - 1) / PAGES, n_tail = g.n % PAGE;
+                const int i0 = rt * p.ipt, ni = min(p.ipt, p.k - i0);
+                const int i_blk = i0 + row / p.G;
+                const bool row_valid = row < ni * p.G;
+                uint32_t present, decoded;
+                attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
+                const int state = (p.row_state && row_valid) ? p.row_state[(size_t)g.b * p.k + i_blk] : 1;
+                // columns of the bf16 tile that this row sees
+                const uint64_t see = ((uint64_t)(attn::visible_rows(p.mask, i_blk, state, present, decoded) & present) << n_tail) | ((1ull << n_tail) - 1ull);
+                const int32_t* pt_row = p.kv.page_table + (size_t)g.s * p.kv.max_pages;
+
+                // Scales of the group's tiles, fetched ahead: lane l < 4 has the K scale of page l of a tile, lane 4 + l its V
+                // scale; the page id is a tile further ahead.
+                auto page_of = [&](int t) -> int {
+                    const int lp = t * PAGES + (lane & 3);
+                    if (lane >= 8 || t >= g.t_b || lp >= full || lp >= p.kv.max_pages) return -1;
+                    const int pg = pt_row[lp];
+                    return pg < p.kv.num_pages ? pg : -1;
+                };
+                auto scale_of_page = [&](int pg) -> float {
+                    return pg < 0 ? 1.f : __ldcg((lane < 4 ? qp.kq.k_scale : qp.kq.v_scale) + (size_t)pg * Hkv + kvh);
+                };
+                const int t0 = g.t_a + ((it ^ grp) & 1);                   // the group's first tile
+                float sc_next = scale_of_page(page_of(t0));
+                int pg_next = page_of(t0 + 2);
+
+                float m_ref = 0.f, v_ref = 1.f, i_ref = 1.f, l_run = 0.f;
+                bool first = true;
+                const int qb = sg & 1;
+                {
+                    const bool got = mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
+                }
+                const float f_row = sh.q_factor[qb][row];
+                for (int t = g.t_a; t < g.t_b; ++t, ++it) {
+                    if ((it & 1) != grp) continue;
+                    const uint32_t ph = (uint32_t)(it >> 1) & 1u;
+                    const float sc_cur = sc_next;
+                    sc_next = scale_of_page(pg_next);
+                    pg_next = page_of(t + 4);
+                    const bool is_bt = t == last_tile;
+                    const int n_pages = is_bt ? 0 : min(PAGES, full - t * PAGES);
+
+                    const bool got = mbar_wait(bar(BAR_S_FULL + grp), ph, abort_flag);
+                    if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
+                    tcgen05_fence_after();
+                    uint32_t sr[TILE];
+                    TMEM_LD_X32(s_tmem, (sr));
+                    TMEM_LD_X32(s_tmem + 32, (sr + 32));
+                    tmem_wait_ld();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(BAR_S_FREE + grp));
+
+                    // score of column c in the log2 domain = sr[c] * ka, ka > 0 (the bf16 tile: scaled and masked here, column
+                    // by column); V scale va.  A page that does not exist (zeros in shared memory) gets the weight 2^-inf.
+                    float ka[PAGES], va[PAGES], m_t = -INFINITY, v_t = 0.f;
+                    if (is_bt) {
+                        const bool bf = mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag);      // (for bt_k / bt_v)
+                        if (!__all_sync(0xffffffffu, bf)) { alive = false; break; }
+#pragma unroll
+                        for (int c = 0; c < TILE; ++c)
+                            sr[c] = (c < BT_COLS && ((see >> c) & 1u)) ? __float_as_uint(__uint_as_float(sr[c]) * (sh.bt_k[c] * f_row)) : 0xff800000u;
+                        for (int c = 0; c < BT_COLS; ++c) v_t = fmaxf(v_t, sh.bt_v[c]);
+#pragma unroll
+                        for (int x = 0; x < PAGES; ++x) {
+                            ka[x] = 1.f;
+                            va[x] = 0.f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < PAGES; ++x) {
+                            ka[x] = f_row * __shfl_sync(0xffffffffu, sc_cur, x);
+                            va[x] = __shfl_sync(0xffffffffu, sc_cur, 4 + x);
+                            if (x < n_pages) v_t = fmaxf(v_t, va[x]);
+                        }
+                    }
+#pragma unroll
+                    for (int x = 0; x < PAGES; ++x) {
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int c = 0; c < PAGE; c += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(sr[x * PAGE + c]), __uint_as_float(sr[x * PAGE + c + 1])));
+                        if (is_bt || x < n_pages) m_t = fmaxf(m_t, mx * ka[x]);
+                    }
+                    if (!(fabsf(m_t) < INFINITY)) m_t = first ? 0.f : m_ref;       // nothing visible here, or not finite
+                    if (!(v_t > 0.f && v_t < INFINITY)) v_t = first ? 1.f : v_ref;
+                    // The group's first tile sets the references.  A later one whose weights would pass 2^15 (2^40 without their V
+                    // scale) raises them: O and l shrink in place.
+                    const float p_t = first ? 0.f : ex2_approx(m_t - m_ref + BIAS);
+                    const bool raise = !first && (p_t * (v_t * i_ref) >= 32768.f || p_t >= 1.0995116e12f);
+                    const bool od = it < 2 || mbar_wait(bar(BAR_O_DONE + grp), ph ^ 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, od)) { alive = false; break; }
+                    // (phase (it >> 1) - 1 of o_done: the group's previous tile is in O, and its P may be overwritten)
+                    if (first) {
+                        m_ref = m_t;
+                        v_ref = v_t;
+                        i_ref = 1.f / v_ref;
+                    } else if (__any_sync(0xffffffffu, raise)) {
+                        const float m_new = fmaxf(m_ref, m_t), v_new = fmaxf(v_ref, v_t);
+                        const float al = ex2_approx(m_ref - m_new), ao = al * (v_ref / v_new);
+                        tcgen05_fence_after();
+#pragma unroll
+                        for (int cc = 0; cc < HD / 16; ++cc) {
+                            uint32_t o[16];
+                            TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ao);
+                            TMEM_ST_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
+                        }
+                        tmem_wait_st();
+                        l_run *= al;
+                        m_ref = m_new;
+                        v_ref = v_new;
+                        i_ref = 1.f / v_ref;
+                    }
+                    first = false;
+                    // weights 2^(score - m_ref + 11); times V scale / v_ref in fp16; three e5m2 terms of that: the upper byte, the
+                    // upper byte of what is left, and what is left then, rounded
+                    float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t t1[16], t2[16], t3[16];
+#pragma unroll
+                    for (int w = 0; w < 16; ++w) {                         // four keys per word
+                        const int x = w >> 2;
+                        const float nm = (is_bt || x < n_pages) ? BIAS - m_ref : -INFINITY;
+                        uint32_t hi1[2], hi2[2], c3[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int c = 4 * w + 2 * e;
+                            const float p0 = ex2_approx(fmaf(__uint_as_float(sr[c]), ka[x], nm));
+                            const float p1 = ex2_approx(fmaf(__uint_as_float(sr[c + 1]), ka[x], nm));
+                            sum4[(2 * w + e) & 3] += p0 + p1;
+                            float w0 = va[x], w1 = va[x];
+                            if (is_bt) {
+                                w0 = c < BT_COLS ? sh.bt_v[c] : 0.f;
+                                w1 = c < BT_COLS ? sh.bt_v[c + 1] : 0.f;
+                            }
+                            const __half2 hw = __floats2half2_rn(p0 * (w0 * i_ref), p1 * (w1 * i_ref));
+                            hi1[e] = *reinterpret_cast<const uint32_t*>(&hw) & 0xff00ff00u;
+                            const __half2 r1 = __hsub2(hw, *reinterpret_cast<const __half2*>(&hi1[e]));
+                            hi2[e] = *reinterpret_cast<const uint32_t*>(&r1) & 0xff00ff00u;
+                            const __half2 r2 = __hsub2(r1, *reinterpret_cast<const __half2*>(&hi2[e]));
+                            c3[e] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(r2), __NV_SATFINITE, __NV_E5M2);
+                        }
+                        t1[w] = __byte_perm(hi1[0], hi1[1], 0x7531);
+                        t2[w] = __byte_perm(hi2[0], hi2[1], 0x7531);
+                        t3[w] = c3[0] | (c3[1] << 16);
+                    }
+                    l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+                    TMEM_ST_X16(p_tmem, t1);
+                    TMEM_ST_X16(p_tmem + 16, t2);
+                    TMEM_ST_X16(p_tmem + 32, t3);
+                    tmem_wait_st();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(BAR_P_READY + grp));
+                }
+                if (!alive) break;
+                if (g.t_b == last_tile + 1) ++nb;
+
+                // ---- the segment's result: the groups meet; each takes half of the columns of both accumulators ----
+                if (!first) {
+                    // the last tile of this group in the segment is tile number `last_it` of the block
+                    const int last_it = it - 1 - ((it - 1 - grp) & 1);
+                    const bool od = mbar_wait(bar(BAR_O_DONE + grp), (uint32_t)(last_it >> 1) & 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, od)) { alive = false; break; }
+                }
+                sh.meet[grp][0][row] = first ? -INFINITY : m_ref;
+                sh.meet[grp][1][row] = first ? 0.f : l_run;
+                sh.meet[grp][2][row] = v_ref;
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_MEET + quarter));
+                {
+                    const bool got = mbar_wait(bar(BAR_MEET + quarter), (uint32_t)sg & 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
+                }
+                tcgen05_fence_after();
+                const float m0 = sh.meet[0][0][row], m1 = sh.meet[1][0][row], l0 = sh.meet[0][1][row], l1 = sh.meet[1][1][row];
+                const float mx = fmaxf(m0, m1);                            // one of the groups had a tile
+                const float e0 = m0 == -INFINITY ? 0.f : ex2_approx(m0 - mx), e1 = m1 == -INFINITY ? 0.f : ex2_approx(m1 - mx);
+                const float l = e0 * l0 + e1 * l1;
+                const bool gone = !row_valid || state < 0;                 // no query row, or an absent one
+                const float inv = l != 0.f ? 1.f / l : 0.f;
+                const float w0 = e0 * sh.meet[0][2][row] * inv, w1 = e1 * sh.meet[1][2][row] * inv;
+                const bool has0 = m0 != -INFINITY, has1 = m1 != -INFINITY;
+                const bool bad_v = g.t_b == last_tile + 1 && *(volatile int*)&sh.bt_bad[(nb - 1) & 1] == nb;
+                const int hq = kvh * p.G + row % p.G;
+                const size_t unit = (size_t)g.b * HR + g.hr;
+                const bool whole = g.t_a == 0 && g.t_b == last_tile + 1;
+                const size_t slot = ((size_t)g.b * Hkv + kvh + jg) * p.row_tiles + rt;
+#pragma unroll
+                for (int cc = 0; cc < 4; ++cc) {
+                    const int col = grp * 64 + cc * 16;
+                    uint32_t a[16], b[16];
+                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + col), a);
+                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + HD + col), b);
+                    tmem_wait_ld();
+                    float v[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        v[c] = has0 ? __uint_as_float(a[c]) * w0 : 0.f;
+                        if (has1) v[c] = fmaf(__uint_as_float(b[c]), w1, v[c]);
+                    }
+                    if (bad_v) {                                           // what the bf16 tile's values could not carry
+                        for (int x = 0; x < n_tail + p.k; ++x) {
+                            if (!((see >> x) & 1u)) continue;
+                            const __nv_bfloat16* src = x < n_tail
+                                ? static_cast<const __nv_bfloat16*>(qp.kq.v_tail) + (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (full % 3) * PAGE + x) * HD
+                                : p.v_blk + ((size_t)(g.b * p.k + x - n_tail) * Hkv + kvh) * HD;
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) {
+                                const float f = __bfloat162float(src[col + c]);
+                                if (quant::mag_bits(f) >= 0x7f800000u) v[c] += f;
+                            }
+                        }
+                    }
+                    if (gone) {
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) v[c] = 0.f;
+                    }
+                    if (row_valid && whole) {
+                        __nv_bfloat16* dst = p.out + ((size_t)(g.b * p.k + i_blk) * p.Hq + hq) * HD + col;
+#pragma unroll
+                        for (int c = 0; c < 16; c += 8)
+                            *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[c], v[c + 1]), pack_bf16(v[c + 2], v[c + 3]),
+                                                                            pack_bf16(v[c + 4], v[c + 5]), pack_bf16(v[c + 6], v[c + 7]));
+                    } else if (row_valid) {
+                        float* dst = p.part_o + (slot * 128 + row) * HD + col;
+#pragma unroll
+                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                    }
+                }
+                if (grp == 0) {
+                    if (whole) {
+                        if (row == 0) p.unit_parts[unit] = make_int2(-1, -1);       // nothing for the merge kernel to do
+                    } else {
+                        // a NaN sum must reach the output: the merge gives such a piece all the weight
+                        if (row_valid) p.part_lse[slot * 128 + row] = gone || l == 0.f ? -INFINITY : l != l ? 3.0e38f : mx + log2f(l) - BIAS;
+                        if (g.t_a == 0 && row == 0) {                      // tells the merge kernel which blocks share the unit
+                            const int tiles_u = last_tile + 1;
+                            const int j_lo = (int)(((g.u0 + 1) * ncg + T - 1) / T) - 1;
+                            const int j_hi = (int)(((g.u0 + tiles_u) * ncg + T - 1) / T) - 1;
+                            p.unit_parts[unit] = make_int2(j_lo, j_hi);
+                        }
+                    }
+                }
+                // both groups have read both accumulators before either goes on to overwrite its own
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_PART + quarter));
+                const bool parted = mbar_wait(bar(BAR_PART + quarter), (uint32_t)sg & 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, parted)) { alive = false; break; }
+            }
+        }
+        __syncthreads();                                                   // every role is done with this list
+        if (*abort_flag) break;
+    }
+
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) deer_report(p.kv.status, DEER_ERR_TIMEOUT);
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);                   // copies still in flight land before the memory goes away
+        __syncthreads();
+    }
+    if (warp == 1) {
+        __syncwarp();
+        tcgen05_fence_after();
+        tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+}
+
+// Thread blocks for a call: one per SM, fewer when the tiles would not give each of them a few.
+static int pick_blocks(int B, int Hkv, int row_tiles, int max_seq_len) {
+    const long long t_max = (long long)B * Hkv * ((max_seq_len / PAGE + PAGES - 1) / PAGES + 1);
+    long long groups = t_max / 4, most = deer_sm_count() / row_tiles;
+    if (groups > most) groups = most;
+    if (groups < 1) groups = 1;
+    return (int)groups * row_tiles;
+}
+
+}  // namespace umma
+
+// More query rows than a warp's tile of 16 hold share the KV stream here; fewer leave the 128 lanes idle while the
+// warp-level kernel reads the same bytes with less latency.
+bool umma_supported(int D, int k, int G, long long pool_rows, float scale) {
+    return D == umma::HD && G <= 128 && k * G > ROWS_SMALL && pool_rows < (1LL << 31) - 16 && scale > 0.f;
+}
+
+size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len) {
+    const int row_tiles = attn::umma_row_tiles(k, Hq / Hkv);
+    const size_t units = (size_t)B * Hkv * row_tiles, slots = units + umma::pick_blocks(B, Hkv, row_tiles, max_seq_len);
+    return slots * 128 * (umma::HD + 1) * sizeof(float) + units * sizeof(int2) + sizeof(long long);
+}
+
+int launch_umma(const Params& q, void* workspace, cudaStream_t st) {
+    using namespace umma;
+    QParams qp = {};
+    AttnParams& p = qp.a;
+    qp.kq = q.kq;
+    p.kv = q.kv;
+    p.seq_ids = q.seq_ids;
+    p.row_state = q.row_state;
+    p.q = q.q;
+    p.k_blk = q.k_blk;
+    p.v_blk = q.v_blk;
+    p.out = q.out;
+    p.B = q.B;
+    p.k = q.k;
+    p.Hq = q.Hq;
+    p.G = q.G;
+    p.R = q.G * q.k;
+    p.mask = q.mask;
+    p.scale_log2 = q.scale_log2;
+    p.max_seq_len = q.max_seq_len;
+    p.ipt = 128 / p.G;
+    p.row_tiles = attn::umma_row_tiles(p.k, p.G);
+    const int Hkv = p.kv.n_kv_heads;
+    p.nc = pick_blocks(p.B, Hkv, p.row_tiles, p.max_seq_len);
+    const size_t units = (size_t)p.B * Hkv * p.row_tiles, slots = units + p.nc;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = p.part_o + slots * 128 * HD;
+    p.total_tiles = reinterpret_cast<long long*>(p.part_lse + slots * 128);
+    p.unit_parts = reinterpret_cast<int2*>(p.total_tiles + 1);
+    CUtensorMap tm_k, tm_v;
+    const uint64_t dims[2] = {HD, (uint64_t)p.kv.num_pages * Hkv * PAGE}, str[1] = {HD};
+    const uint32_t box[2] = {HD, PAGE};
+    int rc = make_map_u8(&tm_k, p.kv.k_pool, 2, dims, str, box);
+    if (rc != DEER_OK) return rc;
+    rc = make_map_u8(&tm_v, p.kv.v_pool, 2, dims, str, box);
+    if (rc != DEER_OK) return rc;
+    DEER_CUDA(cudaFuncSetAttribute(attn_quant_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+    DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_k, tm_v, qp));
+    return attn::launch_umma_merge(p, st);
+}
+
+}  // namespace attnq

@@ -35,7 +35,7 @@
 // block's abort flag and the cache's status word, every role leaves its loops,
 // TMEM is freed and the kernel returns.
 
-#include "attn.cuh"
+#include "attn_share.cuh"
 #include "sm100.cuh"
 
 #ifdef DEER_TIMING_PROBES
@@ -65,7 +65,6 @@ constexpr int THREADS = 256;
 constexpr int TMEM_COLS = 512;                 // S0..S3 [0,256)  P0 [256,288)  P1 [288,320)  O [384,512)
 constexpr int P_COL = 256;
 constexpr int O_COL = 384;
-constexpr int MAX_SEGS = 48;                   // segments listed at a time; longer shares go in several rounds
 constexpr float RESCALE_SUM = 4294967296.f;    // 2^32: a row sum over one tile beyond this raises the running maximum
 // Slot layout.  A K (or V) tile of 64 tokens x 128 dims is 16 KB of 1 KB swizzle atoms (8 tokens x 64 dims).
 //   prefix tile: [page 0..3][token group 0..1][dim half 0..1][8 tokens][128 B] -- what one 5-D TMA box per page
@@ -85,13 +84,6 @@ constexpr int BAR_P_READY = BAR_S_FREE + NS;         // [2]   count 4
 constexpr int BAR_O_DONE = BAR_P_READY + 2;
 constexpr int N_BARS = BAR_O_DONE + 1;
 
-struct Seg {             // one (unit, block) piece
-    int b, hr;           // sequence index in the call; KV head * row_tiles + row tile
-    int t_a, t_b;        // tile range within the unit; tile ceil(n / 64) is the block rows' own K/V
-    int n, s;            // committed length and cache slot of the sequence
-    long long u0;        // flattened position of the unit's first tile
-};
-
 constexpr int SMEM_BYTES = 2 * Q_BYTES + NSLOT * SLOT_BYTES + 1024 /*alignment slack*/ + N_BARS * 8 + 32 + MAX_SEGS * (int)sizeof(Seg);
 
 __device__ __forceinline__ float ex2_approx(float x) {   // 2^x, one MUFU op; -inf gives 0
@@ -109,78 +101,6 @@ __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out,
     if (s_out) *s_out = s;
     if (n < 0 || n > p.max_seq_len) return 0;
     return (n + ATT_TILE - 1) / ATT_TILE + 1;
-}
-
-// Share of thread block j out of nc over T tiles: [share_begin(j), share_begin(j + 1)).
-__device__ __forceinline__ long long share_begin(long long T, int j, int nc) { return T * j / nc; }
-
-// Warp-collective: lists up to MAX_SEGS segments of the flattened tile range [cursor, end) into segs[], in order.
-// Returns their number; *cursor_out is where the next round starts (== end when the share is exhausted).
-__device__ int build_segments(const AttnParams& p, int HL, int rt, long long cursor, long long end, Seg* segs,
-                              long long* cursor_out, int lane) {
-    int n_seg = 0;
-    long long base = 0;                                   // flattened position of sequence b0's first tile
-    long long next_cursor = end;
-    bool cut = false;
-    for (int b0 = 0; b0 < p.B && base < end && n_seg < MAX_SEGS; b0 += 32) {
-        const int b = b0 + lane;
-        int n = 0, s = 0;
-        const int tiles = (b < p.B) ? seq_tiles(p, b, &n, &s) : 0;
-        if (b < p.B && tiles == 0) deer_report(p.kv.status, DEER_ERR_INVALID_ARG);
-        const long long span = (long long)tiles * HL;     // tiles this sequence contributes to the list
-        long long incl = span;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long t = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += t;
-        }
-        const long long my0 = base + incl - span, my1 = base + incl;
-        // units of my sequence that meet [cursor, end)
-        int hr_lo = 0, hr_hi = -1;
-        if (tiles > 0 && my1 > cursor && my0 < end) {
-            hr_lo = cursor > my0 ? (int)((cursor - my0) / tiles) : 0;
-            hr_hi = (int)(((end < my1 ? end : my1) - 1 - my0) / tiles);
-        }
-        const int cnt = hr_hi - hr_lo + 1 > 0 ? hr_hi - hr_lo + 1 : 0;
-        int cincl = cnt;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, cincl, o);
-            if (lane >= o) cincl += t;
-        }
-        const int off = n_seg + cincl - cnt;
-        for (int e = 0; e < cnt; ++e) {
-            const int idx = off + e;
-            const int hr = hr_lo + e;
-            const long long u0 = my0 + (long long)hr * tiles;
-            if (idx < MAX_SEGS) {
-                Seg sg;
-                sg.b = b;
-                sg.hr = hr * p.row_tiles + rt;
-                sg.t_a = cursor > u0 ? (int)(cursor - u0) : 0;
-                sg.t_b = end < u0 + tiles ? (int)(end - u0) : tiles;
-                sg.n = n;
-                sg.s = s;
-                sg.u0 = u0;
-                segs[idx] = sg;
-            } else if (idx == MAX_SEGS) {
-                next_cursor = u0;                          // the first segment that did not fit starts the next round
-            }
-        }
-        const int total = __shfl_sync(0xffffffffu, cincl, 31);
-        // at most one lane owns index MAX_SEGS; share its cursor
-        const unsigned who = __ballot_sync(0xffffffffu, off <= MAX_SEGS && MAX_SEGS < off + cnt);
-        if (who) next_cursor = __shfl_sync(0xffffffffu, next_cursor, __ffs(who) - 1);
-        n_seg = n_seg + total < MAX_SEGS ? n_seg + total : MAX_SEGS;
-        base += __shfl_sync(0xffffffffu, incl, 31);
-        if (who) {
-            cut = true;
-            break;
-        }
-    }
-    if (!cut && n_seg == MAX_SEGS) next_cursor = base < end ? base : end;   // the list filled up exactly at a sequence boundary
-    *cursor_out = next_cursor;
-    return n_seg;
 }
 
 __global__ void __launch_bounds__(THREADS, 1)
@@ -268,7 +188,8 @@ block_attn_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         // ---- list the next segments of the share (warp 0), then every role walks the list ----
         if (warp == 0) {
             long long next;
-            const int ns = build_segments(p, Hkv, rt_blk, cursor, share_hi, segs, &next, lane);
+            const int ns = build_segments(p, Hkv, rt_blk, cursor, share_hi, segs, &next, lane,
+                                          [&](int b, int* n, int* s) { return seq_tiles(p, b, n, s); });
             if (lane == 0) {
                 *sh_nseg = ns;
                 *sh_cursor = next;
@@ -832,6 +753,12 @@ int launch_umma(AttnParams p, cudaStream_t st) {
     }
     DEER_CUDA(cudaFuncSetAttribute(block_attn_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
     DEER_CUDA(launch_pdl(block_attn_umma_kernel, dim3(p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_kb, tm_vb, tm_kp, tm_vp, p));
+    return launch_umma_merge(p, st);
+}
+
+int launch_umma_merge(const AttnParams& p, cudaStream_t st) {
+    using namespace umma;
+    const int HR = p.kv.n_kv_heads * p.row_tiles;
     if ((long long)p.B * HR * 4 >= 2 * deer_sm_count())
         DEER_CUDA(launch_pdl(attn_umma_merge_kernel<4>, dim3((unsigned)(p.B * HR * 4)), dim3(256), 0, st, p));
     else

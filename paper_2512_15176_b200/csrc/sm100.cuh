@@ -151,6 +151,16 @@ __device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uin
         : "memory");
 }
 
+// The same with the 128-row operand in tensor memory (row = lane, four 8-bit values per column).
+__device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
 // Shared-memory operand descriptor, 128-byte swizzle, tile base 1024-byte aligned.
 //   K-major operand ([rows][64] bf16, the contraction index contiguous): sbo = bytes between 8-row groups.
 //   MN-major operand ([k][64] bf16, the row/column index contiguous): lbo = bytes between 64-element groups
@@ -174,6 +184,8 @@ __device__ __forceinline__ uint32_t make_idesc_bf16(int n, int b_mn_major) {
 
 // kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N = n, both operands K-major.
 __device__ __forceinline__ uint32_t make_idesc_e4m3(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+// e5m2 x e4m3 -> fp32, M = 128, N = n, the second operand's column index contiguous in shared memory.
+__device__ __forceinline__ uint32_t make_idesc_e5m2_e4m3_mn(int n) { return (1u << 4) | (1u << 7) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 // The same with M = 256 across a CTA pair.
 __device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (16u << 24); }
 
@@ -193,6 +205,12 @@ __device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 
                    "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), \
                    "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) \
                  : "r"(taddr))
+
+#define TMEM_ST_X16(taddr, r)                                                                                          \
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"  \
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),    \
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])           \
+                 : "memory")
 
 #define TMEM_ST_X32(taddr, r)                                                                                          \
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "                                                       \
