@@ -35,6 +35,17 @@ size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len);
 int launch_umma(const Params& p, void* workspace, cudaStream_t st);
 
 #ifdef __CUDACC__
+// Two e4m3 codes (the low or the high half of w) as fp16, exactly.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
+    uint32_t r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l;}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+    uint32_t r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, h;}" : "=r"(r) : "r"(w));
+    return r;
+}
 // Sequence of index b in the call: its cache slot and committed length; false (and the status word) if it cannot be used.
 __device__ __forceinline__ bool sequence_of(const Params& p, int b, int* s, int* n, bool report) {
     *s = p.seq_ids[b];

@@ -4,22 +4,22 @@
 // tiles of 64 -- four full pages, and one last tile for what is bf16, the tail rows and the block's own -- and the tiles
 // of all units, laid end to end, are cut into one equal share per thread block (attn_share.cuh).
 //
-// Both products run on 8-bit operands as the cache holds them; nothing of the KV stream is converted:
-//   S = Q K^T   Q is split into two e4m3 terms per row, q = 2^x (q1 + q2): a bf16 value has 8 significant bits, e4m3 has 4,
-//               so the two terms are exact except for elements below 2^-17 of their row's largest (absolute error 2^-18 of
-//               that).  Two e4m3 MMAs at twice the bf16 rate cost what one bf16 MMA would, and K needs half the bytes.
-//   O += P V    P is split into three e5m2 terms, the leading 9 bits of its fp16 form (an e5m2 value is an fp16 one with
-//               the low byte cut off): three bits each, and fp16's range, which the weights of a long flat context need
-//               (e4m3's two terms would lose every key 2^-17 below the row's largest).
-// A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  The bf16 tile is
-// split into two e4m3 terms per token, scaled by a power of two of its own, and meets the same operand layouts.
+//   S = Q K^T   on the codes as the cache holds them.  Q is split into two e4m3 terms per row, q = 2^x (q1 + q2): a bf16 value
+//               has 8 significant bits, e4m3 has 4, so the two terms are exact except for elements below 2^-13 of their row's
+//               largest (absolute error 2^-18 of that).  Two e4m3 MMAs at twice the bf16 rate cost what one bf16 MMA would,
+//               and K needs half the shared memory and no conversion.
+//   O += P V    in fp16: four warps turn the codes of V into fp16 (exact) in shared memory.  The weights P need eleven bits and
+//               a range that 8-bit terms only reach with three of them (built: splitting P cost the softmax twice the
+//               instructions of the exponentials, V's conversion costs a quarter of that).
+// A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  In the bf16 tile K
+// is split into two e4m3 terms, scaled by a power of two per token, and V is fp16, scaled by one per 16 tokens.
 //
 // Exponentials are taken against a reference per row, chosen in the first tile (the row's maximum there, held as 2^11, and
 // the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
 //
 // Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
-// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 TMA producer, 1 / 2 issuers
-// of S for group 0 / 1, 3 issuer of O, 4..7 and 8..11 softmax, 12..15 splitters (queries of the next segment, bf16 tiles).
+// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 TMA producer, 1 issuer of S, 2 issuer of
+// O, 3 splitter (the next segment's queries, bf16 tiles), 4..7 and 8..11 softmax, 12..15 V to fp16.
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 
 #include <cuda_fp16.h>
@@ -41,35 +41,42 @@ constexpr int TILE = 64;                       // keys per tile
 constexpr int PAGES = TILE / PAGE;
 constexpr int T_BYTES = TILE * HD;             // one 8-bit operand tile, 8 KB
 constexpr int SLOT_BYTES = 2 * T_BYTES;        // K then V
-constexpr int NSLOT = 6;
+constexpr int NSLOT = 5;
+constexpr int NSCALE = 16;                      // page tiles whose scales are kept: the producer is at most NSLOT tiles ahead of
+                                               // the issuer of S, and that one NS ahead of the softmax, so none is overwritten too early
+constexpr int VH_BYTES = 2 * T_BYTES;          // V of a tile in fp16: [dim half][64 tokens][128 B]; two buffers
+constexpr int VH_HALF = T_BYTES;
 constexpr int Q_BYTES = 2 * 128 * HD;          // both terms, 32 KB; two of them: the next segment's queries are split early
-constexpr int BT_BYTES = 4 * T_BYTES;          // bf16 tile: K terms, V terms
-constexpr int BT_COLS = 48;                    // 15 tail rows and 32 block rows at most
+constexpr int BT_BYTES = 2 * T_BYTES + VH_BYTES;   // bf16 tile: K terms, V in fp16
 constexpr int THREADS = 512;
-constexpr int TMEM_COLS = 512;                 // S [g * 64, +64)  P [128 + g * 48, +48)  O [256 + g * 128, +128)
-constexpr int P_COL = 128, P_COLS = 48, O_COL = 256;
-constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^28 above e5m2's last bit
+constexpr int TMEM_COLS = 512;                 // S [b * 64, +64) b < 3  P [192 + g * 32, +32)  O [256 + g * 128, +128)
+constexpr int NS = 3;                          // S buffers: the next two tiles' scores are ready while a tile's are being read
+constexpr int P_COL = NS * TILE, P_COLS = 32, O_COL = 256;
+constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^35 above fp16's last bit
 
 // mbarrier indices
-constexpr int BAR_Q_FULL = 0;                  // [2]  count 4: the splitter warps
-constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 2: both S issuers
-constexpr int BAR_BT_FULL = 4;                 // count 4
-constexpr int BAR_BT_EMPTY = 5;                // count 1: the issuer of O
-constexpr int BAR_S_FULL = 6;                  // [2]
-constexpr int BAR_S_FREE = 8;                  // [2]  count 4: the group's warps
-constexpr int BAR_P_READY = 10;                // [2]  count 4
-constexpr int BAR_O_DONE = 12;                 // [2]
-constexpr int BAR_MEET = 14;                   // [4]  count 2: the two warps of a lane quarter
-constexpr int BAR_PART = 18;                   // [4]  count 2
-constexpr int BAR_K_FULL = 22;                 // [NSLOT]
+constexpr int BAR_Q_FULL = 0;                  // [2]  count 8: the softmax warps (first segment) or eight lanes of the splitter
+constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 9: the issuer of S, the softmax warps (they have read the factors)
+constexpr int BAR_BT_FULL = 4;
+constexpr int BAR_BT_EMPTY = 5;                // the issuer of O
+constexpr int BAR_S_FULL = 6;                  // [NS]  count 2: the issuer's MMAs, and the issuer itself, who has seen the tile's scales arrive
+constexpr int BAR_S_FREE = BAR_S_FULL + NS;    // [NS]  count 4: the warps of the group that has the tile
+constexpr int BAR_P_READY = BAR_S_FREE + NS;   // [2]  count 4
+constexpr int BAR_O_DONE = BAR_P_READY + 2;    // [2]
+constexpr int BAR_MEET = BAR_O_DONE + 2;       // [4]  count 2: the two warps of a lane quarter
+constexpr int BAR_PART = BAR_MEET + 4;         // [4]  count 2
+constexpr int BAR_K_FULL = BAR_PART + 4;       // [NSLOT]
 constexpr int BAR_V_FULL = BAR_K_FULL + NSLOT;
-constexpr int BAR_SLOT_EMPTY = BAR_V_FULL + NSLOT;
-constexpr int N_BARS = BAR_SLOT_EMPTY + NSLOT;
+constexpr int BAR_SLOT_EMPTY = BAR_V_FULL + NSLOT;   // count 5: the issuer of S, the four warps that convert V
+constexpr int BAR_VH_FULL = BAR_SLOT_EMPTY + NSLOT;  // [2]  count 4
+constexpr int BAR_VH_EMPTY = BAR_VH_FULL + 2;        // [2]  the issuer of O
+constexpr int N_BARS = BAR_VH_EMPTY + 2;
 
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
     float q_factor[2][128];                    // per query row: scale * log2(e) * the power of two taken out of it
-    float bt_k[BT_COLS], bt_v[BT_COLS];        // powers of two taken out of the bf16 tile's tokens
+    float bt_k[TILE], bt_scale[2 * PAGES];     // powers of two taken out of the bf16 tile's tokens: K; V, 16 tokens together (behind PAGES unused)
+    float scales[NSCALE][2 * PAGES];           // K scales, V scales of a page tile's pages
     float meet[2][3][128];                     // per group and row: reference, sum, V reference
     uint32_t tmem_slot;
     int abort_flag;
@@ -78,7 +85,7 @@ struct Shared {                                // behind the operand buffers
     long long cursor;
     Seg segs[MAX_SEGS];
 };
-constexpr int SMEM_BYTES = 2 * Q_BYTES + NSLOT * SLOT_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
+constexpr int SMEM_BYTES = 2 * Q_BYTES + NSLOT * SLOT_BYTES + 2 * VH_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
 
 struct QParams {
     AttnParams a;
@@ -107,7 +114,8 @@ __device__ __forceinline__ float to_256(uint32_t amax_bits) {
     const int f = amax_bits ? 127 + 7 + 127 - (int)(amax_bits >> 23) : 127;
     return __uint_as_float((uint32_t)min(max(f, 1), 254) << 23);
 }
-// Sixteen values times `up`, as two terms of e4m3 codes (a row with a NaN or an infinity: NaN codes).
+// Sixteen bf16 values times `up`, as two terms of e4m3 codes: the leading four significant bits, cut off, and the four
+// behind them.  Below e4m3's normal range (2^-6) the second term takes the value as a whole.
 __device__ __forceinline__ void split16(const float (&v)[16], float up, bool bad, uint4* t1, uint4* t2) {
     uint32_t a[4], b[4];
 #pragma unroll
@@ -115,11 +123,14 @@ __device__ __forceinline__ void split16(const float (&v)[16], float up, bool bad
         uint32_t lo[2], hi[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float x0 = v[j * 4 + h * 2] * up, x1 = v[j * 4 + h * 2 + 1] * up;
-            lo[h] = __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
-            const __half2_raw back = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)lo[h], __NV_E4M3);
-            const float2 y = __half22float2(__half2(back));
-            hi[h] = __nv_cvt_float2_to_fp8x2(make_float2(x0 - y.x, x1 - y.y), __NV_SATFINITE, __NV_E4M3);
+            float x[2], y[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                x[e] = v[j * 4 + h * 2 + e] * up;
+                y[e] = fabsf(x[e]) < 0.015625f ? 0.f : __uint_as_float(__float_as_uint(x[e]) & 0xfff00000u);
+            }
+            lo[h] = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
+            hi[h] = __nv_cvt_float2_to_fp8x2(make_float2(x[0] - y[0], x[1] - y[1]), __NV_SATFINITE, __NV_E4M3);
         }
         a[j] = bad ? 0x7f7f7f7fu : (lo[0] | (lo[1] << 16));
         b[j] = bad ? 0u : (hi[0] | (hi[1] << 16));
@@ -128,13 +139,45 @@ __device__ __forceinline__ void split16(const float (&v)[16], float up, bool bad
     *t2 = make_uint4(b[0], b[1], b[2], b[3]);
 }
 
+// The segment's query rows first, first + step, ... (four rows per warp at a time, eight lanes each) as two terms, and the
+// factor that turns their products into scores in the log2 domain.  Whole-warp call; the caller makes the writes visible.
+__device__ __forceinline__ void split_queries(const AttnParams& p, const Seg& g, int rt, int first, int step, unsigned char* dst_q, float* factor) {
+    const int c16 = threadIdx.x & 7;                               // 16-dim piece of a row
+    const int kvh = g.hr / p.row_tiles, i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
+#pragma unroll 2
+    for (int r = first; r < 128; r += step) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = 0.f;
+        if (r < rows)
+            quant::load_bf16x16(p.q + ((size_t)(g.b * p.k + i0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * HD + c16 * 16, v);
+        const uint32_t m = quant::max8(quant::amax16(v));
+        const float up = to_256(m);
+        uint4 t1, t2;
+        split16(v, up, m >= 0x7f800000u, &t1, &t2);
+        unsigned char* dst = dst_q + r * HD + ((c16 ^ (r & 7)) << 4);
+        *reinterpret_cast<uint4*>(dst) = t1;
+        *reinterpret_cast<uint4*>(dst + Q_BYTES / 2) = t2;
+        if (c16 == 0) factor[r] = p.scale_log2 / up;
+    }
+}
+
+// Columns of the bf16 tile (tail rows, then block rows) that a query row sees.
+__device__ __forceinline__ uint64_t columns_seen(const AttnParams& p, const Seg& g, int rt, int row, uint32_t present, uint32_t decoded) {
+    const int i0 = rt * p.ipt, i_blk = i0 + row / p.G, n_tail = g.n % PAGE;
+    const bool row_valid = row < min(p.ipt, p.k - i0) * p.G;
+    const int state = (p.row_state && row_valid) ? p.row_state[(size_t)g.b * p.k + i_blk] : 1;
+    return ((uint64_t)(attn::visible_rows(p.mask, i_blk, state, present, decoded) & present) << n_tail) | ((1ull << n_tail) - 1ull);
+}
+
 __global__ void __launch_bounds__(THREADS, 1)
 attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const QParams qp) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* sQ = smem;                                  // [2 buffers][2 terms][128 rows][128 B]
     unsigned char* ring = sQ + 2 * Q_BYTES;                    // [NSLOT][K, V][64 tokens][128 B]
-    unsigned char* bt = ring + NSLOT * SLOT_BYTES;             // [K term 1, K term 2, V term 1, V term 2][64][128 B]
+    unsigned char* vh = ring + NSLOT * SLOT_BYTES;             // [2]
+    unsigned char* bt = vh + 2 * VH_BYTES;                     // [K term 1, K term 2][64][128 B], V
     Shared& sh = *reinterpret_cast<Shared*>(bt + BT_BYTES);
     volatile int* abort_flag = &sh.abort_flag;
     const AttnParams& p = qp.a;
@@ -150,14 +193,18 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
     auto bar = [&](int idx) { return bar_base + 8u * idx; };
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(BAR_Q_FULL + i), 4);
-            mbar_init(bar(BAR_Q_EMPTY + i), 2);
-            mbar_init(bar(BAR_S_FULL + i), 1);
-            mbar_init(bar(BAR_S_FREE + i), 4);
+            mbar_init(bar(BAR_Q_FULL + i), 8);
+            mbar_init(bar(BAR_Q_EMPTY + i), 9);
             mbar_init(bar(BAR_P_READY + i), 4);
             mbar_init(bar(BAR_O_DONE + i), 1);
+            mbar_init(bar(BAR_VH_FULL + i), 4);
+            mbar_init(bar(BAR_VH_EMPTY + i), 1);
         }
-        mbar_init(bar(BAR_BT_FULL), 4);
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(bar(BAR_S_FULL + i), 2);
+            mbar_init(bar(BAR_S_FREE + i), 4);
+        }
+        mbar_init(bar(BAR_BT_FULL), 1);
         mbar_init(bar(BAR_BT_EMPTY), 1);
         for (int i = 0; i < 4; ++i) {
             mbar_init(bar(BAR_MEET + i), 2);
@@ -166,7 +213,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
         for (int i = 0; i < NSLOT; ++i) {
             mbar_init(bar(BAR_K_FULL + i), 1);
             mbar_init(bar(BAR_V_FULL + i), 1);
-            mbar_init(bar(BAR_SLOT_EMPTY + i), 1);
+            mbar_init(bar(BAR_SLOT_EMPTY + i), 5);
         }
         sh.abort_flag = 0;
         sh.bt_bad[0] = sh.bt_bad[1] = 0;
@@ -198,11 +245,11 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem_base = sh.tmem_slot;
-    const uint32_t q_addr = smem_u32(sQ), ring_addr = smem_u32(ring), bt_addr = smem_u32(bt);
+    const uint32_t q_addr = smem_u32(sQ), ring_addr = smem_u32(ring), vh_addr = smem_u32(vh), bt_addr = smem_u32(bt);
 
     // Counters that run across segments and rounds; every role advances its own copy identically.
-    int it = 0;          // tiles so far: group it & 1, that group's phase it >> 1
-    int rs = 0;          // page tiles so far: ring slot rs % NSLOT
+    int it = 0;          // tiles so far: group it & 1, that group's phase it >> 1; S buffer it % NS, its phase it / NS
+    int rs = 0;          // page tiles so far: ring slot rs % NSLOT, fp16 buffer rs & 1
     int nb = 0;          // bf16 tiles so far
     int sg = 0;          // segments so far: Q buffer sg & 1
     long long cursor = share_lo;
@@ -235,16 +282,28 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                     if (lane >= 8 || t >= g.t_b || lp >= full) return -2;          // nothing there
                     return lp < p.kv.max_pages ? pt_row[lp] : -1;
                 };
-                int pg_cur = page_of(g.t_a), pg_next = page_of(g.t_a + 1);
+                auto scale_of = [&](int pg) -> float {
+                    if (pg < 0 || pg >= p.kv.num_pages) return 0.f;
+                    return __ldcg((is_v ? qp.kq.v_scale : qp.kq.k_scale) + (size_t)pg * Hkv + kvh);
+                };
+                // page ids are fetched three tiles ahead, their scales two tiles ahead
+                int pg_cur = page_of(g.t_a), pg_next = page_of(g.t_a + 1), pg_third = page_of(g.t_a + 2);
+                float sc_cur = scale_of(pg_cur), sc_next = scale_of(pg_next);
                 for (int t = g.t_a; t < g.t_b && t < last_tile; ++t, ++rs) {
                     const int sl = rs % NSLOT;
                     int pg = pg_cur;
+                    const float sc = sc_cur;
                     pg_cur = pg_next;
-                    pg_next = page_of(t + 2);
+                    pg_next = pg_third;
+                    pg_third = page_of(t + 3);
+                    sc_cur = sc_next;
+                    sc_next = scale_of(pg_next);
                     int oks = 1;
                     if (lane == 0) oks = mbar_wait(bar(BAR_SLOT_EMPTY + sl), ((uint32_t)(rs / NSLOT) & 1u) ^ 1u, abort_flag) ? 1 : 0;
                     if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
-                    if (lane == 0) {
+                    if (lane < 8) sh.scales[rs % NSCALE][lane] = sc;
+                    __syncwarp();
+                    if (lane == 0) {                                       // (the arrivals publish the scales as well)
                         mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);
                         mbar_expect_tx(bar(BAR_V_FULL + sl), T_BYTES);
                     }
@@ -259,12 +318,10 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                     }
                 }
             }
-        } else if (warp <= 2) {
-            // ---------------- issuers of S: warp 1 for group 0, warp 2 for group 1 ----------------
+        } else if (warp == 1) {
+            // ---------------- issuer of S ----------------
             if (lane == 0) {
-                const int grp = warp - 1;
                 const uint32_t idesc = make_idesc_e4m3(TILE);
-                const uint32_t d_tmem = tmem_base + (uint32_t)(grp * TILE);
                 bool ok = true;
                 for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                     const Seg g = sh.segs[si];
@@ -273,39 +330,40 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                     if (!mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
                     const uint64_t qd = smem_desc_sw128_kmajor(q_addr + qb * Q_BYTES);
                     for (int t = g.t_a; t < g.t_b; ++t, ++it) {
-                        const bool blk = t == last_tile;
-                        if ((it & 1) == grp) {
-                            if (!mbar_wait(bar(BAR_S_FREE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                            if (!blk) {
-                                const int sl = rs % NSLOT;
-                                if (!mbar_wait(bar(BAR_K_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
-                                tcgen05_fence_after();
-                                const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * SLOT_BYTES);
+                        const int sb = it % NS;
+                        const uint32_t d_tmem = tmem_base + (uint32_t)(sb * TILE);
+                        if (!mbar_wait(bar(BAR_S_FREE + sb), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                        if (t != last_tile) {
+                            const int sl = rs % NSLOT;
+                            if (!mbar_wait(bar(BAR_K_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
+                            tcgen05_fence_after();
+                            const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * SLOT_BYTES);
 #pragma unroll
-                                for (int kk = 0; kk < 8; ++kk)             // four steps of 32 dims for each term of Q
-                                    umma_f8_ss(d_tmem, qd + (uint64_t)(((kk >> 2) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
-                                               kd + (uint64_t)((kk & 3) * 2), idesc, kk != 0 ? 1u : 0u);
-                            } else {
-                                if (!mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag)) { ok = false; break; }
-                                tcgen05_fence_after();
-                                const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
+                            for (int kk = 0; kk < 8; ++kk)                 // four steps of 32 dims for each term of Q
+                                umma_f8_ss(d_tmem, qd + (uint64_t)(((kk >> 2) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4), kd + (uint64_t)((kk & 3) * 2),
+                                           idesc, kk != 0 ? 1u : 0u);
+                            umma_commit(bar(BAR_SLOT_EMPTY + sl));
+                            ++rs;
+                        } else {
+                            if (!mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag)) { ok = false; break; }
+                            tcgen05_fence_after();
+                            const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
 #pragma unroll
-                                for (int kk = 0; kk < 16; ++kk)            // and for each term of K
-                                    umma_f8_ss(d_tmem, qd + (uint64_t)((((kk >> 2) & 1) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
-                                               kd + (uint64_t)(((kk >> 3) * T_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0 ? 1u : 0u);
-                            }
-                            umma_commit(bar(BAR_S_FULL + grp));
+                            for (int kk = 0; kk < 16; ++kk)                // and for each term of K
+                                umma_f8_ss(d_tmem, qd + (uint64_t)((((kk >> 2) & 1) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
+                                           kd + (uint64_t)(((kk >> 3) * T_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0 ? 1u : 0u);
+                            ++nb;
                         }
-                        if (blk) ++nb;
-                        else ++rs;
+                        umma_commit(bar(BAR_S_FULL + sb));
+                        mbar_arrive(bar(BAR_S_FULL + sb));
                     }
                     if (ok) umma_commit(bar(BAR_Q_EMPTY + qb));
                 }
             }
-        } else if (warp == 3) {
+        } else if (warp == 2) {
             // ---------------- issuer of O += P V, both groups ----------------
             if (lane == 0) {
-                const uint32_t idesc = make_idesc_e5m2_e4m3_mn(HD);
+                const uint32_t idesc = make_idesc_f16(HD, 1);
                 bool ok = true;
                 for (int si = 0; si < n_seg && ok; ++si) {
                     const Seg g = sh.segs[si];
@@ -314,63 +372,38 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                         const int grp = it & 1;
                         const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(P_COL + grp * P_COLS);
                         const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
+                        const bool blk = t == last_tile;
+                        const int vb = rs & 1;
+                        if (!blk && !mbar_wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs >> 1) & 1u, abort_flag)) { ok = false; break; }
                         if (!mbar_wait(bar(BAR_P_READY + grp), (uint32_t)(it >> 1) & 1u, abort_flag)) { ok = false; break; }
-                        if (t != last_tile) {
-                            const int sl = rs % NSLOT;
-                            if (!mbar_wait(bar(BAR_V_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
-                            tcgen05_fence_after();
-                            // 32 tokens per MMA: four groups of eight, 1 KB apart; term x of P in columns x * 16 ..
-                            const uint64_t vd = smem_desc_sw128(ring_addr + sl * SLOT_BYTES + T_BYTES, 1024, 1024);
+                        tcgen05_fence_after();                             // (a bf16 tile was full before its S)
+                        // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
+                        const uint64_t vd = smem_desc_sw128(blk ? bt_addr + 2 * T_BYTES : vh_addr + vb * VH_BYTES, VH_HALF, 1024);
 #pragma unroll
-                            for (int kk = 0; kk < 6; ++kk)
-                                umma_f8_ts(o_tmem, p_tmem + (uint32_t)((kk >> 1) * 16 + (kk & 1) * 8), vd + (uint64_t)(((kk & 1) * 4096) >> 4), idesc,
-                                           kk != 0 ? 1u : keep);
-                            umma_commit(bar(BAR_SLOT_EMPTY + sl));         // S of this tile was complete before its softmax
-                            ++rs;
-                        } else {
-                            tcgen05_fence_after();                         // (the tile was full before its S)
-                            const uint64_t vd = smem_desc_sw128(bt_addr + 2 * T_BYTES, 1024, 1024);
-#pragma unroll
-                            for (int kk = 0; kk < 12; ++kk)
-                                umma_f8_ts(o_tmem, p_tmem + (uint32_t)(((kk >> 1) % 3) * 16 + (kk & 1) * 8),
-                                           vd + (uint64_t)(((kk / 6) * T_BYTES + (kk & 1) * 4096) >> 4), idesc, kk != 0 ? 1u : keep);
-                            umma_commit(bar(BAR_BT_EMPTY));
-                        }
+                        for (int kk = 0; kk < TILE / 16; ++kk)
+                            umma_bf16_ts(o_tmem, p_tmem + (uint32_t)(kk * 8), vd + (uint64_t)((kk * 2048) >> 4), idesc, kk != 0 ? 1u : keep);
                         umma_commit(bar(BAR_O_DONE + grp));
+                        umma_commit(blk ? bar(BAR_BT_EMPTY) : bar(BAR_VH_EMPTY + vb));
+                        if (!blk) ++rs;
                     }
                 }
             }
-        } else if (warp >= 12) {
-            // ---------------- splitters ----------------
-            const int st = tid - 384;                                      // 0..127
-            const int c16 = st & 7;                                        // 16-dim piece of a row
+        } else if (warp == 3) {
+            // ---------------- splitter ----------------
+            const int c16 = lane & 7;                                      // 16-dim piece of a row
             bool ok = true;
             for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                 const Seg g = sh.segs[si];
                 const int kvh = g.hr / p.row_tiles, last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                const int i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
                 const int qb = sg & 1;
-                ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-#pragma unroll 2
-                for (int r = st >> 3; r < 128; r += 16) {
-                    float v[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = 0.f;
-                    if (r < rows)
-                        quant::load_bf16x16(p.q + ((size_t)(g.b * p.k + i0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * HD + c16 * 16, v);
-                    const uint32_t m = quant::max8(quant::amax16(v));
-                    const float up = to_256(m);
-                    uint4 t1, t2;
-                    split16(v, up, m >= 0x7f800000u, &t1, &t2);
-                    unsigned char* dst = sQ + qb * Q_BYTES + r * HD + ((c16 ^ (r & 7)) << 4);
-                    *reinterpret_cast<uint4*>(dst) = t1;
-                    *reinterpret_cast<uint4*>(dst + Q_BYTES / 2) = t2;
-                    if (c16 == 0) sh.q_factor[qb][r] = p.scale_log2 / up;
+                if (sg > 0) {                                              // (the first segment's: the softmax warps, who have to wait anyway)
+                    ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    split_queries(p, g, rt, lane >> 3, 4, sQ + qb * Q_BYTES, sh.q_factor[qb]);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane < 8) mbar_arrive(bar(BAR_Q_FULL + qb));
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(BAR_Q_FULL + qb));
                 if (g.t_b != last_tile + 1) continue;
                 // the bf16 tile: tail rows, then block rows
                 ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
@@ -380,33 +413,62 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const int n_tail = g.n % PAGE;
                 const size_t tail0 = (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (g.n / PAGE % 3) * PAGE) * HD;
                 int bad_v = 0;
-#pragma unroll 2
-                for (int x = st >> 3; x < 2 * TILE; x += 16) {
-                    const int tok = x & (TILE - 1), is_v = x / TILE, jb = tok - n_tail;
-                    float v[16];
+                // token `tok` of the tile, this lane's 16 dims; zeros where there is none
+                auto load_row = [&](int tok, const void* tail, const __nv_bfloat16* blk, float (&v)[16]) {
+                    const int jb = tok - n_tail;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] = 0.f;
                     if (tok < n_tail)
-                        quant::load_bf16x16(static_cast<const __nv_bfloat16*>(is_v ? qp.kq.v_tail : qp.kq.k_tail) + tail0 + (size_t)tok * HD + c16 * 16, v);
+                        quant::load_bf16x16(static_cast<const __nv_bfloat16*>(tail) + tail0 + (size_t)tok * HD + c16 * 16, v);
                     else if (jb < p.k && ((present >> jb) & 1u))
-                        quant::load_bf16x16((is_v ? p.v_blk : p.k_blk) + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16, v);
-                    uint32_t m = quant::amax16(v);
-                    if (is_v && m >= 0x7f800000u) {                        // added to the rows that see it at the end
-                        bad_v = 1;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (quant::mag_bits(v[e]) >= 0x7f800000u) v[e] = 0.f;
-                        m = quant::amax16(v);
-                    }
-                    m = quant::max8(m);
-                    const bool bad = m >= 0x7f800000u;
+                        quant::load_bf16x16(blk + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16, v);
+                };
+#pragma unroll 2
+                for (int tok = lane >> 3; tok < TILE; tok += 4) {
+                    float v[16];
+                    load_row(tok, qp.kq.k_tail, p.k_blk, v);
+                    const uint32_t m = quant::max8(quant::amax16(v));
                     const float up = to_256(m);
                     uint4 t1, t2;
                     split16(v, up, false, &t1, &t2);
-                    unsigned char* dst = bt + is_v * 2 * T_BYTES + tok * HD + ((c16 ^ (tok & 7)) << 4);
+                    unsigned char* dst = bt + tok * HD + ((c16 ^ (tok & 7)) << 4);
                     *reinterpret_cast<uint4*>(dst) = t1;
                     *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
-                    if (c16 == 0 && tok < BT_COLS) (is_v ? sh.bt_v : sh.bt_k)[tok] = bad ? __uint_as_float(0x7fc00000u) : 1.f / up;
+                    if (c16 == 0) sh.bt_k[tok] = m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 1.f / up;
+                }
+#pragma unroll 1
+                for (int x = 0; x < PAGES; ++x) {                          // 16 tokens at a time
+                    float v[4][16];
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        load_row(x * PAGE + y * 4 + (lane >> 3), qp.kq.v_tail, p.v_blk, v[y]);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (quant::mag_bits(v[y][e]) >= 0x7f800000u) { // joins the rows that see it at the segment's end
+                                bad_v = 1;
+                                v[y][e] = 0.f;
+                            }
+                            m = max(m, quant::mag_bits(v[y][e]));
+                        }
+                    }
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    const float up = to_256(m);                            // exact down to 2^-21 of the largest, 2^-32 of it absolutely
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int tok = x * PAGE + y * 4 + (lane >> 3), c8 = (c16 & 3) * 2;
+                        uint32_t w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
+                            w[e] = *reinterpret_cast<const uint32_t*>(&hv);
+                        }
+                        unsigned char* dst = bt + 2 * T_BYTES + (c16 >> 2) * VH_HALF + tok * 128;
+                        *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                    if (lane == 0) sh.bt_scale[PAGES + x] = 1.f / up;
                 }
                 if (__any_sync(0xffffffffu, bad_v) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
                 fence_proxy_async_smem();
@@ -414,117 +476,172 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 if (lane == 0) mbar_arrive(bar(BAR_BT_FULL));
                 ++nb;
             }
+        } else if (warp >= 12) {
+            // ---------------- V to fp16: a thread takes four pieces of 16 codes of every page tile ----------------
+            const int st = tid - 384, c16 = st & 7, c8 = (c16 & 3) * 2;
+            bool ok = true;
+            for (int si = 0; si < n_seg && ok; ++si) {
+                const Seg g = sh.segs[si];
+                const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                for (int t = g.t_a; t < g.t_b && t < last_tile; ++t, ++rs) {
+                    const int sl = rs % NSLOT, vb = rs & 1;
+                    ok = mbar_wait(bar(BAR_V_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag) &&
+                         mbar_wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs >> 1) & 1u) ^ 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    const unsigned char* src = ring + sl * SLOT_BYTES + T_BYTES;
+                    unsigned char* dst = vh + vb * VH_BYTES + (c16 >> 2) * VH_HALF;
+                    uint4 codes[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int tok = (st >> 3) + x * 16;
+                        codes[x] = *reinterpret_cast<const uint4*>(src + tok * HD + ((c16 ^ (tok & 7)) << 4));
+                    }
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int tok = (st >> 3) + x * 16;
+                        const uint32_t w[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
+                        uint32_t f[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            f[2 * e] = codes_lo(w[e]);
+                            f[2 * e + 1] = codes_hi(w[e]);
+                        }
+                        *reinterpret_cast<uint4*>(dst + tok * 128 + ((c8 ^ (tok & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
+                        *reinterpret_cast<uint4*>(dst + tok * 128 + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(BAR_VH_FULL + vb));
+                        mbar_arrive(bar(BAR_SLOT_EMPTY + sl));
+                    }
+                }
+            }
         } else {
             // ---------------- softmax: one query row per thread, the group's tiles ----------------
             const int grp = (warp - 4) >> 2, quarter = warp & 3;
             const int row = quarter * 32 + lane;
             const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
-            const uint32_t s_tmem = t_lane + (uint32_t)(grp * TILE), p_tmem = t_lane + (uint32_t)(P_COL + grp * P_COLS);
+            const uint32_t p_tmem = t_lane + (uint32_t)(P_COL + grp * P_COLS);
             bool alive = true;
             for (int si = 0; si < n_seg && alive; ++si, ++sg) {
-                const Seg g = sh.segs[si];
-                const int kvh = g.hr / p.row_tiles, full = g.n / PAGE, last_tile = (full + PAGES - 1) / PAGES, n_tail = g.n % PAGE;
-                const int i0 = rt * p.ipt, ni = min(p.ipt, p.k - i0);
-                const int i_blk = i0 + row / p.G;
-                const bool row_valid = row < ni * p.G;
-                uint32_t present, decoded;
-                attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
-                const int state = (p.row_state && row_valid) ? p.row_state[(size_t)g.b * p.k + i_blk] : 1;
-                // columns of the bf16 tile that this row sees
-                const uint64_t see = ((uint64_t)(attn::visible_rows(p.mask, i_blk, state, present, decoded) & present) << n_tail) | ((1ull << n_tail) - 1ull);
-                const int32_t* pt_row = p.kv.page_table + (size_t)g.s * p.kv.max_pages;
-
-                // Scales of the group's tiles, fetched ahead: lane l < 4 has the K scale of page l of a tile, lane 4 + l its V
-                // scale; the page id is a tile further ahead.
-                auto page_of = [&](int t) -> int {
-                    const int lp = t * PAGES + (lane & 3);
-                    if (lane >= 8 || t >= g.t_b || lp >= full || lp >= p.kv.max_pages) return -1;
-                    const int pg = pt_row[lp];
-                    return pg < p.kv.num_pages ? pg : -1;
-                };
-                auto scale_of_page = [&](int pg) -> float {
-                    return pg < 0 ? 1.f : __ldcg((lane < 4 ? qp.kq.k_scale : qp.kq.v_scale) + (size_t)pg * Hkv + kvh);
-                };
-                const int t0 = g.t_a + ((it ^ grp) & 1);                   // the group's first tile
-                float sc_next = scale_of_page(page_of(t0));
-                int pg_next = page_of(t0 + 2);
-
+                const Seg& g = sh.segs[si];
+                const int full = g.n / PAGE, last_tile = (full + PAGES - 1) / PAGES, t_b = g.t_b;
                 float m_ref = 0.f, v_ref = 1.f, i_ref = 1.f, l_run = 0.f;
                 bool first = true;
                 const int qb = sg & 1;
+                if (sg == 0) {
+                    split_queries(p, g, rt, (warp - 4) * 4 + (lane >> 3), 32, sQ, sh.q_factor[0]);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(BAR_Q_FULL));
+                }
                 {
                     const bool got = mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                 }
                 const float f_row = sh.q_factor[qb][row];
-                for (int t = g.t_a; t < g.t_b; ++t, ++it) {
-                    if ((it & 1) != grp) continue;
-                    const uint32_t ph = (uint32_t)(it >> 1) & 1u;
-                    const float sc_cur = sc_next;
-                    sc_next = scale_of_page(pg_next);
-                    pg_next = page_of(t + 4);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_Q_EMPTY + qb));         // (a short segment's MMAs may all be done before this point)
+                for (int t = g.t_a; t < t_b; ++t, ++it) {
                     const bool is_bt = t == last_tile;
-                    const int n_pages = is_bt ? 0 : min(PAGES, full - t * PAGES);
-
-                    const bool got = mbar_wait(bar(BAR_S_FULL + grp), ph, abort_flag);
+                    const int sb = it % NS;
+                    const float* kv_scale = is_bt ? sh.bt_scale : sh.scales[rs % NSCALE];
+                    if (!is_bt) ++rs;
+                    if ((it & 1) != grp) continue;
+                    const int n_pages = is_bt ? PAGES : min(PAGES, full - t * PAGES);
+                    const uint32_t s_tmem = t_lane + (uint32_t)(sb * TILE);
+                    // The group's previous tile is in O (phase (it >> 1) - 1), so its P may be overwritten; the scores, and with them
+                    // the scales.  (Not K_FULL or BT_FULL for those: a slot may be on its next tile but one by now, and a parity
+                    // wait cannot tell.)
+                    const bool got = (it < 2 || mbar_wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) &&
+                                     mbar_wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                     tcgen05_fence_after();
-                    uint32_t sr[TILE];
-                    TMEM_LD_X32(s_tmem, (sr));
-                    TMEM_LD_X32(s_tmem + 32, (sr + 32));
-                    tmem_wait_ld();
-                    tcgen05_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(BAR_S_FREE + grp));
-
-                    // score of column c in the log2 domain = sr[c] * ka, ka > 0 (the bf16 tile: scaled and masked here, column
-                    // by column); V scale va.  A page that does not exist (zeros in shared memory) gets the weight 2^-inf.
-                    float ka[PAGES], va[PAGES], m_t = -INFINITY, v_t = 0.f;
+                    uint64_t see = 0;
                     if (is_bt) {
-                        const bool bf = mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag);      // (for bt_k / bt_v)
-                        if (!__all_sync(0xffffffffu, bf)) { alive = false; break; }
-#pragma unroll
-                        for (int c = 0; c < TILE; ++c)
-                            sr[c] = (c < BT_COLS && ((see >> c) & 1u)) ? __float_as_uint(__uint_as_float(sr[c]) * (sh.bt_k[c] * f_row)) : 0xff800000u;
-                        for (int c = 0; c < BT_COLS; ++c) v_t = fmaxf(v_t, sh.bt_v[c]);
-#pragma unroll
-                        for (int x = 0; x < PAGES; ++x) {
-                            ka[x] = 1.f;
-                            va[x] = 0.f;
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < PAGES; ++x) {
-                            ka[x] = f_row * __shfl_sync(0xffffffffu, sc_cur, x);
-                            va[x] = __shfl_sync(0xffffffffu, sc_cur, 4 + x);
-                            if (x < n_pages) v_t = fmaxf(v_t, va[x]);
-                        }
+                        uint32_t present, decoded;
+                        attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
+                        see = columns_seen(p, g, rt, row, present, decoded);
                     }
+                    // 32 scores: column c of half h in the log2 domain = sr[c] * ka of its page (the bf16 tile's are scaled and
+                    // masked here, token by token)
+                    uint32_t sr[32];
+                    auto load_half = [&](int h) {
+                        TMEM_LD_X32(s_tmem + (uint32_t)(h * 32), sr);
+                        tmem_wait_ld();
+                        if (is_bt) {
 #pragma unroll
-                    for (int x = 0; x < PAGES; ++x) {
-                        float mx = -INFINITY;
+                            for (int c = 0; c < 32; ++c)
+                                sr[c] = ((see >> (h * 32 + c)) & 1u) ? __float_as_uint(__uint_as_float(sr[c]) * (sh.bt_k[h * 32 + c] * f_row)) : 0xff800000u;
+                        }
+                    };
+                    auto tile_max = [&](float m, float& v) -> float {
+                        float mt = -INFINITY;
+                        v = 0.f;
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            load_half(h);
 #pragma unroll
-                        for (int c = 0; c < PAGE; c += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(sr[x * PAGE + c]), __uint_as_float(sr[x * PAGE + c + 1])));
-                        if (is_bt || x < n_pages) m_t = fmaxf(m_t, mx * ka[x]);
-                    }
-                    if (!(fabsf(m_t) < INFINITY)) m_t = first ? 0.f : m_ref;       // nothing visible here, or not finite
-                    if (!(v_t > 0.f && v_t < INFINITY)) v_t = first ? 1.f : v_ref;
-                    // The group's first tile sets the references.  A later one whose weights would pass 2^15 (2^40 without their V
-                    // scale) raises them: O and l shrink in place.
-                    const float p_t = first ? 0.f : ex2_approx(m_t - m_ref + BIAS);
-                    const bool raise = !first && (p_t * (v_t * i_ref) >= 32768.f || p_t >= 1.0995116e12f);
-                    const bool od = it < 2 || mbar_wait(bar(BAR_O_DONE + grp), ph ^ 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, od)) { alive = false; break; }
-                    // (phase (it >> 1) - 1 of o_done: the group's previous tile is in O, and its P may be overwritten)
+                            for (int x = 0; x < 2; ++x) {
+                                if (h * 2 + x >= n_pages) break;
+                                const float ka = is_bt ? 1.f : f_row * kv_scale[h * 2 + x];
+                                v = fmaxf(v, kv_scale[PAGES + h * 2 + x]);
+#pragma unroll
+                                for (int c = 0; c < PAGE; ++c) mt = fmaxf(mt, __uint_as_float(sr[x * PAGE + c]) * ka);
+                            }
+                        }
+                        return fabsf(mt) < INFINITY ? mt : m;              // (nothing visible here, or not finite)
+                    };
                     if (first) {
-                        m_ref = m_t;
-                        v_ref = v_t;
+                        float v;
+                        m_ref = tile_max(0.f, v);
+                        v_ref = v > 0.f && v < INFINITY ? v : 1.f;
                         i_ref = 1.f / v_ref;
-                    } else if (__any_sync(0xffffffffu, raise)) {
-                        const float m_new = fmaxf(m_ref, m_t), v_new = fmaxf(v_ref, v_t);
-                        const float al = ex2_approx(m_ref - m_new), ao = al * (v_ref / v_new);
-                        tcgen05_fence_after();
+                    }
+                    // weights 2^(score - m_ref + 11), and in fp16 those times V scale / v_ref
+                    float tile_sum;
+                    uint32_t top;
+                    auto weights = [&]() {
+                        uint64_t sum2[2] = {0, 0};
+                        __half2 top2 = __float2half2_rn(0.f);
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            load_half(h);
+                            uint32_t pr[16];
 #pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const float nm = h * 2 + x < n_pages ? BIAS - m_ref : -INFINITY;
+                                const float ka = is_bt ? 1.f : f_row * kv_scale[h * 2 + x], va = kv_scale[PAGES + h * 2 + x] * i_ref;
+                                const uint64_t nm2 = pack_f32x2(nm, nm), ka2 = pack_f32x2(ka, ka), va2 = pack_f32x2(va, va);
+#pragma unroll
+                                for (int c = x * PAGE; c < (x + 1) * PAGE; c += 2) {
+                                    float p0, p1, w0, w1;
+                                    unpack_f32x2(fma2(pack_f32x2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), ka2, nm2), p0, p1);
+                                    const uint64_t p2 = pack_f32x2(ex2_approx(p0), ex2_approx(p1));
+                                    sum2[(c >> 1) & 1] = add2(sum2[(c >> 1) & 1], p2);
+                                    unpack_f32x2(mul2(p2, va2), w0, w1);
+                                    const __half2 hw = __floats2half2_rn(w0, w1);
+                                    top2 = __hmax2(top2, hw);
+                                    pr[c >> 1] = *reinterpret_cast<const uint32_t*>(&hw);
+                                }
+                            }
+                            TMEM_ST_X16(p_tmem + (uint32_t)(h * 16), pr);
+                        }
+                        float a, b;
+                        unpack_f32x2(add2(sum2[0], sum2[1]), a, b);
+                        tile_sum = a + b;
+                        const uint32_t tb = *reinterpret_cast<const uint32_t*>(&top2);
+                        top = max(tb & 0x7fffu, (tb >> 16) & 0x7fffu);
+                    };
+                    weights();
+                    // A weight of 2^15 (0x7800 in fp16) or a sum of 2^40 raises the references: O and l shrink in place, the tile
+                    // is done again (its scores are still there).
+                    if (!first && __any_sync(0xffffffffu, top >= 0x7800u || !(tile_sum < 1.0995116e12f))) {
+                        float v_t;
+                        const float m_new = fmaxf(m_ref, tile_max(m_ref, v_t)), v_new = v_t < INFINITY ? fmaxf(v_ref, v_t) : v_ref;
+                        const float al = ex2_approx(m_ref - m_new), ao = al * (v_ref / v_new);
+#pragma unroll 1
                         for (int cc = 0; cc < HD / 16; ++cc) {
                             uint32_t o[16];
                             TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
@@ -533,55 +650,24 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                             for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ao);
                             TMEM_ST_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
                         }
-                        tmem_wait_st();
                         l_run *= al;
                         m_ref = m_new;
                         v_ref = v_new;
                         i_ref = 1.f / v_ref;
+                        weights();
                     }
                     first = false;
-                    // weights 2^(score - m_ref + 11); times V scale / v_ref in fp16; three e5m2 terms of that: the upper byte, the
-                    // upper byte of what is left, and what is left then, rounded
-                    float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t t1[16], t2[16], t3[16];
-#pragma unroll
-                    for (int w = 0; w < 16; ++w) {                         // four keys per word
-                        const int x = w >> 2;
-                        const float nm = (is_bt || x < n_pages) ? BIAS - m_ref : -INFINITY;
-                        uint32_t hi1[2], hi2[2], c3[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int c = 4 * w + 2 * e;
-                            const float p0 = ex2_approx(fmaf(__uint_as_float(sr[c]), ka[x], nm));
-                            const float p1 = ex2_approx(fmaf(__uint_as_float(sr[c + 1]), ka[x], nm));
-                            sum4[(2 * w + e) & 3] += p0 + p1;
-                            float w0 = va[x], w1 = va[x];
-                            if (is_bt) {
-                                w0 = c < BT_COLS ? sh.bt_v[c] : 0.f;
-                                w1 = c < BT_COLS ? sh.bt_v[c + 1] : 0.f;
-                            }
-                            const __half2 hw = __floats2half2_rn(p0 * (w0 * i_ref), p1 * (w1 * i_ref));
-                            hi1[e] = *reinterpret_cast<const uint32_t*>(&hw) & 0xff00ff00u;
-                            const __half2 r1 = __hsub2(hw, *reinterpret_cast<const __half2*>(&hi1[e]));
-                            hi2[e] = *reinterpret_cast<const uint32_t*>(&r1) & 0xff00ff00u;
-                            const __half2 r2 = __hsub2(r1, *reinterpret_cast<const __half2*>(&hi2[e]));
-                            c3[e] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(r2), __NV_SATFINITE, __NV_E5M2);
-                        }
-                        t1[w] = __byte_perm(hi1[0], hi1[1], 0x7531);
-                        t2[w] = __byte_perm(hi2[0], hi2[1], 0x7531);
-                        t3[w] = c3[0] | (c3[1] << 16);
-                    }
-                    l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
-                    TMEM_ST_X16(p_tmem, t1);
-                    TMEM_ST_X16(p_tmem + 16, t2);
-                    TMEM_ST_X16(p_tmem + 32, t3);
+                    l_run += tile_sum;
                     tmem_wait_st();
                     tcgen05_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(BAR_P_READY + grp));
+                    if (lane == 0) {
+                        mbar_arrive(bar(BAR_P_READY + grp));
+                        mbar_arrive(bar(BAR_S_FREE + sb));
+                    }
                 }
                 if (!alive) break;
-                if (g.t_b == last_tile + 1) ++nb;
+                if (t_b == last_tile + 1) ++nb;
 
                 // ---- the segment's result: the groups meet; each takes half of the columns of both accumulators ----
                 if (!first) {
@@ -605,7 +691,10 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const float mx = fmaxf(m0, m1);                            // one of the groups had a tile
                 const float e0 = m0 == -INFINITY ? 0.f : ex2_approx(m0 - mx), e1 = m1 == -INFINITY ? 0.f : ex2_approx(m1 - mx);
                 const float l = e0 * l0 + e1 * l1;
-                const bool gone = !row_valid || state < 0;                 // no query row, or an absent one
+                const int kvh = g.hr / p.row_tiles, n_tail = g.n % PAGE, i_blk = rt * p.ipt + row / p.G;
+                const bool row_valid = row < min(p.ipt, p.k - rt * p.ipt) * p.G;
+                // no query row, or an absent one
+                const bool gone = !row_valid || (p.row_state && p.row_state[(size_t)g.b * p.k + i_blk] < 0);
                 const float inv = l != 0.f ? 1.f / l : 0.f;
                 const float w0 = e0 * sh.meet[0][2][row] * inv, w1 = e1 * sh.meet[1][2][row] * inv;
                 const bool has0 = m0 != -INFINITY, has1 = m1 != -INFINITY;
@@ -614,7 +703,13 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const size_t unit = (size_t)g.b * HR + g.hr;
                 const bool whole = g.t_a == 0 && g.t_b == last_tile + 1;
                 const size_t slot = ((size_t)g.b * Hkv + kvh + jg) * p.row_tiles + rt;
-#pragma unroll
+                uint64_t see = 0;
+                if (bad_v) {                                               // (warp-uniform)
+                    uint32_t present, decoded;
+                    attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
+                    see = columns_seen(p, g, rt, row, present, decoded);
+                }
+#pragma unroll 1
                 for (int cc = 0; cc < 4; ++cc) {
                     const int col = grp * 64 + cc * 16;
                     uint32_t a[16], b[16];

@@ -602,7 +602,8 @@ __global__ void __launch_bounds__(256) attn_umma_merge_kernel(const AttnParams p
     pdl_wait();                                                   // the attention kernel's partial results
     // written by the block that holds the unit's first tile (by block 0 for a sequence that was skipped)
     const int2 parts = p.unit_parts[unit];
-    if (parts.x < 0) return;
+    // (a block that gave up on a wait may have left its units' entries unwritten: nothing outside the workspace is read then)
+    if (parts.x < 0 || parts.y < parts.x || parts.y >= p.nc / p.row_tiles) return;
     const int kvh = hr / p.row_tiles, rt = hr % p.row_tiles;
     const int i0 = rt * p.ipt;
     const int n_rows_u = min(p.ipt, p.k - i0) * p.G;

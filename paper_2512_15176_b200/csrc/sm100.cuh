@@ -131,7 +131,8 @@ __device__ __forceinline__ void umma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, u
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// D[tmem] (+)= A[tmem] * B[smem]: the 128-row operand comes from tensor memory (row = lane, two bf16 per column).
+// D[tmem] (+)= A[tmem] * B[smem]: the 128-row operand comes from tensor memory (row = lane, two bf16 -- or fp16, as the
+// instruction descriptor says -- per column).
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -148,16 +149,6 @@ __device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uin
         "setp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-// The same with the 128-row operand in tensor memory (row = lane, four 8-bit values per column).
-__device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 
@@ -182,10 +173,13 @@ __device__ __forceinline__ uint32_t make_idesc_bf16(int n, int b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(b_mn_major & 1) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 
+// The same for fp16 x fp16.
+__device__ __forceinline__ uint32_t make_idesc_f16(int n, int b_mn_major) {
+    return (1u << 4) | ((uint32_t)(b_mn_major & 1) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
 // kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N = n, both operands K-major.
 __device__ __forceinline__ uint32_t make_idesc_e4m3(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
-// e5m2 x e4m3 -> fp32, M = 128, N = n, the second operand's column index contiguous in shared memory.
-__device__ __forceinline__ uint32_t make_idesc_e5m2_e4m3_mn(int n) { return (1u << 4) | (1u << 7) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 // The same with M = 256 across a CTA pair.
 __device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (16u << 24); }
 
@@ -227,6 +221,21 @@ __device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 
 __device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
     uint64_t v;
     asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
     return v;
 }
 __device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {

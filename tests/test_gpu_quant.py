@@ -280,6 +280,29 @@ def test_attention(lengths, k, Hq, Hkv, D, mask):
     assert out[B].isnan().all() and (ws[need:] == 255).all()
 
 
+@pytest.mark.parametrize("B,k,Hq,Hkv,hi,mask", [(24, 9, 16, 8, 70, "causal"), (40, 32, 8, 2, 300, "states"), (900, 5, 32, 8, 20, "causal"),
+                                                (12, 32, 32, 4, 900, "bidir")])
+def test_attention_many_short_sequences(B, k, Hq, Hkv, hi, mask):
+    """More (sequence, KV head) units than thread blocks: a block walks many of them, most with one to a few tiles, in
+    lists of at most 48; two calls in a row (a block's hand-overs between units may not depend on timing)."""
+    from paper_2512_15176_b200 import binding as L
+    rng = np.random.default_rng(410)
+    lengths = [int(x) for x in rng.integers(0, hi + 1, size=B)]
+    D = 128
+    kv, okv = _cache(lengths, Hkv, D, 0, 410)
+    q, kb, vb = (W.normal(410, n, (B, k, h, D), 1.0) for n, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    states = rng.integers(-1, 2, size=(B, k)).astype(np.int32) if mask == "states" else None
+    m = L.DEER_MASK_CAUSAL if mask == "causal" else L.DEER_MASK_BIDIR
+    ws = torch.full((L.deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, hi),), 255, dtype=torch.uint8, device="cuda")
+    outs = [torch.full((B, k, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    dev = [t.cuda() for t in (q, kb, vb)]
+    for out in outs:
+        L.deer_block_attn_quant(kv, _ids(B), *dev, out, None if states is None else torch.from_numpy(states).cuda(), m, 1 / math.sqrt(D), hi, ws)
+    assert L.deer_kv_status(kv) == 0
+    assert torch.equal(outs[0], outs[1])
+    check_attention(outs[0], q, kb, vb, okv, list(range(B)), m, 1 / math.sqrt(D), states, f"{B} {k} {mask}")
+
+
 @pytest.mark.parametrize("k,Hq,Hkv,D", [(1, 4, 1, 128), (8, 4, 2, 64), (32, 16, 4, 128), (16, 8, 1, 128)])
 def test_attention_spread_scales_and_scores(k, Hq, Hkv, D):
     """Page scales over forty octaves (pages of zeros among them), a dominating key late in the context over a long
