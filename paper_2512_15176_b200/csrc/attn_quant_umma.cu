@@ -11,8 +11,8 @@
 //   O += P V    in fp16: four warps turn the codes of V into fp16 (exact) in shared memory.  The weights P need eleven bits and
 //               a range that 8-bit terms only reach with three of them (built: splitting P cost the softmax twice the
 //               instructions of the exponentials, V's conversion costs a quarter of that).
-// A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  In the bf16 tile K
-// is split into two e4m3 terms, scaled by a power of two per token, and V is fp16, scaled by one per 16 tokens.
+// A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  The bf16 tile has
+// the same form: K as two e4m3 terms, V as fp16, a power of two for every 16 tokens in the place of the scales.
 //
 // Exponentials are taken against a reference per row, chosen in the first tile (the row's maximum there, held as 2^11, and
 // the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
@@ -70,12 +70,13 @@ constexpr int BAR_V_FULL = BAR_K_FULL + NSLOT;
 constexpr int BAR_SLOT_EMPTY = BAR_V_FULL + NSLOT;   // count 5: the issuer of S, the four warps that convert V
 constexpr int BAR_VH_FULL = BAR_SLOT_EMPTY + NSLOT;  // [2]  count 4
 constexpr int BAR_VH_EMPTY = BAR_VH_FULL + 2;        // [2]  the issuer of O
-constexpr int N_BARS = BAR_VH_EMPTY + 2;
+constexpr int BAR_Q_RAW = BAR_VH_EMPTY + 2;          // [2]  the queries as bf16
+constexpr int N_BARS = BAR_Q_RAW + 2;
 
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
     float q_factor[2][128];                    // per query row: scale * log2(e) * the power of two taken out of it
-    float bt_k[TILE], bt_scale[2 * PAGES];     // powers of two taken out of the bf16 tile's tokens: K; V, 16 tokens together (behind PAGES unused)
+    float bt_scale[2 * PAGES];                 // powers of two taken out of the bf16 tile's tokens, 16 together: K, V
     float scales[NSCALE][2 * PAGES];           // K scales, V scales of a page tile's pages
     float meet[2][3][128];                     // per group and row: reference, sum, V reference
     uint32_t tmem_slot;
@@ -139,26 +140,32 @@ __device__ __forceinline__ void split16(const float (&v)[16], float up, bool bad
     *t2 = make_uint4(b[0], b[1], b[2], b[3]);
 }
 
-// The segment's query rows first, first + step, ... (four rows per warp at a time, eight lanes each) as two terms, and the
-// factor that turns their products into scores in the log2 domain.  Whole-warp call; the caller makes the writes visible.
-__device__ __forceinline__ void split_queries(const AttnParams& p, const Seg& g, int rt, int first, int step, unsigned char* dst_q, float* factor) {
+// A 16-dim piece of a bf16 row that lies in two halves of 64 dims (128-byte rows, swizzled), `half` bytes apart.
+__device__ __forceinline__ const uint4* piece(const unsigned char* tile, int half, int r, int c16, int x) {
+    return reinterpret_cast<const uint4*>(tile + (c16 >> 2) * half + r * 128 + ((((c16 & 3) * 2 + x) ^ (r & 7)) << 4));
+}
+// The query rows first, first + step, ... (four rows per warp at a time, eight lanes each) of a tile that TMA has brought as
+// bf16 [dim half][128 rows][128 B], in place as two terms [term][128 rows][128 B], and the factor that turns their products
+// into scores in the log2 domain.  A row's raw form and its terms are the same 256 bytes.  Whole-warp call; the caller
+// makes the writes visible.  (A call, not inlined: a block runs it a few times, and instructions that are not yet cached
+// cost more than it does.)
+__device__ __noinline__ void split_queries(unsigned char* tile, float* factor, float scale_log2, int rows, int first, int step) {
     const int c16 = threadIdx.x & 7;                               // 16-dim piece of a row
-    const int kvh = g.hr / p.row_tiles, i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
-#pragma unroll 2
+#pragma unroll 1
     for (int r = first; r < 128; r += step) {
         float v[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = 0.f;
-        if (r < rows)
-            quant::load_bf16x16(p.q + ((size_t)(g.b * p.k + i0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * HD + c16 * 16, v);
-        const uint32_t m = quant::max8(quant::amax16(v));
+        uint4 a = *piece(tile, Q_BYTES / 2, r, c16, 0), b = *piece(tile, Q_BYTES / 2, r, c16, 1);
+        if (r >= rows) a = b = make_uint4(0, 0, 0, 0);             // whatever was there
+        quant::unpack_bf16x8(a, v);
+        quant::unpack_bf16x8(b, v + 8);
+        const uint32_t m = quant::max8(quant::amax16(v));          // (every lane of the row has read its piece)
         const float up = to_256(m);
         uint4 t1, t2;
         split16(v, up, m >= 0x7f800000u, &t1, &t2);
-        unsigned char* dst = dst_q + r * HD + ((c16 ^ (r & 7)) << 4);
+        unsigned char* dst = tile + r * HD + ((c16 ^ (r & 7)) << 4);
         *reinterpret_cast<uint4*>(dst) = t1;
         *reinterpret_cast<uint4*>(dst + Q_BYTES / 2) = t2;
-        if (c16 == 0) factor[r] = p.scale_log2 / up;
+        if (c16 == 0) factor[r] = scale_log2 / up;
     }
 }
 
@@ -171,7 +178,8 @@ __device__ __forceinline__ uint64_t columns_seen(const AttnParams& p, const Seg&
 }
 
 __global__ void __launch_bounds__(THREADS, 1)
-attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const QParams qp) {
+attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                       const QParams qp) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* sQ = smem;                                  // [2 buffers][2 terms][128 rows][128 B]
@@ -194,6 +202,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(BAR_Q_FULL + i), 8);
+            mbar_init(bar(BAR_Q_RAW + i), 1);
             mbar_init(bar(BAR_Q_EMPTY + i), 9);
             mbar_init(bar(BAR_P_READY + i), 4);
             mbar_init(bar(BAR_O_DONE + i), 1);
@@ -218,6 +227,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
         sh.abort_flag = 0;
         sh.bt_bad[0] = sh.bt_bad[1] = 0;
         mbar_init_fence();
+        prefetch_tensormap(&tm_q);
         prefetch_tensormap(&tm_k);
         prefetch_tensormap(&tm_v);
     }
@@ -396,10 +406,18 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const Seg g = sh.segs[si];
                 const int kvh = g.hr / p.row_tiles, last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
                 const int qb = sg & 1;
+                ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                const int i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
+                if (lane == 0) {
+                    mbar_expect_tx(bar(BAR_Q_RAW + qb), (uint32_t)(2 * p.G * min(p.ipt, p.k) * 128));
+                    tma_load_3d(q_addr + qb * Q_BYTES, &tm_q, 0, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
+                    tma_load_3d(q_addr + qb * Q_BYTES + Q_BYTES / 2, &tm_q, 64, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
+                }
                 if (sg > 0) {                                              // (the first segment's: the softmax warps, who have to wait anyway)
-                    ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
+                    ok = mbar_wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    split_queries(p, g, rt, lane >> 3, 4, sQ + qb * Q_BYTES, sh.q_factor[qb]);
+                    split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, rows, lane >> 3, 4);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane < 8) mbar_arrive(bar(BAR_Q_FULL + qb));
@@ -413,62 +431,70 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const int n_tail = g.n % PAGE;
                 const size_t tail0 = (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (g.n / PAGE % 3) * PAGE) * HD;
                 int bad_v = 0;
-                // token `tok` of the tile, this lane's 16 dims; zeros where there is none
-                auto load_row = [&](int tok, const void* tail, const __nv_bfloat16* blk, float (&v)[16]) {
-                    const int jb = tok - n_tail;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = 0.f;
-                    if (tok < n_tail)
-                        quant::load_bf16x16(static_cast<const __nv_bfloat16*>(tail) + tail0 + (size_t)tok * HD + c16 * 16, v);
-                    else if (jb < p.k && ((present >> jb) & 1u))
-                        quant::load_bf16x16(blk + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16, v);
-                };
-#pragma unroll 2
-                for (int tok = lane >> 3; tok < TILE; tok += 4) {
-                    float v[16];
-                    load_row(tok, qp.kq.k_tail, p.k_blk, v);
-                    const uint32_t m = quant::max8(quant::amax16(v));
-                    const float up = to_256(m);
-                    uint4 t1, t2;
-                    split16(v, up, false, &t1, &t2);
-                    unsigned char* dst = bt + tok * HD + ((c16 ^ (tok & 7)) << 4);
-                    *reinterpret_cast<uint4*>(dst) = t1;
-                    *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
-                    if (c16 == 0) sh.bt_k[tok] = m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 1.f / up;
-                }
+                // All rows as bf16 to where their split form will be, [dim half][64 tokens][128 B], zeros where there is no token;
+                // each lane copies what it will split.
 #pragma unroll 1
-                for (int x = 0; x < PAGES; ++x) {                          // 16 tokens at a time
+                for (int x = 0; x < 2 * TILE; x += 4) {
+                    const bool is_v = x >= TILE;
+                    const int tok = (x & (TILE - 1)) + (lane >> 3), jb = tok - n_tail;
+                    const __nv_bfloat16* src = nullptr;
+                    if (tok < n_tail)
+                        src = static_cast<const __nv_bfloat16*>(is_v ? qp.kq.v_tail : qp.kq.k_tail) + tail0 + (size_t)tok * HD + c16 * 16;
+                    else if (jb < p.k && ((present >> jb) & 1u))
+                        src = (is_v ? p.v_blk : p.k_blk) + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16;
+                    unsigned char* tile = bt + (is_v ? 2 * T_BYTES : 0);
+                    cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 0)), src ? src : p.k_blk, src ? 16 : 0);
+                    cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 1)), src ? src + 8 : p.k_blk, src ? 16 : 0);
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                __syncwarp();
+#pragma unroll 1
+                for (int x = 0; x < 2 * PAGES; ++x) {                      // 16 tokens at a time: K, then V
+                    const bool is_v = x >= PAGES;
+                    const int tok0 = (x & (PAGES - 1)) * PAGE + (lane >> 3);
                     float v[4][16];
                     uint32_t m = 0;
+                    bool bad[4];
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
-                        load_row(x * PAGE + y * 4 + (lane >> 3), qp.kq.v_tail, p.v_blk, v[y]);
+                        const unsigned char* tile = bt + (is_v ? 2 * T_BYTES : 0);
+                        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok0 + y * 4, c16, 0), v[y]);
+                        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok0 + y * 4, c16, 1), v[y] + 8);
+                        bad[y] = quant::max8(quant::amax16(v[y])) >= 0x7f800000u;
+                        if (bad[y]) {                                      // K: the token's codes are NaN.  V: joins the rows that see it at the end
+                            bad_v |= is_v;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (quant::mag_bits(v[y][e]) >= 0x7f800000u) { // joins the rows that see it at the segment's end
-                                bad_v = 1;
-                                v[y][e] = 0.f;
+                            for (int e = 0; e < 16; ++e)
+                                if (quant::mag_bits(v[y][e]) >= 0x7f800000u) v[y][e] = 0.f;
+                        }
+                        m = max(m, quant::amax16(v[y]));
+                    }
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));      // (and every lane has read)
+                    const float up = to_256(m);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int tok = tok0 + y * 4, c8 = (c16 & 3) * 2;
+                        if (!is_v) {
+                            uint4 t1, t2;
+                            split16(v[y], up, bad[y], &t1, &t2);
+                            unsigned char* dst = bt + tok * HD + ((c16 ^ (tok & 7)) << 4);
+                            *reinterpret_cast<uint4*>(dst) = t1;
+                            *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
+                        } else {                                           // exact down to 2^-21 of the largest, 2^-32 of it absolutely
+                            uint32_t w[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
+                                w[e] = *reinterpret_cast<const uint32_t*>(&hv);
                             }
-                            m = max(m, quant::mag_bits(v[y][e]));
+                            unsigned char* dst = bt + 2 * T_BYTES + (c16 >> 2) * VH_HALF + tok * 128;
+                            *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
                         }
                     }
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    const float up = to_256(m);                            // exact down to 2^-21 of the largest, 2^-32 of it absolutely
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int tok = x * PAGE + y * 4 + (lane >> 3), c8 = (c16 & 3) * 2;
-                        uint32_t w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
-                            w[e] = *reinterpret_cast<const uint32_t*>(&hv);
-                        }
-                        unsigned char* dst = bt + 2 * T_BYTES + (c16 >> 2) * VH_HALF + tok * 128;
-                        *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                    if (lane == 0) sh.bt_scale[PAGES + x] = 1.f / up;
+                    if (lane == 0) sh.bt_scale[x] = 1.f / up;
                 }
                 if (__any_sync(0xffffffffu, bad_v) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
                 fence_proxy_async_smem();
@@ -531,7 +557,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 bool first = true;
                 const int qb = sg & 1;
                 if (sg == 0) {
-                    split_queries(p, g, rt, (warp - 4) * 4 + (lane >> 3), 32, sQ, sh.q_factor[0]);
+                    const bool raw = mbar_wait(bar(BAR_Q_RAW), 0u, abort_flag);
+                    if (!__all_sync(0xffffffffu, raw)) { alive = false; break; }
+                    split_queries(sQ, sh.q_factor[0], p.scale_log2, min(p.ipt, p.k - rt * p.ipt) * p.G, (warp - 4) * 4 + (lane >> 3), 32);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(BAR_Q_FULL));
@@ -564,45 +592,62 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                         attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
                         see = columns_seen(p, g, rt, row, present, decoded);
                     }
-                    // 32 scores: column c of half h in the log2 domain = sr[c] * ka of its page (the bf16 tile's are scaled and
-                    // masked here, token by token)
+                    // 32 scores: column c of half h in the log2 domain = sr[c] * factor * its page's K scale
                     uint32_t sr[32];
                     auto load_half = [&](int h) {
                         TMEM_LD_X32(s_tmem + (uint32_t)(h * 32), sr);
                         tmem_wait_ld();
                         if (is_bt) {
+                            const uint32_t bits = (uint32_t)(see >> (h * 32));
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
-                                sr[c] = ((see >> (h * 32 + c)) & 1u) ? __float_as_uint(__uint_as_float(sr[c]) * (sh.bt_k[h * 32 + c] * f_row)) : 0xff800000u;
+                                if (!((bits >> c) & 1u)) sr[c] = 0xff800000u;
                         }
                     };
-                    auto tile_max = [&](float m, float& v) -> float {
-                        float mt = -INFINITY;
-                        v = 0.f;
-#pragma unroll 1
-                        for (int h = 0; h < 2; ++h) {
-                            load_half(h);
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                if (h * 2 + x >= n_pages) break;
-                                const float ka = is_bt ? 1.f : f_row * kv_scale[h * 2 + x];
-                                v = fmaxf(v, kv_scale[PAGES + h * 2 + x]);
-#pragma unroll
-                                for (int c = 0; c < PAGE; ++c) mt = fmaxf(mt, __uint_as_float(sr[x * PAGE + c]) * ka);
-                            }
-                        }
-                        return fabsf(mt) < INFINITY ? mt : m;              // (nothing visible here, or not finite)
-                    };
-                    if (first) {
-                        float v;
-                        m_ref = tile_max(0.f, v);
-                        v_ref = v > 0.f && v < INFINITY ? v : 1.f;
-                        i_ref = 1.f / v_ref;
-                    }
-                    // weights 2^(score - m_ref + 11), and in fp16 those times V scale / v_ref
+                    // The group's first tile sets the references.  Later a weight of 2^15 (0x7800 in fp16) or a sum of 2^40 raises
+                    // them: O and l shrink in place, the tile is done again (its scores are still there).
+                    bool set = first;
                     float tile_sum;
-                    uint32_t top;
-                    auto weights = [&]() {
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        if (set) {
+                            float m_t = -INFINITY, v_t = 0.f;
+#pragma unroll 1
+                            for (int h = 0; h < 2; ++h) {
+                                load_half(h);
+#pragma unroll
+                                for (int x = 0; x < 2; ++x) {
+                                    if (h * 2 + x >= n_pages) break;
+                                    float mx = -INFINITY;
+#pragma unroll
+                                    for (int c = 0; c < PAGE; ++c) mx = fmaxf(mx, __uint_as_float(sr[x * PAGE + c]));
+                                    m_t = fmaxf(m_t, mx * (f_row * kv_scale[h * 2 + x]));
+                                    v_t = fmaxf(v_t, kv_scale[PAGES + h * 2 + x]);
+                                }
+                            }
+                            if (!(fabsf(m_t) < INFINITY)) m_t = m_ref;     // nothing visible here, or not finite
+                            if (!(v_t > 0.f && v_t < INFINITY)) v_t = v_ref;
+                            if (!first) {
+                                m_t = fmaxf(m_t, m_ref);
+                                v_t = fmaxf(v_t, v_ref);
+                                const float al = ex2_approx(m_ref - m_t), ao = al * (v_ref / v_t);
+#pragma unroll 1
+                                for (int cc = 0; cc < HD / 16; ++cc) {
+                                    uint32_t o[16];
+                                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ao);
+                                    TMEM_ST_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
+                                }
+                                tmem_wait_st();
+                                l_run *= al;
+                            }
+                            m_ref = m_t;
+                            v_ref = v_t;
+                            i_ref = 1.f / v_ref;
+                        }
+                        // weights 2^(score - m_ref + 11), and in fp16 those times V scale / v_ref
                         uint64_t sum2[2] = {0, 0};
                         __half2 top2 = __float2half2_rn(0.f);
 #pragma unroll 1
@@ -612,7 +657,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
                                 const float nm = h * 2 + x < n_pages ? BIAS - m_ref : -INFINITY;
-                                const float ka = is_bt ? 1.f : f_row * kv_scale[h * 2 + x], va = kv_scale[PAGES + h * 2 + x] * i_ref;
+                                float ka = f_row * kv_scale[h * 2 + x];
+                                if (ka == 0.f) ka = quant::SCALE_MIN;      // a masked -inf must stay one
+                                const float va = kv_scale[PAGES + h * 2 + x] * i_ref;
                                 const uint64_t nm2 = pack_f32x2(nm, nm), ka2 = pack_f32x2(ka, ka), va2 = pack_f32x2(va, va);
 #pragma unroll
                                 for (int c = x * PAGE; c < (x + 1) * PAGE; c += 2) {
@@ -632,29 +679,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                         unpack_f32x2(add2(sum2[0], sum2[1]), a, b);
                         tile_sum = a + b;
                         const uint32_t tb = *reinterpret_cast<const uint32_t*>(&top2);
-                        top = max(tb & 0x7fffu, (tb >> 16) & 0x7fffu);
-                    };
-                    weights();
-                    // A weight of 2^15 (0x7800 in fp16) or a sum of 2^40 raises the references: O and l shrink in place, the tile
-                    // is done again (its scores are still there).
-                    if (!first && __any_sync(0xffffffffu, top >= 0x7800u || !(tile_sum < 1.0995116e12f))) {
-                        float v_t;
-                        const float m_new = fmaxf(m_ref, tile_max(m_ref, v_t)), v_new = v_t < INFINITY ? fmaxf(v_ref, v_t) : v_ref;
-                        const float al = ex2_approx(m_ref - m_new), ao = al * (v_ref / v_new);
-#pragma unroll 1
-                        for (int cc = 0; cc < HD / 16; ++cc) {
-                            uint32_t o[16];
-                            TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ao);
-                            TMEM_ST_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
-                        }
-                        l_run *= al;
-                        m_ref = m_new;
-                        v_ref = v_new;
-                        i_ref = 1.f / v_ref;
-                        weights();
+                        set = __any_sync(0xffffffffu, max(tb & 0x7fffu, (tb >> 16) & 0x7fffu) >= 0x7800u || !(tile_sum < 1.0995116e12f));
+                        if (first || !set) break;
                     }
                     first = false;
                     l_run += tile_sum;
@@ -843,15 +869,20 @@ int launch_umma(const Params& q, void* workspace, cudaStream_t st) {
     p.part_lse = p.part_o + slots * 128 * HD;
     p.total_tiles = reinterpret_cast<long long*>(p.part_lse + slots * 128);
     p.unit_parts = reinterpret_cast<int2*>(p.total_tiles + 1);
-    CUtensorMap tm_k, tm_v;
+    CUtensorMap tm_q, tm_k, tm_v;
     const uint64_t dims[2] = {HD, (uint64_t)p.kv.num_pages * Hkv * PAGE}, str[1] = {HD};
     const uint32_t box[2] = {HD, PAGE};
-    int rc = make_map_u8(&tm_k, p.kv.k_pool, 2, dims, str, box);
+    // q [B*k][Hq][128]: a box brings G heads of box_i block rows, 64 dims wide -> shared-memory row = i * G + g
+    const uint64_t dims_q[3] = {HD, (uint64_t)p.Hq, (uint64_t)p.B * p.k}, str_q[2] = {HD * 2, (uint64_t)p.Hq * HD * 2};
+    const uint32_t box_q[3] = {64, (uint32_t)p.G, (uint32_t)(p.ipt < p.k ? p.ipt : p.k)};
+    int rc = make_map_bf16(&tm_q, p.q, 3, dims_q, str_q, box_q);
+    if (rc != DEER_OK) return rc;
+    rc = make_map_u8(&tm_k, p.kv.k_pool, 2, dims, str, box);
     if (rc != DEER_OK) return rc;
     rc = make_map_u8(&tm_v, p.kv.v_pool, 2, dims, str, box);
     if (rc != DEER_OK) return rc;
     DEER_CUDA(cudaFuncSetAttribute(attn_quant_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
-    DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_k, tm_v, qp));
+    DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_k, tm_v, qp));
     return attn::launch_umma_merge(p, st);
 }
 
