@@ -19,7 +19,7 @@
 //
 // Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
 // its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 TMA producer, 1 issuer of S, 2 issuer of
-// O, 3 splitter (the next segment's queries, bf16 tiles), 4..7 and 8..11 softmax, 12..15 V to fp16.
+// O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V to fp16 and the bf16 tile (warp 3: none).
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 
 #include <cuda_fp16.h>
@@ -55,9 +55,9 @@ constexpr int P_COL = NS * TILE, P_COLS = 32, O_COL = 256;
 constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^35 above fp16's last bit
 
 // mbarrier indices
-constexpr int BAR_Q_FULL = 0;                  // [2]  count 8: the softmax warps (first segment) or eight lanes of the splitter
+constexpr int BAR_Q_FULL = 0;                  // [2]  count 8: the softmax warps
 constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 9: the issuer of S, the softmax warps (they have read the factors)
-constexpr int BAR_BT_FULL = 4;
+constexpr int BAR_BT_FULL = 4;                 // count 4: the warps that convert
 constexpr int BAR_BT_EMPTY = 5;                // the issuer of O
 constexpr int BAR_S_FULL = 6;                  // [NS]  count 2: the issuer's MMAs, and the issuer itself, who has seen the tile's scales arrive
 constexpr int BAR_S_FREE = BAR_S_FULL + NS;    // [NS]  count 4: the warps of the group that has the tile
@@ -147,9 +147,8 @@ __device__ __forceinline__ const uint4* piece(const unsigned char* tile, int hal
 // The query rows first, first + step, ... (four rows per warp at a time, eight lanes each) of a tile that TMA has brought as
 // bf16 [dim half][128 rows][128 B], in place as two terms [term][128 rows][128 B], and the factor that turns their products
 // into scores in the log2 domain.  A row's raw form and its terms are the same 256 bytes.  Whole-warp call; the caller
-// makes the writes visible.  (A call, not inlined: a block runs it a few times, and instructions that are not yet cached
-// cost more than it does.)
-__device__ __noinline__ void split_queries(unsigned char* tile, float* factor, float scale_log2, int rows, int first, int step) {
+// makes the writes visible.
+__device__ __forceinline__ void split_queries(unsigned char* tile, float* factor, float scale_log2, int rows, int first, int step) {
     const int c16 = threadIdx.x & 7;                               // 16-dim piece of a row
 #pragma unroll 1
     for (int r = first; r < 128; r += step) {
@@ -167,6 +166,75 @@ __device__ __noinline__ void split_queries(unsigned char* tile, float* factor, f
         *reinterpret_cast<uint4*>(dst + Q_BYTES / 2) = t2;
         if (c16 == 0) factor[r] = scale_log2 / up;
     }
+}
+
+// Sixteen tokens (tok0 ..) of the bf16 tile's K in place as two terms, with one power of two for them; a token with a NaN
+// or an infinity gets NaN codes.  Whole-warp call, for rows that this warp's lanes have brought, each its pieces.
+__device__ __forceinline__ void split_keys(unsigned char* tile, float* scale, int tok0) {
+    const int lane = threadIdx.x & 31, c16 = lane & 7;
+    float v[4][16];
+    bool bad[4];
+    uint32_t m = 0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int tok = tok0 + y * 4 + (lane >> 3);
+        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 0), v[y]);
+        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 1), v[y] + 8);
+        const uint32_t mt = quant::max8(quant::amax16(v[y]));
+        bad[y] = mt >= 0x7f800000u;
+        m = max(m, bad[y] ? 0u : mt);
+    }
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));                // (and every lane has read)
+    const float up = to_256(m);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int tok = tok0 + y * 4 + (lane >> 3);
+        uint4 t1, t2;
+        split16(v[y], up, bad[y], &t1, &t2);
+        unsigned char* dst = tile + tok * HD + ((c16 ^ (tok & 7)) << 4);
+        *reinterpret_cast<uint4*>(dst) = t1;
+        *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
+    }
+    if (lane == 0) *scale = 1.f / up;
+}
+// The same for V, in place as fp16 (exact down to 2^-21 of the largest of the sixteen tokens, 2^-32 of it absolutely).  NaN
+// and infinities become zeros -- they join the rows that see them at the segment's end -- and the call returns true.
+__device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale, int tok0) {
+    const int lane = threadIdx.x & 31, c16 = lane & 7;
+    float v[4][16];
+    uint32_t m = 0, any = 0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int tok = tok0 + y * 4 + (lane >> 3);
+        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 0), v[y]);
+        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 1), v[y] + 8);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t mag = quant::mag_bits(v[y][e]);
+            any = max(any, mag);
+            if (mag >= 0x7f800000u) v[y][e] = 0.f;
+            else m = max(m, mag);
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float up = to_256(m);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int tok = tok0 + y * 4 + (lane >> 3), c8 = (c16 & 3) * 2;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
+            w[e] = *reinterpret_cast<const uint32_t*>(&hv);
+        }
+        unsigned char* dst = tile + (c16 >> 2) * VH_HALF + tok * 128;
+        *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    if (lane == 0) *scale = 1.f / up;
+    return __any_sync(0xffffffffu, any >= 0x7f800000u);
 }
 
 // Columns of the bf16 tile (tail rows, then block rows) that a query row sees.
@@ -213,7 +281,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(bar(BAR_S_FULL + i), 2);
             mbar_init(bar(BAR_S_FREE + i), 4);
         }
-        mbar_init(bar(BAR_BT_FULL), 1);
+        mbar_init(bar(BAR_BT_FULL), 4);
         mbar_init(bar(BAR_BT_EMPTY), 1);
         for (int i = 0; i < 4; ++i) {
             mbar_init(bar(BAR_MEET + i), 2);
@@ -282,7 +350,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int pj = lane & 3, is_v = (lane >> 2) & 1;
             const int no_row = p.kv.num_pages * Hkv * PAGE;    // beyond the pool: reads as zero
             bool ok = true;
-            for (int si = 0; si < n_seg && ok; ++si) {
+            for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                 const Seg g = sh.segs[si];
                 const int kvh = g.hr / p.row_tiles, full = g.n / PAGE;
                 const int last_tile = (full + PAGES - 1) / PAGES;
@@ -296,6 +364,18 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (pg < 0 || pg >= p.kv.num_pages) return 0.f;
                     return __ldcg((is_v ? qp.kq.v_scale : qp.kq.k_scale) + (size_t)pg * Hkv + kvh);
                 };
+                // the segment's queries
+                {
+                    const int qb = sg & 1, i0 = rt * p.ipt;
+                    int okq = 1;
+                    if (lane == 0) okq = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                    if (!__shfl_sync(0xffffffffu, okq, 0)) { ok = false; break; }
+                    if (lane == 0) {
+                        mbar_expect_tx(bar(BAR_Q_RAW + qb), (uint32_t)(2 * p.G * min(p.ipt, p.k) * 128));
+                        tma_load_3d(q_addr + qb * Q_BYTES, &tm_q, 0, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
+                        tma_load_3d(q_addr + qb * Q_BYTES + Q_BYTES / 2, &tm_q, 64, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
+                    }
+                }
                 // page ids are fetched three tiles ahead, their scales two tiles ahead
                 int pg_cur = page_of(g.t_a), pg_next = page_of(g.t_a + 1), pg_third = page_of(g.t_a + 2);
                 float sc_cur = scale_of(pg_cur), sc_next = scale_of(pg_next);
@@ -398,110 +478,6 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                 }
             }
-        } else if (warp == 3) {
-            // ---------------- splitter ----------------
-            const int c16 = lane & 7;                                      // 16-dim piece of a row
-            bool ok = true;
-            for (int si = 0; si < n_seg && ok; ++si, ++sg) {
-                const Seg g = sh.segs[si];
-                const int kvh = g.hr / p.row_tiles, last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                const int qb = sg & 1;
-                ok = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const int i0 = rt * p.ipt, rows = min(p.ipt, p.k - i0) * p.G;
-                if (lane == 0) {
-                    mbar_expect_tx(bar(BAR_Q_RAW + qb), (uint32_t)(2 * p.G * min(p.ipt, p.k) * 128));
-                    tma_load_3d(q_addr + qb * Q_BYTES, &tm_q, 0, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
-                    tma_load_3d(q_addr + qb * Q_BYTES + Q_BYTES / 2, &tm_q, 64, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
-                }
-                if (sg > 0) {                                              // (the first segment's: the softmax warps, who have to wait anyway)
-                    ok = mbar_wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, rows, lane >> 3, 4);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane < 8) mbar_arrive(bar(BAR_Q_FULL + qb));
-                }
-                if (g.t_b != last_tile + 1) continue;
-                // the bf16 tile: tail rows, then block rows
-                ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                uint32_t present, decoded;
-                attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
-                const int n_tail = g.n % PAGE;
-                const size_t tail0 = (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (g.n / PAGE % 3) * PAGE) * HD;
-                int bad_v = 0;
-                // All rows as bf16 to where their split form will be, [dim half][64 tokens][128 B], zeros where there is no token;
-                // each lane copies what it will split.
-#pragma unroll 1
-                for (int x = 0; x < 2 * TILE; x += 4) {
-                    const bool is_v = x >= TILE;
-                    const int tok = (x & (TILE - 1)) + (lane >> 3), jb = tok - n_tail;
-                    const __nv_bfloat16* src = nullptr;
-                    if (tok < n_tail)
-                        src = static_cast<const __nv_bfloat16*>(is_v ? qp.kq.v_tail : qp.kq.k_tail) + tail0 + (size_t)tok * HD + c16 * 16;
-                    else if (jb < p.k && ((present >> jb) & 1u))
-                        src = (is_v ? p.v_blk : p.k_blk) + ((size_t)(g.b * p.k + jb) * Hkv + kvh) * HD + c16 * 16;
-                    unsigned char* tile = bt + (is_v ? 2 * T_BYTES : 0);
-                    cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 0)), src ? src : p.k_blk, src ? 16 : 0);
-                    cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 1)), src ? src + 8 : p.k_blk, src ? 16 : 0);
-                }
-                cp_async_commit();
-                cp_async_wait<0>();
-                __syncwarp();
-#pragma unroll 1
-                for (int x = 0; x < 2 * PAGES; ++x) {                      // 16 tokens at a time: K, then V
-                    const bool is_v = x >= PAGES;
-                    const int tok0 = (x & (PAGES - 1)) * PAGE + (lane >> 3);
-                    float v[4][16];
-                    uint32_t m = 0;
-                    bool bad[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const unsigned char* tile = bt + (is_v ? 2 * T_BYTES : 0);
-                        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok0 + y * 4, c16, 0), v[y]);
-                        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok0 + y * 4, c16, 1), v[y] + 8);
-                        bad[y] = quant::max8(quant::amax16(v[y])) >= 0x7f800000u;
-                        if (bad[y]) {                                      // K: the token's codes are NaN.  V: joins the rows that see it at the end
-                            bad_v |= is_v;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (quant::mag_bits(v[y][e]) >= 0x7f800000u) v[y][e] = 0.f;
-                        }
-                        m = max(m, quant::amax16(v[y]));
-                    }
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));      // (and every lane has read)
-                    const float up = to_256(m);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int tok = tok0 + y * 4, c8 = (c16 & 3) * 2;
-                        if (!is_v) {
-                            uint4 t1, t2;
-                            split16(v[y], up, bad[y], &t1, &t2);
-                            unsigned char* dst = bt + tok * HD + ((c16 ^ (tok & 7)) << 4);
-                            *reinterpret_cast<uint4*>(dst) = t1;
-                            *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
-                        } else {                                           // exact down to 2^-21 of the largest, 2^-32 of it absolutely
-                            uint32_t w[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
-                                w[e] = *reinterpret_cast<const uint32_t*>(&hv);
-                            }
-                            unsigned char* dst = bt + 2 * T_BYTES + (c16 >> 2) * VH_HALF + tok * 128;
-                            *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                            *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                        }
-                    }
-                    if (lane == 0) sh.bt_scale[x] = 1.f / up;
-                }
-                if (__any_sync(0xffffffffu, bad_v) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(BAR_BT_FULL));
-                ++nb;
-            }
         } else if (warp >= 12) {
             // ---------------- V to fp16: a thread takes four pieces of 16 codes of every page tile ----------------
             const int st = tid - 384, c16 = st & 7, c8 = (c16 & 3) * 2;
@@ -509,7 +485,43 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             for (int si = 0; si < n_seg && ok; ++si) {
                 const Seg g = sh.segs[si];
                 const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                for (int t = g.t_a; t < g.t_b && t < last_tile; ++t, ++rs) {
+                for (int t = g.t_a; t < g.t_b; ++t) {
+                    if (t == (g.t_a + 2 < last_tile ? g.t_a + 2 : last_tile) && g.t_b == last_tile + 1) {
+                        // The bf16 tile, as early as its buffer allows (two page tiles are on their way to O meanwhile): warp w
+                        // takes 16 tokens of K, then of V.
+                        const int w = warp - 12, kvh = g.hr / p.row_tiles, n_tail = g.n % PAGE;
+                        ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
+                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        uint32_t present, decoded;
+                        attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
+                        const size_t tail0 = (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (g.n / PAGE % 3) * PAGE) * HD;
+                        const size_t blk0 = ((size_t)g.b * p.k * Hkv + kvh) * HD;
+                        // rows as bf16 to where their split form will be, [dim half][64 tokens][128 B], zeros where there is no
+                        // token; each lane copies what it will split
+#pragma unroll 1
+                        for (int x = 0; x < 8; ++x) {
+                            const bool is_v = x >= 4;
+                            const int tok = w * PAGE + (x & 3) * 4 + (lane >> 3), jb = tok - n_tail;
+                            const __nv_bfloat16* src = nullptr;
+                            if (tok < n_tail)
+                                src = static_cast<const __nv_bfloat16*>(is_v ? qp.kq.v_tail : qp.kq.k_tail) + tail0 + (size_t)(tok * HD + c16 * 16);
+                            else if (jb < p.k && ((present >> jb) & 1u))
+                                src = (is_v ? p.v_blk : p.k_blk) + blk0 + (size_t)jb * Hkv * HD + c16 * 16;
+                            unsigned char* tile = bt + (is_v ? 2 * T_BYTES : 0);
+                            cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 0)), src ? src : p.k_blk, src ? 16 : 0);
+                            cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 1)), src ? src + 8 : p.k_blk, src ? 16 : 0);
+                        }
+                        cp_async_commit();
+                        cp_async_wait<0>();
+                        __syncwarp();
+                        split_keys(bt, sh.bt_scale + w, w * PAGE);
+                        if (values_to_f16(bt + 2 * T_BYTES, sh.bt_scale + PAGES + w, w * PAGE) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(BAR_BT_FULL));
+                        ++nb;
+                    }
+                    if (t == last_tile) break;
                     const int sl = rs % NSLOT, vb = rs & 1;
                     ok = mbar_wait(bar(BAR_V_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag) &&
                          mbar_wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs >> 1) & 1u) ^ 1u, abort_flag);
@@ -541,9 +553,10 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         mbar_arrive(bar(BAR_VH_FULL + vb));
                         mbar_arrive(bar(BAR_SLOT_EMPTY + sl));
                     }
+                    ++rs;
                 }
             }
-        } else {
+        } else if (warp >= 4) {
             // ---------------- softmax: one query row per thread, the group's tiles ----------------
             const int grp = (warp - 4) >> 2, quarter = warp & 3;
             const int row = quarter * 32 + lane;
@@ -556,13 +569,13 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float m_ref = 0.f, v_ref = 1.f, i_ref = 1.f, l_run = 0.f;
                 bool first = true;
                 const int qb = sg & 1;
-                if (sg == 0) {
-                    const bool raw = mbar_wait(bar(BAR_Q_RAW), 0u, abort_flag);
+                {
+                    const bool raw = mbar_wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, raw)) { alive = false; break; }
-                    split_queries(sQ, sh.q_factor[0], p.scale_log2, min(p.ipt, p.k - rt * p.ipt) * p.G, (warp - 4) * 4 + (lane >> 3), 32);
+                    split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, min(p.ipt, p.k - rt * p.ipt) * p.G, (warp - 4) * 4 + (lane >> 3), 32);
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(BAR_Q_FULL));
+                    if (lane == 0) mbar_arrive(bar(BAR_Q_FULL + qb));
                 }
                 {
                     const bool got = mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
