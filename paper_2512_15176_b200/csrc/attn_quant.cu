@@ -439,7 +439,7 @@ extern "C" size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, in
     // room for whichever kernel the call ends up using
     const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
     const size_t small = pl.chunks == 1 ? 16 : (size_t)pl.chunks * B * k * Hq * (D + 1) * sizeof(float);
-    if (!umma_supported(D, k, Hq / Hkv, 0, 1.f)) return small;
+    if (!umma_supported(D, k, Hq / Hkv, 1.f)) return small;
     const size_t large = umma_workspace_bytes(B, k, Hq, Hkv, max_seq_len);
     return large > small ? large : small;
 }
@@ -487,7 +487,7 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     p.row_tiles = pl.row_tiles;
     p.chunk_pages = pl.chunk_pages;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (umma_supported(D, k, p.G, (long long)kv->d.num_pages * Hkv * PAGE, scale)) return launch_umma(p, workspace, st);
+    if (umma_supported(D, k, p.G, scale)) return launch_umma(p, workspace, st);
     const dim3 grid((unsigned)pl.chunks, (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
     DEER_CUDA(launch_pdl(D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
     if (pl.chunks > 1)

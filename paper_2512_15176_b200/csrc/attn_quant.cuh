@@ -30,7 +30,7 @@ struct Params {
 constexpr int ROWS_SMALL = 16;   // query rows of a warp-level tile
 
 // tcgen05 variant (attn_quant_umma.cu).
-bool umma_supported(int D, int k, int G, long long pool_rows, float scale);
+bool umma_supported(int D, int k, int G, float scale);
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len);
 int launch_umma(const Params& p, void* workspace, cudaStream_t st);
 

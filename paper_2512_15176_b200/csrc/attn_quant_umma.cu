@@ -18,8 +18,8 @@
 // the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
 //
 // Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
-// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 TMA producer, 1 issuer of S, 2 issuer of
-// O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V to fp16 and the bf16 tile (warp 3: none).
+// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 loader of Q and K, 1 issuer of S and 3 its gate, 2 issuer
+// of O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V and the bf16 tile.
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 
 #include <cuda_fp16.h>
@@ -40,11 +40,12 @@ constexpr int HD = 128;
 constexpr int TILE = 64;                       // keys per tile
 constexpr int PAGES = TILE / PAGE;
 constexpr int T_BYTES = TILE * HD;             // one 8-bit operand tile, 8 KB
-constexpr int SLOT_BYTES = 2 * T_BYTES;        // K then V
-constexpr int NSLOT = 5;
-constexpr int NSCALE = 16;                      // page tiles whose scales are kept: the producer is at most NSLOT tiles ahead of
-                                               // the issuer of S, and that one NS ahead of the softmax, so none is overwritten too early
-constexpr int VH_BYTES = 2 * T_BYTES;          // V of a tile in fp16: [dim half][64 tokens][128 B]; two buffers
+constexpr int NK = 5;                          // ring slots of K tiles
+constexpr int VR_BYTES = 2 * PAGE * HD;        // a converting warp's two pages of a tile, as codes; two of them per warp
+constexpr int NVH = 3;                         // tiles of V in fp16
+constexpr int NSCALE = 16;                      // page tiles whose scales are kept: the loader of K is at most NK tiles ahead of the
+                                               // issuer of S, and that one NS ahead of the softmax, so none is overwritten too early
+constexpr int VH_BYTES = 2 * T_BYTES;          // V of a tile in fp16: [dim half][64 tokens][128 B]
 constexpr int VH_HALF = T_BYTES;
 constexpr int Q_BYTES = 2 * 128 * HD;          // both terms, 32 KB; two of them: the next segment's queries are split early
 constexpr int BT_BYTES = 2 * T_BYTES + VH_BYTES;   // bf16 tile: K terms, V in fp16
@@ -59,19 +60,19 @@ constexpr int BAR_Q_FULL = 0;                  // [2]  count 8: the softmax warp
 constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 9: the issuer of S, the softmax warps (they have read the factors)
 constexpr int BAR_BT_FULL = 4;                 // count 4: the warps that convert
 constexpr int BAR_BT_EMPTY = 5;                // the issuer of O
-constexpr int BAR_S_FULL = 6;                  // [NS]  count 2: the issuer's MMAs, and the issuer itself, who has seen the tile's scales arrive
+constexpr int BAR_S_FULL = 6;                  // [NS]  count 2: the issuer's MMAs, and the gate, who has seen the tile's scales arrive
 constexpr int BAR_S_FREE = BAR_S_FULL + NS;    // [NS]  count 4: the warps of the group that has the tile
 constexpr int BAR_P_READY = BAR_S_FREE + NS;   // [2]  count 4
 constexpr int BAR_O_DONE = BAR_P_READY + 2;    // [2]
 constexpr int BAR_MEET = BAR_O_DONE + 2;       // [4]  count 2: the two warps of a lane quarter
 constexpr int BAR_PART = BAR_MEET + 4;         // [4]  count 2
-constexpr int BAR_K_FULL = BAR_PART + 4;       // [NSLOT]
-constexpr int BAR_V_FULL = BAR_K_FULL + NSLOT;
-constexpr int BAR_SLOT_EMPTY = BAR_V_FULL + NSLOT;   // count 5: the issuer of S, the four warps that convert V
-constexpr int BAR_VH_FULL = BAR_SLOT_EMPTY + NSLOT;  // [2]  count 4
-constexpr int BAR_VH_EMPTY = BAR_VH_FULL + 2;        // [2]  the issuer of O
-constexpr int BAR_Q_RAW = BAR_VH_EMPTY + 2;          // [2]  the queries as bf16
-constexpr int N_BARS = BAR_Q_RAW + 2;
+constexpr int BAR_K_FULL = BAR_PART + 4;       // [NK]
+constexpr int BAR_K_EMPTY = BAR_K_FULL + NK;   // [NK]  the issuer of S
+constexpr int BAR_VH_FULL = BAR_K_EMPTY + NK;  // [NVH]  count 2: the two warps that convert the tile
+constexpr int BAR_VH_EMPTY = BAR_VH_FULL + NVH;      // [NVH]  the issuer of O
+constexpr int BAR_Q_RAW = BAR_VH_EMPTY + NVH;    // [2]  the queries as bf16
+constexpr int BAR_GO = BAR_Q_RAW + 2;          // [NS]  the gate: everything that S of a tile needs is there
+constexpr int N_BARS = BAR_GO + NS;
 
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
@@ -86,7 +87,7 @@ struct Shared {                                // behind the operand buffers
     long long cursor;
     Seg segs[MAX_SEGS];
 };
-constexpr int SMEM_BYTES = 2 * Q_BYTES + NSLOT * SLOT_BYTES + 2 * VH_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
+constexpr int SMEM_BYTES = 2 * Q_BYTES + NK * T_BYTES + 8 * VR_BYTES + NVH * VH_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
 
 struct QParams {
     AttnParams a;
@@ -172,26 +173,27 @@ __device__ __forceinline__ void split_queries(unsigned char* tile, float* factor
 // or an infinity gets NaN codes.  Whole-warp call, for rows that this warp's lanes have brought, each its pieces.
 __device__ __forceinline__ void split_keys(unsigned char* tile, float* scale, int tok0) {
     const int lane = threadIdx.x & 31, c16 = lane & 7;
-    float v[4][16];
-    bool bad[4];
     uint32_t m = 0;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int tok = tok0 + y * 4 + (lane >> 3);
-        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 0), v[y]);
-        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 1), v[y] + 8);
-        const uint32_t mt = quant::max8(quant::amax16(v[y]));
-        bad[y] = mt >= 0x7f800000u;
-        m = max(m, bad[y] ? 0u : mt);
-    }
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));                // (and every lane has read)
-    const float up = to_256(m);
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int tok = tok0 + y * 4 + (lane >> 3);
+    float up = 1.f;
+#pragma unroll 1
+    for (int x = 0; x < 8; ++x) {                                  // the largest magnitude of four rows four times, then their terms
+        const int tok = tok0 + (x & 3) * 4 + (lane >> 3);
+        float v[16];
+        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 0), v);
+        quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 1), v + 8);
+        const uint32_t mt = quant::max8(quant::amax16(v));         // (every lane of the row has read)
+        const bool bad = mt >= 0x7f800000u;
+        if (x < 4) {
+            m = max(m, bad ? 0u : mt);
+            if (x == 3) {
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                up = to_256(m);
+            }
+            continue;
+        }
         uint4 t1, t2;
-        split16(v[y], up, bad[y], &t1, &t2);
+        split16(v, up, bad, &t1, &t2);
         unsigned char* dst = tile + tok * HD + ((c16 ^ (tok & 7)) << 4);
         *reinterpret_cast<uint4*>(dst) = t1;
         *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
@@ -201,32 +203,34 @@ __device__ __forceinline__ void split_keys(unsigned char* tile, float* scale, in
 // The same for V, in place as fp16 (exact down to 2^-21 of the largest of the sixteen tokens, 2^-32 of it absolutely).  NaN
 // and infinities become zeros -- they join the rows that see them at the segment's end -- and the call returns true.
 __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale, int tok0) {
-    const int lane = threadIdx.x & 31, c16 = lane & 7;
-    float v[4][16];
+    const int lane = threadIdx.x & 31, c16 = lane & 7, c8 = (c16 & 3) * 2;
     uint32_t m = 0, any = 0;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int tok = tok0 + y * 4 + (lane >> 3);
-        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 0), v[y]);
-        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 1), v[y] + 8);
+    float up = 1.f;
+#pragma unroll 1
+    for (int x = 0; x < 8; ++x) {
+        const int tok = tok0 + (x & 3) * 4 + (lane >> 3);
+        float v[16];
+        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 0), v);
+        quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 1), v + 8);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const uint32_t mag = quant::mag_bits(v[y][e]);
+            const uint32_t mag = quant::mag_bits(v[e]);
             any = max(any, mag);
-            if (mag >= 0x7f800000u) v[y][e] = 0.f;
+            if (mag >= 0x7f800000u) v[e] = 0.f;
             else m = max(m, mag);
         }
-    }
+        if (x < 4) {
+            if (x == 3) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float up = to_256(m);
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int tok = tok0 + y * 4 + (lane >> 3), c8 = (c16 & 3) * 2;
+                for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                up = to_256(m);
+            }
+            continue;
+        }
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const __half2 hv = __floats2half2_rn(v[y][2 * e] * up, v[y][2 * e + 1] * up);
+            const __half2 hv = __floats2half2_rn(v[2 * e] * up, v[2 * e + 1] * up);
             w[e] = *reinterpret_cast<const uint32_t*>(&hv);
         }
         unsigned char* dst = tile + (c16 >> 2) * VH_HALF + tok * 128;
@@ -246,14 +250,14 @@ __device__ __forceinline__ uint64_t columns_seen(const AttnParams& p, const Seg&
 }
 
 __global__ void __launch_bounds__(THREADS, 1)
-attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                       const QParams qp) {
+attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const QParams qp) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* sQ = smem;                                  // [2 buffers][2 terms][128 rows][128 B]
-    unsigned char* ring = sQ + 2 * Q_BYTES;                    // [NSLOT][K, V][64 tokens][128 B]
-    unsigned char* vh = ring + NSLOT * SLOT_BYTES;             // [2]
-    unsigned char* bt = vh + 2 * VH_BYTES;                     // [K term 1, K term 2][64][128 B], V
+    unsigned char* ring = sQ + 2 * Q_BYTES;                    // [NK][64 tokens][128 B]
+    unsigned char* vraw = ring + NK * T_BYTES;                 // [4 warps][2][2 pages][16 tokens][128 B]
+    unsigned char* vh = vraw + 8 * VR_BYTES;                   // [NVH]
+    unsigned char* bt = vh + NVH * VH_BYTES;                     // [K term 1, K term 2][64][128 B], V
     Shared& sh = *reinterpret_cast<Shared*>(bt + BT_BYTES);
     volatile int* abort_flag = &sh.abort_flag;
     const AttnParams& p = qp.a;
@@ -274,12 +278,11 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(bar(BAR_Q_EMPTY + i), 9);
             mbar_init(bar(BAR_P_READY + i), 4);
             mbar_init(bar(BAR_O_DONE + i), 1);
-            mbar_init(bar(BAR_VH_FULL + i), 4);
-            mbar_init(bar(BAR_VH_EMPTY + i), 1);
         }
         for (int i = 0; i < NS; ++i) {
             mbar_init(bar(BAR_S_FULL + i), 2);
             mbar_init(bar(BAR_S_FREE + i), 4);
+            mbar_init(bar(BAR_GO + i), 1);
         }
         mbar_init(bar(BAR_BT_FULL), 4);
         mbar_init(bar(BAR_BT_EMPTY), 1);
@@ -287,17 +290,18 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(bar(BAR_MEET + i), 2);
             mbar_init(bar(BAR_PART + i), 2);
         }
-        for (int i = 0; i < NSLOT; ++i) {
+        for (int i = 0; i < NVH; ++i) {
+            mbar_init(bar(BAR_VH_FULL + i), 2);
+            mbar_init(bar(BAR_VH_EMPTY + i), 1);
+        }
+        for (int i = 0; i < NK; ++i) {
             mbar_init(bar(BAR_K_FULL + i), 1);
-            mbar_init(bar(BAR_V_FULL + i), 1);
-            mbar_init(bar(BAR_SLOT_EMPTY + i), 5);
+            mbar_init(bar(BAR_K_EMPTY + i), 1);
         }
         sh.abort_flag = 0;
         sh.bt_bad[0] = sh.bt_bad[1] = 0;
         mbar_init_fence();
         prefetch_tensormap(&tm_q);
-        prefetch_tensormap(&tm_k);
-        prefetch_tensormap(&tm_v);
     }
     pdl_trigger();
     pdl_wait();
@@ -327,7 +331,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 
     // Counters that run across segments and rounds; every role advances its own copy identically.
     int it = 0;          // tiles so far: group it & 1, that group's phase it >> 1; S buffer it % NS, its phase it / NS
-    int rs = 0;          // page tiles so far: ring slot rs % NSLOT, fp16 buffer rs & 1
+    int rs = 0;          // page tiles so far: ring slot rs % NK, fp16 buffer rs % NVH
     int nb = 0;          // bf16 tiles so far
     int sg = 0;          // segments so far: Q buffer sg & 1
     long long cursor = share_lo;
@@ -346,65 +350,89 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         cursor = sh.cursor;
 
         if (warp == 0) {
-            // ---------------- TMA producer: lanes 0..3 the pages of K, 4..7 those of V ----------------
-            const int pj = lane & 3, is_v = (lane >> 2) & 1;
-            const int no_row = p.kv.num_pages * Hkv * PAGE;    // beyond the pool: reads as zero
+            // ---------------- loader of Q (TMA, as bf16) and K ----------------
+            // (A page is a copy of its own, and a warp gets one out every ~200 cycles: it could not bring V as well.)
             bool ok = true;
             for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                 const Seg g = sh.segs[si];
                 const int kvh = g.hr / p.row_tiles, full = g.n / PAGE;
                 const int last_tile = (full + PAGES - 1) / PAGES;
                 const int32_t* pt_row = p.kv.page_table + (size_t)g.s * p.kv.max_pages;
-                auto page_of = [&](int t) -> int {
-                    const int lp = t * PAGES + pj;
-                    if (lane >= 8 || t >= g.t_b || lp >= full) return -2;          // nothing there
-                    return lp < p.kv.max_pages ? pt_row[lp] : -1;
-                };
-                auto scale_of = [&](int pg) -> float {
-                    if (pg < 0 || pg >= p.kv.num_pages) return 0.f;
-                    return __ldcg((is_v ? qp.kq.v_scale : qp.kq.k_scale) + (size_t)pg * Hkv + kvh);
-                };
-                // the segment's queries
                 {
-                    const int qb = sg & 1, i0 = rt * p.ipt;
+                    const int qb = sg & 1;
                     int okq = 1;
                     if (lane == 0) okq = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag) ? 1 : 0;
                     if (!__shfl_sync(0xffffffffu, okq, 0)) { ok = false; break; }
                     if (lane == 0) {
                         mbar_expect_tx(bar(BAR_Q_RAW + qb), (uint32_t)(2 * p.G * min(p.ipt, p.k) * 128));
-                        tma_load_3d(q_addr + qb * Q_BYTES, &tm_q, 0, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
-                        tma_load_3d(q_addr + qb * Q_BYTES + Q_BYTES / 2, &tm_q, 64, kvh * p.G, g.b * p.k + i0, bar(BAR_Q_RAW + qb));
+                        tma_load_3d(q_addr + qb * Q_BYTES, &tm_q, 0, kvh * p.G, g.b * p.k + rt * p.ipt, bar(BAR_Q_RAW + qb));
+                        tma_load_3d(q_addr + qb * Q_BYTES + Q_BYTES / 2, &tm_q, 64, kvh * p.G, g.b * p.k + rt * p.ipt, bar(BAR_Q_RAW + qb));
+                    }
+                    __syncwarp();
+                }
+                // Page ids and scales, eight tiles at a time: lane l holds page l of the eight tiles; the scales are fetched a batch
+                // ahead, the ids they need two.  (Tile by tile their latencies, one behind the other, would set the pace.)
+                auto ids_at = [&](int t0) -> int {
+                    const int lp = t0 * PAGES + lane;
+                    if (t0 + lane / PAGES >= g.t_b || lp >= full) return -2;       // nothing there
+                    return lp < p.kv.max_pages ? pt_row[lp] : -1;
+                };
+                auto scale_of = [&](const float* scales, int pg) -> float {
+                    return pg < 0 || pg >= p.kv.num_pages ? 0.f : __ldcg(scales + (size_t)pg * Hkv + kvh);
+                };
+                int id_cur = ids_at(g.t_a), id_next = ids_at(g.t_a + 8), id_third = ids_at(g.t_a + 16);
+                float ks_cur = scale_of(qp.kq.k_scale, id_cur), vs_cur = scale_of(qp.kq.v_scale, id_cur);
+                float ks_next = scale_of(qp.kq.k_scale, id_next), vs_next = scale_of(qp.kq.v_scale, id_next);
+                const int t_end = min(g.t_b, last_tile);
+                for (int t = g.t_a; t < t_end; ++t) {
+                    if (t < t_end) {
+                        const int sl = rs % NK, at = (t - g.t_a) & 7;
+                        if (at == 0 && t != g.t_a) {
+                            id_cur = id_next;
+                            ks_cur = ks_next;
+                            vs_cur = vs_next;
+                            id_next = id_third;
+                            ks_next = scale_of(qp.kq.k_scale, id_next);
+                            vs_next = scale_of(qp.kq.v_scale, id_next);
+                            id_third = ids_at(t + 16);
+                        }
+                        const float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3)), vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
+                        int oks = 1;
+                        if (lane == 0) oks = mbar_wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                        if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
+                        if (lane < 8) sh.scales[rs % NSCALE][lane] = lane < 4 ? ks : vs;
+                        __syncwarp();
+                        if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);
+                        __syncwarp();
+                        int pg = __shfl_sync(0xffffffffu, id_cur, at * PAGES + (lane & 3));
+                        if (lane < 4) {
+                            if (pg != -2 && (pg < 0 || pg >= p.kv.num_pages)) { deer_report(p.kv.status, DEER_ERR_BAD_PAGE); pg = -2; }
+                            tma_load_2d(ring_addr + sl * T_BYTES + lane * PAGE * HD, &tm_k, 0, pg == -2 ? p.kv.num_pages * Hkv * PAGE : (pg * Hkv + kvh) * PAGE, bar(BAR_K_FULL + sl));
+                        }
+                        ++rs;
                     }
                 }
-                // page ids are fetched three tiles ahead, their scales two tiles ahead
-                int pg_cur = page_of(g.t_a), pg_next = page_of(g.t_a + 1), pg_third = page_of(g.t_a + 2);
-                float sc_cur = scale_of(pg_cur), sc_next = scale_of(pg_next);
-                for (int t = g.t_a; t < g.t_b && t < last_tile; ++t, ++rs) {
-                    const int sl = rs % NSLOT;
-                    int pg = pg_cur;
-                    const float sc = sc_cur;
-                    pg_cur = pg_next;
-                    pg_next = pg_third;
-                    pg_third = page_of(t + 3);
-                    sc_cur = sc_next;
-                    sc_next = scale_of(pg_next);
-                    int oks = 1;
-                    if (lane == 0) oks = mbar_wait(bar(BAR_SLOT_EMPTY + sl), ((uint32_t)(rs / NSLOT) & 1u) ^ 1u, abort_flag) ? 1 : 0;
-                    if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
-                    if (lane < 8) sh.scales[rs % NSCALE][lane] = sc;
-                    __syncwarp();
-                    if (lane == 0) {                                       // (the arrivals publish the scales as well)
-                        mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);
-                        mbar_expect_tx(bar(BAR_V_FULL + sl), T_BYTES);
-                    }
-                    __syncwarp();
-                    if (lane < 8) {
-                        if (pg != -2 && (pg < 0 || pg >= p.kv.num_pages)) {
-                            deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
-                            pg = -2;
+            }
+        } else if (warp == 3) {
+            // ---------------- gate of S: does the issuer's waiting (a wait takes 100 cycles and more even when it need not wait) ----------------
+            if (lane == 0) {
+                bool ok = true;
+                for (int si = 0; si < n_seg && ok; ++si, ++sg) {
+                    const Seg g = sh.segs[si];
+                    const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                    if (!mbar_wait(bar(BAR_Q_FULL + (sg & 1)), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
+                    for (int t = g.t_a; t < g.t_b; ++t, ++it) {
+                        const int sb = it % NS;
+                        const bool blk = t == last_tile;
+                        if (!mbar_wait(blk ? bar(BAR_BT_FULL) : bar(BAR_K_FULL + rs % NK), (uint32_t)(blk ? nb : rs / NK) & 1u, abort_flag) ||
+                            !mbar_wait(bar(BAR_S_FREE + sb), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag)) {
+                            ok = false;
+                            break;
                         }
-                        tma_load_2d(ring_addr + sl * SLOT_BYTES + is_v * T_BYTES + pj * PAGE * HD, is_v ? &tm_v : &tm_k, 0,
-                                    pg == -2 ? no_row : (pg * Hkv + kvh) * PAGE, bar((is_v ? BAR_V_FULL : BAR_K_FULL) + sl));
+                        mbar_arrive(bar(BAR_GO + sb));
+                        mbar_arrive(bar(BAR_S_FULL + sb));
+                        if (blk) ++nb;
+                        else ++rs;
                     }
                 }
             }
@@ -417,35 +445,30 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const Seg g = sh.segs[si];
                     const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
                     const int qb = sg & 1;
-                    if (!mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
                     const uint64_t qd = smem_desc_sw128_kmajor(q_addr + qb * Q_BYTES);
                     for (int t = g.t_a; t < g.t_b; ++t, ++it) {
                         const int sb = it % NS;
                         const uint32_t d_tmem = tmem_base + (uint32_t)(sb * TILE);
-                        if (!mbar_wait(bar(BAR_S_FREE + sb), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait(bar(BAR_GO + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
+                        tcgen05_fence_after();
                         if (t != last_tile) {
-                            const int sl = rs % NSLOT;
-                            if (!mbar_wait(bar(BAR_K_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag)) { ok = false; break; }
-                            tcgen05_fence_after();
-                            const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * SLOT_BYTES);
+                            const int sl = rs % NK;
+                            const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * T_BYTES);
 #pragma unroll
                             for (int kk = 0; kk < 8; ++kk)                 // four steps of 32 dims for each term of Q
                                 umma_f8_ss(d_tmem, qd + (uint64_t)(((kk >> 2) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4), kd + (uint64_t)((kk & 3) * 2),
                                            idesc, kk != 0 ? 1u : 0u);
-                            umma_commit(bar(BAR_SLOT_EMPTY + sl));
+                            umma_commit(bar(BAR_S_FULL + sb));
+                            umma_commit(bar(BAR_K_EMPTY + sl));
                             ++rs;
                         } else {
-                            if (!mbar_wait(bar(BAR_BT_FULL), (uint32_t)nb & 1u, abort_flag)) { ok = false; break; }
-                            tcgen05_fence_after();
                             const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
 #pragma unroll
                             for (int kk = 0; kk < 16; ++kk)                // and for each term of K
                                 umma_f8_ss(d_tmem, qd + (uint64_t)((((kk >> 2) & 1) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
                                            kd + (uint64_t)(((kk >> 3) * T_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0 ? 1u : 0u);
-                            ++nb;
+                            umma_commit(bar(BAR_S_FULL + sb));
                         }
-                        umma_commit(bar(BAR_S_FULL + sb));
-                        mbar_arrive(bar(BAR_S_FULL + sb));
                     }
                     if (ok) umma_commit(bar(BAR_Q_EMPTY + qb));
                 }
@@ -463,8 +486,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(P_COL + grp * P_COLS);
                         const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
                         const bool blk = t == last_tile;
-                        const int vb = rs & 1;
-                        if (!blk && !mbar_wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs >> 1) & 1u, abort_flag)) { ok = false; break; }
+                        const int vb = rs % NVH;
+                        if (!blk && !mbar_wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) { ok = false; break; }
                         if (!mbar_wait(bar(BAR_P_READY + grp), (uint32_t)(it >> 1) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();                             // (a bf16 tile was full before its S)
                         // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
@@ -479,17 +502,49 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
             }
         } else if (warp >= 12) {
-            // ---------------- V to fp16: a thread takes four pieces of 16 codes of every page tile ----------------
-            const int st = tid - 384, c16 = st & 7, c8 = (c16 & 3) * 2;
+            // ---------------- V to fp16, and the bf16 tile ----------------
+            // Warps 12, 13 take the even page tiles, 14, 15 the odd ones, two pages each: codes to a buffer of the warp's own (each
+            // lane copies what it will convert; two tiles of its own ahead within a segment), from there as fp16 to the operand tile.
+            const int w = warp - 12, c16 = lane & 7, c8 = (c16 & 3) * 2, mine = w >> 1, pair = (w & 1) * 2;
+            unsigned char* my_raw = vraw + w * 2 * VR_BYTES;
             bool ok = true;
             for (int si = 0; si < n_seg && ok; ++si) {
                 const Seg g = sh.segs[si];
-                const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
+                const int kvh = g.hr / p.row_tiles, full = g.n / PAGE, last_tile = (full + PAGES - 1) / PAGES;
+                const int32_t* pt_row = p.kv.page_table + (size_t)g.s * p.kv.max_pages;
+                const int t_end = min(g.t_b, last_tile), t_first = g.t_a + ((rs ^ mine) & 1);       // this warp's first tile of the segment
+                auto ids_at = [&](int t0) -> int {                         // lane l: page `pair` + (l & 1) of tile t0 + (l & ~1)
+                    const int t = t0 + (lane & ~1), lp = t * PAGES + pair + (lane & 1);
+                    return t < t_end && lp < full && lp < p.kv.max_pages ? pt_row[lp] : -1;
+                };
+                int id_cur = ids_at(t_first), id_next = ids_at(t_first + 32), t_next = t_first;
+                auto fetch = [&](int buf) {                                // this warp's next tile to its buffer; zeros for a page that is not there
+                    const int at = (t_next - t_first) & 31;
+                    if (at == 0 && t_next != t_first) {
+                        id_cur = id_next;
+                        id_next = ids_at(t_next + 32);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int pg = __shfl_sync(0xffffffffu, id_cur, at + h);
+                        const bool there = pg >= 0 && pg < p.kv.num_pages;
+                        const unsigned char* src = static_cast<const unsigned char*>(p.kv.v_pool) + ((size_t)(there ? pg : 0) * Hkv + kvh) * PAGE * HD + lane * 16;
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            cp_async16(smem_u32(my_raw + buf * VR_BYTES) + (uint32_t)(h * PAGE * HD + y * 512 + lane * 16), src + y * 512, there ? 16 : 0);
+                    }
+                    cp_async_commit();
+                    t_next += 2;
+                };
+                int buf = 0;
+                cp_async_wait<0>();                                        // (copies that the last segment asked for beyond its end)
+                fetch(0);
+                fetch(1);
                 for (int t = g.t_a; t < g.t_b; ++t) {
                     if (t == (g.t_a + 2 < last_tile ? g.t_a + 2 : last_tile) && g.t_b == last_tile + 1) {
                         // The bf16 tile, as early as its buffer allows (two page tiles are on their way to O meanwhile): warp w
                         // takes 16 tokens of K, then of V.
-                        const int w = warp - 12, kvh = g.hr / p.row_tiles, n_tail = g.n % PAGE;
+                        const int n_tail = g.n % PAGE;
                         ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         uint32_t present, decoded;
@@ -512,7 +567,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             cp_async16(smem_u32(piece(tile, T_BYTES, tok, c16, 1)), src ? src + 8 : p.k_blk, src ? 16 : 0);
                         }
                         cp_async_commit();
-                        cp_async_wait<0>();
+                        cp_async_wait<0>();                                // (and whatever V is on its way)
                         __syncwarp();
                         split_keys(bt, sh.bt_scale + w, w * PAGE);
                         if (values_to_f16(bt + 2 * T_BYTES, sh.bt_scale + PAGES + w, w * PAGE) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
@@ -522,36 +577,32 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         ++nb;
                     }
                     if (t == last_tile) break;
-                    const int sl = rs % NSLOT, vb = rs & 1;
-                    ok = mbar_wait(bar(BAR_V_FULL + sl), (uint32_t)(rs / NSLOT) & 1u, abort_flag) &&
-                         mbar_wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs >> 1) & 1u) ^ 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    const unsigned char* src = ring + sl * SLOT_BYTES + T_BYTES;
-                    unsigned char* dst = vh + vb * VH_BYTES + (c16 >> 2) * VH_HALF;
-                    uint4 codes[4];
+                    if ((rs & 1) == mine) {
+                        const int vb = rs % NVH;
+                        ok = mbar_wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs / NVH) & 1u) ^ 1u, abort_flag);
+                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        cp_async_wait<1>();
+                        unsigned char* dst = vh + vb * VH_BYTES + (c16 >> 2) * VH_HALF;
+                        const uint4* src = reinterpret_cast<const uint4*>(my_raw + buf * VR_BYTES) + lane;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int tok = (st >> 3) + x * 16;
-                        codes[x] = *reinterpret_cast<const uint4*>(src + tok * HD + ((c16 ^ (tok & 7)) << 4));
-                    }
+                        for (int x = 0; x < 8; ++x) {
+                            const int tok = (pair + (x >> 2)) * PAGE + (x & 3) * 4 + (lane >> 3);
+                            const uint4 codes = src[x * 32];
+                            const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
+                            uint32_t f[8];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int tok = (st >> 3) + x * 16;
-                        const uint32_t w[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
-                        uint32_t f[8];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            f[2 * e] = codes_lo(w[e]);
-                            f[2 * e + 1] = codes_hi(w[e]);
+                            for (int e = 0; e < 4; ++e) {
+                                f[2 * e] = codes_lo(cw[e]);
+                                f[2 * e + 1] = codes_hi(cw[e]);
+                            }
+                            *reinterpret_cast<uint4*>(dst + tok * 128 + ((c8 ^ (tok & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
+                            *reinterpret_cast<uint4*>(dst + tok * 128 + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
                         }
-                        *reinterpret_cast<uint4*>(dst + tok * 128 + ((c8 ^ (tok & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-                        *reinterpret_cast<uint4*>(dst + tok * 128 + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar(BAR_VH_FULL + vb));
-                        mbar_arrive(bar(BAR_SLOT_EMPTY + sl));
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(BAR_VH_FULL + vb));
+                        fetch(buf);
+                        buf ^= 1;
                     }
                     ++rs;
                 }
@@ -843,8 +894,8 @@ static int pick_blocks(int B, int Hkv, int row_tiles, int max_seq_len) {
 
 // More query rows than a warp's tile of 16 hold share the KV stream here; fewer leave the 128 lanes idle while the
 // warp-level kernel reads the same bytes with less latency.
-bool umma_supported(int D, int k, int G, long long pool_rows, float scale) {
-    return D == umma::HD && G <= 128 && k * G > ROWS_SMALL && pool_rows < (1LL << 31) - 16 && scale > 0.f;
+bool umma_supported(int D, int k, int G, float scale) {
+    return D == umma::HD && G <= 128 && k * G > ROWS_SMALL && scale > 0.f;
 }
 
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len) {
@@ -882,7 +933,7 @@ int launch_umma(const Params& q, void* workspace, cudaStream_t st) {
     p.part_lse = p.part_o + slots * 128 * HD;
     p.total_tiles = reinterpret_cast<long long*>(p.part_lse + slots * 128);
     p.unit_parts = reinterpret_cast<int2*>(p.total_tiles + 1);
-    CUtensorMap tm_q, tm_k, tm_v;
+    CUtensorMap tm_q, tm_k;
     const uint64_t dims[2] = {HD, (uint64_t)p.kv.num_pages * Hkv * PAGE}, str[1] = {HD};
     const uint32_t box[2] = {HD, PAGE};
     // q [B*k][Hq][128]: a box brings G heads of box_i block rows, 64 dims wide -> shared-memory row = i * G + g
@@ -892,10 +943,8 @@ int launch_umma(const Params& q, void* workspace, cudaStream_t st) {
     if (rc != DEER_OK) return rc;
     rc = make_map_u8(&tm_k, p.kv.k_pool, 2, dims, str, box);
     if (rc != DEER_OK) return rc;
-    rc = make_map_u8(&tm_v, p.kv.v_pool, 2, dims, str, box);
-    if (rc != DEER_OK) return rc;
     DEER_CUDA(cudaFuncSetAttribute(attn_quant_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
-    DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_k, tm_v, qp));
+    DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_k, qp));
     return attn::launch_umma_merge(p, st);
 }
 
