@@ -44,15 +44,15 @@ constexpr int NK = 5;                          // ring slots of K tiles
 constexpr int VR_BYTES = 2 * PAGE * HD;        // a converting warp's two pages of a tile, as codes; two of them per warp
 constexpr int NVH = 3;                         // tiles of V in fp16
 constexpr int NSCALE = 16;                      // page tiles whose scales are kept: the loader of K is at most NK tiles ahead of the
-                                               // issuer of S, and that one NS ahead of the softmax, so none is overwritten too early
+                                               // issuer of S, and that one NS ahead of O, so none is overwritten too early
 constexpr int VH_BYTES = 2 * T_BYTES;          // V of a tile in fp16: [dim half][64 tokens][128 B]
 constexpr int VH_HALF = T_BYTES;
 constexpr int Q_BYTES = 2 * 128 * HD;          // both terms, 32 KB; two of them: the next segment's queries are split early
 constexpr int BT_BYTES = 2 * T_BYTES + VH_BYTES;   // bf16 tile: K terms, V in fp16
 constexpr int THREADS = 512;
-constexpr int TMEM_COLS = 512;                 // S [b * 64, +64) b < 3  P [192 + g * 32, +32)  O [256 + g * 128, +128)
-constexpr int NS = 3;                          // S buffers: the next two tiles' scores are ready while a tile's are being read
-constexpr int P_COL = NS * TILE, P_COLS = 32, O_COL = 256;
+constexpr int TMEM_COLS = 512;                 // S, and P in its place (columns 0..31 of it): [b * 64, +64) b < 4;  O [256 + g * 128, +128)
+constexpr int NS = 4;                          // a tile's buffer is free once O has taken P from it
+constexpr int O_COL = 256;
 constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^35 above fp16's last bit
 
 // mbarrier indices
@@ -61,9 +61,9 @@ constexpr int BAR_Q_EMPTY = 2;                 // [2]  count 9: the issuer of S,
 constexpr int BAR_BT_FULL = 4;                 // count 4: the warps that convert
 constexpr int BAR_BT_EMPTY = 5;                // the issuer of O
 constexpr int BAR_S_FULL = 6;                  // [NS]  count 2: the issuer's MMAs, and the gate, who has seen the tile's scales arrive
-constexpr int BAR_S_FREE = BAR_S_FULL + NS;    // [NS]  count 4: the warps of the group that has the tile
-constexpr int BAR_P_READY = BAR_S_FREE + NS;   // [2]  count 4
-constexpr int BAR_O_DONE = BAR_P_READY + 2;    // [2]
+constexpr int BAR_S_FREE = BAR_S_FULL + NS;    // [NS]  the issuer of O
+constexpr int BAR_P_READY = BAR_S_FREE + NS;   // [NS]  count 4: the warps of the group that has the tile
+constexpr int BAR_O_DONE = BAR_P_READY + NS;   // [2]   per group
 constexpr int BAR_MEET = BAR_O_DONE + 2;       // [4]  count 2: the two warps of a lane quarter
 constexpr int BAR_PART = BAR_MEET + 4;         // [4]  count 2
 constexpr int BAR_K_FULL = BAR_PART + 4;       // [NK]
@@ -72,7 +72,8 @@ constexpr int BAR_VH_FULL = BAR_K_EMPTY + NK;  // [NVH]  count 2: the two warps 
 constexpr int BAR_VH_EMPTY = BAR_VH_FULL + NVH;      // [NVH]  the issuer of O
 constexpr int BAR_Q_RAW = BAR_VH_EMPTY + NVH;    // [2]  the queries as bf16
 constexpr int BAR_GO = BAR_Q_RAW + 2;          // [NS]  the gate: everything that S of a tile needs is there
-constexpr int N_BARS = BAR_GO + NS;
+constexpr int BAR_SEG = BAR_GO + NS;           // the issuer of O: a segment's products are all in O
+constexpr int N_BARS = BAR_SEG + 1;
 
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
@@ -276,16 +277,17 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(bar(BAR_Q_FULL + i), 8);
             mbar_init(bar(BAR_Q_RAW + i), 1);
             mbar_init(bar(BAR_Q_EMPTY + i), 9);
-            mbar_init(bar(BAR_P_READY + i), 4);
             mbar_init(bar(BAR_O_DONE + i), 1);
         }
         for (int i = 0; i < NS; ++i) {
             mbar_init(bar(BAR_S_FULL + i), 2);
-            mbar_init(bar(BAR_S_FREE + i), 4);
+            mbar_init(bar(BAR_S_FREE + i), 1);
+            mbar_init(bar(BAR_P_READY + i), 4);
             mbar_init(bar(BAR_GO + i), 1);
         }
         mbar_init(bar(BAR_BT_FULL), 4);
         mbar_init(bar(BAR_BT_EMPTY), 1);
+        mbar_init(bar(BAR_SEG), 1);
         for (int i = 0; i < 4; ++i) {
             mbar_init(bar(BAR_MEET + i), 2);
             mbar_init(bar(BAR_PART + i), 2);
@@ -483,22 +485,25 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
                     for (int t = g.t_a; t < g.t_b; ++t, ++it) {
                         const int grp = it & 1;
-                        const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(P_COL + grp * P_COLS);
+                        const int sb = it % NS;
+                        const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(sb * TILE);
                         const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
                         const bool blk = t == last_tile;
                         const int vb = rs % NVH;
                         if (!blk && !mbar_wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) { ok = false; break; }
-                        if (!mbar_wait(bar(BAR_P_READY + grp), (uint32_t)(it >> 1) & 1u, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait(bar(BAR_P_READY + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();                             // (a bf16 tile was full before its S)
                         // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
                         const uint64_t vd = smem_desc_sw128(blk ? bt_addr + 2 * T_BYTES : vh_addr + vb * VH_BYTES, VH_HALF, 1024);
 #pragma unroll
                         for (int kk = 0; kk < TILE / 16; ++kk)
                             umma_bf16_ts(o_tmem, p_tmem + (uint32_t)(kk * 8), vd + (uint64_t)((kk * 2048) >> 4), idesc, kk != 0 ? 1u : keep);
+                        umma_commit(bar(BAR_S_FREE + sb));
                         umma_commit(bar(BAR_O_DONE + grp));
                         umma_commit(blk ? bar(BAR_BT_EMPTY) : bar(BAR_VH_EMPTY + vb));
                         if (!blk) ++rs;
                     }
+                    if (ok) umma_commit(bar(BAR_SEG));
                 }
             }
         } else if (warp >= 12) {
@@ -612,7 +617,6 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int grp = (warp - 4) >> 2, quarter = warp & 3;
             const int row = quarter * 32 + lane;
             const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
-            const uint32_t p_tmem = t_lane + (uint32_t)(P_COL + grp * P_COLS);
             bool alive = true;
             for (int si = 0; si < n_seg && alive; ++si, ++sg) {
                 const Seg& g = sh.segs[si];
@@ -643,11 +647,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if ((it & 1) != grp) continue;
                     const int n_pages = is_bt ? PAGES : min(PAGES, full - t * PAGES);
                     const uint32_t s_tmem = t_lane + (uint32_t)(sb * TILE);
-                    // The group's previous tile is in O (phase (it >> 1) - 1), so its P may be overwritten; the scores, and with them
-                    // the scales.  (Not K_FULL or BT_FULL for those: a slot may be on its next tile but one by now, and a parity
-                    // wait cannot tell.)
-                    const bool got = (it < 2 || mbar_wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) &&
-                                     mbar_wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
+                    // The scores, and with them the scales.  (Not K_FULL or BT_FULL for those: a slot may be on its next tile but one
+                    // by now, and a parity wait cannot tell.)
+                    const bool got = mbar_wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                     tcgen05_fence_after();
                     uint64_t see = 0;
@@ -669,9 +671,10 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         }
                     };
                     // The group's first tile sets the references.  Later a weight of 2^15 (0x7800 in fp16) or a sum of 2^40 raises
-                    // them: O and l shrink in place, the tile is done again (its scores are still there).
-                    bool set = first;
+                    // them: O and l shrink in place, the tile is done again (P has not taken the scores' place yet).
+                    bool set = first, stop = false;
                     float tile_sum;
+                    uint32_t pr[TILE / 2];
 #pragma unroll 1
                     for (int pass = 0; pass < 2; ++pass) {
                         if (set) {
@@ -695,6 +698,11 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 m_t = fmaxf(m_t, m_ref);
                                 v_t = fmaxf(v_t, v_ref);
                                 const float al = ex2_approx(m_ref - m_t), ao = al * (v_ref / v_t);
+                                // phase (it >> 1) - 1 of o_done: the group's previous tile is in O.  (The one before it is: its
+                                // buffer is the one that this tile's scores are in.)
+                                const bool od = mbar_wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
+                                if (!__all_sync(0xffffffffu, od)) { stop = true; break; }
+                                tcgen05_fence_after();
 #pragma unroll 1
                                 for (int cc = 0; cc < HD / 16; ++cc) {
                                     uint32_t o[16];
@@ -714,10 +722,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         // weights 2^(score - m_ref + 11), and in fp16 those times V scale / v_ref
                         uint64_t sum2[2] = {0, 0};
                         __half2 top2 = __float2half2_rn(0.f);
-#pragma unroll 1
+#pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             load_half(h);
-                            uint32_t pr[16];
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
                                 const float nm = h * 2 + x < n_pages ? BIAS - m_ref : -INFINITY;
@@ -734,10 +741,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                     unpack_f32x2(mul2(p2, va2), w0, w1);
                                     const __half2 hw = __floats2half2_rn(w0, w1);
                                     top2 = __hmax2(top2, hw);
-                                    pr[c >> 1] = *reinterpret_cast<const uint32_t*>(&hw);
+                                    pr[h * 16 + (c >> 1)] = *reinterpret_cast<const uint32_t*>(&hw);
                                 }
                             }
-                            TMEM_ST_X16(p_tmem + (uint32_t)(h * 16), pr);
                         }
                         float a, b;
                         unpack_f32x2(add2(sum2[0], sum2[1]), a, b);
@@ -746,26 +752,22 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         set = __any_sync(0xffffffffu, max(tb & 0x7fffu, (tb >> 16) & 0x7fffu) >= 0x7800u || !(tile_sum < 1.0995116e12f));
                         if (first || !set) break;
                     }
+                    if (stop) { alive = false; break; }
                     first = false;
                     l_run += tile_sum;
+                    TMEM_ST_X32(s_tmem, pr);
                     tmem_wait_st();
                     tcgen05_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar(BAR_P_READY + grp));
-                        mbar_arrive(bar(BAR_S_FREE + sb));
-                    }
+                    if (lane == 0) mbar_arrive(bar(BAR_P_READY + sb));
                 }
                 if (!alive) break;
                 if (t_b == last_tile + 1) ++nb;
 
                 // ---- the segment's result: the groups meet; each takes half of the columns of both accumulators ----
-                if (!first) {
-                    // the last tile of this group in the segment is tile number `last_it` of the block
-                    const int last_it = it - 1 - ((it - 1 - grp) & 1);
-                    const bool od = mbar_wait(bar(BAR_O_DONE + grp), (uint32_t)(last_it >> 1) & 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, od)) { alive = false; break; }
-                }
+                // (one phase per segment: the phases of o_done are not all waited for, so the last one could not be told)
+                const bool done = mbar_wait(bar(BAR_SEG), (uint32_t)sg & 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, done)) { alive = false; break; }
                 sh.meet[grp][0][row] = first ? -INFINITY : m_ref;
                 sh.meet[grp][1][row] = first ? 0.f : l_run;
                 sh.meet[grp][2][row] = v_ref;
