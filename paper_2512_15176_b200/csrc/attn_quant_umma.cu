@@ -2,7 +2,9 @@
 //
 // The work is split as in the bf16 kernel: a unit is one (sequence, KV head, row tile of 128 query rows), its keys come in
 // tiles of 64 -- four full pages, and one last tile for what is bf16, the tail rows and the block's own -- and the tiles
-// of all units, laid end to end, are cut into one equal share per thread block (attn_share.cuh).
+// of all units, laid end to end, are cut into one equal share per thread block (attn_share.cuh).  Beginning and ending a
+// unit costs as much as several tiles (its queries are split, two accumulators joined, and the pipeline runs dry), so every
+// unit's tiles are preceded in that list by HEAD places with no work in them.
 //
 //   S = Q K^T   on the codes as the cache holds them.  Q is split into two e4m3 terms per row, q = 2^x (q1 + q2): a bf16 value
 //               has 8 significant bits, e4m3 has 4, so the two terms are exact except for elements below 2^-13 of their row's
@@ -53,6 +55,7 @@ constexpr int THREADS = 512;
 constexpr int TMEM_COLS = 512;                 // S, and P in its place (columns 0..31 of it): [b * 64, +64) b < 4;  O [256 + g * 128, +128)
 constexpr int NS = 4;                          // a tile's buffer is free once O has taken P from it
 constexpr int O_COL = 256;
+constexpr int HEAD = 8;                         // what a unit costs beside its tiles, in tiles
 constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^35 above fp16's last bit
 
 // mbarrier indices
@@ -101,7 +104,14 @@ __device__ __forceinline__ float ex2_approx(float x) {
     return y;
 }
 
-// Tiles of sequence b: its full pages four at a time and the bf16 tile; 0 if the sequence cannot be used.
+// A wait that usually need not wait is one instruction here; the rest is out of line (instruction fetches are what this
+// kernel has least of).
+__device__ __noinline__ bool wait_slowly(uint32_t bar, uint32_t parity, volatile int* abort_flag) { return mbar_wait(bar, parity, abort_flag); }
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    return mbar_try_wait(bar, parity) || wait_slowly(bar, parity, abort_flag);
+}
+
+// Places in the list for sequence b: HEAD, its full pages four at a time, the bf16 tile; 0 if the sequence cannot be used.
 __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out, int* s_out) {
     const int s = p.seq_ids[b];
     int n = -1;
@@ -109,7 +119,7 @@ __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out,
     if (n_out) *n_out = n;
     if (s_out) *s_out = s;
     if (n < 0 || n > p.max_seq_len) return 0;
-    return (n / PAGE + PAGES - 1) / PAGES + 1;
+    return HEAD + (n / PAGE + PAGES - 1) / PAGES + 1;
 }
 
 // Power of two that brings a group's largest magnitude to [128, 256) (nothing but zeros: 1).
@@ -342,8 +352,16 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             long long next;
             const int ns = attn::build_segments(p, Hkv, rt, cursor, share_hi, sh.segs, &next, lane,
                                                 [&](int b, int* n, int* s) { return seq_tiles(p, b, n, s); });
-            if (lane == 0) {
-                sh.n_seg = ns;
+            if (lane == 0) {                                               // from places to tiles
+                int kept = 0;
+                for (int x = 0; x < ns; ++x) {
+                    Seg g = sh.segs[x];
+                    if (g.t_b <= HEAD) continue;
+                    g.t_a = max(g.t_a - HEAD, 0);
+                    g.t_b -= HEAD;
+                    sh.segs[kept++] = g;
+                }
+                sh.n_seg = kept;
                 sh.cursor = next;
             }
         }
@@ -354,6 +372,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if (warp == 0) {
             // ---------------- loader of Q (TMA, as bf16) and K ----------------
             // (A page is a copy of its own, and a warp gets one out every ~200 cycles: it could not bring V as well.)
+            const int no_row = p.kv.num_pages * Hkv * PAGE;    // beyond the pool: reads as zero
             bool ok = true;
             for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                 const Seg g = sh.segs[si];
@@ -363,7 +382,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 {
                     const int qb = sg & 1;
                     int okq = 1;
-                    if (lane == 0) okq = mbar_wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                    if (lane == 0) okq = wait(bar(BAR_Q_EMPTY + qb), ((uint32_t)(sg >> 1) & 1u) ^ 1u, abort_flag) ? 1 : 0;
                     if (!__shfl_sync(0xffffffffu, okq, 0)) { ok = false; break; }
                     if (lane == 0) {
                         mbar_expect_tx(bar(BAR_Q_RAW + qb), (uint32_t)(2 * p.G * min(p.ipt, p.k) * 128));
@@ -400,16 +419,17 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         }
                         const float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3)), vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
                         int oks = 1;
-                        if (lane == 0) oks = mbar_wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                        if (lane == 0) oks = wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
                         if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
                         if (lane < 8) sh.scales[rs % NSCALE][lane] = lane < 4 ? ks : vs;
                         __syncwarp();
-                        if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);
+                        if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);      // (the arrival publishes the scales as well)
                         __syncwarp();
-                        int pg = __shfl_sync(0xffffffffu, id_cur, at * PAGES + (lane & 3));
+                        const int pg = __shfl_sync(0xffffffffu, id_cur, at * PAGES + (lane & 3));
                         if (lane < 4) {
-                            if (pg != -2 && (pg < 0 || pg >= p.kv.num_pages)) { deer_report(p.kv.status, DEER_ERR_BAD_PAGE); pg = -2; }
-                            tma_load_2d(ring_addr + sl * T_BYTES + lane * PAGE * HD, &tm_k, 0, pg == -2 ? p.kv.num_pages * Hkv * PAGE : (pg * Hkv + kvh) * PAGE, bar(BAR_K_FULL + sl));
+                            const bool there = pg >= 0 && pg < p.kv.num_pages;
+                            if (!there && pg != -2) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
+                            tma_load_2d(ring_addr + sl * T_BYTES + lane * PAGE * HD, &tm_k, 0, there ? (pg * Hkv + kvh) * PAGE : no_row, bar(BAR_K_FULL + sl));
                         }
                         ++rs;
                     }
@@ -422,12 +442,12 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 for (int si = 0; si < n_seg && ok; ++si, ++sg) {
                     const Seg g = sh.segs[si];
                     const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                    if (!mbar_wait(bar(BAR_Q_FULL + (sg & 1)), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
+                    if (!wait(bar(BAR_Q_FULL + (sg & 1)), (uint32_t)(sg >> 1) & 1u, abort_flag)) { ok = false; break; }
                     for (int t = g.t_a; t < g.t_b; ++t, ++it) {
                         const int sb = it % NS;
                         const bool blk = t == last_tile;
-                        if (!mbar_wait(blk ? bar(BAR_BT_FULL) : bar(BAR_K_FULL + rs % NK), (uint32_t)(blk ? nb : rs / NK) & 1u, abort_flag) ||
-                            !mbar_wait(bar(BAR_S_FREE + sb), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag)) {
+                        if (!wait(blk ? bar(BAR_BT_FULL) : bar(BAR_K_FULL + rs % NK), (uint32_t)(blk ? nb : rs / NK) & 1u, abort_flag) ||
+                            !wait(bar(BAR_S_FREE + sb), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag)) {
                             ok = false;
                             break;
                         }
@@ -451,7 +471,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     for (int t = g.t_a; t < g.t_b; ++t, ++it) {
                         const int sb = it % NS;
                         const uint32_t d_tmem = tmem_base + (uint32_t)(sb * TILE);
-                        if (!mbar_wait(bar(BAR_GO + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
+                        if (!wait(bar(BAR_GO + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();
                         if (t != last_tile) {
                             const int sl = rs % NK;
@@ -490,8 +510,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
                         const bool blk = t == last_tile;
                         const int vb = rs % NVH;
-                        if (!blk && !mbar_wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) { ok = false; break; }
-                        if (!mbar_wait(bar(BAR_P_READY + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
+                        if (!blk && !wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) { ok = false; break; }
+                        if (!wait(bar(BAR_P_READY + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();                             // (a bf16 tile was full before its S)
                         // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
                         const uint64_t vd = smem_desc_sw128(blk ? bt_addr + 2 * T_BYTES : vh_addr + vb * VH_BYTES, VH_HALF, 1024);
@@ -550,7 +570,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         // The bf16 tile, as early as its buffer allows (two page tiles are on their way to O meanwhile): warp w
                         // takes 16 tokens of K, then of V.
                         const int n_tail = g.n % PAGE;
-                        ok = mbar_wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
+                        ok = wait(bar(BAR_BT_EMPTY), ((uint32_t)nb & 1u) ^ 1u, abort_flag);
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         uint32_t present, decoded;
                         attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
@@ -584,7 +604,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (t == last_tile) break;
                     if ((rs & 1) == mine) {
                         const int vb = rs % NVH;
-                        ok = mbar_wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs / NVH) & 1u) ^ 1u, abort_flag);
+                        ok = wait(bar(BAR_VH_EMPTY + vb), ((uint32_t)(rs / NVH) & 1u) ^ 1u, abort_flag);
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         cp_async_wait<1>();
                         unsigned char* dst = vh + vb * VH_BYTES + (c16 >> 2) * VH_HALF;
@@ -625,7 +645,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 bool first = true;
                 const int qb = sg & 1;
                 {
-                    const bool raw = mbar_wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
+                    const bool raw = wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, raw)) { alive = false; break; }
                     split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, min(p.ipt, p.k - rt * p.ipt) * p.G, (warp - 4) * 4 + (lane >> 3), 32);
                     fence_proxy_async_smem();
@@ -633,7 +653,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (lane == 0) mbar_arrive(bar(BAR_Q_FULL + qb));
                 }
                 {
-                    const bool got = mbar_wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
+                    const bool got = wait(bar(BAR_Q_FULL + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                 }
                 const float f_row = sh.q_factor[qb][row];
@@ -649,7 +669,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const uint32_t s_tmem = t_lane + (uint32_t)(sb * TILE);
                     // The scores, and with them the scales.  (Not K_FULL or BT_FULL for those: a slot may be on its next tile but one
                     // by now, and a parity wait cannot tell.)
-                    const bool got = mbar_wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
+                    const bool got = wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                     tcgen05_fence_after();
                     uint64_t see = 0;
@@ -700,7 +720,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 const float al = ex2_approx(m_ref - m_t), ao = al * (v_ref / v_t);
                                 // phase (it >> 1) - 1 of o_done: the group's previous tile is in O.  (The one before it is: its
                                 // buffer is the one that this tile's scores are in.)
-                                const bool od = mbar_wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
+                                const bool od = wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
                                 if (!__all_sync(0xffffffffu, od)) { stop = true; break; }
                                 tcgen05_fence_after();
 #pragma unroll 1
@@ -766,7 +786,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 
                 // ---- the segment's result: the groups meet; each takes half of the columns of both accumulators ----
                 // (one phase per segment: the phases of o_done are not all waited for, so the last one could not be told)
-                const bool done = mbar_wait(bar(BAR_SEG), (uint32_t)sg & 1u, abort_flag);
+                const bool done = wait(bar(BAR_SEG), (uint32_t)sg & 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, done)) { alive = false; break; }
                 sh.meet[grp][0][row] = first ? -INFINITY : m_ref;
                 sh.meet[grp][1][row] = first ? 0.f : l_run;
@@ -775,7 +795,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(BAR_MEET + quarter));
                 {
-                    const bool got = mbar_wait(bar(BAR_MEET + quarter), (uint32_t)sg & 1u, abort_flag);
+                    const bool got = wait(bar(BAR_MEET + quarter), (uint32_t)sg & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                 }
                 tcgen05_fence_after();
@@ -801,12 +821,13 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
                     see = columns_seen(p, g, rt, row, present, decoded);
                 }
+                __nv_bfloat16* out_row = row_valid && whole ? p.out + ((size_t)(g.b * p.k + i_blk) * p.Hq + hq) * HD + grp * 64 : nullptr;
+                float* part_row = row_valid && !whole ? p.part_o + (slot * 128 + row) * HD + grp * 64 : nullptr;
 #pragma unroll 1
                 for (int cc = 0; cc < 4; ++cc) {
-                    const int col = grp * 64 + cc * 16;
                     uint32_t a[16], b[16];
-                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + col), a);
-                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + HD + col), b);
+                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * 64 + cc * 16), a);
+                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + HD + grp * 64 + cc * 16), b);
                     tmem_wait_ld();
                     float v[16];
 #pragma unroll
@@ -820,27 +841,27 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             const __nv_bfloat16* src = x < n_tail
                                 ? static_cast<const __nv_bfloat16*>(qp.kq.v_tail) + (((size_t)g.s * Hkv + kvh) * DEER_TAIL_ROWS + (full % 3) * PAGE + x) * HD
                                 : p.v_blk + ((size_t)(g.b * p.k + x - n_tail) * Hkv + kvh) * HD;
+                            src += grp * 64 + cc * 16;
 #pragma unroll
                             for (int c = 0; c < 16; ++c) {
-                                const float f = __bfloat162float(src[col + c]);
+                                const float f = __bfloat162float(src[c]);
                                 if (quant::mag_bits(f) >= 0x7f800000u) v[c] += f;
                             }
                         }
                     }
-                    if (gone) {
+                    if (gone) {                                            // (zero times a NaN would be one)
 #pragma unroll
                         for (int c = 0; c < 16; ++c) v[c] = 0.f;
                     }
-                    if (row_valid && whole) {
-                        __nv_bfloat16* dst = p.out + ((size_t)(g.b * p.k + i_blk) * p.Hq + hq) * HD + col;
+                    if (out_row) {
 #pragma unroll
                         for (int c = 0; c < 16; c += 8)
-                            *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[c], v[c + 1]), pack_bf16(v[c + 2], v[c + 3]),
-                                                                            pack_bf16(v[c + 4], v[c + 5]), pack_bf16(v[c + 6], v[c + 7]));
-                    } else if (row_valid) {
-                        float* dst = p.part_o + (slot * 128 + row) * HD + col;
+                            *reinterpret_cast<uint4*>(out_row + cc * 16 + c) = make_uint4(pack_bf16(v[c], v[c + 1]), pack_bf16(v[c + 2], v[c + 3]),
+                                                                                          pack_bf16(v[c + 4], v[c + 5]), pack_bf16(v[c + 6], v[c + 7]));
+                    }
+                    if (part_row) {
 #pragma unroll
-                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(part_row + cc * 16 + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
                     }
                 }
                 if (grp == 0) {
@@ -850,9 +871,9 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         // a NaN sum must reach the output: the merge gives such a piece all the weight
                         if (row_valid) p.part_lse[slot * 128 + row] = gone || l == 0.f ? -INFINITY : l != l ? 3.0e38f : mx + log2f(l) - BIAS;
                         if (g.t_a == 0 && row == 0) {                      // tells the merge kernel which blocks share the unit
-                            const int tiles_u = last_tile + 1;
-                            const int j_lo = (int)(((g.u0 + 1) * ncg + T - 1) / T) - 1;
-                            const int j_hi = (int)(((g.u0 + tiles_u) * ncg + T - 1) / T) - 1;
+                            const long long u0 = g.u0 + HEAD;              // the groups that hold its first and its last tile
+                            const int j_lo = (int)(((u0 + 1) * ncg + T - 1) / T) - 1;
+                            const int j_hi = (int)(((u0 + last_tile + 1) * ncg + T - 1) / T) - 1;
                             p.unit_parts[unit] = make_int2(j_lo, j_hi);
                         }
                     }
@@ -861,7 +882,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(BAR_PART + quarter));
-                const bool parted = mbar_wait(bar(BAR_PART + quarter), (uint32_t)sg & 1u, abort_flag);
+                const bool parted = wait(bar(BAR_PART + quarter), (uint32_t)sg & 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, parted)) { alive = false; break; }
             }
         }
