@@ -252,11 +252,9 @@ __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale,
     return __any_sync(0xffffffffu, any >= 0x7f800000u);
 }
 
-// Columns of the bf16 tile (tail rows, then block rows) that a query row sees.
-__device__ __forceinline__ uint64_t columns_seen(const AttnParams& p, const Seg& g, int rt, int row, uint32_t present, uint32_t decoded) {
-    const int i0 = rt * p.ipt, i_blk = i0 + row / p.G, n_tail = g.n % PAGE;
-    const bool row_valid = row < min(p.ipt, p.k - i0) * p.G;
-    const int state = (p.row_state && row_valid) ? p.row_state[(size_t)g.b * p.k + i_blk] : 1;
+// Columns of the bf16 tile (tail rows, then block rows) that a query row of block row i_blk sees.
+__device__ __forceinline__ uint64_t columns_seen(const AttnParams& p, const Seg& g, int i_blk, bool row_valid, uint32_t present, uint32_t decoded) {
+    const int n_tail = g.n % PAGE, state = (p.row_state && row_valid) ? p.row_state[(size_t)g.b * p.k + i_blk] : 1;
     return ((uint64_t)(attn::visible_rows(p.mask, i_blk, state, present, decoded) & present) << n_tail) | ((1ull << n_tail) - 1ull);
 }
 
@@ -637,6 +635,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int grp = (warp - 4) >> 2, quarter = warp & 3;
             const int row = quarter * 32 + lane;
             const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+            const int i_blk = rt * p.ipt + row / p.G, g_row = row % p.G, rows = min(p.ipt, p.k - rt * p.ipt) * p.G;      // this row's block row and head
+            const bool row_valid = row < rows;
             bool alive = true;
             for (int si = 0; si < n_seg && alive; ++si, ++sg) {
                 const Seg& g = sh.segs[si];
@@ -647,7 +647,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 {
                     const bool raw = wait(bar(BAR_Q_RAW + qb), (uint32_t)(sg >> 1) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, raw)) { alive = false; break; }
-                    split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, min(p.ipt, p.k - rt * p.ipt) * p.G, (warp - 4) * 4 + (lane >> 3), 32);
+                    split_queries(sQ + qb * Q_BYTES, sh.q_factor[qb], p.scale_log2, rows, (warp - 4) * 4 + (lane >> 3), 32);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(BAR_Q_FULL + qb));
@@ -676,7 +676,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (is_bt) {
                         uint32_t present, decoded;
                         attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
-                        see = columns_seen(p, g, rt, row, present, decoded);
+                        see = columns_seen(p, g, i_blk, row_valid, present, decoded);
                     }
                     // 32 scores: column c of half h in the log2 domain = sr[c] * factor * its page's K scale
                     uint32_t sr[32];
@@ -803,15 +803,14 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const float mx = fmaxf(m0, m1);                            // one of the groups had a tile
                 const float e0 = m0 == -INFINITY ? 0.f : ex2_approx(m0 - mx), e1 = m1 == -INFINITY ? 0.f : ex2_approx(m1 - mx);
                 const float l = e0 * l0 + e1 * l1;
-                const int kvh = g.hr / p.row_tiles, n_tail = g.n % PAGE, i_blk = rt * p.ipt + row / p.G;
-                const bool row_valid = row < min(p.ipt, p.k - rt * p.ipt) * p.G;
+                const int kvh = g.hr / p.row_tiles, n_tail = g.n % PAGE;
                 // no query row, or an absent one
                 const bool gone = !row_valid || (p.row_state && p.row_state[(size_t)g.b * p.k + i_blk] < 0);
                 const float inv = l != 0.f ? 1.f / l : 0.f;
                 const float w0 = e0 * sh.meet[0][2][row] * inv, w1 = e1 * sh.meet[1][2][row] * inv;
                 const bool has0 = m0 != -INFINITY, has1 = m1 != -INFINITY;
                 const bool bad_v = g.t_b == last_tile + 1 && *(volatile int*)&sh.bt_bad[(nb - 1) & 1] == nb;
-                const int hq = kvh * p.G + row % p.G;
+                const int hq = kvh * p.G + g_row;
                 const size_t unit = (size_t)g.b * HR + g.hr;
                 const bool whole = g.t_a == 0 && g.t_b == last_tile + 1;
                 const size_t slot = ((size_t)g.b * Hkv + kvh + jg) * p.row_tiles + rt;
@@ -819,7 +818,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (bad_v) {                                               // (warp-uniform)
                     uint32_t present, decoded;
                     attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
-                    see = columns_seen(p, g, rt, row, present, decoded);
+                    see = columns_seen(p, g, i_blk, row_valid, present, decoded);
                 }
                 __nv_bfloat16* out_row = row_valid && whole ? p.out + ((size_t)(g.b * p.k + i_blk) * p.Hq + hq) * HD + grp * 64 : nullptr;
                 float* part_row = row_valid && !whole ? p.part_o + (slot * 128 + row) * HD + grp * 64 : nullptr;
