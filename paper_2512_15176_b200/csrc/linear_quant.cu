@@ -28,6 +28,7 @@ using quant::GROUP;
 
 constexpr int BN = 128;                        // weight rows (output columns) of a tile
 constexpr int W_BYTES = BN * GROUP;            // 16 KB per stage
+constexpr int MAX_SPLIT = 8;                   // blocks of a cluster: the portable limit
 
 // NT rows of x per tile; stages such that two blocks fit an SM, whose tensor memory then suffices for both (a block
 // allocates it before it lets the next kernel in, so blocks that share an SM never wait for one another's columns).
@@ -35,11 +36,15 @@ template <int NT>
 struct Cfg {
     static constexpr int STAGE = W_BYTES + NT * GROUP;
     static constexpr int STAGES = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3;
-    static constexpr int NBUF = NT <= 64 ? 4 : 2;                 // accumulators in TMEM
-    static constexpr int TMEM_COLS = NT * NBUF < 64 ? 64 : NT * NBUF;
+    // Column groups that change hands together (each with NT accumulator columns of its own): a hand-over costs the issuer and
+    // the epilogue several hundred cycles of waits and arrivals, as much as four MMAs.  Two hand-overs' worth of accumulators.
+    static constexpr int H = NT <= 32 ? 4 : NT == 64 ? 2 : 1;
+    static constexpr int NBUF = 2;
+    static constexpr int TMEM_COLS = NT * H * NBUF;
+    static constexpr int CH = NT < 32 ? 16 : 32;                  // columns of one tensor-memory load
     static constexpr int EPI_WARPS = 4;
     static constexpr int THREADS = 64 + EPI_WARPS * 32;
-    static constexpr int SMEM = STAGES * STAGE + 1024 /*alignment slack*/ + 2 * NT * 4 /*scales*/ + (2 * STAGES + 2 * NBUF) * 8 + 16;
+    static constexpr int SMEM = STAGES * STAGE + 1024 /*alignment slack*/ + 2 * H * NT * 4 /*scales*/ + (2 * STAGES + 2 * NBUF) * 8 + 16;
 };
 
 struct Args {
@@ -68,8 +73,8 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     constexpr int EPI_THREADS = C::EPI_WARPS * 32;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float* sc = reinterpret_cast<float*>(ring + C::STAGES * C::STAGE);           // [2][NT] x_scale * w_scale of a column group
-    uint64_t* bars = reinterpret_cast<uint64_t*>(sc + 2 * NT);                   // full, empty [STAGES]; tfull, tempty [NBUF]
+    float* sc = reinterpret_cast<float*>(ring + C::STAGES * C::STAGE);           // [2][H][NT] x_scale * w_scale of a hand-over's column groups
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sc + 2 * C::H * NT);            // full, empty [STAGES]; tfull, tempty [NBUF]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 2 * C::NBUF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -124,17 +129,21 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     } else if (warp == 1) {
         if (lane == 0) {
             const uint32_t idesc = make_idesc_e4m3(NT);
-            for (int i = 0; i < ng; ++i) {
-                const int s = i % C::STAGES, b = i % C::NBUF;
-                if (!mbar_wait(tempty(b), ((uint32_t)(i / C::NBUF) & 1u) ^ 1u, abort_flag)) break;
-                if (!mbar_wait(full(s), (uint32_t)(i / C::STAGES) & 1u, abort_flag)) break;
-                tcgen05_fence_after();
-                const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
-                const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + W_BYTES);
+            bool ok = true;
+            for (int i0 = 0, n = 0; i0 < ng && ok; i0 += C::H, ++n) {
+                const int b = n % C::NBUF;
+                if (!mbar_wait(tempty(b), ((uint32_t)(n / C::NBUF) & 1u) ^ 1u, abort_flag)) break;
+                for (int u = 0; u < C::H && i0 + u < ng; ++u) {
+                    const int i = i0 + u, s = i % C::STAGES;
+                    if (!mbar_wait(full(s), (uint32_t)(i / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    tcgen05_fence_after();
+                    const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
+                    const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + W_BYTES);
 #pragma unroll
-                for (int kk = 0; kk < GROUP / 32; ++kk)
-                    umma_f8_ss(tmem_base + (uint32_t)(b * NT), wd + (uint64_t)(kk * 2), xd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
-                umma_commit(empty(s));
+                    for (int kk = 0; kk < GROUP / 32; ++kk)
+                        umma_f8_ss(tmem_base + (uint32_t)((b * C::H + u) * NT), wd + (uint64_t)(kk * 2), xd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
+                    umma_commit(empty(s));
+                }
                 umma_commit(tfull(b));
             }
         }
@@ -143,54 +152,43 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll
         for (int j = 0; j < NT / 2; ++j) acc[j] = 0;
-        // thread et brings the scale of row m0 + et, a column group ahead (eight groups share a 32-byte sector)
-        const bool brings = et < NT;
-        const float* xs = (brings && m0 + et < a.M) ? a.x_scale + (size_t)(m0 + et) * a.groups + g0 : nullptr;
-        const float* ws = a.w_scale + (size_t)(n0 / GROUP) * a.groups + g0;
-        float nx = xs ? xs[0] : 0.f, nw = xs ? ws[0] : 0.f;
+        // thread et brings the scale of row et / H and column group et % H of a hand-over, one hand-over ahead
+        const int my_row = et / C::H, my_u = et % C::H;
+        const bool brings = my_row < NT;
+        const float* xs = (brings && m0 + my_row < a.M) ? a.x_scale + (size_t)(m0 + my_row) * a.groups + g0 + my_u : nullptr;
+        const float* ws = a.w_scale + (size_t)(n0 / GROUP) * a.groups + g0 + my_u;
+        float nx = xs && my_u < ng ? xs[0] : 0.f, nw = xs && my_u < ng ? ws[0] : 0.f;
         bool alive = true;
-        for (int i = 0; i < ng; ++i) {
-            const int b = i % C::NBUF;
-            float* slot = sc + (i & 1) * NT;
-            if (brings) slot[et] = nx * nw;
-            if (xs && i + 1 < ng) {
-                nx = xs[i + 1];
-                nw = ws[i + 1];
+        for (int i0 = 0, n = 0; i0 < ng; i0 += C::H, ++n) {
+            const int b = n % C::NBUF, cnt = min(C::H, ng - i0);
+            float* slot = sc + (n & 1) * C::H * NT;
+            if (brings) slot[my_u * NT + my_row] = nx * nw;
+            if (xs && i0 + C::H + my_u < ng) {
+                nx = xs[i0 + C::H];
+                nw = ws[i0 + C::H];
             }
             asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
             // a warp whose wait ran out keeps meeting the others at the barrier
-            const bool got = alive && mbar_wait(tfull(b), (uint32_t)(i / C::NBUF) & 1u, abort_flag);
+            const bool got = alive && mbar_wait(tfull(b), (uint32_t)(n / C::NBUF) & 1u, abort_flag);
             if (!__all_sync(0xffffffffu, got)) {
                 alive = false;
                 continue;
             }
             tcgen05_fence_after();
             const ulonglong2* s_row = reinterpret_cast<const ulonglong2*>(slot);
-            const uint32_t taddr = t_lane + (uint32_t)(b * NT);
-            auto add16 = [&](int c, const uint32_t (&v)[16]) {
+            const uint32_t taddr = t_lane + (uint32_t)(b * C::H * NT);
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    const ulonglong2 s = s_row[(c + j) / 4];
-                    fma_f32x2(acc[(c + j) / 2], v[j], v[j + 1], s.x);
-                    fma_f32x2(acc[(c + j) / 2 + 1], v[j + 2], v[j + 3], s.y);
-                }
-            };
-            if (NT <= 64) {                                        // 16 columns in flight while the 16 before them are added
-                uint32_t r[2][16];
-                TMEM_LD_X16(taddr, r[0]);
+            for (int c0 = 0; c0 < C::H * NT; c0 += C::CH) {        // columns c0 .. of column group c0 / NT
+                if (c0 / NT >= cnt) break;
+                uint32_t v[C::CH];
+                if constexpr (C::CH == 16) TMEM_LD_X16(taddr + c0, v);
+                else TMEM_LD_X32(taddr + c0, v);
+                tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < NT; c += 16) {
-                    tmem_wait_ld();
-                    if (c + 16 < NT) TMEM_LD_X16(taddr + c + 16, r[(c / 16 + 1) & 1]);
-                    add16(c, r[(c / 16) & 1]);
-                }
-            } else {                                               // 128 sums leave no registers for that
-#pragma unroll
-                for (int c = 0; c < NT; c += 16) {
-                    uint32_t r[16];
-                    TMEM_LD_X16(taddr + c, r);
-                    tmem_wait_ld();
-                    add16(c, r);
+                for (int j = 0; j < C::CH; j += 4) {
+                    const ulonglong2 s = s_row[(c0 + j) / 4];
+                    fma_f32x2(acc[((c0 + j) % NT) / 2], v[j], v[j + 1], s.x);
+                    fma_f32x2(acc[((c0 + j) % NT) / 2 + 1], v[j + 2], v[j + 3], s.y);
                 }
             }
             tcgen05_fence_before();
@@ -233,16 +231,28 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         }
         __syncwarp();
         cluster_sync();
-        bool good = true;
+        // (every load is on its way before the first is used: one at a time they would take 16 remote latencies and more)
         const uint32_t flag_addr = smem_u32(const_cast<int*>(abort_flag));
-        for (int r = 0; r < a.split; ++r) good = good && ld_cluster_u32(map_to_cta(flag_addr, (uint32_t)r)) == 0;
-        if (warp >= 2 && good) {
-            const int lo = NT * rank / a.split, hi = NT * (rank + 1) / a.split;
-            for (int j = lo; j < hi; ++j) {
-                if (m0 + j >= a.M) break;
-                float v = 0.f;
-                for (int r = 0; r < a.split; ++r) v += ld_cluster_f32(map_to_cta(ring_addr + (uint32_t)((j * BN + lane_row) * 4), (uint32_t)r));
-                put(j, v);
+        uint32_t bad = 0;
+#pragma unroll
+        for (int r = 0; r < MAX_SPLIT; ++r)
+            if (r < a.split) bad |= ld_cluster_u32(map_to_cta(flag_addr, (uint32_t)r));
+        if (warp >= 2) {
+            const int lo = NT * rank / a.split, hi = min(NT * (rank + 1) / a.split, a.M - m0);
+            for (int j0 = lo; j0 < hi; j0 += 4) {
+                float v[4][MAX_SPLIT];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int r = 0; r < MAX_SPLIT; ++r)
+                        v[q][r] = (j0 + q < hi && r < a.split) ? ld_cluster_f32(map_to_cta(ring_addr + (uint32_t)(((j0 + q) * BN + lane_row) * 4), (uint32_t)r)) : 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float sum = v[q][0];
+#pragma unroll
+                    for (int r = 1; r < MAX_SPLIT; ++r) sum += v[q][r];
+                    if (j0 + q < hi && bad == 0) put(j0 + q, sum);
+                }
             }
         }
         __syncwarp();
@@ -480,7 +490,7 @@ int launch(Args a, const void* x, const void* w, cudaStream_t st) {
     // As many blocks to a cluster as still fit beside each other (two per SM), with at least four column groups each.
     const long long room = 2LL * deer_sm_count();
     a.split = 1;
-    while (a.split < 8 && tiles * a.split * 2 <= room && a.groups >= a.split * 2 * 4) a.split *= 2;
+    while (a.split < MAX_SPLIT && tiles * a.split * 2 <= room && a.groups >= a.split * 2 * 4) a.split *= 2;
     DEER_CHECK_ARG(tiles * a.split <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_linear_quant: too many tiles");
     DEER_CUDA(cudaFuncSetAttribute(linear_quant_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
     cudaLaunchConfig_t cfg = {};
