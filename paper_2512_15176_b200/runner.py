@@ -366,3 +366,94 @@ class VerifierStack:
             x = layer.forward(x, xn=xn, next_ln=nxt)
             xn = layer.xn_next if nxt is not None else None
         return x
+
+
+def quantise_weight(w: torch.Tensor):
+    """A weight [N, K] as e4m3 codes and one fp32 scale per 128 x 128 block, as ``deer_linear_quant`` takes them (once,
+    when the weights are loaded)."""
+    N, K = w.shape
+    n, g = -(-N // 128), -(-K // 128)
+    blocks = torch.zeros(n * 128, g * 128, dtype=torch.float32, device=w.device)
+    blocks[:N, :K] = w
+    blocks = blocks.view(n, 128, g, 128)
+    amax = blocks.abs().amax(dim=(1, 3))
+    # (a tensor as the divisor: torch turns a division by a number into a product with its reciprocal on the device)
+    scale = (amax / torch.full_like(amax, 448.0)).clamp_min(2.0 ** -126)
+    codes = (blocks / scale[:, None, :, None]).to(torch.float8_e4m3fn).view(n * 128, g * 128)[:N, :K].contiguous()
+    return codes, scale.contiguous()
+
+
+class VerifierLayerQuant:
+    """``VerifierLayer`` (dense MLP) with its weights, its projections' inputs and its KV cache in 8 bits: the same
+    pre-norm layer at the M = B k rows of a draft block, ten calls.  ``kv`` is a ``binding.KVCacheQuant``; ``weights``
+    are the bf16 tensors that ``VerifierLayer`` takes ("wqkv", "wo", "wgu", "wd", "ln1", "ln2", optional "q_norm" /
+    "k_norm"); the four matrices are quantised here, once.  The residual stream stays bf16.
+    The block's keys and values are NOT in the cache after ``forward``: the cache takes only accepted rows, with
+    ``store`` after the acceptance and before the commit."""
+
+    def __init__(self, cfg: StepConfig, kv: L.KVCacheQuant, weights: dict, max_seq_len: int, inter: int, eps=1e-6, theta=1.0e6,
+                 device="cuda", reserve=True):
+        self.cfg, self.kv, self.max_seq_len = cfg, kv, int(max_seq_len)
+        self.inter, self.eps, self.theta, self.reserve = int(inter), float(eps), float(theta), bool(reserve)
+        B, k, Hq, Hkv, D, M, hid = cfg.B, cfg.k, cfg.Hq, cfg.Hkv, cfg.D, cfg.M, cfg.hid
+        self.norms = {n: weights.get(n) for n in ("ln1", "ln2", "q_norm", "k_norm")}
+        self.w = {n: quantise_weight(weights[n]) for n in ("wqkv", "wo", "wgu", "wd")}
+        e = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device=device)
+        # codes and scales of a projection's input
+        pair = lambda K: (torch.empty(M, K, dtype=torch.float8_e4m3fn, device=device),
+                          torch.empty(M, -(-K // 128), dtype=torch.float32, device=device))
+        self.seq_ids = torch.arange(B, dtype=torch.int32, device=device)
+        self.xn, self.xn2, self.attn_in, self.act = pair(hid), pair(hid), pair(Hq * D), pair(self.inter)
+        self.qkv, self.gu = e(M, (Hq + 2 * Hkv) * D), e(M, 2 * self.inter)
+        self.q, self.k_blk, self.v_blk, self.attn_out = e(B, k, Hq, D), e(B, k, Hkv, D), e(B, k, Hkv, D), e(B, k, Hq, D)
+        self.x1, self.x2 = e(M, hid), e(M, hid)
+        self.attn_ws = _ws(L.deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, self.max_seq_len), device)
+        self.scale = 1.0 / math.sqrt(D)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        """x [M, hid] bf16: the layer's input; returns its output (a buffer of the layer)."""
+        c, w, n = self.cfg, self.w, self.norms
+        M = c.M
+        L.deer_rmsnorm_quant(x, n["ln1"], *self.xn, self.eps)
+        L.deer_linear_quant(*self.xn, *w["wqkv"], self.qkv)
+        L.deer_qkv_split_norm_rope(self.kv, self.seq_ids, self.qkv, self.q, self.k_blk, self.v_blk, n["q_norm"], n["k_norm"],
+                                   self.eps, self.theta)
+        if self.reserve:
+            L.deer_kv_reserve(self.kv, self.seq_ids, c.k)
+        L.deer_block_attn_quant(self.kv, self.seq_ids, self.q, self.k_blk, self.v_blk, self.attn_out, None, L.DEER_MASK_CAUSAL,
+                                self.scale, self.max_seq_len, self.attn_ws)
+        L.deer_quantize(self.attn_out.view(M, -1), *self.attn_in)
+        L.deer_linear_quant(*self.attn_in, *w["wo"], self.x1, residual=x)
+        L.deer_rmsnorm_quant(self.x1, n["ln2"], *self.xn2, self.eps)
+        L.deer_linear_quant(*self.xn2, *w["wgu"], self.gu)
+        L.deer_quantize(self.gu, *self.act, gated=True)
+        L.deer_linear_quant(*self.act, *w["wd"], self.x2, residual=self.x1)
+        return self.x2
+
+    def store(self, keep: Optional[torch.Tensor]):
+        """The first keep[b] rows of each block join the cache (None: all k); the commit follows, once for all layers."""
+        L.deer_kv_store(self.kv, self.seq_ids, self.k_blk, self.v_blk, keep)
+
+
+class VerifierStackQuant:
+    """``VerifierStack`` of ``VerifierLayerQuant`` layers: ``kvs[0]`` a ``binding.KVCacheQuant``, the others its
+    ``layer()``.  A step is ``forward`` (reserves, runs the layers), the acceptance, and ``commit(keep)``."""
+
+    def __init__(self, cfg: StepConfig, kvs, weights, max_seq_len: int, inter: int, eps=1e-6, theta=1.0e6, device="cuda"):
+        assert len(kvs) == len(weights)
+        self.cfg, self.kvs = cfg, kvs
+        self.layers = [VerifierLayerQuant(cfg, kv, w, max_seq_len, inter, eps, theta, device, reserve=False)
+                       for kv, w in zip(kvs, weights)]
+        self.seq_ids = self.layers[0].seq_ids
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        L.deer_kv_reserve(self.kvs[0], self.seq_ids, self.cfg.k)
+        for layer in self.layers:
+            x = layer.forward(x)
+        return x
+
+    def commit(self, keep: torch.Tensor):
+        """The accepted rows enter every layer's cache, then the lengths grow, once."""
+        for layer in self.layers:
+            layer.store(keep)
+        L.deer_kv_commit(self.kvs[0], self.seq_ids, keep, self.cfg.k)
