@@ -11,17 +11,19 @@
 // multiplies the page's product before it joins the fp32 sums, so scales of any size work.  Queries are brought to
 // fp16 by a power of two per row (exact to 2^-24 of the row's largest), probabilities are at most 2^12 and keep fp16's
 // 11 bits down to 2^-26 of the row's maximum.  The warps of a block take pages in turn with running maxima of their
-// own, and meet in shared memory at the end; a context is cut into chunks over thread blocks, which a second kernel
-// joins.
+// own, and meet in shared memory at the end.  A context is cut into chunks over thread blocks; up to eight of them form
+// a cluster and meet in its shared memory, and where a context has more a second kernel joins the clusters' parts.
 
 #include <cuda_fp16.h>
 
 #include "attn_quant.cuh"
+#include "sm100.cuh"
 
 namespace attnq {
 
 constexpr int ROWS = ROWS_SMALL;
 constexpr int WARPS = 4;
+constexpr int CLUSTER_MAX = 8;                 // the portable limit
 constexpr float P_BIAS = 12.f;                 // probabilities are held as 2^12 p
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -51,22 +53,29 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
     constexpr int HC = D / 64;                 // 16-byte pieces of a key row per lane
     constexpr int ND = D / 8;                  // column tiles of the output
     constexpr int VW = D / 32;                 // 32-bit words of a value row per lane (16-byte or 8-byte piece)
-    __shared__ float s_o[WARPS][ROWS][D];
-    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
+    constexpr int QD = D / 4 + 1;              // a lane's dims of a row, one word apart from the next lane's: no two lanes share a bank
+    __shared__ float s_o[WARPS][ROWS][4 * QD];
+    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS], s_lse[ROWS];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
     const int Hkv = p.kv.n_kv_heads;
     const int c = blockIdx.x, kvh = blockIdx.y / p.row_tiles, rt = blockIdx.y % p.row_tiles, b = blockIdx.z;
     pdl_trigger();
     pdl_wait();
+    const int page_lo = c * p.chunk_pages;
+    // the sequence's length and this warp's first page number are on their way together
+    const int slot_id = p.seq_ids[b];
+    const bool known = slot_id >= 0 && slot_id < p.kv.max_seqs;
+    const int32_t* pt_row = p.kv.page_table + (size_t)(known ? slot_id : 0) * p.kv.max_pages;
+    int pg_next = page_lo + warp < p.kv.max_pages ? __ldcg(pt_row + page_lo + warp) : -1;
     int s, n;
     if (!sequence_of(p, b, &s, &n, c == 0 && blockIdx.y == 0 && tid == 0)) return;
     const int n_chunks = chunks_of(p, n);
-    if (c >= n_chunks) return;
+    if (c / p.cluster * p.cluster >= n_chunks) return;         // none of the cluster's blocks has a chunk
     const int R = p.G * p.k;
-    const int page_lo = c * p.chunk_pages, page_hi = min(n / PAGE, page_lo + p.chunk_pages);
+    const bool busy = c < n_chunks;
+    const int page_hi = busy ? min(n / PAGE, page_lo + p.chunk_pages) : page_lo;
     const int n_tail = n % PAGE;
-    const int32_t* pt_row = p.kv.page_table + (size_t)s * p.kv.max_pages;
 
     uint32_t present, decoded;
     attn::row_state_sets(p.row_state, b, p.k, lane, &present, &decoded);
@@ -154,8 +163,9 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
         uint32_t v[4][VW];                     // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
         float ks, vs;
     };
-    auto load_page = [&](int page, Page& x) {
-        int pg = page < p.kv.max_pages ? pt_row[page] : -1;
+    auto load_page = [&](int page, Page& x) {                  // page number in pg_next; the one after it is fetched meanwhile
+        int pg = pg_next;
+        pg_next = page + WARPS < min(page_hi, p.kv.max_pages) ? __ldcg(pt_row + page + WARPS) : -1;
         if (pg < 0 || pg >= p.kv.num_pages) {
             if (lane == 0) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
             pg = 0;                                            // inside the pool; the status word flags the result
@@ -220,7 +230,7 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
     }
 
     // ---- what is bf16: the tail rows and the block's own, 16 at a time, with the chunk that is last ----
-    if (c == n_chunks - 1) {
+    if (c == n_chunks - 1) {                                   // (a block without a chunk has nothing here either)
         const int n_blk = (p.k + PAGE - 1) / PAGE;
         for (int it = (n_tail ? 0 : 1) + warp; it <= n_blk; it += WARPS) {         // 0: the tail, 1 ..: block rows
             const bool is_tail = it == 0;
@@ -329,16 +339,15 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
         }
 #pragma unroll
         for (int j = 0; j < ND; ++j) {
-            s_o[warp][g8 + u * 8][t4 * (D / 4) + j] = o[j][2 * u];
-            s_o[warp][g8 + u * 8][t4 * (D / 4) + ND + j] = o[j][2 * u + 1];
+            s_o[warp][g8 + u * 8][t4 * QD + j] = o[j][2 * u];
+            s_o[warp][g8 + u * 8][t4 * QD + ND + j] = o[j][2 * u + 1];
         }
     }
     __syncthreads();
     // 8 threads per row, D / 8 dims each
     const int r = tid >> 3, d0 = (tid & 7) * (D / 8), rr = rt * ROWS + r;
-    if (rr >= R) return;
-    const int i = rr / p.G;
-    const bool absent = p.row_state && p.row_state[(size_t)b * p.k + i] < 0;
+    const int i = min(rr, R - 1) / p.G;
+    const bool absent = rr >= R || (p.row_state && p.row_state[(size_t)b * p.k + i] < 0);
     float mx = -INFINITY;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, s_m[w][r]);
@@ -352,30 +361,69 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
     }
     const float inv = (absent || l == 0.f) ? 0.f : 1.f / l;
     float acc[D / 8];
+    float* mine = &s_o[0][r][(tid & 7) / 2 * QD + (tid & 1) * ND];                 // where dim d0 of row r is, with each warp's copy
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
         acc[d] = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) acc[d] = wt[w] != 0.f ? fmaf(wt[w], s_o[w][r][d0 + d], acc[d]) : acc[d];
+        for (int w = 0; w < WARPS; ++w) acc[d] = wt[w] != 0.f ? fmaf(wt[w], mine[w * ROWS * 4 * QD + d], acc[d]) : acc[d];
         acc[d] = absent ? 0.f : acc[d] * inv;
     }
-    const size_t orow = (size_t)(b * p.k + i) * p.Hq + kvh * p.G + rr % p.G;
-    if (n_chunks == 1) {
-        __nv_bfloat16* dst = p.out + orow * D + d0;
+    if (p.cluster == 1) {
+        if (rr >= R) return;
+        __nv_bfloat16* dst = p.out + ((size_t)(b * p.k + i) * p.Hq + kvh * p.G + rr % p.G) * D + d0;
 #pragma unroll
         for (int d = 0; d < D / 8; d += 8)
             *reinterpret_cast<uint4*>(dst + d) = make_uint4(pack_bf16(acc[d], acc[d + 1]), pack_bf16(acc[d + 2], acc[d + 3]),
                                                             pack_bf16(acc[d + 4], acc[d + 5]), pack_bf16(acc[d + 6], acc[d + 7]));
-    } else {
-        const size_t slot = (size_t)c * p.B * p.k * p.Hq + orow;
-        float* dst = p.part_o + slot * D + d0;
-#pragma unroll
-        for (int d = 0; d < D / 8; d += 4) *reinterpret_cast<float4*>(dst + d) = make_float4(acc[d], acc[d + 1], acc[d + 2], acc[d + 3]);
-        if ((tid & 7) == 0) p.part_lse[slot] = (absent || l == 0.f) ? -INFINITY : mx + log2f(l);
+        return;
     }
+
+    // ---- the cluster's blocks meet: each joins its share of the rows, two dims a thread ----
+#pragma unroll
+    for (int d = 0; d < D / 8; ++d) mine[d] = acc[d];          // (this thread alone reads these words above)
+    if ((tid & 7) == 0) s_lse[r] = (absent || l == 0.f) ? -INFINITY : mx + log2f(l);
+    sm100::cluster_sync();
+    const int part = c / p.cluster, rank = c % p.cluster;
+    const int in_part = min(p.cluster, n_chunks - part * p.cluster), n_parts = (n_chunks + p.cluster - 1) / p.cluster;
+    const uint32_t lse_addr = smem_u32(s_lse), o_addr = smem_u32(&s_o[0][0][0]);
+    for (int it = rank * WARPS * 32 + tid; it < min(ROWS, R - rt * ROWS) * (D / 2); it += p.cluster * WARPS * 32) {
+        const int jr = it / (D / 2), jd = it % (D / 2) * 2;    // row of the tile, dim
+        const uint32_t at = o_addr + (uint32_t)((jr * 4 * QD + jd / (D / 4) * QD + jd % (D / 4)) * 4);
+        float lse[CLUSTER_MAX], x0[CLUSTER_MAX], x1[CLUSTER_MAX], top = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < CLUSTER_MAX; ++q) {
+            lse[q] = q < in_part ? sm100::ld_cluster_f32(sm100::map_to_cta(lse_addr + (uint32_t)jr * 4u, (uint32_t)q)) : -INFINITY;
+            x0[q] = q < in_part ? sm100::ld_cluster_f32(sm100::map_to_cta(at, (uint32_t)q)) : 0.f;
+            x1[q] = q < in_part ? sm100::ld_cluster_f32(sm100::map_to_cta(at + 4u, (uint32_t)q)) : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < CLUSTER_MAX; ++q) top = fmaxf(top, lse[q]);
+        float sum = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+        for (int q = 0; q < CLUSTER_MAX; ++q) {
+            const float w = lse[q] == -INFINITY ? 0.f : exp2f(lse[q] - (top == -INFINITY ? 0.f : top));   // a NaN joins
+            sum += w;
+            y0 = w != 0.f ? fmaf(w, x0[q], y0) : y0;
+            y1 = w != 0.f ? fmaf(w, x1[q], y1) : y1;
+        }
+        const float norm = sum == 0.f ? 0.f : 1.f / sum;
+        y0 *= norm;
+        y1 *= norm;
+        const int jrr = rt * ROWS + jr;
+        const size_t orow = (size_t)(b * p.k + jrr / p.G) * p.Hq + kvh * p.G + jrr % p.G;
+        if (n_parts == 1) {
+            *reinterpret_cast<__nv_bfloat162*>(p.out + orow * D + jd) = __floats2bfloat162_rn(y0, y1);
+        } else {
+            const size_t slot = (size_t)part * p.B * p.k * p.Hq + orow;
+            *reinterpret_cast<float2*>(p.part_o + slot * D + jd) = make_float2(y0, y1);
+            if (jd == 0) p.part_lse[slot] = sum == 0.f ? -INFINITY : top + log2f(sum);
+        }
+    }
+    sm100::cluster_sync();                                     // nobody's shared memory goes away while it is being read
 }
 
-// One warp per output row: joins the chunks' partial results.
+// One warp per output row: joins the clusters' partial results.
 template <int D>
 __global__ void __launch_bounds__(256) attn_quant_merge_kernel(const Params p) {
     constexpr int PER = D / 32;
@@ -387,17 +435,17 @@ __global__ void __launch_bounds__(256) attn_quant_merge_kernel(const Params p) {
     if (orow >= n_rows) return;
     int s, n;
     if (!sequence_of(p, (int)(orow / ((size_t)p.k * p.Hq)), &s, &n, false)) return;
-    const int n_chunks = chunks_of(p, n);
-    if (n_chunks == 1) return;                                 // written by its only chunk
+    const int n_parts = (chunks_of(p, n) + p.cluster - 1) / p.cluster;
+    if (n_parts == 1) return;                                  // written by its only cluster
     float mx = -INFINITY;
-    for (int c = lane; c < n_chunks; c += 32) mx = fmaxf(mx, p.part_lse[(size_t)c * n_rows + orow]);
+    for (int c = lane; c < n_parts; c += 32) mx = fmaxf(mx, p.part_lse[(size_t)c * n_rows + orow]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     const float base = mx == -INFINITY ? 0.f : mx;
     float acc[PER], sum = 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-    for (int c = 0; c < n_chunks; ++c) {
+    for (int c = 0; c < n_parts; ++c) {
         const float lse = p.part_lse[(size_t)c * n_rows + orow];
         const float w = lse == -INFINITY ? 0.f : exp2f(lse - base);
         const float* src = p.part_o + ((size_t)c * n_rows + orow) * D + lane * PER;
@@ -414,7 +462,7 @@ __global__ void __launch_bounds__(256) attn_quant_merge_kernel(const Params p) {
 }
 
 struct Plan {
-    int row_tiles, chunk_pages, chunks;
+    int row_tiles, chunk_pages, chunks, cluster, parts;
 };
 // The context is cut so that about four blocks per SM share the work, in chunks of two pages per warp at least.
 static Plan plan(int B, int k, int Hq, int Hkv, int max_seq_len) {
@@ -427,6 +475,8 @@ static Plan plan(int B, int k, int Hq, int Hkv, int max_seq_len) {
     per = (per + WARPS - 1) / WARPS * WARPS;
     pl.chunk_pages = (int)per;
     pl.chunks = pages > per ? (int)((pages + per - 1) / per) : 1;
+    pl.cluster = pl.chunks < CLUSTER_MAX ? pl.chunks : CLUSTER_MAX;
+    pl.parts = (pl.chunks + pl.cluster - 1) / pl.cluster;
     return pl;
 }
 
@@ -438,7 +488,7 @@ extern "C" size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, in
     if (B <= 0 || k <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || D <= 0 || max_seq_len < 0) return 0;
     // room for whichever kernel the call ends up using
     const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
-    const size_t small = pl.chunks == 1 ? 16 : (size_t)pl.chunks * B * k * Hq * (D + 1) * sizeof(float);
+    const size_t small = pl.parts == 1 ? 16 : (size_t)pl.parts * B * k * Hq * (D + 1) * sizeof(float);
     if (!umma_supported(D, k, Hq / Hkv, 1.f)) return small;
     const size_t large = umma_workspace_bytes(B, k, Hq, Hkv, max_seq_len);
     return large > small ? large : small;
@@ -476,7 +526,7 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     p.out = static_cast<__nv_bfloat16*>(out);
     const size_t n_rows = (size_t)B * k * Hq;
     p.part_o = static_cast<float*>(workspace);
-    p.part_lse = p.part_o + (size_t)pl.chunks * n_rows * D;
+    p.part_lse = p.part_o + (size_t)pl.parts * n_rows * D;
     p.B = B;
     p.k = k;
     p.Hq = Hq;
@@ -486,11 +536,12 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     p.scale_log2 = scale * LOG2E;
     p.row_tiles = pl.row_tiles;
     p.chunk_pages = pl.chunk_pages;
+    p.cluster = pl.cluster;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (umma_supported(D, k, p.G, scale)) return launch_umma(p, workspace, st);
-    const dim3 grid((unsigned)pl.chunks, (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
-    DEER_CUDA(launch_pdl(D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
-    if (pl.chunks > 1)
+    const dim3 grid((unsigned)(pl.parts * pl.cluster), (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
+    DEER_CUDA(launch_pdl_cluster(pl.cluster, D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
+    if (pl.parts > 1)
         DEER_CUDA(launch_pdl(D == 128 ? attn_quant_merge_kernel<128> : attn_quant_merge_kernel<64>, dim3((unsigned)((n_rows + 7) / 8)), dim3(256), 0, st, p));
     return DEER_OK;
 }

@@ -18,13 +18,14 @@ struct Params {
     const __nv_bfloat16* k_blk;
     const __nv_bfloat16* v_blk;
     __nv_bfloat16* out;
-    float* part_o;             // [chunks][B*k*Hq][D]  normalised partial outputs of the context chunks
-    float* part_lse;           // [chunks][B*k*Hq]     their log2-sum-exp
+    float* part_o;             // [parts][B*k*Hq][D]  normalised partial outputs, one per cluster of context chunks
+    float* part_lse;           // [parts][B*k*Hq]     their log2-sum-exp
     int B, k, Hq, G, mask;
     int max_seq_len;
     float scale_log2;
     int row_tiles;             // tiles of 16 query rows (block row major, then query head) per KV head
     int chunk_pages;           // full pages per context chunk
+    int cluster;               // chunks (thread blocks) that meet in a cluster
 };
 
 constexpr int ROWS_SMALL = 16;   // query rows of a warp-level tile

@@ -55,17 +55,6 @@ struct Args {
     int M, K, N, groups, m_tiles, split;
 };
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
-    return v;
-}
-
 template <int NT>
 __global__ void __launch_bounds__(Cfg<NT>::THREADS, 2)
 linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Args a) {
@@ -493,21 +482,7 @@ int launch(Args a, const void* x, const void* w, cudaStream_t st) {
     while (a.split < MAX_SPLIT && tiles * a.split * 2 <= room && a.groups >= a.split * 2 * 4) a.split *= 2;
     DEER_CHECK_ARG(tiles * a.split <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_linear_quant: too many tiles");
     DEER_CUDA(cudaFuncSetAttribute(linear_quant_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * a.split));
-    cfg.blockDim = dim3(C::THREADS);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)a.split;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    DEER_CUDA(cudaLaunchKernelEx(&cfg, linear_quant_kernel<NT>, tm_w, tm_x, a));
+    DEER_CUDA(launch_pdl_cluster(a.split, linear_quant_kernel<NT>, dim3((unsigned)(tiles * a.split)), dim3(C::THREADS), C::SMEM, st, tm_w, tm_x, a));
     return DEER_OK;
 }
 
