@@ -4,10 +4,10 @@
 // head, n mod 16 tail rows in bf16, and the block's own k rows in bf16.
 //
 // Warp-level kernel.  A page of one KV head is 16 tokens: exactly one contraction step of the second product and two
-// column tiles of the first.  A warp takes whole pages: each lane brings 16-byte pieces of K and V straight into
-// registers -- the pieces are laid out so that they ARE the operand fragments (the contraction index of q . k and the
-// column index of p v may be permuted freely, as long as the other side is permuted alike), so no byte passes through
-// shared memory -- and the codes become fp16 exactly.  The page's K scale multiplies the 16 scores; its V scale
+// column tiles of the first.  A warp takes whole pages: each lane copies, pages ahead and asynchronously, the
+// 16-byte pieces of K and V that it will use to shared memory of its own -- the pieces are laid out so that they ARE the
+// operand fragments (the contraction index of q . k and the column index of p v may be permuted freely, as long as the
+// other side is permuted alike), so the lanes exchange nothing -- and the codes become fp16 exactly.  The page's K scale multiplies the 16 scores; its V scale
 // multiplies the page's product before it joins the fp32 sums, so scales of any size work.  Queries are brought to
 // fp16 by a power of two per row (exact to 2^-24 of the row's largest), probabilities are at most 2^12 and keep fp16's
 // 11 bits down to 2^-26 of the row's maximum.  The warps of a block take pages in turn with running maxima of their
@@ -24,6 +24,19 @@ namespace attnq {
 constexpr int ROWS = ROWS_SMALL;
 constexpr int WARPS = 4;
 constexpr int CLUSTER_MAX = 8;                 // the portable limit
+constexpr int RESIDENT = 2;                    // blocks per SM
+constexpr int STAGES = 4;                      // pages of a warp under way or in use
+
+// Shared memory of a block: a ring of pages per warp, then (over it) the warps' results.
+template <int D>
+struct Smem {
+    static constexpr int LANE = D / 64 * 32 + D / 32 * 16;       // bytes of K and V of a page that a lane uses
+    static constexpr int STAGE = LANE * 32 + 16;                 // and the two scales
+    static constexpr int RING = WARPS * STAGES * STAGE;
+    static constexpr int QD = D / 4 + 1;       // a lane's dims of a row, one word apart from the next lane's: no two lanes share a bank
+    static constexpr int RESULTS = (WARPS * ROWS * 4 * QD + 2 * WARPS * ROWS + ROWS) * 4;
+    static constexpr int BYTES = RING > RESULTS ? RING : RESULTS;
+};
 constexpr float P_BIAS = 12.f;                 // probabilities are held as 2^12 p
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -49,13 +62,15 @@ __device__ __forceinline__ float quad_sum(float v) {
 // the dims hc * 64 + t4 * 16 + w * 4 + 0..3.  Column tile j of p v: column g8 is dim g8 * (D / 8) + j, so that this
 // lane's accumulators are the dims t4 * (D / 4) + 0 .. D / 4 - 1 of rows g8 and g8 + 8.
 template <int D>
-__global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) {
+__global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const Params p) {
     constexpr int HC = D / 64;                 // 16-byte pieces of a key row per lane
     constexpr int ND = D / 8;                  // column tiles of the output
     constexpr int VW = D / 32;                 // 32-bit words of a value row per lane (16-byte or 8-byte piece)
-    constexpr int QD = D / 4 + 1;              // a lane's dims of a row, one word apart from the next lane's: no two lanes share a bank
-    __shared__ float s_o[WARPS][ROWS][4 * QD];
-    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS], s_lse[ROWS];
+    constexpr int QD = Smem<D>::QD;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float (*s_o)[ROWS][4 * QD] = reinterpret_cast<float (*)[ROWS][4 * QD]>(smem);
+    float (*s_m)[ROWS] = reinterpret_cast<float (*)[ROWS]>(s_o + WARPS), (*s_l)[ROWS] = s_m + WARPS;
+    float* s_lse = s_l[WARPS];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
     const int Hkv = p.kv.n_kv_heads;
@@ -63,19 +78,58 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
     pdl_trigger();
     pdl_wait();
     const int page_lo = c * p.chunk_pages;
-    // the sequence's length and this warp's first page number are on their way together
+    // the sequence's length and the numbers of this warp's pages (lane j: its j-th one) are on their way together
     const int slot_id = p.seq_ids[b];
     const bool known = slot_id >= 0 && slot_id < p.kv.max_seqs;
     const int32_t* pt_row = p.kv.page_table + (size_t)(known ? slot_id : 0) * p.kv.max_pages;
-    int pg_next = page_lo + warp < p.kv.max_pages ? __ldcg(pt_row + page_lo + warp) : -1;
+    auto page_numbers = [&](int j0) {
+        const int page = page_lo + warp + (j0 + lane) * WARPS;
+        return page < p.kv.max_pages ? __ldcg(pt_row + page) : -1;
+    };
+    int pgs = page_numbers(0);
     int s, n;
     if (!sequence_of(p, b, &s, &n, c == 0 && blockIdx.y == 0 && tid == 0)) return;
     const int n_chunks = chunks_of(p, n);
     if (c / p.cluster * p.cluster >= n_chunks) return;         // none of the cluster's blocks has a chunk
     const int R = p.G * p.k;
     const bool busy = c < n_chunks;
-    const int page_hi = busy ? min(n / PAGE, page_lo + p.chunk_pages) : page_lo;
+    const int n_pages = busy ? max(0, (min(n / PAGE - page_lo, p.chunk_pages) - warp + WARPS - 1) / WARPS) : 0;   // this warp's
     const int n_tail = n % PAGE;
+
+    // Page j of this warp into its ring: the next call's page numbers are fetched with every 32nd.
+    int pgs_next = n_pages > 32 ? page_numbers(32) : -1;
+    auto bring = [&](int j) {
+        if (j > 0 && (j & 31) == 0) {
+            pgs = pgs_next;
+            pgs_next = n_pages > j + 32 ? page_numbers(j + 32) : -1;
+        }
+        int pg = __shfl_sync(0xffffffffu, pgs, j & 31);
+        if (pg < 0 || pg >= p.kv.num_pages) {
+            if (lane == 0) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
+            pg = 0;                                            // inside the pool; the status word flags the result
+        }
+        const size_t slab = (size_t)pg * Hkv + kvh;
+        const uint8_t* kp = static_cast<const uint8_t*>(p.kv.k_pool) + slab * PAGE * D;
+        const uint8_t* vp = static_cast<const uint8_t*>(p.kv.v_pool) + slab * PAGE * D;
+        const uint32_t st = smem_u32(smem + (warp * STAGES + j % STAGES) * Smem<D>::STAGE);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)            // keys g8, g8 + 8 of the page
+#pragma unroll
+            for (int hc = 0; hc < HC; ++hc) cp_async16(st + ((t * HC + hc) * 32 + lane) * 16, kp + (t * 8 + g8) * D + hc * 64 + t4 * 16, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {          // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
+            const uint8_t* src = vp + (2 * t4 + (e & 1) + (e >> 1) * 8) * D + g8 * (D / 8);
+            const uint32_t dst = st + 2 * HC * 512 + (e * 32 + lane) * (VW * 4);
+            if (D == 128) cp_async16(dst, src, 16);
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(dst), "l"(src));
+        }
+        if (lane < 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(st + Smem<D>::LANE * 32 + lane * 4), "l"((lane ? p.kq.v_scale : p.kq.k_scale) + slab));
+    };
+#pragma unroll 1
+    for (int j = 0; j < STAGES - 1; ++j) {
+        if (j < n_pages) bring(j);
+        cp_async_commit();
+    }
 
     uint32_t present, decoded;
     attn::row_state_sets(p.row_state, b, p.k, lane, &present, &decoded);
@@ -157,73 +211,56 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
         }
     };
 
-    // ---- full pages: this warp takes every WARPS-th page of the chunk ----
-    struct Page {
-        uint4 k[2][HC];                        // keys g8, g8 + 8 of the page
-        uint32_t v[4][VW];                     // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
-        float ks, vs;
-    };
-    auto load_page = [&](int page, Page& x) {                  // page number in pg_next; the one after it is fetched meanwhile
-        int pg = pg_next;
-        pg_next = page + WARPS < min(page_hi, p.kv.max_pages) ? __ldcg(pt_row + page + WARPS) : -1;
-        if (pg < 0 || pg >= p.kv.num_pages) {
-            if (lane == 0) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
-            pg = 0;                                            // inside the pool; the status word flags the result
-        }
-        const size_t slab = (size_t)pg * Hkv + kvh;
-        const uint8_t* kp = static_cast<const uint8_t*>(p.kv.k_pool) + slab * PAGE * D;
-        const uint8_t* vp = static_cast<const uint8_t*>(p.kv.v_pool) + slab * PAGE * D;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int hc = 0; hc < HC; ++hc) x.k[t][hc] = __ldcg(reinterpret_cast<const uint4*>(kp + (t * 8 + g8) * D + hc * 64 + t4 * 16));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint8_t* src = vp + (2 * t4 + (e & 1) + (e >> 1) * 8) * D + g8 * (D / 8);
-            if (D == 128) {
-                const uint4 w = __ldcg(reinterpret_cast<const uint4*>(src));
-                x.v[e][0] = w.x; x.v[e][1] = w.y; x.v[e][VW - 2] = w.z; x.v[e][VW - 1] = w.w;
-            } else {
-                const uint2 w = __ldcg(reinterpret_cast<const uint2*>(src));
-                x.v[e][0] = w.x; x.v[e][1] = w.y;
-            }
-        }
-        x.ks = __ldcg(p.kq.k_scale + slab);
-        x.vs = __ldcg(p.kq.v_scale + slab);
-    };
-    Page nx;
-    if (page_lo + warp < page_hi) load_page(page_lo + warp, nx);
-    for (int page = page_lo + warp; page < page_hi; page += WARPS) {
-        const Page x = nx;
-        if (page + WARPS < page_hi) load_page(page + WARPS, nx);
+    // ---- full pages ----
+    for (int j = 0; j < n_pages; ++j) {
+        __syncwarp();
+        if (j + STAGES - 1 < n_pages) bring(j + STAGES - 1);
+        cp_async_commit();
+        cp_async_wait<STAGES - 1>();
+        __syncwarp();
+        const unsigned char* st = smem + (warp * STAGES + j % STAGES) * Smem<D>::STAGE;
+        const float ks = *reinterpret_cast<const float*>(st + Smem<D>::LANE * 32), vs = *reinterpret_cast<const float*>(st + Smem<D>::LANE * 32 + 4);
         float sc[2][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
 #pragma unroll
             for (int hc = 0; hc < HC; ++hc) {
-                const uint32_t w[4] = {x.k[t][hc].x, x.k[t][hc].y, x.k[t][hc].z, x.k[t][hc].w};
+                const uint4 kw = *reinterpret_cast<const uint4*>(st + ((t * HC + hc) * 32 + lane) * 16);
+                const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mma_f16_16816(sc[t], qf[hc * 4 + i], codes_lo(w[i]), codes_hi(w[i]));
             }
-            const float f0 = f_row[0] * x.ks, f1 = f_row[1] * x.ks;
+            const float f0 = f_row[0] * ks, f1 = f_row[1] * ks;
             sc[t][0] *= f0; sc[t][1] *= f0; sc[t][2] *= f1; sc[t][3] *= f1;
         }
         softmax16(sc);
         const uint32_t pa[4] = {pack_f16(sc[0][0], sc[0][1]), pack_f16(sc[0][2], sc[0][3]), pack_f16(sc[1][0], sc[1][1]), pack_f16(sc[1][2], sc[1][3])};
+        uint32_t v[4][VW];                     // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned char* src = st + 2 * HC * 512 + (e * 32 + lane) * (VW * 4);
+            if (D == 128) {
+                const uint4 w = *reinterpret_cast<const uint4*>(src);
+                v[e][0] = w.x; v[e][1] = w.y; v[e][VW - 2] = w.z; v[e][VW - 1] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(src);
+                v[e][0] = w.x; v[e][1] = w.y;
+            }
+        }
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {      // dims 4 w + 2 h, + 1: the codes of two tokens side by side
-                const uint32_t a = __byte_perm(x.v[0][w], x.v[1][w], h ? 0x7362 : 0x5140);
-                const uint32_t d = __byte_perm(x.v[2][w], x.v[3][w], h ? 0x7362 : 0x5140);
+                const uint32_t a = __byte_perm(v[0][w], v[1][w], h ? 0x7362 : 0x5140);
+                const uint32_t d = __byte_perm(v[2][w], v[3][w], h ? 0x7362 : 0x5140);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float r[4] = {0.f, 0.f, 0.f, 0.f};
                     mma_f16_16816(r, pa, e ? codes_hi(a) : codes_lo(a), e ? codes_hi(d) : codes_lo(d));
-                    const int j = w * 4 + h * 2 + e;
+                    const int i = w * 4 + h * 2 + e;
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) o[j][z] = fmaf(r[z], x.vs, o[j][z]);
+                    for (int z = 0; z < 4; ++z) o[i][z] = fmaf(r[z], vs, o[i][z]);
                 }
             }
         }
@@ -329,7 +366,8 @@ __global__ void __launch_bounds__(WARPS * 32) attn_quant_kernel(const Params p) 
         }
     }
 
-    // ---- the warps meet ----
+    // ---- the warps meet (every page that was brought has been used) ----
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const float l = quad_sum(l_run[u]);
@@ -464,15 +502,18 @@ __global__ void __launch_bounds__(256) attn_quant_merge_kernel(const Params p) {
 struct Plan {
     int row_tiles, chunk_pages, chunks, cluster, parts;
 };
-// The context is cut so that about four blocks per SM share the work, in chunks of two pages per warp at least.
+// The context is cut so that the blocks of all units fill the SMs once (clusters of eight do not quite: they stay within
+// groups of SMs), in chunks of two pages per warp at least.  One cluster without a second kernel is the better choice up
+// to six pages per warp (one token, 8 heads: 10.2 against 11.9 us at 2048 tokens, 13.6 against 12.2 at 4096).
 static Plan plan(int B, int k, int Hq, int Hkv, int max_seq_len) {
     Plan pl;
     pl.row_tiles = (Hq / Hkv * k + ROWS - 1) / ROWS;
     const long long units = (long long)B * Hkv * pl.row_tiles, pages = max_seq_len / PAGE;
-    const long long want = (4LL * deer_sm_count() + units - 1) / units;
+    long long want = RESIDENT * deer_sm_count() * 9LL / 10 / units;
+    if (want < 1) want = 1;
+    if (want > CLUSTER_MAX) want = pages <= CLUSTER_MAX * WARPS * 6 ? CLUSTER_MAX : want / CLUSTER_MAX * CLUSTER_MAX;
     long long per = (pages + want - 1) / want;
     if (per < 2 * WARPS) per = 2 * WARPS;
-    per = (per + WARPS - 1) / WARPS * WARPS;
     pl.chunk_pages = (int)per;
     pl.chunks = pages > per ? (int)((pages + per - 1) / per) : 1;
     pl.cluster = pl.chunks < CLUSTER_MAX ? pl.chunks : CLUSTER_MAX;
@@ -540,7 +581,10 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (umma_supported(D, k, p.G, scale)) return launch_umma(p, workspace, st);
     const dim3 grid((unsigned)(pl.parts * pl.cluster), (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
-    DEER_CUDA(launch_pdl_cluster(pl.cluster, D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>, grid, dim3(WARPS * 32), 0, st, p));
+    const auto kernel = D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>;
+    const int smem = D == 128 ? Smem<128>::BYTES : Smem<64>::BYTES;
+    DEER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    DEER_CUDA(launch_pdl_cluster(pl.cluster, kernel, grid, dim3(WARPS * 32), smem, st, p));
     if (pl.parts > 1)
         DEER_CUDA(launch_pdl(D == 128 ? attn_quant_merge_kernel<128> : attn_quant_merge_kernel<64>, dim3((unsigned)((n_rows + 7) / 8)), dim3(256), 0, st, p));
     return DEER_OK;
