@@ -7,8 +7,9 @@
 
 namespace quant {
 
-// y = (x + residual) / rms * gamma per row.  A thread keeps its 16 columns (per chunk of 16 * THREADS) in registers
-// between the two phases -- the sum of squares over the row, the codes of the eight-lane groups -- so a row is read once.
+// y = (x + residual) / rms * gamma per row.  A thread keeps its columns, CHUNKS pieces of 8, in registers between the two
+// phases -- the sum of squares over the row, the codes of the sixteen-lane groups -- so a row is read once; with one or two
+// pieces all loads, the gain's too, are on their way before the first value is used (more would not fit the registers).
 template <int THREADS, int CHUNKS>
 __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloat16* x, const __nv_bfloat16* residual,
                                                                 const __nv_bfloat16* __restrict__ gamma, __nv_bfloat16* total,
@@ -19,31 +20,41 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
     const int groups = (hid + GROUP - 1) / GROUP;
     pdl_trigger();
     pdl_wait();
-    float h[CHUNKS][16];
+    constexpr bool EARLY = CHUNKS <= 2;
+    uint4 xv[CHUNKS], rv[CHUNKS], gv[CHUNKS];
+    auto piece = [&](const __nv_bfloat16* p, int c) {
+        const int col = (c * THREADS + tid) * 8;
+        return col < hid && p ? *reinterpret_cast<const uint4*>(p + col) : make_uint4(0, 0, 0, 0);
+    };
+    const __nv_bfloat16 *x_row = x + row * hid, *r_row = residual ? residual + row * hid : nullptr;
+    if (EARLY) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            xv[c] = piece(x_row, c);
+            rv[c] = piece(r_row, c);
+            gv[c] = piece(gamma, c);
+        }
+    }
+    float h[CHUNKS][8];
     float ss = 0.f;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const int col = (c * THREADS + tid) * 16;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) h[c][j] = 0.f;
-        if (col < hid) {
-            load_bf16x16(x + row * hid + col, h[c]);
-            if (residual) {
-                float r[16];
-                load_bf16x16(residual + row * hid + col, r);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) h[c][j] += r[j];
-            }
-            if (total) {
-                uint32_t t[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = pack_bf16(h[c][2 * j], h[c][2 * j + 1]);
-                *reinterpret_cast<uint4*>(total + row * hid + col) = make_uint4(t[0], t[1], t[2], t[3]);
-                *reinterpret_cast<uint4*>(total + row * hid + col + 8) = make_uint4(t[4], t[5], t[6], t[7]);
-            }
+        const int col = (c * THREADS + tid) * 8;
+        float r[8];
+        if (!EARLY) {
+            xv[c] = piece(x_row, c);
+            rv[c] = piece(r_row, c);
         }
+        unpack_bf16x8(xv[c], h[c]);
+        unpack_bf16x8(rv[c], r);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) ss += h[c][j] * h[c][j];
+        for (int j = 0; j < 8; ++j) {
+            if (residual) h[c][j] += r[j];
+            ss += h[c][j] * h[c][j];
+        }
+        if (total && col < hid)
+            *reinterpret_cast<uint4*>(total + row * hid + col) =
+                make_uint4(pack_bf16(h[c][0], h[c][1]), pack_bf16(h[c][2], h[c][3]), pack_bf16(h[c][4], h[c][5]), pack_bf16(h[c][6], h[c][7]));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -55,72 +66,78 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
     const float inv = rsqrtf(tot / (float)hid + eps);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const int col = (c * THREADS + tid) * 16;
-        if (c * THREADS * 16 >= hid) break;
-        if (col < hid) {
-            float g[16];
-            load_bf16x16(gamma + col, g);
+        const int col = (c * THREADS + tid) * 8;
+        if (c * THREADS * 8 >= hid) break;
+        if (!EARLY) gv[c] = piece(gamma, c);
+        float g[8];
+        unpack_bf16x8(gv[c], g);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) h[c][j] = h[c][j] * inv * g[j];
-        }
-        const float s = scale_of(max8(amax16(h[c])));
+        for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * inv * g[j];
+        const Divisor by(scale_of(max_of_16(col < hid ? amax8(h[c]) : 0u)));
         if (col < hid) {
-            *reinterpret_cast<uint4*>(codes + row * hid + col) = codes16(h[c], s);
-            if ((lane & 7) == 0) scales[row * groups + col / GROUP] = s;
+            *reinterpret_cast<uint2*>(codes + row * hid + col) = codes8(h[c], by);
+            if ((lane & 15) == 0) scales[row * groups + col / GROUP] = by.s;
         }
     }
 }
 
-// Eight lanes per group of 128 columns, groups of all rows laid end to end.
+// Sixteen lanes per group of 128 columns, groups of all rows laid end to end.
 template <bool GATED>
 __global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __restrict__ x, uint8_t* __restrict__ codes,
                                                        float* __restrict__ scales, int M, int K) {
     const int groups = (K + GROUP - 1) / GROUP;
-    const size_t item = (size_t)blockIdx.x * 32 + (threadIdx.x >> 3);          // group index over all rows
+    const size_t item = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);          // group index over all rows
     const size_t row = item / groups;
     const int g = (int)(item % groups);
-    const int col = g * GROUP + (threadIdx.x & 7) * 16;
+    const int col = g * GROUP + (threadIdx.x & 15) * 8;
     pdl_trigger();
     pdl_wait();
     const bool on = row < (size_t)M && col < K;
-    float v[16];
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
     if (on) {
         const __nv_bfloat16* src = x + row * (size_t)(GATED ? 2 * (size_t)K : K) + col;
-        load_bf16x16(src, v);
+        const uint4 a = *reinterpret_cast<const uint4*>(src);
         if (GATED) {
-            float u[16];
-            load_bf16x16(src + K, u);
+            const uint4 b = *reinterpret_cast<const uint4*>(src + K);
+            float u[8];
+            unpack_bf16x8(a, v);
+            unpack_bf16x8(b, u);
+            // (the quotient to 2 ulp: the gate's own exponential is no closer)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = v[j] / (1.f + __expf(-v[j])) * u[j];
+            for (int j = 0; j < 8; ++j) v[j] = __fdividef(v[j], 1.f + __expf(-v[j])) * u[j];
+        } else {
+            unpack_bf16x8(a, v);
         }
     }
-    const float s = scale_of(max8(amax16(v)));
+    const Divisor by(scale_of(max_of_16(amax8(v))));
     if (on) {
-        *reinterpret_cast<uint4*>(codes + row * K + col) = codes16(v, s);
-        if ((threadIdx.x & 7) == 0) scales[row * groups + g] = s;
+        *reinterpret_cast<uint2*>(codes + row * K + col) = codes8(v, by);
+        if ((threadIdx.x & 15) == 0) scales[row * groups + g] = by.s;
     }
 }
 
 // ---- the store into an 8-bit paged cache -----------------------------------------------------------------------
-// One thread block per (page that the new rows can touch, KV head, sequence), its first half for K, its second for V;
-// a thread holds 16 dims of one token.  Index 0 is the page that seq_len stands in; it alone reads tail rows, and it
-// also writes the new ones -- after its own are in registers -- because the page behind the last full one may share
-// their places (page mod 3).
+// One thread block per (run of PP pages that the new rows can touch, KV head, sequence), its first half for K, its second
+// for V; a thread holds 16 dims of one token, and the next page's while it works on one.  Page 0 is the one that seq_len
+// stands in; its block alone reads tail rows, and it also writes the new ones, last, because the page behind the last full
+// one may share their places (page mod 3).
 template <int D>
 __global__ void __launch_bounds__(2 * D) kv_store_kernel(deer_kv_desc kv, deer_kv_quant_desc q, const int32_t* __restrict__ seq_ids,
                                                          const __nv_bfloat16* __restrict__ k_rows, const __nv_bfloat16* __restrict__ v_rows,
-                                                         const int32_t* __restrict__ keep, int k) {
+                                                         const int32_t* __restrict__ keep, int k, int pages_per_block) {
     constexpr int PER_ROW = D / 16;                       // threads of a token
-    __shared__ uint32_t part[2 * D / 32];
+    __shared__ uint32_t part[2][2 * D / 32];
     const int tid = threadIdx.x;
     const bool is_v = tid >= D;
     const int t16 = (tid % D) / PER_ROW, col = (tid % PER_ROW) * 16;
-    const int h = blockIdx.y, b = blockIdx.z, Hkv = kv.n_kv_heads;
+    const int Hkv = kv.n_kv_heads;
+    const int h = (int)(blockIdx.x % (unsigned)Hkv), run = (int)(blockIdx.x / (unsigned)Hkv), b = blockIdx.y;   // the heads of a token are neighbours in memory
     pdl_trigger();
     pdl_wait();
     const int s = seq_ids[b];
+    const int kp = keep ? min(max(keep[b], 0), k) : k;
     if (s < 0 || s >= kv.max_seqs) {
         if (tid == 0) deer_report(kv.status, DEER_ERR_INVALID_ARG);
         return;
@@ -130,37 +147,48 @@ __global__ void __launch_bounds__(2 * D) kv_store_kernel(deer_kv_desc kv, deer_k
         if (tid == 0) deer_report(kv.status, DEER_ERR_INVALID_ARG);
         return;
     }
-    const int kp = keep ? min(max(keep[b], 0), k) : k;
-    const int end = n + kp;
-    const int page = n / DEER_PAGE_SIZE + (int)blockIdx.x;
-    const bool full = (page + 1) * DEER_PAGE_SIZE <= end;
-    if (kp == 0 || (!full && blockIdx.x != 0)) return;
+    if (kp == 0) return;
+    const int end = n + kp, full_pages = end / DEER_PAGE_SIZE;
     const __nv_bfloat16* rows = (is_v ? v_rows : k_rows) + (size_t)b * k * Hkv * D;
     __nv_bfloat16* tail = static_cast<__nv_bfloat16*>(is_v ? q.v_tail : q.k_tail) + ((size_t)s * Hkv + h) * DEER_TAIL_ROWS * D;
-    const int t = page * DEER_PAGE_SIZE + t16;            // this thread's token
-    if (full) {
-        float v[16];
-        load_bf16x16(t < n ? tail + (size_t)(t % DEER_TAIL_ROWS) * D + col : rows + ((size_t)(t - n) * Hkv + h) * D + col, v);
-        uint32_t m = amax16(v);
+    uint8_t* pool = static_cast<uint8_t*>(is_v ? kv.v_pool : kv.k_pool);
+    const int first = n / DEER_PAGE_SIZE + run * pages_per_block, last = min(first + pages_per_block, full_pages);
+    uint4 next[2];
+    int pg_next = -1;
+    auto bring = [&](int page) {                          // this thread's token of a full page, and the page's number
+        const int t = page * DEER_PAGE_SIZE + t16;
+        const uint4* src = reinterpret_cast<const uint4*>(t < n ? tail + (size_t)(t % DEER_TAIL_ROWS) * D + col
+                                                                : rows + ((size_t)(t - n) * Hkv + h) * D + col);
+        next[0] = src[0];
+        next[1] = src[1];
+        pg_next = page < kv.max_pages ? kv.page_table[(size_t)s * kv.max_pages + page] : -1;
+    };
+    if (first < last) bring(first);
+    for (int page = first; page < last; ++page) {
+        float v[2][8];
+        unpack_bf16x8(next[0], v[0]);
+        unpack_bf16x8(next[1], v[1]);
+        const int pg = pg_next;
+        if (page + 1 < last) bring(page + 1);
+        uint32_t m = max(amax8(v[0]), amax8(v[1]));
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if ((tid & 31) == 0) part[tid >> 5] = m;
-        __syncthreads();                                  // (also: the tail rows of this page are in registers)
+        if ((tid & 31) == 0) part[page & 1][tid >> 5] = m;
+        __syncthreads();                                  // (the first time also: the tail rows are in registers)
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w) m = max(m, part[(is_v ? D / 32 : 0) + w]);
-        const float sc = scale_of(m);
-        const int pg = page < kv.max_pages ? kv.page_table[(size_t)s * kv.max_pages + page] : -1;
+        for (int w = 0; w < D / 32; ++w) m = max(m, part[page & 1][(is_v ? D / 32 : 0) + w]);
+        const Divisor by(scale_of(m));
         if (pg < 0 || pg >= kv.num_pages) {
             if (tid == 0) deer_report(kv.status, DEER_ERR_BAD_PAGE);
-        } else {
-            const size_t slab = (size_t)pg * Hkv + h;
-            uint8_t* pool = static_cast<uint8_t*>(is_v ? kv.v_pool : kv.k_pool) + (slab * DEER_PAGE_SIZE + t16) * D + col;
-            *reinterpret_cast<uint4*>(pool) = codes16(v, sc);
-            if (tid % D == 0) (is_v ? q.v_scale : q.k_scale)[slab] = sc;
+            continue;
         }
+        const size_t slab = (size_t)pg * Hkv + h;
+        const uint2 lo = codes8(v[0], by), hi = codes8(v[1], by);
+        *reinterpret_cast<uint4*>(pool + (slab * DEER_PAGE_SIZE + t16) * D + col) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        if (tid % D == 0) (is_v ? q.v_scale : q.k_scale)[slab] = by.s;
     }
-    if (blockIdx.x == 0) {                                // the rows behind the last full page
-        const int tt = end / DEER_PAGE_SIZE * DEER_PAGE_SIZE + t16;
+    if (run == 0) {                                       // the rows behind the last full page
+        const int tt = full_pages * DEER_PAGE_SIZE + t16;
         if (tt >= n && tt < end) {
             const uint4* src = reinterpret_cast<const uint4*>(rows + ((size_t)(tt - n) * Hkv + h) * D + col);
             uint4* dst = reinterpret_cast<uint4*>(tail + (size_t)(tt % DEER_TAIL_ROWS) * D + col);
@@ -190,11 +218,12 @@ extern "C" int deer_rmsnorm_quant(const void* x, const void* residual, const voi
                           static_cast<const __nv_bfloat16*>(residual), static_cast<const __nv_bfloat16*>(gamma),
                           static_cast<__nv_bfloat16*>(total), static_cast<uint8_t*>(codes), scales, hid, eps);
     };
-    if (hid <= 2048) DEER_CUDA(run(rmsnorm_quant_kernel<128, 1>, 128));
-    else if (hid <= 4096) DEER_CUDA(run(rmsnorm_quant_kernel<256, 1>, 256));
-    else if (hid <= 8192) DEER_CUDA(run(rmsnorm_quant_kernel<512, 1>, 512));
-    else if (hid <= 16384) DEER_CUDA(run(rmsnorm_quant_kernel<512, 2>, 512));
-    else DEER_CUDA(run(rmsnorm_quant_kernel<1024, 4>, 1024));
+    if (hid <= 1024) DEER_CUDA(run(rmsnorm_quant_kernel<128, 1>, 128));
+    else if (hid <= 2048) DEER_CUDA(run(rmsnorm_quant_kernel<256, 1>, 256));
+    else if (hid <= 4096) DEER_CUDA(run(rmsnorm_quant_kernel<256, 2>, 256));
+    else if (hid <= 8192) DEER_CUDA(run(rmsnorm_quant_kernel<512, 2>, 512));
+    else if (hid <= 16384) DEER_CUDA(run(rmsnorm_quant_kernel<512, 4>, 512));
+    else DEER_CUDA(run(rmsnorm_quant_kernel<1024, 8>, 1024));
     return DEER_OK;
 }
 
@@ -205,7 +234,7 @@ extern "C" int deer_quantize(const void* x, int gated, void* codes, float* scale
     DEER_CHECK_ARG(M >= 0, DEER_ERR_INVALID_ARG, "deer_quantize: M must be >= 0");
     DEER_CHECK_ARG(K >= 16 && K % 16 == 0, DEER_ERR_UNSUPPORTED, "deer_quantize: K must be a multiple of 16");
     if (M == 0) return DEER_OK;
-    const long long items = (long long)M * ((K + GROUP - 1) / GROUP), blocks = (items + 31) / 32;
+    const long long items = (long long)M * ((K + GROUP - 1) / GROUP), blocks = (items + 15) / 16;
     DEER_CHECK_ARG(blocks <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_quantize: too many rows");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     DEER_CUDA(launch_pdl(gated ? quantize_kernel<true> : quantize_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st,
@@ -223,11 +252,19 @@ extern "C" int deer_kv_store(deer_kv* kv, const int32_t* seq_ids, const void* k_
     DEER_CHECK_ARG(kv->d.n_kv_heads <= 65535, DEER_ERR_UNSUPPORTED, "deer_kv_store: too many KV heads");
     if (B == 0 || k == 0) return DEER_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // k rows that start anywhere in a page fill at most (15 + k) / 16 pages to their end (at least one block: k >= 1)
-    const dim3 grid((unsigned)((15 + k) / DEER_PAGE_SIZE), (unsigned)kv->d.n_kv_heads, (unsigned)B);
+    // k rows that start anywhere in a page fill at most (15 + k) / 16 pages to their end (at least one: k >= 1).  A page per
+    // block while all blocks fit the SMs at once; a block starts with three loads that wait for one another, so long
+    // prompts give it up to eight (4 prompts of 4096 rows, a random part of each kept, 8 heads of 128: 1 page 24.1, 2 18.8,
+    // 8 15.7, 16 21.5 us, the last because blocks behind the kept rows have nothing to do).
+    const long long pages = (15 + k) / DEER_PAGE_SIZE, blocks = pages * kv->d.n_kv_heads * B;
+    const long long rounds = (blocks + 4LL * deer_sm_count() - 1) / (4LL * deer_sm_count());
+    const int per = rounds > 8 ? 8 : (int)rounds;
+    const long long runs = (pages + per - 1) / per * kv->d.n_kv_heads;
+    DEER_CHECK_ARG(runs <= 0x7fffffffLL, DEER_ERR_UNSUPPORTED, "deer_kv_store: too many rows");
+    const dim3 grid((unsigned)runs, (unsigned)B);
     auto run = [&](auto kernel, int threads) {
         return launch_pdl(kernel, grid, dim3((unsigned)threads), 0, st, kv->d, kv->q, seq_ids, static_cast<const __nv_bfloat16*>(k_rows),
-                          static_cast<const __nv_bfloat16*>(v_rows), keep, k);
+                          static_cast<const __nv_bfloat16*>(v_rows), keep, k, per);
     };
     if (kv->d.head_dim == 128) DEER_CUDA(run(kv_store_kernel<128>, 256));
     else DEER_CUDA(run(kv_store_kernel<64>, 128));
