@@ -530,7 +530,7 @@ extern "C" size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, in
     // room for whichever kernel the call ends up using
     const Plan pl = plan(B, k, Hq, Hkv, max_seq_len);
     const size_t small = pl.parts == 1 ? 16 : (size_t)pl.parts * B * k * Hq * (D + 1) * sizeof(float);
-    if (!umma_supported(D, k, Hq / Hkv, 1.f)) return small;
+    if (!use_umma(B, D, k, Hq, Hkv, max_seq_len, 1.f)) return small;
     const size_t large = umma_workspace_bytes(B, k, Hq, Hkv, max_seq_len);
     return large > small ? large : small;
 }
@@ -579,7 +579,7 @@ extern "C" int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids, const 
     p.chunk_pages = pl.chunk_pages;
     p.cluster = pl.cluster;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (umma_supported(D, k, p.G, scale)) return launch_umma(p, workspace, st);
+    if (use_umma(B, D, k, Hq, Hkv, max_seq_len, scale)) return launch_umma(p, workspace, st);
     const dim3 grid((unsigned)(pl.parts * pl.cluster), (unsigned)(Hkv * pl.row_tiles), (unsigned)B);
     const auto kernel = D == 128 ? attn_quant_kernel<128> : attn_quant_kernel<64>;
     const int smem = D == 128 ? Smem<128>::BYTES : Smem<64>::BYTES;

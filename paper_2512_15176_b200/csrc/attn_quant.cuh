@@ -31,7 +31,7 @@ struct Params {
 constexpr int ROWS_SMALL = 16;   // query rows of a warp-level tile
 
 // tcgen05 variant (attn_quant_umma.cu).
-bool umma_supported(int D, int k, int G, float scale);
+bool use_umma(int B, int D, int k, int Hq, int Hkv, int max_seq_len, float scale);
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len);
 int launch_umma(const Params& p, void* workspace, cudaStream_t st);
 

@@ -916,8 +916,16 @@ static int pick_blocks(int B, int Hkv, int row_tiles, int max_seq_len) {
 
 // More query rows than a warp's tile of 16 hold share the KV stream here; fewer leave the 128 lanes idle while the
 // warp-level kernel reads the same bytes with less latency.
-bool umma_supported(int D, int k, int G, float scale) {
-    return D == umma::HD && G <= 128 && k * G > ROWS_SMALL && scale > 0.f;
+// This kernel takes about 19 us for any call, however short (its pipeline's start, the queries' split, two joins); the
+// warp-level one 6 to 8, and then the time for its pages, of which each costs 16 query rows as much as this one spends on
+// 128.  Measured in us, warp-level against this, 32 query and 8 KV heads, tokens: 32 rows x 1003 13.7 / 22.4, x 2048
+// 19.3 / 22.7, x 4096 28.1 / 27.5, x 8192 45.4 / 31.0; 8 sequences of 8 rows x 1003 20.2 / 27.4, x 4096 47.7 / 42.5;
+// and with more row tiles than fit the SMs at once (16 sequences, 4 KV heads, 32 rows x 200) 36.0 / 20.5.
+bool use_umma(int B, int D, int k, int Hq, int Hkv, int max_seq_len, float scale) {
+    const int G = Hq / Hkv;
+    if (D != umma::HD || G > 128 || !(scale > 0.f) || k * G <= ROWS_SMALL) return false;
+    const long long tiles = (long long)B * Hkv * ((k * G + ROWS_SMALL - 1) / ROWS_SMALL);    // the warp-level kernel's
+    return tiles > 2LL * deer_sm_count() || tiles * (max_seq_len / PAGE + 3) > 16384;
 }
 
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len) {

@@ -438,3 +438,63 @@ def test_reserve_store_commit_soak():
         assert (kv.seq_len.cpu().numpy() == okv.seq_len).all()
         assert (kv.n_pages.cpu().numpy() == -(-okv.seq_len // 16)).all()
         _same_cache(kv, okv, f"turn {turn}")
+
+
+@pytest.fixture()
+def long_bound(monkeypatch):
+    """The attention called with a bound on the lengths that is far above them: the kernel for long contexts, whatever the
+    lengths are (short calls take another one)."""
+    from paper_2512_15176_b200 import binding as L
+    real = L.deer_block_attn_quant
+
+    def call(kv, ids, q, kb, vb, out, states, mask, scale, msl, ws):
+        B, k, Hq, D = q.shape
+        ws = torch.full((L.deer_block_attn_quant_workspace_bytes(B, k, Hq, kv.n_kv_heads, D, 1 << 20),), 255, dtype=torch.uint8, device="cuda")
+        real(kv, ids, q, kb, vb, out, states, mask, scale, 1 << 20, ws)
+
+    monkeypatch.setattr(L, "deer_block_attn_quant", call)
+
+
+@pytest.mark.parametrize("lengths,k,Hq,Hkv,D,mask", CASES)
+def test_attention_under_a_long_bound(long_bound, lengths, k, Hq, Hkv, D, mask):
+    test_attention(lengths, k, Hq, Hkv, D, mask)
+
+
+@pytest.mark.parametrize("k,Hq,Hkv,D", [(32, 16, 4, 128), (16, 8, 1, 128), (5, 16, 2, 128)])
+def test_spread_scales_under_a_long_bound(long_bound, k, Hq, Hkv, D):
+    test_attention_spread_scales_and_scores(k, Hq, Hkv, D)
+
+
+@pytest.mark.parametrize("k,Hq,Hkv,D", [(32, 16, 4, 128), (20, 8, 1, 128)])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_nonfinite_rows_under_a_long_bound(long_bound, k, Hq, Hkv, D, what):
+    test_attention_nonfinite_rows_reach_only_rows_that_see_them(k, Hq, Hkv, D, what)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.05])
+@pytest.mark.parametrize("n,msl", [(100, 100), (3000, 1 << 20)])
+def test_attention_with_a_scale_that_is_not_positive(n, msl, scale):
+    """Zero: every visible key weighs the same; below zero: the least similar key weighs most."""
+    from paper_2512_15176_b200 import binding as L
+    k, Hq, Hkv, D = 32, 16, 4, 128
+    kv, okv = _cache([n], Hkv, D, 0, 412)
+    q, kb, vb = (W.normal(412, x, (1, k, h, D), 1.0) for x, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    out = torch.empty(1, k, Hq, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((L.deer_block_attn_quant_workspace_bytes(1, k, Hq, Hkv, D, msl),), 255, dtype=torch.uint8, device="cuda")
+    L.deer_block_attn_quant(kv, _ids(1), q.cuda(), kb.cuda(), vb.cuda(), out, None, 0, scale, msl, ws)
+    check_attention(out, q, kb, vb, okv, [0], 0, scale, None, f"scale {scale}")
+
+
+def test_attention_of_one_long_sequence_and_few_rows():
+    """More chunks than one cluster takes, and more pages than a warp's lanes hold numbers of: clusters whose parts a second
+    kernel joins, next to a sequence that leaves whole clusters and chunks without work."""
+    from paper_2512_15176_b200 import binding as L
+    lengths, k, Hq, Hkv, D = [40000, 37, 9000], 3, 8, 2, 128
+    kv, okv = _cache(lengths, Hkv, D, 0, 413)
+    q, kb, vb = (W.normal(413, x, (3, k, h, D), 1.0) for x, h in (("q", Hq), ("k", Hkv), ("v", Hkv)))
+    for msl in (40000, 600000):                                  # (the larger bound: fewer, longer chunks)
+        out = torch.full((3, k, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        ws = torch.full((L.deer_block_attn_quant_workspace_bytes(3, k, Hq, Hkv, D, msl),), 255, dtype=torch.uint8, device="cuda")
+        L.deer_block_attn_quant(kv, _ids(3), q.cuda(), kb.cuda(), vb.cuda(), out, None, 0, 1 / math.sqrt(D), msl, ws)
+        assert L.deer_kv_status(kv) == 0
+        check_attention(out, q, kb, vb, okv, [0, 1, 2], 0, 1 / math.sqrt(D), None, f"bound {msl}")
