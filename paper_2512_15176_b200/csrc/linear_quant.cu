@@ -10,10 +10,12 @@
 // few hundred, above that the MMAs together with those scaled sums.
 //
 // Few output columns do not fill the SMs, so a cluster of `split` blocks shares an output tile, each with a range of
-// the column groups; the partial sums meet in shared memory (every block of the cluster adds up, in rank order, its
-// part of the tile's rows of x), so there is no workspace, no second kernel, and the order of the sums is fixed.
+// the column groups.  Every block of the cluster owns a part of the tile's rows of x: the others send it their partial sums
+// for those, into its shared memory, and it adds them up in rank order, so there is no workspace, no second kernel, and the
+// order of the sums is fixed.  (Sent, not fetched: a remote load takes about 700 cycles, and a block whose memory nobody
+// reads needs no barrier at its end.  32 rows, 12288 x 4096: fetched 15.4, sent 13.9 us.)
 //
-// More than 128 rows: the second kernel, pairs of blocks, the rows of x on the lanes (see there).
+// Many rows: the second kernel, pairs of blocks, the rows of x on the lanes (see there).
 //
 // Warp roles: warp 0 = TMA producer, warp 1 = MMA issuer (+ TMEM owner), the others = epilogue.  All waits are bounded;
 // a block whose wait runs out leaves its output unwritten (and so does its cluster).
@@ -35,16 +37,19 @@ constexpr int MAX_SPLIT = 8;                   // blocks of a cluster: the porta
 template <int NT>
 struct Cfg {
     static constexpr int STAGE = W_BYTES + NT * GROUP;
-    static constexpr int STAGES = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3;
+    static constexpr int STAGES = NT == 16 ? 5 : 4;
     // Column groups that change hands together (each with NT accumulator columns of its own): a hand-over costs the issuer and
     // the epilogue several hundred cycles of waits and arrivals, as much as four MMAs.  Two hand-overs' worth of accumulators.
-    static constexpr int H = NT <= 32 ? 4 : NT == 64 ? 2 : 1;
+    static constexpr int H = NT <= 32 ? 4 : 2;
     static constexpr int NBUF = 2;
     static constexpr int TMEM_COLS = NT * H * NBUF;
     static constexpr int CH = NT < 32 ? 16 : 32;                  // columns of one tensor-memory load
     static constexpr int EPI_WARPS = 4;
     static constexpr int THREADS = 64 + EPI_WARPS * 32;
-    static constexpr int SMEM = STAGES * STAGE + 1024 /*alignment slack*/ + 2 * H * NT * 4 /*scales*/ + (2 * STAGES + 2 * NBUF) * 8 + 16;
+    // The cluster's partial sums have a place of their own where it is small; in the ring they have to wait for the slowest block.
+    static constexpr bool OWN_PLACE = NT <= 32;
+    static constexpr int PLACE = NT * BN * 4;
+    static constexpr int SMEM = (OWN_PLACE ? PLACE : 0) + STAGES * STAGE + 1024 /*alignment slack*/ + 2 * H * NT * 4 /*scales*/ + (2 * STAGES + 2 * NBUF) * 8 + 16 + MAX_SPLIT * EPI_WARPS * 4;
 };
 
 struct Args {
@@ -62,10 +67,12 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     constexpr int EPI_THREADS = C::EPI_WARPS * 32;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float* sc = reinterpret_cast<float*>(ring + C::STAGES * C::STAGE);           // [2][H][NT] x_scale * w_scale of a hand-over's column groups
+    unsigned char* place = ring + (C::OWN_PLACE ? C::STAGES * C::STAGE : 0);     // [rank][4 rows][128 columns][4] partial sums
+    float* sc = reinterpret_cast<float*>(ring + C::STAGES * C::STAGE + (C::OWN_PLACE ? C::PLACE : 0));   // [2][H][NT] x_scale * w_scale of a hand-over's column groups
     uint64_t* bars = reinterpret_cast<uint64_t*>(sc + 2 * C::H * NT);            // full, empty [STAGES]; tfull, tempty [NBUF]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 2 * C::NBUF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    uint32_t* whole = tmem_slot + 4;                                             // [rank][epilogue warp]: its sums are complete
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)blockIdx.x % a.split;
@@ -103,8 +110,19 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (C::OWN_PLACE && a.split > 1) cluster_arrive();             // (waited for before anything is sent)
 
     uint64_t acc[NT / 2];                          // two rows of x each
+    bool alive = true;
+    const int lane_row = (warp & 3) * 32 + lane;                   // TMEM lane = output column within the tile
+    const int n = n0 + lane_row;
+    // the rows that this block writes, and the residual of the first of them, which may have to come from far
+    const int own_rows = NT / a.split, own0 = m0 + rank * own_rows;
+    float res[4] = {0.f, 0.f, 0.f, 0.f};
+    auto fetch_residual = [&](int m) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) res[q] = a.residual && q < own_rows && m + q < a.M && n < a.N ? __bfloat162float(a.residual[(size_t)(m + q) * a.N + n]) : 0.f;
+    };
     if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < ng; ++i) {
@@ -147,7 +165,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         const float* xs = (brings && m0 + my_row < a.M) ? a.x_scale + (size_t)(m0 + my_row) * a.groups + g0 + my_u : nullptr;
         const float* ws = a.w_scale + (size_t)(n0 / GROUP) * a.groups + g0 + my_u;
         float nx = xs && my_u < ng ? xs[0] : 0.f, nw = xs && my_u < ng ? ws[0] : 0.f;
-        bool alive = true;
+        fetch_residual(own0);
         for (int i0 = 0, n = 0; i0 < ng; i0 += C::H, ++n) {
             const int b = n % C::NBUF, cnt = min(C::H, ng - i0);
             float* slot = sc + (n & 1) * C::H * NT;
@@ -186,66 +204,70 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         }
     }
 
-    // ---- the tile's rows of x: this block writes all of them, or adds up its part of the cluster's partial sums ----
-    const int lane_row = (warp & 3) * 32 + lane;                   // TMEM lane = output column within the tile
-    const int n = n0 + lane_row;
-    auto put = [&](int j, float v) {                               // row m0 + j of the output
-        const int m = m0 + j;
-        if (m >= a.M || n >= a.N) return;
-        const size_t at = (size_t)m * a.N + n;
-        if (a.residual) v += __bfloat162float(a.residual[at]);
-        a.y[at] = __float2bfloat16(v);
+    // ---- the tile's rows of x: this block writes all of them, or its part of them ----
+    auto put = [&](int m, const float (&v)[4], int rows) {         // rows m .. of the output
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < rows && m + q < a.M && n < a.N) a.y[(size_t)(m + q) * a.N + n] = __float2bfloat16(v[q] + res[q]);
     };
     if (a.split == 1) {
-        if (warp >= 2 && !*abort_flag) {
+        if (warp >= 2 && alive) {
 #pragma unroll
-            for (int j = 0; j < NT; j += 2) {
-                float lo, hi;
-                unpack_f32x2(acc[j / 2], lo, hi);
-                put(j, lo);
-                put(j + 1, hi);
+            for (int j = 0; j < NT; j += 4) {
+                float v[4];
+                unpack_f32x2(acc[j / 2], v[0], v[1]);
+                unpack_f32x2(acc[j / 2 + 1], v[2], v[3]);
+                if (j > 0) fetch_residual(m0 + j);
+                put(m0 + j, v, 4);
             }
         }
     } else {
-        // every operand that was requested has been consumed (or the block is aborting and writes nothing): the ring is free
-        float* buf = reinterpret_cast<float*>(ring);               // [NT][128]
-        if (warp >= 2 && !*abort_flag) {
-#pragma unroll
-            for (int j = 0; j < NT; j += 2) {
-                float lo, hi;
-                unpack_f32x2(acc[j / 2], lo, hi);
-                buf[j * BN + lane_row] = lo;
-                buf[(j + 1) * BN + lane_row] = hi;
-            }
-        }
         __syncwarp();
-        cluster_sync();
-        // (every load is on its way before the first is used: one at a time they would take 16 remote latencies and more)
-        const uint32_t flag_addr = smem_u32(const_cast<int*>(abort_flag));
-        uint32_t bad = 0;
-#pragma unroll
-        for (int r = 0; r < MAX_SPLIT; ++r)
-            if (r < a.split) bad |= ld_cluster_u32(map_to_cta(flag_addr, (uint32_t)r));
+        // every block has begun, or (its ring is the place) every operand that was requested has been consumed
+        if (!C::OWN_PLACE) cluster_arrive();
+        cluster_wait();
         if (warp >= 2) {
-            const int lo = NT * rank / a.split, hi = min(NT * (rank + 1) / a.split, a.M - m0);
-            for (int j0 = lo; j0 < hi; j0 += 4) {
-                float v[4][MAX_SPLIT];
+            const uint32_t place_addr = smem_u32(place);
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int r = 0; r < MAX_SPLIT; ++r)
-                        v[q][r] = (j0 + q < hi && r < a.split) ? ld_cluster_f32(map_to_cta(ring_addr + (uint32_t)(((j0 + q) * BN + lane_row) * 4), (uint32_t)r)) : 0.f;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float sum = v[q][0];
-#pragma unroll
-                    for (int r = 1; r < MAX_SPLIT; ++r) sum += v[q][r];
-                    if (j0 + q < hi && bad == 0) put(j0 + q, sum);
+            for (int j = 0; j < NT; j += 4) {                      // rows j .. j + 3 belong to one owner, or two each to two
+                if (m0 + j >= a.M) break;
+                float v[4];
+                unpack_f32x2(acc[j / 2], v[0], v[1]);
+                unpack_f32x2(acc[j / 2 + 1], v[2], v[3]);
+                if (own_rows >= 4) {
+                    const uint32_t at = place_addr + (uint32_t)(((rank * own_rows + j % own_rows) * BN + lane_row * 4) * 4);
+                    st_cluster_f32x4(map_to_cta(at, (uint32_t)(j / own_rows)), v[0], v[1], v[2], v[3]);
+                } else {
+                    const uint32_t at = place_addr + (uint32_t)((rank * 2 * BN + lane_row * 2) * 4);
+                    st_cluster_f32x2(map_to_cta(at, (uint32_t)(j / 2)), v[0], v[1]);
+                    st_cluster_f32x2(map_to_cta(at, (uint32_t)(j / 2 + 1)), v[2], v[3]);
                 }
             }
+            if (lane < a.split) st_cluster_u32(map_to_cta(smem_u32(whole + rank * C::EPI_WARPS + (warp & 3)), (uint32_t)lane), alive ? 1u : 0u);
         }
         __syncwarp();
-        cluster_sync();                                            // nobody's shared memory goes away while it is being read
+        cluster_arrive();
+        cluster_wait();
+        if (warp >= 2 && !*abort_flag) {
+            bool ok = true;
+            for (int r = 0; r < a.split; ++r) ok = ok && whole[r * C::EPI_WARPS + (warp & 3)] != 0u;
+            for (int j = 0; j < own_rows && own0 + j < a.M && ok; j += 4) {
+                if (j > 0) fetch_residual(own0 + j);
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < MAX_SPLIT; ++r) {
+                    if (r >= a.split) break;
+                    if (own_rows >= 4) {
+                        const float4 w = *reinterpret_cast<const float4*>(place + ((r * own_rows + j) * BN + lane_row * 4) * 4);
+                        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+                    } else {
+                        const float2 w = *reinterpret_cast<const float2*>(place + (r * 2 * BN + lane_row * 2) * 4);
+                        v[0] += w.x; v[1] += w.y;
+                    }
+                }
+                put(own0 + j, v, own_rows);
+            }
+        }
     }
 
     tcgen05_fence_before();
@@ -261,7 +283,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     }
 }
 
-// ---- more than 128 rows of x: pairs of blocks ---------------------------------------------------------------------
+// ---- many rows of x: pairs of blocks ---------------------------------------------------------------------
 // A cluster of two shares tiles of 256 rows of x (128 on each block's TMEM lanes) by BNP rows of w: one cta_group::2 MMA
 // reads half of the weight rows from each block's shared memory, so a block stages 128 + BNP / 2 rows per column group
 // where a tile of its own would take 128 + BNP.  A row of x per thread makes the scale of a column group ONE number per
@@ -274,10 +296,11 @@ struct PairCfg {
     static constexpr int HALF = BNP / 2;                          // weight rows a block stages; columns of an epilogue warp
     static constexpr int X_BYTES = 128 * GROUP;
     static constexpr int STAGE = X_BYTES + HALF * GROUP;
-    static constexpr int STAGES = BNP == 256 ? 6 : 8;
-    static constexpr int TMEM_COLS = 2 * BNP;
-    static constexpr int THREADS = 64 + 8 * 32;
-    static constexpr int SMEM = STAGES * STAGE + 1024 + (2 * STAGES + 4) * 8 + 16;
+    static constexpr int STAGES = 216 * 1024 / STAGE;
+    static constexpr int NBUF = 512 / BNP;                        // accumulators: all of tensor memory
+    static constexpr int EPI_WARPS = 8;
+    static constexpr int THREADS = 64 + EPI_WARPS * 32;
+    static constexpr int SMEM = STAGES * STAGE + 1024 + (2 * STAGES + 2 * NBUF) * 8 + 16;
 };
 
 template <int BNP>
@@ -286,11 +309,11 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
     using C = PairCfg<BNP>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + C::STAGES * C::STAGE);   // full, empty [STAGES]; tfull, tempty [2]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + C::STAGES * C::STAGE);   // full, empty [STAGES]; tfull, tempty [NBUF]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 2 * C::NBUF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // (uniform, and known to be)
     const uint32_t rank = cluster_ctarank();
     const int cluster = (int)blockIdx.x >> 1, n_clusters = (int)gridDim.x >> 1;
     const int tiles = a.m_tiles * ((a.N + BNP - 1) / BNP);
@@ -299,15 +322,15 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
     auto full = [&](int s) { return bar_base + 8u * s; };
     auto empty = [&](int s) { return bar_base + 8u * (C::STAGES + s); };
     auto tfull = [&](int b) { return bar_base + 8u * (2 * C::STAGES + b); };
-    auto tempty = [&](int b) { return bar_base + 8u * (2 * C::STAGES + 2 + b); };
+    auto tempty = [&](int b) { return bar_base + 8u * (2 * C::STAGES + C::NBUF + b); };
     if (tid == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < C::NBUF; ++b) {
             mbar_init(tfull(b), 1);
-            mbar_init(tempty(b), 16);                              // eight epilogue warps in each of the two blocks
+            mbar_init(tempty(b), 2 * C::EPI_WARPS);                // both blocks' epilogue warps
         }
         *abort_flag = 0;
         mbar_init_fence();
@@ -318,7 +341,7 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
         const int n0 = cluster / a.m_tiles * BNP + (int)rank * C::HALF;
         for (int i = 0; i < a.groups && i < C::STAGES && n0 < a.N; ++i) tma_prefetch_2d(&tm_w, i * GROUP, n0);
     }
-    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), C::TMEM_COLS);
+    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
     pdl_trigger();
     tcgen05_fence_before();
     __syncthreads();
@@ -344,23 +367,29 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
             }
         }
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
             const uint32_t idesc = make_idesc_e4m3_pair(BNP);
+            const bool leader = elect_one();
             int it = 0;
             bool ok = true;
             for (int t = cluster; t < tiles && ok; t += n_clusters) {
                 for (int i = 0; i < a.groups; ++i, ++it) {
-                    const int s = it % C::STAGES, b = it & 1;
-                    if (!mbar_wait(tempty(b), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                    if (!mbar_wait(full(s), (uint32_t)(it / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    const int s = it % C::STAGES, b = it % C::NBUF;
+                    ok = mbar_wait(tempty(b), ((uint32_t)(it / C::NBUF) & 1u) ^ 1u, abort_flag) &&
+                         mbar_wait(full(s), (uint32_t)(it / C::STAGES) & 1u, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
                     tcgen05_fence_after();
                     const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
                     const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + C::X_BYTES);
+                    if (leader) {
 #pragma unroll
-                    for (int kk = 0; kk < GROUP / 32; ++kk)
-                        umma_f8_ss_pair(tmem_base + (uint32_t)(b * BNP), xd + (uint64_t)(kk * 2), wd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
-                    umma_commit_pair(tfull(b), 3);
-                    umma_commit_pair(empty(s), 3);
+                        for (int kk = 0; kk < GROUP / 32; ++kk)
+                            umma_f8_ss_pair(tmem_base + (uint32_t)(b * BNP), xd + (uint64_t)(kk * 2), wd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
+                        umma_commit_pair(tfull(b), 3);
+                        umma_commit_pair(empty(s), 3);
+                    }
+                    __syncwarp();
                 }
             }
         }
@@ -380,13 +409,13 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
             for (int j = 0; j < C::HALF / 2; ++j) acc[j] = 0;
             float nx = xs[0], nw = ws[0];
             for (int i = 0; i < a.groups; ++i, ++it) {
-                const int b = it & 1;
+                const int b = it % C::NBUF;
                 const float sc = nx * nw;
                 if (i + 1 < a.groups) {                            // the next column group's scales
                     nx = xs[i + 1];
                     nw = ws[i + 1];
                 }
-                const bool got = mbar_wait(tfull(b), (uint32_t)(it >> 1) & 1u, abort_flag);
+                const bool got = mbar_wait(tfull(b), (uint32_t)(it / C::NBUF) & 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                 tcgen05_fence_after();
                 const uint64_t s2 = pack_f32x2(sc, sc);
@@ -441,7 +470,7 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
     if (warp == 1) {
         __syncwarp();
         tcgen05_fence_after();
-        tmem_dealloc_pair(tmem_base, C::TMEM_COLS);
+        tmem_dealloc_pair(tmem_base, 512);
     }
 }
 
@@ -512,7 +541,14 @@ extern "C" int deer_linear_quant(const void* x, const float* x_scale, const void
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M <= 16) return launch<16>(a, x, w, st);
     if (M <= 32) return launch<32>(a, x, w, st);
-    if (M <= 64) return launch<64>(a, x, w, st);
-    if (M <= 128) return launch<128>(a, x, w, st);
-    return launch_pair<256>(a, x, w, st);
+    // Above 32 rows: the first kernel while its tiles leave room for four blocks each at the least, or there are not more
+    // rows than one of them has (us, first kernel / pairs: 128 x 4096 x 4096 13.2 / 14.3, 128 x 12288 x 4096 23.9 / 33, 128 x 4096 x 8192 21.7 / 14.5,
+    // 256 x 4096 x 4096 20.2 / 14.5, 64 x 4096 x 24576 34.5 / 41.4).
+    const long long few = (long long)((M + 63) / 64) * ((N + BN - 1) / BN);
+    if (M <= 64 || few <= deer_sm_count() / 2) return launch<64>(a, x, w, st);
+    // Pairs: the tiles of the product are done in rounds of one per pair of SMs; a round of 128 weight rows takes 0.57 of
+    // one of 256 (512 rows, 12288 x 4096, one round: 34.0 / 58.4 us; 4096 x 24576, six rounds or three: 80.4 / 75.3).
+    const long long pairs = deer_sm_count() / 2, m_tiles = (M + 255) / 256;
+    const long long wide = (m_tiles * ((N + 255) / 256) + pairs - 1) / pairs, narrow = (m_tiles * ((N + 127) / 128) + pairs - 1) / pairs;
+    return narrow * 57 < wide * 100 ? launch_pair<128>(a, x, w, st) : launch_pair<256>(a, x, w, st);
 }
