@@ -111,6 +111,9 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     return mbar_try_wait(bar, parity) || wait_slowly(bar, parity, abort_flag);
 }
 
+// A value that is the same in every lane, told to the compiler: what follows from it can live in uniform registers.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // Places in the list for sequence b: HEAD, its full pages four at a time, the bf16 tile; 0 if the sequence cannot be used.
 __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out, int* s_out) {
     const int s = p.seq_ids[b];
@@ -271,7 +274,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     volatile int* abort_flag = &sh.abort_flag;
     const AttnParams& p = qp.a;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int Hkv = p.kv.n_kv_heads;
     const int HR = Hkv * p.row_tiles;
     const int j = blockIdx.x;
@@ -458,31 +461,34 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
         } else if (warp == 1) {
             // ---------------- issuer of S ----------------
-            if (lane == 0) {
-                const uint32_t idesc = make_idesc_e4m3(TILE);
-                bool ok = true;
-                for (int si = 0; si < n_seg && ok; ++si, ++sg) {
-                    const Seg g = sh.segs[si];
-                    const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                    const int qb = sg & 1;
-                    const uint64_t qd = smem_desc_sw128_kmajor(q_addr + qb * Q_BYTES);
-                    for (int t = g.t_a; t < g.t_b; ++t, ++it) {
-                        const int sb = it % NS;
-                        const uint32_t d_tmem = tmem_base + (uint32_t)(sb * TILE);
-                        if (!wait(bar(BAR_GO + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
-                        tcgen05_fence_after();
-                        if (t != last_tile) {
-                            const int sl = rs % NK;
-                            const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * T_BYTES);
+            const uint32_t idesc = make_idesc_e4m3(TILE);
+            const bool leader = elect_one();
+            bool ok = true;
+            for (int si = 0; si < n_seg && ok; ++si, ++sg) {
+                const int last_tile = uniform((sh.segs[si].n / PAGE + PAGES - 1) / PAGES), t_a = uniform(sh.segs[si].t_a), t_b = uniform(sh.segs[si].t_b);
+                const int qb = sg & 1;
+                const uint64_t qd = smem_desc_sw128_kmajor(q_addr + qb * Q_BYTES);
+                for (int t = t_a; t < t_b; ++t, ++it) {
+                    const int sb = it % NS;
+                    const uint32_t d_tmem = tmem_base + (uint32_t)(sb * TILE);
+                    ok = __all_sync(0xffffffffu, wait(bar(BAR_GO + sb), (uint32_t)(it / NS) & 1u, abort_flag));
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    if (t != last_tile) {
+                        const int sl = rs % NK;
+                        const uint64_t kd = smem_desc_sw128_kmajor(ring_addr + sl * T_BYTES);
+                        if (leader) {
 #pragma unroll
                             for (int kk = 0; kk < 8; ++kk)                 // four steps of 32 dims for each term of Q
                                 umma_f8_ss(d_tmem, qd + (uint64_t)(((kk >> 2) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4), kd + (uint64_t)((kk & 3) * 2),
                                            idesc, kk != 0 ? 1u : 0u);
                             umma_commit(bar(BAR_S_FULL + sb));
                             umma_commit(bar(BAR_K_EMPTY + sl));
-                            ++rs;
-                        } else {
-                            const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
+                        }
+                        ++rs;
+                    } else {
+                        const uint64_t kd = smem_desc_sw128_kmajor(bt_addr);
+                        if (leader) {
 #pragma unroll
                             for (int kk = 0; kk < 16; ++kk)                // and for each term of K
                                 umma_f8_ss(d_tmem, qd + (uint64_t)((((kk >> 2) & 1) * (Q_BYTES / 2) + (kk & 3) * 32) >> 4),
@@ -490,39 +496,45 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             umma_commit(bar(BAR_S_FULL + sb));
                         }
                     }
-                    if (ok) umma_commit(bar(BAR_Q_EMPTY + qb));
+                    __syncwarp();
                 }
+                if (ok && leader) umma_commit(bar(BAR_Q_EMPTY + qb));
+                __syncwarp();
             }
         } else if (warp == 2) {
             // ---------------- issuer of O += P V, both groups ----------------
-            if (lane == 0) {
-                const uint32_t idesc = make_idesc_f16(HD, 1);
-                bool ok = true;
-                for (int si = 0; si < n_seg && ok; ++si) {
-                    const Seg g = sh.segs[si];
-                    const int last_tile = (g.n / PAGE + PAGES - 1) / PAGES;
-                    for (int t = g.t_a; t < g.t_b; ++t, ++it) {
-                        const int grp = it & 1;
-                        const int sb = it % NS;
-                        const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(sb * TILE);
-                        const uint32_t keep = t - g.t_a < 2 ? 0u : 1u;     // the group's first tile of the segment starts a new sum
-                        const bool blk = t == last_tile;
-                        const int vb = rs % NVH;
-                        if (!blk && !wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) { ok = false; break; }
-                        if (!wait(bar(BAR_P_READY + sb), (uint32_t)(it / NS) & 1u, abort_flag)) { ok = false; break; }
-                        tcgen05_fence_after();                             // (a bf16 tile was full before its S)
-                        // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
-                        const uint64_t vd = smem_desc_sw128(blk ? bt_addr + 2 * T_BYTES : vh_addr + vb * VH_BYTES, VH_HALF, 1024);
+            const uint32_t idesc = make_idesc_f16(HD, 1);
+            const bool leader = elect_one();
+            bool ok = true;
+            for (int si = 0; si < n_seg && ok; ++si) {
+                const int last_tile = uniform((sh.segs[si].n / PAGE + PAGES - 1) / PAGES), t_a = uniform(sh.segs[si].t_a), t_b = uniform(sh.segs[si].t_b);
+                for (int t = t_a; t < t_b; ++t, ++it) {
+                    const int grp = it & 1;
+                    const int sb = it % NS;
+                    const uint32_t o_tmem = tmem_base + (uint32_t)(O_COL + grp * HD), p_tmem = tmem_base + (uint32_t)(sb * TILE);
+                    const uint32_t keep = t - t_a < 2 ? 0u : 1u;           // the group's first tile of the segment starts a new sum
+                    const bool blk = t == last_tile;
+                    const int vb = rs % NVH;
+                    ok = (blk || wait(bar(BAR_VH_FULL + vb), (uint32_t)(rs / NVH) & 1u, abort_flag)) &&
+                         wait(bar(BAR_P_READY + sb), (uint32_t)(it / NS) & 1u, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tcgen05_fence_after();                                 // (a bf16 tile was full before its S)
+                    // 16 tokens per MMA: two groups of eight, 1 KB apart; the dim halves 8 KB apart
+                    const uint64_t vd = smem_desc_sw128(blk ? bt_addr + 2 * T_BYTES : vh_addr + vb * VH_BYTES, VH_HALF, 1024);
+                    if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < TILE / 16; ++kk)
                             umma_bf16_ts(o_tmem, p_tmem + (uint32_t)(kk * 8), vd + (uint64_t)((kk * 2048) >> 4), idesc, kk != 0 ? 1u : keep);
                         umma_commit(bar(BAR_S_FREE + sb));
                         umma_commit(bar(BAR_O_DONE + grp));
                         umma_commit(blk ? bar(BAR_BT_EMPTY) : bar(BAR_VH_EMPTY + vb));
-                        if (!blk) ++rs;
                     }
-                    if (ok) umma_commit(bar(BAR_SEG));
+                    __syncwarp();
+                    if (!blk) ++rs;
                 }
+                if (ok && leader) umma_commit(bar(BAR_SEG));
+                __syncwarp();
             }
         } else if (warp >= 12) {
             // ---------------- V to fp16, and the bf16 tile ----------------
