@@ -74,7 +74,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     uint32_t* whole = tmem_slot + 4;                                             // [rank][epilogue warp]: its sums are complete
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;   // (uniform, and known to be)
     const int rank = (int)blockIdx.x % a.split;
     const int tile = (int)blockIdx.x / a.split;
     const int m0 = (tile % a.m_tiles) * NT, n0 = (tile / a.m_tiles) * BN;
@@ -134,25 +134,29 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = make_idesc_e4m3(NT);
-            bool ok = true;
-            for (int i0 = 0, n = 0; i0 < ng && ok; i0 += C::H, ++n) {
-                const int b = n % C::NBUF;
-                if (!mbar_wait(tempty(b), ((uint32_t)(n / C::NBUF) & 1u) ^ 1u, abort_flag)) break;
-                for (int u = 0; u < C::H && i0 + u < ng; ++u) {
-                    const int i = i0 + u, s = i % C::STAGES;
-                    if (!mbar_wait(full(s), (uint32_t)(i / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
-                    tcgen05_fence_after();
-                    const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
-                    const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + W_BYTES);
+        const uint32_t idesc = make_idesc_e4m3(NT);
+        const bool leader = elect_one();
+        bool ok = true;
+        for (int i0 = 0, n = 0; i0 < ng && ok; i0 += C::H, ++n) {
+            const int b = n % C::NBUF;
+            ok = __all_sync(0xffffffffu, mbar_wait(tempty(b), ((uint32_t)(n / C::NBUF) & 1u) ^ 1u, abort_flag));
+            for (int u = 0; u < C::H && i0 + u < ng && ok; ++u) {
+                const int i = i0 + u, s = i % C::STAGES;
+                ok = __all_sync(0xffffffffu, mbar_wait(full(s), (uint32_t)(i / C::STAGES) & 1u, abort_flag));
+                if (!ok) break;
+                tcgen05_fence_after();
+                const uint64_t wd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE);
+                const uint64_t xd = smem_desc_sw128_kmajor(ring_addr + s * C::STAGE + W_BYTES);
+                if (leader) {
 #pragma unroll
                     for (int kk = 0; kk < GROUP / 32; ++kk)
                         umma_f8_ss(tmem_base + (uint32_t)((b * C::H + u) * NT), wd + (uint64_t)(kk * 2), xd + (uint64_t)(kk * 2), idesc, kk != 0 ? 1u : 0u);
                     umma_commit(empty(s));
                 }
-                umma_commit(tfull(b));
+                __syncwarp();
             }
+            if (ok && leader) umma_commit(tfull(b));
+            __syncwarp();
         }
     } else {
         const int et = tid - 64;                                   // 0 .. EPI_THREADS - 1
