@@ -125,11 +125,9 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
         }
         if (lane < 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(st + Smem<D>::LANE * 32 + lane * 4), "l"((lane ? p.kq.v_scale : p.kq.k_scale) + slab));
     };
-#pragma unroll 1
-    for (int j = 0; j < STAGES - 1; ++j) {
-        if (j < n_pages) bring(j);
-        cp_async_commit();
-    }
+    if (n_pages > 0) bring(0);
+    if (n_pages > 1) bring(1);
+    cp_async_commit();
 
     uint32_t present, decoded;
     attn::row_state_sets(p.row_state, b, p.k, lane, &present, &decoded);
@@ -181,12 +179,15 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
     for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};     // l: this lane's columns only, until the end
 
-    // Scores of 16 keys (two column tiles) in the log2 domain -> probabilities; raises the running maximum.
-    auto softmax16 = [&](float (&sc)[2][4]) {
+    // Scores (of two or four column tiles of 8 keys) in the log2 domain -> probabilities; raises the running maximum.
+    auto softmax = [&](auto& sc) {
+        constexpr int N = sizeof(sc) / sizeof(sc[0]);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const float mx = quad_max(fmaxf(fmaxf(sc[0][2 * u], sc[0][2 * u + 1]), fmaxf(sc[1][2 * u], sc[1][2 * u + 1])));
-            const float mn = fmaxf(m_run[u], mx);
+            float mx = fmaxf(sc[0][2 * u], sc[0][2 * u + 1]);
+#pragma unroll
+            for (int t = 1; t < N; ++t) mx = fmaxf(mx, fmaxf(sc[t][2 * u], sc[t][2 * u + 1]));
+            const float mn = fmaxf(m_run[u], quad_max(mx));
             if (__any_sync(0xffffffffu, mn > m_run[u])) {
                 const float corr = mn == -INFINITY ? 1.f : exp2f(m_run[u] - mn);
                 l_run[u] *= corr;
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
             const float base = (mn == -INFINITY ? 0.f : mn) - P_BIAS;
             float sum = 0.f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < N; ++t)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float pr = exp2f(sc[t][2 * u + e] - base);
@@ -211,56 +212,74 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
         }
     };
 
-    // ---- full pages ----
-    for (int j = 0; j < n_pages; ++j) {
+    // ---- full pages, two at a time: one page's chain of products and shuffles hides the other's ----
+    for (int j = 0; j < n_pages; j += 2) {
+        const bool two = j + 1 < n_pages;
+        cp_async_wait<0>();
         __syncwarp();
-        if (j + STAGES - 1 < n_pages) bring(j + STAGES - 1);
+        const unsigned char* st[2] = {smem + (warp * STAGES + j % STAGES) * Smem<D>::STAGE, smem + (warp * STAGES + (j + 1) % STAGES) * Smem<D>::STAGE};
+        // (the pair before has been used by every lane: its places take the pair after this one)
+        if (j + 2 < n_pages) bring(j + 2);
+        if (j + 3 < n_pages) bring(j + 3);
         cp_async_commit();
-        cp_async_wait<STAGES - 1>();
-        __syncwarp();
-        const unsigned char* st = smem + (warp * STAGES + j % STAGES) * Smem<D>::STAGE;
-        const float ks = *reinterpret_cast<const float*>(st + Smem<D>::LANE * 32), vs = *reinterpret_cast<const float*>(st + Smem<D>::LANE * 32 + 4);
-        float sc[2][4];
+        float sc[4][4], vs[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+        for (int x = 0; x < 2; ++x) {
+            if (x == 1 && !two) {
+                vs[1] = 0.f;
 #pragma unroll
-            for (int hc = 0; hc < HC; ++hc) {
-                const uint4 kw = *reinterpret_cast<const uint4*>(st + ((t * HC + hc) * 32 + lane) * 16);
-                const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mma_f16_16816(sc[t], qf[hc * 4 + i], codes_lo(w[i]), codes_hi(w[i]));
+                for (int e = 0; e < 4; ++e) sc[2][e] = sc[3][e] = -INFINITY;
+                break;
             }
+            const float ks = *reinterpret_cast<const float*>(st[x] + Smem<D>::LANE * 32);
+            vs[x] = *reinterpret_cast<const float*>(st[x] + Smem<D>::LANE * 32 + 4);
             const float f0 = f_row[0] * ks, f1 = f_row[1] * ks;
-            sc[t][0] *= f0; sc[t][1] *= f0; sc[t][2] *= f1; sc[t][3] *= f1;
-        }
-        softmax16(sc);
-        const uint32_t pa[4] = {pack_f16(sc[0][0], sc[0][1]), pack_f16(sc[0][2], sc[0][3]), pack_f16(sc[1][0], sc[1][1]), pack_f16(sc[1][2], sc[1][3])};
-        uint32_t v[4][VW];                     // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned char* src = st + 2 * HC * 512 + (e * 32 + lane) * (VW * 4);
-            if (D == 128) {
-                const uint4 w = *reinterpret_cast<const uint4*>(src);
-                v[e][0] = w.x; v[e][1] = w.y; v[e][VW - 2] = w.z; v[e][VW - 1] = w.w;
-            } else {
-                const uint2 w = *reinterpret_cast<const uint2*>(src);
-                v[e][0] = w.x; v[e][1] = w.y;
+            for (int t = 0; t < 2; ++t) {
+                float (&d)[4] = sc[2 * x + t];
+                d[0] = d[1] = d[2] = d[3] = 0.f;
+#pragma unroll
+                for (int hc = 0; hc < HC; ++hc) {
+                    const uint4 kw = *reinterpret_cast<const uint4*>(st[x] + ((t * HC + hc) * 32 + lane) * 16);
+                    const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma_f16_16816(d, qf[hc * 4 + i], codes_lo(w[i]), codes_hi(w[i]));
+                }
+                d[0] *= f0; d[1] *= f0; d[2] *= f1; d[3] *= f1;
             }
         }
+        softmax(sc);
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
+        for (int x = 0; x < 2; ++x) {
+            if (x == 1 && !two) break;
+            const uint32_t pa[4] = {pack_f16(sc[2 * x][0], sc[2 * x][1]), pack_f16(sc[2 * x][2], sc[2 * x][3]), pack_f16(sc[2 * x + 1][0], sc[2 * x + 1][1]),
+                                    pack_f16(sc[2 * x + 1][2], sc[2 * x + 1][3])};
+            uint32_t v[4][VW];                 // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {      // dims 4 w + 2 h, + 1: the codes of two tokens side by side
-                const uint32_t a = __byte_perm(v[0][w], v[1][w], h ? 0x7362 : 0x5140);
-                const uint32_t d = __byte_perm(v[2][w], v[3][w], h ? 0x7362 : 0x5140);
+            for (int e = 0; e < 4; ++e) {
+                const unsigned char* src = st[x] + 2 * HC * 512 + (e * 32 + lane) * (VW * 4);
+                if (D == 128) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(src);
+                    v[e][0] = w.x; v[e][1] = w.y; v[e][VW - 2] = w.z; v[e][VW - 1] = w.w;
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2*>(src);
+                    v[e][0] = w.x; v[e][1] = w.y;
+                }
+            }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float r[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_f16_16816(r, pa, e ? codes_hi(a) : codes_lo(a), e ? codes_hi(d) : codes_lo(d));
-                    const int i = w * 4 + h * 2 + e;
+            for (int w = 0; w < VW; ++w) {
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) o[i][z] = fmaf(r[z], vs, o[i][z]);
+                for (int h = 0; h < 2; ++h) {  // dims 4 w + 2 h, + 1: the codes of two tokens side by side
+                    const uint32_t a = __byte_perm(v[0][w], v[1][w], h ? 0x7362 : 0x5140);
+                    const uint32_t d = __byte_perm(v[2][w], v[3][w], h ? 0x7362 : 0x5140);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float r[4] = {0.f, 0.f, 0.f, 0.f};
+                        mma_f16_16816(r, pa, e ? codes_hi(a) : codes_lo(a), e ? codes_hi(d) : codes_lo(d));
+                        const int i = w * 4 + h * 2 + e;
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) o[i][z] = fmaf(r[z], vs[x], o[i][z]);
+                    }
                 }
             }
         }
@@ -302,7 +321,7 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
                 for (int z = 0; z < 4; ++z)
                     sc[t][z] = (see[z >> 1] >> (t * 8 + t4 * 2 + (z & 1))) & 1u ? sc[t][z] * p.scale_log2 : -INFINITY;
             }
-            softmax16(sc);
+            softmax(sc);
             // values: a NaN or an infinity must reach only the rows that see it, so such a group of rows goes element by element
             uint4 vv[4][D / 64];               // D / 8 bf16 of four tokens
             uint32_t worst = 0;

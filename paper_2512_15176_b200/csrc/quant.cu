@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __re
                                                        float* __restrict__ scales, int M, int K) {
     const int groups = (K + GROUP - 1) / GROUP;
     const size_t item = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);          // group index over all rows
-    const size_t row = item / groups;
-    const int g = (int)(item % groups);
+    const size_t row = item <= 0xffffffffu ? (uint32_t)item / (uint32_t)groups : item / (size_t)groups;   // (32 bits where they do)
+    const int g = (int)(item - row * (size_t)groups);
     const int col = g * GROUP + (threadIdx.x & 15) * 8;
     pdl_trigger();
     pdl_wait();
