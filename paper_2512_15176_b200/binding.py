@@ -248,6 +248,26 @@ class KVCacheQuant(KVCache):
                    z(max_seqs), z(max_seqs), torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device),
                    torch.full((1,), num_pages, dtype=torch.int32, device=device))
 
+    @classmethod
+    def from_layout(cls, layout, k_pool, v_pool, device="cuda"):
+        """The tokens of a bf16 cache (``workload.KVLayout`` and its pools) as an 8-bit one: full pages quantised, the
+        tokens behind each sequence's last full page as tail rows."""
+        kv = cls.empty(k_pool.shape[0], k_pool.shape[1], k_pool.shape[3], *layout.page_table.shape, device=device)
+        i32 = lambda a: torch.from_numpy(a.copy()).to(device=device, dtype=torch.int32)
+        for dst, src in ((kv.page_table, layout.page_table), (kv.seq_len, layout.seq_len), (kv.n_pages, layout.n_pages),
+                         (kv.free_stack, layout.free_stack), (kv.free_top, layout.free_top)):
+            dst.copy_(i32(src))
+        for pool, codes, scale, tail in ((k_pool, kv.k_pool, kv.k_scale, kv.k_tail), (v_pool, kv.v_pool, kv.v_scale, kv.v_tail)):
+            pool = pool.to(device)
+            amax = pool.abs().amax(dim=(2, 3)).float()
+            scale.copy_((amax / torch.full_like(amax, 448.0)).clamp_min(2.0 ** -126))
+            codes.copy_((pool.float() / scale[:, :, None, None]).to(torch.float8_e4m3fn))
+            for s, n in enumerate(layout.seq_len):
+                first, rest = int(n) // 16, int(n) % 16
+                if rest:
+                    tail[s, :, first % 3 * 16:first % 3 * 16 + rest] = pool[int(layout.page_table[s, first]), :, :rest]
+        return kv
+
     def layer(self):
         """Another layer's cache over the same page table, lengths and free stack, with pools of its own."""
         same = lambda t: torch.zeros_like(t)

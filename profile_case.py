@@ -41,6 +41,7 @@ def main():
     ap.add_argument("--peaked", action="store_true", help="trunc: rows with a language model's rank-frequency shape")
     ap.add_argument("--inter", type=int, default=12288)
     ap.add_argument("--separate", action="store_true", help="layer: every step as a call of its own instead of the fused calls")
+    ap.add_argument("--quant", action="store_true", help="attn, layer: weights, activations and the KV cache in 8 bits")
     ap.add_argument("--experts", type=int, default=0, help="layer: routed MLP with this many experts (0 = dense)")
     ap.add_argument("--top-k", type=int, default=8)
     ap.add_argument("--M", type=int, default=32)
@@ -87,22 +88,28 @@ def main():
         lengths = W.seq_lengths(cfg)
         lay = W.kv_layout(cfg, lengths)
         kp, vp = W.kv_pools(cfg, lay.num_pages, device=dev, sigma=1.0)
-        kv = L.KVCache.from_layout(lay, kp, vp, dev)
+        kv = (L.KVCacheQuant if a.quant else L.KVCache).from_layout(lay, kp, vp, dev)
         q, kb, vb = (t.to(dev) for t in W.block_qkv(cfg, sigma=1.0))
         out = torch.empty_like(q)
         seq_ids = torch.arange(a.B, dtype=torch.int32, device=dev)
         ws = torch.empty(L.deer_block_attn_workspace_bytes(a.B, a.k, a.Hq, a.Hkv, a.D, a.ctx), dtype=torch.uint8, device=dev)
         call = lambda: L.deer_block_attn(kv, seq_ids, q, kb, vb, out, cfg.mask, 0, 1.0 / math.sqrt(a.D), a.ctx, ws)
         nbytes = W.algorithmic_bytes(cfg, lengths)["attn"]
+        if a.quant:
+            ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(a.B, a.k, a.Hq, a.Hkv, a.D, a.ctx), dtype=torch.uint8, device=dev)
+            call = lambda: L.deer_block_attn_quant(kv, seq_ids, q, kb, vb, out, None, cfg.mask, 1.0 / math.sqrt(a.D), a.ctx, ws)
+            nbytes -= a.B * a.ctx * a.Hkv * a.D * 2                  # a byte per element of the cached tokens instead of two
         flops = float(W.algorithmic_flops(cfg, lengths)["attn"])
     elif a.what == "layer":
         # one verifier layer (Qwen3-8B shape by default) at M = B k rows, replayed from a CUDA graph
-        from paper_2512_15176_b200.runner import VerifierLayer
+        from paper_2512_15176_b200.runner import VerifierLayer, VerifierLayerQuant
+        if a.quant and a.experts:
+            ap.error("--quant has the dense MLP only")
         cfg = W.StepConfig("prof", a.B, a.Hq, a.Hkv, a.D, a.k, a.hid, 64, (a.ctx, a.ctx), seed=34, growth=a.k)
         lengths = W.seq_lengths(cfg)
         lay = W.kv_layout(cfg, lengths)
         kp, vp = W.kv_pools(cfg, lay.num_pages, device=dev, sigma=1.0)
-        kv = L.KVCache.from_layout(lay, kp, vp, dev)
+        kv = (L.KVCacheQuant if a.quant else L.KVCache).from_layout(lay, kp, vp, dev)
         hid, QD, KD = a.hid, a.Hq * a.D, a.Hkv * a.D
         mk = lambda n, shape, sig: W.normal(34, n, shape, sig, device=dev)
         w = {"ln1": mk("ln1", (hid,), 1.0), "ln2": mk("ln2", (hid,), 1.0), "q_norm": mk("qn", (a.D,), 1.0),
@@ -115,8 +122,11 @@ def main():
         else:
             w.update({"wgu": mk("wgu", (2 * a.inter, hid), hid ** -0.5), "wd": mk("wd", (hid, a.inter), a.inter ** -0.5)})
         x = mk("x", (cfg.M, hid), 1.0)
-        layer = VerifierLayer(cfg, kv, w, a.ctx + a.k, a.inter, fused=not a.separate,
-                              moe=(a.experts, a.top_k) if a.experts else None)
+        if a.quant:
+            layer = VerifierLayerQuant(cfg, kv, w, a.ctx + a.k, a.inter)
+        else:
+            layer = VerifierLayer(cfg, kv, w, a.ctx + a.k, a.inter, fused=not a.separate,
+                                  moe=(a.experts, a.top_k) if a.experts else None)
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())       # the weights and pools were drawn on the current stream
         with torch.cuda.stream(side):
@@ -136,6 +146,8 @@ def main():
             torch.cuda.synchronize()
             dense += int(torch.unique(e_ids).numel()) * 3 * a.inter * hid * 2      # the experts the rows really chose
         nbytes = dense + W.algorithmic_bytes(cfg, lengths)["attn"]
+        if a.quant:
+            nbytes -= dense // 2 + a.B * a.ctx * a.Hkv * a.D * 2
         flops = 2.0 * cfg.M * (dense / 2 if not a.experts else sum(t.numel() for n, t in w.items() if n in ("wqkv", "wo"))
                                + a.top_k * 3 * a.inter * hid)
     elif a.what == "trunc":

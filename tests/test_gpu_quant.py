@@ -498,3 +498,134 @@ def test_attention_of_one_long_sequence_and_few_rows():
         L.deer_block_attn_quant(kv, _ids(3), q.cuda(), kb.cuda(), vb.cuda(), out, None, 0, 1 / math.sqrt(D), msl, ws)
         assert L.deer_kv_status(kv) == 0
         check_attention(out, q, kb, vb, okv, [0, 1, 2], 0, 1 / math.sqrt(D), None, f"bound {msl}")
+
+
+@pytest.mark.parametrize("M,K,N,res", [(2, 4096, 16, True), (16, 2064, 256, False), (40, 4096, 256, True), (64, 1040, 4096, False), (100, 1024, 2000, True),
+                                       (200, 400, 2448, True), (257, 1168, 2400, False), (1000, 272, 2448, True), (700, 640, 4992, False)])
+def test_linear_quant_more_shapes(M, K, N, res):
+    """Both sides of the rules that choose a kernel: clusters of two to eight blocks for each row tile, pairs of blocks with
+    128 and with 256 weight rows, column groups that do not divide evenly, edges in every direction."""
+    test_linear_quant(M, K, N, res)
+
+
+def test_calls_on_two_streams_at_once():
+    """The same calls on two streams, each with outputs and a workspace of its own, give what one stream gives."""
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache([900, 333], 4, 128, 0, 420)
+    dev, _, _ = _linear_inputs(33, 1024, 512, seed=421)
+    jobs = []
+    for k, Hq in ((2, 16), (32, 32)):
+        q, kb, vb = (W.normal(420 + k, x, (2, k, h, 128), 1.0).cuda() for x, h in (("q", Hq), ("k", 4), ("v", 4)))
+        for msl in (900, 1 << 20):
+            ws = torch.empty(L.deer_block_attn_quant_workspace_bytes(2, k, Hq, 4, 128, msl), dtype=torch.uint8, device="cuda")
+            jobs.append((q, kb, vb, msl, ws))
+    act = W.normal(422, "x", (64, 1024), 1.0).cuda()
+
+    def run(mine):
+        outs = []
+        for q, kb, vb, msl, ws in mine:
+            outs.append(torch.empty_like(q))
+            L.deer_block_attn_quant(kv, _ids(2), q, kb, vb, outs[-1], None, 0, 0.088, msl, ws)
+        y = torch.empty(33, 512, dtype=torch.bfloat16, device="cuda")
+        L.deer_linear_quant(*dev, y)
+        codes, scales = torch.empty(64, 1024, dtype=F8, device="cuda"), torch.empty(64, 8, device="cuda")
+        L.deer_quantize(act, codes, scales)
+        return outs + [y, codes.view(torch.uint8), scales]
+
+    want = run(jobs)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    own = [jobs, [(q, kb, vb, msl, torch.empty_like(ws)) for q, kb, vb, msl, ws in jobs]]
+    got = [[], []]
+    for _ in range(3):
+        for i, st in enumerate(streams):
+            st.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(st):
+                got[i].append(run(own[i]))
+    torch.cuda.synchronize()
+    assert L.deer_kv_status(kv) == 0
+    for runs in got:
+        for outs in runs:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("k", [2, 32])
+def test_the_same_sequence_twice_and_padding_entries(k):
+    """Reading calls may name a sequence twice; an entry that names none (padding) is reported and its rows stay."""
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache([300, 45], 2, 128, 0, 423)
+    ids = [1, 0, 0, -1]
+    q, kb, vb = (W.normal(423, x, (4, k, h, 128), 1.0) for x, h in (("q", 8), ("k", 2), ("v", 2)))
+    for msl in (300, 1 << 20):
+        out = torch.full((4, k, 8, 128), 5.0, dtype=torch.bfloat16, device="cuda")
+        ws = torch.full((L.deer_block_attn_quant_workspace_bytes(4, k, 8, 2, 128, msl),), 255, dtype=torch.uint8, device="cuda")
+        L.deer_block_attn_quant(kv, torch.tensor(ids, dtype=torch.int32, device="cuda"), q.cuda(), kb.cuda(), vb.cuda(), out, None, 0, 0.088, msl, ws)
+        assert L.deer_kv_status(kv) == L.DEER_ERR_INVALID_ARG
+        check_attention(out[:3], q[:3], kb[:3], vb[:3], okv, ids[:3], 0, 0.088, None, f"bound {msl}")
+        assert (out[3] == 5).all()
+
+
+def test_two_recorded_graphs_share_a_workspace():
+    """Two graphs recorded with the same workspace, replayed in turn on one stream."""
+    from paper_2512_15176_b200 import binding as L
+    kv, okv = _cache([2000], 2, 128, 0, 424)
+    data = [[W.normal(424 + i, x, (1, 32, h, 128), 1.0) for x, h in (("q", 8), ("k", 2), ("v", 2))] for i in range(2)]
+    for msl in (2000, 1 << 20):
+        ws = torch.full((L.deer_block_attn_quant_workspace_bytes(1, 32, 8, 2, 128, msl),), 255, dtype=torch.uint8, device="cuda")
+        graphs, outs, keep = [], [], []
+        for q, kb, vb in data:
+            t = [x.cuda() for x in (q, kb, vb)]
+            out, ids = torch.zeros(1, 32, 8, 128, dtype=torch.bfloat16, device="cuda"), _ids(1)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+                L.deer_block_attn_quant(kv, ids, *t, out, None, 0, 0.088, msl, ws)
+            graphs.append(g)
+            outs.append(out)
+            keep.append((t, ids))
+        for _ in range(3):
+            for g in graphs:
+                g.replay()
+        torch.cuda.synchronize()
+        for (q, kb, vb), out in zip(data, outs):
+            check_attention(out, q, kb, vb, okv, [0], 0, 0.088, None, f"bound {msl}")
+
+
+def test_quantise_at_the_edges_of_the_quotient():
+    """Groups whose scales span fp32's range, and values at e4m3's rounding borders: the codes are those of the
+    correctly rounded quotient, bit for bit."""
+    from paper_2512_15176_b200 import binding as L
+    rng = np.random.default_rng(425)
+    M, K = 512, 1024
+    x = rng.standard_normal((M, K)).astype(np.float32)
+    x *= np.exp2(rng.integers(-126, 127, size=(M, K // 128)).astype(np.float32)).repeat(128, 1)
+    ties = np.array([1.0625, 1.1875, 17.0, 18.0, 19.0, 440.0, 2.0 ** -10, 3 * 2.0 ** -10, 464.0, 0.0], dtype=np.float32)
+    x[:, :128] = ties[rng.integers(0, len(ties), size=(M, 128))] * np.exp2(rng.integers(-20, 20, size=(M, 1)).astype(np.float32))
+    x[:, 0] = 448.0 * np.exp2(np.floor(rng.uniform(-20, 20, size=M))).astype(np.float32)
+    t = torch.from_numpy(x).to(torch.bfloat16)
+    codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, K // 128, device="cuda")
+    L.deer_quantize(t.cuda(), codes, scales)
+    want_c, want_s = O.quantise_rows(f64(t))
+    assert (scales.cpu().numpy() == want_s).all() and (f64(codes) == want_c).all()
+
+
+def test_a_bf16_cache_as_an_8_bit_one():
+    from paper_2512_15176_b200 import binding as L
+    cfg = W.StepConfig("conv", 3, 4, 2, 128, 8, 64, 64, (1, 90), seed=426, growth=8)
+    lengths = np.array([48, 1, 90])
+    lay = W.kv_layout(cfg, lengths)
+    kp, vp = W.kv_pools(cfg, lay.num_pages, sigma=1.0)
+    kv = L.KVCacheQuant.from_layout(lay, kp, vp)
+    z = lambda *s: np.zeros(s)
+    okv = O.QuantKV(z(lay.num_pages, 2, 16, 128), z(lay.num_pages, 2, 16, 128), z(lay.num_pages, 2), z(lay.num_pages, 2), z(3, 2, 48, 128),
+                    z(3, 2, 48, 128), lay.page_table, np.zeros(3, dtype=np.int64))
+    rows = [np.zeros((3, 90, 2, 128)) for _ in range(2)]
+    for x, pool in enumerate((kp, vp)):
+        for s, n in enumerate(lengths):
+            for tok in range(n):
+                rows[x][s, tok] = f64(pool[int(lay.page_table[s, tok // 16]), :, tok % 16])
+    okv.store([0, 1, 2], rows[0], rows[1], lengths)
+    okv.seq_len = lengths
+    got = O.QuantKV(f64(kv.k_pool), f64(kv.v_pool), kv.k_scale.cpu().numpy(), kv.v_scale.cpu().numpy(), f64(kv.k_tail), f64(kv.v_tail), lay.page_table, lengths)
+    for s in range(3):
+        assert all((a == b).all() for a, b in zip(got.gather(s), okv.gather(s)))
