@@ -77,8 +77,4 @@ bool umma_supported(int D, int G, float scale);
 int umma_row_tiles(int k, int G);
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len);
 int launch_umma(AttnParams p, cudaStream_t st);
-// The merge of cut units alone (head_dim 128): kv, B, k, Hq, G, row_tiles, ipt, nc, part_o, part_lse, unit_parts,
-// total_tiles and out of `p` say where the partial results are and where the output goes.
-int launch_umma_merge(const AttnParams& p, cudaStream_t st);
-
 }  // namespace attn

@@ -833,7 +833,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     see = columns_seen(p, g, i_blk, row_valid, present, decoded);
                 }
                 __nv_bfloat16* out_row = row_valid && whole ? p.out + ((size_t)(g.b * p.k + i_blk) * p.Hq + hq) * HD + grp * 64 : nullptr;
-                float* part_row = row_valid && !whole ? p.part_o + (slot * 128 + row) * HD + grp * 64 : nullptr;
+                // partial results [four dims][row][4]: the lanes of a warp, who have a row each, write side by side
+                float* part_row = row_valid && !whole ? p.part_o + slot * 128 * HD + (size_t)(grp * 16 * 128 + row) * 4 : nullptr;
 #pragma unroll 1
                 for (int cc = 0; cc < 4; ++cc) {
                     uint32_t a[16], b[16];
@@ -872,7 +873,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     }
                     if (part_row) {
 #pragma unroll
-                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(part_row + cc * 16 + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(part_row + (cc * 4 + c / 4) * 128 * 4) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
                     }
                 }
                 if (grp == 0) {
@@ -924,20 +925,76 @@ static int pick_blocks(int B, int Hkv, int row_tiles, int max_seq_len) {
     return (int)groups * row_tiles;
 }
 
+// Joins the pieces of the units that were cut: a thread per row and four dims, the pieces' sums and results eight at a time
+// (they come from L2, and a load of one at a time would cost its latency eighteen times over in a long context).  Blocks
+// small enough to sit beside the attention kernel's, waiting for it.  (C2 block: joined by a warp per row, two pieces at a
+// time, and stored by rows 27.0 us; like this 22.5.)
+__global__ void __launch_bounds__(128, 8) attn_quant_merge_kernel(const AttnParams p) {
+    const int unit = blockIdx.x >> 5, c4 = blockIdx.x & 31, r = threadIdx.x;
+    const int Hkv = p.kv.n_kv_heads, HR = Hkv * p.row_tiles, RT = p.row_tiles, ncg = p.nc / RT;
+    const int b = unit / HR, hr = unit % HR, kvh = hr / RT, rt = hr % RT;
+    const int rows = min(p.ipt, p.k - rt * p.ipt) * p.G;
+    pdl_trigger();
+    pdl_wait();                                                   // the attention kernel's partial results
+    const int2 parts = p.unit_parts[unit];
+    const long long T = *p.total_tiles;
+    // (a block that gave up on a wait may have left its units' entries unwritten: nothing outside the workspace is read then)
+    if (parts.x < 0 || parts.y < parts.x || parts.y >= ncg || r >= rows) return;
+    const int nj = parts.y - parts.x + 1;
+    const size_t slot0 = ((size_t)b * Hkv + kvh + parts.x) * RT + rt;      // the pieces of a unit sit RT slots apart
+    const float* lse = p.part_lse + slot0 * 128 + r;
+    const float* o = p.part_o + slot0 * 128 * HD + (size_t)(c4 * 128 + r) * 4;
+    const bool dense = T >= ncg;                                  // with fewer tiles than groups some shares are empty
+    float m = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < nj; j0 += 8) {
+        float l[8];
+        float4 v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int jj = j0 + e;
+            const bool on = jj < nj && (dense || attn::share_begin(T, parts.x + jj + 1, ncg) > attn::share_begin(T, parts.x + jj, ncg));
+            l[e] = on ? lse[(size_t)jj * RT * 128] : -INFINITY;
+            v[e] = on ? *reinterpret_cast<const float4*>(o + (size_t)jj * RT * 128 * HD) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float top = m;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, l[e]);
+        if (top == -INFINITY) continue;
+        const float corr = m == -INFINITY ? 0.f : exp2f(m - top);
+        sum *= corr;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] *= corr;
+        m = top;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (l[e] == -INFINITY) continue;
+            const float w = exp2f(l[e] - m);
+            sum += w;
+            acc[0] = fmaf(w, v[e].x, acc[0]);
+            acc[1] = fmaf(w, v[e].y, acc[1]);
+            acc[2] = fmaf(w, v[e].z, acc[2]);
+            acc[3] = fmaf(w, v[e].w, acc[3]);
+        }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    __nv_bfloat16* dst = p.out + ((size_t)(b * p.k + rt * p.ipt + r / p.G) * p.Hq + kvh * p.G + r % p.G) * HD + c4 * 4;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+}
+
 }  // namespace umma
 
 // More query rows than a warp's tile of 16 hold share the KV stream here; fewer leave the 128 lanes idle while the
 // warp-level kernel reads the same bytes with less latency.
-// This kernel takes about 19 us for any call, however short (its pipeline's start, the queries' split, two joins); the
+// This kernel takes about 15 us for any call, however short (its pipeline's start, the queries' split, two joins); the
 // warp-level one 6 to 8, and then the time for its pages, of which each costs 16 query rows as much as this one spends on
-// 128.  Measured in us, warp-level against this, 32 query and 8 KV heads, tokens: 32 rows x 1003 13.7 / 22.4, x 2048
-// 19.3 / 22.7, x 4096 28.1 / 27.5, x 8192 45.4 / 31.0; 8 sequences of 8 rows x 1003 20.2 / 27.4, x 4096 47.7 / 42.5;
-// and with more row tiles than fit the SMs at once (16 sequences, 4 KV heads, 32 rows x 200) 36.0 / 20.5.
+// 128.  Measured in us, warp-level against this, 32 query and 8 KV heads, tokens: 32 rows x 1003 13.3 / 18, x 2048
+// 18.9 / 18.3, x 4096 27.1 / 22.4, x 8192 45 / 27.0; 8 rows x 8192 21.9 / 21; 8 sequences of 8 rows x 1003 19.7 / 23,
+// x 4096 47.7 / 40.6; and with more row tiles than fit the SMs at once (16 sequences, 4 KV heads, 32 rows x 200) 36.0 / 17.
 bool use_umma(int B, int D, int k, int Hq, int Hkv, int max_seq_len, float scale) {
     const int G = Hq / Hkv;
     if (D != umma::HD || G > 128 || !(scale > 0.f) || k * G <= ROWS_SMALL) return false;
     const long long tiles = (long long)B * Hkv * ((k * G + ROWS_SMALL - 1) / ROWS_SMALL);    // the warp-level kernel's
-    return tiles > 2LL * deer_sm_count() || tiles * (max_seq_len / PAGE + 3) > 16384;
+    return tiles > 2LL * deer_sm_count() || tiles * (max_seq_len / PAGE + 3) > 9000;
 }
 
 size_t umma_workspace_bytes(int B, int k, int Hq, int Hkv, int max_seq_len) {
@@ -987,7 +1044,8 @@ int launch_umma(const Params& q, void* workspace, cudaStream_t st) {
     if (rc != DEER_OK) return rc;
     DEER_CUDA(cudaFuncSetAttribute(attn_quant_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
     DEER_CUDA(launch_pdl(attn_quant_umma_kernel, dim3((unsigned)p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_k, qp));
-    return attn::launch_umma_merge(p, st);
+    DEER_CUDA(launch_pdl(attn_quant_merge_kernel, dim3((unsigned)(units * 32)), dim3(128), 0, st, p));
+    return DEER_OK;
 }
 
 }  // namespace attnq

@@ -754,12 +754,6 @@ int launch_umma(AttnParams p, cudaStream_t st) {
     }
     DEER_CUDA(cudaFuncSetAttribute(block_attn_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
     DEER_CUDA(launch_pdl(block_attn_umma_kernel, dim3(p.nc), dim3(THREADS), (size_t)SMEM_BYTES, st, tm_q, tm_kb, tm_vb, tm_kp, tm_vp, p));
-    return launch_umma_merge(p, st);
-}
-
-int launch_umma_merge(const AttnParams& p, cudaStream_t st) {
-    using namespace umma;
-    const int HR = p.kv.n_kv_heads * p.row_tiles;
     if ((long long)p.B * HR * 4 >= 2 * deer_sm_count())
         DEER_CUDA(launch_pdl(attn_umma_merge_kernel<4>, dim3((unsigned)(p.B * HR * 4)), dim3(256), 0, st, p));
     else
