@@ -7,6 +7,8 @@
 
 namespace quant {
 
+using namespace sm100;
+
 // y = (x + residual) / rms * gamma per row.  A thread keeps its columns, CHUNKS pieces of 8, in registers between the two
 // phases -- the sum of squares over the row, the codes of the sixteen-lane groups -- so a row is read once; with one or two
 // pieces all loads, the gain's too, are on their way before the first value is used (more would not fit the registers).
@@ -35,27 +37,28 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
             gv[c] = piece(gamma, c);
         }
     }
-    float h[CHUNKS][8];
-    float ss = 0.f;
+    V8 h[CHUNKS];
+    uint64_t ss2 = 0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int col = (c * THREADS + tid) * 8;
-        float r[8];
         if (!EARLY) {
             xv[c] = piece(x_row, c);
             rv[c] = piece(r_row, c);
         }
-        unpack_bf16x8(xv[c], h[c]);
-        unpack_bf16x8(rv[c], r);
+        h[c] = unpack8(xv[c]);
+        if (residual) {
+            const V8 r = unpack8(rv[c]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (residual) h[c][j] += r[j];
-            ss += h[c][j] * h[c][j];
+            for (int j = 0; j < 4; ++j) h[c].p[j] = add2(h[c].p[j], r.p[j]);
         }
-        if (total && col < hid)
-            *reinterpret_cast<uint4*>(total + row * hid + col) =
-                make_uint4(pack_bf16(h[c][0], h[c][1]), pack_bf16(h[c][2], h[c][3]), pack_bf16(h[c][4], h[c][5]), pack_bf16(h[c][6], h[c][7]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ss2 = fma2(h[c].p[j], h[c].p[j], ss2);
+        if (total && col < hid) *reinterpret_cast<uint4*>(total + row * hid + col) = to_bf16(h[c]);
     }
+    float ss, ss_hi;
+    unpack_f32x2(ss2, ss, ss_hi);
+    ss += ss_hi;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if (lane == 0) part[warp] = ss;
@@ -64,21 +67,46 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) tot += part[w];
     const float inv = rsqrtf(tot / (float)hid + eps);
+    const uint64_t inv2 = pack_f32x2(inv, inv);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int col = (c * THREADS + tid) * 8;
         if (c * THREADS * 8 >= hid) break;
         if (!EARLY) gv[c] = piece(gamma, c);
-        float g[8];
-        unpack_bf16x8(gv[c], g);
+        const V8 g = unpack8(gv[c]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * inv * g[j];
-        const Divisor by(scale_of(max_of_16(col < hid ? amax8(h[c]) : 0u)));
+        for (int j = 0; j < 4; ++j) h[c].p[j] = mul2(mul2(h[c].p[j], inv2), g.p[j]);
+        const Divisor by(scale_of(max_mag_of<16>(col < hid ? max_mag(h[c]) : 0.f)));
         if (col < hid) {
             *reinterpret_cast<uint2*>(codes + row * hid + col) = codes8(h[c], by);
             if ((lane & 15) == 0) scales[row * groups + col / GROUP] = by.s;
         }
     }
+}
+
+// v / (1 + exp(-v)) * u for two values.  exp(-v) = 2^t with t = -v log2(e) to twice fp32's precision: what its rounding left
+// out (an fma has it exactly, and the part of log2(e) that fp32 does not hold is added) comes back as a factor 1 + rest * ln 2.
+// The quotient is that of v and an approximate reciprocal, corrected once by its remainder.  So the result is off by
+// about what its last two products round away, as close as the same formula in fp32 with a full exp and a division
+// (512 x 12288: 10.7 us with those, 8.1 like this).  exp(-v) stops at 2^100, where the quotient is 0 but for -inf, a NaN.
+__device__ __forceinline__ uint64_t gate2(uint64_t v, uint64_t neg_u) {
+    constexpr float L = 1.44269502f, L_LO = 1.92596299e-8f, LN2 = 0.693147182f;
+    const uint64_t t = mul2(v, pack_f32x2(-L, -L));
+    const uint64_t lack = fma2(v, pack_f32x2(L_LO, L_LO), fma2(v, pack_f32x2(L, L), t));     // t - (-v log2(e))
+    float t0, t1, e0, e1, d0, d1, r0, r1;
+    unpack_f32x2(t, t0, t1);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
+    uint64_t e = pack_f32x2(e0, e1);
+    e = fma2(mul2(e, pack_f32x2(-LN2, -LN2)), lack, e);
+    unpack_f32x2(e, e0, e1);
+    const uint64_t d = add2(pack_f32x2(fminf(e0, 1.26765060e30f), fminf(e1, 1.26765060e30f)), pack_f32x2(1.f, 1.f));
+    unpack_f32x2(d, d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d1));
+    const uint64_t neg_r = pack_f32x2(-r0, -r1);
+    const uint64_t neg_q = mul2(v, neg_r);
+    return mul2(fma2(fma2(neg_q, d, v), neg_r, neg_q), neg_u);
 }
 
 // Sixteen lanes per group of 128 columns, groups of all rows laid end to end.
@@ -93,25 +121,23 @@ __global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __re
     pdl_trigger();
     pdl_wait();
     const bool on = row < (size_t)M && col < K;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    V8 v = {};
     if (on) {
         const __nv_bfloat16* src = x + row * (size_t)(GATED ? 2 * (size_t)K : K) + col;
         const uint4 a = *reinterpret_cast<const uint4*>(src);
+        v = unpack8(a);
         if (GATED) {
-            const uint4 b = *reinterpret_cast<const uint4*>(src + K);
-            float u[8];
-            unpack_bf16x8(a, v);
-            unpack_bf16x8(b, u);
-            // (the quotient to 2 ulp: the gate's own exponential is no closer)
+            uint4 b = *reinterpret_cast<const uint4*>(src + K);
+            b.x ^= 0x80008000u;
+            b.y ^= 0x80008000u;
+            b.z ^= 0x80008000u;
+            b.w ^= 0x80008000u;
+            const V8 neg_u = unpack8(b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __fdividef(v[j], 1.f + __expf(-v[j])) * u[j];
-        } else {
-            unpack_bf16x8(a, v);
+            for (int j = 0; j < 4; ++j) v.p[j] = gate2(v.p[j], neg_u.p[j]);
         }
     }
-    const Divisor by(scale_of(max_of_16(amax8(v))));
+    const Divisor by(scale_of(max_mag_of<16>(max_mag(v))));
     if (on) {
         *reinterpret_cast<uint2*>(codes + row * K + col) = codes8(v, by);
         if ((threadIdx.x & 15) == 0) scales[row * groups + g] = by.s;
@@ -128,7 +154,7 @@ __global__ void __launch_bounds__(2 * D) kv_store_kernel(deer_kv_desc kv, deer_k
                                                          const __nv_bfloat16* __restrict__ k_rows, const __nv_bfloat16* __restrict__ v_rows,
                                                          const int32_t* __restrict__ keep, int k, int pages_per_block) {
     constexpr int PER_ROW = D / 16;                       // threads of a token
-    __shared__ uint32_t part[2][2 * D / 32];
+    __shared__ float part[2][2 * D / 32];
     const int tid = threadIdx.x;
     const bool is_v = tid >= D;
     const int t16 = (tid % D) / PER_ROW, col = (tid % PER_ROW) * 16;
@@ -165,25 +191,22 @@ __global__ void __launch_bounds__(2 * D) kv_store_kernel(deer_kv_desc kv, deer_k
     };
     if (first < last) bring(first);
     for (int page = first; page < last; ++page) {
-        float v[2][8];
-        unpack_bf16x8(next[0], v[0]);
-        unpack_bf16x8(next[1], v[1]);
+        const V8 v0 = unpack8(next[0]), v1 = unpack8(next[1]);
         const int pg = pg_next;
         if (page + 1 < last) bring(page + 1);
-        uint32_t m = max(amax8(v[0]), amax8(v[1]));
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if ((tid & 31) == 0) part[page & 1][tid >> 5] = m;
+        const float mine = max_mag_of<32>(max_mag(v1, max_mag(v0)));
+        if ((tid & 31) == 0) part[page & 1][tid >> 5] = mine;
         __syncthreads();                                  // (the first time also: the tail rows are in registers)
+        float m = 0.f;
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w) m = max(m, part[page & 1][(is_v ? D / 32 : 0) + w]);
+        for (int w = 0; w < D / 32; w += 2) m = max_mag(m, part[page & 1][(is_v ? D / 32 : 0) + w], part[page & 1][(is_v ? D / 32 : 0) + w + 1]);
         const Divisor by(scale_of(m));
         if (pg < 0 || pg >= kv.num_pages) {
             if (tid == 0) deer_report(kv.status, DEER_ERR_BAD_PAGE);
             continue;
         }
         const size_t slab = (size_t)pg * Hkv + h;
-        const uint2 lo = codes8(v[0], by), hi = codes8(v[1], by);
+        const uint2 lo = codes8(v0, by), hi = codes8(v1, by);
         *reinterpret_cast<uint4*>(pool + (slab * DEER_PAGE_SIZE + t16) * D + col) = make_uint4(lo.x, lo.y, hi.x, hi.y);
         if (tid % D == 0) (is_v ? q.v_scale : q.k_scale)[slab] = by.s;
     }
