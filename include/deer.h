@@ -466,7 +466,7 @@ int deer_moe_mlp(const void* x, const void* w_router, const void* w_gate_up, con
  *   (gated = 1).  K a multiple of 16.
  * deer_linear_quant: y[m][n] = sum_c x[m][c] w[n][c] (+ residual[m][n]) of the values that codes and scales stand for.
  *   x e4m3 [M][K], x_scale f32 [M][ceil(K / 128)]; w e4m3 [N][K], w_scale f32 [ceil(N / 128)][ceil(K / 128)];
- *   residual, y bf16 [M][N] (residual may be NULL or y itself).  K and N multiples of 16, at least 16.
+ *   residual, y bf16 [M][N] (residual may be NULL or y itself).  K and N multiples of 16, at least 16; M, K, N <= 2^30.
  *   Products and the sums over 128 columns come from the tensor cores' fp32 accumulator; the scaled sums over the
  *   column groups are fp32.  No workspace.
  * ---------------------------------------------------------------------- */

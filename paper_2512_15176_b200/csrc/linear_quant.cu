@@ -530,6 +530,7 @@ extern "C" int deer_linear_quant(const void* x, const float* x_scale, const void
                        deer_aligned4(w_scale),
                    DEER_ERR_INVALID_ARG, "deer_linear_quant: pointers must be 16-byte aligned (scales: 4)");
     DEER_CHECK_ARG(M >= 0, DEER_ERR_INVALID_ARG, "deer_linear_quant: M must be >= 0");
+    DEER_CHECK_ARG(M <= 1 << 30 && N <= 1 << 30 && K <= 1 << 30, DEER_ERR_UNSUPPORTED, "deer_linear_quant: M, K and N must be at most 2^30");
     DEER_CHECK_ARG(K >= 16 && K % 16 == 0 && N >= 16 && N % 16 == 0, DEER_ERR_UNSUPPORTED,
                    "deer_linear_quant: K and N must be multiples of 16, at least 16");
     if (M == 0) return DEER_OK;

@@ -629,3 +629,32 @@ def test_a_bf16_cache_as_an_8_bit_one():
     got = O.QuantKV(f64(kv.k_pool), f64(kv.v_pool), kv.k_scale.cpu().numpy(), kv.v_scale.cpu().numpy(), f64(kv.k_tail), f64(kv.v_tail), lay.page_table, lengths)
     for s in range(3):
         assert all((a == b).all() for a, b in zip(got.gather(s), okv.gather(s)))
+
+
+def test_rows_past_four_gigabytes():
+    """Operands whose last rows lie behind 2^32 bytes and 2^31 elements: those rows against the oracle."""
+    from paper_2512_15176_b200 import binding as L
+    M, K = 140000, 16384
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    tail = W.normal(430, "x", (2, K), 1.0)
+    x[-2:] = tail.cuda()
+    codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, K // 128, device="cuda")
+    L.deer_quantize(x, codes, scales)
+    want_c, want_s = O.quantise_rows(f64(tail))
+    assert (f64(codes[-2:]) == want_c).all() and (scales[-2:].cpu().numpy() == want_s).all() and (scales[:-2] == 2.0 ** -126).all()
+    g = W.normal(430, "g", (K,), 1.0)
+    L.deer_rmsnorm_quant(x, g.cuda(), codes, scales, 1e-6)
+    check_codes(codes[-2:], scales[-2:], O.rmsnorm(f64(tail), f64(g), 1e-6), 2e-6, "far rows")
+    N = 16384
+    xs, w64 = torch.ones(M, 1, device="cuda"), W.normal(431, "w", (N, 16), 1.0, dtype=torch.float32)
+    wc, ws = O.quantise_weight(f64(w64))
+    xr = torch.zeros(M, 16, device="cuda")
+    xr[-2:] = torch.arange(32, device="cuda").view(2, 16) % 9 - 4.0
+    xr[0] = 1.0
+    y = x[:, :N]
+    L.deer_linear_quant(xr.to(F8), xs, torch.from_numpy(wc).float().to(F8).cuda(), torch.from_numpy(ws).cuda(), y)
+    w64 = O.dequantise_weight(wc, ws)
+    for r in (0, M - 2, M - 1):
+        want = w64 @ f64(xr[r])
+        assert (np.abs(f64(y[r]) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -16 * (np.abs(w64) @ np.abs(f64(xr[r])))).all()
+    assert not y[1:-2].any()

@@ -114,3 +114,10 @@ def test_row_wise_and_linear_refusals(L):
     for K, N in ((100, 128), (128, 100), (0, 128), (128, 8)):
         assert lib.deer_linear_quant(f, f, f, f, None, f, 4, K, N, None) == L.DEER_ERR_UNSUPPORTED
     assert lib.deer_linear_quant(f, f, f, f, None, f, 0, 128, 128, None) == L.DEER_OK
+
+
+def test_linear_refuses_sizes_whose_indices_would_not_fit(L):
+    lib, f = L.lib(), 0x1000
+    big = (1 << 30) + 16
+    for M, K, N in ((big, 128, 128), (4, big, 128), (4, 128, big)):
+        assert lib.deer_linear_quant(f, f, f, f, None, f, M, K, N, None) == L.DEER_ERR_UNSUPPORTED
