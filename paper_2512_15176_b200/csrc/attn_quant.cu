@@ -13,6 +13,10 @@
 // 11 bits down to 2^-26 of the row's maximum.  The warps of a block take pages in turn with running maxima of their
 // own, and meet in shared memory at the end.  A context is cut into chunks over thread blocks; up to eight of them form
 // a cluster and meet in its shared memory, and where a context has more a second kernel joins the clusters' parts.
+//
+// What bounds it: latencies in short contexts (one token, 32 query and 8 KV heads, over 1003: 7.8 us, two pages per warp,
+// most of it the chain length -> page number -> page -> products -> meeting in the cluster), the instructions of a page
+// (about 400 a warp, and their latencies) in long ones: 16 x 4096 tokens 43.7 us = 3.1 TB/s.
 
 #include <cuda_fp16.h>
 

@@ -23,6 +23,11 @@
 // its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 loader of Q and K, 1 issuer of S and 3 its gate, 2 issuer
 // of O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V and the bf16 tile.
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
+//
+// What bounds it: not a unit but the way of a tile through the roles (16 ragged sequences of 2048 to 16384 tokens, 32 query
+// and 4 KV heads, 32 rows: 115 us, 0.95 us a tile and block, where its MMAs take 0.45, its exponentials 0.27 and its bytes
+// 0.2).  Taking away half of any one role's work changes the time by 5 % at most; the four score buffers that tensor memory
+// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22.5 us.
 
 #include <cuda_fp16.h>
 

