@@ -165,10 +165,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# (a call's tensors are on the device, so torch has initialised it by now)
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         # the handle itself: torch.cuda.current_stream() builds a Stream object first, which takes longer than a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        return _raw_stream(_current_device()) or None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream or None
     return stream or None
