@@ -25,9 +25,10 @@
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 //
 // What bounds it: not a unit but the way of a tile through the roles (16 ragged sequences of 2048 to 16384 tokens, 32 query
-// and 4 KV heads, 32 rows: 115 us, 0.95 us a tile and block, where its MMAs take 0.45, its exponentials 0.27 and its bytes
+// and 4 KV heads, 32 rows: 112 us, 0.9 us a tile and block, where its MMAs take 0.45, its exponentials 0.27 and its bytes
 // 0.2).  Taking away half of any one role's work changes the time by 5 % at most; the four score buffers that tensor memory
-// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22.5 us.
+// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22 us, of
+// which a block spends 27000 cycles: 9000 until the queries are there, 4500 on their terms, 7500 on four tiles, 6000 on joining.
 
 #include <cuda_fp16.h>
 
@@ -60,7 +61,7 @@ constexpr int THREADS = 512;
 constexpr int TMEM_COLS = 512;                 // S, and P in its place (columns 0..31 of it): [b * 64, +64) b < 4;  O [256 + g * 128, +128)
 constexpr int NS = 4;                          // a tile's buffer is free once O has taken P from it
 constexpr int O_COL = 256;
-constexpr int HEAD = 8;                         // what a unit costs beside its tiles, in tiles
+constexpr int HEAD = 12;                        // what a unit costs beside its tiles, in tiles
 constexpr float BIAS = 11.f;                   // the reference weight is 2^11: 2^4 below the raise, 2^35 above fp16's last bit
 
 // mbarrier indices
@@ -320,14 +321,22 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         sh.bt_bad[0] = sh.bt_bad[1] = 0;
         mbar_init_fence();
         prefetch_tensormap(&tm_q);
+        prefetch_tensormap(&tm_k);
     }
     pdl_trigger();
     pdl_wait();
 
     // ---- this block's share of the flattened tile list ----
     long long T = 0;
+    int my_n = -1, my_s = -1, my_tiles = 0;                    // of sequence `lane`: the list of segments asks for them again
     for (int b = lane; b < p.B; b += 32) {
-        const int tiles = seq_tiles(p, b, nullptr, nullptr);
+        int n, s;
+        const int tiles = seq_tiles(p, b, &n, &s);
+        if (b == lane) {
+            my_n = n;
+            my_s = s;
+            my_tiles = tiles;
+        }
         T += tiles;
         // a sequence that cannot be used has no tiles, so no block will write its units' merge entries: do it here
         if (tiles == 0 && j == 0 && warp == 0)
@@ -357,7 +366,12 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if (warp == 0) {
             long long next;
             const int ns = attn::build_segments(p, Hkv, rt, cursor, share_hi, sh.segs, &next, lane,
-                                                [&](int b, int* n, int* s) { return seq_tiles(p, b, n, s); });
+                                                [&](int b, int* n, int* s) {
+                                                    if (b != lane) return seq_tiles(p, b, n, s);
+                                                    if (n) *n = my_n;
+                                                    if (s) *s = my_s;
+                                                    return my_tiles;
+                                                });
             if (lane == 0) {                                               // from places to tiles
                 int kept = 0;
                 for (int x = 0; x < ns; ++x) {
