@@ -236,6 +236,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         cluster_wait();
         if (warp >= 2) {
             const uint32_t place_addr = smem_u32(place);
+            const int own_log = __ffs(own_rows) - 1;               // (a power of two)
 #pragma unroll
             for (int j = 0; j < NT; j += 4) {                      // rows j .. j + 3 belong to one owner, or two each to two
                 if (m0 + j >= a.M) break;
@@ -243,8 +244,8 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
                 unpack_f32x2(acc[j / 2], v[0], v[1]);
                 unpack_f32x2(acc[j / 2 + 1], v[2], v[3]);
                 if (own_rows >= 4) {
-                    const uint32_t at = place_addr + (uint32_t)(((rank * own_rows + j % own_rows) * BN + lane_row * 4) * 4);
-                    st_cluster_f32x4(map_to_cta(at, (uint32_t)(j / own_rows)), v[0], v[1], v[2], v[3]);
+                    const uint32_t at = place_addr + (uint32_t)(((rank * own_rows + (j & (own_rows - 1))) * BN + lane_row * 4) * 4);
+                    st_cluster_f32x4(map_to_cta(at, (uint32_t)(j >> own_log)), v[0], v[1], v[2], v[3]);
                 } else {
                     const uint32_t at = place_addr + (uint32_t)((rank * 2 * BN + lane_row * 2) * 4);
                     st_cluster_f32x2(map_to_cta(at, (uint32_t)(j / 2)), v[0], v[1]);
@@ -259,6 +260,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         if (warp >= 2 && !*abort_flag) {
             bool ok = true;
             for (int r = 0; r < a.split; ++r) ok = ok && whole[r * C::EPI_WARPS + (warp & 3)] != 0u;
+#pragma unroll 1                                                   // (code that runs once waits for its fetching: 64 x 1024 x 1024 9.2 us unrolled, 8.3)
             for (int j = 0; j < own_rows && own0 + j < a.M && ok; j += 4) {
                 if (j > 0) fetch_residual(own0 + j);
                 float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -568,14 +570,16 @@ extern "C" int deer_linear_quant(const void* x, const float* x_scale, const void
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M <= 16) return launch<16>(a, x, w, st);
     if (M <= 32) return launch<32>(a, x, w, st);
-    // Above 32 rows: the first kernel while its tiles leave room for four blocks each at the least, or there are not more
-    // rows than one of them has (us, first kernel / pairs: 128 x 4096 x 4096 13.2 / 14.3, 128 x 12288 x 4096 23.9 / 33, 128 x 4096 x 8192 21.7 / 14.5,
-    // 256 x 4096 x 4096 20.2 / 14.5, 64 x 4096 x 24576 34.5 / 41.4).
-    const long long few = (long long)((M + 63) / 64) * ((N + BN - 1) / BN);
-    if (M <= 64 || few <= deer_sm_count() / 2) return launch<64>(a, x, w, st);
     // Pairs: the tiles of the product are done in rounds of one per pair of SMs; a round of 128 weight rows takes 0.57 of
     // one of 256 (512 rows, 12288 x 4096, one round: 34.0 / 58.4 us; 4096 x 24576, six rounds or three: 80.4 / 75.3).
     const long long pairs = deer_sm_count() / 2, m_tiles = (M + 255) / 256;
     const long long wide = (m_tiles * ((N + 255) / 256) + pairs - 1) / pairs, narrow = (m_tiles * ((N + 127) / 128) + pairs - 1) / pairs;
+    // The first kernel above 32 rows: where its tiles leave room for four blocks each at the least, or there are not more rows
+    // than one of them has (us, first kernel / pairs: 128 x 4096 x 4096 13.2 / 14.3, 128 x 12288 x 4096 23.9 / 33, 128 x 4096 x 8192
+    // 21.7 / 14.5, 256 x 4096 x 4096 20.2 / 14.5, 64 x 4096 x 24576 34.5 / 41.4); but not where the product is so shallow that one round
+    // of pairs is over before a cluster has met (64 x 256 x 1024 8.4 / 4.8, 64 x 1536 x 4096 9.8 / 7.5, 64 x 2048 x 256 7.2 / 8.1).
+    const bool room = M <= 64 || (long long)((M + 63) / 64) * ((N + BN - 1) / BN) <= pairs;
+    const bool shallow = a.groups <= 12 && narrow == 1;
+    if (room && !shallow) return launch<64>(a, x, w, st);
     return narrow * 57 < wide * 100 ? launch_pair<128>(a, x, w, st) : launch_pair<256>(a, x, w, st);
 }

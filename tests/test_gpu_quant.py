@@ -658,3 +658,10 @@ def test_rows_past_four_gigabytes():
         want = w64 @ f64(xr[r])
         assert (np.abs(f64(y[r]) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -16 * (np.abs(w64) @ np.abs(f64(xr[r])))).all()
     assert not y[1:-2].any()
+
+
+@pytest.mark.parametrize("M,K,N,res", [(64, 1680, 384, True), (70, 1680, 272, False), (128, 2048, 1040, True), (40, 144, 16, True), (48, 1536, 4112, False),
+                                       (64, 1024, 9600, True)])
+def test_linear_quant_shallow_and_deep(M, K, N, res):
+    """More than 32 rows, few tiles: deep products in clusters, shallow ones in one round of pairs."""
+    test_linear_quant(M, K, N, res)
