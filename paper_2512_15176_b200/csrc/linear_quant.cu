@@ -10,7 +10,7 @@
 //
 // What bounds it.  Few rows: the weight bytes (one row, 4096 x 4096, 6.8 us, 2.6 of them HBM's; 32 rows, 12288 x 4096,
 // 13.3 us = 3.9 TB/s, 7.8 HBM's): the loads run at HBM's rate, the rest is the first tile's latency (1.5 us), the cluster's
-// meeting (2 us) and a launch.  Many rows (512 x 4096 x 24576, 56 us = 1.84 PFLOP/s, twice the bf16 rate would take 31):
+// meeting (2 us) and a launch.  Many rows (512 x 4096 x 24576, 55 us = 1.86 PFLOP/s, twice the bf16 rate would take 31):
 // the way of an accumulator from the MMAs through the epilogue and back, which tensor memory can hold only 512 columns of.
 //
 // Few output columns do not fill the SMs, so a cluster of `split` blocks shares an output tile, each with a range of
