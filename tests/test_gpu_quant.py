@@ -665,3 +665,26 @@ def test_rows_past_four_gigabytes():
 def test_linear_quant_shallow_and_deep(M, K, N, res):
     """More than 32 rows, few tiles: deep products in clusters, shallow ones in one round of pairs."""
     test_linear_quant(M, K, N, res)
+
+
+def test_rmsnorm_quant_of_extreme_rows():
+    """Rows of zeros, of tiny and of huge values next to ordinary ones, and a gain over thirty octaves: codes and scales of
+    each row as the oracle has them; a NaN or an infinity spoils its own row and no other."""
+    from paper_2512_15176_b200 import binding as L
+    M, K = 9, 1040
+    x, g = W.normal(440, "x", (M, K), 1.0), W.normal(440, "g", (K,), 1.0)
+    g *= torch.exp2((torch.arange(K) % 31 - 15).float()).to(torch.bfloat16)
+    x[0] = 0.0
+    x[1] *= 2.0 ** -60
+    x[2] *= 2.0 ** 50
+    x[3, 5] = float("nan")
+    x[4, 700] = float("inf")
+    x[5, :128] = 0.0
+    x[6] = 2.0 ** -100
+    codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, 9, device="cuda")
+    L.deer_rmsnorm_quant(x.cuda(), g.cuda(), codes, scales, 1e-6)
+    torch.cuda.synchronize()
+    fine = [0, 1, 2, 5, 6, 7, 8]
+    check_codes(codes[fine], scales[fine], O.rmsnorm(f64(x[fine]), f64(g), 1e-6), 2e-6, "extreme rows")
+    v = codes.float() * scales.repeat_interleave(128, 1)[:, :K]
+    assert v[3].isnan().all() and not v[4].isfinite().all() and v[fine].isfinite().all()
