@@ -20,15 +20,16 @@
 // the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
 //
 // Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
-// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 loader of Q and K, 1 issuer of S and 3 its gate, 2 issuer
-// of O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V and the bf16 tile.
+// its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 loader of Q and K, 1 issuer of
+// S and 3 its gate, 2 issuer of O, 4..7 and 8..11 softmax (and, as a segment begins, its queries' terms), 12..15 V and the
+// bf16 tile.
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 //
 // What bounds it: not a unit but the way of a tile through the roles (16 ragged sequences of 2048 to 16384 tokens, 32 query
 // and 4 KV heads, 32 rows: 112 us, 0.9 us a tile and block, where its MMAs take 0.45, its exponentials 0.27 and its bytes
 // 0.2).  Taking away half of any one role's work changes the time by 5 % at most; the four score buffers that tensor memory
-// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22 us, of
-// which a block spends 27000 cycles: 9000 until the queries are there, 4500 on their terms, 7500 on four tiles, 6000 on joining.
+// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22 us, 27000 cycles of them in a block: 9000
+// until the queries are there, 4500 on their terms, 7500 on four tiles, 6000 on joining.
 
 #include <cuda_fp16.h>
 
