@@ -86,29 +86,47 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
     }
 }
 
-// v / (1 + exp(-v)) * u for two values.  exp(-v) = 2^t with t = -v log2(e) to twice fp32's precision: what its rounding left
-// out (an fma has it exactly, and the part of log2(e) that fp32 does not hold is added) comes back as a factor 1 + rest * ln 2.
-// The quotient is that of v and an approximate reciprocal, corrected once by its remainder.  So the result is off by
-// about what its last two products round away, as close as the same formula in fp32 with a full exp and a division
-// (512 x 12288: 10.7 us with those, 8.1 like this).  exp(-v) stops at 2^100, where the quotient is 0 but for -inf, a NaN.
-__device__ __forceinline__ uint64_t gate2(uint64_t v, uint64_t neg_u) {
-    constexpr float L = 1.44269502f, L_LO = 1.92596299e-8f, LN2 = 0.693147182f;
-    const uint64_t t = mul2(v, pack_f32x2(-L, -L));
-    const uint64_t lack = fma2(v, pack_f32x2(L_LO, L_LO), fma2(v, pack_f32x2(L, L), t));     // t - (-v log2(e))
-    float t0, t1, e0, e1, d0, d1, r0, r1;
+// v / (1 + exp(-v)) * u for two values.
+//
+// 2^t with t = a multiple of log2(e) to twice fp32's precision: what the product's rounding left out (an fma has it exactly, and
+// the part of log2(e) that fp32 does not hold is added) comes back as a factor 1 + rest * ln 2.
+__device__ __forceinline__ uint64_t exp_of(uint64_t x, float l, float l_lo) {
+    constexpr float LN2 = 0.693147182f;
+    const uint64_t t = mul2(x, pack_f32x2(-l, -l));
+    const uint64_t lack = fma2(x, pack_f32x2(l_lo, l_lo), fma2(x, pack_f32x2(l, l), t));     // t - (-x log2(e))
+    float t0, t1, e0, e1;
     unpack_f32x2(t, t0, t1);
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
-    uint64_t e = pack_f32x2(e0, e1);
-    e = fma2(mul2(e, pack_f32x2(-LN2, -LN2)), lack, e);
-    unpack_f32x2(e, e0, e1);
-    const uint64_t d = add2(pack_f32x2(fminf(e0, 1.26765060e30f), fminf(e1, 1.26765060e30f)), pack_f32x2(1.f, 1.f));
+    const uint64_t e = pack_f32x2(e0, e1);
+    return fma2(mul2(e, pack_f32x2(-LN2, -LN2)), lack, e);
+}
+// -n / d by an approximate reciprocal, corrected once by its remainder.
+__device__ __forceinline__ uint64_t neg_quotient(uint64_t n, uint64_t d) {
+    float d0, d1, r0, r1;
     unpack_f32x2(d, d0, d1);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d0));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d1));
-    const uint64_t neg_r = pack_f32x2(-r0, -r1);
-    const uint64_t neg_q = mul2(v, neg_r);
-    return mul2(fma2(fma2(neg_q, d, v), neg_r, neg_q), neg_u);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(-d0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(-d1));
+    const uint64_t neg_r = pack_f32x2(r0, r1), neg_q = mul2(n, neg_r);
+    return fma2(fma2(neg_q, d, n), neg_r, neg_q);
+}
+// Gates below GATE_NEAR in magnitude: exp(-v) is at most 2^93, and nothing on the way leaves fp32's normal range.  Off by about
+// what the last two products round away, as close as the same formula in fp32 with a full exp and a division (512 x 12288:
+// 10.7 us with those, 8.2 like this, 9.0 with the form below for all).
+constexpr float GATE_NEAR = 64.f;
+__device__ __forceinline__ uint64_t gate_near2(uint64_t v, uint64_t neg_u) {
+    const uint64_t e = exp_of(v, 1.44269502f, 1.92596299e-8f);
+    return mul2(neg_quotient(v, add2(e, pack_f32x2(1.f, 1.f))), neg_u);
+}
+// Gates of any size.  With w = exp(-|v|) the quotient is v / (1 + w) or, below zero, v w / (1 + w) -- the larger of v and v w over
+// 1 + w -- so nothing overflows; and w is multiplied in as two factors exp(-|v| / 2), so that the quotient leaves fp32 gradually,
+// as a number does, and not where w would.  |v| stops at 400, where the factors are 0, so that t stays finite.  -inf gives a NaN.
+__device__ __forceinline__ uint64_t gate_any2(uint64_t v, uint64_t neg_u) {
+    float v0, v1, n0, n1;
+    unpack_f32x2(v, v0, v1);
+    const uint64_t h = exp_of(pack_f32x2(fminf(fabsf(v0), 400.f), fminf(fabsf(v1), 400.f)), 0.72134751f, 9.62981496e-9f);
+    unpack_f32x2(mul2(mul2(v, h), h), n0, n1);
+    return mul2(neg_quotient(pack_f32x2(fmaxf(v0, n0), fmaxf(v1, n1)), fma2(h, h, pack_f32x2(1.f, 1.f))), neg_u);
 }
 
 // Sixteen lanes per group of 128 columns, groups of all rows laid end to end.
@@ -135,8 +153,13 @@ __global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __re
             b.z ^= 0x80008000u;
             b.w ^= 0x80008000u;
             const V8 neg_u = unpack8(b);
+            if (max_mag(v) < GATE_NEAR) {                  // (not for a NaN)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v.p[j] = gate2(v.p[j], neg_u.p[j]);
+                for (int j = 0; j < 4; ++j) v.p[j] = gate_near2(v.p[j], neg_u.p[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v.p[j] = gate_any2(v.p[j], neg_u.p[j]);
+            }
         }
     }
     const Divisor by(scale_of(max_mag_of<16>(max_mag(v))));

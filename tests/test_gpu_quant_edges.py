@@ -1,0 +1,81 @@
+"""The 8-bit calls at the ends of their ranges, against the oracle in 64 bits (tolerances as in test_gpu_quant)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import deer_oracle as O
+from paper_2512_15176_b200 import workload as W
+from tests.test_gpu_quant import F8, _cache, _ids, check_attention, f64
+
+pytestmark = pytest.mark.gpu
+
+
+GATES = [s * 2.0 ** e for s in (1.0, -1.0) for e in range(-133, 128)] + \
+    [-60.0, -69.0, -70.0, -75.0, -80.0, -87.0, -87.5, -88.0, -88.5, -89.0, -95.0, -100.0, -103.0, -104.0, -173.0, -175.0, -200.0, -253.0, -400.0, -1e4, -1e20,
+     -1e27, -1e30, -3e38, 2.3e38, 2.4e38, 3e38, torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).min, 0.0, -0.0]
+
+
+def _gated(x):
+    """Device codes and scales of gated rows x [M, 2 K], and the definition in 64 bits."""
+    from paper_2512_15176_b200 import binding as L
+    M, K = x.shape[0], x.shape[1] // 2
+    codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, -(-K // 128), device="cuda")
+    L.deer_quantize(x.cuda(), codes, scales, gated=True)
+    x64 = f64(x)
+    with np.errstate(over="ignore"):                       # exp(-v) = inf: the quotient is 0
+        y = x64[:, :K] / (1.0 + np.exp(-x64[:, :K])) * x64[:, K:]
+    return f64(codes), scales.cpu().numpy().astype(np.float64), y
+
+
+def _check_gated(got, s, y, label):
+    """As test_gpu_quant.check_codes; and where a gated value is subnormal, it has been rounded four times to a multiple of 2^-149
+    (two steps of the numerator, the quotient, the product with up <= 8 in magnitude): 2^-145 / 2^-126 in a code's quotient."""
+    delta = 8e-6
+    amax = np.abs(y).reshape(y.shape[0], -1, 128).max(axis=2)
+    want_s = np.maximum(amax / 448.0, 2.0 ** -126)
+    assert (np.abs(s - want_s) <= 2 * delta * want_s).all(), label
+    q = np.clip(y / want_s.repeat(128, 1), -448, 448)
+    tol = O.e4m3_step(q) / 2 + 4 * delta * np.abs(q) + 2.0 ** -18
+    assert np.isfinite(got).all() and (np.abs(got - q) <= tol).all(), f"{label}: {np.max(np.abs(got - q) - tol)}"
+
+
+def test_gates_of_every_size_alone_in_their_group():
+    """A row per gate value, which fills its group: scales and codes follow v / (1 + exp(-v)) * u over all of bf16's exponents."""
+    x = torch.empty(len(GATES), 256, dtype=torch.bfloat16)
+    x[:, :128] = torch.tensor(GATES)[:, None].to(torch.bfloat16)
+    u = W.normal(450, "u", (len(GATES), 128), 1.0).clamp(-0.98, 0.98)
+    x[:, 128:] = u
+    _check_gated(*_gated(x), "alone")
+
+
+def test_one_far_gate_leaves_its_neighbours_their_codes():
+    """A strongly negative gate among ordinary ones is a zero among them: the group's scale is the ordinary values'."""
+    far = [v for v in GATES if v <= -60.0]
+    x = W.normal(451, "x", (len(far), 512), 2.0).clamp(-7.9, 7.9)
+    x[:, 37] = torch.tensor(far).to(torch.bfloat16)
+    x[:, 130] = torch.finfo(torch.bfloat16).min
+    x[:, 255] = -1e30
+    _check_gated(*_gated(x), "among others")
+
+
+def test_gated_groups_of_zeros_nan_and_infinities():
+    """A NaN or an infinity, as a gate or as the value that it gates, spoils its own group of 128 columns and no other."""
+    x = W.normal(452, "x", (7, 1024), 1.0)
+    x[0, :128] = 0.0                                       # gates of zero
+    x[0, 640:768] = 0.0                                    # values of zero
+    bad = {1: (3, float("nan")), 2: (130, float("inf")), 3: (260, -float("inf")), 4: (512 + 5, float("nan")), 5: (512 + 140, float("inf")),
+           6: (512 + 390, -float("inf"))}
+    for m, (c, v) in bad.items():
+        x[m, c] = v
+    clean = x.clone()
+    for m, (c, v) in bad.items():
+        clean[m, c] = 0.0
+    got, s, _ = _gated(x)
+    _, _, y = _gated(clean)
+    for m, (c, v) in bad.items():
+        g = c % 512 // 128
+        assert not np.isfinite(got[m, g * 128:(g + 1) * 128] * s[m, g]).any()
+        got[m, g * 128:(g + 1) * 128], s[m, g], y[m, g * 128:(g + 1) * 128] = 0.0, 2.0 ** -126, 0.0
+    _check_gated(got, s, y, "the other groups")
