@@ -35,7 +35,6 @@ __device__ int build_segments(const AttnParams& p, int HL, int rt, long long cur
         const int b = b0 + lane;
         int n = 0, s = 0;
         const int tiles = (b < p.B) ? tiles_of(b, &n, &s) : 0;
-        if (b < p.B && tiles == 0) deer_report(p.kv.status, DEER_ERR_INVALID_ARG);
         const long long span = (long long)tiles * HL;     // tiles this sequence contributes to the list
         long long incl = span;
 #pragma unroll

@@ -160,9 +160,11 @@ block_attn_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     for (int b = lane; b < p.B; b += 32) {
         const int tiles = seq_tiles(p, b, nullptr, nullptr);
         T += tiles;
-        // a sequence that cannot be used has no tiles, so no block will write its units' merge entries: do it here
-        if (tiles == 0 && j == 0 && warp == 0)
+        // a sequence that cannot be used has no tiles, so no block need ever list it: its units' merge entries and the report are written here
+        if (tiles == 0 && j == 0 && warp == 0) {
+            deer_report(p.kv.status, DEER_ERR_INVALID_ARG);
             for (int hr = 0; hr < HR; ++hr) p.unit_parts[(size_t)b * HR + hr] = make_int2(-1, -1);
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) T += __shfl_xor_sync(0xffffffffu, T, o);
