@@ -258,7 +258,7 @@ __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale,
         *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
     }
-    if (lane == 0) *scale = 1.f / up;
+    if (lane == 0) *scale = m != 0 ? 1.f / up : 0.f;               // (nothing but zeros: no say in the reference of the weights)
     return __any_sync(0xffffffffu, any >= 0x7f800000u);
 }
 

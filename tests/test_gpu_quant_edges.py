@@ -79,3 +79,36 @@ def test_gated_groups_of_zeros_nan_and_infinities():
         assert not np.isfinite(got[m, g * 128:(g + 1) * 128] * s[m, g]).any()
         got[m, g * 128:(g + 1) * 128], s[m, g], y[m, g * 128:(g + 1) * 128] = 0.0, 2.0 ** -126, 0.0
     _check_gated(got, s, y, "the other groups")
+
+
+def _attend(kv, q, kb, vb, msl, mask=0, states=None):
+    from paper_2512_15176_b200 import binding as L
+    B, k, Hq, D = q.shape
+    out = torch.full((B, k, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((L.deer_block_attn_quant_workspace_bytes(B, k, Hq, kv.n_kv_heads, D, msl),), 255, dtype=torch.uint8, device="cuda")
+    L.deer_block_attn_quant(kv, _ids(B), q.cuda(), kb.cuda(), vb.cuda(), out, None if states is None else torch.from_numpy(states).cuda(), mask,
+                            1 / math.sqrt(D), msl, ws)
+    assert L.deer_kv_status(kv) == 0
+    return out
+
+
+def _block(seed, k, Hq, Hkv, D=128):
+    return [W.normal(seed, n, (1, k, h, D), 1.0) for n, h in (("q", Hq), ("k", Hkv), ("v", Hkv))]
+
+
+BOUNDS = pytest.mark.parametrize("long", [False, True])            # True: the tensor-memory kernel, whatever the lengths are
+
+
+@BOUNDS
+@pytest.mark.parametrize("n", [0, 40, 200])
+@pytest.mark.parametrize("octaves", [-30, -60, 30])
+def test_values_of_any_magnitude(n, octaves, long):
+    """All values scaled by one power of two scale the result, whichever tile comes first and however many tokens the last holds."""
+    kv, okv = _cache([n], 2, 128, 0, 460)
+    okv.scale[1] *= np.float32(2.0 ** octaves)
+    okv.tail[1] *= 2.0 ** octaves
+    kv.v_scale.mul_(2.0 ** octaves)
+    kv.v_tail.mul_(2.0 ** octaves)
+    q, kb, vb = _block(460, 32, 8, 2)
+    vb *= 2.0 ** octaves
+    check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(128), None, f"{n} 2^{octaves}")
