@@ -16,8 +16,10 @@
 // A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  The bf16 tile has
 // the same form: K as two e4m3 terms, V as fp16, a power of two for every 16 tokens in the place of the scales.
 //
-// Exponentials are taken against a reference per row, chosen in the first tile (the row's maximum there, held as 2^11, and
-// the largest V scale) and raised only when a tile outgrows 2^15: O and l are then rescaled in place.
+// Exponentials are taken against a reference per row, chosen in the first tile and raised only when a tile outgrows 2^15: O and l
+// are then rescaled in place.  The weights of O, which hold a V scale, have one of their own: m_ref is the row's largest score, and
+// v_ref the power of two above the largest product of a weight and its V scale, both held as 2^11.  (With the largest V scale
+// as v_ref, a page of large values that weighs next to nothing would take the others' bits.)
 //
 // Two groups of four softmax warps take alternate tiles of a segment, each with an accumulator, a sum and a reference of
 // its own, so that neither waits for the other; they meet at the segment's end.  Warp roles: 0 loader of Q and K, 1 issuer of
@@ -31,6 +33,7 @@
 // has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22 us, 27000 cycles of them in a block: 9000
 // until the queries are there, 4500 on their terms, 7500 on four tiles, 6000 on joining.
 
+#include <cfloat>
 #include <cuda_fp16.h>
 
 #include "attn_quant.cuh"
@@ -88,8 +91,8 @@ constexpr int N_BARS = BAR_SEG + 1;
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
     float q_factor[2][128];                    // per query row: scale * log2(e) * the power of two taken out of it
-    float bt_scale[2 * PAGES];                 // powers of two taken out of the bf16 tile's tokens, 16 together: K, V
-    float scales[NSCALE][2 * PAGES];           // K scales, V scales of a page tile's pages
+    float bt_scale[3 * PAGES];                 // powers of two taken out of the bf16 tile's tokens, 16 together: K, V, log2 of V's
+    float scales[NSCALE][3 * PAGES];           // K scales, V scales of a page tile's pages, log2 of those
     float meet[2][3][128];                     // per group and row: reference, sum, V reference
     uint32_t tmem_slot;
     int abort_flag;
@@ -132,6 +135,7 @@ __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out,
     return HEAD + (n / PAGE + PAGES - 1) / PAGES + 1;
 }
 
+__device__ __forceinline__ float power_of_two(float e) { return __uint_as_float((uint32_t)((int)e + 127) << 23); }   // 2^e, -126 <= e <= 127
 // Power of two that brings a group's largest magnitude to [128, 256) (nothing but zeros: 1).
 __device__ __forceinline__ float to_256(uint32_t amax_bits) {
     const int f = amax_bits ? 127 + 7 + 127 - (int)(amax_bits >> 23) : 127;
@@ -258,7 +262,10 @@ __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale,
         *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
     }
-    if (lane == 0) *scale = m != 0 ? 1.f / up : 0.f;               // (nothing but zeros: no say in the reference of the weights)
+    if (lane == 0) {                                               // (nothing but zeros: no say in the reference of the weights)
+        scale[0] = m != 0 ? 1.f / up : 0.f;
+        scale[PAGES] = m != 0 ? 127.f - (float)(__float_as_uint(up) >> 23) : -INFINITY;
+    }
     return __any_sync(0xffffffffu, any >= 0x7f800000u);
 }
 
@@ -440,11 +447,13 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             vs_next = scale_of(qp.kq.v_scale, id_next);
                             id_third = ids_at(t + 16);
                         }
-                        const float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3)), vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
+                        float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3));
+                        const float vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
+                        if (!(fabsf(vs) < INFINITY)) ks = NAN;             // makes every row that sees the page NaN, as vs would
                         int oks = 1;
                         if (lane == 0) oks = wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
                         if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
-                        if (lane < 8) sh.scales[rs % NSCALE][lane] = lane < 4 ? ks : vs;
+                        if (lane < 3 * PAGES) sh.scales[rs % NSCALE][lane] = lane < PAGES ? ks : lane < 2 * PAGES ? vs : __log2f(vs);
                         __syncwarp();
                         if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);      // (the arrival publishes the scales as well)
                         __syncwarp();
@@ -675,7 +684,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             for (int si = 0; si < n_seg && alive; ++si, ++sg) {
                 const Seg& g = sh.segs[si];
                 const int full = g.n / PAGE, last_tile = (full + PAGES - 1) / PAGES, t_b = g.t_b;
-                float m_ref = 0.f, v_ref = 1.f, i_ref = 1.f, l_run = 0.f;
+                float m_ref = 0.f, lv_ref = 0.f, i_ref = 1.f, l_run = 0.f;      // lv_ref: log2 of v_ref, i_ref: 1 / v_ref
                 bool first = true;
                 const int qb = sg & 1;
                 {
@@ -732,7 +741,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll 1
                     for (int pass = 0; pass < 2; ++pass) {
                         if (set) {
-                            float m_t = -INFINITY, v_t = 0.f;
+                            float m_t = -INFINITY, j_t = -INFINITY;        // largest score; largest score + log2 of its V scale
 #pragma unroll 1
                             for (int h = 0; h < 2; ++h) {
                                 load_half(h);
@@ -742,16 +751,22 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                     float mx = -INFINITY;
 #pragma unroll
                                     for (int c = 0; c < PAGE; ++c) mx = fmaxf(mx, __uint_as_float(sr[x * PAGE + c]));
-                                    m_t = fmaxf(m_t, mx * (f_row * kv_scale[h * 2 + x]));
-                                    v_t = fmaxf(v_t, kv_scale[PAGES + h * 2 + x]);
+                                    mx *= f_row * kv_scale[h * 2 + x];
+                                    m_t = fmaxf(m_t, mx);
+                                    j_t = fmaxf(j_t, mx + kv_scale[2 * PAGES + h * 2 + x]);
                                 }
                             }
-                            if (!(fabsf(m_t) < INFINITY)) m_t = m_ref;     // nothing visible here, or not finite
-                            if (!(v_t > 0.f && v_t < INFINITY)) v_t = v_ref;
+                            if (!(fabsf(m_t) < INFINITY)) {                // nothing visible here, or not finite
+                                m_t = m_ref;
+                                j_t = m_ref + lv_ref;
+                            }
                             if (!first) {
                                 m_t = fmaxf(m_t, m_ref);
-                                v_t = fmaxf(v_t, v_ref);
-                                const float al = ex2_approx(m_ref - m_t), ao = al * (v_ref / v_t);
+                                j_t = fmaxf(j_t, m_ref + lv_ref);
+                            }
+                            const float lv_t = fminf(fmaxf(ceilf(j_t - m_t), -126.f), 126.f);
+                            if (!first) {
+                                const float al = ex2_approx(m_ref - m_t), ao = ex2_approx((m_ref - m_t) + (lv_ref - lv_t));
                                 // phase (it >> 1) - 1 of o_done: the group's previous tile is in O.  (The one before it is: its
                                 // buffer is the one that this tile's scores are in.)
                                 const bool od = wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
@@ -770,8 +785,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 l_run *= al;
                             }
                             m_ref = m_t;
-                            v_ref = v_t;
-                            i_ref = 1.f / v_ref;
+                            lv_ref = lv_t;
+                            i_ref = power_of_two(-lv_ref);
                         }
                         // weights 2^(score - m_ref + 11), and in fp16 those times V scale / v_ref
                         uint64_t sum2[2] = {0, 0};
@@ -784,7 +799,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 const float nm = h * 2 + x < n_pages ? BIAS - m_ref : -INFINITY;
                                 float ka = f_row * kv_scale[h * 2 + x];
                                 if (ka == 0.f) ka = quant::SCALE_MIN;      // a masked -inf must stay one
-                                const float va = kv_scale[PAGES + h * 2 + x] * i_ref;
+                                const float va = fminf(kv_scale[PAGES + h * 2 + x] * i_ref, FLT_MAX);      // (beyond that: masked, or next to nothing)
                                 const uint64_t nm2 = pack_f32x2(nm, nm), ka2 = pack_f32x2(ka, ka), va2 = pack_f32x2(va, va);
 #pragma unroll
                                 for (int c = x * PAGE; c < (x + 1) * PAGE; c += 2) {
@@ -824,7 +839,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 if (!__all_sync(0xffffffffu, done)) { alive = false; break; }
                 sh.meet[grp][0][row] = first ? -INFINITY : m_ref;
                 sh.meet[grp][1][row] = first ? 0.f : l_run;
-                sh.meet[grp][2][row] = v_ref;
+                sh.meet[grp][2][row] = power_of_two(lv_ref);
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(BAR_MEET + quarter));

@@ -112,3 +112,30 @@ def test_values_of_any_magnitude(n, octaves, long):
     q, kb, vb = _block(460, 32, 8, 2)
     vb *= 2.0 ** octaves
     check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(128), None, f"{n} 2^{octaves}")
+
+
+@pytest.mark.parametrize("long", [True])
+@pytest.mark.parametrize("k,Hq,Hkv", [(32, 8, 2)])
+@pytest.mark.parametrize("at,lift", [(0, 0.0), (20, 0.0), (0, 30.0), (0, -30.0)])
+@pytest.mark.parametrize("octaves", [30, 60])
+def test_a_page_of_large_values_and_little_weight(at, lift, octaves, k, Hq, Hkv, long):
+    """Page `at` has values 2^octaves times the others', and weights so small that it adds a part of the result that is about as
+    large as the others' or far smaller.  The scores behind the first four pages lie `lift` above those of the first four."""
+    n, D = 640, 128
+    kv, okv = _cache([n], Hkv, D, 0, 461)
+    q, kb, vb = _block(461, k, Hq, Hkv)
+    q = q * 0.05
+    q[..., 0] = 8.0                                        # dim 0 carries the level of a page's scores
+    key = lambda level: level * math.sqrt(D) / 8.0
+    okv.scale[0][:] = 0.5
+    K = O.e4m3_round(np.clip(okv.codes[0] / 30.0, -4.0, 4.0))
+    for p in range(n // 16):
+        level = -(octaves * math.log(2.0) + 1.0) if p == at else lift if p >= 4 else 0.0
+        K[okv.page_table[0, p], :, :, 0] = O.e4m3_round(key(level) / 0.5)
+    okv.codes[0] = K
+    okv.scale[1][okv.page_table[0, at]] *= np.float32(2.0 ** octaves)
+    kb[..., 0] = key(max(lift, 0.0))
+    kv.k_pool.copy_(torch.from_numpy(okv.codes[0]).float().to(F8))
+    kv.k_scale.copy_(torch.from_numpy(okv.scale[0]))
+    kv.v_scale.copy_(torch.from_numpy(okv.scale[1]))
+    check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, f"page {at}")
