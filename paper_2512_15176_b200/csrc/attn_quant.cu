@@ -9,14 +9,14 @@
 // operand fragments (the contraction index of q . k and the column index of p v may be permuted freely, as long as the
 // other side is permuted alike), so the lanes exchange nothing -- and the codes become fp16 exactly.  The page's K scale multiplies the 16 scores; its V scale
 // multiplies the page's product before it joins the fp32 sums, so scales of any size work.  Queries are brought to
-// fp16 by a power of two per row (exact to 2^-24 of the row's largest), probabilities are at most 2^12 and keep fp16's
-// 11 bits down to 2^-26 of the row's maximum.  The warps of a block take pages in turn with running maxima of their
+// fp16 by a power of two per row (exact to 2^-24 of the row's largest), probabilities are taken against their page's maximum, at
+// most 2^12, and keep fp16's 11 bits down to 2^-26 of it; the page's own weight joins its product in fp32.  The warps of a block take pages in turn with running maxima of their
 // own, and meet in shared memory at the end.  A context is cut into chunks over thread blocks; up to eight of them form
 // a cluster and meet in its shared memory, and where a context has more a second kernel joins the clusters' parts.
 //
 // What bounds it: latencies in short contexts (one token, 32 query and 8 KV heads, over 1003: 7.8 us, two pages per warp,
 // most of it the chain length -> page number -> page -> products -> meeting in the cluster), the instructions of a page
-// (about 400 a warp, and their latencies) in long ones: 16 x 4096 tokens 43.7 us = 3.1 TB/s.
+// (about 400 a warp, and their latencies) in long ones: 16 x 4096 tokens 44.4 us = 3.1 TB/s.
 
 #include <cuda_fp16.h>
 
@@ -52,6 +52,12 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+// 2^x of differences to a maximum; 0 below 2^-126.
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ float quad_max(float v) {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
@@ -183,15 +189,19 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
     for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};     // l: this lane's columns only, until the end
 
-    // Scores (of two or four column tiles of 8 keys) in the log2 domain -> probabilities; raises the running maximum.
-    auto softmax = [&](auto& sc) {
-        constexpr int N = sizeof(sc) / sizeof(sc[0]);
+    // Scores (N groups of two column tiles of 8 keys each) in the log2 domain -> probabilities against their group's maximum, and
+    // the weight of each group against the running maximum, which rises.  (A page's probabilities are rounded to fp16 before
+    // its V scale joins them: against the running maximum a page of large values and little weight would lose them.)
+    auto softmax = [&](auto& sc, auto& weight) {
+        constexpr int N = sizeof(sc) / sizeof(sc[0]) / 2;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            float mx = fmaxf(sc[0][2 * u], sc[0][2 * u + 1]);
+            float mx[N], mn = m_run[u];
 #pragma unroll
-            for (int t = 1; t < N; ++t) mx = fmaxf(mx, fmaxf(sc[t][2 * u], sc[t][2 * u + 1]));
-            const float mn = fmaxf(m_run[u], quad_max(mx));
+            for (int x = 0; x < N; ++x) {
+                mx[x] = quad_max(fmaxf(fmaxf(sc[2 * x][2 * u], sc[2 * x][2 * u + 1]), fmaxf(sc[2 * x + 1][2 * u], sc[2 * x + 1][2 * u + 1])));
+                mn = fmaxf(mn, mx[x]);
+            }
             if (__any_sync(0xffffffffu, mn > m_run[u])) {
                 const float corr = mn == -INFINITY ? 1.f : exp2f(m_run[u] - mn);
                 l_run[u] *= corr;
@@ -202,17 +212,19 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
                 }
                 m_run[u] = mn;
             }
-            const float base = (mn == -INFINITY ? 0.f : mn) - P_BIAS;
-            float sum = 0.f;
 #pragma unroll
-            for (int t = 0; t < N; ++t)
+            for (int x = 0; x < N; ++x) {
+                const float base = (mx[x] == -INFINITY ? 0.f : mx[x]) - P_BIAS;
+                float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float pr = exp2f(sc[t][2 * u + e] - base);
-                    sc[t][2 * u + e] = pr;
-                    sum += pr;
+                for (int e = 0; e < 4; ++e) {
+                    float& s = sc[2 * x + (e >> 1)][2 * u + (e & 1)];
+                    s = ex2(s - base);
+                    sum += s;
                 }
-            l_run[u] += sum;
+                weight[x][u] = mx[x] == -INFINITY ? 1.f : ex2(mx[x] - mn);
+                l_run[u] = fmaf(sum, weight[x][u], l_run[u]);
+            }
         }
     };
 
@@ -226,7 +238,7 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
         if (j + 2 < n_pages) bring(j + 2);
         if (j + 3 < n_pages) bring(j + 3);
         cp_async_commit();
-        float sc[4][4], vs[2];
+        float sc[4][4], vs[2], weight[2][2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             if (x == 1 && !two) {
@@ -252,10 +264,11 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
                 d[0] *= f0; d[1] *= f0; d[2] *= f1; d[3] *= f1;
             }
         }
-        softmax(sc);
+        softmax(sc, weight);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             if (x == 1 && !two) break;
+            const float f[2] = {vs[x] * weight[x][0], vs[x] * weight[x][1]};
             const uint32_t pa[4] = {pack_f16(sc[2 * x][0], sc[2 * x][1]), pack_f16(sc[2 * x][2], sc[2 * x][3]), pack_f16(sc[2 * x + 1][0], sc[2 * x + 1][1]),
                                     pack_f16(sc[2 * x + 1][2], sc[2 * x + 1][3])};
             uint32_t v[4][VW];                 // values 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
@@ -282,7 +295,7 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
                         mma_f16_16816(r, pa, e ? codes_hi(a) : codes_lo(a), e ? codes_hi(d) : codes_lo(d));
                         const int i = w * 4 + h * 2 + e;
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) o[i][z] = fmaf(r[z], vs[x], o[i][z]);
+                        for (int z = 0; z < 4; ++z) o[i][z] = fmaf(r[z], f[z >> 1], o[i][z]);
                     }
                 }
             }
@@ -325,7 +338,12 @@ __global__ void __launch_bounds__(WARPS * 32, RESIDENT) attn_quant_kernel(const 
                 for (int z = 0; z < 4; ++z)
                     sc[t][z] = (see[z >> 1] >> (t * 8 + t4 * 2 + (z & 1))) & 1u ? sc[t][z] * p.scale_log2 : -INFINITY;
             }
-            softmax(sc);
+            float weight[1][2];
+            softmax(sc, weight);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) sc[t][z] *= weight[0][z >> 1];         // (fp32, and bf16's range below)
             // values: a NaN or an infinity must reach only the rows that see it, so such a group of rows goes element by element
             uint4 vv[4][D / 64];               // D / 8 bf16 of four tokens
             uint32_t worst = 0;

@@ -114,8 +114,8 @@ def test_values_of_any_magnitude(n, octaves, long):
     check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(128), None, f"{n} 2^{octaves}")
 
 
-@pytest.mark.parametrize("long", [True])
-@pytest.mark.parametrize("k,Hq,Hkv", [(32, 8, 2)])
+@BOUNDS
+@pytest.mark.parametrize("k,Hq,Hkv", [(32, 8, 2), (4, 4, 2)])
 @pytest.mark.parametrize("at,lift", [(0, 0.0), (20, 0.0), (0, 30.0), (0, -30.0)])
 @pytest.mark.parametrize("octaves", [30, 60])
 def test_a_page_of_large_values_and_little_weight(at, lift, octaves, k, Hq, Hkv, long):
