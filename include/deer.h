@@ -514,8 +514,9 @@ int deer_kv_commit_rows(deer_kv* kv, const int32_t* seq_ids, const int32_t* keep
 /* Block attention (as deer_block_attn_rows, without the append) against an 8-bit cache: the keys are the tokens of the
  * full pages (codes times their page's scale), the tail rows, and the block rows that mask and row_state allow.
  * row_state: bidirectional mask only, or NULL; the output rows of absent positions are zero.  Scores and probabilities:
- * fp32; queries enter exactly (to 2^-18 of a row's largest magnitude); probabilities enter the second product rounded to
- * 11 bits.  A NaN or an infinity in a value row reaches only the rows that see it.
+ * fp32; queries, and the keys that are bf16, enter exactly down to 2^-9 of their row's largest magnitude and to an absolute
+ * error of 2^-17 of that below it; probabilities enter the second product rounded to 11 bits.  What a row does not see has no
+ * part in its result: a NaN, an infinity or a finite value of any size in a key or value row reaches only the rows that see it.
  *   workspace  >= deer_block_attn_quant_workspace_bytes(...) bytes, 16-byte aligned, contents arbitrary; one call at a
  *              time per workspace. */
 size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, int Hkv, int D, int max_seq_len);

@@ -7,14 +7,15 @@
 // unit's tiles are preceded in that list by HEAD places with no work in them.
 //
 //   S = Q K^T   on the codes as the cache holds them.  Q is split into two e4m3 terms per row, q = 2^x (q1 + q2): a bf16 value
-//               has 8 significant bits, e4m3 has 4, so the two terms are exact except for elements below 2^-13 of their row's
-//               largest (absolute error 2^-18 of that).  Two e4m3 MMAs at twice the bf16 rate cost what one bf16 MMA would,
+//               has 8 significant bits, e4m3 has 4, so the two terms are exact except for elements below 2^-9 of their row's
+//               largest (absolute error at most 2^-17 of that).  Two e4m3 MMAs at twice the bf16 rate cost what one bf16 MMA would,
 //               and K needs half the shared memory and no conversion.
 //   O += P V    in fp16: four warps turn the codes of V into fp16 (exact) in shared memory.  The weights P need eleven bits and
 //               a range that 8-bit terms only reach with three of them (built: splitting P cost the softmax twice the
 //               instructions of the exponentials, V's conversion costs a quarter of that).
 // A page's K scale multiplies its 16 score columns, its V scale its 16 columns of P, both in the softmax.  The bf16 tile has
-// the same form: K as two e4m3 terms, V as fp16, a power of two for every 16 tokens in the place of the scales.
+// the same form, K as two e4m3 terms and V as fp16, but a power of two for every token in the place of the scales: not every row
+// sees every token, and what a row does not see must not take its bits.
 //
 // Exponentials are taken against a reference per row, chosen in the first tile and raised only when a tile outgrows 2^15: O and l
 // are then rescaled in place.  The weights of O, which hold a V scale, have one of their own: m_ref is the row's largest score, and
@@ -91,7 +92,7 @@ constexpr int N_BARS = BAR_SEG + 1;
 struct Shared {                                // behind the operand buffers
     uint64_t bars[N_BARS];
     float q_factor[2][128];                    // per query row: scale * log2(e) * the power of two taken out of it
-    float bt_scale[3 * PAGES];                 // powers of two taken out of the bf16 tile's tokens, 16 together: K, V, log2 of V's
+    float bt_k[TILE], bt_lv[TILE];             // powers of two taken out of the bf16 tile's tokens: of K, log2 of V's
     float scales[NSCALE][3 * PAGES];           // K scales, V scales of a page tile's pages, log2 of those
     float meet[2][3][128];                     // per group and row: reference, sum, V reference
     uint32_t tmem_slot;
@@ -136,6 +137,22 @@ __device__ __forceinline__ int seq_tiles(const AttnParams& p, int b, int* n_out,
 }
 
 __device__ __forceinline__ float power_of_two(float e) { return __uint_as_float((uint32_t)((int)e + 127) << 23); }   // 2^e, -126 <= e <= 127
+// log2 of the reference of the weights of O from that of the largest product of a weight and its V scale, both against m_ref.
+__device__ __forceinline__ float log2_reference(float j) { return fminf(fmaxf(ceilf(j), -126.f), 126.f); }
+// This thread's row of an accumulator times a factor.  (Out of line: two places need it, neither often.)
+__device__ __noinline__ void scale_accumulator(uint32_t taddr, float by) {
+#pragma unroll 1
+    for (int cc = 0; cc < HD / 16; ++cc) {
+        uint32_t o[16];
+        TMEM_LD_X16(taddr + (uint32_t)(cc * 16), o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * by);
+        TMEM_ST_X16(taddr + (uint32_t)(cc * 16), o);
+    }
+    tmem_wait_st();
+}
+
 // Power of two that brings a group's largest magnitude to [128, 256) (nothing but zeros: 1).
 __device__ __forceinline__ float to_256(uint32_t amax_bits) {
     const int f = amax_bits ? 127 + 7 + 127 - (int)(amax_bits >> 23) : 127;
@@ -194,49 +211,40 @@ __device__ __forceinline__ void split_queries(unsigned char* tile, float* factor
     }
 }
 
-// Sixteen tokens (tok0 ..) of the bf16 tile's K in place as two terms, with one power of two for them; a token with a NaN
-// or an infinity gets NaN codes.  Whole-warp call, for rows that this warp's lanes have brought, each its pieces.
+// Sixteen tokens (tok0 ..) of the bf16 tile's K in place as two terms, with a power of two for each; a token with a NaN or an
+// infinity gets NaN codes.  Whole-warp call, for rows that this warp's lanes have brought, each its pieces.
 __device__ __forceinline__ void split_keys(unsigned char* tile, float* scale, int tok0) {
     const int lane = threadIdx.x & 31, c16 = lane & 7;
-    uint32_t m = 0;
-    float up = 1.f;
 #pragma unroll 1
-    for (int x = 0; x < 8; ++x) {                                  // the largest magnitude of four rows four times, then their terms
-        const int tok = tok0 + (x & 3) * 4 + (lane >> 3);
+    for (int x = 0; x < 4; ++x) {
+        const int tok = tok0 + x * 4 + (lane >> 3);
         float v[16];
         quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 0), v);
         quant::unpack_bf16x8(*piece(tile, T_BYTES, tok, c16, 1), v + 8);
-        const uint32_t mt = quant::max8(quant::amax16(v));         // (every lane of the row has read)
-        const bool bad = mt >= 0x7f800000u;
-        if (x < 4) {
-            m = max(m, bad ? 0u : mt);
-            if (x == 3) {
-                m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                up = to_256(m);
-            }
-            continue;
-        }
+        const uint32_t m = quant::max8(quant::amax16(v));          // (every lane of the row has read)
+        const bool bad = m >= 0x7f800000u;
+        const float up = bad ? 1.f : to_256(m);
         uint4 t1, t2;
         split16(v, up, bad, &t1, &t2);
         unsigned char* dst = tile + tok * HD + ((c16 ^ (tok & 7)) << 4);
         *reinterpret_cast<uint4*>(dst) = t1;
         *reinterpret_cast<uint4*>(dst + T_BYTES) = t2;
+        if (c16 == 0) scale[tok] = 1.f / up;
     }
-    if (lane == 0) *scale = 1.f / up;
 }
-// The same for V, in place as fp16 (exact down to 2^-21 of the largest of the sixteen tokens, 2^-32 of it absolutely).  NaN
-// and infinities become zeros -- they join the rows that see them at the segment's end -- and the call returns true.
-__device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale, int tok0) {
+// The same for V, in place as fp16 (exact down to 2^-21 of the token's largest, 2^-32 of it absolutely), and log2 of the power of
+// two (-infinity for nothing but zeros: no say in the reference of the weights).  NaN and infinities become zeros -- they join the
+// rows that see them at the segment's end -- and the call returns true.
+__device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* log2_scale, int tok0) {
     const int lane = threadIdx.x & 31, c16 = lane & 7, c8 = (c16 & 3) * 2;
-    uint32_t m = 0, any = 0;
-    float up = 1.f;
+    uint32_t any = 0;
 #pragma unroll 1
-    for (int x = 0; x < 8; ++x) {
-        const int tok = tok0 + (x & 3) * 4 + (lane >> 3);
+    for (int x = 0; x < 4; ++x) {
+        const int tok = tok0 + x * 4 + (lane >> 3);
         float v[16];
         quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 0), v);
         quant::unpack_bf16x8(*piece(tile, VH_HALF, tok, c16, 1), v + 8);
+        uint32_t m = 0;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const uint32_t mag = quant::mag_bits(v[e]);
@@ -244,14 +252,8 @@ __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale,
             if (mag >= 0x7f800000u) v[e] = 0.f;
             else m = max(m, mag);
         }
-        if (x < 4) {
-            if (x == 3) {
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                up = to_256(m);
-            }
-            continue;
-        }
+        m = quant::max8(m);
+        const float up = to_256(m);
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -261,10 +263,7 @@ __device__ __forceinline__ bool values_to_f16(unsigned char* tile, float* scale,
         unsigned char* dst = tile + (c16 >> 2) * VH_HALF + tok * 128;
         *reinterpret_cast<uint4*>(dst + ((c8 ^ (tok & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         *reinterpret_cast<uint4*>(dst + (((c8 + 1) ^ (tok & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-    if (lane == 0) {                                               // (nothing but zeros: no say in the reference of the weights)
-        scale[0] = m != 0 ? 1.f / up : 0.f;
-        scale[PAGES] = m != 0 ? 127.f - (float)(__float_as_uint(up) >> 23) : -INFINITY;
+        if (c16 == 0) log2_scale[tok] = m != 0 ? 127.f - (float)(__float_as_uint(up) >> 23) : -INFINITY;
     }
     return __any_sync(0xffffffffu, any >= 0x7f800000u);
 }
@@ -635,8 +634,8 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         cp_async_commit();
                         cp_async_wait<0>();                                // (and whatever V is on its way)
                         __syncwarp();
-                        split_keys(bt, sh.bt_scale + w, w * PAGE);
-                        if (values_to_f16(bt + 2 * T_BYTES, sh.bt_scale + PAGES + w, w * PAGE) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
+                        split_keys(bt, sh.bt_k, w * PAGE);
+                        if (values_to_f16(bt + 2 * T_BYTES, sh.bt_lv, w * PAGE) && lane == 0) *(volatile int*)&sh.bt_bad[nb & 1] = nb + 1;
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(BAR_BT_FULL));
@@ -705,33 +704,90 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 for (int t = g.t_a; t < t_b; ++t, ++it) {
                     const bool is_bt = t == last_tile;
                     const int sb = it % NS;
-                    const float* kv_scale = is_bt ? sh.bt_scale : sh.scales[rs % NSCALE];
+                    const float* kv_scale = sh.scales[rs % NSCALE];        // (of a page tile)
                     if (!is_bt) ++rs;
                     if ((it & 1) != grp) continue;
-                    const int n_pages = is_bt ? PAGES : min(PAGES, full - t * PAGES);
+                    const int n_pages = min(PAGES, full - t * PAGES);
                     const uint32_t s_tmem = t_lane + (uint32_t)(sb * TILE);
                     // The scores, and with them the scales.  (Not K_FULL or BT_FULL for those: a slot may be on its next tile but one
                     // by now, and a parity wait cannot tell.)
                     const bool got = wait(bar(BAR_S_FULL + sb), (uint32_t)(it / NS) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, got)) { alive = false; break; }
                     tcgen05_fence_after();
-                    uint64_t see = 0;
+                    // O times a factor.  Phase (it >> 1) - 1 of o_done: the group's previous tile is in O.  (The one before it is: its
+                    // buffer is the one that this tile's scores are in.)
+                    auto shrink = [&](float by) {
+                        const bool od = wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
+                        if (!__all_sync(0xffffffffu, od)) return false;
+                        tcgen05_fence_after();
+                        scale_accumulator(t_lane + (uint32_t)(O_COL + grp * HD), by);
+                        return true;
+                    };
                     if (is_bt) {
+                        // Every column has factors of its own, and not every row sees it.  Whether a row's references have to rise is seen
+                        // before its weights are made, for the row alone; P takes the scores' place sixteen columns at a time.
                         uint32_t present, decoded;
                         attn::row_state_sets(p.row_state, g.b, p.k, lane, &present, &decoded);
-                        see = columns_seen(p, g, i_blk, row_valid, present, decoded);
+                        const uint64_t see = columns_seen(p, g, i_blk, row_valid, present, decoded);
+                        auto load = [&](int q, float (&sc)[16]) {          // scores in the log2 domain
+                            uint32_t r[16];
+                            TMEM_LD_X16(s_tmem + (uint32_t)(q * 16), r);
+                            tmem_wait_ld();
+                            const uint32_t bits = (uint32_t)(see >> (q * 16));
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) sc[c] = (bits >> c) & 1u ? __uint_as_float(r[c]) * (f_row * sh.bt_k[q * 16 + c]) : -INFINITY;
+                        };
+                        float m_t = -INFINITY, j_t = -INFINITY;            // largest score; largest score + log2 of its value's factor
+#pragma unroll 1
+                        for (int q = 0; q < TILE / 16; ++q) {
+                            float sc[16];
+                            load(q, sc);
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) {
+                                m_t = fmaxf(m_t, sc[c]);
+                                j_t = fmaxf(j_t, sc[c] + sh.bt_lv[q * 16 + c]);
+                            }
+                        }
+                        // (nothing visible, or not finite: the references stay)
+                        const bool rise = fabsf(m_t) < INFINITY && (first || m_t > m_ref + 28.f || j_t > m_ref + lv_ref + 4.f);
+                        if (!first) {
+                            m_t = fmaxf(m_t, m_ref);
+                            j_t = fmaxf(j_t, m_ref + lv_ref);
+                        }
+                        const float m_n = rise ? m_t : m_ref, lv_n = rise ? log2_reference(j_t - m_t) : lv_ref;
+                        if (!first && __any_sync(0xffffffffu, rise)) {
+                            l_run *= ex2_approx(m_ref - m_n);
+                            if (!shrink(ex2_approx((m_ref - m_n) + (lv_ref - lv_n)))) { alive = false; break; }
+                        }
+                        m_ref = m_n;
+                        lv_ref = lv_n;
+                        first = false;
+#pragma unroll 1
+                        for (int q = 0; q < TILE / 16; ++q) {
+                            float sc[16];
+                            uint32_t w[8];
+                            load(q, sc);
+#pragma unroll
+                            for (int c = 0; c < 16; c += 2) {
+                                const float p0 = sc[c] + (BIAS - m_ref), p1 = sc[c + 1] + (BIAS - m_ref);
+                                l_run += ex2_approx(p0) + ex2_approx(p1);
+                                const __half2 hw = __floats2half2_rn(ex2_approx(p0 + (sh.bt_lv[q * 16 + c] - lv_ref)),
+                                                                     ex2_approx(p1 + (sh.bt_lv[q * 16 + c + 1] - lv_ref)));
+                                w[c >> 1] = *reinterpret_cast<const uint32_t*>(&hw);
+                            }
+                            TMEM_ST_X8(s_tmem + (uint32_t)(q * 8), w);
+                        }
+                        tmem_wait_st();
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(BAR_P_READY + sb));
+                        continue;                                          // (the unit's last tile)
                     }
                     // 32 scores: column c of half h in the log2 domain = sr[c] * factor * its page's K scale
                     uint32_t sr[32];
                     auto load_half = [&](int h) {
                         TMEM_LD_X32(s_tmem + (uint32_t)(h * 32), sr);
                         tmem_wait_ld();
-                        if (is_bt) {
-                            const uint32_t bits = (uint32_t)(see >> (h * 32));
-#pragma unroll
-                            for (int c = 0; c < 32; ++c)
-                                if (!((bits >> c) & 1u)) sr[c] = 0xff800000u;
-                        }
                     };
                     // The group's first tile sets the references.  Later a weight of 2^15 (0x7800 in fp16) or a sum of 2^40 raises
                     // them: O and l shrink in place, the tile is done again (P has not taken the scores' place yet).
@@ -756,7 +812,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                     j_t = fmaxf(j_t, mx + kv_scale[2 * PAGES + h * 2 + x]);
                                 }
                             }
-                            if (!(fabsf(m_t) < INFINITY)) {                // nothing visible here, or not finite
+                            if (!(fabsf(m_t) < INFINITY)) {                // not finite
                                 m_t = m_ref;
                                 j_t = m_ref + lv_ref;
                             }
@@ -764,25 +820,10 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 m_t = fmaxf(m_t, m_ref);
                                 j_t = fmaxf(j_t, m_ref + lv_ref);
                             }
-                            const float lv_t = fminf(fmaxf(ceilf(j_t - m_t), -126.f), 126.f);
+                            const float lv_t = log2_reference(j_t - m_t);
                             if (!first) {
-                                const float al = ex2_approx(m_ref - m_t), ao = ex2_approx((m_ref - m_t) + (lv_ref - lv_t));
-                                // phase (it >> 1) - 1 of o_done: the group's previous tile is in O.  (The one before it is: its
-                                // buffer is the one that this tile's scores are in.)
-                                const bool od = wait(bar(BAR_O_DONE + grp), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
-                                if (!__all_sync(0xffffffffu, od)) { stop = true; break; }
-                                tcgen05_fence_after();
-#pragma unroll 1
-                                for (int cc = 0; cc < HD / 16; ++cc) {
-                                    uint32_t o[16];
-                                    TMEM_LD_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
-                                    tmem_wait_ld();
-#pragma unroll
-                                    for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ao);
-                                    TMEM_ST_X16(t_lane + (uint32_t)(O_COL + grp * HD + cc * 16), o);
-                                }
-                                tmem_wait_st();
-                                l_run *= al;
+                                l_run *= ex2_approx(m_ref - m_t);
+                                if (!shrink(ex2_approx((m_ref - m_t) + (lv_ref - lv_t)))) { stop = true; break; }
                             }
                             m_ref = m_t;
                             lv_ref = lv_t;
@@ -797,8 +838,7 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
                                 const float nm = h * 2 + x < n_pages ? BIAS - m_ref : -INFINITY;
-                                float ka = f_row * kv_scale[h * 2 + x];
-                                if (ka == 0.f) ka = quant::SCALE_MIN;      // a masked -inf must stay one
+                                const float ka = f_row * kv_scale[h * 2 + x];
                                 const float va = fminf(kv_scale[PAGES + h * 2 + x] * i_ref, FLT_MAX);      // (beyond that: masked, or next to nothing)
                                 const uint64_t nm2 = pack_f32x2(nm, nm), ka2 = pack_f32x2(ka, ka), va2 = pack_f32x2(va, va);
 #pragma unroll

@@ -139,3 +139,48 @@ def test_a_page_of_large_values_and_little_weight(at, lift, octaves, k, Hq, Hkv,
     kv.k_scale.copy_(torch.from_numpy(okv.scale[0]))
     kv.v_scale.copy_(torch.from_numpy(okv.scale[1]))
     check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, f"page {at}")
+
+
+@BOUNDS
+@pytest.mark.parametrize("k,Hq,Hkv", [(32, 16, 4), (20, 8, 1), (4, 4, 2)])
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 40, torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).min])
+@pytest.mark.parametrize("what", ["key", "value"])
+def test_large_finite_rows_reach_only_rows_that_see_them(what, size, k, Hq, Hkv, long):
+    """The last draft row, which the rows before it do not see, has a key or a value of any finite size."""
+    n, D = 200, 128
+    kv, okv = _cache([n], Hkv, D, 0, 462)
+    q, kb, vb = _block(462, k, Hq, Hkv)
+    clean = [t.clone() for t in (q, kb, vb)]
+    without = _attend(kv, q, kb, vb, 1 << 20 if long else n)
+    (kb if what == "key" else vb)[0, k - 1] = size
+    out = _attend(kv, q, kb, vb, 1 << 20 if long else n)
+    assert torch.equal(out[:, :-1], without[:, :-1])
+    check_attention(out[:, :-1], *[t[:, :-1] for t in clean], okv, [0], 0, 1 / math.sqrt(D), None, what)
+    # as a row that is still masked, the decoded rows do not see it either
+    states = np.zeros((1, k), dtype=np.int32)
+    states[0, -1] = 1
+    out = _attend(kv, q, kb, vb, 1 << 20 if long else n, 1, states)
+    st = states.copy()
+    st[0, -1] = -1
+    want = _attend(kv, clean[0], clean[1], clean[2], 1 << 20 if long else n, 1, st)
+    assert torch.equal(out[:, :-1], want[:, :-1])
+
+
+@BOUNDS
+@pytest.mark.parametrize("k,Hq,Hkv", [(32, 16, 4), (4, 4, 2)])
+def test_tail_and_block_rows_of_very_different_size(k, Hq, Hkv, long):
+    """Neighbouring tokens whose keys and values differ by many octaves in size; the largest keys lie across the queries, so that the
+    smaller ones' scores decide."""
+    n, D = 206, 128
+    kv, okv = _cache([n], Hkv, D, 0, 463)
+    q, kb, vb = _block(463, k, Hq, Hkv)
+    q[..., 5] = 0.0
+    kb[:, ::5] = 0.0
+    kb[:, ::5, :, 5] = 2.0 ** 30
+    okv.tail[0][:, :, 1::5] = 0.0
+    okv.tail[0][:, :, 1::5, 5] = -2.0 ** 25
+    vb[:, ::7] *= 2.0 ** -20
+    okv.tail[1][:, :, ::3] *= 2.0 ** -40
+    kv.k_tail.copy_(torch.from_numpy(okv.tail[0]).to(torch.bfloat16))
+    kv.v_tail.copy_(torch.from_numpy(okv.tail[1]).to(torch.bfloat16))
+    check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, "sizes")
