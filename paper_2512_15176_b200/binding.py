@@ -165,13 +165,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
-# (a call's tensors are on the device, so torch has initialised it by now)
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# The handle itself, where torch has it: torch.cuda.current_stream() builds a Stream object first, which takes longer than a
+# launch.  (A call's tensors are on the device, so torch has initialised it by now.)
+_raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        # the handle itself: torch.cuda.current_stream() builds a Stream object first, which takes longer than a launch
+        if _raw_stream is None or _current_device is None:
+            return torch.cuda.current_stream().cuda_stream or None
         return _raw_stream(_current_device()) or None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream or None
