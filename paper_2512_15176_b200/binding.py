@@ -240,6 +240,7 @@ class KVCacheQuant(KVCache):
         assert k_tail.dtype == v_tail.dtype == torch.bfloat16
         self._describe(k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top)
         self.k_scale, self.v_scale, self.k_tail, self.v_tail = k_scale, v_scale, k_tail, v_tail
+        self._heads = Hkv, D
         quant = deer_kv_quant_desc(_ptr(k_scale), _ptr(v_scale), _ptr(k_tail), _ptr(v_tail))
         _check(lib().deer_kv_create_quant(ctypes.byref(self.handle), ctypes.byref(self.desc), ctypes.byref(quant)))
 
@@ -281,8 +282,21 @@ class KVCacheQuant(KVCache):
                             same(self.v_tail), self.page_table, self.seq_len, self.n_pages, self.free_stack, self.free_top)
 
 
+# The library sees pointers and sizes only: what a call would read or write past an operand's end is refused here.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _refuse(call: str, what: str):
+    raise DeerError(DEER_ERR_INVALID_ARG, f"{call}: {what}")
+
+
 def deer_kv_store(kv: KVCacheQuant, seq_ids, k_rows, v_rows, keep=None, stream=None) -> None:
-    B, k = k_rows.shape[:2]
+    B, k, *heads = k_rows.shape
+    if not (k_rows.dtype is _BF16 and v_rows.dtype is _BF16 and v_rows.shape == k_rows.shape and tuple(heads) == kv._heads):
+        _refuse("deer_kv_store", "k_rows and v_rows must be bf16 [B][k][Hkv][D] of the cache's Hkv and D")
+    if not (seq_ids.dtype is _I32 and seq_ids.numel() == B and (keep is None or keep.dtype is _I32 and keep.numel() == B)):
+        _refuse("deer_kv_store", "seq_ids and keep must be int32 [B]")
     _check(lib().deer_kv_store(kv.handle, _ptr(seq_ids), _ptr(k_rows), _ptr(v_rows), _ptr(keep), B, k, _stream(stream)))
 
 
@@ -300,6 +314,13 @@ def deer_block_attn_quant_workspace_bytes(B, k, Hq, Hkv, D, max_seq_len) -> int:
 
 def deer_block_attn_quant(kv: KVCacheQuant, seq_ids, q, k_blk, v_blk, out, row_state, mask, scale, max_seq_len, workspace, stream=None):
     B, k, Hq, D = q.shape
+    Hkv, D_kv = kv._heads
+    if not (q.dtype is _BF16 and out.dtype is _BF16 and out.numel() == B * k * Hq * D and D == D_kv):
+        _refuse("deer_block_attn_quant", "q and out must be bf16 [B][k][Hq][D] of the cache's D")
+    if not (k_blk.dtype is _BF16 and v_blk.dtype is _BF16 and k_blk.numel() == v_blk.numel() == B * k * Hkv * D):
+        _refuse("deer_block_attn_quant", "k_blk and v_blk must be bf16 [B][k][Hkv][D] of the cache's Hkv")
+    if not (seq_ids.dtype is _I32 and seq_ids.numel() == B and (row_state is None or row_state.dtype is _I32 and row_state.numel() == B * k)):
+        _refuse("deer_block_attn_quant", "seq_ids must be int32 [B], row_state int32 [B][k]")
     _check(lib().deer_block_attn_quant(kv.handle, _ptr(seq_ids), _ptr(q), _ptr(k_blk), _ptr(v_blk), _ptr(out), _ptr(row_state), B, k, Hq,
                                        int(mask), float(scale), int(max_seq_len), _ptr(workspace),
                                        workspace.numel() * workspace.element_size() if workspace is not None else 0,
@@ -308,19 +329,35 @@ def deer_block_attn_quant(kv: KVCacheQuant, seq_ids, q, k_blk, v_blk, out, row_s
 
 def deer_rmsnorm_quant(x, gamma, codes, scales, eps, residual=None, total=None, stream=None):
     M, hid = x.shape
+    if not (x.dtype is _BF16 and gamma.dtype is _BF16 and gamma.numel() == hid and (residual is None or residual.dtype is _BF16 and residual.numel() == M * hid)
+            and (total is None or total.dtype is _BF16 and total.numel() == M * hid)):
+        _refuse("deer_rmsnorm_quant", "x, residual and total must be bf16 [M][hid], gamma bf16 [hid]")
+    if not (codes.dtype in _CODES and codes.numel() == M * hid and scales.dtype is _F32 and scales.numel() == M * ((hid + 127) // 128)):
+        _refuse("deer_rmsnorm_quant", "codes must be e4m3 [M][hid], scales f32 [M][ceil(hid / 128)]")
     _check(lib().deer_rmsnorm_quant(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(total), _ptr(codes), _ptr(scales), M, hid, float(eps),
                                     _stream(stream)))
 
 
 def deer_quantize(x, codes, scales, gated=False, stream=None):
     M, K = codes.shape
+    if not (x.dtype is _BF16 and x.numel() == M * K * (2 if gated else 1)):
+        _refuse("deer_quantize", "x must be bf16 [M][K], or [M][2 K] gated, of the codes' M and K")
+    if not (codes.dtype in _CODES and scales.dtype is _F32 and scales.numel() == M * ((K + 127) // 128)):
+        _refuse("deer_quantize", "codes must be e4m3 [M][K], scales f32 [M][ceil(K / 128)]")
     _check(lib().deer_quantize(_ptr(x), 1 if gated else 0, _ptr(codes), _ptr(scales), M, K, _stream(stream)))
 
 
 def deer_linear_quant(x, x_scale, w, w_scale, y, residual=None, stream=None):
     M, K = x.shape
-    _check(lib().deer_linear_quant(_ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(residual), _ptr(y), M, K, w.shape[0],
-                                   _stream(stream)))
+    N, K_w = w.shape
+    G = (K + 127) // 128
+    if not (x.dtype in _CODES and w.dtype in _CODES and K_w == K):
+        _refuse("deer_linear_quant", "x must be e4m3 [M][K], w e4m3 [N][K]")
+    if not (x_scale.dtype is _F32 and w_scale.dtype is _F32 and x_scale.numel() == M * G and w_scale.numel() == (N + 127) // 128 * G):
+        _refuse("deer_linear_quant", "x_scale must be f32 [M][ceil(K / 128)], w_scale f32 [ceil(N / 128)][ceil(K / 128)]")
+    if not (y.dtype is _BF16 and y.numel() == M * N and (residual is None or residual.dtype is _BF16 and residual.numel() == M * N)):
+        _refuse("deer_linear_quant", "y and residual must be bf16 [M][N]")
+    _check(lib().deer_linear_quant(_ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(residual), _ptr(y), M, K, N, _stream(stream)))
 
 
 def deer_kv_reserve(kv: KVCache, seq_ids: torch.Tensor, k: int, stream=None) -> None:
