@@ -196,7 +196,7 @@ class KVCache:
         self.desc = deer_kv_desc(_ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(seq_len), _ptr(n_pages),
                                  _ptr(free_stack), _ptr(free_top), _ptr(self.status),
                                  num_pages, Hkv, D, page, page_table.shape[0], page_table.shape[1])
-        self.handle = c_void_p()
+        self.handle, self._heads = c_void_p(), (Hkv, D)
 
     @classmethod
     def from_layout(cls, layout, k_pool, v_pool, device="cuda"):
@@ -240,7 +240,6 @@ class KVCacheQuant(KVCache):
         assert k_tail.dtype == v_tail.dtype == torch.bfloat16
         self._describe(k_pool, v_pool, page_table, seq_len, n_pages, free_stack, free_top)
         self.k_scale, self.v_scale, self.k_tail, self.v_tail = k_scale, v_scale, k_tail, v_tail
-        self._heads = Hkv, D
         quant = deer_kv_quant_desc(_ptr(k_scale), _ptr(v_scale), _ptr(k_tail), _ptr(v_tail))
         _check(lib().deer_kv_create_quant(ctypes.byref(self.handle), ctypes.byref(self.desc), ctypes.byref(quant)))
 

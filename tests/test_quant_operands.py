@@ -62,3 +62,15 @@ def test_store_and_attention_operands(L):
     _refused(L, L.deer_block_attn_quant, good, dict(
         seq_ids=[z(2, dtype=I32), z(3, dtype=torch.int64)], q=[z(3, 5, 4, 128), z(3, 5, 4, 64, dtype=F32)], k_blk=[other, z(3, 4, 2, 64), rows.float()],
         v_blk=[other, z(3, 4, 2, 64), rows.float()], out=[z(3, 5, 2, 64), z(3, 5, 4, 64, dtype=F32)], row_state=[z(3, 4, dtype=I32), z(3, 5, dtype=torch.int64)]))
+
+
+def test_a_bf16_cache_is_the_librarys_to_refuse(L):
+    i32 = lambda *shape: z(*shape, dtype=I32)
+    kv = L.KVCache(z(8, 2, 16, 64), z(8, 2, 16, 64), i32(3, 4), i32(3), i32(3), i32(8), i32(1))
+    rows, ids = z(3, 5, 2, 64), i32(3)
+    with pytest.raises(L.DeerError) as e:
+        L.deer_kv_store(kv, ids, rows, rows, stream=1)
+    assert e.value.code == L.DEER_ERR_UNSUPPORTED
+    with pytest.raises(L.DeerError) as e:
+        L.deer_block_attn_quant(kv, ids, z(3, 5, 4, 64), rows, rows, z(3, 5, 4, 64), None, L.DEER_MASK_CAUSAL, 0.125, 48, i32(1 << 16), stream=1)
+    assert e.value.code == L.DEER_ERR_UNSUPPORTED
