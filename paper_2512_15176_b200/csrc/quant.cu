@@ -1,8 +1,8 @@
 // The row-wise quantisers of the 8-bit verifier layer -- residual + RMSNorm, a plain copy, the SiLU gate, each with
 // e4m3 codes and one scale per 128 columns as output -- and the store of a step's kept rows into an 8-bit paged cache.
 // All are one pass over their data.  With few rows a launch and two dependent memory round trips bound them (32 x 4096
-// normalised 2.1 us, copied 1.3 us, the store of 16 blocks 3.2 us); with many the bytes, and close behind them the
-// instructions (2048 x 4096 normalised 11.6 us = 5.0 TB/s; 512 x 12288 gated 8.1 us = 3.9 TB/s; four prompts' store
+// normalised 2.2 us, copied 1.3 us, the store of 16 blocks 3.2 us); with many the bytes, and close behind them the
+// instructions (2048 x 4096 normalised 12.1 us = 4.9 TB/s; 512 x 12288 gated 8.1 us = 3.9 TB/s; four prompts' store
 // 14.9 us = 3.8 TB/s).
 
 #include "quant.cuh"
@@ -10,6 +10,26 @@
 namespace quant {
 
 using namespace sm100;
+
+// 1 / rms of a row whose squares fp32 does not hold, from the squares of its values times `by`, a power of two.  By all threads
+// of the block.  (Out of line, and from memory: with the row's registers kept for it 2048 x 4096 took 13.7 us, like this 12.2, without 11.8.)
+__device__ __noinline__ float inverse_rms_of_far_row(const __nv_bfloat16* x, const __nv_bfloat16* residual, int hid, float eps, float by, float* part) {
+    float ss = 0.f;
+#pragma unroll 1
+    for (int c = threadIdx.x; c < hid; c += blockDim.x) {
+        const float v = (__bfloat162float(x[c]) + (residual ? __bfloat162float(residual[c]) : 0.f)) * by;
+        ss = fmaf(v, v, ss);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    __syncthreads();                                               // (everyone has the first sum)
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = ss;
+    __syncthreads();                                               // (and has read the row: `total` may be it)
+    ss = 0.f;
+#pragma unroll 1
+    for (int w = 0; w < blockDim.x / 32; ++w) ss += part[w];
+    return rsqrtf(ss / (float)hid + eps * by * by) * by;
+}
 
 // y = (x + residual) / rms * gamma per row.  A thread keeps its columns, CHUNKS pieces of 8, in registers between the two
 // phases -- the sum of squares over the row, the codes of the sixteen-lane groups -- so a row is read once; with one or two
@@ -56,7 +76,6 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) ss2 = fma2(h[c].p[j], h[c].p[j], ss2);
-        if (total && col < hid) *reinterpret_cast<uint4*>(total + row * hid + col) = to_bf16(h[c]);
     }
     float ss, ss_hi;
     unpack_f32x2(ss2, ss, ss_hi);
@@ -68,13 +87,16 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_quant_kernel(const __nv_bfloa
     float tot = 0.f;
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) tot += part[w];
-    const float inv = rsqrtf(tot / (float)hid + eps);
+    float inv = rsqrtf(tot / (float)hid + eps);
+    if (!(tot < 1e36f) || (tot < 1e-24f && eps < 1e-24f))
+        inv = inverse_rms_of_far_row(x_row, r_row, hid, eps, tot < 1.f ? 1.26765060e30f : 7.88860905e-31f, part);       // 2^100, 2^-100
     const uint64_t inv2 = pack_f32x2(inv, inv);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int col = (c * THREADS + tid) * 8;
         if (c * THREADS * 8 >= hid) break;
         if (!EARLY) gv[c] = piece(gamma, c);
+        if (total && col < hid) *reinterpret_cast<uint4*>(total + row * hid + col) = to_bf16(h[c]);
         const V8 g = unpack8(gv[c]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[c].p[j] = mul2(mul2(h[c].p[j], inv2), g.p[j]);

@@ -7,7 +7,7 @@ import torch
 
 from oracle import deer_oracle as O
 from paper_2512_15176_b200 import workload as W
-from tests.test_gpu_quant import F8, _cache, _ids, check_attention, f64
+from tests.test_gpu_quant import F8, _cache, _ids, check_attention, check_codes, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -79,6 +79,33 @@ def test_gated_groups_of_zeros_nan_and_infinities():
         assert not np.isfinite(got[m, g * 128:(g + 1) * 128] * s[m, g]).any()
         got[m, g * 128:(g + 1) * 128], s[m, g], y[m, g * 128:(g + 1) * 128] = 0.0, 2.0 ** -126, 0.0
     _check_gated(got, s, y, "the other groups")
+
+
+@pytest.mark.parametrize("K", [64, 2064, 4096, 8208, 20000])
+def test_rows_whose_squares_leave_fp32(K):
+    """Rows so large, or with eps 0 so small, that the sum of their squares is beyond fp32: the normalised row is an ordinary one."""
+    from paper_2512_15176_b200 import binding as L
+    M, G = 8, -(-K // 128)
+    x, g = W.normal(453, "x", (M, K), 1.0), W.normal(453, "g", (K,), 1.0)
+    x[0] *= 2.0 ** 62
+    x[1] *= 2.0 ** 70
+    x[2] *= 2.0 ** 124
+    x[3, 7] = torch.finfo(torch.bfloat16).max
+    x[4] *= 2.0 ** -40
+    x[5] *= 2.0 ** -75
+    x[6] *= 2.0 ** -115
+    r = torch.zeros_like(x)
+    r[3] = W.normal(453, "r", (1, K), 1.0)[0] * 2.0 ** 115
+    for eps, rows, res in ((1e-6, [0, 1, 2, 3, 7], True), (0.0, list(range(M)), False)):
+        codes, scales = torch.empty(M, K, dtype=F8, device="cuda"), torch.empty(M, G, device="cuda")
+        dev = x.cuda()
+        tot = torch.empty_like(dev) if res else dev        # (in place as well)
+        L.deer_rmsnorm_quant(dev, g.cuda(), codes, scales, eps, residual=r.cuda() if res else None, total=tot)
+        h = f64(x) + (f64(r) if res else 0.0)
+        with np.errstate(over="ignore"):
+            h32 = h.astype(np.float32)
+        assert (f64(tot) == f64(torch.from_numpy(h32).to(torch.bfloat16))).all()
+        check_codes(codes[rows], scales[rows], O.rmsnorm(h[rows], f64(g), eps), 2e-6, f"eps {eps}")
 
 
 def _attend(kv, q, kb, vb, msl, mask=0, states=None):
