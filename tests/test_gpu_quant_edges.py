@@ -81,7 +81,7 @@ def test_gated_groups_of_zeros_nan_and_infinities():
     _check_gated(got, s, y, "the other groups")
 
 
-@pytest.mark.parametrize("K", [64, 2064, 4096, 8208, 20000])
+@pytest.mark.parametrize("K", [64, 1040, 4096, 6000, 8208, 20000])
 def test_rows_whose_squares_leave_fp32(K):
     """Rows so large, or with eps 0 so small, that the sum of their squares is beyond fp32: the normalised row is an ordinary one."""
     from paper_2512_15176_b200 import binding as L
@@ -211,3 +211,19 @@ def test_tail_and_block_rows_of_very_different_size(k, Hq, Hkv, long):
     kv.k_tail.copy_(torch.from_numpy(okv.tail[0]).to(torch.bfloat16))
     kv.v_tail.copy_(torch.from_numpy(okv.tail[1]).to(torch.bfloat16))
     check_attention(_attend(kv, q, kb, vb, 1 << 20 if long else n), q, kb, vb, okv, [0], 0, 1 / math.sqrt(D), None, "sizes")
+
+
+@BOUNDS
+@pytest.mark.parametrize("k,Hq,Hkv", [(32, 8, 2), (4, 4, 2)])
+@pytest.mark.parametrize("which,bad", [("k_scale", float("nan")), ("v_scale", float("nan")), ("v_scale", float("inf"))])
+def test_a_page_scale_that_is_not_finite(which, bad, k, Hq, Hkv, long):
+    """Every row of the page's head sees the page, and no row of another head does."""
+    kv, okv = _cache([330], Hkv, 128, 0, 464)
+    q, kb, vb = _block(464, k, Hq, Hkv)
+    getattr(kv, which)[int(okv.page_table[0, 9]), 1] = bad
+    out = _attend(kv, q, kb, vb, 1 << 20 if long else 330)
+    G = Hq // Hkv
+    assert not out[:, :, G:].isfinite().any()
+    fine = [t[:, :, :1] for t in (kb, vb)]
+    one = O.QuantKV(*[c[:, :1] for c in okv.codes], *[c[:, :1] for c in okv.scale], *[c[:, :1] for c in okv.tail], okv.page_table, okv.seq_len)
+    check_attention(out[:, :, :G], q[:, :, :G], *fine, one, [0], 0, 1 / math.sqrt(128), None, which)
