@@ -460,15 +460,16 @@ int deer_moe_mlp(const void* x, const void* w_router, const void* w_gate_up, con
  * deer_rmsnorm_quant: h = x + residual (residual may be NULL: h = x);
  *   codes, scales of y = h / sqrt(mean(h^2) + eps) * gamma;  total = h in bf16.
  *   x, residual, total bf16 [M][hid]; gamma bf16 [hid]; codes e4m3 [M][hid]; scales f32 [M][ceil(hid / 128)].
- *   total may be NULL; it may be x or residual itself.  fp32 throughout: y is taken from the unrounded h and
- *   rounded once, to its code.  hid a multiple of 16, at most 65536.
+ *   total may be NULL; it may be x or residual itself.  fp32 throughout, for finite h of any size: y is taken from the
+ *   unrounded h and rounded once, to its code.  hid a multiple of 16, at most 65536.
  * deer_quantize: codes, scales of x bf16 [M][K] (gated = 0), or of silu(x[m][c]) * x[m][K + c], x bf16 [M][2 K]
- *   (gated = 1).  K a multiple of 16.
+ *   (gated = 1), for finite x of any size (a product beyond fp32 is an infinity).  K a multiple of 16.
  * deer_linear_quant: y[m][n] = sum_c x[m][c] w[n][c] (+ residual[m][n]) of the values that codes and scales stand for.
  *   x e4m3 [M][K], x_scale f32 [M][ceil(K / 128)]; w e4m3 [N][K], w_scale f32 [ceil(N / 128)][ceil(K / 128)];
  *   residual, y bf16 [M][N] (residual may be NULL or y itself).  K and N multiples of 16, at least 16; M, K, N <= 2^30.
  *   Products and the sums over 128 columns come from the tensor cores' fp32 accumulator; the scaled sums over the
- *   column groups are fp32.  No workspace.
+ *   column groups are fp32.  No workspace.  (As deer_linear: a thread block whose bounded wait runs out leaves its
+ *   output tiles unwritten; the call has no status word of its own.)
  * ---------------------------------------------------------------------- */
 int deer_rmsnorm_quant(const void* x, const void* residual, const void* gamma, void* total, void* codes, float* scales,
                        int M, int hid, float eps, void* stream);
@@ -499,10 +500,11 @@ int deer_kv_create_quant(deer_kv** kv, const deer_kv_desc* desc, const deer_kv_q
 /* The rows that a step keeps enter an 8-bit cache: rows 0 .. keep[b] - 1 of k_rows / v_rows bf16 [B][k][Hkv][D] become
  * the tokens seq_len[s] .. of sequence s = seq_ids[b] (keep clamped to [0, k]; NULL keeps all k).  Pages that become
  * full are quantised, the tokens behind them become tail rows.  seq_len is NOT changed: call deer_kv_commit (or
- * deer_kv_commit_rows) with the same keep afterwards, once for all layers that share the integer state.  The pages
- * must be mapped (deer_kv_reserve).  k is not limited to a draft block: a prompt enters with one call.  seq_ids
- * distinct.  Repeating a call before the commit gives the same cache again if k <= 32, or if seq_len is a multiple
- * of 16 (a longer run that starts inside a page may end on tail rows that it read).
+ * deer_kv_commit_rows) with the same keep afterwards, once for all layers that share the integer state.  (So the
+ * acceptance is a call of its own, deer_accept: deer_accept_commit moves seq_len in the launch that finds accept_len, and
+ * leaves no place for the store between.)  The pages must be mapped (deer_kv_reserve).  k is not limited to a draft block: a
+ * prompt enters with one call.  seq_ids distinct.  Repeating a call before the commit gives the same cache again if k <= 32, or
+ * if seq_len is a multiple of 16 (a longer run that starts inside a page may end on tail rows that it read).
  * Errors: the status word as deer_kv_commit (DEER_ERR_BAD_PAGE: a page that becomes full is not mapped; it is skipped). */
 int deer_kv_store(deer_kv* kv, const int32_t* seq_ids, const void* k_rows, const void* v_rows, const int32_t* keep, int B, int k,
                   void* stream);
@@ -515,8 +517,9 @@ int deer_kv_commit_rows(deer_kv* kv, const int32_t* seq_ids, const int32_t* keep
  * full pages (codes times their page's scale), the tail rows, and the block rows that mask and row_state allow.
  * row_state: bidirectional mask only, or NULL; the output rows of absent positions are zero.  Scores and probabilities:
  * fp32; queries, and the keys that are bf16, enter exactly down to 2^-9 of their row's largest magnitude and to an absolute
- * error of 2^-17 of that below it; probabilities enter the second product rounded to 11 bits.  What a row does not see has no
- * part in its result: a NaN, an infinity or a finite value of any size in a key or value row reaches only the rows that see it.
+ * error of 2^-17 of that below it (an infinity among them may count as a NaN); probabilities enter the second product rounded
+ * to 11 bits, those below 2^-24 of the largest to 2^-35 of it.  What a row does not see has no part in its result: a NaN, an
+ * infinity or a finite value of any size in a key or value row reaches only the rows that see it.
  *   workspace  >= deer_block_attn_quant_workspace_bytes(...) bytes, 16-byte aligned, contents arbitrary; one call at a
  *              time per workspace. */
 size_t deer_block_attn_quant_workspace_bytes(int B, int k, int Hq, int Hkv, int D, int max_seq_len);

@@ -14,9 +14,10 @@
 // own, and meet in shared memory at the end.  A context is cut into chunks over thread blocks; up to eight of them form
 // a cluster and meet in its shared memory, and where a context has more a second kernel joins the clusters' parts.
 //
-// What bounds it: latencies in short contexts (one token, 32 query and 8 KV heads, over 1003: 7.8 us, two pages per warp,
+// What bounds it: latencies in short contexts (one token, 32 query and 8 KV heads, over 1003: 8.0 us, two pages per warp,
 // most of it the chain length -> page number -> page -> products -> meeting in the cluster), the instructions of a page
-// (about 400 a warp, and their latencies) in long ones: 16 x 4096 tokens 44.4 us = 3.1 TB/s.
+// (about 400 a warp, and their latencies) in long ones: 16 x 4096 tokens 44.4 us = 3.0 TB/s, one token over 32768 29.5 us; and, for many rows over heads of 64, that each 16 of them read the pages again (16 x 32 rows,
+// 32 query and 4 KV heads of 64, 2048 to 16384 tokens 305 us).
 
 #include <cuda_fp16.h>
 

@@ -29,10 +29,11 @@
 // All waits are bounded: one that runs out raises the block's abort flag and the cache's status word, and every role leaves.
 //
 // What bounds it: not a unit but the way of a tile through the roles (16 ragged sequences of 2048 to 16384 tokens, 32 query
-// and 4 KV heads, 32 rows: 112 us, 0.9 us a tile and block, where its MMAs take 0.45, its exponentials 0.27 and its bytes
-// 0.2).  Taking away half of any one role's work changes the time by 5 % at most; the four score buffers that tensor memory
-// has room for are what is in flight.  32 rows over 4096 tokens, 8 KV heads: 22 us, 27000 cycles of them in a block: 9000
-// until the queries are there, 4500 on their terms, 7500 on four tiles, 6000 on joining.
+// and 4 KV heads, 32 rows: 113 us in a graph of twenty calls, 119 to 122 in a long row of calls; 0.9 us a tile and block, where
+// its MMAs take 0.45, its exponentials 0.27 and its bytes 0.2).  Taking away half of any one role's work changes the time by
+// 5 % at most; the four score buffers that tensor memory has room for are what is in flight.  32 rows over 4096 tokens, 8 KV
+// heads: 22.5 us (23 in a row of calls), 27000 cycles of them in a block: 9000 until the queries are there, 4500 on their terms,
+// 7500 on four tiles, 6000 on joining.
 
 #include <cfloat>
 #include <cuda_fp16.h>
@@ -103,6 +104,7 @@ struct Shared {                                // behind the operand buffers
     Seg segs[MAX_SEGS];
 };
 constexpr int SMEM_BYTES = 2 * Q_BYTES + NK * T_BYTES + 8 * VR_BYTES + NVH * VH_BYTES + BT_BYTES + 1024 + (int)sizeof(Shared);
+static_assert(SMEM_BYTES <= 227 * 1024, "a block's shared memory");
 
 struct QParams {
     AttnParams a;
@@ -435,35 +437,33 @@ attn_quant_umma_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 float ks_next = scale_of(qp.kq.k_scale, id_next), vs_next = scale_of(qp.kq.v_scale, id_next);
                 const int t_end = min(g.t_b, last_tile);
                 for (int t = g.t_a; t < t_end; ++t) {
-                    if (t < t_end) {
-                        const int sl = rs % NK, at = (t - g.t_a) & 7;
-                        if (at == 0 && t != g.t_a) {
-                            id_cur = id_next;
-                            ks_cur = ks_next;
-                            vs_cur = vs_next;
-                            id_next = id_third;
-                            ks_next = scale_of(qp.kq.k_scale, id_next);
-                            vs_next = scale_of(qp.kq.v_scale, id_next);
-                            id_third = ids_at(t + 16);
-                        }
-                        float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3));
-                        const float vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
-                        if (!(fabsf(vs) < INFINITY)) ks = NAN;             // makes every row that sees the page NaN, as vs would
-                        int oks = 1;
-                        if (lane == 0) oks = wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
-                        if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
-                        if (lane < 3 * PAGES) sh.scales[rs % NSCALE][lane] = lane < PAGES ? ks : lane < 2 * PAGES ? vs : __log2f(vs);
-                        __syncwarp();
-                        if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);      // (the arrival publishes the scales as well)
-                        __syncwarp();
-                        const int pg = __shfl_sync(0xffffffffu, id_cur, at * PAGES + (lane & 3));
-                        if (lane < 4) {
-                            const bool there = pg >= 0 && pg < p.kv.num_pages;
-                            if (!there && pg != -2) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
-                            tma_load_2d(ring_addr + sl * T_BYTES + lane * PAGE * HD, &tm_k, 0, there ? (pg * Hkv + kvh) * PAGE : no_row, bar(BAR_K_FULL + sl));
-                        }
-                        ++rs;
+                    const int sl = rs % NK, at = (t - g.t_a) & 7;
+                    if (at == 0 && t != g.t_a) {
+                        id_cur = id_next;
+                        ks_cur = ks_next;
+                        vs_cur = vs_next;
+                        id_next = id_third;
+                        ks_next = scale_of(qp.kq.k_scale, id_next);
+                        vs_next = scale_of(qp.kq.v_scale, id_next);
+                        id_third = ids_at(t + 16);
                     }
+                    float ks = __shfl_sync(0xffffffffu, ks_cur, at * PAGES + (lane & 3));
+                    const float vs = __shfl_sync(0xffffffffu, vs_cur, at * PAGES + (lane & 3));
+                    if (!(fabsf(vs) < INFINITY)) ks = NAN;             // makes every row that sees the page NaN, as vs would
+                    int oks = 1;
+                    if (lane == 0) oks = wait(bar(BAR_K_EMPTY + sl), ((uint32_t)(rs / NK) & 1u) ^ 1u, abort_flag) ? 1 : 0;
+                    if (!__shfl_sync(0xffffffffu, oks, 0)) { ok = false; break; }
+                    if (lane < 3 * PAGES) sh.scales[rs % NSCALE][lane] = lane < PAGES ? ks : lane < 2 * PAGES ? vs : __log2f(vs);
+                    __syncwarp();
+                    if (lane == 0) mbar_expect_tx(bar(BAR_K_FULL + sl), T_BYTES);      // (the arrival publishes the scales as well)
+                    __syncwarp();
+                    const int pg = __shfl_sync(0xffffffffu, id_cur, at * PAGES + (lane & 3));
+                    if (lane < 4) {
+                        const bool there = pg >= 0 && pg < p.kv.num_pages;
+                        if (!there && pg != -2) deer_report(p.kv.status, DEER_ERR_BAD_PAGE);
+                        tma_load_2d(ring_addr + sl * T_BYTES + lane * PAGE * HD, &tm_k, 0, there ? (pg * Hkv + kvh) * PAGE : no_row, bar(BAR_K_FULL + sl));
+                    }
+                    ++rs;
                 }
             }
         } else if (warp == 3) {

@@ -10,8 +10,11 @@
 //
 // What bounds it.  Few rows: the weight bytes (one row, 4096 x 4096, 6.8 us, 2.6 of them HBM's; 32 rows, 12288 x 4096,
 // 13.3 us = 3.9 TB/s, 7.8 HBM's): the loads run at HBM's rate, the rest is the first tile's latency (1.5 us), the cluster's
-// meeting (2 us) and a launch.  Many rows (512 x 4096 x 24576, 55 us = 1.86 PFLOP/s, twice the bf16 rate would take 31):
-// the way of an accumulator from the MMAs through the epilogue and back, which tensor memory can hold only 512 columns of.
+// meeting (2 us) and a launch.  Many rows (512 x 4096 x 24576, 56 us = 1.85 PFLOP/s in a graph of twenty calls, 64 to 66 us
+// in a long row of calls, where power caps the clock; twice the bf16 rate would take 31): the epilogue.  A column group takes
+// it about 1100 cycles with 256 weight rows and 0.57 of that with 128, so about 120 for 16 columns and 150 for a hand-over: the
+// tensor-memory load of the next 16 columns is under way while eight multiply-adds scale the present ones, which does not cover
+// its latency, and the registers (168, of which 128 are sums; the form for 256 weight rows spills two) hold no more loads.
 //
 // Few output columns do not fill the SMs, so a cluster of `split` blocks shares an output tile, each with a range of
 // the column groups.  Every block of the cluster owns a part of the tile's rows of x: the others send it their partial sums
@@ -260,7 +263,7 @@ linear_quant_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         if (warp >= 2 && !*abort_flag) {
             bool ok = true;
             for (int r = 0; r < a.split; ++r) ok = ok && whole[r * C::EPI_WARPS + (warp & 3)] != 0u;
-#pragma unroll 1                                                   // (code that runs once waits for its fetching: 64 x 1024 x 1024 9.2 us unrolled, 8.3)
+#pragma unroll 1                                                   // (code that runs once waits for its fetching: 64 x 2048 x 4096 9.0 us unrolled, 8.8)
             for (int j = 0; j < own_rows && own0 + j < a.M && ok; j += 4) {
                 if (j > 0) fetch_residual(own0 + j);
                 float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -513,6 +516,7 @@ static int operand_maps(CUtensorMap* tm_w, CUtensorMap* tm_x, const Args& a, con
 template <int BNP>
 int launch_pair(Args a, const void* x, const void* w, cudaStream_t st) {
     using C = PairCfg<BNP>;
+    static_assert(C::SMEM <= 227 * 1024, "a block's shared memory");
     CUtensorMap tm_w, tm_x;
     const int rc = operand_maps(&tm_w, &tm_x, a, w, x, C::HALF, 128);
     if (rc != DEER_OK) return rc;
@@ -528,6 +532,7 @@ int launch_pair(Args a, const void* x, const void* w, cudaStream_t st) {
 template <int NT>
 int launch(Args a, const void* x, const void* w, cudaStream_t st) {
     using C = Cfg<NT>;
+    static_assert(2 * (C::SMEM + 1024) <= 228 * 1024, "two blocks (each with a system kilobyte) on an SM");
     CUtensorMap tm_w, tm_x;
     const int rc = operand_maps(&tm_w, &tm_x, a, w, x, BN, NT);
     if (rc != DEER_OK) return rc;

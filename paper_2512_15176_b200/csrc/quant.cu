@@ -2,7 +2,7 @@
 // e4m3 codes and one scale per 128 columns as output -- and the store of a step's kept rows into an 8-bit paged cache.
 // All are one pass over their data.  With few rows a launch and two dependent memory round trips bound them (32 x 4096
 // normalised 2.2 us, copied 1.3 us, the store of 16 blocks 3.2 us); with many the bytes, and close behind them the
-// instructions (2048 x 4096 normalised 12.1 us = 4.9 TB/s; 512 x 12288 gated 8.1 us = 3.9 TB/s; four prompts' store
+// instructions (2048 x 4096 normalised 12.1 us = 4.9 TB/s; 512 x 12288 gated 8.2 us = 3.9 TB/s; four prompts' store
 // 14.9 us = 3.8 TB/s).
 
 #include "quant.cuh"
@@ -293,7 +293,7 @@ extern "C" int deer_rmsnorm_quant(const void* x, const void* residual, const voi
     else if (hid <= 4096) DEER_CUDA(run(rmsnorm_quant_kernel<256, 2>, 256));
     else if (hid <= 8192) DEER_CUDA(run(rmsnorm_quant_kernel<512, 2>, 512));
     else if (hid <= 16384) DEER_CUDA(run(rmsnorm_quant_kernel<512, 4>, 512));
-    else DEER_CUDA(run(rmsnorm_quant_kernel<1024, 8>, 1024));
+    else DEER_CUDA(run(rmsnorm_quant_kernel<1024, 8>, 1024));      // (64 values a thread spill: 512 x 20000 33.8 us, 512 x 16384 16.0)
     return DEER_OK;
 }
 

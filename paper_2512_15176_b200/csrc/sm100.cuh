@@ -229,8 +229,7 @@ __device__ __forceinline__ uint32_t make_idesc_e4m3_pair(int n) { return (1u << 
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])         \
                  : "memory")
 
-// Two fp32 at once: acc += r * s, both halves.  (Volatile: the operands come from tensor memory, whose loads are complete
-// only after tmem_wait_ld, an ordering the compiler cannot see in the registers.)
+// Two fp32 at once.
 __device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
     uint64_t v;
     asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
@@ -254,6 +253,8 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
 }
+// acc += r * s, both halves.  (Volatile: the operands come from tensor memory, whose loads are complete only after
+// tmem_wait_ld, an ordering the compiler cannot see in the registers.)
 __device__ __forceinline__ void fma_f32x2(uint64_t& acc, uint32_t r_lo, uint32_t r_hi, uint64_t s) {
     asm volatile("{\n\t.reg .b64 r;\n\tmov.b64 r, {%1, %2};\n\tfma.rn.f32x2 %0, r, %3, %0;\n\t}" : "+l"(acc) : "r"(r_lo), "r"(r_hi), "l"(s));
 }
@@ -280,7 +281,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 __device__ __forceinline__ void mbar_arrive_peer(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// All threads of both CTAs.
+// Loads from and stores to the shared memory of a block of the cluster.
 __device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
     float v;
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
@@ -298,6 +299,7 @@ __device__ __forceinline__ void st_cluster_f32x4(uint32_t cluster_addr, float x,
 // The two halves of cluster_sync(), for work between them.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// All threads of all blocks of the cluster.
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
