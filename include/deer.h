@@ -529,6 +529,56 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * (8) Training the drafter's LM head: the losses that decide how often its drafts are accepted, as calls beside
+ * deer_lmhead_select.  z = h w^T over the whole vocabulary is reduced on the fly and never stored.
+ *
+ * deer_lmhead_loss: softmax cross entropy at the rows that have a target (Eq. 1-2: the masked positions, row_weight
+ *   1 / t; Eq. 3-4: the last R tokens of an answer, row_weight alpha^(R - i)),
+ *       loss[m] = row_weight[m] (logsumexp(z[m]) - z[m][targets[m]]).
+ * deer_lmhead_distill: the Kullback-Leibler divergence from a teacher that is known by its top logits (deer_top_logits
+ *   of the verifier's rows).  A row's list is ids[m][0 ..], ended by K or by the first negative id; t = softmax(teacher /
+ *   temperature) over the list (an entry of -inf has probability 0; an id that is listed twice has the sum), p =
+ *   softmax(z / temperature) over the vocabulary:
+ *       loss[m] = row_weight[m] temperature^2 sum_j t_j (log t_j - log p[ids_j]).
+ * Rows without a target (targets[m] < 0, ids[m][0] < 0) or with row_weight 0 are dead: loss, lse, target_logit and
+ *   gradient 0; what h holds there is not used, and they cost nothing (the live rows are moved together first).  A list
+ *   whose entries are all -inf has loss and gradient 0.  An id of V or more makes its row's loss NaN and its gradient 0.
+ * The *_grad calls return the gradients of sum_m grad_loss[m] loss[m]:
+ *       dh = G w,  dw = G^T h,  G[m][v] = row_weight[m] grad_loss[m] temperature (p[m][v] - t[m][v]),
+ *   from the same inputs and the forward call's lse and target_logit.  z is computed a second time, in pieces of the
+ *   vocabulary; G is rounded to bf16 for the two products (p - t of a listed token is formed in fp32), all sums are fp32
+ *   and in a fixed order: the same inputs give the same bits.
+ *   h             bf16 [M][hid];  w bf16 [V][hid];  hid a multiple of 64, at most 65536;  M <= 2^18, V <= 2^30
+ *   targets       i32 [M];  ids i32 [M][K], teacher f32 [M][K], K <= 128;  temperature > 0
+ *   row_weight    f32 [M] or NULL (1);  grad_loss f32 [M] or NULL (1)
+ *   loss, lse     f32 [M]      out: the loss;  logsumexp(z / temperature)
+ *   target_logit  f32 [M][K] (K = 1: [M])  out: z at the listed tokens, 0 behind a list's end
+ *   dh bf16 [M][hid], dw bf16 [V][hid]     out, overwritten; either may be NULL
+ *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls), 16-byte
+ *                 aligned, contents arbitrary, nothing kept in it between calls; one call at a time per workspace.
+ * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).
+ * A bounded wait that runs out makes the call's losses, or dh, NaN. */
+size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad);
+int deer_lmhead_loss(const void* h, const void* w, const int32_t* targets, const float* row_weight, int M, int hid, int V,
+                     float* loss, float* lse, float* target_logit, void* workspace, size_t workspace_bytes, void* stream);
+int deer_lmhead_loss_grad(const void* h, const void* w, const int32_t* targets, const float* row_weight, const float* grad_loss,
+                          const float* lse, const float* target_logit, int M, int hid, int V, void* dh, void* dw,
+                          void* workspace, size_t workspace_bytes, void* stream);
+int deer_lmhead_distill(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
+                        const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int deer_lmhead_distill_grad(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
+                             const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit,
+                             int M, int hid, int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The K largest logits of each row, falling, the lowest index first among equals: what a teacher's row leaves for
+ * deer_lmhead_distill (deer_lmhead_select's out_logits of the verifier, or any fp32 rows).
+ *   logits f32 [M][V];  ids i32 [M][K], values f32 [M][K] out;  1 <= K <= 128, M <= 2^24, V <= 2^30
+ * A NaN ranks below -inf (and comes out as the NaN it is), -0 as 0.  K > V: ids -1 and values -inf behind the V-th entry.
+ * No workspace. */
+int deer_top_logits(int M, int V, const float* logits, int K, int32_t* ids, float* values, void* stream);
+
+/* ------------------------------------------------------------------------
  * One whole greedy verify step with HOST inputs and outputs (Algorithm 1, one
  * iteration of the while loop on the verifier side): copies the block's
  * q/k_blk/v_blk, hidden states and draft ids from host memory to the device

@@ -687,3 +687,81 @@ def quant_block_attention(q, k_blk, v_blk, qkv, seq_ids, mask, scale, row_state=
                                     np.array([n]), [0], mask, scale, page_size=max(n, 1),
                                     row_state=None if row_state is None else row_state[b:b + 1]))
     return np.concatenate(outs)
+
+
+# --------------------------------------------------------------------------
+# training the drafter's LM head (Eq. 1-4: weighted cross entropy; distillation from top logits)
+# --------------------------------------------------------------------------
+
+def head_targets(ids, V, teacher=None, temperature=1.0):
+    """Rows' targets as dense distributions [M, V] and which rows have one.  ids [M, K]: a row's list ends at its first
+    negative id; teacher [M, K]: softmax(teacher / temperature) over the list, None: all of it on the (single) entry."""
+    M, K = ids.shape
+    t, live = np.zeros((M, V)), np.zeros(M, dtype=bool)
+    for m in range(M):
+        n = 0
+        while n < K and ids[m, n] >= 0:
+            n += 1
+        if n == 0:
+            continue
+        live[m] = True
+        if teacher is None:
+            p = np.ones(n)
+        else:
+            u = np.asarray(teacher[m, :n], dtype=np.float64) / temperature
+            if np.all(u == -np.inf):
+                continue                                       # no distribution: neither loss nor gradient
+            p = np.exp(u - u.max())
+            p = p / p.sum()
+        for j in range(n):
+            t[m, ids[m, j]] += p[j]
+    return t, live
+
+
+def head_loss(h, w, ids, teacher=None, temperature=1.0, row_weight=None):
+    """loss [M], lse [M], p [M, V], t [M, V] and which rows count: row_weight tau^2 KL(t || softmax(h w^T / tau))."""
+    z = h @ w.T / temperature
+    M, V = z.shape
+    a = np.ones(M) if row_weight is None else np.asarray(row_weight, dtype=np.float64)
+    t, live = head_targets(ids, V, teacher, temperature)
+    live = live & (a != 0)
+    top = z.max(axis=1, keepdims=True)
+    lse = (top + np.log(np.exp(z - top).sum(axis=1, keepdims=True)))[:, 0]
+    # an entry's own t enters its logarithm, not the sum over a repeated id
+    loss = np.zeros(M)
+    for m in np.nonzero(live)[0]:
+        n = 0
+        while n < ids.shape[1] and ids[m, n] >= 0:
+            n += 1
+        u = np.zeros(n) if teacher is None else np.asarray(teacher[m, :n], dtype=np.float64) / temperature
+        if np.all(u == -np.inf):
+            continue
+        log_t = u - u.max()
+        log_t = log_t - np.log(np.exp(log_t).sum()) if teacher is not None else u
+        for j in range(n):
+            if log_t[j] > -np.inf:
+                loss[m] += np.exp(log_t[j]) * (log_t[j] - z[m, ids[m, j]] + lse[m])
+        loss[m] *= a[m] * temperature ** 2
+    return loss, np.where(live, lse, 0.0), np.exp(z - lse[:, None]), t, live
+
+
+def head_loss_grad(h, w, ids, teacher=None, temperature=1.0, row_weight=None, grad_loss=None):
+    """dh [M, hid], dw [V, hid] of sum(grad_loss * loss), and G = d/d(h w^T)."""
+    M = h.shape[0]
+    _, _, p, t, live = head_loss(h, w, ids, teacher, temperature, row_weight)
+    c = (1.0 if row_weight is None else row_weight) * (1.0 if grad_loss is None else grad_loss) * temperature * live * (t.sum(axis=1) > 0)
+    G = np.where(np.broadcast_to(np.asarray(c)[:, None], p.shape) != 0, (p - t) * np.asarray(c)[:, None], 0.0)
+    hl = np.where(live[:, None], h, 0.0)
+    return G @ w, G.T @ hl, G
+
+
+def top_logits(z, K):
+    """ids and values of the K largest logits of each row, falling, the lowest index first among equals; NaN below
+    everything; -1 and -inf behind a row's last entry."""
+    M, V = z.shape
+    ids, values = np.full((M, K), -1, dtype=np.int32), np.full((M, K), -np.inf, dtype=z.dtype)
+    for m in range(M):
+        nan = np.isnan(z[m])
+        order = sorted(range(V), key=lambda v: (bool(nan[v]), 0.0 if nan[v] else -float(z[m, v]), v))[:K]
+        ids[m, :len(order)], values[m, :len(order)] = order, z[m, order]
+    return ids, values

@@ -5,6 +5,7 @@ PyTorch fallback, and a missing library is a hard error.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_size_t, c_void_p
@@ -34,6 +35,8 @@ EXPORTS = [
     "deer_layer_workspace_bytes", "deer_linear_qkv_rope", "deer_linear_residual_norm", "deer_linear_swiglu",
     "deer_rmsnorm_quant", "deer_quantize", "deer_linear_quant", "deer_kv_create_quant", "deer_kv_store",
     "deer_kv_reserve_rows", "deer_kv_commit_rows", "deer_block_attn_quant_workspace_bytes", "deer_block_attn_quant",
+    "deer_lmhead_loss_workspace_bytes", "deer_lmhead_loss", "deer_lmhead_loss_grad", "deer_lmhead_distill",
+    "deer_lmhead_distill_grad", "deer_top_logits",
 ]
 
 
@@ -147,6 +150,14 @@ def lib() -> ctypes.CDLL:
     L.deer_block_attn_quant_workspace_bytes.argtypes = [c_int] * 6
     L.deer_block_attn_quant.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                         c_int, c_float, c_int, c_void_p, c_size_t, c_void_p]
+    L.deer_lmhead_loss_workspace_bytes.restype = c_size_t
+    L.deer_lmhead_loss_workspace_bytes.argtypes = [c_int] * 5
+    L.deer_lmhead_loss.argtypes = [c_void_p] * 4 + [c_int] * 3 + [c_void_p] * 4 + [c_size_t, c_void_p]
+    L.deer_lmhead_loss_grad.argtypes = [c_void_p] * 7 + [c_int] * 3 + [c_void_p] * 3 + [c_size_t, c_void_p]
+    L.deer_lmhead_distill.argtypes = [c_void_p] * 4 + [c_int, c_float, c_void_p] + [c_int] * 3 + [c_void_p] * 4 + [c_size_t, c_void_p]
+    L.deer_lmhead_distill_grad.argtypes = ([c_void_p] * 4 + [c_int, c_float] + [c_void_p] * 4 + [c_int] * 3 + [c_void_p] * 3
+                                           + [c_size_t, c_void_p])
+    L.deer_top_logits.argtypes = [c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]
     for name in EXPORTS:
         getattr(L, name)          # every declared entry point must be exported
     _lib = L
@@ -562,6 +573,115 @@ def deer_refill(ids, logprob, log_threshold, row_state, tokens, left=None, strea
 def deer_refresh_rows(appended, row_state, stream=None):
     B, k = row_state.shape
     _check(lib().deer_refresh_rows(B, k, _ptr(appended), _ptr(row_state), _stream(stream)))
+
+
+def _on_device(call: str, first: torch.Tensor, *others):
+    """Every operand on the first one's device; that device made current for the call where it is not."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            _refuse(call, "operands on different devices")
+    if not first.is_cuda:
+        _refuse(call, "operands must be on a CUDA device")
+    if _current_device is not None and _current_device() == first.device.index:
+        return _HERE_ALREADY
+    return torch.cuda.device(first.device)
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _rows_of(call: str, h, w):
+    if not (h.dim() == w.dim() == 2 and h.dtype is _BF16 and w.dtype is _BF16 and h.shape[1] == w.shape[1]):
+        _refuse(call, "h must be bf16 [M][hid], w bf16 [V][hid]")
+    return h.shape[0], h.shape[1], w.shape[0]
+
+
+def _of(call: str, dtype, what: str, **operands):
+    """``operands``: name -> (tensor or None, number of elements)."""
+    for name, (t, n) in operands.items():
+        if t is not None and not (t.dtype is dtype and t.numel() == n):
+            _refuse(call, f"{name} must be {what}")
+
+
+def _need(call: str, **operands):
+    for name, t in operands.items():
+        if t is None:
+            _refuse(call, f"{name} is required")
+
+
+def _bytes_of(workspace) -> int:
+    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def deer_lmhead_loss_workspace_bytes(M, hid, V, K=1, grad=False) -> int:
+    return lib().deer_lmhead_loss_workspace_bytes(M, hid, V, K, 1 if grad else 0)
+
+
+def deer_lmhead_loss(h, w, targets, loss, lse, target_logit, workspace, row_weight=None, stream=None):
+    call = "deer_lmhead_loss"
+    M, hid, V = _rows_of(call, h, w)
+    _need(call, targets=targets, loss=loss, lse=lse, target_logit=target_logit)
+    _of(call, _I32, "int32 [M]", targets=(targets, M))
+    _of(call, _F32, "f32 [M]", row_weight=(row_weight, M), loss=(loss, M), lse=(lse, M), target_logit=(target_logit, M))
+    with _on_device(call, h, w, targets, loss, lse, target_logit, workspace, row_weight):
+        _check(lib().deer_lmhead_loss(_ptr(h), _ptr(w), _ptr(targets), _ptr(row_weight), M, hid, V, _ptr(loss), _ptr(lse), _ptr(target_logit),
+                                      _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+
+
+def deer_lmhead_loss_grad(h, w, targets, lse, target_logit, dh, dw, workspace, row_weight=None, grad_loss=None, stream=None):
+    call = "deer_lmhead_loss_grad"
+    M, hid, V = _rows_of(call, h, w)
+    _need(call, targets=targets, lse=lse, target_logit=target_logit)
+    _of(call, _I32, "int32 [M]", targets=(targets, M))
+    _of(call, _F32, "f32 [M]", row_weight=(row_weight, M), grad_loss=(grad_loss, M), lse=(lse, M), target_logit=(target_logit, M))
+    _of(call, _BF16, "bf16 of h's (dh) or w's (dw) size", dh=(dh, M * hid), dw=(dw, V * hid))
+    with _on_device(call, h, w, targets, lse, target_logit, dh, dw, workspace, row_weight, grad_loss):
+        _check(lib().deer_lmhead_loss_grad(_ptr(h), _ptr(w), _ptr(targets), _ptr(row_weight), _ptr(grad_loss), _ptr(lse), _ptr(target_logit),
+                                           M, hid, V, _ptr(dh), _ptr(dw), _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+
+
+def _top_of(call: str, M: int, ids, teacher):
+    _need(call, ids=ids, teacher=teacher)
+    if not (ids.dim() == teacher.dim() == 2 and ids.dtype is _I32 and teacher.dtype is _F32 and ids.shape == teacher.shape and ids.shape[0] == M):
+        _refuse(call, "ids must be int32 [M][K], teacher f32 [M][K]")
+    return ids.shape[1]
+
+
+def deer_lmhead_distill(h, w, ids, teacher, temperature, loss, lse, target_logit, workspace, row_weight=None, stream=None):
+    call = "deer_lmhead_distill"
+    M, hid, V = _rows_of(call, h, w)
+    K = _top_of(call, M, ids, teacher)
+    _need(call, loss=loss, lse=lse, target_logit=target_logit)
+    _of(call, _F32, "f32 [M] (target_logit: [M][K])", row_weight=(row_weight, M), loss=(loss, M), lse=(lse, M), target_logit=(target_logit, M * K))
+    with _on_device(call, h, w, ids, teacher, loss, lse, target_logit, workspace, row_weight):
+        _check(lib().deer_lmhead_distill(_ptr(h), _ptr(w), _ptr(ids), _ptr(teacher), K, float(temperature), _ptr(row_weight), M, hid, V,
+                                         _ptr(loss), _ptr(lse), _ptr(target_logit), _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+
+
+def deer_lmhead_distill_grad(h, w, ids, teacher, temperature, lse, target_logit, dh, dw, workspace, row_weight=None, grad_loss=None,
+                             stream=None):
+    call = "deer_lmhead_distill_grad"
+    M, hid, V = _rows_of(call, h, w)
+    K = _top_of(call, M, ids, teacher)
+    _need(call, lse=lse, target_logit=target_logit)
+    _of(call, _F32, "f32 [M] (target_logit: [M][K])", row_weight=(row_weight, M), grad_loss=(grad_loss, M), lse=(lse, M),
+        target_logit=(target_logit, M * K))
+    _of(call, _BF16, "bf16 of h's (dh) or w's (dw) size", dh=(dh, M * hid), dw=(dw, V * hid))
+    with _on_device(call, h, w, ids, teacher, lse, target_logit, dh, dw, workspace, row_weight, grad_loss):
+        _check(lib().deer_lmhead_distill_grad(_ptr(h), _ptr(w), _ptr(ids), _ptr(teacher), K, float(temperature), _ptr(row_weight),
+                                              _ptr(grad_loss), _ptr(lse), _ptr(target_logit), M, hid, V, _ptr(dh), _ptr(dw), _ptr(workspace),
+                                              _bytes_of(workspace), _stream(stream)))
+
+
+def deer_top_logits(logits, ids, values, stream=None):
+    call = "deer_top_logits"
+    if not (logits.dim() == 2 and logits.dtype is _F32):
+        _refuse(call, "logits must be f32 [M][V]")
+    M, V = logits.shape
+    if not (ids.dim() == values.dim() == 2 and ids.dtype is _I32 and values.dtype is _F32 and ids.shape == values.shape and ids.shape[0] == M):
+        _refuse(call, "ids must be int32 [M][K], values f32 [M][K]")
+    with _on_device(call, logits, ids, values):
+        _check(lib().deer_top_logits(M, V, _ptr(logits), ids.shape[1], _ptr(ids), _ptr(values), _stream(stream)))
 
 
 def deer_verify_step_host(kv: KVCache, dev: deer_step_dev, w, q_host, k_blk_host, v_blk_host, h_host, draft_ids_host,

@@ -1,0 +1,465 @@
+// The losses of the LM head and their gradients: entry points, workspace, and the kernels that work by rows.
+//
+// A row's target is a distribution t over a list of tokens (cross entropy: one token, t = 1; distillation: the softmax of
+// the teacher's logits of the list).  With z = h w^T / tau and lse = log sum exp z over the vocabulary,
+//     loss    = a tau^2 sum_j t_j (log t_j - z_j + lse)
+//     G[m][v] = a g tau (exp(z_v - lse) - t_v),     dh = G w,     dw = G^T h
+// (a: the row's weight, g: the upstream gradient of its loss).  The logits are never kept: the forward pass reduces each
+// tile of z to (max, sum exp) per row, the backward pass computes z a second time, a piece of the vocabulary at a time,
+// and keeps only that piece's G.  Four products of 2 live V hid operations in all bound both, at every size but the
+// smallest; at few rows it is the reading of w (three times) and the writing of dw.
+//
+// The loss is linear in the rows, and rows without a target are common (positions that are not masked, padding), so the
+// live rows are moved together first and everything behind works on those alone.  Their number stays on the device.
+#include <limits.h>
+#include <math.h>
+
+#include "headloss.cuh"
+
+namespace headloss {
+
+constexpr int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
+constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time (more pieces: more part-filled waves; fewer: more memory)
+constexpr float LOG2E = 1.4426950408889634f;
+
+// Columns of a tile, a multiple of `unit` up to 256: the one whose tiles over `rows` row tiles and `cols` columns keep
+// the busiest pair of blocks shortest, a tile costing what 32 columns do beside its own (151936 columns at one row tile:
+// 594 tiles of 256 take 74 pairs 9 rounds = 2304 columns, 792 of 192 take 11 = 2112).
+static int tile_columns(long rows, long cols, int unit, int pairs) {
+    int best = 256;
+    long best_cost = LONG_MAX;
+    for (int n = 256; n >= 64; n -= unit) {
+        const long cost = (rows * ((cols + n - 1) / n) + pairs - 1) / pairs * (n + 32);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = n;
+        }
+    }
+    return best;
+}
+
+Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
+    Space s = {};
+    const int pairs = deer_sm_count() / 2;
+    s.Mp = (M + TILE - 1) / TILE * TILE;
+    const int mt = s.Mp / TILE;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* p = base ? static_cast<char*>(base) + at : nullptr;
+        at += (bytes + 1023) / 1024 * 1024;
+        return p;
+    };
+    s.hdr = (int*)take(16);
+    s.slot = (int*)take((size_t)M * 4);
+    s.row = (int*)take((size_t)s.Mp * 4);
+    s.ids = (int*)take((size_t)K * s.Mp * 4);
+    s.h = (__nv_bfloat16*)take((size_t)s.Mp * hid * 2);
+    if (!grad) {
+        s.stats_n = tile_columns(mt, V, 32, pairs);
+        s.pos = (int*)take((size_t)K * s.Mp * 4);
+        s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * 8);
+        s.bytes = at;
+        return s;
+    }
+    // equal pieces, whole tiles of dw
+    const long room = (long)(PIECE_BYTES / ((size_t)s.Mp * 2)) / TILE * TILE;
+    const long most = room < 1024 ? 1024 : room;
+    s.pieces = (int)((V + most - 1) / most);
+    s.piece = (int)(((V + s.pieces - 1) / s.pieces + TILE - 1) / TILE * TILE);
+    s.pieces = (V + s.piece - 1) / s.piece;
+    s.grad_n = tile_columns(mt, s.piece < V ? s.piece : V, 64, pairs);
+    s.hid_n = tile_columns(1, hid, 64, 1);
+    // space for dh's partial sums: whatever number of rows turns out to be live
+    const int ht = (hid + s.hid_n - 1) / s.hid_n, steps = (s.piece + STEP - 1) / STEP, cap = mt > pairs ? mt : pairs;
+    for (int i = 1; i <= mt; ++i) {
+        const int tiles = i * dh_ranges(i, ht, steps, pairs, cap);
+        if (tiles > s.slab_tiles) s.slab_tiles = tiles;
+    }
+    s.coef = (float*)take((size_t)s.Mp * 4);
+    s.lse2 = (float*)take((size_t)s.Mp * 4);
+    s.gval = (float*)take((size_t)K * s.Mp * 4);
+    s.g = (__nv_bfloat16*)take((size_t)s.Mp * s.piece * 2);
+    s.slab = (float*)take((size_t)s.slab_tiles * TILE * hid * 4);
+    s.bytes = at;
+    return s;
+}
+
+struct RowArgs {
+    int M, hid, V, K, per_block;
+    const __nv_bfloat16* h;
+    const int* ids;              // [M][K]
+    const float* teacher;        // [M][K] or NULL (K = 1, t = 1)
+    const float* weight;         // [M] or NULL
+    const float* grad;           // [M] or NULL                     (gradient)
+    const float* lse;            // [M]                             (loss: out; gradient: in)
+    const float* target_logit;   // [M][K]
+    float tau;
+    int ht, steps, pairs, slab_tiles;
+    Space s;
+};
+
+__device__ __forceinline__ bool is_live(const RowArgs& a, int m) {
+    return a.ids[(size_t)m * a.K] >= 0 && (a.weight == nullptr || a.weight[m] != 0.f);
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ int warp_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }
+
+// A warp's view of one row's list: lane l holds entries l, l + 32, ...
+struct List {
+    int n;                       // entries in front of the first negative id
+    bool beyond;                 // an id of V or more among them
+    int id[MAX_TOP / 32];
+    __device__ __forceinline__ List(const RowArgs& a, int m, int lane) {
+        n = a.K;
+        int out = 0;
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) {
+            const int j = i * 32 + lane;
+            id[i] = j < a.K ? a.ids[(size_t)m * a.K + j] : -1;
+            const unsigned end = __ballot_sync(0xffffffffu, id[i] < 0);
+            if (end && i * 32 + __ffs(end) - 1 < n) n = i * 32 + __ffs(end) - 1;
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) out |= i * 32 + lane < n && id[i] >= a.V;
+        beyond = __any_sync(0xffffffffu, out);
+    }
+};
+
+// log t of a list's entries: the log-softmax of teacher / tau over the list, 0 for a list without a teacher.  False: the
+// list holds no entry above -inf, so that there is no distribution (the row then has neither loss nor gradient).
+__device__ __forceinline__ bool log_targets(const RowArgs& a, const List& l, int m, int lane, float (&log_t)[MAX_TOP / 32]) {
+    if (!a.teacher) {
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) log_t[i] = i * 32 + lane < l.n ? 0.f : -INFINITY;
+        return true;
+    }
+    float top = -INFINITY, sum = 0.f;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        const int j = i * 32 + lane;
+        log_t[i] = j < l.n ? a.teacher[(size_t)m * a.K + j] / a.tau : -INFINITY;
+        some |= !(log_t[i] == -INFINITY);
+        top = fmaxf(top, log_t[i]);
+    }
+    top = warp_max(top);
+    if (!__any_sync(0xffffffffu, some)) return false;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        log_t[i] -= top;                                   // (NaN where the teacher's is, or the largest is infinite)
+        if (i * 32 + lane < l.n) sum += expf(log_t[i]);
+    }
+    const float log_sum = logf(warp_sum(sum));
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) log_t[i] -= log_sum;
+    return true;
+}
+
+// Moves the live rows together and lists their tokens by rising id.  A block takes `per_block` rows and counts the live
+// ones among all rows itself (M flags from L2: less than the launch of a kernel that counts); a warp takes a row.
+// GRAD: also what the products' epilogue needs of a row and of its listed tokens.
+template <bool GRAD>
+__global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a) {
+    __shared__ int sums[2][ROW_WARPS];
+    __shared__ int list_id[ROW_WARPS][MAX_TOP];
+    __shared__ float list_t[ROW_WARPS][MAX_TOP];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    pdl_trigger();
+    pdl_wait();
+    const int base = blockIdx.x * a.per_block;
+    int before = 0, total = 0;
+    for (int m = tid; m < a.M; m += ROW_THREADS) {
+        const int f = is_live(a, m);
+        total += f;
+        before += m < base ? f : 0;
+    }
+    before = warp_sum(before);
+    total = warp_sum(total);
+    if (lane == 0) {
+        sums[0][warp] = before;
+        sums[1][warp] = total;
+    }
+    __syncthreads();
+    before = total = 0;
+#pragma unroll
+    for (int i = 0; i < ROW_WARPS; ++i) {
+        before += sums[0][i];
+        total += sums[1][i];
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        a.s.hdr[HDR_LIVE] = total;
+        a.s.hdr[HDR_RANGES] = GRAD ? dh_ranges((total + TILE - 1) / TILE, a.ht, a.steps, a.pairs, a.slab_tiles) : 1;
+        a.s.hdr[HDR_GAVE_UP] = 0;
+    }
+    const int fill_end = min((total + STEP - 1) / STEP * STEP, a.s.Mp);
+    const int chunks = a.hid / 8;                          // 16 bytes each
+    for (int g = 0; g < a.per_block; g += 32) {
+        const int here = min(32, a.per_block - g);
+        const unsigned mask = __ballot_sync(0xffffffffu, lane < here && base + g + lane < a.M && is_live(a, base + g + lane));
+        for (int r = warp; r < here; r += ROW_WARPS) {
+            const int m = base + g + r;
+            if (m >= total && m < fill_end) {              // places behind the live rows that the last step of dw's contraction meets
+                uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)m * a.hid);
+                for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
+            }
+            if (m >= a.M) continue;
+            if (!((mask >> r) & 1u)) {
+                if (lane == 0) a.s.slot[m] = -1;
+                continue;
+            }
+            const int slot = before + __popc(mask & ((1u << r) - 1u));
+            if (lane == 0) {
+                a.s.slot[m] = slot;
+                a.s.row[slot] = m;
+            }
+            const uint4* src = reinterpret_cast<const uint4*>(a.h + (size_t)m * a.hid);
+            uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)slot * a.hid);
+            for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+
+            const List l(a, m, lane);
+            float log_t[MAX_TOP / 32], coef = 0.f, lse = 0.f;
+            if (GRAD) {
+                const bool some = log_targets(a, l, m, lane, log_t);
+                lse = a.lse[m];
+                coef = some && !l.beyond ? (a.weight ? a.weight[m] : 1.f) * (a.grad ? a.grad[m] : 1.f) * a.tau : 0.f;
+                if (lane == 0) {
+                    a.s.coef[slot] = coef;
+                    a.s.lse2[slot] = lse * LOG2E;
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < MAX_TOP / 32; ++i) {
+                list_id[warp][i * 32 + lane] = l.id[i];
+                if (GRAD) list_t[warp][i * 32 + lane] = expf(log_t[i]);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < MAX_TOP / 32; ++i) {
+                const int j = i * 32 + lane;
+                if (j >= a.K) continue;
+                int place = j;
+                float t = 0.f;                             // the token's probability, wherever the list names it
+                if (j < l.n) {
+                    place = 0;
+                    for (int o = 0; o < l.n; ++o) {
+                        const int other = list_id[warp][o];
+                        place += other < l.id[i] || (other == l.id[i] && o < j);
+                        if (GRAD && other == l.id[i]) t += list_t[warp][o];
+                    }
+                }
+                const size_t at = (size_t)place * a.s.Mp + slot;
+                a.s.ids[at] = j < l.n ? l.id[i] : INT_MAX;
+                if (!GRAD) a.s.pos[at] = j;
+                if (GRAD && j < l.n) {
+                    const float z = a.target_logit[(size_t)m * a.K + j];
+                    a.s.gval[at] = coef == 0.f ? 0.f : coef * (expf(z / a.tau - lse) - t);
+                }
+            }
+        }
+        before += __popc(mask);
+    }
+}
+
+// lse and loss of every row from its tiles' (max, sum exp): a warp per row.
+__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int tiles, float c2, float* loss, float* lse_out, float* target_logit) {
+    const int lane = threadIdx.x & 31, m = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
+    pdl_trigger();
+    pdl_wait();
+    if (m >= a.M) return;
+    const int slot = a.s.slot[m];
+    if (slot < 0) {
+        for (int j = lane; j < a.K; j += 32) target_logit[(size_t)m * a.K + j] = 0.f;
+        if (lane == 0) loss[m] = lse_out[m] = 0.f;
+        return;
+    }
+    const float2* part = a.s.part + (size_t)slot * tiles;
+    float top = -INFINITY, sum = 0.f;
+    for (int i = lane; i < tiles; i += 32) top = fmaxf(top, part[i].x);
+    top = warp_max(top);
+    for (int i = lane; i < tiles; i += 32) sum += part[i].y * exp2f((part[i].x - top) * c2);
+    float lse = top / a.tau + logf(warp_sum(sum));
+    if (a.s.hdr[HDR_GAVE_UP]) lse = NAN;
+    const List l(a, m, lane);
+    float log_t[MAX_TOP / 32], each = 0.f;
+    const bool some = log_targets(a, l, m, lane, log_t);
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        const int j = i * 32 + lane;
+        if (j < a.K && (j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
+        if (j < l.n && l.id[i] < a.V && !(log_t[i] == -INFINITY))
+            each += expf(log_t[i]) * (log_t[i] - target_logit[(size_t)m * a.K + j] / a.tau + lse);
+    }
+    each = warp_sum(each);
+    if (lane == 0) {
+        const float x = (a.weight ? a.weight[m] : 1.f) * (a.tau * a.tau) * each;
+        loss[m] = l.beyond ? NAN : some ? x : 0.f;
+        lse_out[m] = lse;
+    }
+}
+
+// dh of every row: the partial sums of its ranges in their order, zeros for a dead row.  A warp per row.
+__global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, __nv_bfloat16* dh) {
+    const int lane = threadIdx.x & 31, m = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
+    pdl_trigger();
+    pdl_wait();
+    if (m >= a.M) return;
+    const int slot = a.s.slot[m], live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
+    const size_t range_rows = (size_t)((live + TILE - 1) / TILE) * TILE;
+    const bool gave_up = a.s.hdr[HDR_GAVE_UP] != 0;
+    __nv_bfloat16* dst = dh + (size_t)m * a.hid;
+    for (int c = lane * 8; c < a.hid; c += 256) {
+        float v[8] = {};
+        if (slot >= 0)
+            for (int r = 0; r < ranges; ++r) {
+                const float4* src = reinterpret_cast<const float4*>(a.s.slab + ((size_t)r * range_rows + slot) * a.hid + c);
+                const float4 x = src[0], y = src[1];
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+            }
+        if (gave_up)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = NAN;
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+}
+
+static int check(const char* call, const void* h, const void* w, const int32_t* ids, int K, float tau, const float* row_weight, int M, int hid, int V) {
+    DEER_CHECK_ARG(M >= 0 && V >= 1, DEER_ERR_INVALID_ARG, "%s: M must not be negative, V at least 1", call);
+    DEER_CHECK_ARG(M <= (1 << 18) && V <= (1 << 30), DEER_ERR_UNSUPPORTED, "%s: more than 2^18 rows or 2^30 tokens", call);
+    DEER_CHECK_ARG(hid >= 64 && hid % 64 == 0 && hid <= 65536, DEER_ERR_UNSUPPORTED, "%s: hid must be a multiple of 64, at most 65536", call);
+    DEER_CHECK_ARG(K >= 1 && K <= MAX_TOP, DEER_ERR_UNSUPPORTED, "%s: a list has 1 to %d entries", call, MAX_TOP);
+    DEER_CHECK_ARG(tau > 0.f && tau < INFINITY, DEER_ERR_INVALID_ARG, "%s: temperature must be positive and finite", call);
+    DEER_CHECK_ARG(h && w && ids, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
+    DEER_CHECK_ARG(deer_aligned16(h) && deer_aligned16(w), DEER_ERR_INVALID_ARG, "%s: h and w must be 16-byte aligned", call);
+    DEER_CHECK_ARG(deer_aligned4(ids) && deer_aligned4(row_weight), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
+    return DEER_OK;
+}
+
+static RowArgs row_args(const Space& s, const void* h, const int32_t* ids, const float* teacher, int K, float tau, const float* row_weight,
+                        int M, int hid, int V) {
+    RowArgs a = {};
+    a.M = M;
+    a.hid = hid;
+    a.V = V;
+    a.K = K;
+    a.per_block = ROW_WARPS * ((M + 2047) / 2048);         // at most 256 blocks: each of them counts all rows
+    a.h = static_cast<const __nv_bfloat16*>(h);
+    a.ids = ids;
+    a.teacher = teacher;
+    a.weight = row_weight;
+    a.tau = tau;
+    a.s = s;
+    return a;
+}
+static unsigned row_blocks(const RowArgs& a) {             // all rows, and the places that are filled up behind them
+    return (unsigned)(((a.M + STEP - 1) / STEP * STEP + a.per_block - 1) / a.per_block);
+}
+
+static int loss_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float tau,
+                     const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    int rc = check(call, h, w, ids, K, tau, row_weight, M, hid, V);
+    if (rc != DEER_OK) return rc;
+    DEER_CHECK_ARG(loss && lse && target_logit, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
+    DEER_CHECK_ARG(deer_aligned4(loss) && deer_aligned4(lse) && deer_aligned4(target_logit), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
+    if (M == 0) return DEER_OK;
+    const Space s = lay_out(workspace, M, hid, V, K, false);
+    DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
+                   "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
+    const float c2 = LOG2E / tau;
+    DEER_CUDA(launch_pdl(head_rows_kernel<false>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
+    rc = launch_product(STATS, s, w, M, hid, V, K, 0, c2, target_logit, nullptr, st);
+    if (rc != DEER_OK) return rc;
+    DEER_CUDA(launch_pdl(head_loss_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (V + s.stats_n - 1) / s.stats_n, c2,
+                         loss, lse, target_logit));
+    return DEER_OK;
+}
+
+static int grad_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float tau,
+                     const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid, int V,
+                     void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check(call, h, w, ids, K, tau, row_weight, M, hid, V);
+    if (rc != DEER_OK) return rc;
+    DEER_CHECK_ARG(lse && target_logit, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
+    DEER_CHECK_ARG(dh || dw, DEER_ERR_INVALID_ARG, "%s: neither dh nor dw is asked for", call);
+    DEER_CHECK_ARG(deer_aligned16(dh) && deer_aligned16(dw), DEER_ERR_INVALID_ARG, "%s: dh and dw must be 16-byte aligned", call);
+    DEER_CHECK_ARG(deer_aligned4(lse) && deer_aligned4(target_logit) && deer_aligned4(grad_loss), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (M == 0) {
+        if (dw) DEER_CUDA(cudaMemsetAsync(dw, 0, (size_t)V * hid * 2, st));
+        return DEER_OK;
+    }
+    const Space s = lay_out(workspace, M, hid, V, K, true);
+    DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
+                   "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
+    RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
+    a.grad = grad_loss;
+    a.lse = lse;
+    a.target_logit = target_logit;
+    a.ht = (hid + s.hid_n - 1) / s.hid_n;
+    a.steps = (s.piece + STEP - 1) / STEP;
+    a.pairs = deer_sm_count() / 2;
+    a.slab_tiles = s.slab_tiles;
+    DEER_CUDA(launch_pdl(head_rows_kernel<true>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
+    for (int p = 0; p < s.pieces; ++p) {
+        rc = launch_product(GRAD, s, w, M, hid, V, K, p, LOG2E / tau, nullptr, nullptr, st);
+        if (rc == DEER_OK && dh) rc = launch_product(DH, s, w, M, hid, V, K, p, 0.f, nullptr, nullptr, st);
+        if (rc == DEER_OK && dw) rc = launch_product(DW, s, w, M, hid, V, K, p, 0.f, nullptr, dw, st);
+        if (rc != DEER_OK) return rc;
+    }
+    if (dh)
+        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, static_cast<__nv_bfloat16*>(dh)));
+    return DEER_OK;
+}
+
+}  // namespace headloss
+
+extern "C" {
+
+size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad) {
+    if (M <= 0 || M > (1 << 18) || hid < 64 || hid % 64 || hid > 65536 || V < 1 || V > (1 << 30) || K < 1 || K > headloss::MAX_TOP) return 0;
+    return headloss::lay_out(nullptr, M, hid, V, K, grad != 0).bytes;
+}
+
+int deer_lmhead_loss(const void* h, const void* w, const int32_t* targets, const float* row_weight, int M, int hid, int V, float* loss,
+                     float* lse, float* target_logit, void* workspace, size_t workspace_bytes, void* stream) {
+    return headloss::loss_call("deer_lmhead_loss", h, w, targets, nullptr, 1, 1.f, row_weight, M, hid, V, loss, lse, target_logit, workspace,
+                               workspace_bytes, stream);
+}
+
+int deer_lmhead_loss_grad(const void* h, const void* w, const int32_t* targets, const float* row_weight, const float* grad_loss,
+                          const float* lse, const float* target_logit, int M, int hid, int V, void* dh, void* dw, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    return headloss::grad_call("deer_lmhead_loss_grad", h, w, targets, nullptr, 1, 1.f, row_weight, grad_loss, lse, target_logit, M, hid, V, dh,
+                               dw, workspace, workspace_bytes, stream);
+}
+
+int deer_lmhead_distill(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
+                        const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    DEER_CHECK_ARG(teacher && deer_aligned4(teacher), DEER_ERR_INVALID_ARG, "deer_lmhead_distill: teacher is null or misaligned");
+    return headloss::loss_call("deer_lmhead_distill", h, w, ids, teacher, K, temperature, row_weight, M, hid, V, loss, lse, target_logit,
+                               workspace, workspace_bytes, stream);
+}
+
+int deer_lmhead_distill_grad(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
+                             const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid,
+                             int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    DEER_CHECK_ARG(teacher && deer_aligned4(teacher), DEER_ERR_INVALID_ARG, "deer_lmhead_distill_grad: teacher is null or misaligned");
+    return headloss::grad_call("deer_lmhead_distill_grad", h, w, ids, teacher, K, temperature, row_weight, grad_loss, lse, target_logit, M, hid,
+                               V, dh, dw, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

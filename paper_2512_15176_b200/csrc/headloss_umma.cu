@@ -1,0 +1,481 @@
+// The products of the LM head's losses on the tensor cores:
+//
+//   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid
+//   GRAD   G = coef (p - t)          [live][piece]  the same z again, softmax and targets in the epilogue
+//   DH     dh = G w                  [live][hid]    contraction over the piece's vocabulary
+//   DW     dw = G^T h                [piece][hid]   contraction over the live rows
+//
+// One kernel body.  Pairs of blocks (tcgen05.mma.cta_group::2, 256 x n tiles, n <= 256, fp32 accumulators in two
+// tensor-memory buffers) walk a list of tiles: a warp per block brings 64-deep steps of both operands by TMA into a ring
+// of six 32 KB stages, one warp of the pair issues the MMAs, four warps per block take the finished tile while the next
+// one is computed.  h and G are stored row-major once; where the contraction runs along their rows (DW, and w in DH) the
+// operand is read MN-major: boxes of 64 contraction rows x 64 columns, two of them side by side.
+//
+// G is rounded to bf16 once, as a product of the tensor cores wants it (2^-9 relative to each term, as dh and dw
+// themselves); at a listed token p - t is formed in fp32 first, so that a target the model is sure of keeps its
+// difference.  lse, p and all sums are fp32.
+#include <math.h>
+
+#include "headloss.cuh"
+#include "sm100.cuh"
+
+using namespace sm100;
+
+namespace headloss {
+
+constexpr int STAGES = 6;
+constexpr int OPERAND = 16384;             // bytes of one operand's share of a stage: 128 rows (columns) x 64 bf16
+constexpr int STAGE_BYTES = 2 * OPERAND;
+constexpr int STAGING = 4 * 2 * 4096;      // two boxes of 32 rows x 128 bytes for each epilogue warp
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
+constexpr int THREADS = 192;
+constexpr int ACC = 256;                   // columns of one accumulator
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* tm, uint32_t src, int x, int y) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
+#define TMEM_LD_X1(taddr, r) asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr))
+
+// kind::f16 instruction descriptor: bf16 x bf16 -> fp32, M = 256 across the pair, N = n.
+__device__ __forceinline__ uint32_t idesc_pair(int n, bool a_mn, bool b_mn) {
+    return make_idesc_bf16_pair(n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+}
+
+// Tile u of the list: rows and columns of the product, range of the contraction in steps.
+struct Tile {
+    int r, c, k0, kb, y;       // y: DH: row of the slabs
+};
+template <int P>
+struct List {
+    int mt, ct, live, steps, ranges, n;
+    __device__ __forceinline__ List(const ProductArgs& a) {
+        live = a.hdr_in[HDR_LIVE];
+        mt = (live + TILE - 1) / TILE;
+        ct = a.col_tiles;
+        ranges = 1;
+        if (P == STATS || P == GRAD) {
+            steps = a.hid / STEP;
+            n = mt * ct;
+        } else if (P == DH) {
+            steps = (a.vn + STEP - 1) / STEP;
+            ranges = a.hdr_in[HDR_RANGES];
+            n = mt * ct * ranges;
+        } else {
+            steps = (live + STEP - 1) / STEP;
+            n = a.row_tiles * ct;
+        }
+    }
+    __device__ __forceinline__ Tile tile(int u) const {
+        Tile t;
+        t.k0 = 0;
+        t.kb = steps;
+        t.y = 0;
+        if (P == STATS || P == GRAD) {      // row tiles fastest: the pairs share a few tiles of w at a time
+            t.r = u % mt;
+            t.c = u / mt;
+        } else {                            // columns (of hid) fastest: the pairs share tiles of G
+            t.c = u % ct;
+            t.r = u / ct;
+            if (P == DH) {
+                const int s = t.r / mt;
+                t.y = t.r * TILE;
+                t.r -= s * mt;
+                t.k0 = (int)((long)s * steps / ranges);
+                t.kb = (int)((long)(s + 1) * steps / ranges) - t.k0;
+            }
+        }
+        return t;
+    }
+};
+
+template <int P>
+__device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const List<P>& list, int quarter, int lane, int rank,
+                                         uint32_t tmem_base, uint32_t tfull0, uint32_t tempty0, uint32_t staging, volatile int* abort_flag) {
+    const uint32_t stg = staging + (uint32_t)quarter * 8192u, stg_row = (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
+    const int lane_row = rank * 128 + quarter * 32 + lane;                 // the thread's row within a tile
+    const int pairs = gridDim.x >> 1;
+    uint32_t stg_i = 0;
+    int it = 0;
+    for (int u = blockIdx.x >> 1; u < list.n; u += pairs) {
+        const Tile t = list.tile(u);
+        if (t.kb == 0 && P != DW) continue;                               // DH: nothing to add; DW without a live row: zeros
+        const int buf = it & 1;
+        const bool computed = t.kb > 0;
+        if (computed) {
+            const bool got = mbar_wait(tfull0 + 8u * buf, (uint32_t)(it >> 1) & 1u, abort_flag);
+            if (!__all_sync(0xffffffffu, got)) break;                     // warp-uniform, so the aligned TMEM loads stay converged
+            tcgen05_fence_after();
+            ++it;
+        }
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * ACC);
+        const int slot = t.r * TILE + lane_row;                           // STATS, GRAD: place among the live rows
+        const bool row_ok = slot < list.live;
+        const int col0 = t.c * a.n;
+
+        if (P == STATS) {
+            const int width = min(a.n, a.vn - col0);                      // columns that exist
+            float run_m = -INFINITY, run_s = 0.f;
+            for (int c = 0; c < width; c += 32) {
+                uint32_t v[32];
+                TMEM_LD_X32(taddr + c, v);
+                tmem_wait_ld();
+                const int have = width - c;
+                float m = -INFINITY;
+                if (have >= 32) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) m = fmaxf(m, __uint_as_float(v[j]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        if (j >= have) v[j] = 0xff800000u;
+                        m = fmaxf(m, __uint_as_float(v[j]));
+                    }
+                }
+                m = fmaxf(m, run_m);
+                const float shift = m == -INFINITY ? 0.f : m * a.c2;       // a row of -inf so far: its exponentials are 0
+                run_s *= ex2(run_m * a.c2 - shift);
+                run_m = m;
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    s0 += ex2(fmaf(__uint_as_float(v[j]), a.c2, -shift));
+                    s1 += ex2(fmaf(__uint_as_float(v[j + 1]), a.c2, -shift));
+                }
+                run_s += s0 + s1;
+            }
+            if (row_ok) a.part[(size_t)slot * a.tiles + t.c] = make_float2(run_m, run_s);
+            // The z of listed tokens in this tile.  Few rows have one here, so each distinct column is read again.
+            int e = 0, next = 0x7fffffff;
+            const int first = a.v0 + col0, last = first + width;
+            if (row_ok) {
+                int hi = a.K;                                              // first entry at or behind the tile's start
+                while (e < hi) {
+                    const int mid = (e + hi) >> 1;
+                    if (a.ids[(size_t)mid * a.Mp + slot] < first) e = mid + 1;
+                    else hi = mid;
+                }
+                if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
+            }
+            for (;;) {
+                const int col = __reduce_min_sync(0xffffffffu, next);
+                if (col >= last) break;
+                uint32_t z;
+                TMEM_LD_X1(taddr + (uint32_t)(col - first), z);
+                tmem_wait_ld();
+                while (next == col) {
+                    a.target_logit[(size_t)a.row[slot] * a.K + a.pos[(size_t)e * a.Mp + slot]] = __uint_as_float(z);
+                    ++e;
+                    next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
+                }
+                __syncwarp();
+            }
+        } else if (P == GRAD || P == DW) {
+            float coef = 0.f, nlse = 0.f;
+            int e = 0, next = 0x7fffffff;
+            if (P == GRAD && row_ok) {
+                coef = a.coef[slot];
+                nlse = -a.lse2[slot];
+                int hi = a.K;
+                while (e < hi) {
+                    const int mid = (e + hi) >> 1;
+                    if (a.ids[(size_t)mid * a.Mp + slot] < a.v0 + col0) e = mid + 1;
+                    else hi = mid;
+                }
+                if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
+            }
+            const int limit = P == GRAD ? a.vn : a.hid;
+            for (int c = 0; c < a.n && col0 + c < limit; c += 64) {
+                if (lane == 0) bulk_wait_read<1>();                       // the store from this box two chunks ago has read it
+                __syncwarp();
+                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row;
+                stg_i ^= 1;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t v[32];
+                    if (computed) {
+                        TMEM_LD_X32(taddr + c + 32 * half, v);
+                        tmem_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0;
+                    }
+                    uint32_t o[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float x = __uint_as_float(v[2 * j]), y = __uint_as_float(v[2 * j + 1]);
+                        if (P == GRAD) {
+                            x = coef * ex2(fmaf(x, a.c2, nlse));
+                            y = coef * ex2(fmaf(y, a.c2, nlse));
+                        }
+                        o[j] = pack_bf16(x, y);
+                        if (P == GRAD && !row_ok) o[j] = 0;               // places behind the live rows: DW's contraction meets them
+                    }
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j)
+                        st_shared_v4(b + (((4 * half + j) ^ sw) << 4), o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                }
+                if (P == GRAD) {
+                    const int first = a.v0 + col0 + c;
+                    while (next < first + 64) {                           // listed tokens: p - t, formed in fp32 beforehand
+                        const uint32_t k = (uint32_t)(next - first);
+                        const __nv_bfloat16 val = __float2bfloat16(a.gval[(size_t)e * a.Mp + slot]);
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2),
+                                     "h"(*reinterpret_cast<const uint16_t*>(&val))
+                                     : "memory");
+                        ++e;
+                        next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                const int y = (P == DW ? a.v0 : 0) + t.r * TILE + rank * 128 + quarter * 32;
+                if (lane == 0 && (P == GRAD || y < a.V)) {                // rows and columns beyond the tensor are clipped
+                    tma_store_2d(tm_out, box, col0 + c, y);
+                    bulk_commit();
+                }
+            }
+        } else {                                                          // DH: fp32, 32 columns to a box
+            for (int c = 0; c < a.n && col0 + c < a.hid; c += 32) {
+                if (lane == 0) bulk_wait_read<1>();
+                __syncwarp();
+                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row;
+                stg_i ^= 1;
+                uint32_t v[32];
+                TMEM_LD_X32(taddr + c, v);
+                tmem_wait_ld();
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) st_shared_v4(b + ((j ^ sw) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    const int y = t.y + rank * 128 + quarter * 32;
+                    if (a.add) tma_reduce_add_2d(tm_out, box, col0 + c, y);
+                    else tma_store_2d(tm_out, box, col0 + c, y);
+                    bulk_commit();
+                }
+            }
+        }
+        if (computed) {
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_peer(map_to_cta(tempty0 + 8u * buf, 0));
+        }
+    }
+    if (lane == 0) bulk_wait<0>();               // the staging area outlives every store that reads it
+}
+
+template <int P>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_out,
+               const ProductArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + STAGING);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    constexpr bool A_MN = P == DW, B_MN = P == DH || P == DW;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const int pairs = gridDim.x >> 1;
+    const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
+    auto full_bar = [&](int s) { return bar_base + 8u * s; };
+    auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+    const uint32_t tfull0 = bar_base + 8u * (2 * STAGES), tempty0 = tfull0 + 16u;
+
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(tfull0 + 8u * b, 1);
+            mbar_init(tempty0 + 8u * b, 8);      // four epilogue warps in each of the two blocks
+        }
+        *abort_flag = 0;
+        mbar_init_fence();
+        prefetch_tensormap(&tm_a);
+        prefetch_tensormap(&tm_b);
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    pdl_trigger();
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync();                              // the peer's barriers exist before anything signals them
+    tcgen05_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();                                  // (the weights too: in training an optimiser step may be what ran before)
+    const List<P> list(a);
+
+    if (warp == 0) {
+        // ---------------- TMA producer (each block: its rows of one operand, its half of the columns of the other) --------
+        if (lane == 0) {
+            const int half = a.n / 2;                                      // columns of the tile that this block brings
+            const bool has_a = A_MN || leader || a.a_second;
+            const int b_boxes = B_MN ? (half + 63) / 64 : 1;
+            const uint32_t a_bytes = A_MN ? OPERAND : (uint32_t)a.a_rows * 128u;
+            const uint32_t b_bytes = B_MN ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u;
+            const uint32_t stage_tx = a_bytes * ((A_MN || a.a_second) ? 2u : 1u) + 2u * b_bytes;
+            int it = 0;
+            bool ok = true;
+            for (int u = blockIdx.x >> 1; u < list.n && ok; u += pairs) {
+                const Tile t = list.tile(u);
+                const int ra = t.r * TILE + (int)rank * 128, cb = t.c * a.n + (int)rank * half;
+                for (int kb = 0; kb < t.kb; ++kb, ++it) {
+                    const int s = it % STAGES, k = (t.k0 + kb) * STEP;
+                    if (!mbar_wait(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                    if (leader) mbar_expect_tx(full_bar(s), stage_tx);
+                    const uint32_t full = map_to_cta(full_bar(s), 0), sa = smem_base + s * STAGE_BYTES, sb = sa + OPERAND;
+                    if (A_MN) {
+                        tma_load_2d_pair(sa, &tm_a, ra, k, full);
+                        tma_load_2d_pair(sa + 8192, &tm_a, ra + 64, k, full);
+                    } else if (has_a) {
+                        tma_load_2d_pair(sa, &tm_a, k, ra, full);
+                    }
+                    if (B_MN) {
+                        const int y = P == DH ? a.v0 + k : k;
+                        tma_load_2d_pair(sb, &tm_b, cb, y, full);
+                        if (b_boxes > 1) tma_load_2d_pair(sb + 8192, &tm_b, cb + 64, y, full);
+                    } else {
+                        tma_load_2d_pair(sb, &tm_b, k, a.v0 + cb, full);
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer (first block of the pair) ----------------
+        if (leader && lane == 0) {
+            const uint32_t idesc = idesc_pair(a.n, A_MN, B_MN);
+            int it = 0, done = 0;
+            bool ok = true;
+            for (int u = blockIdx.x >> 1; u < list.n && ok; u += pairs) {
+                const Tile t = list.tile(u);
+                if (t.kb == 0) continue;
+                const int buf = done & 1;
+                if (!mbar_wait(tempty0 + 8u * buf, ((uint32_t)(done >> 1) & 1u) ^ 1u, abort_flag)) break;
+                ++done;
+                tcgen05_fence_after();
+                const uint32_t d_tmem = tmem_base + (uint32_t)(buf * ACC);
+                for (int kb = 0; kb < t.kb; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!mbar_wait(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    tcgen05_fence_after();
+                    const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + OPERAND;
+                    // K-major: 16 contraction columns are 32 bytes; MN-major: 16 contraction rows are 2048 bytes
+                    const uint64_t ad = A_MN ? smem_desc_sw128(sa, 8192, 1024) : smem_desc_sw128_kmajor(sa);
+                    const uint64_t bd = B_MN ? smem_desc_sw128(sb, 8192, 1024) : smem_desc_sw128_kmajor(sb);
+#pragma unroll
+                    for (int k = 0; k < STEP / 16; ++k)
+                        umma_bf16_ss_pair(d_tmem, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, (kb | k) != 0 ? 1u : 0u);
+                    umma_commit_pair(empty_bar(s), 3);
+                }
+                if (ok) umma_commit_pair(tfull0 + 8u * buf, 3);
+            }
+        }
+    } else {
+        epilogue<P>(a, &tm_out, list, warp & 3, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
+    }
+
+    // ---- tear-down: neither block leaves while the other may still signal it or read its shared memory ----
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) a.hdr[HDR_GAVE_UP] = 1;    // the last kernel of the call turns this into NaN
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+        __syncthreads();
+    }
+    cluster_sync();
+    if (warp == 1) {
+        __syncwarp();
+        tcgen05_fence_after();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+// 2-D bf16 tensor [rows][cols] of `pitch` columns, box = box_rows x 64 columns.
+static int map_bf16(CUtensorMap* tm, const void* base, long rows, long cols, long pitch, int box_rows) {
+    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
+    const uint64_t strides[1] = {(uint64_t)pitch * 2};
+    const uint32_t box[2] = {64, (uint32_t)box_rows};
+    return make_map_bf16(tm, base, 2, dims, strides, box);
+}
+
+template <int P>
+static int launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const ProductArgs& a, long most_tiles, cudaStream_t st) {
+    long pairs = deer_sm_count() / 2;
+    if (pairs > most_tiles) pairs = most_tiles;
+    DEER_CUDA(cudaFuncSetAttribute(product_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+    DEER_CUDA(launch_pdl(product_kernel<P>, dim3((unsigned)(2 * pairs)), dim3(THREADS), (size_t)SMEM_BYTES, st, ta, tb, to, a));
+    return DEER_OK;
+}
+
+int launch_product(Product what, const Space& s, const void* w, int M, int hid, int V, int K, int piece, float c2, float* target_logit,
+                   void* dw, cudaStream_t st) {
+    ProductArgs a = {};
+    a.hdr_in = a.hdr = s.hdr;
+    a.hid = hid;
+    a.V = V;
+    a.Mp = s.Mp;
+    a.K = K;
+    a.c2 = c2;
+    a.ids = s.ids;
+    a.pos = s.pos;
+    a.row = s.row;
+    a.target_logit = target_logit;
+    a.part = s.part;
+    a.coef = s.coef;
+    a.lse2 = s.lse2;
+    a.gval = s.gval;
+    a.v0 = what == STATS ? 0 : piece * s.piece;
+    a.vn = what == STATS ? V : (V - a.v0 < s.piece ? V - a.v0 : s.piece);
+    // Fewer rows than a block's 128 are loaded where there are fewer: the MMA reads whatever the stage holds behind
+    // them, into lanes that nothing reads back.
+    a.a_rows = M < 128 ? (M + 7) / 8 * 8 : 128;
+    a.a_second = M > 128;
+    const int mt = s.Mp / TILE;
+    CUtensorMap ta, tb, to;
+    int rc;
+#define MAP(call)                     \
+    do {                              \
+        rc = (call);                  \
+        if (rc != DEER_OK) return rc; \
+    } while (0)
+    if (what == STATS || what == GRAD) {
+        a.n = what == STATS ? s.stats_n : s.grad_n;
+        a.col_tiles = a.tiles = (a.vn + a.n - 1) / a.n;
+        MAP(map_bf16(&ta, s.h, s.Mp, hid, hid, a.a_rows));
+        MAP(map_bf16(&tb, w, V, hid, hid, a.n / 2));
+        to = ta;
+        if (what == STATS) return launch<STATS>(ta, tb, to, a, (long)mt * a.col_tiles, st);
+        MAP(map_bf16(&to, s.g, s.Mp, a.vn, s.piece, 32));
+        return launch<GRAD>(ta, tb, to, a, (long)mt * a.col_tiles, st);
+    }
+    a.n = s.hid_n;
+    a.col_tiles = (hid + a.n - 1) / a.n;
+    if (what == DH) {
+        a.add = piece > 0;
+        // beyond the piece's columns, and its contraction's last step, G reads as zeros
+        MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, a.a_rows));
+        MAP(map_bf16(&tb, w, V, hid, hid, 64));
+        const uint64_t dims[2] = {(uint64_t)hid, (uint64_t)s.slab_tiles * TILE};
+        const uint64_t strides[1] = {(uint64_t)hid * 4};
+        const uint32_t box[2] = {32, 32};
+        MAP(make_map_f32(&to, s.slab, 2, dims, strides, box));
+        return launch<DH>(ta, tb, to, a, (long)s.slab_tiles * a.col_tiles, st);
+    }
+    a.row_tiles = (a.vn + TILE - 1) / TILE;
+    MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, 64));
+    MAP(map_bf16(&tb, s.h, s.Mp, hid, hid, 64));
+    MAP(map_bf16(&to, dw, V, hid, hid, 32));
+#undef MAP
+    return launch<DW>(ta, tb, to, a, (long)a.row_tiles * a.col_tiles, st);
+}
+
+}  // namespace headloss

@@ -457,3 +457,50 @@ class VerifierStackQuant:
         for layer in self.layers:
             layer.store(keep)
         L.deer_kv_commit(self.kvs[0], self.seq_ids, keep, self.cfg.k)
+
+
+class HeadLoss:
+    """The drafter's training losses over its LM head ``w`` [V, hid] (bf16, on the device), for batches of ``rows`` hidden
+    states: cross entropy (Eq. 1-4 of the paper with their row weights) and distillation from a teacher's ``top`` best
+    logits, each with its gradients.  Buffers and workspace are made once; a step is
+
+        loss = head.cross_entropy(h, targets, row_weight)             # f32 [rows]
+        dh, dw = head.backward(grad_loss)                             # gradients of sum(grad_loss * loss)
+
+    after which ``x.backward(dh)`` of the graph that made ``h = x.detach()`` carries on.  Rows without a target (-1) cost
+    nothing, so a shorter batch is padded with them.  ``loss``, ``dh`` and ``dw`` are this object's buffers: the next step
+    overwrites them.  ``grad=False`` leaves room for the forward calls only."""
+
+    def __init__(self, w: torch.Tensor, rows: int, top: int = 1, grad: bool = True):
+        self.w, self.rows, self.top = w, int(rows), int(top)
+        V, hid = w.shape
+        dev, f32 = w.device, torch.float32
+        self.loss = torch.empty(rows, dtype=f32, device=dev)
+        self.lse = torch.empty(rows, dtype=f32, device=dev)
+        self.target_logit = torch.empty(rows, self.top, dtype=f32, device=dev)
+        self.dh = torch.empty(rows, hid, dtype=torch.bfloat16, device=dev) if grad else None
+        self.dw = torch.empty_like(w) if grad else None
+        self.ws = _ws(max(L.deer_lmhead_loss_workspace_bytes(rows, hid, V, self.top, g) for g in ((False, True) if grad else (False,))), dev)
+        self._step = None
+
+    def cross_entropy(self, h: torch.Tensor, targets: torch.Tensor, row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
+        L.deer_lmhead_loss(h, self.w, targets, self.loss, self.lse, self.target_logit.view(-1)[:self.rows], self.ws, row_weight)
+        self._step = (h, targets, None, 1.0, row_weight)
+        return self.loss
+
+    def distill(self, h: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
+                row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
+        L.deer_lmhead_distill(h, self.w, ids, teacher, temperature, self.loss, self.lse, self.target_logit, self.ws, row_weight)
+        self._step = (h, ids, teacher, temperature, row_weight)
+        return self.loss
+
+    def backward(self, grad_loss: Optional[torch.Tensor] = None, head: bool = True):
+        """(dh, dw) of the latest loss; ``head=False``: the hidden states' alone (a frozen head), dw is None."""
+        assert self._step is not None and self.dh is not None, "backward() follows a loss of an object made with grad=True"
+        h, ids, teacher, temperature, row_weight = self._step
+        dw = self.dw if head else None
+        if teacher is None:
+            L.deer_lmhead_loss_grad(h, self.w, ids, self.lse, self.target_logit.view(-1)[:self.rows], self.dh, dw, self.ws, row_weight, grad_loss)
+        else:
+            L.deer_lmhead_distill_grad(h, self.w, ids, teacher, temperature, self.lse, self.target_logit, self.dh, dw, self.ws, row_weight, grad_loss)
+        return self.dh, dw
