@@ -57,6 +57,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     if (!grad) {
         s.stats_n = tile_columns(mt, V, 32, pairs);
         s.pos = (int*)take((size_t)K * s.Mp * 4);
+        s.z = (float*)take((size_t)K * s.Mp * 4);
         s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * 8);
         s.bytes = at;
         return s;
@@ -100,6 +101,9 @@ struct RowArgs {
 
 __device__ __forceinline__ bool is_live(const RowArgs& a, int m) {
     return a.ids[(size_t)m * a.K] >= 0 && (a.weight == nullptr || a.weight[m] != 0.f);
+}
+__device__ __forceinline__ float row_coef(const RowArgs& a, int m) {
+    return (a.weight ? a.weight[m] : 1.f) * (a.grad ? a.grad[m] : 1.f) * a.tau;
 }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -170,6 +174,7 @@ __device__ __forceinline__ bool log_targets(const RowArgs& a, const List& l, int
 template <bool GRAD>
 __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a) {
     __shared__ int sums[2][ROW_WARPS];
+    __shared__ float tops[ROW_WARPS];
     __shared__ int list_id[ROW_WARPS][MAX_TOP];
     __shared__ float list_t[ROW_WARPS][MAX_TOP];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -177,16 +182,23 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     pdl_wait();
     const int base = blockIdx.x * a.per_block;
     int before = 0, total = 0;
+    float top = 0.f;                           // the largest finite coefficient: what G is relative to
     for (int m = tid; m < a.M; m += ROW_THREADS) {
         const int f = is_live(a, m);
         total += f;
         before += m < base ? f : 0;
+        if (GRAD && f) {
+            const float c = fabsf(row_coef(a, m));
+            if (c < INFINITY) top = fmaxf(top, c);
+        }
     }
     before = warp_sum(before);
     total = warp_sum(total);
+    top = warp_max(top);
     if (lane == 0) {
         sums[0][warp] = before;
         sums[1][warp] = total;
+        tops[warp] = top;
     }
     __syncthreads();
     before = total = 0;
@@ -194,22 +206,29 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     for (int i = 0; i < ROW_WARPS; ++i) {
         before += sums[0][i];
         total += sums[1][i];
+        top = fmaxf(top, tops[i]);
     }
     if (blockIdx.x == 0 && tid == 0) {
         a.s.hdr[HDR_LIVE] = total;
         a.s.hdr[HDR_RANGES] = GRAD ? dh_ranges((total + TILE - 1) / TILE, a.ht, a.steps, a.pairs, a.slab_tiles) : 1;
         a.s.hdr[HDR_GAVE_UP] = 0;
+        a.s.hdr[HDR_SCALE] = __float_as_int(top);
     }
-    const int fill_end = min((total + STEP - 1) / STEP * STEP, a.s.Mp);
+    // what dw's contraction meets behind the live rows is zeros; the second term's rows of G meet a copy of h
+    const int low = GRAD && total <= TWO_TERMS ? low_term(total) : 0;
+    const int fill_end = low ? low : (total + STEP - 1) / STEP * STEP;
     const int chunks = a.hid / 8;                          // 16 bytes each
     for (int g = 0; g < a.per_block; g += 32) {
         const int here = min(32, a.per_block - g);
         const unsigned mask = __ballot_sync(0xffffffffu, lane < here && base + g + lane < a.M && is_live(a, base + g + lane));
         for (int r = warp; r < here; r += ROW_WARPS) {
             const int m = base + g + r;
-            if (m >= total && m < fill_end) {              // places behind the live rows that the last step of dw's contraction meets
+            if (GRAD && m >= total && m < fill_end) {
                 uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)m * a.hid);
-                for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
+                for (int c = lane; c < chunks; c += 32) {
+                    dst[c] = make_uint4(0, 0, 0, 0);
+                    if (low) dst[(size_t)low * chunks + c] = make_uint4(0, 0, 0, 0);
+                }
             }
             if (m >= a.M) continue;
             if (!((mask >> r) & 1u)) {
@@ -223,14 +242,18 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
             }
             const uint4* src = reinterpret_cast<const uint4*>(a.h + (size_t)m * a.hid);
             uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)slot * a.hid);
-            for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+            for (int c = lane; c < chunks; c += 32) {
+                const uint4 x = src[c];
+                dst[c] = x;
+                if (low) dst[(size_t)low * chunks + c] = x;
+            }
 
             const List l(a, m, lane);
             float log_t[MAX_TOP / 32], coef = 0.f, lse = 0.f;
             if (GRAD) {
                 const bool some = log_targets(a, l, m, lane, log_t);
                 lse = a.lse[m];
-                coef = some && !l.beyond ? (a.weight ? a.weight[m] : 1.f) * (a.grad ? a.grad[m] : 1.f) * a.tau : 0.f;
+                coef = some && !l.beyond && top > 0.f ? row_coef(a, m) / top : 0.f;
                 if (lane == 0) {
                     a.s.coef[slot] = coef;
                     a.s.lse2[slot] = lse * LOG2E;
@@ -288,6 +311,15 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
     top = warp_max(top);
     for (int i = lane; i < tiles; i += 32) sum += part[i].y * exp2f((part[i].x - top) * c2);
     float lse = top / a.tau + logf(warp_sum(sum));
+    // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
+    float more = 0.f;
+    for (int e = lane; e < a.K; e += 32) {
+        const int id = a.s.ids[(size_t)e * a.s.Mp + slot];
+        if (id >= a.V || (e > 0 && a.s.ids[(size_t)(e - 1) * a.s.Mp + slot] == id)) continue;
+        const float z = target_logit[(size_t)m * a.K + a.s.pos[(size_t)e * a.s.Mp + slot]];
+        more += expf(z / a.tau - lse) - expf(a.s.z[(size_t)e * a.s.Mp + slot] / a.tau - lse);
+    }
+    lse += log1pf(warp_sum(more));
     if (a.s.hdr[HDR_GAVE_UP]) lse = NAN;
     const List l(a, m, lane);
     float log_t[MAX_TOP / 32], each = 0.f;
@@ -295,10 +327,12 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
 #pragma unroll
     for (int i = 0; i < MAX_TOP / 32; ++i) {
         const int j = i * 32 + lane;
-        if (j < a.K && (j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
         if (j < l.n && l.id[i] < a.V && !(log_t[i] == -INFINITY))
             each += expf(log_t[i]) * (log_t[i] - target_logit[(size_t)m * a.K + j] / a.tau + lse);
     }
+    __syncwarp();
+    for (int j = lane; j < a.K; j += 32)
+        if (j >= l.n || a.ids[(size_t)m * a.K + j] >= a.V) target_logit[(size_t)m * a.K + j] = 0.f;
     each = warp_sum(each);
     if (lane == 0) {
         const float x = (a.weight ? a.weight[m] : 1.f) * (a.tau * a.tau) * each;
@@ -314,21 +348,23 @@ __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, _
     pdl_wait();
     if (m >= a.M) return;
     const int slot = a.s.slot[m], live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
-    const size_t range_rows = (size_t)((live + TILE - 1) / TILE) * TILE;
+    // few live rows: a range's tile holds the two terms' products, 128 rows each
+    const int terms = live <= TWO_TERMS ? 2 : 1;
+    const size_t part_rows = terms == 2 ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
+    const float scale = __int_as_float(a.s.hdr[HDR_SCALE]);
     const bool gave_up = a.s.hdr[HDR_GAVE_UP] != 0;
     __nv_bfloat16* dst = dh + (size_t)m * a.hid;
     for (int c = lane * 8; c < a.hid; c += 256) {
         float v[8] = {};
         if (slot >= 0)
-            for (int r = 0; r < ranges; ++r) {
-                const float4* src = reinterpret_cast<const float4*>(a.s.slab + ((size_t)r * range_rows + slot) * a.hid + c);
+            for (int r = 0; r < ranges * terms; ++r) {
+                const float4* src = reinterpret_cast<const float4*>(a.s.slab + ((size_t)r * part_rows + slot) * a.hid + c);
                 const float4 x = src[0], y = src[1];
                 v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
                 v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
             }
-        if (gave_up)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = NAN;
+        for (int j = 0; j < 8; ++j) v[j] = gave_up ? NAN : v[j] * scale;
         *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
 }

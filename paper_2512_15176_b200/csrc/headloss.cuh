@@ -11,13 +11,17 @@ namespace headloss {
 constexpr int TILE = 256;                  // rows of a product's tile: 128 in each block of a pair
 constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
-constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2;
+constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3;
+// Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in DH, idle
+// then, and the contraction that DW's steps of 64 leave free.  DW sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
+constexpr int TWO_TERMS = 128;
+__host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32; }
 
 enum Product {
     STATS,      // z = h w^T, reduced to (max, sum exp) per row and vocabulary tile, and the listed tokens' z
-    GRAD,       // the same z, as G = coef (exp(z / tau - lse) - t), bf16
-    DH,         // dh = G w, fp32, added up over pieces and ranges
-    DW          // dw = G^T h, bf16
+    GRAD,       // the same z, as G = coef (exp(z / tau - lse) - t), bf16; coef is relative to the largest, HDR_SCALE
+    DH,         // dh / scale = G w, fp32, added up over pieces and ranges
+    DW          // dw = scale G^T h, bf16
 };
 
 // The arrays of one call, all in its workspace.
@@ -27,6 +31,7 @@ struct Space {
     int* row;                  // [Mp]       the row at a place
     int* ids;                  // [K][Mp]    a live row's list by rising id, INT_MAX behind its end
     int* pos;                  // [K][Mp]    where an entry stood in the list            (loss)
+    float* z;                  // [K][Mp]    a listed token's z as the tiles have it      (loss)
     float2* part;              // [Mp][tiles] (max z, sum exp((z - max) / tau))           (loss)
     float* coef;               // [Mp]       what a row's probabilities count            (gradient)
     float* lse2;               // [Mp]       lse log2(e)                                 (gradient)
@@ -49,14 +54,16 @@ struct ProductArgs {
     int col_tiles;             // tiles along the columns (vocabulary or hid)
     int row_tiles;             // DW: tiles along the vocabulary
     int a_rows;                // rows of the 128-row operand one block loads (fewer than 128 only where M is)
-    int a_second;              // whether the second block of a pair has rows
     int Mp, K, tiles;
     int add;                   // DH: a piece behind the first
     float c2;                  // log2(e) / tau
     const int* ids;
     const int* pos;
     const int* row;
+    const __nv_bfloat16* h;
+    const __nv_bfloat16* w;
     float* target_logit;
+    float* z;
     float2* part;
     const float* coef;
     const float* lse2;

@@ -1,6 +1,7 @@
 // The products of the LM head's losses on the tensor cores:
 //
-//   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid
+//   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid; two warps per block beside it
+//                                                   compute the listed tokens' z once more on the CUDA cores
 //   GRAD   G = coef (p - t)          [live][piece]  the same z again, softmax and targets in the epilogue
 //   DH     dh = G w                  [live][hid]    contraction over the piece's vocabulary
 //   DW     dw = G^T h                [piece][hid]   contraction over the live rows
@@ -11,9 +12,16 @@
 // one is computed.  h and G are stored row-major once; where the contraction runs along their rows (DW, and w in DH) the
 // operand is read MN-major: boxes of 64 contraction rows x 64 columns, two of them side by side.
 //
-// G is rounded to bf16 once, as a product of the tensor cores wants it (2^-9 relative to each term, as dh and dw
-// themselves); at a listed token p - t is formed in fp32 first, so that a target the model is sure of keeps its
-// difference.  lse, p and all sums are fp32.
+// G is rounded to bf16 for the products: as much as dh and dw are themselves, and with many rows the errors of different
+// rows are as independent as theirs.  At a listed token p - t is formed in fp32 first, so that a target the model is sure of
+// keeps its difference; coef is taken relative to the call's largest, so that equal rows weigh exactly 1 and a token that the
+// model gives nothing has an exact -1.  With few live rows (TWO_TERMS) a single rounding would show in a whole gradient, and
+// there G is kept as two bf16 terms, which costs no time.  lse, p and all sums are fp32.
+//
+// The tensor cores' accumulation rounds towards zero at every step: z comes out short by 2e-6 of itself at a contraction
+// of 2048, which is all of the loss's error where the target stands out.  Hence the listed tokens' z a second time, as plain
+// fp32 sums (4 % of the products' bytes at lists of 64, and hidden behind them): the loss takes those, and lse is corrected
+// by the difference.
 #include <math.h>
 
 #include "headloss.cuh"
@@ -28,7 +36,8 @@ constexpr int OPERAND = 16384;             // bytes of one operand's share of a 
 constexpr int STAGE_BYTES = 2 * OPERAND;
 constexpr int STAGING = 4 * 2 * 4096;      // two boxes of 32 rows x 128 bytes for each epilogue warp
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
-constexpr int THREADS = 192;
+constexpr int BASE_THREADS = 192, DOT_WARPS = 2;
+__host__ __device__ constexpr int threads_of(int p) { return p == STATS ? BASE_THREADS + 32 * DOT_WARPS : BASE_THREADS; }
 constexpr int ACC = 256;                   // columns of one accumulator
 
 __device__ __forceinline__ float ex2(float x) {
@@ -39,6 +48,9 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* tm, uint32_t src, int x, int y) {
     asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(x), "r"(y)
                  : "memory");
+}
+__device__ __forceinline__ void st_shared_bf16(uint32_t addr, __nv_bfloat16 v) {
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(__bfloat16_as_ushort(v)) : "memory");
 }
 #define TMEM_LD_X1(taddr, r) asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr))
 
@@ -53,12 +65,13 @@ struct Tile {
 };
 template <int P>
 struct List {
-    int mt, ct, live, steps, ranges, n;
+    int mt, ct, live, steps, ranges, n, low;      // low: place of the second term's rows, 0: none
     __device__ __forceinline__ List(const ProductArgs& a) {
         live = a.hdr_in[HDR_LIVE];
         mt = (live + TILE - 1) / TILE;
         ct = a.col_tiles;
         ranges = 1;
+        low = P != STATS && live <= TWO_TERMS ? low_term(live) : 0;
         if (P == STATS || P == GRAD) {
             steps = a.hid / STEP;
             n = mt * ct;
@@ -67,7 +80,7 @@ struct List {
             ranges = a.hdr_in[HDR_RANGES];
             n = mt * ct * ranges;
         } else {
-            steps = (live + STEP - 1) / STEP;
+            steps = ((low ? 2 * low : live) + STEP - 1) / STEP;
             n = a.row_tiles * ct;
         }
     }
@@ -93,6 +106,48 @@ struct List {
         return t;
     }
 };
+
+// z of the listed tokens by plain fp32 sums: a warp takes four entries of a row at a time.
+__device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, int warp, int warps, int lane) {
+    const int groups = (a.K + 3) / 4;
+    for (long i = warp; i < (long)live * groups; i += warps) {
+        const int slot = (int)(i / groups), e0 = (int)(i % groups) * 4;
+        const __nv_bfloat16* w[4];
+        int n = 0;
+        for (; n < 4 && e0 + n < a.K; ++n) {
+            const int id = a.ids[(size_t)(e0 + n) * a.Mp + slot];
+            if (id >= a.V) break;                                          // by rising id: the rest is no token either
+            w[n] = a.w + (size_t)id * a.hid;
+        }
+        for (int j = n; j < 4; ++j) w[j] = n ? w[0] : a.w;
+        if (n == 0) continue;
+        const __nv_bfloat16* h = a.h + (size_t)slot * a.hid;
+        float sum[4][2] = {};
+        for (int c = lane * 8; c < a.hid; c += 256) {
+            const uint4 x = *reinterpret_cast<const uint4*>(h + c);
+            uint4 y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = j < n ? __ldg(reinterpret_cast<const uint4*>(w[j] + c)) : make_uint4(0, 0, 0, 0);
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t ys[4] = {y[j].x, y[j].y, y[j].z, y[j].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    sum[j][0] = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ys[k] << 16), sum[j][0]);
+                    sum[j][1] = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), sum[j][1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float s = sum[j][0] + sum[j][1];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == 0 && j < n) a.target_logit[(size_t)a.row[slot] * a.K + a.pos[(size_t)(e0 + j) * a.Mp + slot]] = s;
+        }
+    }
+}
 
 template <int P>
 __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const List<P>& list, int quarter, int lane, int rank,
@@ -169,7 +224,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 TMEM_LD_X1(taddr + (uint32_t)(col - first), z);
                 tmem_wait_ld();
                 while (next == col) {
-                    a.target_logit[(size_t)a.row[slot] * a.K + a.pos[(size_t)e * a.Mp + slot]] = __uint_as_float(z);
+                    a.z[(size_t)e * a.Mp + slot] = __uint_as_float(z);
                     ++e;
                     next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
                 }
@@ -190,11 +245,18 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
             }
             const int limit = P == GRAD ? a.vn : a.hid;
-            for (int c = 0; c < a.n && col0 + c < limit; c += 64) {
-                if (lane == 0) bulk_wait_read<1>();                       // the store from this box two chunks ago has read it
+            const float scale = P == DW ? __int_as_float(a.hdr_in[HDR_SCALE]) : 1.f;
+            const bool two = P == GRAD && list.low > 0;
+            const bool idle = two && (rank > 0 || quarter * 32 >= list.low);        // no rows of the first term
+            for (int c = 0; c < a.n && col0 + c < limit && !idle; c += 64) {
+                // the store from this box two chunks ago has read it (two terms: both boxes are used at once)
+                if (lane == 0) {
+                    if (two) bulk_wait_read<0>();
+                    else bulk_wait_read<1>();
+                }
                 __syncwarp();
-                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row;
-                stg_i ^= 1;
+                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row, other = 4096u - 2u * 4096u * stg_i;
+                if (!two) stg_i ^= 1;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t v[32];
@@ -212,22 +274,31 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                         if (P == GRAD) {
                             x = coef * ex2(fmaf(x, a.c2, nlse));
                             y = coef * ex2(fmaf(y, a.c2, nlse));
+                            if (!row_ok) x = y = 0.f;                     // places behind the live rows: DW's contraction meets them
+                        } else {
+                            x *= scale;
+                            y *= scale;
                         }
                         o[j] = pack_bf16(x, y);
-                        if (P == GRAD && !row_ok) o[j] = 0;               // places behind the live rows: DW's contraction meets them
+                        if (P == GRAD && two) v[j] = pack_bf16(x - __uint_as_float(o[j] << 16), y - __uint_as_float(o[j] & 0xffff0000u));
                     }
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j)
                         st_shared_v4(b + (((4 * half + j) ^ sw) << 4), o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    if (P == GRAD && two)
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j)
+                            st_shared_v4(b + other + (((4 * half + j) ^ sw) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 }
                 if (P == GRAD) {
                     const int first = a.v0 + col0 + c;
                     while (next < first + 64) {                           // listed tokens: p - t, formed in fp32 beforehand
                         const uint32_t k = (uint32_t)(next - first);
-                        const __nv_bfloat16 val = __float2bfloat16(a.gval[(size_t)e * a.Mp + slot]);
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2),
-                                     "h"(*reinterpret_cast<const uint16_t*>(&val))
-                                     : "memory");
+                        const float val = a.gval[(size_t)e * a.Mp + slot];
+                        const __nv_bfloat16 hi = __float2bfloat16(val), lo = __float2bfloat16(val - __bfloat162float(hi));
+                        const uint32_t at = b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2;
+                        st_shared_bf16(at, hi);
+                        if (two) st_shared_bf16(at + other, lo);
                         ++e;
                         next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
                     }
@@ -237,6 +308,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 const int y = (P == DW ? a.v0 : 0) + t.r * TILE + rank * 128 + quarter * 32;
                 if (lane == 0 && (P == GRAD || y < a.V)) {                // rows and columns beyond the tensor are clipped
                     tma_store_2d(tm_out, box, col0 + c, y);
+                    if (two) tma_store_2d(tm_out, box + other, col0 + c, list.low + quarter * 32);
                     bulk_commit();
                 }
             }
@@ -271,7 +343,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
 }
 
 template <int P>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(P), 1)
 product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_out,
                const ProductArgs a) {
     extern __shared__ unsigned char smem_raw[];
@@ -318,16 +390,17 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         // ---------------- TMA producer (each block: its rows of one operand, its half of the columns of the other) --------
         if (lane == 0) {
             const int half = a.n / 2;                                      // columns of the tile that this block brings
-            const bool has_a = A_MN || leader || a.a_second;
+            // the second block's rows: those behind the first 128, or (DH) the second term
+            const bool second_a = A_MN || list.live > 128 || (P == DH && list.low > 0), has_a = leader || second_a;
             const int b_boxes = B_MN ? (half + 63) / 64 : 1;
             const uint32_t a_bytes = A_MN ? OPERAND : (uint32_t)a.a_rows * 128u;
             const uint32_t b_bytes = B_MN ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u;
-            const uint32_t stage_tx = a_bytes * ((A_MN || a.a_second) ? 2u : 1u) + 2u * b_bytes;
+            const uint32_t stage_tx = a_bytes * (second_a ? 2u : 1u) + 2u * b_bytes;
             int it = 0;
             bool ok = true;
             for (int u = blockIdx.x >> 1; u < list.n && ok; u += pairs) {
                 const Tile t = list.tile(u);
-                const int ra = t.r * TILE + (int)rank * 128, cb = t.c * a.n + (int)rank * half;
+                const int ra = t.r * TILE + (int)rank * (P == DH && list.low > 0 ? list.low : 128), cb = t.c * a.n + (int)rank * half;
                 for (int kb = 0; kb < t.kb; ++kb, ++it) {
                     const int s = it % STAGES, k = (t.k0 + kb) * STEP;
                     if (!mbar_wait(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -379,6 +452,8 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                 if (ok) umma_commit_pair(tfull0 + 8u * buf, 3);
             }
         }
+    } else if (warp >= BASE_THREADS / 32) {
+        if (P == STATS) listed_logits(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - BASE_THREADS / 32, (int)gridDim.x * DOT_WARPS, lane);
     } else {
         epilogue<P>(a, &tm_out, list, warp & 3, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
     }
@@ -412,7 +487,7 @@ static int launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMa
     long pairs = deer_sm_count() / 2;
     if (pairs > most_tiles) pairs = most_tiles;
     DEER_CUDA(cudaFuncSetAttribute(product_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
-    DEER_CUDA(launch_pdl(product_kernel<P>, dim3((unsigned)(2 * pairs)), dim3(THREADS), (size_t)SMEM_BYTES, st, ta, tb, to, a));
+    DEER_CUDA(launch_pdl(product_kernel<P>, dim3((unsigned)(2 * pairs)), dim3(threads_of(P)), (size_t)SMEM_BYTES, st, ta, tb, to, a));
     return DEER_OK;
 }
 
@@ -428,7 +503,10 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
     a.ids = s.ids;
     a.pos = s.pos;
     a.row = s.row;
+    a.h = s.h;
+    a.w = static_cast<const __nv_bfloat16*>(w);
     a.target_logit = target_logit;
+    a.z = s.z;
     a.part = s.part;
     a.coef = s.coef;
     a.lse2 = s.lse2;
@@ -438,7 +516,6 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
     // Fewer rows than a block's 128 are loaded where there are fewer: the MMA reads whatever the stage holds behind
     // them, into lanes that nothing reads back.
     a.a_rows = M < 128 ? (M + 7) / 8 * 8 : 128;
-    a.a_second = M > 128;
     const int mt = s.Mp / TILE;
     CUtensorMap ta, tb, to;
     int rc;
