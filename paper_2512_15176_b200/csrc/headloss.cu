@@ -23,13 +23,13 @@ constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time (more p
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Columns of a tile, a multiple of `unit` up to 256: the one whose tiles over `rows` row tiles and `cols` columns keep
-// the busiest pair of blocks shortest, a tile costing what 32 columns do beside its own (151936 columns at one row tile:
-// 594 tiles of 256 take 74 pairs 9 rounds = 2304 columns, 792 of 192 take 11 = 2112).
-static int tile_columns(long rows, long cols, int unit, int pairs) {
+// the busiest block or pair shortest, a tile costing what 32 columns do beside its own (151936 columns at one row tile:
+// 594 tiles of 256 take 148 blocks 5 rounds = 1280 columns, 731 of 208 take 5 as well = 1040).
+static int tile_columns(long rows, long cols, int unit, int groups) {
     int best = 256;
     long best_cost = LONG_MAX;
     for (int n = 256; n >= 64; n -= unit) {
-        const long cost = (rows * ((cols + n - 1) / n) + pairs - 1) / pairs * (n + 32);
+        const long cost = (rows * ((cols + n - 1) / n) + groups - 1) / groups * (n + 32);
         if (cost < best_cost) {
             best_cost = cost;
             best = n;
@@ -42,7 +42,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     Space s = {};
     const int pairs = deer_sm_count() / 2;
     s.Mp = (M + TILE - 1) / TILE * TILE;
-    const int mt = s.Mp / TILE;
+    const int mt = s.Mp / TILE, groups = M > ONE_BLOCK ? pairs : deer_sm_count();
     size_t at = 0;
     auto take = [&](size_t bytes) {
         char* p = base ? static_cast<char*>(base) + at : nullptr;
@@ -55,7 +55,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.ids = (int*)take((size_t)K * s.Mp * 4);
     s.h = (__nv_bfloat16*)take((size_t)s.Mp * hid * 2);
     if (!grad) {
-        s.stats_n = tile_columns(mt, V, 32, pairs);
+        s.stats_n = tile_columns(mt, V, 16, groups);
         s.pos = (int*)take((size_t)K * s.Mp * 4);
         s.z = (float*)take((size_t)K * s.Mp * 4);
         s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * 8);
@@ -68,7 +68,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.pieces = (int)((V + most - 1) / most);
     s.piece = (int)(((V + s.pieces - 1) / s.pieces + TILE - 1) / TILE * TILE);
     s.pieces = (V + s.piece - 1) / s.piece;
-    s.grad_n = tile_columns(mt, s.piece < V ? s.piece : V, 64, pairs);
+    s.grad_n = tile_columns(mt, s.piece < V ? s.piece : V, 16, groups);
     s.hid_n = tile_columns(1, hid, 64, 1);
     // space for dh's partial sums: whatever number of rows turns out to be live
     const int ht = (hid + s.hid_n - 1) / s.hid_n, steps = (s.piece + STEP - 1) / STEP, cap = mt > pairs ? mt : pairs;
@@ -341,32 +341,32 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
     }
 }
 
-// dh of every row: the partial sums of its ranges in their order, zeros for a dead row.  A warp per row.
+// dh of every row: the partial sums of its ranges in their order, zeros for a dead row.  A thread takes four columns, so that
+// few rows with many ranges still have their loads side by side.
 __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, __nv_bfloat16* dh) {
-    const int lane = threadIdx.x & 31, m = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
     pdl_trigger();
     pdl_wait();
+    const long i = (long)blockIdx.x * ROW_THREADS + threadIdx.x;
+    const int quads = a.hid / 4, m = (int)(i / quads), c = (int)(i % quads) * 4;
     if (m >= a.M) return;
     const int slot = a.s.slot[m], live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
     // few live rows: a range's tile holds the two terms' products, 128 rows each
     const int terms = live <= TWO_TERMS ? 2 : 1;
     const size_t part_rows = terms == 2 ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
-    const float scale = __int_as_float(a.s.hdr[HDR_SCALE]);
-    const bool gave_up = a.s.hdr[HDR_GAVE_UP] != 0;
-    __nv_bfloat16* dst = dh + (size_t)m * a.hid;
-    for (int c = lane * 8; c < a.hid; c += 256) {
-        float v[8] = {};
-        if (slot >= 0)
-            for (int r = 0; r < ranges * terms; ++r) {
-                const float4* src = reinterpret_cast<const float4*>(a.s.slab + ((size_t)r * part_rows + slot) * a.hid + c);
-                const float4 x = src[0], y = src[1];
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-                v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-            }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = gave_up ? NAN : v[j] * scale;
-        *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    const float scale = a.s.hdr[HDR_GAVE_UP] ? NAN : __int_as_float(a.s.hdr[HDR_SCALE]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (slot >= 0) {
+        const float* src = a.s.slab + (size_t)slot * a.hid + c;
+#pragma unroll 8
+        for (int r = 0; r < ranges * terms; ++r) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)r * part_rows * a.hid));
+            v.x += x.x;
+            v.y += x.y;
+            v.z += x.z;
+            v.w += x.w;
+        }
     }
+    *reinterpret_cast<uint2*>(dh + (size_t)m * a.hid + c) = make_uint2(pack_bf16(v.x * scale, v.y * scale), pack_bf16(v.z * scale, v.w * scale));
 }
 
 static int check(const char* call, const void* h, const void* w, const int32_t* ids, int K, float tau, const float* row_weight, int M, int hid, int V) {
@@ -456,7 +456,7 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
         if (rc != DEER_OK) return rc;
     }
     if (dh)
-        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, static_cast<__nv_bfloat16*>(dh)));
+        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((unsigned)(((long)M * hid / 4 + ROW_THREADS - 1) / ROW_THREADS)), dim3(ROW_THREADS), 0, st, a, static_cast<__nv_bfloat16*>(dh)));
     return DEER_OK;
 }
 

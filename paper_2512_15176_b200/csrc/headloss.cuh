@@ -9,6 +9,8 @@
 namespace headloss {
 
 constexpr int TILE = 256;                  // rows of a product's tile: 128 in each block of a pair
+constexpr int ONE_BLOCK = 128;             // up to this many rows STATS and GRAD work by single blocks: a pair would leave half of its
+                                           // lanes empty and the products, not the reading of w, would bound the call
 constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
 constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3;
@@ -68,6 +70,8 @@ struct ProductArgs {
     const float* coef;
     const float* lse2;
     const float* gval;
+    __nv_bfloat16* g;
+    int g_pitch;
 };
 
 // Launches one product of the call: `piece` counts the pieces of the vocabulary (STATS: the whole of it).

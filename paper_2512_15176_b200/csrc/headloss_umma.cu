@@ -31,13 +31,20 @@ using namespace sm100;
 
 namespace headloss {
 
-constexpr int STAGES = 6;
-constexpr int OPERAND = 16384;             // bytes of one operand's share of a stage: 128 rows (columns) x 64 bf16
-constexpr int STAGE_BYTES = 2 * OPERAND;
-constexpr int STAGING = 4 * 2 * 4096;      // two boxes of 32 rows x 128 bytes for each epilogue warp
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
-constexpr int BASE_THREADS = 192, DOT_WARPS = 2;
-__host__ __device__ constexpr int threads_of(int p) { return p == STATS ? BASE_THREADS + 32 * DOT_WARPS : BASE_THREADS; }
+constexpr int BOX = 4096;                  // 32 rows x 128 bytes of a finished tile, as they leave through TMA
+constexpr int DOT_WARPS = 2;
+// What a variant is made of: P the product, CG the blocks that share a tile.
+template <int P, int CG>
+struct Shape {
+    static constexpr int A = 16384;                        // a block's share of an operand's step: 128 rows (columns) x 64 bf16
+    static constexpr int B = 32768 / CG;                   // n columns, or this block's half of them
+    static constexpr int EPI = P == GRAD || P == DW ? 8 : 4;   // epilogue warps, four to 32 x n or two to half of it each
+    static constexpr int STAGING = P == STATS ? 0 : EPI * 2 * BOX;
+    static constexpr int STAGES = (232448 - STAGING - 1024 - 256) / (A + B);
+    static constexpr int SMEM = STAGES * (A + B) + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
+    static constexpr int THREADS = 64 + 32 * EPI + (P == STATS ? 32 * DOT_WARPS : 0);
+    static constexpr int ROWS = 128 * CG;                  // lanes of a tile
+};
 constexpr int ACC = 256;                   // columns of one accumulator
 
 __device__ __forceinline__ float ex2(float x) {
@@ -52,23 +59,29 @@ __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* tm, uint32_
 __device__ __forceinline__ void st_shared_bf16(uint32_t addr, __nv_bfloat16 v) {
     asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(__bfloat16_as_ushort(v)) : "memory");
 }
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 #define TMEM_LD_X1(taddr, r) asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr))
 
-// kind::f16 instruction descriptor: bf16 x bf16 -> fp32, M = 256 across the pair, N = n.
-__device__ __forceinline__ uint32_t idesc_pair(int n, bool a_mn, bool b_mn) {
-    return make_idesc_bf16_pair(n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+// kind::f16 instruction descriptor: bf16 x bf16 -> fp32, M = 128 of each block, N = n.
+template <int CG>
+__device__ __forceinline__ uint32_t idesc_of(int n, bool a_mn, bool b_mn) {
+    return (CG == 2 ? make_idesc_bf16_pair(n) : make_idesc_bf16(n, 0)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
 }
 
 // Tile u of the list: rows and columns of the product, range of the contraction in steps.
 struct Tile {
     int r, c, k0, kb, y;       // y: DH: row of the slabs
 };
-template <int P>
+template <int P, int CG>
 struct List {
     int mt, ct, live, steps, ranges, n, low;      // low: place of the second term's rows, 0: none
     __device__ __forceinline__ List(const ProductArgs& a) {
         live = a.hdr_in[HDR_LIVE];
-        mt = (live + TILE - 1) / TILE;
+        mt = (live + Shape<P, CG>::ROWS - 1) / Shape<P, CG>::ROWS;
         ct = a.col_tiles;
         ranges = 1;
         low = P != STATS && live <= TWO_TERMS ? low_term(live) : 0;
@@ -149,15 +162,17 @@ __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, in
     }
 }
 
-template <int P>
-__device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const List<P>& list, int quarter, int lane, int rank,
+template <int P, int CG>
+__device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const List<P, CG>& list, int warp, int lane, int rank,
                                          uint32_t tmem_base, uint32_t tfull0, uint32_t tempty0, uint32_t staging, volatile int* abort_flag) {
-    const uint32_t stg = staging + (uint32_t)quarter * 8192u, stg_row = (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
+    constexpr int SHARE = Shape<P, CG>::EPI / 4;                           // warps to a quarter of the lanes: they take its columns in turn
+    const int quarter = warp & 3, turn = (warp - 2) >> 2;
+    const uint32_t stg = staging + (uint32_t)(warp - 2) * (2u * BOX), stg_row = (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
     const int lane_row = rank * 128 + quarter * 32 + lane;                 // the thread's row within a tile
-    const int pairs = gridDim.x >> 1;
+    const int groups = gridDim.x / CG;
     uint32_t stg_i = 0;
     int it = 0;
-    for (int u = blockIdx.x >> 1; u < list.n; u += pairs) {
+    for (int u = blockIdx.x / CG; u < list.n; u += groups) {
         const Tile t = list.tile(u);
         if (t.kb == 0 && P != DW) continue;                               // DH: nothing to add; DW without a live row: zeros
         const int buf = it & 1;
@@ -169,7 +184,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             ++it;
         }
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * ACC);
-        const int slot = t.r * TILE + lane_row;                           // STATS, GRAD: place among the live rows
+        const int slot = t.r * Shape<P, CG>::ROWS + lane_row;                           // STATS, GRAD: place among the live rows
         const bool row_ok = slot < list.live;
         const int col0 = t.c * a.n;
 
@@ -248,14 +263,15 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             const float scale = P == DW ? __int_as_float(a.hdr_in[HDR_SCALE]) : 1.f;
             const bool two = P == GRAD && list.low > 0;
             const bool idle = two && (rank > 0 || quarter * 32 >= list.low);        // no rows of the first term
-            for (int c = 0; c < a.n && col0 + c < limit && !idle; c += 64) {
+            for (int c = 64 * turn; c < a.n && col0 + c < limit && !idle; c += 64 * SHARE) {
+                const int wide = min(64, a.n - c);                        // (GRAD: the last chunk may be narrower than a box)
                 // the store from this box two chunks ago has read it (two terms: both boxes are used at once)
                 if (lane == 0) {
                     if (two) bulk_wait_read<0>();
                     else bulk_wait_read<1>();
                 }
                 __syncwarp();
-                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row, other = 4096u - 2u * 4096u * stg_i;
+                const uint32_t box = stg + stg_i * BOX, b = box + stg_row, other = BOX - 2u * BOX * stg_i;
                 if (!two) stg_i ^= 1;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -292,20 +308,32 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 }
                 if (P == GRAD) {
                     const int first = a.v0 + col0 + c;
-                    while (next < first + 64) {                           // listed tokens: p - t, formed in fp32 beforehand
-                        const uint32_t k = (uint32_t)(next - first);
-                        const float val = a.gval[(size_t)e * a.Mp + slot];
-                        const __nv_bfloat16 hi = __float2bfloat16(val), lo = __float2bfloat16(val - __bfloat162float(hi));
-                        const uint32_t at = b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2;
-                        st_shared_bf16(at, hi);
-                        if (two) st_shared_bf16(at + other, lo);
+                    while (next < first + wide) {                         // listed tokens: p - t, formed in fp32 beforehand
+                        if (next >= first) {                              // (the other warp's chunks lie between this one's)
+                            const uint32_t k = (uint32_t)(next - first);
+                            const float val = a.gval[(size_t)e * a.Mp + slot];
+                            const __nv_bfloat16 hi = __float2bfloat16(val), lo = __float2bfloat16(val - __bfloat162float(hi));
+                            const uint32_t at = b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2;
+                            st_shared_bf16(at, hi);
+                            if (two) st_shared_bf16(at + other, lo);
+                        }
                         ++e;
                         next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
                     }
                 }
+                if (P == GRAD && wide < 64) {                             // by plain stores: 32 bytes of a row at a time
+                    __nv_bfloat16* row = a.g + (size_t)(t.r * Shape<P, CG>::ROWS + lane_row) * a.g_pitch + col0 + c;
+                    const int stop = min(wide, a.g_pitch - col0 - c);
+                    for (int k = 0; k < stop; k += 8) {
+                        *reinterpret_cast<uint4*>(row + k) = ld_shared_v4(b + (((uint32_t)(k >> 3) ^ sw) << 4));
+                        if (two) *reinterpret_cast<uint4*>(row + (size_t)list.low * a.g_pitch + k) = ld_shared_v4(b + other + (((uint32_t)(k >> 3) ^ sw) << 4));
+                    }
+                    if (!two) stg_i ^= 1;                                 // no store by TMA has taken this box: it is next again
+                    continue;
+                }
                 fence_proxy_async_smem();
                 __syncwarp();
-                const int y = (P == DW ? a.v0 : 0) + t.r * TILE + rank * 128 + quarter * 32;
+                const int y = (P == DW ? a.v0 : 0) + t.r * Shape<P, CG>::ROWS + rank * 128 + quarter * 32;
                 if (lane == 0 && (P == GRAD || y < a.V)) {                // rows and columns beyond the tensor are clipped
                     tma_store_2d(tm_out, box, col0 + c, y);
                     if (two) tma_store_2d(tm_out, box + other, col0 + c, list.low + quarter * 32);
@@ -316,7 +344,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             for (int c = 0; c < a.n && col0 + c < a.hid; c += 32) {
                 if (lane == 0) bulk_wait_read<1>();
                 __syncwarp();
-                const uint32_t box = stg + stg_i * 4096u, b = box + stg_row;
+                const uint32_t box = stg + stg_i * BOX, b = box + stg_row;
                 stg_i ^= 1;
                 uint32_t v[32];
                 TMEM_LD_X32(taddr + c, v);
@@ -336,27 +364,48 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
         if (computed) {
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_peer(map_to_cta(tempty0 + 8u * buf, 0));
+            if (lane == 0) {
+                if (CG == 2) mbar_arrive_peer(map_to_cta(tempty0 + 8u * buf, 0));
+                else mbar_arrive(tempty0 + 8u * buf);
+            }
         }
     }
     if (lane == 0) bulk_wait<0>();               // the staging area outlives every store that reads it
 }
 
-template <int P>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(P), 1)
+template <int CG>
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
+    if (CG == 2) tma_load_2d_pair(dst, tm, x, y, bar);
+    else tma_load_2d(dst, tm, x, y, bar);
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t accumulate) {
+    if (CG == 2) umma_bf16_ss_pair(d, ad, bd, idesc, accumulate);
+    else umma_bf16_ss(d, ad, bd, idesc, accumulate);
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if (CG == 2) umma_commit_pair(bar, 3);
+    else umma_commit(bar);
+}
+
+template <int P, int CG>
+__global__ void __launch_bounds__(Shape<P, CG>::THREADS, 1)
 product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_out,
                const ProductArgs a) {
+    using S = Shape<P, CG>;
+    constexpr int STAGES = S::STAGES, STAGE_BYTES = S::A + S::B;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + STAGING);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + S::STAGING);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     constexpr bool A_MN = P == DW, B_MN = P == DH || P == DW;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = cluster_ctarank();
+    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
     const bool leader = rank == 0;
-    const int pairs = gridDim.x >> 1;
+    const int groups = gridDim.x / CG;
     const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
@@ -369,55 +418,58 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(tfull0 + 8u * b, 1);
-            mbar_init(tempty0 + 8u * b, 8);      // four epilogue warps in each of the two blocks
+            mbar_init(tempty0 + 8u * b, CG * S::EPI);      // the epilogue warps of all blocks
         }
         *abort_flag = 0;
         mbar_init_fence();
         prefetch_tensormap(&tm_a);
         prefetch_tensormap(&tm_b);
     }
-    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    if (warp == 1) {
+        if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+        else tmem_alloc(smem_u32(tmem_slot), 512);
+    }
     pdl_trigger();
     tcgen05_fence_before();
     __syncthreads();
-    cluster_sync();                              // the peer's barriers exist before anything signals them
+    if (CG == 2) cluster_sync();                 // the peer's barriers exist before anything signals them
     tcgen05_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     pdl_wait();                                  // (the weights too: in training an optimiser step may be what ran before)
-    const List<P> list(a);
+    const List<P, CG> list(a);
 
     if (warp == 0) {
         // ---------------- TMA producer (each block: its rows of one operand, its half of the columns of the other) --------
         if (lane == 0) {
-            const int half = a.n / 2;                                      // columns of the tile that this block brings
+            const int half = a.n / CG;                                     // columns of the tile that this block brings
             // the second block's rows: those behind the first 128, or (DH) the second term
-            const bool second_a = A_MN || list.live > 128 || (P == DH && list.low > 0), has_a = leader || second_a;
+            const bool second_a = CG == 2 && (A_MN || list.live > 128 || (P == DH && list.low > 0)), has_a = leader || second_a;
             const int b_boxes = B_MN ? (half + 63) / 64 : 1;
-            const uint32_t a_bytes = A_MN ? OPERAND : (uint32_t)a.a_rows * 128u;
+            const uint32_t a_bytes = A_MN ? S::A : (uint32_t)a.a_rows * 128u;
             const uint32_t b_bytes = B_MN ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u;
-            const uint32_t stage_tx = a_bytes * (second_a ? 2u : 1u) + 2u * b_bytes;
+            const uint32_t stage_tx = a_bytes * (second_a ? 2u : 1u) + (uint32_t)CG * b_bytes;
             int it = 0;
             bool ok = true;
-            for (int u = blockIdx.x >> 1; u < list.n && ok; u += pairs) {
+            for (int u = blockIdx.x / CG; u < list.n && ok; u += groups) {
                 const Tile t = list.tile(u);
-                const int ra = t.r * TILE + (int)rank * (P == DH && list.low > 0 ? list.low : 128), cb = t.c * a.n + (int)rank * half;
+                const int ra = t.r * S::ROWS + (int)rank * (P == DH && list.low > 0 ? list.low : 128), cb = t.c * a.n + (int)rank * half;
                 for (int kb = 0; kb < t.kb; ++kb, ++it) {
                     const int s = it % STAGES, k = (t.k0 + kb) * STEP;
                     if (!mbar_wait(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
                     if (leader) mbar_expect_tx(full_bar(s), stage_tx);
-                    const uint32_t full = map_to_cta(full_bar(s), 0), sa = smem_base + s * STAGE_BYTES, sb = sa + OPERAND;
+                    const uint32_t full = CG == 2 ? map_to_cta(full_bar(s), 0) : full_bar(s), sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
                     if (A_MN) {
-                        tma_load_2d_pair(sa, &tm_a, ra, k, full);
-                        tma_load_2d_pair(sa + 8192, &tm_a, ra + 64, k, full);
+                        load_2d<CG>(sa, &tm_a, ra, k, full);
+                        load_2d<CG>(sa + 8192, &tm_a, ra + 64, k, full);
                     } else if (has_a) {
-                        tma_load_2d_pair(sa, &tm_a, k, ra, full);
+                        load_2d<CG>(sa, &tm_a, k, ra, full);
                     }
                     if (B_MN) {
                         const int y = P == DH ? a.v0 + k : k;
-                        tma_load_2d_pair(sb, &tm_b, cb, y, full);
-                        if (b_boxes > 1) tma_load_2d_pair(sb + 8192, &tm_b, cb + 64, y, full);
+                        load_2d<CG>(sb, &tm_b, cb, y, full);
+                        if (b_boxes > 1) load_2d<CG>(sb + 8192, &tm_b, cb + 64, y, full);
                     } else {
-                        tma_load_2d_pair(sb, &tm_b, k, a.v0 + cb, full);
+                        load_2d<CG>(sb, &tm_b, k, a.v0 + cb, full);
                     }
                 }
             }
@@ -425,10 +477,10 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     } else if (warp == 1) {
         // ---------------- MMA issuer (first block of the pair) ----------------
         if (leader && lane == 0) {
-            const uint32_t idesc = idesc_pair(a.n, A_MN, B_MN);
+            const uint32_t idesc = idesc_of<CG>(a.n, A_MN, B_MN);
             int it = 0, done = 0;
             bool ok = true;
-            for (int u = blockIdx.x >> 1; u < list.n && ok; u += pairs) {
+            for (int u = blockIdx.x / CG; u < list.n && ok; u += groups) {
                 const Tile t = list.tile(u);
                 if (t.kb == 0) continue;
                 const int buf = done & 1;
@@ -440,22 +492,22 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                     const int s = it % STAGES;
                     if (!mbar_wait(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag)) { ok = false; break; }
                     tcgen05_fence_after();
-                    const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + OPERAND;
+                    const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
                     // K-major: 16 contraction columns are 32 bytes; MN-major: 16 contraction rows are 2048 bytes
                     const uint64_t ad = A_MN ? smem_desc_sw128(sa, 8192, 1024) : smem_desc_sw128_kmajor(sa);
                     const uint64_t bd = B_MN ? smem_desc_sw128(sb, 8192, 1024) : smem_desc_sw128_kmajor(sb);
 #pragma unroll
                     for (int k = 0; k < STEP / 16; ++k)
-                        umma_bf16_ss_pair(d_tmem, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, (kb | k) != 0 ? 1u : 0u);
-                    umma_commit_pair(empty_bar(s), 3);
+                        mma<CG>(d_tmem, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, (kb | k) != 0 ? 1u : 0u);
+                    commit<CG>(empty_bar(s));
                 }
-                if (ok) umma_commit_pair(tfull0 + 8u * buf, 3);
+                if (ok) commit<CG>(tfull0 + 8u * buf);
             }
         }
-    } else if (warp >= BASE_THREADS / 32) {
-        if (P == STATS) listed_logits(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - BASE_THREADS / 32, (int)gridDim.x * DOT_WARPS, lane);
+    } else if (warp >= 2 + S::EPI) {
+        if (P == STATS) listed_logits(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - 2 - S::EPI, (int)gridDim.x * DOT_WARPS, lane);
     } else {
-        epilogue<P>(a, &tm_out, list, warp & 3, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
+        epilogue<P, CG>(a, &tm_out, list, warp, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
     }
 
     // ---- tear-down: neither block leaves while the other may still signal it or read its shared memory ----
@@ -466,11 +518,12 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         for (int i = 0; i < 64; ++i) __nanosleep(10000);
         __syncthreads();
     }
-    cluster_sync();
+    if (CG == 2) cluster_sync();
     if (warp == 1) {
         __syncwarp();
         tcgen05_fence_after();
-        tmem_dealloc_pair(tmem_base, 512);
+        if (CG == 2) tmem_dealloc_pair(tmem_base, 512);
+        else tmem_dealloc(tmem_base, 512);
     }
 }
 
@@ -482,12 +535,13 @@ static int map_bf16(CUtensorMap* tm, const void* base, long rows, long cols, lon
     return make_map_bf16(tm, base, 2, dims, strides, box);
 }
 
-template <int P>
+template <int P, int CG>
 static int launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const ProductArgs& a, long most_tiles, cudaStream_t st) {
-    long pairs = deer_sm_count() / 2;
-    if (pairs > most_tiles) pairs = most_tiles;
-    DEER_CUDA(cudaFuncSetAttribute(product_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
-    DEER_CUDA(launch_pdl(product_kernel<P>, dim3((unsigned)(2 * pairs)), dim3(threads_of(P)), (size_t)SMEM_BYTES, st, ta, tb, to, a));
+    using S = Shape<P, CG>;
+    long groups = deer_sm_count() / CG;
+    if (groups > most_tiles) groups = most_tiles;
+    DEER_CUDA(cudaFuncSetAttribute(product_kernel<P, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+    DEER_CUDA(launch_pdl_cluster(CG, product_kernel<P, CG>, dim3((unsigned)(CG * groups)), dim3(S::THREADS), (size_t)S::SMEM, st, ta, tb, to, a));
     return DEER_OK;
 }
 
@@ -511,6 +565,8 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
     a.coef = s.coef;
     a.lse2 = s.lse2;
     a.gval = s.gval;
+    a.g = s.g;
+    a.g_pitch = s.piece;
     a.v0 = what == STATS ? 0 : piece * s.piece;
     a.vn = what == STATS ? V : (V - a.v0 < s.piece ? V - a.v0 : s.piece);
     // Fewer rows than a block's 128 are loaded where there are fewer: the MMA reads whatever the stage holds behind
@@ -528,11 +584,13 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
         a.n = what == STATS ? s.stats_n : s.grad_n;
         a.col_tiles = a.tiles = (a.vn + a.n - 1) / a.n;
         MAP(map_bf16(&ta, s.h, s.Mp, hid, hid, a.a_rows));
-        MAP(map_bf16(&tb, w, V, hid, hid, a.n / 2));
+        const int cg = M > ONE_BLOCK ? 2 : 1;
+        MAP(map_bf16(&tb, w, V, hid, hid, a.n / cg));
         to = ta;
-        if (what == STATS) return launch<STATS>(ta, tb, to, a, (long)mt * a.col_tiles, st);
+        const long tiles = (long)mt * a.col_tiles;
+        if (what == STATS) return cg == 2 ? launch<STATS, 2>(ta, tb, to, a, tiles, st) : launch<STATS, 1>(ta, tb, to, a, tiles, st);
         MAP(map_bf16(&to, s.g, s.Mp, a.vn, s.piece, 32));
-        return launch<GRAD>(ta, tb, to, a, (long)mt * a.col_tiles, st);
+        return cg == 2 ? launch<GRAD, 2>(ta, tb, to, a, tiles, st) : launch<GRAD, 1>(ta, tb, to, a, tiles, st);
     }
     a.n = s.hid_n;
     a.col_tiles = (hid + a.n - 1) / a.n;
@@ -545,14 +603,14 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
         const uint64_t strides[1] = {(uint64_t)hid * 4};
         const uint32_t box[2] = {32, 32};
         MAP(make_map_f32(&to, s.slab, 2, dims, strides, box));
-        return launch<DH>(ta, tb, to, a, (long)s.slab_tiles * a.col_tiles, st);
+        return launch<DH, 2>(ta, tb, to, a, (long)s.slab_tiles * a.col_tiles, st);
     }
     a.row_tiles = (a.vn + TILE - 1) / TILE;
     MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, 64));
     MAP(map_bf16(&tb, s.h, s.Mp, hid, hid, 64));
     MAP(map_bf16(&to, dw, V, hid, hid, 32));
 #undef MAP
-    return launch<DW>(ta, tb, to, a, (long)a.row_tiles * a.col_tiles, st);
+    return launch<DW, 2>(ta, tb, to, a, (long)a.row_tiles * a.col_tiles, st);
 }
 
 }  // namespace headloss
