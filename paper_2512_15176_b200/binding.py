@@ -575,38 +575,45 @@ def deer_refresh_rows(appended, row_state, stream=None):
     _check(lib().deer_refresh_rows(B, k, _ptr(appended), _ptr(row_state), _stream(stream)))
 
 
-def _on_device(call: str, first: torch.Tensor, *others):
-    """Every operand on the first one's device; that device made current for the call where it is not."""
-    for t in others:
-        if t is not None and t.device != first.device:
-            _refuse(call, "operands on different devices")
-    if not first.is_cuda:
-        _refuse(call, "operands must be on a CUDA device")
-    if _current_device is not None and _current_device() == first.device.index:
-        return _HERE_ALREADY
-    return torch.cuda.device(first.device)
-
-
 _HERE_ALREADY = contextlib.nullcontext()
 
 
-def _rows_of(call: str, h, w):
-    if not (h.dim() == w.dim() == 2 and h.dtype is _BF16 and w.dtype is _BF16 and h.shape[1] == w.shape[1]):
-        _refuse(call, "h must be bf16 [M][hid], w bf16 [V][hid]")
-    return h.shape[0], h.shape[1], w.shape[0]
-
-
-def _of(call: str, dtype, what: str, **operands):
-    """``operands``: name -> (tensor or None, number of elements)."""
-    for name, (t, n) in operands.items():
-        if t is not None and not (t.dtype is dtype and t.numel() == n):
-            _refuse(call, f"{name} must be {what}")
-
-
-def _need(call: str, **operands):
-    for name, t in operands.items():
+def _operands(call: str, *operands):
+    """The operands' addresses (None stays None) and a context in which their device is the current one."""
+    device, at = operands[0].get_device(), []
+    for t in operands:
         if t is None:
-            _refuse(call, f"{name} is required")
+            at.append(None)
+            continue
+        if t.get_device() != device:
+            _refuse(call, "operands on different devices")
+        assert t.is_contiguous(), "tensors passed to libdeer must be contiguous"
+        at.append(t.data_ptr())
+    if device < 0:
+        _refuse(call, "operands must be on a CUDA device")
+    return at, _HERE_ALREADY if _current_device is not None and _current_device() == device else torch.cuda.device(device)
+
+
+def _is(t, dtype, n) -> bool:
+    return t is not None and t.dtype is dtype and t.numel() == n
+
+
+def _may_be(t, dtype, n) -> bool:
+    return t is None or t.dtype is dtype and t.numel() == n
+
+
+def _head_of(call: str, h, w):
+    M, hid = h.shape if h.dim() == 2 else (0, -1)
+    V, hid_w = w.shape if w.dim() == 2 else (0, -2)
+    if hid != hid_w or h.dtype is not _BF16 or w.dtype is not _BF16:
+        _refuse(call, "h must be bf16 [M][hid], w bf16 [V][hid]")
+    return M, hid, V
+
+
+def _top_of(call: str, M: int, ids, teacher):
+    if ids is None or teacher is None or ids.dim() != 2 or ids.shape != teacher.shape or ids.shape[0] != M or ids.dtype is not _I32 or teacher.dtype is not _F32:
+        _refuse(call, "ids must be int32 [M][K], with f32 [M][K] beside them")
+    return ids.shape[1]
 
 
 def _bytes_of(workspace) -> int:
@@ -619,69 +626,65 @@ def deer_lmhead_loss_workspace_bytes(M, hid, V, K=1, grad=False) -> int:
 
 def deer_lmhead_loss(h, w, targets, loss, lse, target_logit, workspace, row_weight=None, stream=None):
     call = "deer_lmhead_loss"
-    M, hid, V = _rows_of(call, h, w)
-    _need(call, targets=targets, loss=loss, lse=lse, target_logit=target_logit)
-    _of(call, _I32, "int32 [M]", targets=(targets, M))
-    _of(call, _F32, "f32 [M]", row_weight=(row_weight, M), loss=(loss, M), lse=(lse, M), target_logit=(target_logit, M))
-    with _on_device(call, h, w, targets, loss, lse, target_logit, workspace, row_weight):
-        _check(lib().deer_lmhead_loss(_ptr(h), _ptr(w), _ptr(targets), _ptr(row_weight), M, hid, V, _ptr(loss), _ptr(lse), _ptr(target_logit),
-                                      _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+    M, hid, V = _head_of(call, h, w)
+    if not (_is(targets, _I32, M) and _is(loss, _F32, M) and _is(lse, _F32, M) and _is(target_logit, _F32, M) and _may_be(row_weight, _F32, M)):
+        _refuse(call, "targets must be int32 [M]; loss, lse, target_logit and row_weight f32 [M]")
+    (h, w, targets, row_weight, loss, lse, target_logit, ws), there = _operands(call, h, w, targets, row_weight, loss, lse, target_logit, workspace)
+    with there:
+        _check(lib().deer_lmhead_loss(h, w, targets, row_weight, M, hid, V, loss, lse, target_logit, ws, _bytes_of(workspace), _stream(stream)))
 
 
 def deer_lmhead_loss_grad(h, w, targets, lse, target_logit, dh, dw, workspace, row_weight=None, grad_loss=None, stream=None):
     call = "deer_lmhead_loss_grad"
-    M, hid, V = _rows_of(call, h, w)
-    _need(call, targets=targets, lse=lse, target_logit=target_logit)
-    _of(call, _I32, "int32 [M]", targets=(targets, M))
-    _of(call, _F32, "f32 [M]", row_weight=(row_weight, M), grad_loss=(grad_loss, M), lse=(lse, M), target_logit=(target_logit, M))
-    _of(call, _BF16, "bf16 of h's (dh) or w's (dw) size", dh=(dh, M * hid), dw=(dw, V * hid))
-    with _on_device(call, h, w, targets, lse, target_logit, dh, dw, workspace, row_weight, grad_loss):
-        _check(lib().deer_lmhead_loss_grad(_ptr(h), _ptr(w), _ptr(targets), _ptr(row_weight), _ptr(grad_loss), _ptr(lse), _ptr(target_logit),
-                                           M, hid, V, _ptr(dh), _ptr(dw), _ptr(workspace), _bytes_of(workspace), _stream(stream)))
-
-
-def _top_of(call: str, M: int, ids, teacher):
-    _need(call, ids=ids, teacher=teacher)
-    if not (ids.dim() == teacher.dim() == 2 and ids.dtype is _I32 and teacher.dtype is _F32 and ids.shape == teacher.shape and ids.shape[0] == M):
-        _refuse(call, "ids must be int32 [M][K], teacher f32 [M][K]")
-    return ids.shape[1]
+    M, hid, V = _head_of(call, h, w)
+    if not (_is(targets, _I32, M) and _is(lse, _F32, M) and _is(target_logit, _F32, M) and _may_be(row_weight, _F32, M) and _may_be(grad_loss, _F32, M)):
+        _refuse(call, "targets must be int32 [M]; lse, target_logit, row_weight and grad_loss f32 [M]")
+    if not (_may_be(dh, _BF16, M * hid) and _may_be(dw, _BF16, V * hid)):
+        _refuse(call, "dh must be bf16 [M][hid], dw bf16 [V][hid]")
+    (h, w, targets, row_weight, grad_loss, lse, target_logit, dh, dw, ws), there = _operands(call, h, w, targets, row_weight, grad_loss, lse,
+                                                                                            target_logit, dh, dw, workspace)
+    with there:
+        _check(lib().deer_lmhead_loss_grad(h, w, targets, row_weight, grad_loss, lse, target_logit, M, hid, V, dh, dw, ws, _bytes_of(workspace),
+                                           _stream(stream)))
 
 
 def deer_lmhead_distill(h, w, ids, teacher, temperature, loss, lse, target_logit, workspace, row_weight=None, stream=None):
     call = "deer_lmhead_distill"
-    M, hid, V = _rows_of(call, h, w)
+    M, hid, V = _head_of(call, h, w)
     K = _top_of(call, M, ids, teacher)
-    _need(call, loss=loss, lse=lse, target_logit=target_logit)
-    _of(call, _F32, "f32 [M] (target_logit: [M][K])", row_weight=(row_weight, M), loss=(loss, M), lse=(lse, M), target_logit=(target_logit, M * K))
-    with _on_device(call, h, w, ids, teacher, loss, lse, target_logit, workspace, row_weight):
-        _check(lib().deer_lmhead_distill(_ptr(h), _ptr(w), _ptr(ids), _ptr(teacher), K, float(temperature), _ptr(row_weight), M, hid, V,
-                                         _ptr(loss), _ptr(lse), _ptr(target_logit), _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+    if not (_is(loss, _F32, M) and _is(lse, _F32, M) and _is(target_logit, _F32, M * K) and _may_be(row_weight, _F32, M)):
+        _refuse(call, "loss, lse and row_weight must be f32 [M], target_logit f32 [M][K]")
+    (h, w, ids, teacher, row_weight, loss, lse, target_logit, ws), there = _operands(call, h, w, ids, teacher, row_weight, loss, lse, target_logit, workspace)
+    with there:
+        _check(lib().deer_lmhead_distill(h, w, ids, teacher, K, temperature, row_weight, M, hid, V, loss, lse, target_logit, ws, _bytes_of(workspace),
+                                         _stream(stream)))
 
 
 def deer_lmhead_distill_grad(h, w, ids, teacher, temperature, lse, target_logit, dh, dw, workspace, row_weight=None, grad_loss=None,
                              stream=None):
     call = "deer_lmhead_distill_grad"
-    M, hid, V = _rows_of(call, h, w)
+    M, hid, V = _head_of(call, h, w)
     K = _top_of(call, M, ids, teacher)
-    _need(call, lse=lse, target_logit=target_logit)
-    _of(call, _F32, "f32 [M] (target_logit: [M][K])", row_weight=(row_weight, M), grad_loss=(grad_loss, M), lse=(lse, M),
-        target_logit=(target_logit, M * K))
-    _of(call, _BF16, "bf16 of h's (dh) or w's (dw) size", dh=(dh, M * hid), dw=(dw, V * hid))
-    with _on_device(call, h, w, ids, teacher, lse, target_logit, dh, dw, workspace, row_weight, grad_loss):
-        _check(lib().deer_lmhead_distill_grad(_ptr(h), _ptr(w), _ptr(ids), _ptr(teacher), K, float(temperature), _ptr(row_weight),
-                                              _ptr(grad_loss), _ptr(lse), _ptr(target_logit), M, hid, V, _ptr(dh), _ptr(dw), _ptr(workspace),
+    if not (_is(lse, _F32, M) and _is(target_logit, _F32, M * K) and _may_be(row_weight, _F32, M) and _may_be(grad_loss, _F32, M)):
+        _refuse(call, "lse, row_weight and grad_loss must be f32 [M], target_logit f32 [M][K]")
+    if not (_may_be(dh, _BF16, M * hid) and _may_be(dw, _BF16, V * hid)):
+        _refuse(call, "dh must be bf16 [M][hid], dw bf16 [V][hid]")
+    (h, w, ids, teacher, row_weight, grad_loss, lse, target_logit, dh, dw, ws), there = _operands(call, h, w, ids, teacher, row_weight, grad_loss, lse,
+                                                                                                 target_logit, dh, dw, workspace)
+    with there:
+        _check(lib().deer_lmhead_distill_grad(h, w, ids, teacher, K, temperature, row_weight, grad_loss, lse, target_logit, M, hid, V, dh, dw, ws,
                                               _bytes_of(workspace), _stream(stream)))
 
 
 def deer_top_logits(logits, ids, values, stream=None):
     call = "deer_top_logits"
-    if not (logits.dim() == 2 and logits.dtype is _F32):
+    if logits.dim() != 2 or logits.dtype is not _F32:
         _refuse(call, "logits must be f32 [M][V]")
     M, V = logits.shape
-    if not (ids.dim() == values.dim() == 2 and ids.dtype is _I32 and values.dtype is _F32 and ids.shape == values.shape and ids.shape[0] == M):
-        _refuse(call, "ids must be int32 [M][K], values f32 [M][K]")
-    with _on_device(call, logits, ids, values):
-        _check(lib().deer_top_logits(M, V, _ptr(logits), ids.shape[1], _ptr(ids), _ptr(values), _stream(stream)))
+    K = _top_of(call, M, ids, values)
+    (logits, ids, values), there = _operands(call, logits, ids, values)
+    with there:
+        _check(lib().deer_top_logits(M, V, logits, K, ids, values, _stream(stream)))
 
 
 def deer_verify_step_host(kv: KVCache, dev: deer_step_dev, w, q_host, k_blk_host, v_blk_host, h_host, draft_ids_host,

@@ -21,6 +21,7 @@ namespace headloss {
 constexpr int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
 constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time (more pieces: more part-filled waves; fewer: more memory)
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f, LN2_LOW = (float)(0.6931471805599453 - (double)LN2);
 
 // Columns of a tile, a multiple of `unit` up to 256: the one whose tiles over `rows` row tiles and `cols` columns keep
 // the busiest block or pair shortest, a tile costing what 32 columns do beside its own (151936 columns at one row tile:
@@ -70,12 +71,9 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.pieces = (V + s.piece - 1) / s.piece;
     s.grad_n = tile_columns(mt, s.piece < V ? s.piece : V, 16, groups);
     s.hid_n = tile_columns(1, hid, 64, 1);
-    // space for dh's partial sums: whatever number of rows turns out to be live
-    const int ht = (hid + s.hid_n - 1) / s.hid_n, steps = (s.piece + STEP - 1) / STEP, cap = mt > pairs ? mt : pairs;
-    for (int i = 1; i <= mt; ++i) {
-        const int tiles = i * dh_ranges(i, ht, steps, pairs, cap);
-        if (tiles > s.slab_tiles) s.slab_tiles = tiles;
-    }
+    // space for dh's partial sums: as many ranges as two rounds of tiles take
+    const int ht = (hid + s.hid_n - 1) / s.hid_n;
+    s.slab_tiles = 2 * pairs / ht > mt ? 2 * pairs / ht : mt;
     s.coef = (float*)take((size_t)s.Mp * 4);
     s.lse2 = (float*)take((size_t)s.Mp * 4);
     s.gval = (float*)take((size_t)K * s.Mp * 4);
@@ -95,13 +93,11 @@ struct RowArgs {
     const float* lse;            // [M]                             (loss: out; gradient: in)
     const float* target_logit;   // [M][K]
     float tau;
-    int ht, steps, pairs, slab_tiles;
+    int ht, steps, dw_tiles, pairs, slab_tiles;
     Space s;
 };
 
-__device__ __forceinline__ bool is_live(const RowArgs& a, int m) {
-    return a.ids[(size_t)m * a.K] >= 0 && (a.weight == nullptr || a.weight[m] != 0.f);
-}
+__device__ __forceinline__ bool is_live(const RowArgs& a, int m) { return is_live(a.ids, a.weight, a.K, m); }
 __device__ __forceinline__ float row_coef(const RowArgs& a, int m) {
     return (a.weight ? a.weight[m] : 1.f) * (a.grad ? a.grad[m] : 1.f) * a.tau;
 }
@@ -117,18 +113,52 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 __device__ __forceinline__ int warp_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }
 
+// Ranges that dh's contraction is cut into: its tiles share `pairs` pairs of blocks with dw's, which even out what they
+// leave.  The count with the shortest run, ranges of four steps at least, as many as there is space for their partial sums.
+// The lanes of a warp try one count each.
+__device__ int dh_ranges(const RowArgs& a, int live, int lane) {
+    const int mt = (live + TILE - 1) / TILE;
+    if (mt == 0) return 1;
+    const int dw_steps = ((live <= TWO_TERMS ? 2 * low_term(live) : live) + STEP - 1) / STEP, most = a.slab_tiles / mt;
+    const uint64_t dw_cost = (uint64_t)a.dw_tiles * dw_tile_cost(dw_steps);
+    uint64_t best = ~uint64_t(0);              // cost, then the count
+    for (int s = 1 + lane; s <= most && (s == 1 || s * 4 <= a.steps); s += 32) {
+        const uint32_t c = (uint32_t)dh_tile_cost(a.steps, s), n = (uint32_t)(mt * a.ht) * s;
+        const uint64_t longest = (uint64_t)((n + a.pairs - 1) / a.pairs) * a.pairs * c, all = (uint64_t)n * c + dw_cost;
+        const uint64_t cost = (longest > all ? longest : all) << 16 | (uint32_t)s;
+        if (cost < best) best = cost;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const uint64_t other = __shfl_xor_sync(0xffffffffu, best, o);
+        if (other < best) best = other;
+    }
+    return (int)(best & 0xffff);
+}
+
 // A warp's view of one row's list: lane l holds entries l, l + 32, ...
 struct List {
     int n;                       // entries in front of the first negative id
     bool beyond;                 // an id of V or more among them
     int id[MAX_TOP / 32];
-    __device__ __forceinline__ List(const RowArgs& a, int m, int lane) {
-        n = a.K;
-        int out = 0;
+    float log_t[MAX_TOP / 32];   // the teacher's logits; after targets(): log t, -inf behind the list's end
+    float z[MAX_TOP / 32];       // target_logit
+    // Only loads, none of which waits for another.
+    __device__ __forceinline__ void load(const RowArgs& a, const float* target_logit, int m, int lane) {
 #pragma unroll
         for (int i = 0; i < MAX_TOP / 32; ++i) {
             const int j = i * 32 + lane;
-            id[i] = j < a.K ? a.ids[(size_t)m * a.K + j] : -1;
+            const size_t at = (size_t)m * a.K + j;
+            id[i] = j < a.K ? a.ids[at] : -1;
+            log_t[i] = j < a.K && a.teacher ? a.teacher[at] : 0.f;
+            z[i] = j < a.K && target_logit ? target_logit[at] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void find_end(const RowArgs& a, int lane) {
+        n = a.K;
+        bool out = false;
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) {
             const unsigned end = __ballot_sync(0xffffffffu, id[i] < 0);
             if (end && i * 32 + __ffs(end) - 1 < n) n = i * 32 + __ffs(end) - 1;
         }
@@ -136,37 +166,31 @@ struct List {
         for (int i = 0; i < MAX_TOP / 32; ++i) out |= i * 32 + lane < n && id[i] >= a.V;
         beyond = __any_sync(0xffffffffu, out);
     }
-};
-
-// log t of a list's entries: the log-softmax of teacher / tau over the list, 0 for a list without a teacher.  False: the
-// list holds no entry above -inf, so that there is no distribution (the row then has neither loss nor gradient).
-__device__ __forceinline__ bool log_targets(const RowArgs& a, const List& l, int m, int lane, float (&log_t)[MAX_TOP / 32]) {
-    if (!a.teacher) {
+    // log t: the log-softmax of teacher / tau over the list, 0 for a list without a teacher.  False: the list holds no entry
+    // above -inf, so that there is no distribution (the row then has neither loss nor gradient).
+    __device__ __forceinline__ bool targets(const RowArgs& a, int lane) {
+        float top = -INFINITY, sum = 0.f;
+        bool some = false;
 #pragma unroll
-        for (int i = 0; i < MAX_TOP / 32; ++i) log_t[i] = i * 32 + lane < l.n ? 0.f : -INFINITY;
+        for (int i = 0; i < MAX_TOP / 32; ++i) {
+            if (i * 32 + lane >= n) log_t[i] = -INFINITY;
+            some |= !(log_t[i] == -INFINITY);
+            top = fmaxf(top, log_t[i]);
+        }
+        if (!a.teacher) return true;
+        top = warp_max(top);
+        if (!__any_sync(0xffffffffu, some)) return false;
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) {
+            log_t[i] = (log_t[i] - top) / a.tau;           // (NaN where the teacher's is, or the largest is infinite)
+            if (i * 32 + lane < n) sum += expf(log_t[i]);
+        }
+        const float log_sum = logf(warp_sum(sum));
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i) log_t[i] -= log_sum;
         return true;
     }
-    float top = -INFINITY, sum = 0.f;
-    bool some = false;
-#pragma unroll
-    for (int i = 0; i < MAX_TOP / 32; ++i) {
-        const int j = i * 32 + lane;
-        log_t[i] = j < l.n ? a.teacher[(size_t)m * a.K + j] / a.tau : -INFINITY;
-        some |= !(log_t[i] == -INFINITY);
-        top = fmaxf(top, log_t[i]);
-    }
-    top = warp_max(top);
-    if (!__any_sync(0xffffffffu, some)) return false;
-#pragma unroll
-    for (int i = 0; i < MAX_TOP / 32; ++i) {
-        log_t[i] -= top;                                   // (NaN where the teacher's is, or the largest is infinite)
-        if (i * 32 + lane < l.n) sum += expf(log_t[i]);
-    }
-    const float log_sum = logf(warp_sum(sum));
-#pragma unroll
-    for (int i = 0; i < MAX_TOP / 32; ++i) log_t[i] -= log_sum;
-    return true;
-}
+};
 
 // Moves the live rows together and lists their tokens by rising id.  A block takes `per_block` rows and counts the live
 // ones among all rows itself (M flags from L2: less than the launch of a kernel that counts); a warp takes a row.
@@ -181,15 +205,29 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     pdl_trigger();
     pdl_wait();
     const int base = blockIdx.x * a.per_block;
+    // what a row brings is on its way one row ahead, the first one's beside the counting
+    const int chunks = a.hid / 8;                          // 16 bytes each
+    List l;
+    float lse = 0.f;
+    uint4 x[4];
+    auto load_row = [&](int m) {
+        if (m >= a.M) return;
+        l.load(a, a.target_logit, m, lane);
+        if (GRAD) lse = a.lse[m];
+        const uint4* src = reinterpret_cast<const uint4*>(a.h + (size_t)m * a.hid);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = lane + 32 * i < chunks ? src[lane + 32 * i] : make_uint4(0, 0, 0, 0);
+    };
+    load_row(base + warp);
     int before = 0, total = 0;
     float top = 0.f;                           // the largest finite coefficient: what G is relative to
     for (int m = tid; m < a.M; m += ROW_THREADS) {
         const int f = is_live(a, m);
         total += f;
         before += m < base ? f : 0;
-        if (GRAD && f) {
+        if (GRAD) {
             const float c = fabsf(row_coef(a, m));
-            if (c < INFINITY) top = fmaxf(top, c);
+            if (f && c < INFINITY) top = fmaxf(top, c);
         }
     }
     before = warp_sum(before);
@@ -210,14 +248,16 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     }
     if (blockIdx.x == 0 && tid == 0) {
         a.s.hdr[HDR_LIVE] = total;
-        a.s.hdr[HDR_RANGES] = GRAD ? dh_ranges((total + TILE - 1) / TILE, a.ht, a.steps, a.pairs, a.slab_tiles) : 1;
         a.s.hdr[HDR_GAVE_UP] = 0;
         a.s.hdr[HDR_SCALE] = __float_as_int(top);
+    }
+    if (GRAD && blockIdx.x == 0 && warp == ROW_WARPS - 1) {
+        const int ranges = dh_ranges(a, total, lane);
+        if (lane == 0) a.s.hdr[HDR_RANGES] = ranges;
     }
     // what dw's contraction meets behind the live rows is zeros; the second term's rows of G meet a copy of h
     const int low = GRAD && total <= TWO_TERMS ? low_term(total) : 0;
     const int fill_end = low ? low : (total + STEP - 1) / STEP * STEP;
-    const int chunks = a.hid / 8;                          // 16 bytes each
     for (int g = 0; g < a.per_block; g += 32) {
         const int here = min(32, a.per_block - g);
         const unsigned mask = __ballot_sync(0xffffffffu, lane < here && base + g + lane < a.M && is_live(a, base + g + lane));
@@ -233,37 +273,42 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
             if (m >= a.M) continue;
             if (!((mask >> r) & 1u)) {
                 if (lane == 0) a.s.slot[m] = -1;
+                load_row(m + ROW_WARPS);
                 continue;
             }
             const int slot = before + __popc(mask & ((1u << r) - 1u));
+            l.find_end(a, lane);
+            float coef = 0.f;
+            if (GRAD) {
+                const bool some = l.targets(a, lane);
+                coef = some && !l.beyond && top > 0.f ? row_coef(a, m) / top : 0.f;
+            }
             if (lane == 0) {
                 a.s.slot[m] = slot;
                 a.s.row[slot] = m;
-            }
-            const uint4* src = reinterpret_cast<const uint4*>(a.h + (size_t)m * a.hid);
-            uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)slot * a.hid);
-            for (int c = lane; c < chunks; c += 32) {
-                const uint4 x = src[c];
-                dst[c] = x;
-                if (low) dst[(size_t)low * chunks + c] = x;
-            }
-
-            const List l(a, m, lane);
-            float log_t[MAX_TOP / 32], coef = 0.f, lse = 0.f;
-            if (GRAD) {
-                const bool some = log_targets(a, l, m, lane, log_t);
-                lse = a.lse[m];
-                coef = some && !l.beyond && top > 0.f ? row_coef(a, m) / top : 0.f;
-                if (lane == 0) {
+                if (GRAD) {
                     a.s.coef[slot] = coef;
                     a.s.lse2[slot] = lse * LOG2E;
                 }
+            }
+            const uint4* src = reinterpret_cast<const uint4*>(a.h + (size_t)m * a.hid);
+            uint4* dst = reinterpret_cast<uint4*>(a.s.h + (size_t)slot * a.hid);
+            for (int c0 = lane; c0 < chunks; c0 += 128) {
+                if (c0 >= 128)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = c0 + 32 * i < chunks ? src[c0 + 32 * i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c0 + 32 * i < chunks) {
+                        dst[c0 + 32 * i] = x[i];
+                        if (low) dst[(size_t)low * chunks + c0 + 32 * i] = x[i];
+                    }
             }
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < MAX_TOP / 32; ++i) {
                 list_id[warp][i * 32 + lane] = l.id[i];
-                if (GRAD) list_t[warp][i * 32 + lane] = expf(log_t[i]);
+                if (GRAD) list_t[warp][i * 32 + lane] = expf(l.log_t[i]);
             }
             __syncwarp();
 #pragma unroll
@@ -272,72 +317,81 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
                 if (j >= a.K) continue;
                 int place = j;
                 float t = 0.f;                             // the token's probability, wherever the list names it
+                bool before_too = false;                   // listed before
                 if (j < l.n) {
                     place = 0;
+#pragma unroll 4
                     for (int o = 0; o < l.n; ++o) {
                         const int other = list_id[warp][o];
-                        place += other < l.id[i] || (other == l.id[i] && o < j);
-                        if (GRAD && other == l.id[i]) t += list_t[warp][o];
+                        const bool same = other == l.id[i];
+                        place += other < l.id[i] || (same && o < j);
+                        before_too |= same && o < j;
+                        if (GRAD && same) t += list_t[warp][o];
                     }
                 }
                 const size_t at = (size_t)place * a.s.Mp + slot;
                 a.s.ids[at] = j < l.n ? l.id[i] : INT_MAX;
-                if (!GRAD) a.s.pos[at] = j;
-                if (GRAD && j < l.n) {
-                    const float z = a.target_logit[(size_t)m * a.K + j];
-                    a.s.gval[at] = coef == 0.f ? 0.f : coef * (expf(z / a.tau - lse) - t);
-                }
+                if (!GRAD) a.s.pos[at] = before_too ? ~j : j;
+                if (GRAD && j < l.n) a.s.gval[at] = coef == 0.f ? 0.f : coef * (expf(l.z[i] / a.tau - lse) - t);
             }
+            load_row(m + ROW_WARPS);
         }
         before += __popc(mask);
     }
 }
 
 // lse and loss of every row from its tiles' (max, sum exp): a warp per row.
-__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int tiles, float c2, float* loss, float* lse_out, float* target_logit) {
+__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int tiles, float c2, float c2_low, float* loss, float* lse_out, float* target_logit) {
     const int lane = threadIdx.x & 31, m = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
     pdl_trigger();
     pdl_wait();
     if (m >= a.M) return;
-    const int slot = a.s.slot[m];
-    if (slot < 0) {
-        for (int j = lane; j < a.K; j += 32) target_logit[(size_t)m * a.K + j] = 0.f;
-        if (lane == 0) loss[m] = lse_out[m] = 0.f;
-        return;
-    }
-    const float2* part = a.s.part + (size_t)slot * tiles;
-    float top = -INFINITY, sum = 0.f;
-    for (int i = lane; i < tiles; i += 32) top = fmaxf(top, part[i].x);
-    top = warp_max(top);
-    for (int i = lane; i < tiles; i += 32) sum += part[i].y * exp2f((part[i].x - top) * c2);
-    float lse = top / a.tau + logf(warp_sum(sum));
-    // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
-    float more = 0.f;
-    for (int e = lane; e < a.K; e += 32) {
-        const int id = a.s.ids[(size_t)e * a.s.Mp + slot];
-        if (id >= a.V || (e > 0 && a.s.ids[(size_t)(e - 1) * a.s.Mp + slot] == id)) continue;
-        const float z = target_logit[(size_t)m * a.K + a.s.pos[(size_t)e * a.s.Mp + slot]];
-        more += expf(z / a.tau - lse) - expf(a.s.z[(size_t)e * a.s.Mp + slot] / a.tau - lse);
-    }
-    lse += log1pf(warp_sum(more));
-    if (a.s.hdr[HDR_GAVE_UP]) lse = NAN;
-    const List l(a, m, lane);
-    float log_t[MAX_TOP / 32], each = 0.f;
-    const bool some = log_targets(a, l, m, lane, log_t);
+    const int slot = a.M <= ONE_BLOCK ? (is_live(a, m) ? m : -1) : a.s.slot[m];      // (as STATS took them)
+    List l;
+    l.load(a, target_logit, m, lane);
+    l.find_end(a, lane);
 #pragma unroll
     for (int i = 0; i < MAX_TOP / 32; ++i) {
         const int j = i * 32 + lane;
-        if (j < l.n && l.id[i] < a.V && !(log_t[i] == -INFINITY))
-            each += expf(log_t[i]) * (log_t[i] - target_logit[(size_t)m * a.K + j] / a.tau + lse);
+        if (j < a.K && (slot < 0 || j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
     }
-    __syncwarp();
-    for (int j = lane; j < a.K; j += 32)
-        if (j >= l.n || a.ids[(size_t)m * a.K + j] >= a.V) target_logit[(size_t)m * a.K + j] = 0.f;
+    if (slot < 0) {
+        if (lane == 0) loss[m] = lse_out[m] = 0.f;
+        return;
+    }
+    const bool some = l.targets(a, lane);
+    // in powers of two, relative to the largest of the tiles' references
+    const float2* part = a.s.part + (size_t)slot * tiles;
+    float top = -INFINITY, sum = 0.f;                      // (a lane's, and its sum relative to that)
+#pragma unroll 4
+    for (int i = lane; i < tiles; i += 32) {
+        const float2 p = part[i];
+        const float m2 = fmaxf(top, p.x), shift = m2 == -INFINITY ? 0.f : m2;
+        sum = sum * exp2f(top - shift) + p.y * exp2f(p.x - shift);
+        top = m2;
+    }
+    const float all = warp_max(top);
+    sum = warp_sum(sum * (top == -INFINITY ? 0.f : exp2f(top - all)));
+    // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
+    float more = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        const int j = i * 32 + lane;
+        if (j >= l.n || l.id[i] >= a.V) continue;
+        const float tile_z = a.s.z[(size_t)j * a.s.Mp + slot];
+        l.z[i] = fmaf(l.z[i], c2_low, fmaf(l.z[i], c2, -all));
+        if (!isnan(tile_z)) more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, c2_low, fmaf(tile_z, c2, -all)));
+    }
+    const float log_sum = logf(sum + warp_sum(more));
+    float each = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i)
+        if (i * 32 + lane < l.n && l.id[i] < a.V && !(l.log_t[i] == -INFINITY)) each += expf(l.log_t[i]) * (l.log_t[i] + fmaf(l.z[i], -LN2, log_sum));
     each = warp_sum(each);
     if (lane == 0) {
         const float x = (a.weight ? a.weight[m] : 1.f) * (a.tau * a.tau) * each;
         loss[m] = l.beyond ? NAN : some ? x : 0.f;
-        lse_out[m] = lse;
+        lse_out[m] = fmaf(all, LN2, fmaf(all, LN2_LOW, log_sum));
     }
 }
 
@@ -359,7 +413,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, _
         const float* src = a.s.slab + (size_t)slot * a.hid + c;
 #pragma unroll 8
         for (int r = 0; r < ranges * terms; ++r) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)r * part_rows * a.hid));
+            const float4 x = *reinterpret_cast<const float4*>(src + (size_t)r * part_rows * a.hid);
             v.x += x.x;
             v.y += x.y;
             v.z += x.z;
@@ -369,16 +423,33 @@ __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, _
     *reinterpret_cast<uint2*>(dh + (size_t)m * a.hid + c) = make_uint2(pack_bf16(v.x * scale, v.y * scale), pack_bf16(v.z * scale, v.w * scale));
 }
 
-static int check(const char* call, const void* h, const void* w, const int32_t* ids, int K, float tau, const float* row_weight, int M, int hid, int V) {
+static int check_sizes(const char* call, int K, float tau, int M, int hid, int V) {
     DEER_CHECK_ARG(M >= 0 && V >= 1, DEER_ERR_INVALID_ARG, "%s: M must not be negative, V at least 1", call);
     DEER_CHECK_ARG(M <= (1 << 18) && V <= (1 << 30), DEER_ERR_UNSUPPORTED, "%s: more than 2^18 rows or 2^30 tokens", call);
     DEER_CHECK_ARG(hid >= 64 && hid % 64 == 0 && hid <= 65536, DEER_ERR_UNSUPPORTED, "%s: hid must be a multiple of 64, at most 65536", call);
     DEER_CHECK_ARG(K >= 1 && K <= MAX_TOP, DEER_ERR_UNSUPPORTED, "%s: a list has 1 to %d entries", call, MAX_TOP);
     DEER_CHECK_ARG(tau > 0.f && tau < INFINITY, DEER_ERR_INVALID_ARG, "%s: temperature must be positive and finite", call);
-    DEER_CHECK_ARG(h && w && ids, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
-    DEER_CHECK_ARG(deer_aligned16(h) && deer_aligned16(w), DEER_ERR_INVALID_ARG, "%s: h and w must be 16-byte aligned", call);
-    DEER_CHECK_ARG(deer_aligned4(ids) && deer_aligned4(row_weight), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
     return DEER_OK;
+}
+static int check_pointers(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, bool needs_teacher,
+                          const float* row_weight, const float* lse, const float* target_logit) {
+    DEER_CHECK_ARG(h && w && ids && lse && target_logit && (teacher || !needs_teacher), DEER_ERR_INVALID_ARG, "%s: null pointer", call);
+    DEER_CHECK_ARG(deer_aligned16(h) && deer_aligned16(w), DEER_ERR_INVALID_ARG, "%s: h and w must be 16-byte aligned", call);
+    DEER_CHECK_ARG(deer_aligned4(ids) && deer_aligned4(teacher) && deer_aligned4(row_weight) && deer_aligned4(lse) && deer_aligned4(target_logit),
+                   DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
+    return DEER_OK;
+}
+
+// The kernels by rows run between products that use an SM's whole shared memory: with the same split of its memory they
+// may start beside the end of one, and the SM need not drain to change the split.
+template <typename Kernel>
+static cudaError_t keep_split(Kernel* kernel, bool (&done)[64]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && done[dev])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (dev < 64) done[dev] = e == cudaSuccess;
+    return e;
 }
 
 static RowArgs row_args(const Space& s, const void* h, const int32_t* ids, const float* teacher, int K, float tau, const float* row_weight,
@@ -401,42 +472,47 @@ static unsigned row_blocks(const RowArgs& a) {             // all rows, and the 
     return (unsigned)(((a.M + STEP - 1) / STEP * STEP + a.per_block - 1) / a.per_block);
 }
 
-static int loss_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float tau,
-                     const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit, void* workspace,
-                     size_t workspace_bytes, void* stream) {
-    int rc = check(call, h, w, ids, K, tau, row_weight, M, hid, V);
+static int loss_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, bool needs_teacher, int K,
+                     float tau, const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_sizes(call, K, tau, M, hid, V);
+    if (rc != DEER_OK || M == 0) return rc;
+    rc = check_pointers(call, h, w, ids, teacher, needs_teacher, row_weight, lse, target_logit);
     if (rc != DEER_OK) return rc;
-    DEER_CHECK_ARG(loss && lse && target_logit, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
-    DEER_CHECK_ARG(deer_aligned4(loss) && deer_aligned4(lse) && deer_aligned4(target_logit), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
-    if (M == 0) return DEER_OK;
+    DEER_CHECK_ARG(loss && deer_aligned4(loss), DEER_ERR_INVALID_ARG, "%s: loss is null or misaligned", call);
     const Space s = lay_out(workspace, M, hid, V, K, false);
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
-    const float c2 = LOG2E / tau;
-    DEER_CUDA(launch_pdl(head_rows_kernel<false>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
-    rc = launch_product(STATS, s, w, M, hid, V, K, 0, c2, target_logit, nullptr, st);
+    float c2, c2_low;
+    scale_of(tau, c2, c2_low);
+    static bool rows_set[64] = {}, loss_set[64] = {};
+    DEER_CUDA(keep_split(head_rows_kernel<false>, rows_set));
+    DEER_CUDA(keep_split(head_loss_kernel, loss_set));
+    if (M > ONE_BLOCK) DEER_CUDA(launch_pdl(head_rows_kernel<false>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
+    rc = launch_product(STATS, s, h, w, ids, row_weight, M, hid, V, K, 0, tau, target_logit, false, nullptr, st);
     if (rc != DEER_OK) return rc;
-    DEER_CUDA(launch_pdl(head_loss_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (V + s.stats_n - 1) / s.stats_n, c2,
+    DEER_CUDA(launch_pdl(head_loss_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (V + s.stats_n - 1) / s.stats_n, c2, c2_low,
                          loss, lse, target_logit));
     return DEER_OK;
 }
 
-static int grad_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float tau,
-                     const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid, int V,
-                     void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = check(call, h, w, ids, K, tau, row_weight, M, hid, V);
+static int grad_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, bool needs_teacher, int K,
+                     float tau, const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid,
+                     int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_sizes(call, K, tau, M, hid, V);
     if (rc != DEER_OK) return rc;
-    DEER_CHECK_ARG(lse && target_logit, DEER_ERR_INVALID_ARG, "%s: null pointer", call);
-    DEER_CHECK_ARG(dh || dw, DEER_ERR_INVALID_ARG, "%s: neither dh nor dw is asked for", call);
     DEER_CHECK_ARG(deer_aligned16(dh) && deer_aligned16(dw), DEER_ERR_INVALID_ARG, "%s: dh and dw must be 16-byte aligned", call);
-    DEER_CHECK_ARG(deer_aligned4(lse) && deer_aligned4(target_logit) && deer_aligned4(grad_loss), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {
         if (dw) DEER_CUDA(cudaMemsetAsync(dw, 0, (size_t)V * hid * 2, st));
         return DEER_OK;
     }
+    rc = check_pointers(call, h, w, ids, teacher, needs_teacher, row_weight, lse, target_logit);
+    if (rc != DEER_OK) return rc;
+    DEER_CHECK_ARG(dh || dw, DEER_ERR_INVALID_ARG, "%s: neither dh nor dw is asked for", call);
+    DEER_CHECK_ARG(deer_aligned4(grad_loss), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
     const Space s = lay_out(workspace, M, hid, V, K, true);
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
@@ -446,13 +522,16 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     a.target_logit = target_logit;
     a.ht = (hid + s.hid_n - 1) / s.hid_n;
     a.steps = (s.piece + STEP - 1) / STEP;
+    a.dw_tiles = dw ? (s.piece + TILE - 1) / TILE * a.ht : 0;
     a.pairs = deer_sm_count() / 2;
     a.slab_tiles = s.slab_tiles;
+    static bool rows_set[64] = {}, dh_set[64] = {};
+    DEER_CUDA(keep_split(head_rows_kernel<true>, rows_set));
+    DEER_CUDA(keep_split(head_dh_kernel, dh_set));
     DEER_CUDA(launch_pdl(head_rows_kernel<true>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
     for (int p = 0; p < s.pieces; ++p) {
-        rc = launch_product(GRAD, s, w, M, hid, V, K, p, LOG2E / tau, nullptr, nullptr, st);
-        if (rc == DEER_OK && dh) rc = launch_product(DH, s, w, M, hid, V, K, p, 0.f, nullptr, nullptr, st);
-        if (rc == DEER_OK && dw) rc = launch_product(DW, s, w, M, hid, V, K, p, 0.f, nullptr, dw, st);
+        rc = launch_product(GRAD, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, false, nullptr, st);
+        if (rc == DEER_OK) rc = launch_product(BACK, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, dh != nullptr, dw, st);
         if (rc != DEER_OK) return rc;
     }
     if (dh)
@@ -471,30 +550,28 @@ size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad) 
 
 int deer_lmhead_loss(const void* h, const void* w, const int32_t* targets, const float* row_weight, int M, int hid, int V, float* loss,
                      float* lse, float* target_logit, void* workspace, size_t workspace_bytes, void* stream) {
-    return headloss::loss_call("deer_lmhead_loss", h, w, targets, nullptr, 1, 1.f, row_weight, M, hid, V, loss, lse, target_logit, workspace,
+    return headloss::loss_call("deer_lmhead_loss", h, w, targets, nullptr, false, 1, 1.f, row_weight, M, hid, V, loss, lse, target_logit, workspace,
                                workspace_bytes, stream);
 }
 
 int deer_lmhead_loss_grad(const void* h, const void* w, const int32_t* targets, const float* row_weight, const float* grad_loss,
                           const float* lse, const float* target_logit, int M, int hid, int V, void* dh, void* dw, void* workspace,
                           size_t workspace_bytes, void* stream) {
-    return headloss::grad_call("deer_lmhead_loss_grad", h, w, targets, nullptr, 1, 1.f, row_weight, grad_loss, lse, target_logit, M, hid, V, dh,
+    return headloss::grad_call("deer_lmhead_loss_grad", h, w, targets, nullptr, false, 1, 1.f, row_weight, grad_loss, lse, target_logit, M, hid, V, dh,
                                dw, workspace, workspace_bytes, stream);
 }
 
 int deer_lmhead_distill(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
                         const float* row_weight, int M, int hid, int V, float* loss, float* lse, float* target_logit, void* workspace,
                         size_t workspace_bytes, void* stream) {
-    DEER_CHECK_ARG(teacher && deer_aligned4(teacher), DEER_ERR_INVALID_ARG, "deer_lmhead_distill: teacher is null or misaligned");
-    return headloss::loss_call("deer_lmhead_distill", h, w, ids, teacher, K, temperature, row_weight, M, hid, V, loss, lse, target_logit,
+    return headloss::loss_call("deer_lmhead_distill", h, w, ids, teacher, true, K, temperature, row_weight, M, hid, V, loss, lse, target_logit,
                                workspace, workspace_bytes, stream);
 }
 
 int deer_lmhead_distill_grad(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
                              const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid,
                              int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
-    DEER_CHECK_ARG(teacher && deer_aligned4(teacher), DEER_ERR_INVALID_ARG, "deer_lmhead_distill_grad: teacher is null or misaligned");
-    return headloss::grad_call("deer_lmhead_distill_grad", h, w, ids, teacher, K, temperature, row_weight, grad_loss, lse, target_logit, M, hid,
+    return headloss::grad_call("deer_lmhead_distill_grad", h, w, ids, teacher, true, K, temperature, row_weight, grad_loss, lse, target_logit, M, hid,
                                V, dh, dw, workspace, workspace_bytes, stream);
 }
 

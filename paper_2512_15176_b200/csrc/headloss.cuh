@@ -4,26 +4,28 @@
 // start of the workspace; how many there are is known on the device alone, so every kernel reads it from `hdr`.
 #pragma once
 
+#include <math.h>
+
 #include "common.cuh"
 
 namespace headloss {
 
 constexpr int TILE = 256;                  // rows of a product's tile: 128 in each block of a pair
 constexpr int ONE_BLOCK = 128;             // up to this many rows STATS and GRAD work by single blocks: a pair would leave half of its
-                                           // lanes empty and the products, not the reading of w, would bound the call
+                                           // lanes empty and the products, not the reading of w, would bound the call.  STATS takes
+                                           // the rows as they are then: a dead one costs nothing in a tile that is not full
 constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
 constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3;
-// Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in DH, idle
-// then, and the contraction that DW's steps of 64 leave free.  DW sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
+// Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in dh's product,
+// idle then, and the contraction that the steps of dw's leave free.  That sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
 constexpr int TWO_TERMS = 128;
 __host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32; }
 
 enum Product {
     STATS,      // z = h w^T, reduced to (max, sum exp) per row and vocabulary tile, and the listed tokens' z
     GRAD,       // the same z, as G = coef (exp(z / tau - lse) - t), bf16; coef is relative to the largest, HDR_SCALE
-    DH,         // dh / scale = G w, fp32, added up over pieces and ranges
-    DW          // dw = scale G^T h, bf16
+    BACK        // dh / scale = G w, fp32, added up over pieces and ranges, and dw = scale G^T h, bf16
 };
 
 // The arrays of one call, all in its workspace.
@@ -32,9 +34,9 @@ struct Space {
     int* slot;                 // [M]        place of a row among the live ones, -1: dead
     int* row;                  // [Mp]       the row at a place
     int* ids;                  // [K][Mp]    a live row's list by rising id, INT_MAX behind its end
-    int* pos;                  // [K][Mp]    where an entry stood in the list            (loss)
-    float* z;                  // [K][Mp]    a listed token's z as the tiles have it      (loss)
-    float2* part;              // [Mp][tiles] (max z, sum exp((z - max) / tau))           (loss)
+    int* pos;                  // [K][Mp]    where an entry stood in the list, ~ that of a token listed before    (loss)
+    float* z;                  // [K][Mp]    by the list's order: a token's z as the tiles have it, NaN: listed before  (loss)
+    float2* part;              // [Mp][tiles] (m, sum 2^(z log2(e) / tau - m))            (loss)
     float* coef;               // [Mp]       what a row's probabilities count            (gradient)
     float* lse2;               // [Mp]       lse log2(e)                                 (gradient)
     float* gval;               // [K][Mp]    G at the listed tokens                      (gradient)
@@ -49,16 +51,19 @@ struct Space {
 Space lay_out(void* base, int M, int hid, int V, int K, bool grad);
 
 struct ProductArgs {
+    int M;
+    const int* list;           // the call's lists and row weights: STATS by single blocks
+    const float* weight;
     const int* hdr_in;
     int* hdr;
     int hid, V, v0, vn;        // vn columns of the vocabulary from v0 on
     int n;                     // columns of a tile
     int col_tiles;             // tiles along the columns (vocabulary or hid)
-    int row_tiles;             // DW: tiles along the vocabulary
+    int want_dh, row_tiles;    // BACK: whether dh is asked for; dw's tiles along the vocabulary (0: not asked for)
     int a_rows;                // rows of the 128-row operand one block loads (fewer than 128 only where M is)
     int Mp, K, tiles;
-    int add;                   // DH: a piece behind the first
-    float c2;                  // log2(e) / tau
+    int add;                   // BACK: a piece behind the first
+    float c2, c2_low;          // log2(e) / tau, and what fp32 leaves of it
     const int* ids;
     const int* pos;
     const int* row;
@@ -75,24 +80,27 @@ struct ProductArgs {
 };
 
 // Launches one product of the call: `piece` counts the pieces of the vocabulary (STATS: the whole of it).
-int launch_product(Product what, const Space& s, const void* w, int M, int hid, int V, int K, int piece, float c2, float* target_logit,
-                   void* dw, cudaStream_t st);
+// h, list, weight: the call's own (STATS); dh and dw: what is asked for (BACK).
+int launch_product(Product what, const Space& s, const void* h, const void* w, const int* list, const float* weight, int M, int hid, int V, int K,
+                   int piece, float tau, float* target_logit, bool want_dh, void* dw, cudaStream_t st);
 
-// Ranges that dh's contraction is cut into, so that mt x ht tiles of `steps` steps fill `pairs` pairs of blocks: the
-// count with the shortest busiest pair, a range costing 24 steps beside its own (filling the pipeline, storing the
-// tile).  At most `cap` tiles in all, for their partial sums' space, and ranges of 8 steps at least.
-__host__ __device__ inline int dh_ranges(int mt, int ht, int steps, int pairs, int cap) {
-    const uint32_t P = (uint32_t)pairs, tiles = (uint32_t)(mt * ht), all = (uint32_t)steps;
-    int best = 1;
-    uint64_t best_cost = (uint64_t)((tiles + P - 1) / P) * (all + 24);
-    for (uint32_t s = 2; (int)s * mt <= cap && s * 8 <= all; ++s) {
-        const uint64_t cost = (uint64_t)((tiles * s + P - 1) / P) * ((all + s - 1) / s + 24);
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = (int)s;
-        }
-    }
-    return best;
+// log2(e) / tau as two fp32 terms, both above 0 (a z of -inf stays one).
+inline void scale_of(float tau, float& c2, float& c2_low) {
+    const double c = 1.4426950408889634 / tau;
+    c2 = (float)c;
+    if (c2 >= c) c2 = nextafterf(c2, 0.f);
+    c2_low = (float)(c - c2);
 }
+
+__device__ __forceinline__ bool is_live(const int* list, const float* weight, int K, int m) {
+    const int id = list[(size_t)m * K];
+    const float a = weight ? weight[m] : 1.f;
+    return id >= 0 && a != 0.f;
+}
+
+// What a tile of dh's and of dw's product costs, in steps of its contraction: filling the pipeline and storing the tile
+// cost eight steps beside them, and a short contraction waits for the tile before it to be stored.
+__host__ __device__ inline int dh_tile_cost(int steps, int ranges) { return (steps + ranges - 1) / ranges + 8; }
+__host__ __device__ inline int dw_tile_cost(int steps) { return steps > 7 ? steps : 7; }
 
 }  // namespace headloss

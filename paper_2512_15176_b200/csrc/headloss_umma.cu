@@ -3,13 +3,14 @@
 //   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid; two warps per block beside it
 //                                                   compute the listed tokens' z once more on the CUDA cores
 //   GRAD   G = coef (p - t)          [live][piece]  the same z again, softmax and targets in the epilogue
-//   DH     dh = G w                  [live][hid]    contraction over the piece's vocabulary
-//   DW     dw = G^T h                [piece][hid]   contraction over the live rows
+//   BACK   dh = G w                  [live][hid]    contraction over the piece's vocabulary, in ranges
+//          dw = G^T h                [piece][hid]   contraction over the live rows
 //
-// One kernel body.  Pairs of blocks (tcgen05.mma.cta_group::2, 256 x n tiles, n <= 256, fp32 accumulators in two
+// One kernel body; the two products of BACK share a launch, so that the many short tiles of dw fill what the few long ones
+// of dh leave of the last wave.  Pairs of blocks (tcgen05.mma.cta_group::2, 256 x n tiles, n <= 256, fp32 accumulators in two
 // tensor-memory buffers) walk a list of tiles: a warp per block brings 64-deep steps of both operands by TMA into a ring
 // of six 32 KB stages, one warp of the pair issues the MMAs, four warps per block take the finished tile while the next
-// one is computed.  h and G are stored row-major once; where the contraction runs along their rows (DW, and w in DH) the
+// one is computed.  h and G are stored row-major once; where the contraction runs along their rows (dw, and w in dh) the
 // operand is read MN-major: boxes of 64 contraction rows x 64 columns, two of them side by side.
 //
 // G is rounded to bf16 for the products: as much as dh and dw are themselves, and with many rows the errors of different
@@ -23,6 +24,8 @@
 // fp32 sums (4 % of the products' bytes at lists of 64, and hidden behind them): the loss takes those, and lse is corrected
 // by the difference.
 #include <math.h>
+
+#include <type_traits>
 
 #include "headloss.cuh"
 #include "sm100.cuh"
@@ -38,7 +41,7 @@ template <int P, int CG>
 struct Shape {
     static constexpr int A = 16384;                        // a block's share of an operand's step: 128 rows (columns) x 64 bf16
     static constexpr int B = 32768 / CG;                   // n columns, or this block's half of them
-    static constexpr int EPI = P == GRAD || P == DW ? 8 : 4;   // epilogue warps, four to 32 x n or two to half of it each
+    static constexpr int EPI = P == GRAD ? 8 : 4;           // epilogue warps, four to 32 x n or two to half of it each
     static constexpr int STAGING = P == STATS ? 0 : EPI * 2 * BOX;
     static constexpr int STAGES = (232448 - STAGING - 1024 - 256) / (A + B);
     static constexpr int SMEM = STAGES * (A + B) + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
@@ -72,75 +75,103 @@ __device__ __forceinline__ uint32_t idesc_of(int n, bool a_mn, bool b_mn) {
     return (CG == 2 ? make_idesc_bf16_pair(n) : make_idesc_bf16(n, 0)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
 }
 
-// Tile u of the list: rows and columns of the product, range of the contraction in steps.
+// STATS by single blocks takes the call's rows and lists as they are, dead rows among them.
+template <int P, int CG>
+__host__ __device__ constexpr bool direct() {
+    return P == STATS && CG == 1;
+}
+
+// A tile: rows and columns of the product, range of the contraction in steps.
 struct Tile {
-    int r, c, k0, kb, y;       // y: DH: row of the slabs
+    int r, c, k0, kb;
+    int y;                     // dh: row of the slabs
+    bool dw;                   // BACK: of dw
 };
+// The tiles of the launch, and those of one block or pair among them, in its order.
 template <int P, int CG>
 struct List {
-    int mt, ct, live, steps, ranges, n, low;      // low: place of the second term's rows, 0: none
+    int live, steps, mt, ct, low, ranges, dw_steps, n, n_dw, group, groups;    // low: place of the second term's rows, 0: none
+    int mine, light, ahead;
     __device__ __forceinline__ List(const ProductArgs& a) {
-        live = a.hdr_in[HDR_LIVE];
+        live = direct<P, CG>() ? a.M : a.hdr_in[HDR_LIVE];
         mt = (live + Shape<P, CG>::ROWS - 1) / Shape<P, CG>::ROWS;
         ct = a.col_tiles;
-        ranges = 1;
         low = P != STATS && live <= TWO_TERMS ? low_term(live) : 0;
-        if (P == STATS || P == GRAD) {
+        group = blockIdx.x / CG;
+        groups = gridDim.x / CG;
+        if (P != BACK) {
             steps = a.hid / STEP;
             n = mt * ct;
-        } else if (P == DH) {
-            steps = (a.vn + STEP - 1) / STEP;
-            ranges = a.hdr_in[HDR_RANGES];
-            n = mt * ct * ranges;
-        } else {
-            steps = ((low ? 2 * low : live) + STEP - 1) / STEP;
-            n = a.row_tiles * ct;
+            return;
         }
+        steps = (a.vn + STEP - 1) / STEP;
+        ranges = a.hdr_in[HDR_RANGES];
+        dw_steps = ((low ? 2 * low : live) + STEP - 1) / STEP;
+        n = a.want_dh ? mt * ct * ranges : 0;
+        n_dw = a.row_tiles * ct;
+        // dh's tiles first, in turn; groups that have one of them less take `ahead` of dw's before the others begin
+        mine = group < n ? (n - group + groups - 1) / groups : 0;
+        light = n % groups ? groups - n % groups : 0;
+        ahead = light ? dh_tile_cost(steps, ranges) / dw_tile_cost(dw_steps) : 0;
     }
-    __device__ __forceinline__ Tile tile(int u) const {
-        Tile t;
-        t.k0 = 0;
+    // The group's k-th tile; false behind its last.
+    __device__ __forceinline__ bool tile(int k, Tile& t) const {
+        t.k0 = t.y = 0;
         t.kb = steps;
-        t.y = 0;
-        if (P == STATS || P == GRAD) {      // row tiles fastest: the pairs share a few tiles of w at a time
+        t.dw = false;
+        int u = group + k * groups;
+        if (P != BACK) {                    // row tiles fastest: the groups share a few tiles of w at a time
+            if (u >= n) return false;
             t.r = u % mt;
             t.c = u / mt;
-        } else {                            // columns (of hid) fastest: the pairs share tiles of G
-            t.c = u % ct;
-            t.r = u / ct;
-            if (P == DH) {
-                const int s = t.r / mt;
-                t.y = t.r * TILE;
-                t.r -= s * mt;
-                t.k0 = (int)((long)s * steps / ranges);
-                t.kb = (int)((long)(s + 1) * steps / ranges) - t.k0;
-            }
+            return true;
         }
-        return t;
+        if (k < mine) {                     // columns (of hid) fastest: the groups share tiles of G
+            const int q = u / ct, s = q / mt;
+            t.c = u - q * ct;
+            t.y = q * TILE;
+            t.r = q - s * mt;
+            t.k0 = (int)((long)s * steps / ranges);
+            t.kb = (int)((long)(s + 1) * steps / ranges) - t.k0;
+            return true;
+        }
+        k -= mine;
+        const int first = group - (groups - light);      // the group's place among the light ones
+        u = light && first >= 0 ? (k < ahead ? k * light + first : light * ahead + (k - ahead) * groups + group)
+                                : light * ahead + k * groups + group;
+        if (u >= n_dw) return false;
+        t.dw = true;
+        t.r = u / ct;
+        t.c = u - t.r * ct;
+        t.kb = dw_steps;
+        return true;
     }
 };
 
 // z of the listed tokens by plain fp32 sums: a warp takes four entries of a row at a time.
+template <bool DIRECT>
 __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, int warp, int warps, int lane) {
     const int groups = (a.K + 3) / 4;
     for (long i = warp; i < (long)live * groups; i += warps) {
         const int slot = (int)(i / groups), e0 = (int)(i % groups) * 4;
+        if (DIRECT && !is_live(a.list, a.weight, a.K, slot)) continue;
         const __nv_bfloat16* w[4];
-        int n = 0;
-        for (; n < 4 && e0 + n < a.K; ++n) {
-            const int id = a.ids[(size_t)(e0 + n) * a.Mp + slot];
-            if (id >= a.V) break;                                          // by rising id: the rest is no token either
-            w[n] = a.w + (size_t)id * a.hid;
+        bool on[4], any = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int id = e0 + j < a.K ? (DIRECT ? a.list[(size_t)slot * a.K + e0 + j] : a.ids[(size_t)(e0 + j) * a.Mp + slot]) : -1;
+            on[j] = id >= 0 && id < a.V;      // (an entry behind a list's end may be summed: what it gives is not read)
+            any |= on[j];
+            w[j] = a.w + (on[j] ? (size_t)id * a.hid : 0);
         }
-        for (int j = n; j < 4; ++j) w[j] = n ? w[0] : a.w;
-        if (n == 0) continue;
+        if (!any) continue;
         const __nv_bfloat16* h = a.h + (size_t)slot * a.hid;
         float sum[4][2] = {};
         for (int c = lane * 8; c < a.hid; c += 256) {
             const uint4 x = *reinterpret_cast<const uint4*>(h + c);
             uint4 y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = j < n ? __ldg(reinterpret_cast<const uint4*>(w[j] + c)) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) y[j] = on[j] ? *reinterpret_cast<const uint4*>(w[j] + c) : make_uint4(0, 0, 0, 0);
             const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -157,26 +188,72 @@ __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, in
             float s = sum[j][0] + sum[j][1];
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (lane == 0 && j < n) a.target_logit[(size_t)a.row[slot] * a.K + a.pos[(size_t)(e0 + j) * a.Mp + slot]] = s;
+            if (lane == 0 && on[j]) {
+                const int pos = DIRECT ? e0 + j : a.pos[(size_t)(e0 + j) * a.Mp + slot];
+                a.target_logit[(size_t)(DIRECT ? slot : a.row[slot]) * a.K + (pos < 0 ? ~pos : pos)] = s;
+            }
         }
     }
 }
 
+// The first token of a row's list at or behind `from`, INT_MAX: none.  With `store`, z goes to the entries that name
+// from - 1, NaN to all of them but the first.
+__device__ __forceinline__ int next_listed(const ProductArgs& a, int m, int from, bool store, float z) {
+    int next = 0x7fffffff;
+    bool open = true;
+    for (int j0 = 0; j0 < a.K; j0 += 4) {
+        int id[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) id[i] = j0 + i < a.K ? a.list[(size_t)m * a.K + j0 + i] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            open &= id[i] >= 0;
+            if (open && id[i] >= from) next = min(next, id[i]);
+            if (open && store && id[i] == from - 1) {
+                a.z[(size_t)(j0 + i) * a.Mp + m] = z;
+                z = NAN;
+            }
+        }
+        if (!open) break;
+    }
+    return next;
+}
+
 template <int P, int CG>
-__device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const List<P, CG>& list, int warp, int lane, int rank,
+__device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const CUtensorMap* tm_out_dw, const List<P, CG>& list, int warp, int lane, int rank,
                                          uint32_t tmem_base, uint32_t tfull0, uint32_t tempty0, uint32_t staging, volatile int* abort_flag) {
     constexpr int SHARE = Shape<P, CG>::EPI / 4;                           // warps to a quarter of the lanes: they take its columns in turn
     const int quarter = warp & 3, turn = (warp - 2) >> 2;
     const uint32_t stg = staging + (uint32_t)(warp - 2) * (2u * BOX), stg_row = (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
     const int lane_row = rank * 128 + quarter * 32 + lane;                 // the thread's row within a tile
-    const int groups = gridDim.x / CG;
     uint32_t stg_i = 0;
     int it = 0;
-    for (int u = blockIdx.x / CG; u < list.n; u += groups) {
-        const Tile t = list.tile(u);
-        if (t.kb == 0 && P != DW) continue;                               // DH: nothing to add; DW without a live row: zeros
+    Tile t;
+    for (int k = 0; list.tile(k, t); ++k) {
+        if (t.kb == 0 && !t.dw) continue;                                 // dh: nothing to add; dw without a live row: zeros
         const int buf = it & 1;
         const bool computed = t.kb > 0;
+        const int slot = t.r * Shape<P, CG>::ROWS + lane_row;             // STATS, GRAD: place among the live rows
+        const bool row_ok = slot < list.live && (!direct<P, CG>() || is_live(a.list, a.weight, a.K, slot));
+        const int col0 = t.c * a.n;
+        // what the tile needs of its rows comes while it is computed: a row's first listed token at or behind its start
+        float coef = 0.f, nlse = 0.f;
+        int e = 0, next = 0x7fffffff;
+        if (direct<P, CG>()) {
+            if (row_ok) next = next_listed(a, slot, col0, false, 0.f);
+        } else if ((P == STATS || P == GRAD) && row_ok) {
+            if (P == GRAD) {
+                coef = a.coef[slot];
+                nlse = -a.lse2[slot];
+            }
+            int hi = a.K;
+            while (e < hi) {
+                const int mid = (e + hi) >> 1;
+                if (a.ids[(size_t)mid * a.Mp + slot] < a.v0 + col0) e = mid + 1;
+                else hi = mid;
+            }
+            if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
+        }
         if (computed) {
             const bool got = mbar_wait(tfull0 + 8u * buf, (uint32_t)(it >> 1) & 1u, abort_flag);
             if (!__all_sync(0xffffffffu, got)) break;                     // warp-uniform, so the aligned TMEM loads stay converged
@@ -184,9 +261,6 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             ++it;
         }
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * ACC);
-        const int slot = t.r * Shape<P, CG>::ROWS + lane_row;                           // STATS, GRAD: place among the live rows
-        const bool row_ok = slot < list.live;
-        const int col0 = t.c * a.n;
 
         if (P == STATS) {
             const int width = min(a.n, a.vn - col0);                      // columns that exist
@@ -207,60 +281,41 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                         m = fmaxf(m, __uint_as_float(v[j]));
                     }
                 }
-                m = fmaxf(m, run_m);
-                const float shift = m == -INFINITY ? 0.f : m * a.c2;       // a row of -inf so far: its exponentials are 0
-                run_s *= ex2(run_m * a.c2 - shift);
+                // relative to a whole row's reference in powers of two: rounded where it is small, not where z is
+                m = fmaxf(m * a.c2, run_m);
+                const float shift = m == -INFINITY ? 0.f : m;              // a row of -inf so far: its exponentials are 0
+                run_s *= ex2(run_m - shift);
                 run_m = m;
                 float s0 = 0.f, s1 = 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) {
-                    s0 += ex2(fmaf(__uint_as_float(v[j]), a.c2, -shift));
-                    s1 += ex2(fmaf(__uint_as_float(v[j + 1]), a.c2, -shift));
+                    const float x = __uint_as_float(v[j]), y = __uint_as_float(v[j + 1]);
+                    s0 += ex2(fmaf(x, a.c2_low, fmaf(x, a.c2, -shift)));
+                    s1 += ex2(fmaf(y, a.c2_low, fmaf(y, a.c2, -shift)));
                 }
                 run_s += s0 + s1;
             }
             if (row_ok) a.part[(size_t)slot * a.tiles + t.c] = make_float2(run_m, run_s);
             // The z of listed tokens in this tile.  Few rows have one here, so each distinct column is read again.
-            int e = 0, next = 0x7fffffff;
             const int first = a.v0 + col0, last = first + width;
-            if (row_ok) {
-                int hi = a.K;                                              // first entry at or behind the tile's start
-                while (e < hi) {
-                    const int mid = (e + hi) >> 1;
-                    if (a.ids[(size_t)mid * a.Mp + slot] < first) e = mid + 1;
-                    else hi = mid;
-                }
-                if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
-            }
             for (;;) {
                 const int col = __reduce_min_sync(0xffffffffu, next);
                 if (col >= last) break;
                 uint32_t z;
                 TMEM_LD_X1(taddr + (uint32_t)(col - first), z);
                 tmem_wait_ld();
-                while (next == col) {
-                    a.z[(size_t)e * a.Mp + slot] = __uint_as_float(z);
+                if (direct<P, CG>() && next == col) next = next_listed(a, slot, col + 1, true, __uint_as_float(z));
+                while (!direct<P, CG>() && next == col) {
+                    const int pos = a.pos[(size_t)e * a.Mp + slot];
+                    a.z[(size_t)(pos < 0 ? ~pos : pos) * a.Mp + slot] = pos < 0 ? NAN : __uint_as_float(z);
                     ++e;
                     next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
                 }
                 __syncwarp();
             }
-        } else if (P == GRAD || P == DW) {
-            float coef = 0.f, nlse = 0.f;
-            int e = 0, next = 0x7fffffff;
-            if (P == GRAD && row_ok) {
-                coef = a.coef[slot];
-                nlse = -a.lse2[slot];
-                int hi = a.K;
-                while (e < hi) {
-                    const int mid = (e + hi) >> 1;
-                    if (a.ids[(size_t)mid * a.Mp + slot] < a.v0 + col0) e = mid + 1;
-                    else hi = mid;
-                }
-                if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
-            }
+        } else if (P == GRAD || t.dw) {
             const int limit = P == GRAD ? a.vn : a.hid;
-            const float scale = P == DW ? __int_as_float(a.hdr_in[HDR_SCALE]) : 1.f;
+            const float scale = P == BACK ? __int_as_float(a.hdr_in[HDR_SCALE]) : 1.f;
             const bool two = P == GRAD && list.low > 0;
             const bool idle = two && (rank > 0 || quarter * 32 >= list.low);        // no rows of the first term
             for (int c = 64 * turn; c < a.n && col0 + c < limit && !idle; c += 64 * SHARE) {
@@ -290,7 +345,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                         if (P == GRAD) {
                             x = coef * ex2(fmaf(x, a.c2, nlse));
                             y = coef * ex2(fmaf(y, a.c2, nlse));
-                            if (!row_ok) x = y = 0.f;                     // places behind the live rows: DW's contraction meets them
+                            if (!row_ok) x = y = 0.f;                     // places behind the live rows: dw's contraction meets them
                         } else {
                             x *= scale;
                             y *= scale;
@@ -333,15 +388,15 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                const int y = (P == DW ? a.v0 : 0) + t.r * Shape<P, CG>::ROWS + rank * 128 + quarter * 32;
+                const int y = (P == BACK ? a.v0 : 0) + t.r * Shape<P, CG>::ROWS + rank * 128 + quarter * 32;
                 if (lane == 0 && (P == GRAD || y < a.V)) {                // rows and columns beyond the tensor are clipped
-                    tma_store_2d(tm_out, box, col0 + c, y);
+                    tma_store_2d(P == BACK ? tm_out_dw : tm_out, box, col0 + c, y);
                     if (two) tma_store_2d(tm_out, box + other, col0 + c, list.low + quarter * 32);
                     bulk_commit();
                 }
             }
-        } else {                                                          // DH: fp32, 32 columns to a box
-            for (int c = 0; c < a.n && col0 + c < a.hid; c += 32) {
+        } else {                                                          // dh: fp32, 32 columns to a box
+            for (int c = 32 * turn; c < a.n && col0 + c < a.hid; c += 32 * SHARE) {
                 if (lane == 0) bulk_wait_read<1>();
                 __syncwarp();
                 const uint32_t box = stg + stg_i * BOX, b = box + stg_row;
@@ -370,8 +425,13 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             }
         }
     }
-    if (lane == 0) bulk_wait<0>();               // the staging area outlives every store that reads it
+    if (lane == 0) bulk_wait_read<0>();          // the staging area outlives every store that reads it
 }
+
+// BACK: the operands and the result of dw's product.
+struct DwMaps {
+    CUtensorMap a, b, out;
+};
 
 template <int CG>
 __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
@@ -392,7 +452,7 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 template <int P, int CG>
 __global__ void __launch_bounds__(Shape<P, CG>::THREADS, 1)
 product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_out,
-               const ProductArgs a) {
+               const __grid_constant__ DwMaps dw, const ProductArgs a) {
     using S = Shape<P, CG>;
     constexpr int STAGES = S::STAGES, STAGE_BYTES = S::A + S::B;
     extern __shared__ unsigned char smem_raw[];
@@ -401,11 +461,10 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-    constexpr bool A_MN = P == DW, B_MN = P == DH || P == DW;
+    constexpr bool B_MN = P == BACK;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
     const bool leader = rank == 0;
-    const int groups = gridDim.x / CG;
     const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
@@ -442,79 +501,98 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         // ---------------- TMA producer (each block: its rows of one operand, its half of the columns of the other) --------
         if (lane == 0) {
             const int half = a.n / CG;                                     // columns of the tile that this block brings
-            // the second block's rows: those behind the first 128, or (DH) the second term
-            const bool second_a = CG == 2 && (A_MN || list.live > 128 || (P == DH && list.low > 0)), has_a = leader || second_a;
+            // the second block's rows: those behind the first 128, or (dh) the second term
+            const bool second_a = CG == 2 && (list.live > 128 || (P == BACK && list.low > 0)), has_a = leader || second_a;
+            const int a_step = P == BACK && list.low > 0 ? list.low : 128;
             const int b_boxes = B_MN ? (half + 63) / 64 : 1;
-            const uint32_t a_bytes = A_MN ? S::A : (uint32_t)a.a_rows * 128u;
-            const uint32_t b_bytes = B_MN ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u;
-            const uint32_t stage_tx = a_bytes * (second_a ? 2u : 1u) + (uint32_t)CG * b_bytes;
+            const uint32_t a_bytes = (uint32_t)a.a_rows * 128u, b_bytes = B_MN ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u;
+            const uint32_t stage_tx = a_bytes * (second_a ? 2u : 1u) + (uint32_t)CG * b_bytes, dw_tx = CG * (S::A + b_bytes);
             int it = 0;
             bool ok = true;
-            for (int u = blockIdx.x / CG; u < list.n && ok; u += groups) {
-                const Tile t = list.tile(u);
-                const int ra = t.r * S::ROWS + (int)rank * (P == DH && list.low > 0 ? list.low : 128), cb = t.c * a.n + (int)rank * half;
-                for (int kb = 0; kb < t.kb; ++kb, ++it) {
-                    const int s = it % STAGES, k = (t.k0 + kb) * STEP;
-                    if (!mbar_wait(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                    if (leader) mbar_expect_tx(full_bar(s), stage_tx);
-                    const uint32_t full = CG == 2 ? map_to_cta(full_bar(s), 0) : full_bar(s), sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
-                    if (A_MN) {
-                        load_2d<CG>(sa, &tm_a, ra, k, full);
-                        load_2d<CG>(sa + 8192, &tm_a, ra + 64, k, full);
-                    } else if (has_a) {
-                        load_2d<CG>(sa, &tm_a, k, ra, full);
+            Tile t;
+            for (int i = 0; ok && list.tile(i, t); ++i) {
+                const int ra = t.r * S::ROWS + (int)rank * (t.dw ? 128 : a_step), cb = t.c * a.n + (int)rank * half;
+                // one loop for each kind of tile
+                auto steps = [&](auto of_dw) {
+                    constexpr bool DW = decltype(of_dw)::value;
+                    for (int kb = 0; kb < t.kb; ++kb, ++it) {
+                        const int s = it % STAGES, k = (t.k0 + kb) * STEP;
+                        if (!mbar_wait(empty_bar(s), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag)) return false;
+                        if (leader) mbar_expect_tx(full_bar(s), DW ? dw_tx : stage_tx);
+                        const uint32_t full = CG == 2 ? map_to_cta(full_bar(s), 0) : full_bar(s), sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
+                        if (DW) {
+                            load_2d<CG>(sa, &dw.a, ra, k, full);
+                            load_2d<CG>(sa + 8192, &dw.a, ra + 64, k, full);
+                        } else if (has_a) {
+                            load_2d<CG>(sa, &tm_a, k, ra, full);
+                        }
+                        if (B_MN) {
+                            const CUtensorMap* tm = DW ? &dw.b : &tm_b;
+                            const int y = DW ? k : a.v0 + k;
+                            load_2d<CG>(sb, tm, cb, y, full);
+                            if (b_boxes > 1) load_2d<CG>(sb + 8192, tm, cb + 64, y, full);
+                        } else {
+                            load_2d<CG>(sb, &tm_b, k, a.v0 + cb, full);
+                        }
                     }
-                    if (B_MN) {
-                        const int y = P == DH ? a.v0 + k : k;
-                        load_2d<CG>(sb, &tm_b, cb, y, full);
-                        if (b_boxes > 1) load_2d<CG>(sb + 8192, &tm_b, cb + 64, y, full);
-                    } else {
-                        load_2d<CG>(sb, &tm_b, k, a.v0 + cb, full);
-                    }
-                }
+                    return true;
+                };
+                ok = P == BACK && t.dw ? steps(std::true_type{}) : steps(std::false_type{});
             }
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer (first block of the pair) ----------------
         if (leader && lane == 0) {
-            const uint32_t idesc = idesc_of<CG>(a.n, A_MN, B_MN);
             int it = 0, done = 0;
             bool ok = true;
-            for (int u = blockIdx.x / CG; u < list.n && ok; u += groups) {
-                const Tile t = list.tile(u);
+            Tile t;
+            for (int i = 0; ok && list.tile(i, t); ++i) {
                 if (t.kb == 0) continue;
                 const int buf = done & 1;
                 if (!mbar_wait(tempty0 + 8u * buf, ((uint32_t)(done >> 1) & 1u) ^ 1u, abort_flag)) break;
                 ++done;
                 tcgen05_fence_after();
                 const uint32_t d_tmem = tmem_base + (uint32_t)(buf * ACC);
-                for (int kb = 0; kb < t.kb; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!mbar_wait(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag)) { ok = false; break; }
-                    tcgen05_fence_after();
-                    const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
-                    // K-major: 16 contraction columns are 32 bytes; MN-major: 16 contraction rows are 2048 bytes
-                    const uint64_t ad = A_MN ? smem_desc_sw128(sa, 8192, 1024) : smem_desc_sw128_kmajor(sa);
-                    const uint64_t bd = B_MN ? smem_desc_sw128(sb, 8192, 1024) : smem_desc_sw128_kmajor(sb);
+                auto steps = [&](auto of_dw) {
+                    constexpr bool A_MN = decltype(of_dw)::value;
+                    const uint32_t idesc = idesc_of<CG>(a.n, A_MN, B_MN);
+                    for (int kb = 0; kb < t.kb; ++kb, ++it) {
+                        const int s = it % STAGES;
+                        if (!mbar_wait(full_bar(s), (uint32_t)(it / STAGES) & 1u, abort_flag)) return false;
+                        tcgen05_fence_after();
+                        const uint32_t sa = smem_base + s * STAGE_BYTES, sb = sa + S::A;
+                        // K-major: 16 contraction columns are 32 bytes; MN-major: 16 contraction rows are 2048 bytes
+                        const uint64_t ad = A_MN ? smem_desc_sw128(sa, 8192, 1024) : smem_desc_sw128_kmajor(sa);
+                        const uint64_t bd = B_MN ? smem_desc_sw128(sb, 8192, 1024) : smem_desc_sw128_kmajor(sb);
 #pragma unroll
-                    for (int k = 0; k < STEP / 16; ++k)
-                        mma<CG>(d_tmem, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, (kb | k) != 0 ? 1u : 0u);
-                    commit<CG>(empty_bar(s));
-                }
+                        for (int k = 0; k < STEP / 16; ++k)
+                            mma<CG>(d_tmem, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, (kb | k) != 0 ? 1u : 0u);
+                        commit<CG>(empty_bar(s));
+                    }
+                    return true;
+                };
+                ok = P == BACK && t.dw ? steps(std::true_type{}) : steps(std::false_type{});
                 if (ok) commit<CG>(tfull0 + 8u * buf);
             }
         }
     } else if (warp >= 2 + S::EPI) {
-        if (P == STATS) listed_logits(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - 2 - S::EPI, (int)gridDim.x * DOT_WARPS, lane);
+        if (P == STATS) listed_logits<direct<P, CG>()>(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - 2 - S::EPI, (int)gridDim.x * DOT_WARPS, lane);
     } else {
-        epilogue<P, CG>(a, &tm_out, list, warp, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
+        epilogue<P, CG>(a, &tm_out, &dw.out, list, warp, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
     }
 
     // ---- tear-down: neither block leaves while the other may still signal it or read its shared memory ----
     tcgen05_fence_before();
     __syncthreads();
     if (*abort_flag) {
-        if (tid == 0) a.hdr[HDR_GAVE_UP] = 1;    // the last kernel of the call turns this into NaN
+        // the last kernel of the call turns this into NaN
+        if (P != STATS && tid == 0) a.hdr[HDR_GAVE_UP] = 1;
+        if (P == STATS) {
+            Tile t;
+            for (int k = 0; list.tile(k, t); ++k)
+                for (int i = tid; i < S::ROWS; i += S::THREADS)
+                    if (t.r * S::ROWS + i < list.live) a.part[(size_t)(t.r * S::ROWS + i) * a.tiles + t.c] = make_float2(NAN, NAN);
+        }
         for (int i = 0; i < 64; ++i) __nanosleep(10000);
         __syncthreads();
     }
@@ -536,28 +614,39 @@ static int map_bf16(CUtensorMap* tm, const void* base, long rows, long cols, lon
 }
 
 template <int P, int CG>
-static int launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const ProductArgs& a, long most_tiles, cudaStream_t st) {
+static int launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const DwMaps& dw, const ProductArgs& a, long most_tiles,
+                  cudaStream_t st) {
     using S = Shape<P, CG>;
     long groups = deer_sm_count() / CG;
     if (groups > most_tiles) groups = most_tiles;
-    DEER_CUDA(cudaFuncSetAttribute(product_kernel<P, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
-    DEER_CUDA(launch_pdl_cluster(CG, product_kernel<P, CG>, dim3((unsigned)(CG * groups)), dim3(S::THREADS), (size_t)S::SMEM, st, ta, tb, to, a));
+    static bool sized[64] = {};                  // (set again by a thread that has not seen it: harmless)
+    int dev = 0;
+    DEER_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !sized[dev]) {
+        DEER_CUDA(cudaFuncSetAttribute(product_kernel<P, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        if (dev < 64) sized[dev] = true;
+    }
+    DEER_CUDA(launch_pdl_cluster(CG, product_kernel<P, CG>, dim3((unsigned)(CG * groups)), dim3(S::THREADS), (size_t)S::SMEM, st, ta, tb, to, dw, a));
     return DEER_OK;
 }
 
-int launch_product(Product what, const Space& s, const void* w, int M, int hid, int V, int K, int piece, float c2, float* target_logit,
-                   void* dw, cudaStream_t st) {
+int launch_product(Product what, const Space& s, const void* h, const void* w, const int* list, const float* weight, int M, int hid, int V, int K,
+                   int piece, float tau, float* target_logit, bool want_dh, void* dw, cudaStream_t st) {
     ProductArgs a = {};
+    a.M = M;
+    a.list = list;
+    a.weight = weight;
     a.hdr_in = a.hdr = s.hdr;
     a.hid = hid;
     a.V = V;
     a.Mp = s.Mp;
     a.K = K;
-    a.c2 = c2;
+    scale_of(tau, a.c2, a.c2_low);
     a.ids = s.ids;
     a.pos = s.pos;
     a.row = s.row;
-    a.h = s.h;
+    const bool as_is = what == STATS && M <= ONE_BLOCK;
+    a.h = as_is ? static_cast<const __nv_bfloat16*>(h) : s.h;
     a.w = static_cast<const __nv_bfloat16*>(w);
     a.target_logit = target_logit;
     a.z = s.z;
@@ -574,6 +663,7 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
     a.a_rows = M < 128 ? (M + 7) / 8 * 8 : 128;
     const int mt = s.Mp / TILE;
     CUtensorMap ta, tb, to;
+    DwMaps td;
     int rc;
 #define MAP(call)                     \
     do {                              \
@@ -583,34 +673,32 @@ int launch_product(Product what, const Space& s, const void* w, int M, int hid, 
     if (what == STATS || what == GRAD) {
         a.n = what == STATS ? s.stats_n : s.grad_n;
         a.col_tiles = a.tiles = (a.vn + a.n - 1) / a.n;
-        MAP(map_bf16(&ta, s.h, s.Mp, hid, hid, a.a_rows));
         const int cg = M > ONE_BLOCK ? 2 : 1;
+        MAP(map_bf16(&ta, a.h, as_is ? M : s.Mp, hid, hid, a.a_rows));
         MAP(map_bf16(&tb, w, V, hid, hid, a.n / cg));
-        to = ta;
+        to = td.a = td.b = td.out = ta;
         const long tiles = (long)mt * a.col_tiles;
-        if (what == STATS) return cg == 2 ? launch<STATS, 2>(ta, tb, to, a, tiles, st) : launch<STATS, 1>(ta, tb, to, a, tiles, st);
+        if (what == STATS) return cg == 2 ? launch<STATS, 2>(ta, tb, to, td, a, tiles, st) : launch<STATS, 1>(ta, tb, to, td, a, tiles, st);
         MAP(map_bf16(&to, s.g, s.Mp, a.vn, s.piece, 32));
-        return cg == 2 ? launch<GRAD, 2>(ta, tb, to, a, tiles, st) : launch<GRAD, 1>(ta, tb, to, a, tiles, st);
+        return cg == 2 ? launch<GRAD, 2>(ta, tb, to, td, a, tiles, st) : launch<GRAD, 1>(ta, tb, to, td, a, tiles, st);
     }
     a.n = s.hid_n;
     a.col_tiles = (hid + a.n - 1) / a.n;
-    if (what == DH) {
-        a.add = piece > 0;
-        // beyond the piece's columns, and its contraction's last step, G reads as zeros
-        MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, a.a_rows));
-        MAP(map_bf16(&tb, w, V, hid, hid, 64));
-        const uint64_t dims[2] = {(uint64_t)hid, (uint64_t)s.slab_tiles * TILE};
-        const uint64_t strides[1] = {(uint64_t)hid * 4};
-        const uint32_t box[2] = {32, 32};
-        MAP(make_map_f32(&to, s.slab, 2, dims, strides, box));
-        return launch<DH, 2>(ta, tb, to, a, (long)s.slab_tiles * a.col_tiles, st);
-    }
-    a.row_tiles = (a.vn + TILE - 1) / TILE;
-    MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, 64));
-    MAP(map_bf16(&tb, s.h, s.Mp, hid, hid, 64));
-    MAP(map_bf16(&to, dw, V, hid, hid, 32));
+    a.add = piece > 0;
+    a.want_dh = want_dh;
+    a.row_tiles = dw ? (a.vn + TILE - 1) / TILE : 0;
+    // beyond the piece's columns, and its contraction's last step, G reads as zeros
+    MAP(map_bf16(&ta, s.g, s.Mp, a.vn, s.piece, a.a_rows));
+    MAP(map_bf16(&tb, w, V, hid, hid, 64));
+    const uint64_t dims[2] = {(uint64_t)hid, (uint64_t)s.slab_tiles * TILE};
+    const uint64_t strides[1] = {(uint64_t)hid * 4};
+    const uint32_t box[2] = {32, 32};
+    MAP(make_map_f32(&to, s.slab, 2, dims, strides, box));
+    MAP(map_bf16(&td.a, s.g, s.Mp, a.vn, s.piece, 64));
+    MAP(map_bf16(&td.b, s.h, s.Mp, hid, hid, 64));
+    MAP(map_bf16(&td.out, dw ? dw : s.h, dw ? V : s.Mp, hid, hid, 32));
 #undef MAP
-    return launch<DW, 2>(ta, tb, to, a, (long)a.row_tiles * a.col_tiles, st);
+    return launch<BACK, 2>(ta, tb, to, td, a, ((want_dh ? (long)s.slab_tiles : 0) + a.row_tiles) * a.col_tiles, st);
 }
 
 }  // namespace headloss

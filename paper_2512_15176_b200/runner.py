@@ -478,13 +478,14 @@ class HeadLoss:
         self.loss = torch.empty(rows, dtype=f32, device=dev)
         self.lse = torch.empty(rows, dtype=f32, device=dev)
         self.target_logit = torch.empty(rows, self.top, dtype=f32, device=dev)
+        self._first_logit = self.target_logit.view(-1)[:rows]           # a cross entropy's [rows]
         self.dh = torch.empty(rows, hid, dtype=torch.bfloat16, device=dev) if grad else None
         self.dw = torch.empty_like(w) if grad else None
         self.ws = _ws(max(L.deer_lmhead_loss_workspace_bytes(rows, hid, V, self.top, g) for g in ((False, True) if grad else (False,))), dev)
         self._step = None
 
     def cross_entropy(self, h: torch.Tensor, targets: torch.Tensor, row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
-        L.deer_lmhead_loss(h, self.w, targets, self.loss, self.lse, self.target_logit.view(-1)[:self.rows], self.ws, row_weight)
+        L.deer_lmhead_loss(h, self.w, targets, self.loss, self.lse, self._first_logit, self.ws, row_weight)
         self._step = (h, targets, None, 1.0, row_weight)
         return self.loss
 
@@ -500,7 +501,7 @@ class HeadLoss:
         h, ids, teacher, temperature, row_weight = self._step
         dw = self.dw if head else None
         if teacher is None:
-            L.deer_lmhead_loss_grad(h, self.w, ids, self.lse, self.target_logit.view(-1)[:self.rows], self.dh, dw, self.ws, row_weight, grad_loss)
+            L.deer_lmhead_loss_grad(h, self.w, ids, self.lse, self._first_logit, self.dh, dw, self.ws, row_weight, grad_loss)
         else:
             L.deer_lmhead_distill_grad(h, self.w, ids, teacher, temperature, self.lse, self.target_logit, self.dh, dw, self.ws, row_weight, grad_loss)
         return self.dh, dw
