@@ -676,6 +676,67 @@ def deer_lmhead_distill_grad(h, w, ids, teacher, temperature, lse, target_logit,
                                               _bytes_of(workspace), _stream(stream)))
 
 
+class HeadLossBuffers:
+    """What the two calls of a loss leave for each other and for their caller, checked and addressed once: f32 [M] loss and
+    lse, f32 [M][K] target_logit, bf16 dh [M][hid] and dw [V][hid] (None: no gradients) and a workspace for both calls."""
+
+    def __init__(self, w, M: int, K: int = 1, grad: bool = True):
+        if w.dim() != 2 or w.dtype is not _BF16 or not w.is_cuda:
+            _refuse("HeadLossBuffers", "w must be bf16 [V][hid] on a CUDA device")
+        self.w, self.M, self.K = w, int(M), int(K)
+        self.V, self.hid = w.shape
+        new = lambda *shape, dtype=_F32: torch.empty(*shape, dtype=dtype, device=w.device)  # noqa: E731
+        self.loss, self.lse, self.target_logit = new(M), new(M), new(M, K)
+        self.dh, self.dw = (new(M, self.hid, dtype=_BF16), torch.empty_like(w, memory_format=torch.contiguous_format)) if grad else (None, None)
+        with torch.cuda.device(w.device):
+            need = max(deer_lmhead_loss_workspace_bytes(M, self.hid, self.V, K, g) for g in ((False, True) if grad else (False,)))
+        self.workspace = new(max(16, need), dtype=torch.uint8)
+        self._device = w.get_device()
+        self._forward = tuple(t.data_ptr() for t in (self.loss, self.lse, self.target_logit, self.workspace)) + (self.workspace.numel(),)
+
+    def _at(self, call: str, h, ids, teacher, row_weight, grad_loss=None):
+        """Addresses of a call's operands after their checks, and the device's context."""
+        M, w = self.M, self.w
+        if h.dtype is not _BF16 or h.shape != (M, self.hid):
+            _refuse(call, "h must be bf16 [M][hid] of the buffers' M and w's hid")
+        if teacher is None:
+            if not _is(ids, _I32, M):
+                _refuse(call, "targets must be int32 [M]")
+        elif _top_of(call, M, ids, teacher) != self.K:
+            _refuse(call, "ids and teacher must be [M][K] of the buffers' K")
+        if not (_may_be(row_weight, _F32, M) and _may_be(grad_loss, _F32, M)):
+            _refuse(call, "row_weight and grad_loss must be f32 [M]")
+        return _operands(call, w, h, ids, teacher, row_weight, grad_loss)
+
+    def run_loss(self, h, ids, teacher=None, temperature=1.0, row_weight=None, stream=None):
+        call = "deer_lmhead_loss" if teacher is None else "deer_lmhead_distill"
+        (w, h, ids, teacher, row_weight, _), there = self._at(call, h, ids, teacher, row_weight)
+        loss, lse, target_logit, ws, ws_bytes = self._forward
+        with there:
+            if teacher is None:
+                rc = lib().deer_lmhead_loss(h, w, ids, row_weight, self.M, self.hid, self.V, loss, lse, target_logit, ws, ws_bytes, _stream(stream))
+            else:
+                rc = lib().deer_lmhead_distill(h, w, ids, teacher, self.K, temperature, row_weight, self.M, self.hid, self.V, loss, lse,
+                                               target_logit, ws, ws_bytes, _stream(stream))
+            _check(rc)
+
+    def run_grad(self, h, ids, teacher=None, temperature=1.0, row_weight=None, grad_loss=None, dw=True, stream=None):
+        call = "deer_lmhead_loss_grad" if teacher is None else "deer_lmhead_distill_grad"
+        if self.dh is None:
+            _refuse(call, "these buffers are without gradients")
+        (w, h, ids, teacher, row_weight, grad_loss), there = self._at(call, h, ids, teacher, row_weight, grad_loss)
+        _, lse, target_logit, ws, ws_bytes = self._forward
+        dh_at, dw_at = self.dh.data_ptr(), self.dw.data_ptr() if dw else None
+        with there:
+            if teacher is None:
+                rc = lib().deer_lmhead_loss_grad(h, w, ids, row_weight, grad_loss, lse, target_logit, self.M, self.hid, self.V, dh_at, dw_at, ws,
+                                                 ws_bytes, _stream(stream))
+            else:
+                rc = lib().deer_lmhead_distill_grad(h, w, ids, teacher, self.K, temperature, row_weight, grad_loss, lse, target_logit, self.M,
+                                                    self.hid, self.V, dh_at, dw_at, ws, ws_bytes, _stream(stream))
+            _check(rc)
+
+
 def deer_top_logits(logits, ids, values, stream=None):
     call = "deer_top_logits"
     if logits.dim() != 2 or logits.dtype is not _F32:

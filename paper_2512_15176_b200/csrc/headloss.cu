@@ -113,17 +113,19 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 __device__ __forceinline__ int warp_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }
 
-// Ranges that dh's contraction is cut into: its tiles share `pairs` pairs of blocks with dw's, which even out what they
-// leave.  The count with the shortest run, ranges of four steps at least, as many as there is space for their partial sums.
-// The lanes of a warp try one count each.
+// Ranges that dh's contraction is cut into: as many as give every pair of blocks a tile, so that all of them read w at once
+// (77 rows, hid 2048: nine ranges and then dw's tiles 290 us, four beside dw's tiles 305 us), and from there on the count
+// with the shortest run of the launch, dw's tiles evening out what dh's leave; ranges of four steps at least, as many as
+// there is space for their partial sums.  The lanes of a warp try one count each.
 __device__ int dh_ranges(const RowArgs& a, int live, int lane) {
-    const int mt = (live + TILE - 1) / TILE;
+    const int mt = (live + TILE - 1) / TILE, tiles = mt * a.ht;
     if (mt == 0) return 1;
-    const int dw_steps = ((live <= TWO_TERMS ? 2 * low_term(live) : live) + STEP - 1) / STEP, most = a.slab_tiles / mt;
+    const int dw_steps = ((live <= TWO_TERMS ? 2 * low_term(live) : live) + STEP - 1) / STEP;
+    const int most = max(1, min(a.slab_tiles / mt, a.steps / 4)), least = max(1, min(a.pairs / tiles, most));
     const uint64_t dw_cost = (uint64_t)a.dw_tiles * dw_tile_cost(dw_steps);
     uint64_t best = ~uint64_t(0);              // cost, then the count
-    for (int s = 1 + lane; s <= most && (s == 1 || s * 4 <= a.steps); s += 32) {
-        const uint32_t c = (uint32_t)dh_tile_cost(a.steps, s), n = (uint32_t)(mt * a.ht) * s;
+    for (int s = least + lane; s <= most; s += 32) {
+        const uint32_t c = (uint32_t)dh_tile_cost(a.steps, s), n = (uint32_t)tiles * s;
         const uint64_t longest = (uint64_t)((n + a.pairs - 1) / a.pairs) * a.pairs * c, all = (uint64_t)n * c + dw_cost;
         const uint64_t cost = (longest > all ? longest : all) << 16 | (uint32_t)s;
         if (cost < best) best = cost;

@@ -107,6 +107,12 @@ class VerifyStep:
             L.deer_draft_stats(c.B, c.k, c.V, self.draft_ids, self.q_logits, self.acc_ws)
         self._stats_forked = True
 
+    def top_logits(self, ids: torch.Tensor, values: torch.Tensor):
+        """The step's rows as a teacher leaves them to the drafter (``HeadLoss.distill``): ids i32 and values f32 [M, K] of the
+        verifier's best tokens.  A step that keeps its logits (sampling, or store_logits)."""
+        assert self.logits is not None, "this step does not store its logits"
+        L.deer_top_logits(self.logits, ids, values)
+
     def accept(self):
         c = self.cfg
         prestats = self._stats_forked
@@ -472,36 +478,26 @@ class HeadLoss:
     overwrites them.  ``grad=False`` leaves room for the forward calls only."""
 
     def __init__(self, w: torch.Tensor, rows: int, top: int = 1, grad: bool = True):
-        self.w, self.rows, self.top = w, int(rows), int(top)
-        V, hid = w.shape
-        dev, f32 = w.device, torch.float32
-        self.loss = torch.empty(rows, dtype=f32, device=dev)
-        self.lse = torch.empty(rows, dtype=f32, device=dev)
-        self.target_logit = torch.empty(rows, self.top, dtype=f32, device=dev)
-        self._first_logit = self.target_logit.view(-1)[:rows]           # a cross entropy's [rows]
-        self.dh = torch.empty(rows, hid, dtype=torch.bfloat16, device=dev) if grad else None
-        self.dw = torch.empty_like(w) if grad else None
-        self.ws = _ws(max(L.deer_lmhead_loss_workspace_bytes(rows, hid, V, self.top, g) for g in ((False, True) if grad else (False,))), dev)
+        self.buffers = b = L.HeadLossBuffers(w, rows, top, grad)
+        self.w, self.rows, self.top = w, b.M, b.K
+        self.loss, self.lse, self.target_logit, self.dh, self.dw = b.loss, b.lse, b.target_logit, b.dh, b.dw
         self._step = None
 
     def cross_entropy(self, h: torch.Tensor, targets: torch.Tensor, row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
-        L.deer_lmhead_loss(h, self.w, targets, self.loss, self.lse, self._first_logit, self.ws, row_weight)
+        """h bf16 [rows, hid], targets i32 [rows] (negative: no target), row_weight f32 [rows]; the losses f32 [rows]."""
+        self.buffers.run_loss(h, targets, row_weight=row_weight)
         self._step = (h, targets, None, 1.0, row_weight)
         return self.loss
 
     def distill(self, h: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
                 row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
-        L.deer_lmhead_distill(h, self.w, ids, teacher, temperature, self.loss, self.lse, self.target_logit, self.ws, row_weight)
+        """ids i32 and teacher f32 [rows, top]: what ``deer_top_logits`` leaves of the verifier's rows."""
+        self.buffers.run_loss(h, ids, teacher, temperature, row_weight)
         self._step = (h, ids, teacher, temperature, row_weight)
         return self.loss
 
     def backward(self, grad_loss: Optional[torch.Tensor] = None, head: bool = True):
         """(dh, dw) of the latest loss; ``head=False``: the hidden states' alone (a frozen head), dw is None."""
         assert self._step is not None and self.dh is not None, "backward() follows a loss of an object made with grad=True"
-        h, ids, teacher, temperature, row_weight = self._step
-        dw = self.dw if head else None
-        if teacher is None:
-            L.deer_lmhead_loss_grad(h, self.w, ids, self.lse, self._first_logit, self.dh, dw, self.ws, row_weight, grad_loss)
-        else:
-            L.deer_lmhead_distill_grad(h, self.w, ids, teacher, temperature, self.lse, self.target_logit, self.dh, dw, self.ws, row_weight, grad_loss)
-        return self.dh, dw
+        self.buffers.run_grad(*self._step, grad_loss, head)
+        return self.dh, self.dw if head else None
