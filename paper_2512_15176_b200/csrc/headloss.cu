@@ -57,9 +57,9 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.h = (__nv_bfloat16*)take((size_t)s.Mp * hid * 2);
     if (!grad) {
         s.stats_n = tile_columns(mt, V, 16, groups);
-        s.pos = (int*)take((size_t)K * s.Mp * 4);
+        s.place = (int*)take((size_t)K * s.Mp * 4);
         s.z = (float*)take((size_t)K * s.Mp * 4);
-        s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * 8);
+        s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * STATS_SHARE * 8);
         s.bytes = at;
         return s;
     }
@@ -70,7 +70,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.piece = (int)(((V + s.pieces - 1) / s.pieces + TILE - 1) / TILE * TILE);
     s.pieces = (V + s.piece - 1) / s.piece;
     s.grad_n = tile_columns(mt, s.piece < V ? s.piece : V, 16, groups);
-    s.hid_n = tile_columns(1, hid, 64, 1);
+    s.hid_n = tile_columns(1, hid, 32, 1);
     // space for dh's partial sums: as many ranges as two rounds of tiles take
     const int ht = (hid + s.hid_n - 1) / s.hid_n;
     s.slab_tiles = 2 * pairs / ht > mt ? 2 * pairs / ht : mt;
@@ -194,6 +194,29 @@ struct List {
     }
 };
 
+// Sorts N x 32 keys of a warp, key i * 32 + lane in key[i], by a bitonic network.
+template <int N>
+__device__ __forceinline__ void sort_warp(uint64_t (&key)[MAX_TOP / 32], int lane) {
+#pragma unroll
+    for (int size = 2; size <= N * 32; size <<= 1)
+#pragma unroll
+        for (int step = size >> 1; step > 0; step >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool rising = ((i * 32 + lane) & size) == 0;
+                if (step < 32) {
+                    const uint64_t other = __shfl_xor_sync(0xffffffffu, key[i], step);
+                    const bool keep_less = ((lane & step) == 0) == rising;
+                    key[i] = (other < key[i]) == keep_less ? other : key[i];
+                } else if ((i & (step / 32)) == 0) {
+                    const uint64_t a = key[i], b = key[i | (step / 32)];
+                    const bool swap = (b < a) == rising;
+                    key[i] = swap ? b : a;
+                    key[i | (step / 32)] = swap ? a : b;
+                }
+            }
+}
+
 // Moves the live rows together and lists their tokens by rising id.  A block takes `per_block` rows and counts the live
 // ones among all rows itself (M flags from L2: less than the launch of a kernel that counts); a warp takes a row.
 // GRAD: also what the products' epilogue needs of a row and of its listed tokens.
@@ -201,8 +224,8 @@ template <bool GRAD>
 __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a) {
     __shared__ int sums[2][ROW_WARPS];
     __shared__ float tops[ROW_WARPS];
-    __shared__ int list_id[ROW_WARPS][MAX_TOP];
-    __shared__ float list_t[ROW_WARPS][MAX_TOP];
+    __shared__ int list_id[GRAD ? ROW_WARPS : 1][MAX_TOP];
+    __shared__ float2 list_t[GRAD ? ROW_WARPS : 1][MAX_TOP];       // t and z by the list's order
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_trigger();
     pdl_wait();
@@ -306,35 +329,50 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
                         if (low) dst[(size_t)low * chunks + c0 + 32 * i] = x[i];
                     }
             }
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < MAX_TOP / 32; ++i) {
-                list_id[warp][i * 32 + lane] = l.id[i];
-                if (GRAD) list_t[warp][i * 32 + lane] = expf(l.log_t[i]);
-            }
+            // the list by rising id (and by its own order among equals): an entry is its id and where it stood
+            uint64_t key[MAX_TOP / 32];
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < MAX_TOP / 32; ++i) {
                 const int j = i * 32 + lane;
-                if (j >= a.K) continue;
-                int place = j;
-                float t = 0.f;                             // the token's probability, wherever the list names it
-                bool before_too = false;                   // listed before
-                if (j < l.n) {
-                    place = 0;
-#pragma unroll 4
-                    for (int o = 0; o < l.n; ++o) {
-                        const int other = list_id[warp][o];
-                        const bool same = other == l.id[i];
-                        place += other < l.id[i] || (same && o < j);
-                        before_too |= same && o < j;
-                        if (GRAD && same) t += list_t[warp][o];
-                    }
+                key[i] = (uint64_t)(j < l.n ? (uint32_t)l.id[i] : 0x7fffffffu) << 32 | (uint32_t)j;
+                if (GRAD) list_t[warp][j] = make_float2(expf(l.log_t[i]), l.z[i]);
+            }
+            __syncwarp();
+            if (a.K <= 32) sort_warp<1>(key, lane);
+            else if (a.K <= 64) sort_warp<2>(key, lane);
+            else sort_warp<4>(key, lane);
+            bool repeats = false;
+            if (GRAD) {
+#pragma unroll
+                for (int i = 0; i < MAX_TOP / 32; ++i) {
+                    const int id = (int)(key[i] >> 32);
+                    int left = __shfl_up_sync(0xffffffffu, id, 1);
+                    const int behind = i > 0 ? (int)(__shfl_sync(0xffffffffu, key[i > 0 ? i - 1 : 0], 31) >> 32) : -1;
+                    if (lane == 0) left = behind;
+                    repeats |= i * 32 + lane < l.n && left == id;
+                    list_id[warp][i * 32 + lane] = l.id[i];
                 }
-                const size_t at = (size_t)place * a.s.Mp + slot;
-                a.s.ids[at] = j < l.n ? l.id[i] : INT_MAX;
-                if (!GRAD) a.s.pos[at] = before_too ? ~j : j;
-                if (GRAD && j < l.n) a.s.gval[at] = coef == 0.f ? 0.f : coef * (expf(l.z[i] / a.tau - lse) - t);
+                repeats = __any_sync(0xffffffffu, repeats);
+                __syncwarp();
+            }
+#pragma unroll
+            for (int i = 0; i < MAX_TOP / 32; ++i) {
+                const int place = i * 32 + lane, id = (int)(key[i] >> 32), j = (int)(key[i] & 0x7f);
+                int left = __shfl_up_sync(0xffffffffu, id, 1);
+                const int behind = i > 0 ? (int)(__shfl_sync(0xffffffffu, key[i > 0 ? i - 1 : 0], 31) >> 32) : -1;
+                if (lane == 0) left = behind;
+                if (place >= a.K) continue;
+                a.s.ids[(size_t)slot * a.K + place] = place < l.n ? id : INT_MAX;
+                if (!GRAD) a.s.place[(size_t)slot * a.K + j] = left == id ? -1 : place;
+                if (GRAD && place < l.n) {
+                    float t = list_t[warp][j].x;           // the token's probability, wherever the list names it
+                    if (repeats) {
+                        t = 0.f;
+                        for (int o = 0; o < l.n; ++o) t += list_id[warp][o] == id ? list_t[warp][o].x : 0.f;
+                    }
+                    a.s.gval[(size_t)slot * a.K + place] = coef == 0.f ? 0.f : coef * (expf(list_t[warp][j].y / a.tau - lse) - t);
+                }
             }
             load_row(m + ROW_WARPS);
         }
@@ -342,47 +380,63 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     }
 }
 
-// lse and loss of every row from its tiles' (max, sum exp): a warp per row.
-__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int tiles, float c2, float c2_low, float* loss, float* lse_out, float* target_logit) {
-    const int lane = threadIdx.x & 31, m = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
+// lse and loss of every row from its tiles' partial sums: a warp per row, or (few rows, which may have thousands) a block.
+__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int as_is, int wide, int tiles, float c2, float c2_low, float* loss, float* lse_out, float* target_logit) {
+    __shared__ float2 warps[ROW_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = wide ? blockIdx.x : blockIdx.x * ROW_WARPS + warp;
     pdl_trigger();
     pdl_wait();
-    if (m >= a.M) return;
-    const int slot = a.M <= ONE_BLOCK ? (is_live(a, m) ? m : -1) : a.s.slot[m];      // (as STATS took them)
+    if (m >= a.M) return;                                  // (never a part of a block, where wide)
+    const int slot = as_is ? (is_live(a, m) ? m : -1) : a.s.slot[m];       // (as STATS took them)
     List l;
     l.load(a, target_logit, m, lane);
     l.find_end(a, lane);
-#pragma unroll
-    for (int i = 0; i < MAX_TOP / 32; ++i) {
-        const int j = i * 32 + lane;
-        if (j < a.K && (slot < 0 || j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
-    }
     if (slot < 0) {
+        if (wide && warp > 0) return;
+        for (int j = lane; j < a.K; j += 32) target_logit[(size_t)m * a.K + j] = 0.f;
         if (lane == 0) loss[m] = lse_out[m] = 0.f;
         return;
     }
-    const bool some = l.targets(a, lane);
     // in powers of two, relative to the largest of the tiles' references
     const float2* part = a.s.part + (size_t)slot * tiles;
     float top = -INFINITY, sum = 0.f;                      // (a lane's, and its sum relative to that)
 #pragma unroll 4
-    for (int i = lane; i < tiles; i += 32) {
+    for (int i = wide ? threadIdx.x : lane; i < tiles; i += wide ? ROW_THREADS : 32) {
         const float2 p = part[i];
         const float m2 = fmaxf(top, p.x), shift = m2 == -INFINITY ? 0.f : m2;
         sum = sum * exp2f(top - shift) + p.y * exp2f(p.x - shift);
         top = m2;
     }
-    const float all = warp_max(top);
+    float all = warp_max(top);
     sum = warp_sum(sum * (top == -INFINITY ? 0.f : exp2f(top - all)));
+    if (wide) {                                            // the first warp goes on with the block's
+        if (lane == 0) warps[warp] = make_float2(all, sum);
+        __syncthreads();
+        if (warp > 0) return;
+        const float2 p = lane < ROW_WARPS ? warps[lane] : make_float2(-INFINITY, 0.f);
+        all = warp_max(p.x);
+        sum = warp_sum(p.y * (p.x == -INFINITY ? 0.f : exp2f(p.x - all)));
+    }
+    const bool some = l.targets(a, lane);
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        const int j = i * 32 + lane;
+        if (j < a.K && (j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
+    }
     // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
     float more = 0.f;
 #pragma unroll
     for (int i = 0; i < MAX_TOP / 32; ++i) {
         const int j = i * 32 + lane;
         if (j >= l.n || l.id[i] >= a.V) continue;
-        const float tile_z = a.s.z[(size_t)j * a.s.Mp + slot];
+        int at = j;                                        // (as they are: each token at its first entry)
+        if (as_is)
+            for (int o = 0; o < j; ++o) at = a.ids[(size_t)m * a.K + o] == l.id[i] ? -1 : at;
+        else at = a.s.place[(size_t)slot * a.K + j];
         l.z[i] = fmaf(l.z[i], c2_low, fmaf(l.z[i], c2, -all));
-        if (!isnan(tile_z)) more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, c2_low, fmaf(tile_z, c2, -all)));
+        if (at < 0) continue;
+        const float tile_z = a.s.z[(size_t)slot * a.K + at];
+        more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, c2_low, fmaf(tile_z, c2, -all)));
     }
     const float log_sum = logf(sum + warp_sum(more));
     float each = 0.f;
@@ -397,32 +451,55 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
     }
 }
 
-// dh of every row: the partial sums of its ranges in their order, zeros for a dead row.  A thread takes four columns, so that
-// few rows with many ranges still have their loads side by side.
-__global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, __nv_bfloat16* dh) {
+// dh of every row: the partial sums of its ranges in a fixed order, zeros for a dead row.  A block takes 128 columns of
+// up to eight rows; where there are many partial sums its warps share a row's, so that they are all on their way at once.
+__global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, int per_block, __nv_bfloat16* dh) {
+    __shared__ float4 sums[ROW_WARPS][ROW_WARPS][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int m0 = blockIdx.x * per_block, rows = min(per_block, a.M - m0), c = (blockIdx.y * 32 + lane) * 4;
+    const bool in = c < a.hid;
     pdl_trigger();
     pdl_wait();
-    const long i = (long)blockIdx.x * ROW_THREADS + threadIdx.x;
-    const int quads = a.hid / 4, m = (int)(i / quads), c = (int)(i % quads) * 4;
-    if (m >= a.M) return;
-    const int slot = a.s.slot[m], live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
+    const int live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
     // few live rows: a range's tile holds the two terms' products, 128 rows each
-    const int terms = live <= TWO_TERMS ? 2 : 1;
-    const size_t part_rows = terms == 2 ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
+    const int parts = live <= TWO_TERMS ? 2 * ranges : ranges;
+    const size_t part_rows = live <= TWO_TERMS ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
     const float scale = a.s.hdr[HDR_GAVE_UP] ? NAN : __int_as_float(a.s.hdr[HDR_SCALE]);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (slot >= 0) {
+    auto part_sum = [&](int slot, int first, int step) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         const float* src = a.s.slab + (size_t)slot * a.hid + c;
 #pragma unroll 8
-        for (int r = 0; r < ranges * terms; ++r) {
+        for (int r = first; r < parts; r += step) {
             const float4 x = *reinterpret_cast<const float4*>(src + (size_t)r * part_rows * a.hid);
             v.x += x.x;
             v.y += x.y;
             v.z += x.z;
             v.w += x.w;
         }
-    }
-    *reinterpret_cast<uint2*>(dh + (size_t)m * a.hid + c) = make_uint2(pack_bf16(v.x * scale, v.y * scale), pack_bf16(v.z * scale, v.w * scale));
+        return v;
+    };
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool share = parts > 4;
+    if (share && in)
+        for (int r = 0; r < rows; ++r) {
+            const int slot = a.s.slot[m0 + r];
+            if (slot >= 0) sums[r][warp][lane] = part_sum(slot, warp, ROW_WARPS);
+        }
+    __syncthreads();
+    if (warp >= rows || !in) return;
+    const int slot = a.s.slot[m0 + warp];
+    float4 v = zero;
+    if (slot >= 0 && !share) v = part_sum(slot, 0, 1);
+    if (slot >= 0 && share)
+#pragma unroll
+        for (int i = 0; i < ROW_WARPS; ++i) {
+            const float4 x = sums[warp][i][lane];
+            v.x += x.x;
+            v.y += x.y;
+            v.z += x.z;
+            v.w += x.w;
+        }
+    *reinterpret_cast<uint2*>(dh + (size_t)(m0 + warp) * a.hid + c) = make_uint2(pack_bf16(v.x * scale, v.y * scale), pack_bf16(v.z * scale, v.w * scale));
 }
 
 static int check_sizes(const char* call, int K, float tau, int M, int hid, int V) {
@@ -461,7 +538,7 @@ static RowArgs row_args(const Space& s, const void* h, const int32_t* ids, const
     a.hid = hid;
     a.V = V;
     a.K = K;
-    a.per_block = ROW_WARPS * ((M + 2047) / 2048);         // at most 256 blocks: each of them counts all rows
+    a.per_block = ROW_WARPS * ((M + 4095) / 4096);         // at most 512 blocks: each of them counts all rows
     a.h = static_cast<const __nv_bfloat16*>(h);
     a.ids = ids;
     a.teacher = teacher;
@@ -492,10 +569,12 @@ static int loss_call(const char* call, const void* h, const void* w, const int32
     static bool rows_set[64] = {}, loss_set[64] = {};
     DEER_CUDA(keep_split(head_rows_kernel<false>, rows_set));
     DEER_CUDA(keep_split(head_loss_kernel, loss_set));
-    if (M > ONE_BLOCK) DEER_CUDA(launch_pdl(head_rows_kernel<false>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
+    const bool as_is = takes_rows_as_they_are(M, K);
+    if (!as_is) DEER_CUDA(launch_pdl(head_rows_kernel<false>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
     rc = launch_product(STATS, s, h, w, ids, row_weight, M, hid, V, K, 0, tau, target_logit, false, nullptr, st);
     if (rc != DEER_OK) return rc;
-    DEER_CUDA(launch_pdl(head_loss_kernel, dim3((M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (V + s.stats_n - 1) / s.stats_n, c2, c2_low,
+    const bool wide = M <= 512;
+    DEER_CUDA(launch_pdl(head_loss_kernel, dim3(wide ? M : (M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (int)as_is, (int)wide, (V + s.stats_n - 1) / s.stats_n * STATS_SHARE, c2, c2_low,
                          loss, lse, target_logit));
     return DEER_OK;
 }
@@ -536,8 +615,11 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
         if (rc == DEER_OK) rc = launch_product(BACK, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, dh != nullptr, dw, st);
         if (rc != DEER_OK) return rc;
     }
-    if (dh)
-        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((unsigned)(((long)M * hid / 4 + ROW_THREADS - 1) / ROW_THREADS)), dim3(ROW_THREADS), 0, st, a, static_cast<__nv_bfloat16*>(dh)));
+    if (dh) {
+        const int per_block = M <= 512 ? 1 : ROW_WARPS;    // (few rows may have many partial sums each)
+        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((unsigned)((M + per_block - 1) / per_block), (unsigned)((hid + 127) / 128)), dim3(ROW_THREADS), 0, st,
+                             a, per_block, static_cast<__nv_bfloat16*>(dh)));
+    }
     return DEER_OK;
 }
 

@@ -12,10 +12,14 @@ namespace headloss {
 
 constexpr int TILE = 256;                  // rows of a product's tile: 128 in each block of a pair
 constexpr int ONE_BLOCK = 128;             // up to this many rows STATS and GRAD work by single blocks: a pair would leave half of its
-                                           // lanes empty and the products, not the reading of w, would bound the call.  STATS takes
-                                           // the rows as they are then: a dead one costs nothing in a tile that is not full
+                                           // lanes empty and the products, not the reading of w, would bound the call
+constexpr int SHORT = 8;                   // lists of up to so many entries are searched as they are: with them single blocks of
+                                           // STATS take the call's rows themselves (a dead one costs nothing in a tile that is
+                                           // not full), which saves a launch
+inline bool takes_rows_as_they_are(int M, int K) { return M <= ONE_BLOCK && K <= SHORT; }
 constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
+constexpr int STATS_SHARE = 2;            // warps that share a tile's columns in STATS: partial sums a row has of a tile
 constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3;
 // Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in dh's product,
 // idle then, and the contraction that the steps of dw's leave free.  That sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
@@ -33,13 +37,13 @@ struct Space {
     int* hdr;                  // [4]
     int* slot;                 // [M]        place of a row among the live ones, -1: dead
     int* row;                  // [Mp]       the row at a place
-    int* ids;                  // [K][Mp]    a live row's list by rising id, INT_MAX behind its end
-    int* pos;                  // [K][Mp]    where an entry stood in the list, ~ that of a token listed before    (loss)
-    float* z;                  // [K][Mp]    by the list's order: a token's z as the tiles have it, NaN: listed before  (loss)
+    int* ids;                  // [Mp][K]    a live row's list by rising id, INT_MAX behind its end
+    int* place;                // [Mp][K]    an entry's place among the rising ids, -1: a token listed before    (loss)
+    float* z;                  // [Mp][K]    by rising id (as they are: by the list): the token's z as the tiles have it  (loss)
     float2* part;              // [Mp][tiles] (m, sum 2^(z log2(e) / tau - m))            (loss)
     float* coef;               // [Mp]       what a row's probabilities count            (gradient)
     float* lse2;               // [Mp]       lse log2(e)                                 (gradient)
-    float* gval;               // [K][Mp]    G at the listed tokens                      (gradient)
+    float* gval;               // [Mp][K]    G at the listed tokens                      (gradient)
     __nv_bfloat16* h;          // [Mp][hid]  live rows
     __nv_bfloat16* g;          // [Mp][piece]                                            (gradient)
     float* slab;               // [slab_tiles * 256][hid]  partial dh                    (gradient)
@@ -52,7 +56,8 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad);
 
 struct ProductArgs {
     int M;
-    const int* list;           // the call's lists and row weights: STATS by single blocks
+    int as_is;                 // STATS: the call's rows and lists, not the live ones moved together
+    const int* list;           // the call's lists and row weights
     const float* weight;
     const int* hdr_in;
     int* hdr;
@@ -61,11 +66,10 @@ struct ProductArgs {
     int col_tiles;             // tiles along the columns (vocabulary or hid)
     int want_dh, row_tiles;    // BACK: whether dh is asked for; dw's tiles along the vocabulary (0: not asked for)
     int a_rows;                // rows of the 128-row operand one block loads (fewer than 128 only where M is)
-    int Mp, K, tiles;
+    int K, tiles;
     int add;                   // BACK: a piece behind the first
     float c2, c2_low;          // log2(e) / tau, and what fp32 leaves of it
     const int* ids;
-    const int* pos;
     const int* row;
     const __nv_bfloat16* h;
     const __nv_bfloat16* w;
@@ -76,11 +80,12 @@ struct ProductArgs {
     const float* lse2;
     const float* gval;
     __nv_bfloat16* g;
+    __nv_bfloat16* dw;
     int g_pitch;
 };
 
 // Launches one product of the call: `piece` counts the pieces of the vocabulary (STATS: the whole of it).
-// h, list, weight: the call's own (STATS); dh and dw: what is asked for (BACK).
+// h, list, weight: the call's own; dh and dw: what is asked for (BACK).
 int launch_product(Product what, const Space& s, const void* h, const void* w, const int* list, const float* weight, int M, int hid, int V, int K,
                    int piece, float tau, float* target_logit, bool want_dh, void* dw, cudaStream_t st);
 

@@ -1,7 +1,7 @@
 // The products of the LM head's losses on the tensor cores:
 //
-//   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid; two warps per block beside it
-//                                                   compute the listed tokens' z once more on the CUDA cores
+//   STATS  z = h w^T                 [live][V]      rows of h on the lanes, contraction hid; eight warps per block beside
+//                                                   it compute the listed tokens' z once more on the CUDA cores
 //   GRAD   G = coef (p - t)          [live][piece]  the same z again, softmax and targets in the epilogue
 //   BACK   dh = G w                  [live][hid]    contraction over the piece's vocabulary, in ranges
 //          dw = G^T h                [piece][hid]   contraction over the live rows
@@ -35,19 +35,20 @@ using namespace sm100;
 namespace headloss {
 
 constexpr int BOX = 4096;                  // 32 rows x 128 bytes of a finished tile, as they leave through TMA
-constexpr int DOT_WARPS = 2;
+constexpr int DOT_WARPS = 8;
 // What a variant is made of: P the product, CG the blocks that share a tile.
 template <int P, int CG>
 struct Shape {
     static constexpr int A = 16384;                        // a block's share of an operand's step: 128 rows (columns) x 64 bf16
     static constexpr int B = 32768 / CG;                   // n columns, or this block's half of them
-    static constexpr int EPI = P == GRAD ? 8 : 4;           // epilogue warps, four to 32 x n or two to half of it each
-    static constexpr int STAGING = P == STATS ? 0 : EPI * 2 * BOX;
+    static constexpr int EPI = P == BACK ? 4 : 8;          // epilogue warps: with eight, two share a quarter of the lanes
+    static constexpr int STAGING = P == STATS ? EPI * BOX : EPI * 2 * BOX;
     static constexpr int STAGES = (232448 - STAGING - 1024 - 256) / (A + B);
     static constexpr int SMEM = STAGES * (A + B) + STAGING + 1024 /*alignment*/ + 256 /*barriers*/;
     static constexpr int THREADS = 64 + 32 * EPI + (P == STATS ? 32 * DOT_WARPS : 0);
     static constexpr int ROWS = 128 * CG;                  // lanes of a tile
 };
+static_assert(Shape<STATS, 1>::EPI == 4 * STATS_SHARE && Shape<STATS, 2>::EPI == 4 * STATS_SHARE, "partial sums of a tile");
 constexpr int ACC = 256;                   // columns of one accumulator
 
 __device__ __forceinline__ float ex2(float x) {
@@ -67,18 +68,16 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-#define TMEM_LD_X1(taddr, r) asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr))
+__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 
 // kind::f16 instruction descriptor: bf16 x bf16 -> fp32, M = 128 of each block, N = n.
 template <int CG>
 __device__ __forceinline__ uint32_t idesc_of(int n, bool a_mn, bool b_mn) {
     return (CG == 2 ? make_idesc_bf16_pair(n) : make_idesc_bf16(n, 0)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
-}
-
-// STATS by single blocks takes the call's rows and lists as they are, dead rows among them.
-template <int P, int CG>
-__host__ __device__ constexpr bool direct() {
-    return P == STATS && CG == 1;
 }
 
 // A tile: rows and columns of the product, range of the contraction in steps.
@@ -93,7 +92,7 @@ struct List {
     int live, steps, mt, ct, low, ranges, dw_steps, n, n_dw, group, groups;    // low: place of the second term's rows, 0: none
     int mine, light, ahead;
     __device__ __forceinline__ List(const ProductArgs& a) {
-        live = direct<P, CG>() ? a.M : a.hdr_in[HDR_LIVE];
+        live = P == STATS && a.as_is ? a.M : a.hdr_in[HDR_LIVE];
         mt = (live + Shape<P, CG>::ROWS - 1) / Shape<P, CG>::ROWS;
         ct = a.col_tiles;
         low = P != STATS && live <= TWO_TERMS ? low_term(live) : 0;
@@ -149,17 +148,16 @@ struct List {
 };
 
 // z of the listed tokens by plain fp32 sums: a warp takes four entries of a row at a time.
-template <bool DIRECT>
 __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, int warp, int warps, int lane) {
     const int groups = (a.K + 3) / 4;
     for (long i = warp; i < (long)live * groups; i += warps) {
-        const int slot = (int)(i / groups), e0 = (int)(i % groups) * 4;
-        if (DIRECT && !is_live(a.list, a.weight, a.K, slot)) continue;
+        const int slot = (int)(i / groups), e0 = (int)(i % groups) * 4, m = a.as_is ? slot : a.row[slot];
+        if (a.as_is && !is_live(a.list, a.weight, a.K, m)) continue;
         const __nv_bfloat16* w[4];
         bool on[4], any = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int id = e0 + j < a.K ? (DIRECT ? a.list[(size_t)slot * a.K + e0 + j] : a.ids[(size_t)(e0 + j) * a.Mp + slot]) : -1;
+            const int id = e0 + j < a.K ? a.list[(size_t)m * a.K + e0 + j] : -1;
             on[j] = id >= 0 && id < a.V;      // (an entry behind a list's end may be summed: what it gives is not read)
             any |= on[j];
             w[j] = a.w + (on[j] ? (size_t)id * a.hid : 0);
@@ -167,19 +165,26 @@ __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, in
         if (!any) continue;
         const __nv_bfloat16* h = a.h + (size_t)slot * a.hid;
         float sum[4][2] = {};
-        for (int c = lane * 8; c < a.hid; c += 256) {
-            const uint4 x = *reinterpret_cast<const uint4*>(h + c);
-            uint4 y[4];
+        for (int c0 = lane * 8; c0 < a.hid; c0 += 512) {
+            uint4 x[2], y[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = on[j] ? *reinterpret_cast<const uint4*>(w[j] + c) : make_uint4(0, 0, 0, 0);
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+            for (int u = 0; u < 2; ++u) {
+                const int c = c0 + u * 256;
+                x[u] = c < a.hid ? *reinterpret_cast<const uint4*>(h + c) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t ys[4] = {y[j].x, y[j].y, y[j].z, y[j].w};
+                for (int j = 0; j < 4; ++j) y[u][j] = on[j] && c < a.hid ? *reinterpret_cast<const uint4*>(w[j] + c) : make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    sum[j][0] = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ys[k] << 16), sum[j][0]);
-                    sum[j][1] = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), sum[j][1]);
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t ys[4] = {y[u][j].x, y[u][j].y, y[u][j].z, y[u][j].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        sum[j][0] = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ys[k] << 16), sum[j][0]);
+                        sum[j][1] = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), sum[j][1]);
+                    }
                 }
             }
         }
@@ -188,36 +193,63 @@ __device__ __forceinline__ void listed_logits(const ProductArgs& a, int live, in
             float s = sum[j][0] + sum[j][1];
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (lane == 0 && on[j]) {
-                const int pos = DIRECT ? e0 + j : a.pos[(size_t)(e0 + j) * a.Mp + slot];
-                a.target_logit[(size_t)(DIRECT ? slot : a.row[slot]) * a.K + (pos < 0 ? ~pos : pos)] = s;
-            }
+            if (lane == 0 && on[j]) a.target_logit[(size_t)m * a.K + e0 + j] = s;
         }
     }
 }
 
-// The first token of a row's list at or behind `from`, INT_MAX: none.  With `store`, z goes to the entries that name
-// from - 1, NaN to all of them but the first.
-__device__ __forceinline__ int next_listed(const ProductArgs& a, int m, int from, bool store, float z) {
-    int next = 0x7fffffff;
-    bool open = true;
-    for (int j0 = 0; j0 < a.K; j0 += 4) {
-        int id[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) id[i] = j0 + i < a.K ? a.list[(size_t)m * a.K + j0 + i] : -1;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            open &= id[i] >= 0;
-            if (open && id[i] >= from) next = min(next, id[i]);
-            if (open && store && id[i] == from - 1) {
-                a.z[(size_t)(j0 + i) * a.Mp + m] = z;
-                z = NAN;
-            }
+// The listed tokens of one row in rising order, from the tile's first column on: `id` is the next, INT_MAX behind the last.
+// What belongs to an entry comes one entry ahead.
+struct Listed {
+    int id = 0x7fffffff, e = 0, next = 0x7fffffff;
+    float val = 0.f, next_val = 0.f;           // GRAD: G at the token
+    __device__ __forceinline__ int id_at(const ProductArgs& a, int slot, int i) const { return i < a.K ? a.ids[(size_t)slot * a.K + i] : 0x7fffffff; }
+    // lists by rising id
+    template <bool VALUES>
+    __device__ __forceinline__ void start(const ProductArgs& a, int slot, int from) {
+        int hi = a.K;
+        e = 0;
+        while (e < hi) {
+            const int mid = (e + hi) >> 1;
+            if (a.ids[(size_t)slot * a.K + mid] < from) e = mid + 1;
+            else hi = mid;
         }
-        if (!open) break;
+        id = id_at(a, slot, e);
+        next = id_at(a, slot, e + 1);
+        if (VALUES) {
+            val = e < a.K ? a.gval[(size_t)slot * a.K + e] : 0.f;
+            next_val = e + 1 < a.K ? a.gval[(size_t)slot * a.K + e + 1] : 0.f;
+        }
     }
-    return next;
-}
+    template <bool VALUES>
+    __device__ __forceinline__ void advance(const ProductArgs& a, int slot) {
+        ++e;
+        id = next;
+        val = next_val;
+        next = id_at(a, slot, e + 1);
+        if (VALUES) next_val = e + 1 < a.K ? a.gval[(size_t)slot * a.K + e + 1] : 0.f;
+    }
+    // a short list as it is; with `store`, z goes to the first entry that names from - 1
+    __device__ __forceinline__ void search(const ProductArgs& a, int m, int from, bool store, float z) {
+        id = 0x7fffffff;
+        bool open = true;
+        for (int j0 = 0; j0 < a.K; j0 += 4) {
+            int at[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) at[i] = j0 + i < a.K ? a.list[(size_t)m * a.K + j0 + i] : -1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                open &= at[i] >= 0;
+                if (open && at[i] >= from) id = min(id, at[i]);
+                if (open && store && at[i] == from - 1) {
+                    a.z[(size_t)m * a.K + j0 + i] = z;
+                    store = false;
+                }
+            }
+            if (!open) break;
+        }
+    }
+};
 
 template <int P, int CG>
 __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap* tm_out, const CUtensorMap* tm_out_dw, const List<P, CG>& list, int warp, int lane, int rank,
@@ -234,25 +266,18 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
         const int buf = it & 1;
         const bool computed = t.kb > 0;
         const int slot = t.r * Shape<P, CG>::ROWS + lane_row;             // STATS, GRAD: place among the live rows
-        const bool row_ok = slot < list.live && (!direct<P, CG>() || is_live(a.list, a.weight, a.K, slot));
+        const bool row_ok = slot < list.live && (P != STATS || !a.as_is || is_live(a.list, a.weight, a.K, slot));
         const int col0 = t.c * a.n;
         // what the tile needs of its rows comes while it is computed: a row's first listed token at or behind its start
         float coef = 0.f, nlse = 0.f;
-        int e = 0, next = 0x7fffffff;
-        if (direct<P, CG>()) {
-            if (row_ok) next = next_listed(a, slot, col0, false, 0.f);
-        } else if ((P == STATS || P == GRAD) && row_ok) {
-            if (P == GRAD) {
-                coef = a.coef[slot];
-                nlse = -a.lse2[slot];
-            }
-            int hi = a.K;
-            while (e < hi) {
-                const int mid = (e + hi) >> 1;
-                if (a.ids[(size_t)mid * a.Mp + slot] < a.v0 + col0) e = mid + 1;
-                else hi = mid;
-            }
-            if (e < a.K) next = a.ids[(size_t)e * a.Mp + slot];
+        Listed listed;
+        if (P == GRAD && row_ok) {
+            coef = a.coef[slot];
+            nlse = -a.lse2[slot];
+        }
+        if ((P == STATS || P == GRAD) && row_ok) {
+            if (P == STATS && a.as_is) listed.search(a, slot, col0, false, 0.f);
+            else listed.start<P == GRAD>(a, slot, a.v0 + col0);
         }
         if (computed) {
             const bool got = mbar_wait(tfull0 + 8u * buf, (uint32_t)(it >> 1) & 1u, abort_flag);
@@ -264,8 +289,9 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
 
         if (P == STATS) {
             const int width = min(a.n, a.vn - col0);                      // columns that exist
+            const bool idle = !__any_sync(0xffffffffu, row_ok);           // (lanes behind the last row)
             float run_m = -INFINITY, run_s = 0.f;
-            for (int c = 0; c < width; c += 32) {
+            for (int c = 32 * turn; c < width && !idle; c += 32 * SHARE) {
                 uint32_t v[32];
                 TMEM_LD_X32(taddr + c, v);
                 tmem_wait_ld();
@@ -294,32 +320,33 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                     s1 += ex2(fmaf(y, a.c2_low, fmaf(y, a.c2, -shift)));
                 }
                 run_s += s0 + s1;
-            }
-            if (row_ok) a.part[(size_t)slot * a.tiles + t.c] = make_float2(run_m, run_s);
-            // The z of listed tokens in this tile.  Few rows have one here, so each distinct column is read again.
-            const int first = a.v0 + col0, last = first + width;
-            for (;;) {
-                const int col = __reduce_min_sync(0xffffffffu, next);
-                if (col >= last) break;
-                uint32_t z;
-                TMEM_LD_X1(taddr + (uint32_t)(col - first), z);
-                tmem_wait_ld();
-                if (direct<P, CG>() && next == col) next = next_listed(a, slot, col + 1, true, __uint_as_float(z));
-                while (!direct<P, CG>() && next == col) {
-                    const int pos = a.pos[(size_t)e * a.Mp + slot];
-                    a.z[(size_t)(pos < 0 ? ~pos : pos) * a.Mp + slot] = pos < 0 ? NAN : __uint_as_float(z);
-                    ++e;
-                    next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
+                // the z of the row's listed tokens among these columns, by way of shared memory: registers have no index
+                const int begin = col0 + c, end = col0 + min(c + 32, width);
+                if (listed.id < end) {
+                    const uint32_t line = staging + (uint32_t)(warp - 2) * BOX + stg_row;
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) st_shared_v4(line + ((j ^ sw) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    do {
+                        const bool here = listed.id >= begin;              // (the other warp's columns lie between this one's)
+                        const uint32_t k = here ? (uint32_t)(listed.id - begin) : 0;
+                        const float z = ld_shared_f32(line + (((k >> 2) ^ sw) << 4) + (k & 3) * 4);
+                        if (a.as_is) {
+                            listed.search(a, slot, listed.id + 1, here, z);
+                        } else {
+                            if (here) a.z[(size_t)slot * a.K + listed.e] = z;
+                            listed.advance<false>(a, slot);
+                        }
+                    } while (listed.id < end);
                 }
-                __syncwarp();
             }
+            if (row_ok) a.part[(size_t)slot * a.tiles + t.c * SHARE + turn] = make_float2(run_m, run_s);
         } else if (P == GRAD || t.dw) {
             const int limit = P == GRAD ? a.vn : a.hid;
             const float scale = P == BACK ? __int_as_float(a.hdr_in[HDR_SCALE]) : 1.f;
             const bool two = P == GRAD && list.low > 0;
             const bool idle = two && (rank > 0 || quarter * 32 >= list.low);        // no rows of the first term
             for (int c = 64 * turn; c < a.n && col0 + c < limit && !idle; c += 64 * SHARE) {
-                const int wide = min(64, a.n - c);                        // (GRAD: the last chunk may be narrower than a box)
+                const int wide = min(64, a.n - c);                        // (the last chunk may be narrower than a box)
                 // the store from this box two chunks ago has read it (two terms: both boxes are used at once)
                 if (lane == 0) {
                     if (two) bulk_wait_read<0>();
@@ -363,32 +390,31 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 }
                 if (P == GRAD) {
                     const int first = a.v0 + col0 + c;
-                    while (next < first + wide) {                         // listed tokens: p - t, formed in fp32 beforehand
-                        if (next >= first) {                              // (the other warp's chunks lie between this one's)
-                            const uint32_t k = (uint32_t)(next - first);
-                            const float val = a.gval[(size_t)e * a.Mp + slot];
-                            const __nv_bfloat16 hi = __float2bfloat16(val), lo = __float2bfloat16(val - __bfloat162float(hi));
+                    while (listed.id < first + wide) {                    // listed tokens: p - t, formed in fp32 beforehand
+                        if (listed.id >= first) {                         // (the other warp's chunks lie between this one's)
+                            const uint32_t k = (uint32_t)(listed.id - first);
+                            const __nv_bfloat16 hi = __float2bfloat16(listed.val), lo = __float2bfloat16(listed.val - __bfloat162float(hi));
                             const uint32_t at = b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2;
                             st_shared_bf16(at, hi);
                             if (two) st_shared_bf16(at + other, lo);
                         }
-                        ++e;
-                        next = e < a.K ? a.ids[(size_t)e * a.Mp + slot] : 0x7fffffff;
+                        listed.advance<true>(a, slot);
                     }
                 }
-                if (P == GRAD && wide < 64) {                             // by plain stores: 32 bytes of a row at a time
-                    __nv_bfloat16* row = a.g + (size_t)(t.r * Shape<P, CG>::ROWS + lane_row) * a.g_pitch + col0 + c;
-                    const int stop = min(wide, a.g_pitch - col0 - c);
+                const int y = (P == BACK ? a.v0 : 0) + t.r * Shape<P, CG>::ROWS + rank * 128 + quarter * 32;
+                if (wide < 64) {                                          // by plain stores, 16 bytes of a row at a time
+                    const int pitch = P == GRAD ? a.g_pitch : a.hid;
+                    __nv_bfloat16* row = (P == GRAD ? a.g : a.dw) + (size_t)(y + lane) * pitch + col0 + c;
+                    const int stop = P == GRAD || y + lane < a.V ? min(wide, pitch - col0 - c) : 0;
                     for (int k = 0; k < stop; k += 8) {
                         *reinterpret_cast<uint4*>(row + k) = ld_shared_v4(b + (((uint32_t)(k >> 3) ^ sw) << 4));
-                        if (two) *reinterpret_cast<uint4*>(row + (size_t)list.low * a.g_pitch + k) = ld_shared_v4(b + other + (((uint32_t)(k >> 3) ^ sw) << 4));
+                        if (two) *reinterpret_cast<uint4*>(row + (size_t)list.low * pitch + k) = ld_shared_v4(b + other + (((uint32_t)(k >> 3) ^ sw) << 4));
                     }
                     if (!two) stg_i ^= 1;                                 // no store by TMA has taken this box: it is next again
                     continue;
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                const int y = (P == BACK ? a.v0 : 0) + t.r * Shape<P, CG>::ROWS + rank * 128 + quarter * 32;
                 if (lane == 0 && (P == GRAD || y < a.V)) {                // rows and columns beyond the tensor are clipped
                     tma_store_2d(P == BACK ? tm_out_dw : tm_out, box, col0 + c, y);
                     if (two) tma_store_2d(tm_out, box + other, col0 + c, list.low + quarter * 32);
@@ -576,7 +602,7 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
             }
         }
     } else if (warp >= 2 + S::EPI) {
-        if (P == STATS) listed_logits<direct<P, CG>()>(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - 2 - S::EPI, (int)gridDim.x * DOT_WARPS, lane);
+        if (P == STATS) listed_logits(a, list.live, (int)blockIdx.x * DOT_WARPS + warp - 2 - S::EPI, (int)gridDim.x * DOT_WARPS, lane);
     } else {
         epilogue<P, CG>(a, &tm_out, &dw.out, list, warp, lane, (int)rank, tmem_base, tfull0, tempty0, smem_base + STAGES * STAGE_BYTES, abort_flag);
     }
@@ -591,7 +617,7 @@ product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
             Tile t;
             for (int k = 0; list.tile(k, t); ++k)
                 for (int i = tid; i < S::ROWS; i += S::THREADS)
-                    if (t.r * S::ROWS + i < list.live) a.part[(size_t)(t.r * S::ROWS + i) * a.tiles + t.c] = make_float2(NAN, NAN);
+                    if (t.r * S::ROWS + i < list.live) a.part[(size_t)(t.r * S::ROWS + i) * a.tiles + t.c * STATS_SHARE] = make_float2(NAN, NAN);
         }
         for (int i = 0; i < 64; ++i) __nanosleep(10000);
         __syncthreads();
@@ -639,14 +665,12 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
     a.hdr_in = a.hdr = s.hdr;
     a.hid = hid;
     a.V = V;
-    a.Mp = s.Mp;
     a.K = K;
     scale_of(tau, a.c2, a.c2_low);
     a.ids = s.ids;
-    a.pos = s.pos;
     a.row = s.row;
-    const bool as_is = what == STATS && M <= ONE_BLOCK;
-    a.h = as_is ? static_cast<const __nv_bfloat16*>(h) : s.h;
+    a.as_is = what == STATS && takes_rows_as_they_are(M, K);
+    a.h = a.as_is ? static_cast<const __nv_bfloat16*>(h) : s.h;
     a.w = static_cast<const __nv_bfloat16*>(w);
     a.target_logit = target_logit;
     a.z = s.z;
@@ -672,9 +696,10 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
     } while (0)
     if (what == STATS || what == GRAD) {
         a.n = what == STATS ? s.stats_n : s.grad_n;
-        a.col_tiles = a.tiles = (a.vn + a.n - 1) / a.n;
+        a.col_tiles = (a.vn + a.n - 1) / a.n;
+        a.tiles = a.col_tiles * STATS_SHARE;
         const int cg = M > ONE_BLOCK ? 2 : 1;
-        MAP(map_bf16(&ta, a.h, as_is ? M : s.Mp, hid, hid, a.a_rows));
+        MAP(map_bf16(&ta, a.h, a.as_is ? M : s.Mp, hid, hid, a.a_rows));
         MAP(map_bf16(&tb, w, V, hid, hid, a.n / cg));
         to = td.a = td.b = td.out = ta;
         const long tiles = (long)mt * a.col_tiles;
@@ -684,6 +709,7 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
     }
     a.n = s.hid_n;
     a.col_tiles = (hid + a.n - 1) / a.n;
+    a.dw = static_cast<__nv_bfloat16*>(dw);
     a.add = piece > 0;
     a.want_dh = want_dh;
     a.row_tiles = dw ? (a.vn + TILE - 1) / TILE : 0;
