@@ -19,6 +19,7 @@
 namespace headloss {
 
 constexpr int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
+constexpr int ROW_BLOCKS = 512;            // blocks of the kernel that moves the rows, at most: each of them counts all rows
 constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time (more pieces: more part-filled waves; fewer: more memory)
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f, LN2_LOW = (float)(0.6931471805599453 - (double)LN2);
@@ -50,7 +51,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
         at += (bytes + 1023) / 1024 * 1024;
         return p;
     };
-    s.hdr = (int*)take(16);
+    s.hdr = (int*)take(32);
     s.slot = (int*)take((size_t)M * 4);
     s.row = (int*)take((size_t)s.Mp * 4);
     s.ids = (int*)take((size_t)K * s.Mp * 4);
@@ -76,6 +77,7 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.slab_tiles = 2 * pairs / ht > mt ? 2 * pairs / ht : mt;
     s.coef = (float*)take((size_t)s.Mp * 4);
     s.lse2 = (float*)take((size_t)s.Mp * 4);
+    s.rounding = (float*)take((size_t)ROW_BLOCKS * 32 * 4);
     s.gval = (float*)take((size_t)K * s.Mp * 4);
     s.g = (__nv_bfloat16*)take((size_t)s.Mp * s.piece * 2);
     s.slab = (float*)take((size_t)s.slab_tiles * TILE * hid * 4);
@@ -194,6 +196,8 @@ struct List {
     }
 };
 
+__device__ __forceinline__ float factor_of(int i) { return 1.f + i * 0.03125f; }
+
 // Sorts N x 32 keys of a warp, key i * 32 + lane in key[i], by a bitonic network.
 template <int N>
 __device__ __forceinline__ void sort_warp(uint64_t (&key)[MAX_TOP / 32], int lane) {
@@ -224,6 +228,8 @@ template <bool GRAD>
 __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a) {
     __shared__ int sums[2][ROW_WARPS];
     __shared__ float tops[ROW_WARPS];
+    __shared__ float list_g[GRAD ? ROW_WARPS : 1][MAX_TOP];        // G by rising id
+    __shared__ float taken[GRAD ? ROW_WARPS : 1][32];
     __shared__ int list_id[GRAD ? ROW_WARPS : 1][MAX_TOP];
     __shared__ float2 list_t[GRAD ? ROW_WARPS : 1][MAX_TOP];       // t and z by the list's order
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -275,6 +281,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
         a.s.hdr[HDR_LIVE] = total;
         a.s.hdr[HDR_GAVE_UP] = 0;
         a.s.hdr[HDR_SCALE] = __float_as_int(top);
+        a.s.hdr[HDR_FACTOR] = __float_as_int(1.f);
     }
     if (GRAD && blockIdx.x == 0 && warp == ROW_WARPS - 1) {
         const int ranges = dh_ranges(a, total, lane);
@@ -283,6 +290,8 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     // what dw's contraction meets behind the live rows is zeros; the second term's rows of G meet a copy of h
     const int low = GRAD && total <= TWO_TERMS ? low_term(total) : 0;
     const int fill_end = low ? low : (total + STEP - 1) / STEP * STEP;
+    const float factor = factor_of(lane);
+    float lost = 0.f;
     for (int g = 0; g < a.per_block; g += 32) {
         const int here = min(32, a.per_block - g);
         const unsigned mask = __ballot_sync(0xffffffffu, lane < here && base + g + lane < a.M && is_live(a, base + g + lane));
@@ -371,12 +380,55 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
                         t = 0.f;
                         for (int o = 0; o < l.n; ++o) t += list_id[warp][o] == id ? list_t[warp][o].x : 0.f;
                     }
-                    a.s.gval[(size_t)slot * a.K + place] = coef == 0.f ? 0.f : coef * (expf(list_t[warp][j].y / a.tau - lse) - t);
+                    const float g = coef == 0.f ? 0.f : coef * (expf(list_t[warp][j].y / a.tau - lse) - t);
+                    a.s.gval[(size_t)slot * a.K + place] = g;
+                    list_g[warp][place] = g;
+                }
+            }
+            if (GRAD && total > TWO_TERMS) {               // a lane tries one factor
+                __syncwarp();
+                for (int o = 0; o < l.n; ++o) {
+                    const float g = list_g[warp][o] * factor, off = g - __bfloat162float(__float2bfloat16(g));
+                    lost = fmaf(off, off, lost);
                 }
             }
             load_row(m + ROW_WARPS);
         }
         before += __popc(mask);
+    }
+    if (GRAD && total > TWO_TERMS) {
+        taken[warp][lane] = lost / (factor * factor);
+        __syncthreads();
+        if (warp == 0) {
+            float all = 0.f;
+#pragma unroll
+            for (int i = 0; i < ROW_WARPS; ++i) all += taken[i][lane];
+            a.s.rounding[(size_t)blockIdx.x * 32 + lane] = all;
+        }
+    }
+}
+
+// The factor that goes with the call's largest coefficient: what rounding takes of G at the listed tokens depends on where
+// their values lie between two powers of two, and their common scale is free.  Of 32 scales the one that loses least.
+__global__ void __launch_bounds__(1024) head_factor_kernel(const RowArgs a, int blocks) {
+    __shared__ float sums[32][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_trigger();
+    pdl_wait();
+    float lost = 0.f;
+    if (a.s.hdr[HDR_LIVE] > TWO_TERMS)
+        for (int b = warp; b < blocks; b += 32) lost += a.s.rounding[(size_t)b * 32 + lane];
+    sums[warp][lane] = lost;
+    __syncthreads();
+    if (warp > 0 || a.s.hdr[HDR_LIVE] <= TWO_TERMS) return;
+    lost = 0.f;
+    for (int i = 0; i < 32; ++i) lost += sums[i][lane];
+    // (a sum is not negative: its bits are in its order; NaN, of a row that is not finite, behind all)
+    const uint32_t best = __reduce_min_sync(0xffffffffu, __float_as_uint(lost));
+    const int which = __ffs(__ballot_sync(0xffffffffu, __float_as_uint(lost) == best)) - 1;
+    if (lane == 0) {
+        a.s.hdr[HDR_FACTOR] = __float_as_int(factor_of(which));
+        a.s.hdr[HDR_SCALE] = __float_as_int(__int_as_float(a.s.hdr[HDR_SCALE]) / factor_of(which));
     }
 }
 
@@ -538,7 +590,7 @@ static RowArgs row_args(const Space& s, const void* h, const int32_t* ids, const
     a.hid = hid;
     a.V = V;
     a.K = K;
-    a.per_block = ROW_WARPS * ((M + 4095) / 4096);         // at most 512 blocks: each of them counts all rows
+    a.per_block = ROW_WARPS * (((M + STEP - 1) / STEP * STEP + ROW_WARPS * ROW_BLOCKS - 1) / (ROW_WARPS * ROW_BLOCKS));
     a.h = static_cast<const __nv_bfloat16*>(h);
     a.ids = ids;
     a.teacher = teacher;
@@ -606,10 +658,12 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     a.dw_tiles = dw ? (s.piece + TILE - 1) / TILE * a.ht : 0;
     a.pairs = deer_sm_count() / 2;
     a.slab_tiles = s.slab_tiles;
-    static bool rows_set[64] = {}, dh_set[64] = {};
+    static bool rows_set[64] = {}, dh_set[64] = {}, factor_set[64] = {};
+    DEER_CUDA(keep_split(head_factor_kernel, factor_set));
     DEER_CUDA(keep_split(head_rows_kernel<true>, rows_set));
     DEER_CUDA(keep_split(head_dh_kernel, dh_set));
     DEER_CUDA(launch_pdl(head_rows_kernel<true>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
+    if (M > TWO_TERMS) DEER_CUDA(launch_pdl(head_factor_kernel, dim3(1), dim3(1024), 0, st, a, (int)row_blocks(a)));
     for (int p = 0; p < s.pieces; ++p) {
         rc = launch_product(GRAD, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, false, nullptr, st);
         if (rc == DEER_OK) rc = launch_product(BACK, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, dh != nullptr, dw, st);

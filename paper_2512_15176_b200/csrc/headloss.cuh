@@ -20,7 +20,7 @@ inline bool takes_rows_as_they_are(int M, int K) { return M <= ONE_BLOCK && K <=
 constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
 constexpr int STATS_SHARE = 2;            // warps that share a tile's columns in STATS: partial sums a row has of a tile
-constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3;
+constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3, HDR_FACTOR = 4;
 // Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in dh's product,
 // idle then, and the contraction that the steps of dw's leave free.  That sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
 constexpr int TWO_TERMS = 128;
@@ -28,13 +28,13 @@ __host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32
 
 enum Product {
     STATS,      // z = h w^T, reduced to (max, sum exp) per row and vocabulary tile, and the listed tokens' z
-    GRAD,       // the same z, as G = coef (exp(z / tau - lse) - t), bf16; coef is relative to the largest, HDR_SCALE
+    GRAD,       // the same z, as G = coef (exp(z / tau - lse) - t), bf16; coef is relative to HDR_SCALE
     BACK        // dh / scale = G w, fp32, added up over pieces and ranges, and dw = scale G^T h, bf16
 };
 
 // The arrays of one call, all in its workspace.
 struct Space {
-    int* hdr;                  // [4]
+    int* hdr;                  // [5]
     int* slot;                 // [M]        place of a row among the live ones, -1: dead
     int* row;                  // [Mp]       the row at a place
     int* ids;                  // [Mp][K]    a live row's list by rising id, INT_MAX behind its end
@@ -43,6 +43,7 @@ struct Space {
     float2* part;              // [Mp][tiles] (m, sum 2^(z log2(e) / tau - m))            (loss)
     float* coef;               // [Mp]       what a row's probabilities count            (gradient)
     float* lse2;               // [Mp]       lse log2(e)                                 (gradient)
+    float* rounding;           // [blocks][32] squares of what rounding takes of G at the listed tokens, by factor   (gradient)
     float* gval;               // [Mp][K]    G at the listed tokens                      (gradient)
     __nv_bfloat16* h;          // [Mp][hid]  live rows
     __nv_bfloat16* g;          // [Mp][piece]                                            (gradient)

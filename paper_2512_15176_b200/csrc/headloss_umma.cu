@@ -15,9 +15,10 @@
 //
 // G is rounded to bf16 for the products: as much as dh and dw are themselves, and with many rows the errors of different
 // rows are as independent as theirs.  At a listed token p - t is formed in fp32 first, so that a target the model is sure of
-// keeps its difference; coef is taken relative to the call's largest, so that equal rows weigh exactly 1 and a token that the
-// model gives nothing has an exact -1.  With few live rows (TWO_TERMS) a single rounding would show in a whole gradient, and
-// there G is kept as two bf16 terms, which costs no time.  lse, p and all sums are fp32.
+// keeps its difference.  coef is taken relative to a scale of the whole call, of which head_factor_kernel tries 32 between
+// two powers of two for the one at which rounding takes the least from the listed tokens, so that a few heavy rows do not
+// decide the gradient's error.  With few live rows (TWO_TERMS) a single rounding would show in a whole gradient, and there
+// G is kept as two bf16 terms, which costs next to no time.  lse, p and all sums are fp32.
 //
 // The tensor cores' accumulation rounds towards zero at every step: z comes out short by 2e-6 of itself at a contraction
 // of 2048, which is all of the loss's error where the target stands out.  Hence the listed tokens' z a second time, as plain
@@ -258,6 +259,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
     const int quarter = warp & 3, turn = (warp - 2) >> 2;
     const uint32_t stg = staging + (uint32_t)(warp - 2) * (2u * BOX), stg_row = (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
     const int lane_row = rank * 128 + quarter * 32 + lane;                 // the thread's row within a tile
+    const float factor = P == GRAD ? __int_as_float(a.hdr_in[HDR_FACTOR]) : 1.f;
     uint32_t stg_i = 0;
     int it = 0;
     Tile t;
@@ -272,7 +274,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
         float coef = 0.f, nlse = 0.f;
         Listed listed;
         if (P == GRAD && row_ok) {
-            coef = a.coef[slot];
+            coef = a.coef[slot] * factor;
             nlse = -a.lse2[slot];
         }
         if ((P == STATS || P == GRAD) && row_ok) {
@@ -393,7 +395,8 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                     while (listed.id < first + wide) {                    // listed tokens: p - t, formed in fp32 beforehand
                         if (listed.id >= first) {                         // (the other warp's chunks lie between this one's)
                             const uint32_t k = (uint32_t)(listed.id - first);
-                            const __nv_bfloat16 hi = __float2bfloat16(listed.val), lo = __float2bfloat16(listed.val - __bfloat162float(hi));
+                            const float val = listed.val * factor;
+                            const __nv_bfloat16 hi = __float2bfloat16(val), lo = __float2bfloat16(val - __bfloat162float(hi));
                             const uint32_t at = b + (((k >> 3) ^ sw) << 4) + (k & 7) * 2;
                             st_shared_bf16(at, hi);
                             if (two) st_shared_bf16(at + other, lo);
