@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(1024) head_factor_kernel(const RowArgs a, int 
 }
 
 // lse and loss of every row from its tiles' partial sums: a warp per row, or (few rows, which may have thousands) a block.
-__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int as_is, int wide, int tiles, float c2, float c2_low, float* loss, float* lse_out, float* target_logit) {
+__global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a, int as_is, int wide, int tiles, float2 plain, float2 tile, float* loss, float* lse_out, float* target_logit) {
     __shared__ float2 warps[ROW_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = wide ? blockIdx.x : blockIdx.x * ROW_WARPS + warp;
     pdl_trigger();
@@ -485,10 +485,10 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
         if (as_is)
             for (int o = 0; o < j; ++o) at = a.ids[(size_t)m * a.K + o] == l.id[i] ? -1 : at;
         else at = a.s.place[(size_t)slot * a.K + j];
-        l.z[i] = fmaf(l.z[i], c2_low, fmaf(l.z[i], c2, -all));
+        l.z[i] = fmaf(l.z[i], plain.y, fmaf(l.z[i], plain.x, -all));
         if (at < 0) continue;
         const float tile_z = a.s.z[(size_t)slot * a.K + at];
-        more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, c2_low, fmaf(tile_z, c2, -all)));
+        more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, tile.y, fmaf(tile_z, tile.x, -all)));
     }
     const float log_sum = logf(sum + warp_sum(more));
     float each = 0.f;
@@ -616,8 +616,9 @@ static int loss_call(const char* call, const void* h, const void* w, const int32
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
-    float c2, c2_low;
-    scale_of(tau, c2, c2_low);
+    float2 plain, tile;
+    scale_of(tau, plain.x, plain.y);
+    tile_scale_of(tau, hid, tile.x, tile.y);
     static bool rows_set[64] = {}, loss_set[64] = {};
     DEER_CUDA(keep_split(head_rows_kernel<false>, rows_set));
     DEER_CUDA(keep_split(head_loss_kernel, loss_set));
@@ -626,7 +627,7 @@ static int loss_call(const char* call, const void* h, const void* w, const int32
     rc = launch_product(STATS, s, h, w, ids, row_weight, M, hid, V, K, 0, tau, target_logit, false, nullptr, st);
     if (rc != DEER_OK) return rc;
     const bool wide = M <= 512;
-    DEER_CUDA(launch_pdl(head_loss_kernel, dim3(wide ? M : (M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (int)as_is, (int)wide, (V + s.stats_n - 1) / s.stats_n * STATS_SHARE, c2, c2_low,
+    DEER_CUDA(launch_pdl(head_loss_kernel, dim3(wide ? M : (M + ROW_WARPS - 1) / ROW_WARPS), dim3(ROW_THREADS), 0, st, a, (int)as_is, (int)wide, (V + s.stats_n - 1) / s.stats_n * STATS_SHARE, plain, tile,
                          loss, lse, target_logit));
     return DEER_OK;
 }

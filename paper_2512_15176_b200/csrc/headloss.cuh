@@ -69,7 +69,7 @@ struct ProductArgs {
     int a_rows;                // rows of the 128-row operand one block loads (fewer than 128 only where M is)
     int K, tiles;
     int add;                   // BACK: a piece behind the first
-    float c2, c2_low;          // log2(e) / tau, and what fp32 leaves of it
+    float c2, c2_low;          // tile_scale_of tau
     const int* ids;
     const int* row;
     const __nv_bfloat16* h;
@@ -91,12 +91,16 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
                    int piece, float tau, float* target_logit, bool want_dh, void* dw, cudaStream_t st);
 
 // log2(e) / tau as two fp32 terms, both above 0 (a z of -inf stays one).
-inline void scale_of(float tau, float& c2, float& c2_low) {
+inline void scale_of(double tau, float& c2, float& c2_low) {
     const double c = 1.4426950408889634 / tau;
     c2 = (float)c;
     if (c2 >= c) c2 = nextafterf(c2, 0.f);
     c2_low = (float)(c - c2);
 }
+// The same for a z that comes from the tensor cores, whose accumulation rounds towards zero: measured against 64 bits, each of
+// its steps of 16 leaves z short by 1.2e-8 (hid 64) to 1.6e-8 (hid 8192) of itself, so that at hid 2048 z of a row's whole
+// vocabulary is 1.8e-6 of itself too near to zero.  The mean of that is given back.
+inline void tile_scale_of(double tau, int hid, float& c2, float& c2_low) { scale_of(tau / (1.0 + 1.5e-8 * (hid / 16)), c2, c2_low); }
 
 __device__ __forceinline__ bool is_live(const int* list, const float* weight, int K, int m) {
     const int id = list[(size_t)m * K];

@@ -20,10 +20,9 @@
 // decide the gradient's error.  With few live rows (TWO_TERMS) a single rounding would show in a whole gradient, and there
 // G is kept as two bf16 terms, which costs next to no time.  lse, p and all sums are fp32.
 //
-// The tensor cores' accumulation rounds towards zero at every step: z comes out short by 2e-6 of itself at a contraction
-// of 2048, which is all of the loss's error where the target stands out.  Hence the listed tokens' z a second time, as plain
-// fp32 sums (4 % of the products' bytes at lists of 64, and hidden behind them): the loss takes those, and lse is corrected
-// by the difference.
+// The tensor cores' accumulation rounds towards zero at every step (tile_scale_of).  Where a target stands out the loss is the
+// difference of two large numbers, lse and the target's z: hence the listed tokens' z a second time, as plain fp32 sums (4 %
+// of the products' bytes at lists of 64, hidden behind them).  The loss takes those, and lse the difference that they make.
 #include <math.h>
 
 #include <type_traits>
@@ -669,7 +668,7 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
     a.hid = hid;
     a.V = V;
     a.K = K;
-    scale_of(tau, a.c2, a.c2_low);
+    tile_scale_of(tau, hid, a.c2, a.c2_low);
     a.ids = s.ids;
     a.row = s.row;
     a.as_is = what == STATS && takes_rows_as_they_are(M, K);
