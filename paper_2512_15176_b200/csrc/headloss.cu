@@ -58,6 +58,10 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.h = (__nv_bfloat16*)take((size_t)s.Mp * hid * 2);
     if (!grad) {
         s.stats_n = tile_columns(mt, V, 16, groups);
+        s.piece = V;
+        s.piece_tiles = (V + s.stats_n - 1) / s.stats_n;
+        s.first_pitch = (s.piece_tiles + 3) / 4 * 4;
+        s.first = (uint8_t*)take(takes_rows_as_they_are(M, K) ? 0 : (size_t)s.Mp * s.first_pitch);
         s.place = (int*)take((size_t)K * s.Mp * 4);
         s.z = (float*)take((size_t)K * s.Mp * 4);
         s.part = (float2*)take((size_t)s.Mp * ((V + s.stats_n - 1) / s.stats_n) * STATS_SHARE * 8);
@@ -77,6 +81,9 @@ Space lay_out(void* base, int M, int hid, int V, int K, bool grad) {
     s.slab_tiles = 2 * pairs / ht > mt ? 2 * pairs / ht : mt;
     s.coef = (float*)take((size_t)s.Mp * 4);
     s.lse2 = (float*)take((size_t)s.Mp * 4);
+    s.piece_tiles = (s.piece + s.grad_n - 1) / s.grad_n;
+    s.first_pitch = (s.pieces * s.piece_tiles + 3) / 4 * 4;
+    s.first = (uint8_t*)take((size_t)s.Mp * s.first_pitch);
     s.rounding = (float*)take((size_t)ROW_BLOCKS * 32 * 4);
     s.gval = (float*)take((size_t)K * s.Mp * 4);
     s.g = (__nv_bfloat16*)take((size_t)s.Mp * s.piece * 2);
@@ -95,6 +102,7 @@ struct RowArgs {
     const float* lse;            // [M]                             (loss: out; gradient: in)
     const float* target_logit;   // [M][K]
     float tau;
+    int tile_n;                  // columns of a tile of STATS or GRAD
     int ht, steps, dw_tiles, pairs, slab_tiles;
     Space s;
 };
@@ -122,7 +130,7 @@ __device__ __forceinline__ int warp_sum(int v) { return __reduce_add_sync(0xffff
 __device__ int dh_ranges(const RowArgs& a, int live, int lane) {
     const int mt = (live + TILE - 1) / TILE, tiles = mt * a.ht;
     if (mt == 0) return 1;
-    const int dw_steps = ((live <= TWO_TERMS ? 2 * low_term(live) : live) + STEP - 1) / STEP;
+    const int dw_steps = dw_contraction(live);
     const int most = max(1, min(a.slab_tiles / mt, a.steps / 4)), least = max(1, min(a.pairs / tiles, most));
     const uint64_t dw_cost = (uint64_t)a.dw_tiles * dw_tile_cost(dw_steps);
     uint64_t best = ~uint64_t(0);              // cost, then the count
@@ -230,7 +238,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     __shared__ float tops[ROW_WARPS];
     __shared__ float list_g[GRAD ? ROW_WARPS : 1][MAX_TOP];        // G by rising id
     __shared__ float taken[GRAD ? ROW_WARPS : 1][32];
-    __shared__ int list_id[GRAD ? ROW_WARPS : 1][MAX_TOP];
+    __shared__ int list_id[GRAD ? ROW_WARPS : 1][MAX_TOP], sorted_id[ROW_WARPS][MAX_TOP];
     __shared__ float2 list_t[GRAD ? ROW_WARPS : 1][MAX_TOP];       // t and z by the list's order
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_trigger();
@@ -252,6 +260,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     load_row(base + warp);
     int before = 0, total = 0;
     float top = 0.f;                           // the largest finite coefficient: what G is relative to
+#pragma unroll 4
     for (int m = tid; m < a.M; m += ROW_THREADS) {
         const int f = is_live(a, m);
         total += f;
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
                 const int behind = i > 0 ? (int)(__shfl_sync(0xffffffffu, key[i > 0 ? i - 1 : 0], 31) >> 32) : -1;
                 if (lane == 0) left = behind;
                 if (place >= a.K) continue;
-                a.s.ids[(size_t)slot * a.K + place] = place < l.n ? id : INT_MAX;
+                a.s.ids[(size_t)slot * a.K + place] = sorted_id[warp][place] = place < l.n ? id : INT_MAX;
                 if (!GRAD) a.s.place[(size_t)slot * a.K + j] = left == id ? -1 : place;
                 if (GRAD && place < l.n) {
                     float t = list_t[warp][j].x;           // the token's probability, wherever the list names it
@@ -385,8 +394,34 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
                     list_g[warp][place] = g;
                 }
             }
-            if (GRAD && total > TWO_TERMS) {               // a lane tries one factor
-                __syncwarp();
+            __syncwarp();
+            // where the list stands at each of the products' tiles: a lane walks a run of them, four to a store
+            const int run = (a.s.first_pitch / 4 + 31) / 32 * 4, tile0 = lane * run, tile1 = min(tile0 + run, a.s.first_pitch);
+            if (tile0 < tile1) {
+                int piece = tile0 / a.s.piece_tiles, in_piece = tile0 - piece * a.s.piece_tiles;
+                int from = piece * a.s.piece + in_piece * a.tile_n, e = 0, hi = l.n;
+                while (e < hi) {
+                    const int mid = (e + hi) >> 1;
+                    if (sorted_id[warp][mid] < from) e = mid + 1;
+                    else hi = mid;
+                }
+                int next = e < l.n ? sorted_id[warp][e] : INT_MAX;
+                for (int tile = tile0; tile < tile1; tile += 4) {
+                    uint32_t four = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        while (next < from) next = ++e < l.n ? sorted_id[warp][e] : INT_MAX;
+                        four |= (uint32_t)e << (8 * i);
+                        from += a.tile_n;
+                        if (++in_piece == a.s.piece_tiles) {
+                            in_piece = 0;
+                            from = ++piece * a.s.piece;
+                        }
+                    }
+                    *reinterpret_cast<uint32_t*>(a.s.first + (size_t)slot * a.s.first_pitch + tile) = four;
+                }
+            }
+            if (GRAD && total > DW_TERMS) {                // a lane tries one factor
                 for (int o = 0; o < l.n; ++o) {
                     const float g = list_g[warp][o] * factor, off = g - __bfloat162float(__float2bfloat16(g));
                     lost = fmaf(off, off, lost);
@@ -396,7 +431,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
         }
         before += __popc(mask);
     }
-    if (GRAD && total > TWO_TERMS) {
+    if (GRAD && total > DW_TERMS) {
         taken[warp][lane] = lost / (factor * factor);
         __syncthreads();
         if (warp == 0) {
@@ -416,11 +451,11 @@ __global__ void __launch_bounds__(1024) head_factor_kernel(const RowArgs a, int 
     pdl_trigger();
     pdl_wait();
     float lost = 0.f;
-    if (a.s.hdr[HDR_LIVE] > TWO_TERMS)
+    if (a.s.hdr[HDR_LIVE] > DW_TERMS)
         for (int b = warp; b < blocks; b += 32) lost += a.s.rounding[(size_t)b * 32 + lane];
     sums[warp][lane] = lost;
     __syncthreads();
-    if (warp > 0 || a.s.hdr[HDR_LIVE] <= TWO_TERMS) return;
+    if (warp > 0 || a.s.hdr[HDR_LIVE] <= DW_TERMS) return;
     lost = 0.f;
     for (int i = 0; i < 32; ++i) lost += sums[i][lane];
     // (a sum is not negative: its bits are in its order; NaN, of a row that is not finite, behind all)
@@ -452,11 +487,15 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
     // in powers of two, relative to the largest of the tiles' references
     const float2* part = a.s.part + (size_t)slot * tiles;
     float top = -INFINITY, sum = 0.f;                      // (a lane's, and its sum relative to that)
-#pragma unroll 4
-    for (int i = wide ? threadIdx.x : lane; i < tiles; i += wide ? ROW_THREADS : 32) {
-        const float2 p = part[i];
-        const float m2 = fmaxf(top, p.x), shift = m2 == -INFINITY ? 0.f : m2;
-        sum = sum * exp2f(top - shift) + p.y * exp2f(p.x - shift);
+    const int step = wide ? ROW_THREADS : 32;
+    for (int i0 = wide ? threadIdx.x : lane; i0 < tiles; i0 += 4 * step) {
+        float2 p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = i0 + i * step < tiles ? part[i0 + i * step] : make_float2(-INFINITY, 0.f);
+        const float m2 = fmaxf(fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), top), shift = m2 == -INFINITY ? 0.f : m2;
+        sum *= exp2f(top - shift);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fmaf(p[i].y, exp2f(p[i].x - shift), sum);
         top = m2;
     }
     float all = warp_max(top);
@@ -615,7 +654,8 @@ static int loss_call(const char* call, const void* h, const void* w, const int32
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
+    RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
+    a.tile_n = s.stats_n;
     float2 plain, tile;
     scale_of(tau, plain.x, plain.y);
     tile_scale_of(tau, hid, tile.x, tile.y);
@@ -651,6 +691,7 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
     RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
+    a.tile_n = s.grad_n;
     a.grad = grad_loss;
     a.lse = lse;
     a.target_logit = target_logit;
@@ -664,7 +705,7 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     DEER_CUDA(keep_split(head_rows_kernel<true>, rows_set));
     DEER_CUDA(keep_split(head_dh_kernel, dh_set));
     DEER_CUDA(launch_pdl(head_rows_kernel<true>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
-    if (M > TWO_TERMS) DEER_CUDA(launch_pdl(head_factor_kernel, dim3(1), dim3(1024), 0, st, a, (int)row_blocks(a)));
+    if (M > DW_TERMS) DEER_CUDA(launch_pdl(head_factor_kernel, dim3(1), dim3(1024), 0, st, a, (int)row_blocks(a)));
     for (int p = 0; p < s.pieces; ++p) {
         rc = launch_product(GRAD, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, false, nullptr, st);
         if (rc == DEER_OK) rc = launch_product(BACK, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, dh != nullptr, dw, st);

@@ -10,6 +10,7 @@
 
 namespace headloss {
 
+constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int TILE = 256;                  // rows of a product's tile: 128 in each block of a pair
 constexpr int ONE_BLOCK = 128;             // up to this many rows STATS and GRAD work by single blocks: a pair would leave half of its
                                            // lanes empty and the products, not the reading of w, would bound the call
@@ -17,14 +18,21 @@ constexpr int SHORT = 8;                   // lists of up to so many entries are
                                            // STATS take the call's rows themselves (a dead one costs nothing in a tile that is
                                            // not full), which saves a launch
 inline bool takes_rows_as_they_are(int M, int K) { return M <= ONE_BLOCK && K <= SHORT; }
-constexpr int STEP = 64;                   // contraction of one pipeline stage
 constexpr int MAX_TOP = 128;               // entries of a row's list
 constexpr int STATS_SHARE = 2;            // warps that share a tile's columns in STATS: partial sums a row has of a tile
 constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3, HDR_FACTOR = 4;
-// Up to this many live rows G is kept as two bf16 terms: the second takes the places of the second block's rows in dh's product,
-// idle then, and the contraction that the steps of dw's leave free.  That sees rows [0, gap) and [gap, 2 gap), gap = low_term(live).
-constexpr int TWO_TERMS = 128;
+// Up to this many live rows G is kept as two bf16 terms, rows [0, low) and [low, 2 low) with low = low_term(live).  In dh's
+// product the second takes the places of the second block's rows, idle then.  In dw's it lengthens the contraction: that
+// covers its first 128 places, all of both terms up to 64 live rows, and beyond them (where rows' errors begin to be
+// independent) what is left of its second step (live 128, hid 2688: 435 -> 330 us for both products).
+constexpr int TWO_TERMS = 128, DW_TERMS = 64;
 __host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32; }
+// Steps of dw's contraction.
+__host__ __device__ inline int dw_contraction(int live) {
+    if (live > TWO_TERMS) return (live + STEP - 1) / STEP;
+    const int rows = 2 * low_term(live) < 2 * DW_TERMS ? 2 * low_term(live) : 2 * DW_TERMS;
+    return (rows + STEP - 1) / STEP;
+}
 
 enum Product {
     STATS,      // z = h w^T, reduced to (max, sum exp) per row and vocabulary tile, and the listed tokens' z
@@ -38,6 +46,7 @@ struct Space {
     int* slot;                 // [M]        place of a row among the live ones, -1: dead
     int* row;                  // [Mp]       the row at a place
     int* ids;                  // [Mp][K]    a live row's list by rising id, INT_MAX behind its end
+    uint8_t* first;            // [Mp][tiles] entries of a row's list in front of a tile of STATS or GRAD
     int* place;                // [Mp][K]    an entry's place among the rising ids, -1: a token listed before    (loss)
     float* z;                  // [Mp][K]    by rising id (as they are: by the list): the token's z as the tiles have it  (loss)
     float2* part;              // [Mp][tiles] (m, sum 2^(z log2(e) / tau - m))            (loss)
@@ -49,6 +58,7 @@ struct Space {
     __nv_bfloat16* g;          // [Mp][piece]                                            (gradient)
     float* slab;               // [slab_tiles * 256][hid]  partial dh                    (gradient)
     size_t bytes;
+    int first_pitch, piece_tiles;      // tiles of a row, of a piece
     int Mp, pieces, piece, stats_n, grad_n, hid_n, slab_tiles;
 };
 
@@ -80,6 +90,8 @@ struct ProductArgs {
     const float* coef;
     const float* lse2;
     const float* gval;
+    const uint8_t* first;
+    int first_pitch, first_tile;
     __nv_bfloat16* g;
     __nv_bfloat16* dw;
     int g_pitch;

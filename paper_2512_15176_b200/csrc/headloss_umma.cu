@@ -105,7 +105,7 @@ struct List {
         }
         steps = (a.vn + STEP - 1) / STEP;
         ranges = a.hdr_in[HDR_RANGES];
-        dw_steps = ((low ? 2 * low : live) + STEP - 1) / STEP;
+        dw_steps = dw_contraction(live);
         n = a.want_dh ? mt * ct * ranges : 0;
         n_dw = a.row_tiles * ct;
         // dh's tiles first, in turn; groups that have one of them less take `ahead` of dw's before the others begin
@@ -204,16 +204,10 @@ struct Listed {
     int id = 0x7fffffff, e = 0, next = 0x7fffffff;
     float val = 0.f, next_val = 0.f;           // GRAD: G at the token
     __device__ __forceinline__ int id_at(const ProductArgs& a, int slot, int i) const { return i < a.K ? a.ids[(size_t)slot * a.K + i] : 0x7fffffff; }
-    // lists by rising id
+    // lists by rising id, from entry `at` on
     template <bool VALUES>
-    __device__ __forceinline__ void start(const ProductArgs& a, int slot, int from) {
-        int hi = a.K;
-        e = 0;
-        while (e < hi) {
-            const int mid = (e + hi) >> 1;
-            if (a.ids[(size_t)slot * a.K + mid] < from) e = mid + 1;
-            else hi = mid;
-        }
+    __device__ __forceinline__ void start(const ProductArgs& a, int slot, int at) {
+        e = at;
         id = id_at(a, slot, e);
         next = id_at(a, slot, e + 1);
         if (VALUES) {
@@ -261,24 +255,41 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
     const float factor = P == GRAD ? __int_as_float(a.hdr_in[HDR_FACTOR]) : 1.f;
     uint32_t stg_i = 0;
     int it = 0;
-    Tile t;
-    for (int k = 0; list.tile(k, t); ++k) {
+    // what a tile needs of its rows comes one tile ahead: where a row's list stands at the tile's first column, G's scale
+    constexpr bool BY_ROWS = P == STATS || P == GRAD;
+    struct Row {
+        float coef = 0.f, nlse = 0.f;
+        int e = 0;
+    } row, row_ahead;
+    auto place_of = [&](const Tile& t) { return t.r * Shape<P, CG>::ROWS + lane_row; };
+    auto load_row = [&](const Tile& t, Row& r) {
+        const int slot = place_of(t);
+        if (slot >= list.live) return;
+        if (P == GRAD) {
+            r.coef = a.coef[slot];
+            r.nlse = -a.lse2[slot];
+        }
+        if (P == GRAD || !a.as_is) r.e = a.first[(size_t)slot * a.first_pitch + a.first_tile + t.c];
+    };
+    Tile t, t_ahead;
+    bool more = list.tile(0, t), more_ahead;
+    if (BY_ROWS && more) load_row(t, row);
+    for (int k = 0; more; ++k, t = t_ahead, more = more_ahead, row = row_ahead) {
+        more_ahead = list.tile(k + 1, t_ahead);
         if (t.kb == 0 && !t.dw) continue;                                 // dh: nothing to add; dw without a live row: zeros
         const int buf = it & 1;
         const bool computed = t.kb > 0;
-        const int slot = t.r * Shape<P, CG>::ROWS + lane_row;             // STATS, GRAD: place among the live rows
-        const bool row_ok = slot < list.live && (P != STATS || !a.as_is || is_live(a.list, a.weight, a.K, slot));
+        const int slot = place_of(t);                                     // STATS, GRAD: place among the live rows
+        const bool row_ok = BY_ROWS && slot < list.live && (P != STATS || !a.as_is || is_live(a.list, a.weight, a.K, slot));
         const int col0 = t.c * a.n;
-        // what the tile needs of its rows comes while it is computed: a row's first listed token at or behind its start
-        float coef = 0.f, nlse = 0.f;
+        const float coef = row.coef * factor, nlse = row.nlse;
         Listed listed;
-        if (P == GRAD && row_ok) {
-            coef = a.coef[slot] * factor;
-            nlse = -a.lse2[slot];
-        }
-        if ((P == STATS || P == GRAD) && row_ok) {
-            if (P == STATS && a.as_is) listed.search(a, slot, col0, false, 0.f);
-            else listed.start<P == GRAD>(a, slot, a.v0 + col0);
+        if (BY_ROWS) {
+            if (row_ok) {
+                if (P == STATS && a.as_is) listed.search(a, slot, col0, false, 0.f);
+                else listed.start<P == GRAD>(a, slot, row.e);
+            }
+            if (more_ahead) load_row(t_ahead, row_ahead);
         }
         if (computed) {
             const bool got = mbar_wait(tfull0 + 8u * buf, (uint32_t)(it >> 1) & 1u, abort_flag);
@@ -297,30 +308,27 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
                 TMEM_LD_X32(taddr + c, v);
                 tmem_wait_ld();
                 const int have = width - c;
-                float m = -INFINITY;
-                if (have >= 32) {
+                if (have < 32) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) m = fmaxf(m, __uint_as_float(v[j]));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
+                    for (int j = 0; j < 32; ++j)
                         if (j >= have) v[j] = 0xff800000u;
-                        m = fmaxf(m, __uint_as_float(v[j]));
-                    }
                 }
+                float m4[4] = {__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])};
+#pragma unroll
+                for (int j = 4; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(v[j]));
+                float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                 // relative to a whole row's reference in powers of two: rounded where it is small, not where z is
                 m = fmaxf(m * a.c2, run_m);
                 const float shift = m == -INFINITY ? 0.f : m;              // a row of -inf so far: its exponentials are 0
                 run_s *= ex2(run_m - shift);
                 run_m = m;
-                float s0 = 0.f, s1 = 0.f;
+                float s4[4] = {};
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    const float x = __uint_as_float(v[j]), y = __uint_as_float(v[j + 1]);
-                    s0 += ex2(fmaf(x, a.c2_low, fmaf(x, a.c2, -shift)));
-                    s1 += ex2(fmaf(y, a.c2_low, fmaf(y, a.c2, -shift)));
+                for (int j = 0; j < 32; ++j) {
+                    const float x = __uint_as_float(v[j]);
+                    s4[j & 3] += ex2(fmaf(x, a.c2_low, fmaf(x, a.c2, -shift)));
                 }
-                run_s += s0 + s1;
+                run_s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                 // the z of the row's listed tokens among these columns, by way of shared memory: registers have no index
                 const int begin = col0 + c, end = col0 + min(c + 32, width);
                 if (listed.id < end) {
@@ -680,6 +688,9 @@ int launch_product(Product what, const Space& s, const void* h, const void* w, c
     a.coef = s.coef;
     a.lse2 = s.lse2;
     a.gval = s.gval;
+    a.first = s.first;
+    a.first_pitch = s.first_pitch;
+    a.first_tile = what == GRAD ? piece * s.piece_tiles : 0;
     a.g = s.g;
     a.g_pitch = s.piece;
     a.v0 = what == STATS ? 0 : piece * s.piece;

@@ -5,7 +5,8 @@ Tolerances (u = 2^-24, half a step of fp32; b = 2^-8, half a step of bf16):
   more inside one: dz = (hid / 16 + 8) 2u sum |h w|.
 * lse: dz / tau, and 2^-20 for the exponentials, their sum and the logarithm, and 8u of its size.
 * loss: tau^2 a times (2 dz / tau + 2^-20 + 16u (|lse| + max |z| / tau + max |log t|)), in the list's mean.
-* G: rounded once to bf16, b |G| (b^2 |G| with up to 128 live rows: two terms); p off by the factor d = 2 dz / tau + 2^-19; 8u of t.
+* G: rounded once to bf16, b |G| (b^2 |G| where it is held as two terms: up to 128
+  live rows for dh, 64 for dw); p off by the factor d = 2 dz / tau + 2^-19; 8u of t.
 * dh, dw: G's errors against |w| (|h|), the accumulator's (n / 16 + 8) 2u of sum |G w| over n terms, and one rounding b."""
 import math
 
@@ -88,10 +89,11 @@ def check(got, h, w, ids, teacher=None, tau=1.0, weight=None, grad=None):
         assert (np.abs(zt[:n] - z[m, ids[m, :n]]) <= dz[m]).all()
     want_dh, want_dw, G = O.head_loss_grad(h, w, ids, teacher, tau, weight, grad)
     c = np.abs((1 if weight is None else weight) * (1 if grad is None else grad) * tau * live)[:, None] * np.ones((M, 1))
-    dG = (B if live.sum() > 128 else B * B) * np.abs(G) + c * (p * (2 * dz / tau + 2.0 ** -19)[:, None] + 8 * U * t)
+    dp = c * (p * (2 * dz / tau + 2.0 ** -19)[:, None] + 8 * U * t)
     for x, want_x, other, n in ((dh, want_dh, aw, V), (dw, want_dw, np.abs(np.where(live[:, None], h, 0)), M)):
         if x is None:
             continue
+        dG = (B if live.sum() > (128 if x is dh else 64) else B * B) * np.abs(G) + dp
         d, s = (dG @ other, np.abs(G) @ other) if x is dh else (dG.T @ other, np.abs(G).T @ other)
         tol = B * np.abs(want_x) + (1 + B) * (d + (n / 16 + 8) * 2 * U * s) + 2.0 ** -133
         err = np.abs(f64(x) - want_x)
