@@ -1,7 +1,7 @@
 // The K largest logits of each row, ids and values, falling, the lowest index first among equals.
 //
 // A row is read once.  A sample of it (16384 values in 128-byte runs spread over the row, which L2 gives again to the pass
-// behind) yields a cut: each of the 512 threads keeps its share's maximum, and the K-th largest of those maxima has K values
+// behind) yields a cut: each of the 512 (short rows: 256) threads keeps its share's maximum, and the K-th largest of those maxima has K values
 // of the row at or above it, whatever the row looks like.  The pass keeps what is not below the cut -- some 10 K of 151936
 // values -- in shared memory, one compare for four values.  The K best of those are found by a histogram of their keys, 256
 // bins over the range that they span, narrowed to the bin that holds the K-th until it is decided, and put in order by
@@ -17,11 +17,15 @@
 
 namespace toplogits {
 
-constexpr int THREADS = 512, WARPS = THREADS / 32;
-constexpr int LIST = 4096;                 // candidates a block holds
-constexpr int MAX_TOP = 128, FAN = THREADS / MAX_TOP;
+constexpr int MAX_TOP = 128;
 constexpr int MAX_CLUSTER = 8;
 constexpr int RUN = 32, SAMPLE_RUNS = 512; // values of a sampled run, runs of a sample
+
+// T: threads of a block.
+template <int T>
+constexpr int LIST = 8 * T;                // candidates that a block holds
+template <int T>
+constexpr int SENT = LIST<T> / MAX_CLUSTER;    // of them, those that a block of a cluster sends as they are
 
 __device__ __forceinline__ uint32_t key_of(float v) {
     uint32_t b = __float_as_uint(v);
@@ -31,21 +35,21 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
-constexpr int SENT = LIST / MAX_CLUSTER;   // candidates that a block of a cluster sends as they are
-
+template <int T>
 struct Shared {
-    uint32_t key[LIST], idx[LIST];
+    uint32_t key[LIST<T>], idx[LIST<T>];
     uint32_t best_key[MAX_TOP], best_idx[MAX_TOP];
     int hist[256];
-    int part[2][WARPS];
+    int part[2][T / 32];
     int count, found, bin, above;
     uint32_t low, high;
-    int sent[MAX_CLUSTER];                 // behind it, with clusters: what the blocks sent, [MAX_CLUSTER][SENT] keys, then indices
+    int sent[MAX_CLUSTER];                 // behind it, with clusters: what the blocks sent, [MAX_CLUSTER][SENT<T>] keys, then indices
 };
 
 // The bin that holds the need-th largest of the values counted in s.hist, and how many lie in bins above it: s.bin, s.above.
 // A warp's work; 1 <= need <= their number.
-__device__ __forceinline__ void find_bin(Shared& s, int need) {
+template <int T>
+__device__ __forceinline__ void find_bin(Shared<T>& s, int need) {
     const int lane = threadIdx.x & 31;
     int n[8], sum = 0;
 #pragma unroll
@@ -68,8 +72,9 @@ __device__ __forceinline__ void find_bin(Shared& s, int need) {
         }
     }
 }
-__device__ __forceinline__ void clear_bins(Shared& s) {
-    for (int i = threadIdx.x; i < 256; i += THREADS) s.hist[i] = 0;
+template <int T>
+__device__ __forceinline__ void clear_bins(Shared<T>& s) {
+    for (int i = threadIdx.x; i < 256; i += T) s.hist[i] = 0;
 }
 // Bits of the differences from `low` behind the eight that number the bins of [low, high].
 __device__ __forceinline__ int bin_shift(uint32_t low, uint32_t high) { return max(0, 24 - __clz(high - low)); }
@@ -81,14 +86,14 @@ struct Cut {
 };
 // Narrows [low, high] to the bin that holds the need-th largest of the values value(j, v), j < n (false: no value), until it
 // is decided or the bins are 2^stop wide.
-template <typename F>
-__device__ __forceinline__ Cut narrow(Shared& s, int n, F value, uint32_t low, uint32_t high, int need, int stop) {
+template <int T, typename F>
+__device__ __forceinline__ Cut narrow(Shared<T>& s, int n, F value, uint32_t low, uint32_t high, int need, int stop) {
     int shift = bin_shift(low, high);
     uint32_t span = high - low;
     for (;;) {
         clear_bins(s);
         __syncthreads();
-        for (int j = threadIdx.x; j < n; j += THREADS) {
+        for (int j = threadIdx.x; j < n; j += T) {
             uint32_t v;
             if (value(j, v) && v >= low && v - low <= span) atomicAdd(&s.hist[(v - low) >> shift], 1);
         }
@@ -105,9 +110,10 @@ __device__ __forceinline__ Cut narrow(Shared& s, int n, F value, uint32_t low, u
     }
 }
 
-// The k best of the n <= LIST entries of keys / idxs, whose keys lie in [low, high]: to best_key / best_idx in any order.
+// The k best of the n <= LIST<T> entries of keys / idxs, whose keys lie in [low, high]: to best_key / best_idx in any order.
 // Returns how many (min(n, k)).
-__device__ int select(Shared& s, const uint32_t* keys, const uint32_t* idxs, int n, int k, uint32_t low, uint32_t high) {
+template <int T>
+__device__ int select(Shared<T>& s, const uint32_t* keys, const uint32_t* idxs, int n, int k, uint32_t low, uint32_t high) {
     const int tid = threadIdx.x;
     if (tid == 0) s.found = 0;
     Cut cut = {0, 0, true};                // taken: all
@@ -118,7 +124,7 @@ __device__ int select(Shared& s, const uint32_t* keys, const uint32_t* idxs, int
             least = narrow(s, n, [&](int j, uint32_t& v) { v = ~idxs[j]; return keys[j] == cut.low; }, 0u, ~0u, cut.need, 0).low;
     }
     __syncthreads();
-    for (int j = tid; j < n; j += THREADS)
+    for (int j = tid; j < n; j += T)
         if (keys[j] > cut.low || (keys[j] == cut.low && ~idxs[j] >= least)) {
             const int at = atomicAdd(&s.found, 1);
             s.best_key[at] = keys[j];
@@ -130,7 +136,7 @@ __device__ int select(Shared& s, const uint32_t* keys, const uint32_t* idxs, int
 
 // Calls f4(four values, the first one's index) for the values [lo, hi) of the row, 16 bytes at a time where the alignment
 // allows it, and f(value, index) for the rest.
-template <typename F4, typename F>
+template <int T, typename F4, typename F>
 __device__ __forceinline__ void for_values(const float* row, int lo, int hi, F4 f4, F f) {
     const int tid = threadIdx.x;
     const int skew = (int)((4 - ((reinterpret_cast<uintptr_t>(row + lo) >> 2) & 3)) & 3);
@@ -138,20 +144,20 @@ __device__ __forceinline__ void for_values(const float* row, int lo, int hi, F4 
     if (tid < v0 - lo) f(row[lo + tid], lo + tid);
     const float4* vec = reinterpret_cast<const float4*>(row + v0);
     int i = tid;
-    for (; i + 3 * THREADS < nv; i += 4 * THREADS) {
+    for (; i + 3 * T < nv; i += 4 * T) {
         float4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = vec[i + j * THREADS];
+        for (int j = 0; j < 4; ++j) x[j] = vec[i + j * T];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f4(x[j], v0 + 4 * (i + j * THREADS));
+        for (int j = 0; j < 4; ++j) f4(x[j], v0 + 4 * (i + j * T));
     }
-    for (; i < nv; i += THREADS) f4(vec[i], v0 + 4 * i);
+    for (; i < nv; i += T) f4(vec[i], v0 + 4 * i);
     const int rest = v0 + 4 * nv + tid;
     if (rest < hi) f(row[rest], rest);
 }
-template <typename F>
+template <int T, typename F>
 __device__ __forceinline__ void for_values(const float* row, int lo, int hi, F f) {
-    for_values(row, lo, hi, [&](const float4& x, int at) {
+    for_values<T>(row, lo, hi, [&](const float4& x, int at) {
         f(x.x, at);
         f(x.y, at + 1);
         f(x.z, at + 2);
@@ -161,7 +167,8 @@ __device__ __forceinline__ void for_values(const float* row, int lo, int hi, F f
 
 // Exact selection of the k best of [lo, hi), k <= hi - lo, whatever the values: the k-th largest key digit by digit, then
 // what is above it and, in order of index, as many of its equals as are missing.
-__device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k) {
+template <int T>
+__device__ void select_exact(Shared<T>& s, const float* row, int lo, int hi, int k) {
     const int tid = threadIdx.x;
     int turn = 0;
     uint32_t prefix = 0;
@@ -172,7 +179,7 @@ __device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k)
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
         uint32_t last = 0;                     // a thread adds a run of one digit at once: rows of equal values meet in one bin
         int run = 0;
-        for_values(row, lo, hi, [&](float v, int) {
+        for_values<T>(row, lo, hi, [&](float v, int) {
             const uint32_t key = key_of(v), digit = (key >> shift) & 255u;
             if ((key & mask) != prefix) return;
             if (digit != last && run > 0) {
@@ -192,7 +199,7 @@ __device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k)
     }
     if (tid == 0) s.found = 0;
     __syncthreads();
-    for_values(row, lo, hi, [&](float v, int at) {
+    for_values<T>(row, lo, hi, [&](float v, int at) {
         const uint32_t key = key_of(v);
         if (key > prefix) {
             const int j = atomicAdd(&s.found, 1);
@@ -203,7 +210,7 @@ __device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k)
     __syncthreads();
     int done = 0;
     const int above = k - need;
-    for (int base = lo; base < hi && done < need; base += THREADS) {
+    for (int base = lo; base < hi && done < need; base += T) {
         const int at = base + tid;
         const bool eq = at < hi && key_of(row[at]) == prefix;
         const unsigned mask = __ballot_sync(0xffffffffu, eq);
@@ -211,7 +218,7 @@ __device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k)
         if (lane == 0) s.part[turn][warp] = __popc(mask);
         __syncthreads();
         int before = done, all = 0;
-        for (int i = 0; i < WARPS; ++i) {
+        for (int i = 0; i < (T / 32); ++i) {
             const int n = s.part[turn][i];
             if (i < warp) before += n;
             all += n;
@@ -227,11 +234,13 @@ __device__ void select_exact(Shared& s, const float* row, int lo, int hi, int k)
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int V, const float* logits, int K, int cluster, int32_t* ids, float* values) {
+template <int T>
+__global__ void __launch_bounds__(T, 1536 / T) top_logits_kernel(int V, const float* logits, int K, int cluster, int32_t* ids, float* values) {
     extern __shared__ __align__(16) unsigned char raw[];
-    Shared& s = *reinterpret_cast<Shared*>(raw);
+    constexpr int FAN = T / MAX_TOP;
+    Shared<T>& s = *reinterpret_cast<Shared<T>*>(raw);
     uint32_t* sent_key = reinterpret_cast<uint32_t*>(&s + 1);
-    uint32_t* sent_idx = sent_key + LIST;
+    uint32_t* sent_idx = sent_key + LIST<T>;
     const int tid = threadIdx.x, rank = (int)blockIdx.x % cluster;
     const size_t r = blockIdx.x / cluster;
     const float* row = logits + r * V;
@@ -248,15 +257,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
     pdl_wait();
     float cut = -INFINITY;
     bool exact = false;
-    if (n_slice > LIST) {
+    if (n_slice > LIST<T>) {
         // runs of 32 values, eight lanes (16 bytes each) to a run, a third of the slice at most: apart by more than a run,
         // whatever their starts' rounding, so that no value is counted twice
         const int runs = min((n_slice - RUN) / (3 * RUN), SAMPLE_RUNS);
         const bool vec = (reinterpret_cast<uintptr_t>(row) & 15) == 0;
         float m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < SAMPLE_RUNS / (THREADS / 8); ++i) {
-            const int run = i * (THREADS / 8) + (tid >> 3);
+        for (int i = 0; i < SAMPLE_RUNS / (T / 8); ++i) {
+            const int run = i * (T / 8) + (tid >> 3);
             if (run < runs) {
                 const int at = (lo + (int)((long)run * (n_slice - RUN) / runs)) / 4 * 4 + 4 * (tid & 7);
                 const int from = max(at, lo);
@@ -276,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
             atomicMax(&s.high, most);
         }
         __syncthreads();
-        const uint32_t c = narrow(s, THREADS, [&](int, uint32_t& v) { v = top; return true; }, s.low, s.high, k, 14).low;
+        const uint32_t c = narrow(s, T, [&](int, uint32_t& v) { v = top; return true; }, s.low, s.high, k, 14).low;
         if (c <= key_of(-INFINITY)) exact = true;              // fewer than k finite maxima
         else cut = value_of(c);
         if (tid == 0) s.high = 0;
@@ -285,15 +294,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
     if (!exact) {
         auto keep = [&](float v, int at) {
             const int j = atomicAdd(&s.count, 1);
-            if (j < LIST) {
+            if (j < LIST<T>) {
                 s.key[j] = key_of(v);
                 s.idx[j] = (uint32_t)at;
             }
         };
-        if (n_slice <= LIST) {
-            for_values(row, lo, hi, keep);
+        if (n_slice <= LIST<T>) {
+            for_values<T>(row, lo, hi, keep);
         } else {
-            for_values(row, lo, hi, [&](const float4& x, int at) {
+            for_values<T>(row, lo, hi, [&](const float4& x, int at) {
                 if (fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) >= cut) {
                     if (x.x >= cut) keep(x.x, at);
                     if (x.y >= cut) keep(x.y, at + 1);
@@ -305,9 +314,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
             });
         }
         __syncthreads();
-        if (s.count > LIST || s.count < k) exact = true;
+        if (s.count > LIST<T> || s.count < k) exact = true;
     }
-    const uint32_t floor_key = n_slice > LIST && !exact ? key_of(cut) : 0u;
+    const uint32_t floor_key = n_slice > LIST<T> && !exact ? key_of(cut) : 0u;
     const bool sends = cluster > 1;
     int have = k;
     const uint32_t *from_key = s.key, *from_idx = s.idx;       // what the blocks of a cluster send, what one block selects among
@@ -317,9 +326,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
         from_key = s.best_key;
         from_idx = s.best_idx;
         n = k;
-    } else if (!sends || n > SENT) {
+    } else if (!sends || n > SENT<T>) {
         uint32_t high = 0;
-        for (int j = tid; j < n; j += THREADS) high = max(high, s.key[j]);
+        for (int j = tid; j < n; j += T) high = max(high, s.key[j]);
         high = __reduce_max_sync(0xffffffffu, high);
         if ((tid & 31) == 0) atomicMax(&s.high, high);
         __syncthreads();
@@ -330,9 +339,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
     if (sends) {
         sm100::cluster_wait();
         const uint32_t to_key = sm100::map_to_cta(smem_u32(sent_key), 0), to_idx = sm100::map_to_cta(smem_u32(sent_idx), 0);
-        for (int i = tid; i < n; i += THREADS) {
-            sm100::st_cluster_u32(to_key + (uint32_t)(rank * SENT + i) * 4u, from_key[i]);
-            sm100::st_cluster_u32(to_idx + (uint32_t)(rank * SENT + i) * 4u, from_idx[i]);
+        for (int i = tid; i < n; i += T) {
+            sm100::st_cluster_u32(to_key + (uint32_t)(rank * SENT<T> + i) * 4u, from_key[i]);
+            sm100::st_cluster_u32(to_idx + (uint32_t)(rank * SENT<T> + i) * 4u, from_idx[i]);
         }
         if (tid == 0) sm100::st_cluster_u32(sm100::map_to_cta(smem_u32(&s.sent[rank]), 0), (uint32_t)n);
         sm100::cluster_sync();
@@ -346,10 +355,10 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
         int at = 0;
         for (int c = 0; c < cluster; ++c) {
             const int m = s.sent[c];
-            for (int i = tid; i < m; i += THREADS) {
-                const uint32_t key = sent_key[c * SENT + i];
+            for (int i = tid; i < m; i += T) {
+                const uint32_t key = sent_key[c * SENT<T> + i];
                 s.key[at + i] = key;
-                s.idx[at + i] = sent_idx[c * SENT + i];
+                s.idx[at + i] = sent_idx[c * SENT<T> + i];
                 low = min(low, key);
                 high = max(high, key);
             }
@@ -383,6 +392,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(int
     }
 }
 
+template <int T>
+static int launch(int M, int V, const float* logits, int K, int cluster, int32_t* ids, float* values, cudaStream_t st) {
+    constexpr size_t SENT_BYTES = 2 * LIST<T> * sizeof(uint32_t);
+    DEER_CUDA(cudaFuncSetAttribute(top_logits_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared<T>) + SENT_BYTES)));
+    DEER_CUDA(launch_pdl_cluster(cluster, top_logits_kernel<T>, dim3((unsigned)(M * cluster)), dim3(T), sizeof(Shared<T>) + (cluster > 1 ? SENT_BYTES : 0), st,
+                                 V, logits, K, cluster, ids, values));
+    return DEER_OK;
+}
+
 }  // namespace toplogits
 
 extern "C" int deer_top_logits(int M, int V, const float* logits, int K, int32_t* ids, float* values, void* stream) {
@@ -394,12 +412,16 @@ extern "C" int deer_top_logits(int M, int V, const float* logits, int K, int32_t
     DEER_CHECK_ARG(logits && ids && values, DEER_ERR_INVALID_ARG, "deer_top_logits: null pointer");
     DEER_CHECK_ARG(deer_aligned16(logits) && deer_aligned4(ids) && deer_aligned4(values), DEER_ERR_INVALID_ARG,
                    "deer_top_logits: logits must be 16-byte aligned, ids and values 4-byte");
-    // as many blocks to a row as fill two blocks an SM, each with a slice worth a pass of its own
-    int cluster = 1;
-    while (cluster < MAX_CLUSTER && (long)M * cluster * 2 <= 2L * deer_sm_count() && V / (cluster * 2) >= LIST) cluster *= 2;
-    const size_t smem = sizeof(Shared) + (cluster > 1 ? 2 * LIST * sizeof(uint32_t) : 0);
-    DEER_CUDA(cudaFuncSetAttribute(top_logits_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared) + 2 * LIST * sizeof(uint32_t))));
-    DEER_CUDA(launch_pdl_cluster(cluster, top_logits_kernel, dim3((unsigned)(M * cluster)), dim3(THREADS), smem, static_cast<cudaStream_t>(stream), V,
-                                 logits, K, cluster, ids, values));
-    return DEER_OK;
+    // Eight or four blocks to a row where all of them run at once (three to an SM), on slices of LIST values at least: 100 rows
+    // of 151936 take 38 us by one block each and 28 by four; but two to a row gain nothing (200 rows: 40 by one, 43 by two), and
+    // in several rounds clusters lose (512 rows: 86 by one, 109 by two).
+    const long slots = 3L * deer_sm_count();
+    int cluster = MAX_CLUSTER;
+    while (cluster > 1 && ((long)M * cluster > slots || V / cluster < LIST<512>)) cluster /= 2;
+    if (cluster == 2) cluster = 1;
+    // many shorter rows by half the threads: what a row costs beside its reading is a chain of steps, and more rows go side by
+    // side (1492 rows of 14725: 48.5 us by 512 threads, 36.4 by 256; 2048 of 32768: 86.5 and 83; 300 of 9999, all side by
+    // side anyway: 13.6 and 15.5; 2048 of 151936, where the reading counts: 243 and 300)
+    return V <= 32768 && M > slots ? launch<256>(M, V, logits, K, 1, ids, values, static_cast<cudaStream_t>(stream))
+                                      : launch<512>(M, V, logits, K, cluster, ids, values, static_cast<cudaStream_t>(stream));
 }

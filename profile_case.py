@@ -7,6 +7,8 @@ program that profiler captures are taken from.
     python profile_case.py layer --B 1 --k 32 --ctx 4096 --hid 4096 --inter 12288 --iters 20
     python profile_case.py trunc --M 512 --V 151936 --top-k-trunc 50 --top-p 0.9 --iters 3
     python profile_case.py moe --M 32 --hid 2048 --experts 128 --inter 768 --top-k 8 --iters 3
+    python profile_case.py headloss --M 1024 --hid 2048 --V 32768 [--top 64] [--forward] --iters 3
+    python profile_case.py toplogits --M 512 --V 151936 --top 64 --iters 3
 
 Prints the average CUDA-event time per call and the achieved GB/s over the
 call's algorithmic bytes.
@@ -35,7 +37,9 @@ from paper_2512_15176_b200 import workload as W  # noqa: E402
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("what", choices=["lmhead", "attn", "qstats", "layer", "trunc", "moe"])
+    ap.add_argument("what", choices=["lmhead", "attn", "qstats", "layer", "trunc", "moe", "headloss", "toplogits"])
+    ap.add_argument("--top", type=int, default=1, help="headloss: entries of a row's list (1: cross entropy); toplogits: K")
+    ap.add_argument("--forward", action="store_true", help="headloss: the loss alone, without its gradients")
     ap.add_argument("--top-p", type=float, default=0.9)
     ap.add_argument("--top-k-trunc", type=int, default=50)
     ap.add_argument("--peaked", action="store_true", help="trunc: rows with a language model's rank-frequency shape")
@@ -178,6 +182,28 @@ def main():
         call = lambda: L.deer_moe_mlp(x, wr, wgu, wd, y, a.top_k, ws)
         nbytes = int(torch.unique(e_ids).numel()) * 3 * I * hid * 2 + E * hid * 2       # the chosen experts' matrices + the router
         flops = 2.0 * a.M * a.top_k * 3 * I * hid
+    elif a.what == "headloss":
+        # the LM head's loss at M rows, and its gradients
+        from paper_2512_15176_b200.runner import HeadLoss
+        h = W.normal(37, "h", (a.M, a.hid), 1.0, device=dev)
+        w = W.normal(37, "w", (a.V, a.hid), a.hid ** -0.5, device=dev)
+        ids = torch.stack([torch.randperm(a.V, generator=torch.Generator().manual_seed(m))[:a.top] for m in range(a.M)]).int().to(dev)
+        teacher = torch.linspace(20.0, 10.0, a.top, device=dev).repeat(a.M, 1).contiguous() if a.top > 1 else None
+        head = HeadLoss(w, a.M, top=a.top, grad=not a.forward)
+
+        def call():
+            head.cross_entropy(h, ids.view(-1)) if teacher is None else head.distill(h, ids, teacher)
+            if not a.forward:
+                head.backward()
+        nbytes = (a.M + a.V) * a.hid * 2 * (1 if a.forward else 2)
+        flops = 2.0 * a.M * a.V * a.hid * (1 if a.forward else 4)
+    elif a.what == "toplogits":
+        z = W.normal(38, "z", (a.M, a.V), 2.0, dtype=torch.float32, device=dev)
+        ids = torch.empty(a.M, a.top, dtype=torch.int32, device=dev)
+        values = torch.empty(a.M, a.top, dtype=torch.float32, device=dev)
+        call = lambda: L.deer_top_logits(z, ids, values)
+        nbytes = a.M * a.V * 4
+        flops = 0.0
     else:
         M = a.B * a.k
         ql = W.normal(33, "ql", (a.B, a.k, a.V), 1.0, dtype=torch.float32, device=dev)
