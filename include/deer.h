@@ -546,14 +546,15 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  * The *_grad calls return the gradients of sum_m grad_loss[m] loss[m]:
  *       dh = G w,  dw = G^T h,  G[m][v] = row_weight[m] grad_loss[m] temperature (p[m][v] - t[m][v]),
  *   from the same inputs and the forward call's lse and target_logit.  z is computed a second time, in pieces of the
- *   vocabulary; G is rounded to bf16 for the two products (p - t of a listed token is formed in fp32), all sums are fp32
- *   and in a fixed order: the same inputs give the same bits.
+ *   vocabulary.  G is rounded to bf16 for the two products (p - t of a listed token is formed in fp32; up to 128 live rows
+ *   two bf16 terms hold G for dh, up to 64 for dw); all sums are fp32 and in a fixed order: the same inputs give the same
+ *   bits, whatever the dead rows hold.
  *   h             bf16 [M][hid];  w bf16 [V][hid];  hid a multiple of 64, at most 65536;  M <= 2^18, V <= 2^30
  *   targets       i32 [M];  ids i32 [M][K], teacher f32 [M][K], K <= 128;  temperature > 0
  *   row_weight    f32 [M] or NULL (1);  grad_loss f32 [M] or NULL (1)
  *   loss, lse     f32 [M]      out: the loss;  logsumexp(z / temperature)
  *   target_logit  f32 [M][K] (K = 1: [M])  out: z at the listed tokens, 0 behind a list's end
- *   dh bf16 [M][hid], dw bf16 [V][hid]     out, overwritten; either may be NULL
+ *   dh bf16 [M][hid], dw bf16 [V][hid]     out, overwritten; either may be NULL; neither may overlap an input
  *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls), 16-byte
  *                 aligned, contents arbitrary, nothing kept in it between calls; one call at a time per workspace.
  * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).

@@ -686,6 +686,7 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     rc = check_pointers(call, h, w, ids, teacher, needs_teacher, row_weight, lse, target_logit);
     if (rc != DEER_OK) return rc;
     DEER_CHECK_ARG(dh || dw, DEER_ERR_INVALID_ARG, "%s: neither dh nor dw is asked for", call);
+    DEER_CHECK_ARG(dh != h && dw != w, DEER_ERR_INVALID_ARG, "%s: a gradient in its operand's place", call);
     DEER_CHECK_ARG(deer_aligned4(grad_loss), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
     const Space s = lay_out(workspace, M, hid, V, K, true);
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,

@@ -19,12 +19,12 @@ constexpr int SHORT = 8;                   // lists of up to so many entries are
                                            // not full), which saves a launch
 inline bool takes_rows_as_they_are(int M, int K) { return M <= ONE_BLOCK && K <= SHORT; }
 constexpr int MAX_TOP = 128;               // entries of a row's list
-constexpr int STATS_SHARE = 2;            // warps that share a tile's columns in STATS: partial sums a row has of a tile
+constexpr int STATS_SHARE = 2;             // warps that share a tile's columns in STATS: partial sums a row has of a tile
 constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3, HDR_FACTOR = 4;
 // Up to this many live rows G is kept as two bf16 terms, rows [0, low) and [low, 2 low) with low = low_term(live).  In dh's
 // product the second takes the places of the second block's rows, idle then.  In dw's it lengthens the contraction: that
 // covers its first 128 places, all of both terms up to 64 live rows, and beyond them (where rows' errors begin to be
-// independent) what is left of its second step (live 128, hid 2688: 435 -> 330 us for both products).
+// independent) what is left of its second step (live 128, hid 2688: 435 -> 380 us for both products).
 constexpr int TWO_TERMS = 128, DW_TERMS = 64;
 __host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32; }
 // Steps of dw's contraction.

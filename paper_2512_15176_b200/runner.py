@@ -501,3 +501,20 @@ class HeadLoss:
         assert self._step is not None and self.dh is not None, "backward() follows a loss of an object made with grad=True"
         self.buffers.run_grad(*self._step, grad_loss, head)
         return self.dh, self.dw if head else None
+
+
+def distill_targets(tokens: torch.Tensor, masked: torch.Tensor, t: torch.Tensor):
+    """Targets and row weights of the paper's first training stage (Eq. 1-2): tokens and masked [B, T], t [B] the sequences'
+    masking levels; a masked position learns its token with weight 1 / t, the others have no target."""
+    targets = torch.where(masked, tokens, -1).to(torch.int32).reshape(-1)
+    return targets, (1.0 / t.float())[:, None].expand(tokens.shape).reshape(-1)
+
+
+def refine_targets(tokens: torch.Tensor, masked: torch.Tensor, R: torch.Tensor, alpha: float = 1.01):
+    """The second stage's (Eq. 3-4): the masked ones of each sequence's last R[b] positions, the i-th of them (i = 1 .. R)
+    with weight alpha^(R - i)."""
+    T = tokens.shape[1]
+    behind = torch.arange(T - 1, -1, -1, device=tokens.device)                 # R - i
+    last = behind[None, :] < R[:, None]
+    targets = torch.where(masked & last, tokens, -1).to(torch.int32).reshape(-1)
+    return targets, torch.where(last, float(alpha) ** behind.float(), 0.0).reshape(-1)

@@ -26,7 +26,7 @@ def test_library_refusals(L):
     def loss(h=FAKE, w=FAKE, ids=FAKE, weight=None, M=5, hid=128, V=300, out=FAKE, ws=FAKE, size=1 << 30):
         return lib.deer_lmhead_loss(h, w, ids, weight, M, hid, V, out, out, out, ws, size, None)
 
-    def grad(K=4, tau=1.0, teacher=FAKE, lse=FAKE, dh=FAKE, dw=FAKE, M=5, hid=128, V=300, ws=FAKE, size=1 << 30):
+    def grad(K=4, tau=1.0, teacher=FAKE, lse=FAKE, dh=2 * FAKE, dw=2 * FAKE, M=5, hid=128, V=300, ws=FAKE, size=1 << 30):
         return lib.deer_lmhead_distill_grad(FAKE, FAKE, FAKE, teacher, K, tau, None, None, lse, FAKE, M, hid, V, dh, dw, ws, size, None)
 
     bad, no = L.DEER_ERR_INVALID_ARG, L.DEER_ERR_UNSUPPORTED
@@ -41,6 +41,7 @@ def test_library_refusals(L):
     assert grad(K=0) == grad(K=129) == no
     assert grad(tau=0.0) == grad(tau=-1.0) == grad(tau=float("nan")) == grad(tau=float("inf")) == bad
     assert grad(teacher=None) == grad(lse=None) == grad(dh=None, dw=None) == grad(dh=FAKE + 8) == grad(dw=FAKE + 4) == bad
+    assert grad(dh=FAKE) == grad(dw=FAKE) == bad                       # in the operand's place
     assert grad(size=L.deer_lmhead_loss_workspace_bytes(5, 128, 300, 4, True) - 1) == L.DEER_ERR_WORKSPACE
     assert grad(M=0, dw=None, ws=None, size=0) == L.DEER_OK
     top = lambda M=2, V=300, x=FAKE, K=8, i=FAKE, v=FAKE: lib.deer_top_logits(M, V, x, K, i, v, None)  # noqa: E731

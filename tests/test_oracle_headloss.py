@@ -93,3 +93,28 @@ def test_top_logits_is_a_stable_sort():
     z[3, 5] = np.nan
     ids, values = O.top_logits(z[3:4, :7], 9)
     assert ids[0, 6] == 5 and np.isnan(values[0, 6]) and (ids[0, 7:] == -1).all() and (values[0, 7:] == -np.inf).all()
+
+
+def test_targets_of_the_two_stages():
+    from paper_2512_15176_b200.runner import distill_targets, refine_targets
+    rng = np.random.default_rng(6)
+    B, T, hid, V = 3, 10, 7, 19
+    tokens, masked = torch.tensor(rng.integers(0, V, (B, T))), torch.tensor(rng.random((B, T)) < 0.6)
+    t, R, alpha = torch.tensor([0.25, 0.5, 1.0]), torch.tensor([1, 4, 10]), 1.01
+    h, w = rng.standard_normal((B * T, hid)), rng.standard_normal((V, hid))
+    z = (h @ w.T).reshape(B, T, V)
+    nll = np.log(np.exp(z).sum(2)) - np.take_along_axis(z, tokens.numpy()[:, :, None], 2)[:, :, 0]
+    targets, weight = distill_targets(tokens, masked, t)
+    assert targets.dtype == torch.int32 and targets.is_contiguous()
+    loss = O.head_loss(h, w, targets.numpy()[:, None], row_weight=weight.numpy().astype(np.float64))[0].reshape(B, T)
+    want = sum(nll[b, i] / float(t[b]) for b in range(B) for i in range(T) if masked[b, i])
+    np.testing.assert_allclose(loss.sum(), want, rtol=1e-12)
+    targets, weight = refine_targets(tokens, masked, R, alpha)
+    loss = O.head_loss(h, w, targets.numpy()[:, None], row_weight=weight.numpy().astype(np.float64))[0].reshape(B, T)
+    want = 0.0
+    for b in range(B):
+        for i in range(1, int(R[b]) + 1):
+            at = T - int(R[b]) + i - 1
+            if masked[b, at]:
+                want += alpha ** (int(R[b]) - i) * nll[b, at]
+    np.testing.assert_allclose(loss.sum(), want, rtol=1e-6)                    # (weights in fp32)
