@@ -1,13 +1,16 @@
 // The K largest logits of each row, ids and values, falling, the lowest index first among equals.
 //
-// A row is read once.  A sample of it (16384 values in 128-byte runs spread over the row, which L2 gives again to the pass
-// behind) yields a cut: each of the 512 (short rows: 256) threads keeps its share's maximum, and the K-th largest of those maxima has K values
-// of the row at or above it, whatever the row looks like.  The pass keeps what is not below the cut -- some 10 K of 151936
-// values -- in shared memory, one compare for four values.  The K best of those are found by a histogram of their keys, 256
-// bins over the range that they span, narrowed to the bin that holds the K-th until it is decided, and put in order by
-// counting.  A row that overfills the list (long ties, a sample that says nothing about the row) is selected exactly instead,
-// by four passes over the digits of the key and one that collects in order of index.  The key is the value's bits in an
-// order of whole numbers: NaN below everything, -0 equal to 0.
+// A row is read once.  A sample of it (16384 values in 128-byte runs spread over the row, which L2 still has when the pass
+// behind comes to them, as that leaves L2 first: load_once) yields a cut: each of the 512 (short rows: 256) threads keeps its
+// share's maximum, and the K-th largest of those maxima has K values of the row at or above it, whatever the row looks like.
+// The pass keeps what is not below the cut -- some 10 K of 151936 values -- in shared memory, one compare for four values.
+// The K best of those are found by a histogram of their keys, 256 bins over the range that they span, narrowed to the bin
+// that holds the K-th until it is decided, and put in order by counting.  A row that overfills the list (long ties, a sample
+// that says nothing about the row) is selected exactly instead, by four passes over the digits of the key and one that
+// collects in order of index.  The key is the value's bits in an order of whole numbers: NaN below everything, -0 equal to 0.
+//
+// The reading bounds it where the rows are many and long: 2048 rows of 151936, the 64 best, 217 us or 0.88 of the measured
+// copy rate.  Few or short rows are a chain of steps, each a meeting of the block: one row 9 us, 32 rows 17.
 //
 // With few rows a cluster of up to eight blocks shares one, each a slice with a cut of its own, and the first block selects
 // among what they kept.
@@ -134,6 +137,13 @@ __device__ int select(Shared<T>& s, const uint32_t* keys, const uint32_t* idxs, 
     return min(n, k);
 }
 
+// What comes so leaves L2 first, and the runs of the sample are still there when the pass comes to them (512 rows of 151936:
+// 356 MB read from HBM without it, 315 with it, of 311; 2048 rows: 243 us and 217).
+__device__ __forceinline__ float4 load_once(const float4* p) {
+    float4 x;
+    asm volatile("ld.global.cs.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
+    return x;
+}
 // Calls f4(four values, the first one's index) for the values [lo, hi) of the row, 16 bytes at a time where the alignment
 // allows it, and f(value, index) for the rest.
 template <int T, typename F4, typename F>
@@ -147,7 +157,7 @@ __device__ __forceinline__ void for_values(const float* row, int lo, int hi, F4 
     for (; i + 3 * T < nv; i += 4 * T) {
         float4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = vec[i + j * T];
+        for (int j = 0; j < 4; ++j) x[j] = load_once(vec + i + j * T);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f4(x[j], v0 + 4 * (i + j * T));
     }
@@ -234,8 +244,8 @@ __device__ void select_exact(Shared<T>& s, const float* row, int lo, int hi, int
     __syncthreads();
 }
 
-template <int T>
-__global__ void __launch_bounds__(T, 1536 / T) top_logits_kernel(int V, const float* logits, int K, int cluster, int32_t* ids, float* values) {
+template <int T, int BLOCKS>
+__global__ void __launch_bounds__(T, BLOCKS) top_logits_kernel(int V, const float* logits, int K, int cluster, int32_t* ids, float* values) {
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr int FAN = T / MAX_TOP;
     Shared<T>& s = *reinterpret_cast<Shared<T>*>(raw);
@@ -392,11 +402,12 @@ __global__ void __launch_bounds__(T, 1536 / T) top_logits_kernel(int V, const fl
     }
 }
 
-template <int T>
+// BLOCKS of T threads to an SM.
+template <int T, int BLOCKS>
 static int launch(int M, int V, const float* logits, int K, int cluster, int32_t* ids, float* values, cudaStream_t st) {
     constexpr size_t SENT_BYTES = 2 * LIST<T> * sizeof(uint32_t);
-    DEER_CUDA(cudaFuncSetAttribute(top_logits_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared<T>) + SENT_BYTES)));
-    DEER_CUDA(launch_pdl_cluster(cluster, top_logits_kernel<T>, dim3((unsigned)(M * cluster)), dim3(T), sizeof(Shared<T>) + (cluster > 1 ? SENT_BYTES : 0), st,
+    DEER_CUDA(cudaFuncSetAttribute(top_logits_kernel<T, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared<T>) + SENT_BYTES)));
+    DEER_CUDA(launch_pdl_cluster(cluster, top_logits_kernel<T, BLOCKS>, dim3((unsigned)(M * cluster)), dim3(T), sizeof(Shared<T>) + (cluster > 1 ? SENT_BYTES : 0), st,
                                  V, logits, K, cluster, ids, values));
     return DEER_OK;
 }
@@ -419,9 +430,17 @@ extern "C" int deer_top_logits(int M, int V, const float* logits, int K, int32_t
     int cluster = MAX_CLUSTER;
     while (cluster > 1 && ((long)M * cluster > slots || V / cluster < LIST<512>)) cluster /= 2;
     if (cluster == 2) cluster = 1;
-    // many shorter rows by half the threads: what a row costs beside its reading is a chain of steps, and more rows go side by
+    // Many shorter rows by half the threads: what a row costs beside its reading is a chain of steps, and more rows go side by
     // side (1492 rows of 14725: 48.5 us by 512 threads, 36.4 by 256; 2048 of 32768: 86.5 and 83; 300 of 9999, all side by
-    // side anyway: 13.6 and 15.5; 2048 of 151936, where the reading counts: 243 and 300)
-    return V <= 32768 && M > slots ? launch<256>(M, V, logits, K, 1, ids, values, static_cast<cudaStream_t>(stream))
-                                      : launch<512>(M, V, logits, K, cluster, ids, values, static_cast<cudaStream_t>(stream));
+    // side anyway: 13.6 and 15.5; 2048 of 151936, where the reading counts: 243 and 300; all before load_once).
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (M <= slots) return launch<512, 3>(M, V, logits, K, cluster, ids, values, st);
+    // A third more rows to an SM, at 32 registers a thread, where that saves a round of them (512 rows of 151936: 78 us in two
+    // rounds, 59 in one; 1184: 131 and 126; 4096: 420 and 405; 2048 of 32768 by 256 threads: 79 and 69); where it saves none, a
+    // round only takes longer (700 rows: 85 and 98; 1332: 140 and 157; 1492 of 14725: 33 and 36).
+    const bool short_rows = V <= 32768;
+    const long wave = short_rows ? 2 * slots : slots, wider = wave / 3 * 4;
+    if ((M + wider - 1) / wider < (M + wave - 1) / wave)
+        return short_rows ? launch<256, 8>(M, V, logits, K, 1, ids, values, st) : launch<512, 4>(M, V, logits, K, 1, ids, values, st);
+    return short_rows ? launch<256, 6>(M, V, logits, K, 1, ids, values, st) : launch<512, 3>(M, V, logits, K, 1, ids, values, st);
 }

@@ -299,6 +299,15 @@ def test_top_logits_of_unlike_rows(L, V):
         check_top(L, z[-3:], K)
 
 
+@pytest.mark.parametrize("M,V,K", [(450, 33001, 20), (600, 40000, 1), (700, 5003, 40), (900, 5003, 128), (1300, 2500, 9)])
+def test_top_logits_of_many_rows(L, M, V, K):
+    """One and two rounds of rows over the device, three and four of them to an SM; every tenth row mostly equal or all -inf."""
+    z = torch.randn(M, V, generator=torch.Generator().manual_seed(M))
+    z[::20] = torch.round(z[::20])
+    z[10::20] = -math.inf
+    check_top(L, z, K)
+
+
 def test_top_logits_with_nan(L):
     g = torch.Generator().manual_seed(1)
     z = torch.randn(6, 5003, generator=g)
