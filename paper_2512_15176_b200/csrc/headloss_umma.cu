@@ -9,9 +9,14 @@
 // One kernel body; the two products of BACK share a launch, so that the many short tiles of dw fill what the few long ones
 // of dh leave of the last wave.  Pairs of blocks (tcgen05.mma.cta_group::2, 256 x n tiles, n <= 256, fp32 accumulators in two
 // tensor-memory buffers) walk a list of tiles: a warp per block brings 64-deep steps of both operands by TMA into a ring
-// of six 32 KB stages, one warp of the pair issues the MMAs, four warps per block take the finished tile while the next
-// one is computed.  h and G are stored row-major once; where the contraction runs along their rows (dw, and w in dh) the
+// of as many stages as fit, one warp of the pair issues the MMAs, eight warps per block (BACK: four) take the finished tile
+// while the next one is computed.  Up to ONE_BLOCK rows STATS and GRAD take single blocks, whose 128 rows pairs would leave
+// half empty.  h and G are stored row-major once; where the contraction runs along their rows (dw, and w in dh) the
 // operand is read MN-major: boxes of 64 contraction rows x 64 columns, two of them side by side.
+//
+// 1024 rows x 32768 x 2048, each launch alone and cold: STATS 95 us (tensor pipe 77 % busy), GRAD 98 (75 %), BACK 188 (81 %):
+// the tensor cores bound them.  96 rows x 65536 x 2048: 50, 54 and 114 us for 269, 284 and 534 MB of HBM traffic: memory does,
+// and in dw's part the way out of the SMs.
 //
 // G is rounded to bf16 for the products: as much as dh and dw are themselves, and with many rows the errors of different
 // rows are as independent as theirs.  At a listed token p - t is formed in fp32 first, so that a target the model is sure of
