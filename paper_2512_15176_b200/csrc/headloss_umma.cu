@@ -310,6 +310,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs& a, const CUtensorMap
             float run_m = -INFINITY, run_s = 0.f;
             for (int c = 32 * turn; c < width && !idle; c += 32 * SHARE) {
                 uint32_t v[32];
+                __syncwarp();                                             // the rows' lists part the lanes; TMEM loads want all of them together
                 TMEM_LD_X32(taddr + c, v);
                 tmem_wait_ld();
                 const int have = width - c;

@@ -1,0 +1,49 @@
+"""Calls of the LM head's losses at the edges of what they take: lists that differ from row to row."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_headloss import draw, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2512_15176_b200 import binding
+    binding.lib()
+    return binding
+
+
+def test_lists_that_differ_from_row_to_row(L):
+    """No two neighbouring rows have their listed tokens in the same columns, or as many of them: nothing, one, or all of a
+    chunk of 32.  Every row's z and lse against the formula, in tiles of the rows as they are (short lists) and of lists by id."""
+    for M, K in ((64, 8), (96, 128), (300, 128), (300, 33)):
+        hid, V = 128, 3000
+        h, w, _, teacher, a, g = draw(M, M, hid, V, K=K)
+        gen = torch.Generator().manual_seed(M + K)
+        ids = torch.full((M, K), -1, dtype=torch.int32)
+        for m in range(M):
+            n = 1 + (m * 37) % K
+            if m % 4 == 0:
+                pick = torch.randperm(V, generator=gen)[:n]
+            elif m % 4 == 1:
+                pick = (32 * (m % 90) + torch.arange(n)) % V    # a chunk, and what is behind it
+            elif m % 4 == 2:
+                pick = V - 1 - torch.arange(n)
+            else:
+                pick = (torch.arange(n) * 32 + m % 32) % V      # one to a chunk
+            ids[m, :n] = pick.int()
+        loss, lse, tl, dh, dw = run(L, h, w, ids, teacher=teacher, weight=a, grad=g)
+        z = h.double() @ w.double().T
+        dz = (hid / 16 + 8) * 2.0 ** -23 * (h.double().abs() @ w.double().abs().T).amax(1)
+        want = torch.logsumexp(z, 1)
+        assert ((lse.cpu().double() - want).abs() <= dz + 2.0 ** -20 + 2.0 ** -21 * want.abs()).all()
+        zt = torch.gather(z, 1, ids.clamp_min(0).long())
+        err = (tl.cpu().double() - zt).abs()
+        assert (err[ids >= 0] <= dz[:, None].expand(M, K)[ids >= 0]).all() and (tl.cpu()[ids < 0] == 0).all()
+        t = torch.softmax(torch.where(ids >= 0, teacher.double(), -math.inf), 1)
+        each = torch.where(ids >= 0, t * (torch.log(torch.where(t > 0, t, 1.0)) - zt + want[:, None]), 0.0).sum(1)
+        tol = a.double() * (2 * dz + 2.0 ** -20 + 2.0 ** -20 * (want.abs() + z.abs().amax(1) + 20))
+        assert ((loss.cpu().double() - a.double() * each).abs() <= tol).all()
