@@ -111,6 +111,9 @@ __device__ __forceinline__ bool is_live(const RowArgs& a, int m) { return is_liv
 __device__ __forceinline__ float row_coef(const RowArgs& a, int m) {
     return (a.weight ? a.weight[m] : 1.f) * (a.grad ? a.grad[m] : 1.f) * a.tau;
 }
+// A row's coefficient relative to the call's largest finite one.  Without a finite one other than 0 it stays as it is: what is
+// not finite must reach the gradients.
+__device__ __forceinline__ float relative(float coef, float top) { return top > 0.f ? coef / top : coef; }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -289,7 +292,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
     if (blockIdx.x == 0 && tid == 0) {
         a.s.hdr[HDR_LIVE] = total;
         a.s.hdr[HDR_GAVE_UP] = 0;
-        a.s.hdr[HDR_SCALE] = __float_as_int(top);
+        a.s.hdr[HDR_SCALE] = __float_as_int(top > 0.f ? top : 1.f);
         a.s.hdr[HDR_FACTOR] = __float_as_int(1.f);
     }
     if (GRAD && blockIdx.x == 0 && warp == ROW_WARPS - 1) {
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
             float coef = 0.f;
             if (GRAD) {
                 const bool some = l.targets(a, lane);
-                coef = some && !l.beyond && top > 0.f ? row_coef(a, m) / top : 0.f;
+                coef = some && !l.beyond ? relative(row_coef(a, m), top) : 0.f;
             }
             if (lane == 0) {
                 a.s.slot[m] = slot;

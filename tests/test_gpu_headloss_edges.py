@@ -1,4 +1,5 @@
-"""Calls of the LM head's losses at the edges of what they take: lists that differ from row to row."""
+"""Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, lists that differ from row
+to row."""
 import math
 
 import pytest
@@ -14,6 +15,52 @@ def L():
     from paper_2512_15176_b200 import binding
     binding.lib()
     return binding
+
+
+# One live row, rows whose G is held as two terms for both products, for dh alone, as one term.
+ROWS = [1, 40, 100, 300]
+
+
+def outside(x):
+    return ~torch.isfinite(x.float())
+
+
+@pytest.mark.parametrize("M", ROWS)
+@pytest.mark.parametrize("K", [None, 5])
+@pytest.mark.parametrize("where", ["weight", "grad"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_coefficients_that_are_not_finite_throughout(L, M, K, where, value):
+    """Every entry of the formula's gradients is a sum with a term of inf or NaN in it."""
+    h, w, ids, teacher, a, g = draw(M, M, 64, 150, K=K)
+    (a if where == "weight" else g).fill_(value)
+    loss, _, _, dh, dw = run(L, h, w, ids, teacher=teacher, weight=a, grad=g)
+    assert outside(dh).all() and outside(dw).all()
+    assert outside(loss).all() if where == "weight" else torch.isfinite(loss).all()
+
+
+@pytest.mark.parametrize("M", ROWS[1:])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("others", [0.0, 1.0])
+def test_one_coefficient_that_is_not_finite(L, M, value, others):
+    """Beside rows without an upstream gradient, and beside ordinary ones: their dh is the same as without that row."""
+    h, w, ids, _, a, g = draw(M, M, 64, 150)
+    g *= others
+    row = M // 3
+    keep = torch.arange(M) != row
+    g[row] = 0.0
+    want = run(L, h, w, ids, weight=a, grad=g)[3]
+    g[row] = value
+    _, _, _, dh, dw = run(L, h, w, ids, weight=a, grad=g)
+    assert outside(dh[row]).all() and outside(dw).all()
+    assert torch.isfinite(dh[keep].float()).all()
+    # (a common scale of G is chosen anew: as much as its rounding to bf16 and dh's own, 2^-8 each of a row's largest terms)
+    assert ((dh[keep].float() - want[keep].float()).abs() <= 2.0 ** -7 * w.float().abs().max() * a[keep].cuda()[:, None] * g[keep].abs().cuda()[:, None] * 2).all()
+
+
+def test_rows_without_a_gradient_stay_at_zero(L):
+    h, w, ids, _, a, _ = draw(2, 30, 64, 150)
+    _, _, _, dh, dw = run(L, h, w, ids, weight=a, grad=torch.zeros(30))
+    assert not dh.any() and not dw.any()
 
 
 def test_lists_that_differ_from_row_to_row(L):
