@@ -537,9 +537,9 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *       loss[m] = row_weight[m] (logsumexp(z[m]) - z[m][targets[m]]).
  * deer_lmhead_distill: the Kullback-Leibler divergence from a teacher that is known by its top logits (deer_top_logits
  *   of the verifier's rows).  A row's list is ids[m][0 ..], ended by K or by the first negative id; t = softmax(teacher /
- *   temperature) over the list (an entry of -inf has probability 0; an id that is listed twice has the sum), p =
- *   softmax(z / temperature) over the vocabulary:
- *       loss[m] = row_weight[m] temperature^2 sum_j t_j (log t_j - log p[ids_j]).
+ *   temperature) over the list (an entry of -inf has probability 0), p = softmax(z / temperature) over the vocabulary:
+ *       loss[m] = row_weight[m] temperature^2 sum_v t_v (log t_v - log p_v)
+ *   over the tokens v of the list: an id that is listed twice is one token, t_v the sum of its entries.
  * Rows without a target (targets[m] < 0, ids[m][0] < 0) or with row_weight 0 are dead: loss, lse, target_logit and
  *   gradient 0; what h holds there is not used, and they cost nothing (the live rows are moved together first).  A list
  *   whose entries are all -inf has loss and gradient 0.  An id of V or more makes its row's loss NaN and its gradient 0.

@@ -727,21 +727,10 @@ def head_loss(h, w, ids, teacher=None, temperature=1.0, row_weight=None):
     live = live & (a != 0)
     top = z.max(axis=1, keepdims=True)
     lse = (top + np.log(np.exp(z - top).sum(axis=1, keepdims=True)))[:, 0]
-    # an entry's own t enters its logarithm, not the sum over a repeated id
     loss = np.zeros(M)
     for m in np.nonzero(live)[0]:
-        n = 0
-        while n < ids.shape[1] and ids[m, n] >= 0:
-            n += 1
-        u = np.zeros(n) if teacher is None else np.asarray(teacher[m, :n], dtype=np.float64) / temperature
-        if np.all(u == -np.inf):
-            continue
-        log_t = u - u.max()
-        log_t = log_t - np.log(np.exp(log_t).sum()) if teacher is not None else u
-        for j in range(n):
-            if log_t[j] > -np.inf:
-                loss[m] += np.exp(log_t[j]) * (log_t[j] - z[m, ids[m, j]] + lse[m])
-        loss[m] *= a[m] * temperature ** 2
+        v = np.nonzero(t[m] != 0)[0]
+        loss[m] = a[m] * temperature ** 2 * (t[m, v] * (np.log(t[m, v]) - z[m, v] + lse[m])).sum()
     return loss, np.where(live, lse, 0.0), np.exp(z - lse[:, None]), t, live
 
 

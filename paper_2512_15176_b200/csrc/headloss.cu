@@ -2,7 +2,7 @@
 //
 // A row's target is a distribution t over a list of tokens (cross entropy: one token, t = 1; distillation: the softmax of
 // the teacher's logits of the list).  With z = h w^T / tau and lse = log sum exp z over the vocabulary,
-//     loss    = a tau^2 sum_j t_j (log t_j - z_j + lse)
+//     loss    = a tau^2 sum_j t_j (log t_j - z_j + lse)          (j: tokens; what a list names twice has the sum of both)
 //     G[m][v] = a g tau (exp(z_v - lse) - t_v),     dh = G w,     dw = G^T h
 // (a: the row's weight, g: the upstream gradient of its loss).  The logits are never kept: the forward pass reduces each
 // tile of z to (max, sum exp) per row, the backward pass computes z a second time, a piece of the vocabulary at a time,
@@ -519,6 +519,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
     }
     // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
     float more = 0.f;
+    bool repeats = false;
 #pragma unroll
     for (int i = 0; i < MAX_TOP / 32; ++i) {
         const int j = i * 32 + lane;
@@ -528,15 +529,32 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
             for (int o = 0; o < j; ++o) at = a.ids[(size_t)m * a.K + o] == l.id[i] ? -1 : at;
         else at = a.s.place[(size_t)slot * a.K + j];
         l.z[i] = fmaf(l.z[i], plain.y, fmaf(l.z[i], plain.x, -all));
+        repeats |= at < 0;
         if (at < 0) continue;
         const float tile_z = a.s.z[(size_t)slot * a.K + at];
         more += exp2f(l.z[i]) - exp2f(fmaf(tile_z, tile.y, fmaf(tile_z, tile.x, -all)));
     }
     const float log_sum = logf(sum + warp_sum(more));
-    float each = 0.f;
+    float t[MAX_TOP / 32], each = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) t[i] = i * 32 + lane < l.n ? expf(l.log_t[i]) : 0.f;
+    if (__any_sync(0xffffffffu, repeats)) {                // log t of a token is that of the sum over its entries
+        float token[MAX_TOP / 32] = {};
+#pragma unroll
+        for (int c = 0; c < MAX_TOP / 32; ++c)
+            for (int from = 0; from < 32; ++from) {
+                const int id = __shfl_sync(0xffffffffu, l.id[c], from);
+                const float some_t = __shfl_sync(0xffffffffu, t[c], from);
+#pragma unroll
+                for (int i = 0; i < MAX_TOP / 32; ++i) token[i] += c * 32 + from < l.n && l.id[i] == id ? some_t : 0.f;
+            }
+#pragma unroll
+        for (int i = 0; i < MAX_TOP / 32; ++i)
+            if (token[i] > t[i]) l.log_t[i] = logf(token[i]);
+    }
 #pragma unroll
     for (int i = 0; i < MAX_TOP / 32; ++i)
-        if (i * 32 + lane < l.n && l.id[i] < a.V && !(l.log_t[i] == -INFINITY)) each += expf(l.log_t[i]) * (l.log_t[i] + fmaf(l.z[i], -LN2, log_sum));
+        if (i * 32 + lane < l.n && l.id[i] < a.V && !(t[i] == 0.f)) each += t[i] * (l.log_t[i] + fmaf(l.z[i], -LN2, log_sum));
     each = warp_sum(each);
     if (lane == 0) {
         const float x = (a.weight ? a.weight[m] : 1.f) * (a.tau * a.tau) * each;

@@ -1,5 +1,5 @@
-"""Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, lists that differ from row
-to row."""
+"""Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, tokens listed twice, lists
+that differ from row to row."""
 import math
 
 import pytest
@@ -61,6 +61,31 @@ def test_rows_without_a_gradient_stay_at_zero(L):
     h, w, ids, _, a, _ = draw(2, 30, 64, 150)
     _, _, _, dh, dw = run(L, h, w, ids, weight=a, grad=torch.zeros(30))
     assert not dh.any() and not dw.any()
+
+
+@pytest.mark.parametrize("M,K", [(5, 6), (40, 8), (40, 9), (200, 20), (150, 128)])
+def test_the_divergence_of_lists_that_repeat_tokens(L, M, K):
+    """The list's distribution over tokens: what stands twice counts by its sum, in the loss as in its gradients."""
+    tau, V, hid = 1.5, 60, 64
+    h, w, _, _, a, g = draw(M + K, M, hid, V)
+    gen = torch.Generator().manual_seed(K)
+    ids = torch.randint(V // 3, (M, K), generator=gen).int()
+    teacher = 3 * torch.randn(M, K, generator=gen)
+    ids[0] = 7                                                  # one token: the divergence of a sure teacher
+    ids[1, K // 2:] = -1
+    teacher[2, ::2] = -math.inf                                 # entries without probability, some of a token that has some
+    teacher[3, 1:] = teacher[3, 0] - 300.0                      # and some whose probability is below fp32's least
+    loss, _, _, dh, dw = run(L, h, w, ids, teacher=teacher, tau=tau, weight=a, grad=g)
+    live = (ids >= 0).double()
+    t = torch.softmax(torch.where(ids >= 0, teacher.double() / tau, -math.inf), 1) * live
+    dense = torch.zeros(M, V, dtype=torch.float64).scatter_add_(1, ids.clamp_min(0).long(), t)
+    logp = torch.log_softmax(h.double() @ w.double().T / tau, 1)
+    each = torch.where(dense > 0, dense * (torch.log(torch.where(dense > 0, dense, 1.0)) - logp), 0.0).sum(1)
+    want = a.double() * tau ** 2 * each
+    # z by plain sums and lse: 2^-19 of the largest of them; a logarithm and an exponential of t each a few 2^-24 of |log t| <= 5
+    tol = a.double() * tau ** 2 * (2.0 ** -19 * logp.abs().amax(1) + 2.0 ** -20)
+    assert ((loss.cpu().double() - want).abs() <= tol).all(), ((loss.cpu().double() - want).abs() / tol).max()
+    assert (loss.cpu() >= -tol).all()                           # a divergence is not negative
 
 
 def test_lists_that_differ_from_row_to_row(L):
