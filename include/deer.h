@@ -559,7 +559,7 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls), 16-byte
  *                 aligned, contents arbitrary, nothing kept in it between calls; one call at a time per workspace.
  * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).
- * A bounded wait that runs out makes the call's losses, or dh, NaN. */
+ * A bounded wait that runs out makes the losses that it was for NaN, or all of the call's dh and dw. */
 size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad);
 int deer_lmhead_loss(const void* h, const void* w, const int32_t* targets, const float* row_weight, int M, int hid, int V,
                      float* loss, float* lse, float* target_logit, void* workspace, size_t workspace_bytes, void* stream);
@@ -572,6 +572,10 @@ int deer_lmhead_distill(const void* h, const void* w, const int32_t* ids, const 
 int deer_lmhead_distill_grad(const void* h, const void* w, const int32_t* ids, const float* teacher, int K, float temperature,
                              const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit,
                              int M, int hid, int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Self-test of what such a wait leaves: the end of a *_grad call once more, on the workspace of one that has just run with
+ * these sizes, as if one of its products had given up.  dh or dw may be NULL. */
+int deer_selftest_lmhead_gave_up(int M, int hid, int V, int K, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The K largest logits of each row, falling, the lowest index first among equals: what a teacher's row leaves for
  * deer_lmhead_distill (deer_lmhead_select's out_logits of the verifier, or any fp32 rows).

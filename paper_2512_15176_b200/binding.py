@@ -36,7 +36,7 @@ EXPORTS = [
     "deer_rmsnorm_quant", "deer_quantize", "deer_linear_quant", "deer_kv_create_quant", "deer_kv_store",
     "deer_kv_reserve_rows", "deer_kv_commit_rows", "deer_block_attn_quant_workspace_bytes", "deer_block_attn_quant",
     "deer_lmhead_loss_workspace_bytes", "deer_lmhead_loss", "deer_lmhead_loss_grad", "deer_lmhead_distill",
-    "deer_lmhead_distill_grad", "deer_top_logits",
+    "deer_lmhead_distill_grad", "deer_top_logits", "deer_selftest_lmhead_gave_up",
 ]
 
 
@@ -157,6 +157,7 @@ def lib() -> ctypes.CDLL:
     L.deer_lmhead_distill.argtypes = [c_void_p] * 4 + [c_int, c_float, c_void_p] + [c_int] * 3 + [c_void_p] * 4 + [c_size_t, c_void_p]
     L.deer_lmhead_distill_grad.argtypes = ([c_void_p] * 4 + [c_int, c_float] + [c_void_p] * 4 + [c_int] * 3 + [c_void_p] * 3
                                            + [c_size_t, c_void_p])
+    L.deer_selftest_lmhead_gave_up.argtypes = [c_int] * 4 + [c_void_p] * 3 + [c_size_t, c_void_p]
     L.deer_top_logits.argtypes = [c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]
     for name in EXPORTS:
         getattr(L, name)          # every declared entry point must be exported
@@ -674,6 +675,16 @@ def deer_lmhead_distill_grad(h, w, ids, teacher, temperature, lse, target_logit,
     with there:
         _check(lib().deer_lmhead_distill_grad(h, w, ids, teacher, K, temperature, row_weight, grad_loss, lse, target_logit, M, hid, V, dh, dw, ws,
                                               _bytes_of(workspace), _stream(stream)))
+
+
+def deer_selftest_lmhead_gave_up(h, w, K, dh, dw, workspace, stream=None):
+    call = "deer_selftest_lmhead_gave_up"
+    M, hid, V = _head_of(call, h, w)
+    if not (_may_be(dh, _BF16, M * hid) and _may_be(dw, _BF16, V * hid)):
+        _refuse(call, "dh must be bf16 [M][hid], dw bf16 [V][hid]")
+    (_, _, dh, dw, ws), there = _operands(call, h, w, dh, dw, workspace)
+    with there:
+        _check(lib().deer_selftest_lmhead_gave_up(M, hid, V, K, dh, dw, ws, _bytes_of(workspace), _stream(stream)))
 
 
 class HeadLossBuffers:

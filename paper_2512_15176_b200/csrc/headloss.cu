@@ -565,13 +565,22 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
 
 // dh of every row: the partial sums of its ranges in a fixed order, zeros for a dead row.  A block takes 128 columns of
 // up to eight rows; where there are many partial sums its warps share a row's, so that they are all on their way at once.
-__global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, int per_block, __nv_bfloat16* dh) {
+// As the call's last kernel it also marks what a product that gave up has left: dh and dw all NaN.  dh, dw: NULL where not
+// asked for.
+__global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, int per_block, __nv_bfloat16* dh, __nv_bfloat16* dw) {
     __shared__ float4 sums[ROW_WARPS][ROW_WARPS][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int m0 = blockIdx.x * per_block, rows = min(per_block, a.M - m0), c = (blockIdx.y * 32 + lane) * 4;
     const bool in = c < a.hid;
     pdl_trigger();
     pdl_wait();
+    if (dw && a.s.hdr[HDR_GAVE_UP]) {
+        uint4* to = reinterpret_cast<uint4*>(dw);          // (rows are a multiple of 16 bytes)
+        const size_t n = (size_t)a.V * a.hid / 8, threads = (size_t)gridDim.x * gridDim.y * ROW_THREADS;
+        for (size_t i = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * ROW_THREADS + threadIdx.x; i < n; i += threads)
+            to[i] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+    }
+    if (!dh) return;
     const int live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
     // few live rows: a range's tile holds the two terms' products, 128 rows each
     const int parts = live <= TWO_TERMS ? 2 * ranges : ranges;
@@ -693,6 +702,16 @@ static int loss_call(const char* call, const void* h, const void* w, const int32
     return DEER_OK;
 }
 
+// What is behind the products of a gradient call.
+static int finish_grad(const RowArgs& a, void* dh, void* dw, cudaStream_t st) {
+    static bool dh_set[64] = {};
+    DEER_CUDA(keep_split(head_dh_kernel, dh_set));
+    const int per_block = a.M <= 512 ? 1 : ROW_WARPS;      // (few rows may have many partial sums each)
+    const dim3 grid = dh ? dim3((unsigned)((a.M + per_block - 1) / per_block), (unsigned)((a.hid + 127) / 128)) : dim3((unsigned)deer_sm_count());
+    DEER_CUDA(launch_pdl(head_dh_kernel, grid, dim3(ROW_THREADS), 0, st, a, per_block, static_cast<__nv_bfloat16*>(dh), static_cast<__nv_bfloat16*>(dw)));
+    return DEER_OK;
+}
+
 static int grad_call(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, bool needs_teacher, int K,
                      float tau, const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit, int M, int hid,
                      int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
@@ -722,10 +741,9 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     a.dw_tiles = dw ? (s.piece + TILE - 1) / TILE * a.ht : 0;
     a.pairs = deer_sm_count() / 2;
     a.slab_tiles = s.slab_tiles;
-    static bool rows_set[64] = {}, dh_set[64] = {}, factor_set[64] = {};
+    static bool rows_set[64] = {}, factor_set[64] = {};
     DEER_CUDA(keep_split(head_factor_kernel, factor_set));
     DEER_CUDA(keep_split(head_rows_kernel<true>, rows_set));
-    DEER_CUDA(keep_split(head_dh_kernel, dh_set));
     DEER_CUDA(launch_pdl(head_rows_kernel<true>, dim3(row_blocks(a)), dim3(ROW_THREADS), 0, st, a));
     if (M > DW_TERMS) DEER_CUDA(launch_pdl(head_factor_kernel, dim3(1), dim3(1024), 0, st, a, (int)row_blocks(a)));
     for (int p = 0; p < s.pieces; ++p) {
@@ -733,17 +751,30 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
         if (rc == DEER_OK) rc = launch_product(BACK, s, h, w, ids, row_weight, M, hid, V, K, p, tau, nullptr, dh != nullptr, dw, st);
         if (rc != DEER_OK) return rc;
     }
-    if (dh) {
-        const int per_block = M <= 512 ? 1 : ROW_WARPS;    // (few rows may have many partial sums each)
-        DEER_CUDA(launch_pdl(head_dh_kernel, dim3((unsigned)((M + per_block - 1) / per_block), (unsigned)((hid + 127) / 128)), dim3(ROW_THREADS), 0, st,
-                             a, per_block, static_cast<__nv_bfloat16*>(dh)));
-    }
-    return DEER_OK;
+    return finish_grad(a, dh, dw, st);
+}
+
+// The end of a gradient call again, as if one of its products had given up.
+static int selftest_gave_up(int M, int hid, int V, int K, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* call = "deer_selftest_lmhead_gave_up";
+    const int rc = check_sizes(call, K, 1.f, M, hid, V);
+    if (rc != DEER_OK) return rc;
+    DEER_CHECK_ARG(M > 0 && (dh || dw) && deer_aligned16(dh) && deer_aligned16(dw), DEER_ERR_INVALID_ARG, "%s: no rows, no gradient or a misaligned one", call);
+    const Space s = lay_out(workspace, M, hid, V, K, true);
+    DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
+                   "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    DEER_CUDA(cudaMemsetAsync(s.hdr + HDR_GAVE_UP, 1, 4, st));
+    return finish_grad(row_args(s, nullptr, nullptr, nullptr, K, 1.f, nullptr, M, hid, V), dh, dw, st);
 }
 
 }  // namespace headloss
 
 extern "C" {
+
+int deer_selftest_lmhead_gave_up(int M, int hid, int V, int K, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream) {
+    return headloss::selftest_gave_up(M, hid, V, K, dh, dw, workspace, workspace_bytes, stream);
+}
 
 size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad) {
     if (M <= 0 || M > (1 << 18) || hid < 64 || hid % 64 || hid > 65536 || V < 1 || V > (1 << 30) || K < 1 || K > headloss::MAX_TOP) return 0;

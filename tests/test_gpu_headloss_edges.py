@@ -1,5 +1,5 @@
 """Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, tokens listed twice, lists
-that differ from row to row."""
+that differ from row to row, products that gave up."""
 import math
 
 import pytest
@@ -119,3 +119,29 @@ def test_lists_that_differ_from_row_to_row(L):
         each = torch.where(ids >= 0, t * (torch.log(torch.where(t > 0, t, 1.0)) - zt + want[:, None]), 0.0).sum(1)
         tol = a.double() * (2 * dz + 2.0 ** -20 + 2.0 ** -20 * (want.abs() + z.abs().amax(1) + 20))
         assert ((loss.cpu().double() - a.double() * each).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("M,V", [(1, 40), (70, 513), (300, 1000), (600, 2049)])
+def test_gradients_of_a_product_that_gave_up_are_nan(L, M, V):
+    """Both gradients, each alone, and nothing behind their ends; the next call is right again."""
+    hid = 192
+    h, w, ids, _, a, g = draw(M, M, hid, V)
+    want = run(L, h, w, ids, weight=a, grad=g)
+    h_, w_, t_, a_, g_ = (x.cuda() for x in (h, w, ids.view(-1), a, g))
+    ws = torch.empty(L.deer_lmhead_loss_workspace_bytes(M, hid, V, 1, True), dtype=torch.uint8, device="cuda")
+    room_h, room_w = (torch.full((n * hid + 64,), 3.0, dtype=torch.bfloat16, device="cuda") for n in (M, V))
+    dh, dw = room_h[:M * hid], room_w[:V * hid]
+
+    def grad(dh, dw):
+        L.deer_lmhead_loss_grad(h_, w_, t_, want[1], want[2], dh, dw, ws, a_, g_)
+
+    for dh_, dw_ in ((dh, dw), (None, dw), (dh, None)):
+        grad(dh_, dw_)
+        for x, y in ((dh_, want[3]), (dw_, want[4])):
+            assert x is None or torch.equal(x.view_as(y), y)
+        L.deer_selftest_lmhead_gave_up(h_, w_, 1, dh_, dw_, ws)
+        for x in (dh_, dw_):
+            assert x is None or torch.isnan(x).all()
+    assert (room_h[M * hid:] == 3).all() and (room_w[V * hid:] == 3).all()
+    grad(dh, dw)
+    assert torch.equal(dh.view_as(want[3]), want[3]) and torch.equal(dw.view_as(want[4]), want[4])
