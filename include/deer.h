@@ -551,7 +551,7 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *   bits, whatever the dead rows hold.
  *   A row_weight or grad_loss of a live row that is NaN or infinite makes that row's dh and all of dw NaN or infinite.
  *   h             bf16 [M][hid];  w bf16 [V][hid];  hid a multiple of 64, at most 65536;  M <= 2^18, V <= 2^30
- *   targets       i32 [M];  ids i32 [M][K], teacher f32 [M][K], K <= 128;  temperature > 0
+ *   targets       i32 [M];  ids i32 [M][K], teacher f32 [M][K], K <= 128;  temperature 2^-20 to 2^20
  *   row_weight    f32 [M] or NULL (1);  grad_loss f32 [M] or NULL (1)
  *   loss, lse     f32 [M]      out: the loss;  logsumexp(z / temperature)
  *   target_logit  f32 [M][K] (K = 1: [M])  out: z at the listed tokens, 0 behind a list's end
@@ -559,6 +559,8 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls), 16-byte
  *                 aligned, contents arbitrary, nothing kept in it between calls; one call at a time per workspace.
  * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).
+ * Logits of more than 2^26 temperature (z is fp32: their differences would be off by some 8) may make their row's lse and loss
+ * infinite or NaN.
  * A bounded wait that runs out makes the losses that it was for NaN, or all of the call's dh and dw. */
 size_t deer_lmhead_loss_workspace_bytes(int M, int hid, int V, int K, int grad);
 int deer_lmhead_loss(const void* h, const void* w, const int32_t* targets, const float* row_weight, int M, int hid, int V,

@@ -517,7 +517,19 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
         const int j = i * 32 + lane;
         if (j < a.K && (j >= l.n || l.id[i] >= a.V)) target_logit[(size_t)m * a.K + j] = 0.f;
     }
-    // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once
+    // the listed tokens' z: by plain sums in target_logit, as the tiles have it in s.z; each token once.  A low temperature makes
+    // their difference large: a plain one far above the reference becomes the reference.
+    float beyond = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_TOP / 32; ++i) {
+        if (i * 32 + lane >= l.n || l.id[i] >= a.V) continue;
+        l.z[i] = fmaf(l.z[i], plain.y, fmaf(l.z[i], plain.x, -all));
+        beyond = fmaxf(beyond, l.z[i]);
+    }
+    beyond = warp_max(beyond);
+    if (beyond < 64.f) beyond = 0.f;                       // (in range as it is)
+    all += beyond;
+    sum *= exp2f(-beyond);
     float more = 0.f;
     bool repeats = false;
 #pragma unroll
@@ -528,7 +540,7 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
         if (as_is)
             for (int o = 0; o < j; ++o) at = a.ids[(size_t)m * a.K + o] == l.id[i] ? -1 : at;
         else at = a.s.place[(size_t)slot * a.K + j];
-        l.z[i] = fmaf(l.z[i], plain.y, fmaf(l.z[i], plain.x, -all));
+        l.z[i] -= beyond;
         repeats |= at < 0;
         if (at < 0) continue;
         const float tile_z = a.s.z[(size_t)slot * a.K + at];
@@ -629,6 +641,8 @@ static int check_sizes(const char* call, int K, float tau, int M, int hid, int V
     DEER_CHECK_ARG(hid >= 64 && hid % 64 == 0 && hid <= 65536, DEER_ERR_UNSUPPORTED, "%s: hid must be a multiple of 64, at most 65536", call);
     DEER_CHECK_ARG(K >= 1 && K <= MAX_TOP, DEER_ERR_UNSUPPORTED, "%s: a list has 1 to %d entries", call, MAX_TOP);
     DEER_CHECK_ARG(tau > 0.f && tau < INFINITY, DEER_ERR_INVALID_ARG, "%s: temperature must be positive and finite", call);
+    // (beyond these fp32 logits have no bits left for a loss: |z| / tau below, z - z' above)
+    DEER_CHECK_ARG(tau >= 0x1p-20f && tau <= 0x1p20f, DEER_ERR_UNSUPPORTED, "%s: temperature must be 2^-20 to 2^20", call);
     return DEER_OK;
 }
 static int check_pointers(const char* call, const void* h, const void* w, const int32_t* ids, const float* teacher, bool needs_teacher,

@@ -1,5 +1,5 @@
-"""Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, tokens listed twice, lists
-that differ from row to row, products that gave up."""
+"""Calls of the LM head's losses at the edges of what they take: coefficients that are not finite, tokens listed twice, low
+temperatures, lists that differ from row to row, products that gave up."""
 import math
 
 import pytest
@@ -86,6 +86,25 @@ def test_the_divergence_of_lists_that_repeat_tokens(L, M, K):
     tol = a.double() * tau ** 2 * (2.0 ** -19 * logp.abs().amax(1) + 2.0 ** -20)
     assert ((loss.cpu().double() - want).abs() <= tol).all(), ((loss.cpu().double() - want).abs() / tol).max()
     assert (loss.cpu() >= -tol).all()                           # a divergence is not negative
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -20, 1e-4, 3e-3])
+@pytest.mark.parametrize("M,K", [(6, 4), (140, 12)])
+@pytest.mark.parametrize("hid,sure", [(64, 8.0), (8192, 50.0)])
+def test_low_temperatures(L, M, K, hid, sure, tau):
+    """p and t are all but sure, the loss about tau times a difference of logits; z's rounding / tau is beyond the exponential's
+    range at the lowest."""
+    h, w, ids, teacher, a, _ = draw(M, M, hid, 90, K=K, sure=sure)
+    loss, lse, _, dh, dw = run(L, h, w, ids, teacher=teacher, tau=tau, weight=a)
+    tau = torch.tensor(tau).double()                            # as the call has it
+    z = h.double() @ w.double().T
+    logp, t = torch.log_softmax(z / tau, 1), torch.softmax(teacher.double() / tau, 1)
+    want = a.double() * tau * tau * torch.where(t > 0, t * (torch.log(torch.where(t > 0, t, 1.0)) - torch.gather(logp, 1, ids.long())), 0.0).sum(1)
+    # z off by (hid / 16 + 8) steps of the accumulator, lse's reference by 2^-24 of it, and 2^-20 for what is left of the sums
+    dz = (hid / 16 + 8) * 2.0 ** -23 * (h.double().abs() @ w.double().abs().T).amax(1)
+    tol = a.double() * tau * (2 * dz + 2.0 ** -20 * z.abs().amax(1) + 2.0 ** -20 * tau)
+    assert ((loss.cpu().double() - want).abs() <= tol).all(), ((loss.cpu().double() - want).abs() / tol).max()
+    assert torch.isfinite(lse).all() and torch.isfinite(dh.float()).all() and torch.isfinite(dw.float()).all()
 
 
 def test_lists_that_differ_from_row_to_row(L):

@@ -25,3 +25,13 @@ def test_the_self_test_checks_its_operands(L):
     for bad in (dict(dh=z(4, 128)), dict(dw=torch.zeros(300, 128)), dict(h=z(5, 64))):
         with pytest.raises(L.DeerError):
             L.deer_selftest_lmhead_gave_up(**{**dict(h=z(5, 128), w=z(300, 128), K=4, dh=z(5, 128), dw=z(300, 128), workspace=None), **bad})
+
+
+def test_temperatures_that_z_has_no_bits_for(L):
+    need = L.deer_lmhead_loss_workspace_bytes(5, 128, 300, 4, True)
+    lib = L.lib()
+    loss = lambda tau, size: lib.deer_lmhead_distill(FAKE, FAKE, FAKE, FAKE, 4, tau, None, 5, 128, 300, FAKE, FAKE, FAKE, FAKE, size, None)  # noqa: E731
+    grad = lambda tau, size: lib.deer_lmhead_distill_grad(FAKE, FAKE, FAKE, FAKE, 4, tau, None, None, FAKE, FAKE, 5, 128, 300, 2 * FAKE, None,  # noqa: E731
+                                                          FAKE, size, None)
+    assert loss(9e-7, need) == grad(1e-39, need) == loss(1.1e6, need) == grad(1e30, need) == L.DEER_ERR_UNSUPPORTED
+    assert loss(2.0 ** -20, 16) == grad(2.0 ** -20, 16) == loss(2.0 ** 20, 16) == L.DEER_ERR_WORKSPACE
