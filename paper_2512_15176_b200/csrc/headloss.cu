@@ -654,6 +654,11 @@ static int check_pointers(const char* call, const void* h, const void* w, const 
     return DEER_OK;
 }
 
+static bool overlap(const void* p, size_t n, const void* q, size_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return p && q && a < b + m && b < a + n;
+}
+
 // The kernels by rows run between products that use an SM's whole shared memory: with the same split of its memory they
 // may start beside the end of one, and the SM need not drain to change the split.
 template <typename Kernel>
@@ -740,11 +745,18 @@ static int grad_call(const char* call, const void* h, const void* w, const int32
     rc = check_pointers(call, h, w, ids, teacher, needs_teacher, row_weight, lse, target_logit);
     if (rc != DEER_OK) return rc;
     DEER_CHECK_ARG(dh || dw, DEER_ERR_INVALID_ARG, "%s: neither dh nor dw is asked for", call);
-    DEER_CHECK_ARG(dh != h && dw != w, DEER_ERR_INVALID_ARG, "%s: a gradient in its operand's place", call);
     DEER_CHECK_ARG(deer_aligned4(grad_loss), DEER_ERR_INVALID_ARG, "%s: misaligned pointer", call);
     const Space s = lay_out(workspace, M, hid, V, K, true);
     DEER_CHECK_ARG(workspace && deer_aligned16(workspace) && workspace_bytes >= s.bytes, DEER_ERR_WORKSPACE,
                    "%s: needs a 16-byte aligned workspace of %zu bytes", call, s.bytes);
+    const size_t h_bytes = (size_t)M * hid * 2, w_bytes = (size_t)V * hid * 2, rows = (size_t)M * 4;
+    auto clear = [&](const void* out, size_t n) {          // of every input and of the workspace
+        return !(overlap(out, n, h, h_bytes) || overlap(out, n, w, w_bytes) || overlap(out, n, ids, rows * K) || overlap(out, n, teacher, rows * K) ||
+                 overlap(out, n, row_weight, rows) || overlap(out, n, grad_loss, rows) || overlap(out, n, lse, rows) ||
+                 overlap(out, n, target_logit, rows * K) || overlap(out, n, workspace, s.bytes));
+    };
+    DEER_CHECK_ARG(clear(dh, h_bytes) && clear(dw, w_bytes) && !overlap(dh, h_bytes, dw, w_bytes), DEER_ERR_INVALID_ARG,
+                   "%s: a gradient overlaps an operand, the other gradient or the workspace", call);
     RowArgs a = row_args(s, h, ids, teacher, K, tau, row_weight, M, hid, V);
     a.tile_n = s.grad_n;
     a.grad = grad_loss;

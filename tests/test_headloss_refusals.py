@@ -35,3 +35,33 @@ def test_temperatures_that_z_has_no_bits_for(L):
                                                           FAKE, size, None)
     assert loss(9e-7, need) == grad(1e-39, need) == loss(1.1e6, need) == grad(1e30, need) == L.DEER_ERR_UNSUPPORTED
     assert loss(2.0 ** -20, 16) == grad(2.0 ** -20, 16) == loss(2.0 ** 20, 16) == L.DEER_ERR_WORKSPACE
+
+
+def test_gradients_that_overlap_an_operand(L):
+    M, hid, V, K = 5, 128, 300, 4
+    need = L.deer_lmhead_loss_workspace_bytes(M, hid, V, K, True)
+    place, at = {}, 0x100000
+    for name, n in (("h", M * hid * 2), ("w", V * hid * 2), ("ids", M * K * 4), ("teacher", M * K * 4), ("weight", M * 4), ("grad", M * 4), ("lse", M * 4),
+                    ("tl", M * K * 4), ("dh", M * hid * 2), ("dw", V * hid * 2), ("ws", need)):
+        place[name] = (at, n)
+        at += (n + 15) // 16 * 16
+
+    def call(cross_entropy=False, size=need, **moved):
+        p = {k: moved.get(k, v[0]) for k, v in place.items()}
+        if cross_entropy:
+            return L.lib().deer_lmhead_loss_grad(p["h"], p["w"], p["ids"], p["weight"], p["grad"], p["lse"], p["tl"], M, hid, V, p["dh"], p["dw"], p["ws"],
+                                                 size, None)
+        return L.lib().deer_lmhead_distill_grad(p["h"], p["w"], p["ids"], p["teacher"], K, 1.0, p["weight"], p["grad"], p["lse"], p["tl"], M, hid, V,
+                                                p["dh"], p["dw"], p["ws"], size, None)
+
+    for out, n in (("dh", M * hid * 2), ("dw", V * hid * 2)):
+        for other, (start, size) in place.items():
+            if other == out:
+                continue
+            # over its first and its last bytes
+            for moved in (start + (size - 1) // 16 * 16, start - (n - 1) // 16 * 16, start):
+                gone = {k: None for k in ("dh", "dw") if k not in (out, other)}
+                assert call(**{out: moved}, **gone) == L.DEER_ERR_INVALID_ARG, (out, other)
+                assert b"overlaps" in L.lib().deer_last_error()
+            if other != "teacher":
+                assert call(True, **{out: start}, **gone) == L.DEER_ERR_INVALID_ARG, (out, other)
