@@ -556,8 +556,9 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *   loss, lse     f32 [M]      out: the loss;  logsumexp(z / temperature)
  *   target_logit  f32 [M][K] (K = 1: [M])  out: z at the listed tokens, 0 behind a list's end
  *   dh bf16 [M][hid], dw bf16 [V][hid]     out, overwritten; either may be NULL; neither may overlap an input or the other
- *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls), 16-byte
- *                 aligned, contents arbitrary, nothing kept in it between calls; one call at a time per workspace.
+ *   workspace     >= deer_lmhead_loss_workspace_bytes(M, hid, V, K, grad) bytes (grad = 1: the *_grad calls; beside what grows
+ *                 with M alone M V / 15 for the losses, M V / 256 for the gradients), 16-byte aligned, contents arbitrary,
+ *                 nothing kept in it between calls; one call at a time per workspace.
  * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).
  * Listed tokens' z are plain fp32 sums.  The others, and so lse where those weigh most, are the tensor cores': off by up to
  *   about 1e-8 hid / 16 of the row's largest logit, or 1e-7 hid / 16 where all of its products have one sign.

@@ -20,7 +20,8 @@ namespace headloss {
 
 constexpr int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
 constexpr int ROW_BLOCKS = 512;            // blocks of the kernel that moves the rows, at most: each of them counts all rows
-constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time (more pieces: more part-filled waves; fewer: more memory)
+constexpr size_t PIECE_BYTES = size_t(256) << 20;      // of G at a time, but 1024 columns at least (more pieces: more part-filled
+                                           // waves; fewer: more memory)
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f, LN2_LOW = (float)(0.6931471805599453 - (double)LN2);
 
