@@ -475,7 +475,8 @@ class HeadLoss:
 
     after which ``x.backward(dh)`` of the graph that made ``h = x.detach()`` carries on.  Rows without a target (-1) cost
     nothing, so a shorter batch is padded with them.  ``loss``, ``dh`` and ``dw`` are this object's buffers: the next step
-    overwrites them.  ``grad=False`` leaves room for the forward calls only."""
+    overwrites them.  ``backward`` reads the loss's inputs and ``w`` once more: they must not change before it has run.
+    ``grad=False`` leaves room for the forward calls only."""
 
     def __init__(self, w: torch.Tensor, rows: int, top: int = 1, grad: bool = True):
         self.buffers = b = L.HeadLossBuffers(w, rows, top, grad)
