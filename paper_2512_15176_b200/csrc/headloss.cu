@@ -527,10 +527,13 @@ __global__ void __launch_bounds__(ROW_THREADS) head_loss_kernel(const RowArgs a,
         l.z[i] = fmaf(l.z[i], plain.y, fmaf(l.z[i], plain.x, -all));
         beyond = fmaxf(beyond, l.z[i]);
     }
-    beyond = warp_max(beyond);
-    if (beyond < 64.f) beyond = 0.f;                       // (in range as it is)
-    all += beyond;
-    sum *= exp2f(-beyond);
+    if (__any_sync(0xffffffffu, beyond > 64.f)) {          // (out of range else)
+        beyond = warp_max(beyond);
+        all += beyond;
+        sum *= exp2f(-beyond);
+    } else {
+        beyond = 0.f;
+    }
     float more = 0.f;
     bool repeats = false;
 #pragma unroll
@@ -587,18 +590,19 @@ __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, i
     const bool in = c < a.hid;
     pdl_trigger();
     pdl_wait();
-    if (dw && a.s.hdr[HDR_GAVE_UP]) {
+    const int gave_up = a.s.hdr[HDR_GAVE_UP], live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
+    const float call_scale = __int_as_float(a.s.hdr[HDR_SCALE]);
+    if (dw && gave_up) {
         uint4* to = reinterpret_cast<uint4*>(dw);          // (rows are a multiple of 16 bytes)
         const size_t n = (size_t)a.V * a.hid / 8, threads = (size_t)gridDim.x * gridDim.y * ROW_THREADS;
         for (size_t i = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * ROW_THREADS + threadIdx.x; i < n; i += threads)
             to[i] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
     }
     if (!dh) return;
-    const int live = a.s.hdr[HDR_LIVE], ranges = a.s.hdr[HDR_RANGES];
     // few live rows: a range's tile holds the two terms' products, 128 rows each
     const int parts = live <= TWO_TERMS ? 2 * ranges : ranges;
     const size_t part_rows = live <= TWO_TERMS ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
-    const float scale = a.s.hdr[HDR_GAVE_UP] ? NAN : __int_as_float(a.s.hdr[HDR_SCALE]);
+    const float scale = gave_up ? NAN : call_scale;
     auto part_sum = [&](int slot, int first, int step) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         const float* src = a.s.slab + (size_t)slot * a.hid + c;
