@@ -578,8 +578,8 @@ int deer_lmhead_distill_grad(const void* h, const void* w, const int32_t* ids, c
                              const float* row_weight, const float* grad_loss, const float* lse, const float* target_logit,
                              int M, int hid, int V, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Self-test of what such a wait leaves: the end of a *_grad call once more, on the workspace of one that has just run with
- * these sizes, as if one of its products had given up.  dh or dw may be NULL. */
+/* Self-test of what such a wait leaves: the end of a *_grad call of these sizes, as if one of its products had given up.
+ * dh or dw may be NULL; what the workspace holds does not matter. */
 int deer_selftest_lmhead_gave_up(int M, int hid, int V, int K, void* dh, void* dw, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The K largest logits of each row, falling, the lowest index first among equals: what a teacher's row leaves for

@@ -599,8 +599,8 @@ __global__ void __launch_bounds__(ROW_THREADS) head_dh_kernel(const RowArgs a, i
             to[i] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
     }
     if (!dh) return;
-    // few live rows: a range's tile holds the two terms' products, 128 rows each
-    const int parts = live <= TWO_TERMS ? 2 * ranges : ranges;
+    // few live rows: a range's tile holds the two terms' products, 128 rows each; nothing is read behind a product that gave up
+    const int parts = gave_up ? 0 : live <= TWO_TERMS ? 2 * ranges : ranges;
     const size_t part_rows = live <= TWO_TERMS ? TILE / 2 : (size_t)((live + TILE - 1) / TILE) * TILE;
     const float scale = gave_up ? NAN : call_scale;
     auto part_sum = [&](int slot, int first, int step) {

@@ -161,6 +161,10 @@ def test_gradients_of_a_product_that_gave_up_are_nan(L, M, V):
         L.deer_selftest_lmhead_gave_up(h_, w_, 1, dh_, dw_, ws)
         for x in (dh_, dw_):
             assert x is None or torch.isnan(x).all()
+    ws.fill_(0x7f)                                              # (no call has left this: places and counts far out of range)
+    dh.fill_(0.0)
+    L.deer_selftest_lmhead_gave_up(h_, w_, 1, dh, dw, ws)
+    assert torch.isnan(dh).all() and torch.isnan(dw).all()
     assert (room_h[M * hid:] == 3).all() and (room_w[V * hid:] == 3).all()
     grad(dh, dw)
     assert torch.equal(dh.view_as(want[3]), want[3]) and torch.equal(dw.view_as(want[4]), want[4])
