@@ -561,7 +561,8 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *                 nothing kept in it between calls; one call at a time per workspace.
  * Unlike the forward calls these do not read w ahead of earlier work in the stream (an optimiser step may precede them).
  * Listed tokens' z are plain fp32 sums.  The others, and so lse where those weigh most, are the tensor cores': off by up to
- *   about 1e-8 hid / 16 of the row's largest logit, or 1e-7 hid / 16 where all of its products have one sign.
+ *   about 1e-8 hid / 16 of the row's largest logit up to hid 8192, by 1e-7 hid / 16 beyond it and where all of its products
+ *   have one sign.
  * Logits of more than 2^26 temperature (z is fp32: their differences would be off by some 8) may make their row's lse and loss
  * infinite or NaN.
  * A bounded wait that runs out makes the losses that it was for NaN, or all of the call's dh and dw. */

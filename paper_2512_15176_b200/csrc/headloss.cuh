@@ -24,7 +24,8 @@ constexpr int HDR_LIVE = 0, HDR_RANGES = 1, HDR_GAVE_UP = 2, HDR_SCALE = 3, HDR_
 // Up to this many live rows G is kept as two bf16 terms, rows [0, low) and [low, 2 low) with low = low_term(live).  In dh's
 // product the second takes the places of the second block's rows, idle then.  In dw's it lengthens the contraction: that
 // covers its first 128 places, all of both terms up to 64 live rows, and beyond them (where rows' errors begin to be
-// independent) what is left of its second step (live 128, hid 2688: 435 -> 380 us for both products).
+// independent) what is left of its second step.  With all of both terms up to 128 rows the gradients take 401 us instead of 391
+// (77 rows x 151936 x 2048) to 607 instead of 566 (128 rows, hid 2688); dw's error at 77 rows is 1.96e-3 so, its own rounding 1.66e-3.
 constexpr int TWO_TERMS = 128, DW_TERMS = 64;
 __host__ __device__ inline int low_term(int live) { return (live + 31) / 32 * 32; }
 // Steps of dw's contraction.

@@ -14,8 +14,8 @@
 // half empty.  h and G are stored row-major once; where the contraction runs along their rows (dw, and w in dh) the
 // operand is read MN-major: boxes of 64 contraction rows x 64 columns, two of them side by side.
 //
-// 1024 rows x 32768 x 2048, each launch alone and cold: STATS 95 us (tensor pipe 77 % busy), GRAD 98 (75 %), BACK 188 (81 %):
-// the tensor cores bound them.  96 rows x 65536 x 2048: 50, 54 and 114 us for 269, 284 and 534 MB of HBM traffic: memory does,
+// 1024 rows x 32768 x 2048, each launch alone and cold: STATS 95 us (tensor pipe 77 % busy), GRAD 96 (76 %), BACK 186 (81 %):
+// the tensor cores bound them.  96 rows x 65536 x 2048: 48, 54 and 112 us for 270, 282 and 534 MB of HBM traffic: memory does,
 // and in dw's part the way out of the SMs.
 //
 // G is rounded to bf16 for the products: as much as dh and dw are themselves, and with many rows the errors of different
@@ -23,7 +23,8 @@
 // keeps its difference.  coef is taken relative to a scale of the whole call, of which head_factor_kernel tries 32 between
 // two powers of two for the one at which rounding takes the least from the listed tokens, so that a few heavy rows do not
 // decide the gradient's error.  With few live rows (TWO_TERMS) a single rounding would show in a whole gradient, and there
-// G is kept as two bf16 terms, which costs next to no time.  lse, p and all sums are fp32.
+// G is kept as two bf16 terms: 1 % of the gradients' time at 20 rows x 151936 x 2048 (363 us and 359 with one), 5 % at 64 and
+// 128 (385 and 369, 409 and 389).  lse, p and all sums are fp32.
 //
 // The tensor cores' accumulation rounds towards zero at every step (tile_scale_of).  Where a target stands out the loss is the
 // difference of two large numbers, lse and the target's z: hence the listed tokens' z a second time, as plain fp32 sums (4 %

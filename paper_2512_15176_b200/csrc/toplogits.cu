@@ -9,7 +9,7 @@
 // that says nothing about the row) is selected exactly instead, by four passes over the digits of the key and one that
 // collects in order of index.  The key is the value's bits in an order of whole numbers: NaN below everything, -0 equal to 0.
 //
-// The reading bounds it where the rows are many and long: 2048 rows of 151936, the 64 best, 217 us or 0.88 of the measured
+// The reading bounds it where the rows are many and long: 2048 rows of 151936, the 64 best, 222 us or 0.86 of the measured
 // copy rate.  Few or short rows are a chain of steps, each a meeting of the block: one row 9 us, 32 rows 17.
 //
 // With few rows a cluster of up to eight blocks shares one, each a slice with a cut of its own, and the first block selects
@@ -138,7 +138,7 @@ __device__ int select(Shared<T>& s, const uint32_t* keys, const uint32_t* idxs, 
 }
 
 // What comes so leaves L2 first, and the runs of the sample are still there when the pass comes to them (512 rows of 151936:
-// 356 MB read from HBM without it, 315 with it, of 311; 2048 rows: 243 us and 217).
+// 356 MB read from HBM without it, 315 with it, of 311; a tenth of the time of 2048 rows).
 __device__ __forceinline__ float4 load_once(const float4* p) {
     float4 x;
     asm volatile("ld.global.cs.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
@@ -423,16 +423,19 @@ extern "C" int deer_top_logits(int M, int V, const float* logits, int K, int32_t
     DEER_CHECK_ARG(logits && ids && values, DEER_ERR_INVALID_ARG, "deer_top_logits: null pointer");
     DEER_CHECK_ARG(deer_aligned16(logits) && deer_aligned4(ids) && deer_aligned4(values), DEER_ERR_INVALID_ARG,
                    "deer_top_logits: logits must be 16-byte aligned, ids and values 4-byte");
-    // Eight or four blocks to a row where all of them run at once (three to an SM), on slices of LIST values at least: 100 rows
-    // of 151936 take 38 us by one block each and 28 by four; but two to a row gain nothing (200 rows: 40 by one, 43 by two), and
-    // in several rounds clusters lose (512 rows: 86 by one, 109 by two).
+    // Eight or four blocks to a row where there is room for all of them at once (three to an SM), on slices of LIST values at
+    // least.  Rows of 151936, the 64 best: 32 rows 17 us by eight blocks, 19 by two, 25 by one; 100 rows 25 by four, 33 by one;
+    // 200 rows 36 by one, 39 by two, and in several rounds clusters lose (512 rows: 59 by one, 103 by two).  Where clusters fill
+    // the room to the last place not all of them fit side by side, and the rule loses: 55 rows 27.5 by eight, 23 by two; 110 rows
+    // 37.5 by four, 28 by two, 33 by one.
     const long slots = 3L * deer_sm_count();
     int cluster = MAX_CLUSTER;
     while (cluster > 1 && ((long)M * cluster > slots || V / cluster < LIST<512>)) cluster /= 2;
     if (cluster == 2) cluster = 1;
     // Many shorter rows by half the threads: what a row costs beside its reading is a chain of steps, and more rows go side by
-    // side (1492 rows of 14725: 48.5 us by 512 threads, 36.4 by 256; 2048 of 32768: 86.5 and 83; 300 of 9999, all side by
-    // side anyway: 13.6 and 15.5; 2048 of 151936, where the reading counts: 243 and 300; all before load_once).
+    // side (2048 rows of 5000: 35 us by 512 threads, 24 by 256; 1492 of 14725: 41 and 33; 2048 of 32768: 75 and 69).  Longer rows
+    // go either way (2048 of 40000: 82 and 78; 1332 of 50257: 94 and 102) until the reading counts (512 of 151936: 60 and 72,
+    // 2048: 222 and 228).
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M <= slots) return launch<512, 3>(M, V, logits, K, cluster, ids, values, st);
     // A third more rows to an SM, at 32 registers a thread, where that saves a round of them (512 rows of 151936: 78 us in two
