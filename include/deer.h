@@ -550,6 +550,7 @@ int deer_block_attn_quant(deer_kv* kv, const int32_t* seq_ids,
  *   two bf16 terms hold G for dh, up to 64 for dw); all sums are fp32 and in a fixed order: the same inputs give the same
  *   bits, whatever the dead rows hold.
  *   A row_weight or grad_loss of a live row that is NaN or infinite makes that row's dh and all of dw NaN or infinite.
+ *   G is held relative to the call's largest coefficient: rows whose own is below 2^-90 of it lose small terms, then all.
  *   h             bf16 [M][hid];  w bf16 [V][hid];  hid a multiple of 64, at most 65536;  M <= 2^18, V <= 2^30
  *   targets       i32 [M];  ids i32 [M][K], teacher f32 [M][K], K <= 128;  temperature 2^-20 to 2^20
  *   row_weight    f32 [M] or NULL (1);  grad_loss f32 [M] or NULL (1)
